@@ -6,7 +6,9 @@
  * curve, the batched neighbour search that builds fixed-size neighbourhoods over
  * irregular 2-D token coordinates, local attention, forward and backward, over
  * each token's K neighbours, the neighbourhood merging that downsamples the token
- * set between stages, and the point decoder's virtual sampled tokens.
+ * set between stages, and the point decoder's virtual sampled tokens; and the dense
+ * operators of a block around them: matrix products with their epilogue, group and
+ * layer norm with an activation, dropout.
  *
  * Conventions for every entry point
  *   - All tensor pointers are DEVICE pointers owned by the caller; the library
@@ -53,6 +55,10 @@ typedef enum {
 } affmae_status;
 
 typedef enum { AFFMAE_F32 = 0, AFFMAE_BF16 = 1 } affmae_dtype;
+
+/* Activations of the dense operators: x, max(x, 0), x Phi(x) with Phi the normal
+ * distribution's (the exact form, not the tanh one), x / (1 + exp(-x)). */
+typedef enum { AFFMAE_ACT_NONE = 0, AFFMAE_ACT_RELU = 1, AFFMAE_ACT_GELU = 2, AFFMAE_ACT_SILU = 3 } affmae_act;
 
 /* Implemented limits (AFFMAE_ERR_UNSUPPORTED beyond them). */
 #define AFFMAE_MAX_K 64          /* neighbours per token                         */
@@ -428,6 +434,111 @@ int affmae_pla_bwd_relpos(const void* q, const void* k, const void* v, const flo
                           const void* dout, int B, int N, int H, int d, int K, int S, int M, float scale, int R,
                           float rate, int dtype, void* dq, void* dk, void* dv, float* drel_table, float* dk_blank,
                           float* dv_blank, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Dropout from a counter-based generator, with a mask that is never stored (the
+ * dropout behind a block's projections and MLP in fine-tuning).
+ *
+ * drop(v)_i = 0 where word(i) < floor(p 2^32), else v_i / (1 - p), for element i in
+ * the order of memory: a value that is dropped is replaced, whatever it was.
+ * word(i) is word i % 4 of the Philox 4x32 generator with ten rounds (Salmon, Moraes,
+ * Dror, Shaw, "Parallel random numbers: as easy as 1, 2, 3", 2011) with key = seed and
+ * counter = (i / 4, call number), both 64 bits, low words first.  Forward and backward
+ * work the mask out alike from
+ *   rng    in  device [2] int64: seed, call number; read when the kernels run, so that
+ *              a replayed graph takes the state of the time of its replay.  Calls whose
+ *              masks should differ take different call numbers.  May be NULL if p is 0.
+ *   p      0 <= p < 1, taken as the fp32 value
+ *
+ * affmae_dropout_fwd   out = residual + drop(x)       affmae_dropout_bwd   dx = drop(dout)
+ *   x, residual, out, dout, dx  [n] dtype; residual NULL = 0; out may be x or residual,
+ *              dx may be dout
+ *
+ * Any n and alignment (to the element); n a multiple of 8 (bf16) or 4 (fp32) in 16-byte
+ * aligned tensors runs the fast kernel, others a slower one, same results.
+ * Errors: AFFMAE_ERR_NULL (x, out; rng with p > 0), AFFMAE_ERR_DTYPE, AFFMAE_ERR_SHAPE
+ * (n < 1, p outside [0, 1), misaligned tensors).
+ */
+int affmae_dropout_fwd(const void* x, const void* residual, int64_t n, float p, const int64_t* rng, int dtype, void* out,
+                       void* stream);
+int affmae_dropout_bwd(const void* dout, int64_t n, float p, const int64_t* rng, int dtype, void* dx, void* stream);
+
+/*
+ * Dense layers of the tokens: the products in front of and behind the attention, the
+ * two of a block's MLP, merging's score layer and projection, the decoder's offsets.
+ *
+ * affmae_linear_fwd    z = x W^T + bias,  out = residual + drop(act(z)),  the sums,
+ *                      the activation and the mask in one kernel
+ *   x        in  [rows,Cin]    weight  in  [Cout,Cin]    bias  in  [Cout] or NULL
+ *   residual in  [rows,Cout] or NULL
+ *   out      out [rows,Cout]; may be residual
+ *   pre      out [rows,Cout] or NULL: z, which the backward of an activation needs
+ *   all in `dtype`, sums in fp32, one rounding (to nearest even) of each output; act,
+ *   p, rng: affmae_act and the dropout above, over the elements of out.
+ *
+ * affmae_linear_bwd    gradients of L = <dout, out>, with dz = drop(dout) act'(pre):
+ *   dx       out [rows,Cin]  = dz W          or NULL
+ *   dweight  out [Cout,Cin]  = dz^T x        or NULL (not both NULL)
+ *   dbias    out [Cout]      = sum of dz     or NULL (only with dweight)
+ *   all in `dtype` like the tensors that they belong to, sums in fp32 in a fixed order.
+ *   (The gradient of residual is dout itself.)  For bf16 dz is rounded to bf16: it is
+ *   an operand of both products.  relu's slope at 0 is 0.
+ *   weight is read for dx only, x for dweight only, pre with an activation only: each
+ *   may be NULL otherwise.
+ *   workspace  affmae_linear_bwd_workspace_bytes(...) bytes, may be 0
+ *
+ * Limits: rows <= 2^30, Cin, Cout <= 2^20, rows * Cin and rows * Cout <= 2^35
+ * (AFFMAE_ERR_UNSUPPORTED beyond).  Any sizes and any alignment (to the element) run;
+ * rows of whole 16-byte pieces in 16-byte aligned tensors are the fastest.
+ * Errors: AFFMAE_ERR_NULL, AFFMAE_ERR_DTYPE, AFFMAE_ERR_SHAPE (sizes < 1, unknown act,
+ * p outside [0, 1), misaligned tensors), AFFMAE_ERR_UNSUPPORTED, AFFMAE_ERR_WORKSPACE.
+ */
+int affmae_linear_fwd(const void* x, const void* weight, const void* bias, const void* residual, int rows, int Cin, int Cout,
+                      int act, float p, const int64_t* rng, int dtype, void* out, void* pre, void* stream);
+size_t affmae_linear_bwd_workspace_bytes(int rows, int Cin, int Cout, int act, float p, int dtype, int want_dx,
+                                         int want_dweight);
+int affmae_linear_bwd(const void* x, const void* weight, const void* pre, const void* dout, int rows, int Cin, int Cout,
+                      int act, float p, const int64_t* rng, int dtype, void* dx, void* dweight, void* dbias,
+                      void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Group norm with an activation over token tensors, channels last.  The C channels are
+ * cut into `groups` runs of equal length; per image and group, over its N * C / groups
+ * values,
+ *     mean, rstd = 1 / sqrt(variance + eps)   (variance: mean square about the mean)
+ *     z = gamma (x - mean) rstd + beta,  out = act(z)
+ * A layer norm of every token is the case of its tokens as B images of N = 1 with one
+ * group.
+ *
+ * affmae_norm_fwd
+ *   x in, out out [B,N,C] dtype     gamma, beta in [C] dtype, or both NULL (1 and 0)
+ *   mean, rstd    out [B,groups] fp32
+ *   workspace     affmae_norm_fwd_workspace_bytes(...) bytes, may be 0
+ *
+ * affmae_norm_bwd   gradients of L = <dout, out>, with dz = dout act'(z), z worked out
+ *                   again from x, mean and rstd:
+ *   dx            out [B,N,C] dtype
+ *   dgamma, dbeta out [C] fp32: sums of dz (x - mean) rstd and of dz; or both NULL
+ *   workspace     affmae_norm_bwd_workspace_bytes(...) bytes, may be 0
+ *
+ * Statistics and sums are fp32, added in a fixed order; a variance is the mean square
+ * about the mean (never a difference of squares), so that offsets large against the
+ * spread cost no digits.
+ * Limits: groups divides C <= 2^20, B*N below 2^31 - 8, B*groups <= 2^24
+ * (AFFMAE_ERR_UNSUPPORTED beyond).  Any sizes and any alignment (to the element) run;
+ * C / groups a multiple of 8 (bf16) or 4 (fp32) in 16-byte aligned tensors runs the
+ * fastest kernels.
+ * Errors: AFFMAE_ERR_NULL, AFFMAE_ERR_DTYPE, AFFMAE_ERR_SHAPE (sizes < 1, C % groups,
+ * unknown act, eps not positive and finite, misaligned tensors), AFFMAE_ERR_UNSUPPORTED,
+ * AFFMAE_ERR_WORKSPACE.
+ */
+size_t affmae_norm_fwd_workspace_bytes(int B, int N, int C, int groups, int dtype);
+int affmae_norm_fwd(const void* x, const void* gamma, const void* beta, int B, int N, int C, int groups, float eps, int act,
+                    int dtype, void* out, float* mean, float* rstd, void* workspace, size_t workspace_bytes, void* stream);
+size_t affmae_norm_bwd_workspace_bytes(int B, int N, int C, int groups, int dtype);
+int affmae_norm_bwd(const void* x, const void* gamma, const void* beta, const float* mean, const float* rstd,
+                    const void* dout, int B, int N, int C, int groups, int act, int dtype, void* dx, float* dgamma,
+                    float* dbeta, void* workspace, size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

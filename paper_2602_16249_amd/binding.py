@@ -20,6 +20,7 @@ _libs = {}         # path -> loaded library
 
 AFFMAE_F32 = 0
 AFFMAE_BF16 = 1
+_ACTS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
 
 _c_int = ctypes.c_int
 _c_void_p = ctypes.c_void_p
@@ -119,6 +120,26 @@ def _load(path: str):
     lib.affmae_pla_plan_bytes.argtypes = [_c_int] * 5
     lib.affmae_pla_plan.restype = _c_int
     lib.affmae_pla_plan.argtypes = [_c_void_p, _c_void_p] + [_c_int] * 5 + [_c_void_p, _c_size_t, _c_void_p]
+    lib.affmae_linear_fwd.restype = _c_int
+    lib.affmae_linear_fwd.argtypes = [_c_void_p] * 4 + [_c_int] * 4 + [_c_float, _c_void_p, _c_int] + [_c_void_p] * 3
+    lib.affmae_linear_bwd_workspace_bytes.restype = _c_size_t
+    lib.affmae_linear_bwd_workspace_bytes.argtypes = [_c_int] * 4 + [_c_float] + [_c_int] * 3
+    lib.affmae_linear_bwd.restype = _c_int
+    lib.affmae_linear_bwd.argtypes = ([_c_void_p] * 4 + [_c_int] * 4 + [_c_float, _c_void_p, _c_int] + [_c_void_p] * 4
+                                      + [_c_size_t, _c_void_p])
+    for name in ("affmae_norm_fwd_workspace_bytes", "affmae_norm_bwd_workspace_bytes"):
+        f = getattr(lib, name)
+        f.restype = _c_size_t
+        f.argtypes = [_c_int] * 5
+    lib.affmae_norm_fwd.restype = _c_int
+    lib.affmae_norm_fwd.argtypes = ([_c_void_p] * 3 + [_c_int] * 4 + [_c_float, _c_int, _c_int] + [_c_void_p] * 4
+                                    + [_c_size_t, _c_void_p])
+    lib.affmae_norm_bwd.restype = _c_int
+    lib.affmae_norm_bwd.argtypes = [_c_void_p] * 6 + [_c_int] * 6 + [_c_void_p] * 4 + [_c_size_t, _c_void_p]
+    lib.affmae_dropout_fwd.restype = _c_int
+    lib.affmae_dropout_fwd.argtypes = [_c_void_p, _c_void_p, ctypes.c_int64, _c_float, _c_void_p, _c_int, _c_void_p, _c_void_p]
+    lib.affmae_dropout_bwd.restype = _c_int
+    lib.affmae_dropout_bwd.argtypes = [_c_void_p, ctypes.c_int64, _c_float, _c_void_p, _c_int, _c_void_p, _c_void_p]
     _libs[path] = lib
     return lib
 
@@ -599,6 +620,240 @@ def affmae_pla_bwd_relpos(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, coo
     if rc != 0:
         raise AffmaeError("affmae_pla_bwd_relpos", rc)
     return g
+
+
+def _act_code(act: str) -> int:
+    code = _ACTS.get(act)
+    if code is None:
+        raise ValueError(f"act must be one of {', '.join(_ACTS)}, got {act!r}")
+    return code
+
+
+def _one_device(first: torch.Tensor, *others: Optional[torch.Tensor]) -> None:
+    """All tensors on the current device, whose current stream the call runs on."""
+    if not first.is_cuda:
+        raise ValueError("tensors must be device tensors")
+    index = first.get_device()
+    current = torch.cuda.current_device() if _raw_device is None else _raw_device()
+    if index != current:
+        raise ValueError(f"tensors are on device {index}, but device {current} is current")
+    for t in others:
+        if t is not None and t.get_device() != index:
+            raise ValueError(f"tensors must share one device, got {index} and {t.get_device()}")
+
+
+def _rng_ptr(rng: Optional[torch.Tensor], p: float):
+    """The generator's state, (seed, call number) in device memory; not needed where p is 0."""
+    if rng is None:
+        if p:
+            raise ValueError("dropout needs rng, [2] int64 on the device: seed, call number")
+        return None
+    return _dev(rng, "rng", torch.int64, (2,)).data_ptr()
+
+
+def _own_workspace(workspace: Optional[torch.Tensor], need: int, device) -> Tuple[Optional[torch.Tensor], int]:
+    if workspace is None:
+        workspace = _workspace(need, device)
+    return workspace, 0 if workspace is None else workspace.numel() * workspace.element_size()
+
+
+def affmae_linear_fwd(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] = None,
+                      residual: Optional[torch.Tensor] = None, act: str = "none", p: float = 0.0,
+                      rng: Optional[torch.Tensor] = None, want_pre: bool = False, out: Optional[torch.Tensor] = None,
+                      pre: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
+    """Dense layer: out = residual + dropout(act(x W^T + bias)) -> (out [..., Cout], pre [..., Cout]: x W^T + bias,
+    which the backward of an activation needs, or None unless asked for).
+
+    x [..., Cin], weight [Cout,Cin], bias [Cout], residual [..., Cout] in one dtype; act "none", "relu", "gelu" (exact) or
+    "silu"; p: probability of dropout, with rng [2] int64 on the device (seed, call number)."""
+    lib = load_library()
+    code = _dtype_code(x)
+    _one_device(x, weight, bias, residual, rng, out, pre)
+    _dev(x, "x")
+    _dev(weight, "weight", x.dtype)
+    if x.dim() < 1 or weight.dim() != 2 or x.shape[-1] != weight.shape[1]:
+        raise ValueError(f"x must be [..., Cin] and weight [Cout, Cin], got {tuple(x.shape)} and {tuple(weight.shape)}")
+    Cout, Cin = weight.shape
+    shape = x.shape[:-1] + (Cout,)
+    if bias is not None:
+        _dev(bias, "bias", x.dtype, (Cout,))
+    if residual is not None:
+        _dev(residual, "residual", x.dtype, shape)
+    if out is None:
+        out = torch.empty(shape, dtype=x.dtype, device=x.device)
+    else:
+        _dev(out, "out", x.dtype, shape)
+    if pre is not None:
+        _dev(pre, "pre", x.dtype, shape)
+    elif want_pre:
+        pre = torch.empty(shape, dtype=x.dtype, device=x.device)
+    rc = lib.affmae_linear_fwd(_ptr(x), _ptr(weight), _ptr(bias), _ptr(residual), x.numel() // max(Cin, 1), Cin, Cout,
+                               _act_code(act), float(p), _rng_ptr(rng, p), code, _ptr(out), _ptr(pre), _stream())
+    if rc != 0:
+        raise AffmaeError("affmae_linear_fwd", rc)
+    return out, pre
+
+
+def affmae_linear_bwd(x: Optional[torch.Tensor], weight: Optional[torch.Tensor], dout: torch.Tensor,
+                      pre: Optional[torch.Tensor] = None, act: str = "none", p: float = 0.0,
+                      rng: Optional[torch.Tensor] = None, want_dx: bool = True, want_dweight: bool = True,
+                      want_dbias: bool = True, grads: Optional[Dict[str, torch.Tensor]] = None,
+                      workspace: Optional[torch.Tensor] = None) -> Dict[str, torch.Tensor]:
+    """Gradients of affmae_linear_fwd -> dict(dx [..., Cin], dweight [Cout,Cin], dbias [Cout]), those asked for, in dout's dtype
+    (dbias comes with dweight only).  weight is needed for dx, x for dweight, pre with an activation; p and rng as in the forward."""
+    lib = load_library()
+    code = _dtype_code(dout)
+    g = dict(grads) if grads else {}
+    _one_device(dout, x, weight, pre, rng, workspace, *g.values())
+    _dev(dout, "dout")
+    if (x is None and want_dweight) or (weight is None and want_dx) or not (want_dx or want_dweight):
+        raise ValueError("dweight needs x, dx needs weight, and one of them must be asked for")
+    if dout.dim() < 1:
+        raise ValueError("dout must be [..., Cout]")
+    Cout = dout.shape[-1]
+    Cin = weight.shape[-1] if x is None else x.shape[-1]
+    if x is not None:
+        _dev(x, "x", dout.dtype, dout.shape[:-1] + (Cin,))
+    if weight is not None:
+        _dev(weight, "weight", dout.dtype, (Cout, Cin))
+    if pre is not None:
+        _dev(pre, "pre", dout.dtype, dout.shape)
+    elif act != "none":
+        raise ValueError("an activation's backward needs pre")
+    shapes = {}
+    if want_dx:
+        shapes["dx"] = dout.shape[:-1] + (Cin,)
+    if want_dweight:
+        shapes["dweight"] = (Cout, Cin)
+        if want_dbias:
+            shapes["dbias"] = (Cout,)
+    for name, shape in shapes.items():
+        if name not in g:
+            g[name] = torch.empty(shape, dtype=dout.dtype, device=dout.device)
+        else:
+            _dev(g[name], name, dout.dtype, shape)
+    rows = dout.numel() // max(Cout, 1)
+    a = _act_code(act)
+    need = lib.affmae_linear_bwd_workspace_bytes(rows, Cin, Cout, a, float(p), code, int(want_dx), int(want_dweight))
+    workspace, size = _own_workspace(workspace, need, dout.device)
+    rc = lib.affmae_linear_bwd(_ptr(x), _ptr(weight), _ptr(pre), _ptr(dout), rows, Cin, Cout, a, float(p), _rng_ptr(rng, p), code,
+                               _ptr(g["dx"]) if want_dx else None, _ptr(g["dweight"]) if want_dweight else None,
+                               _ptr(g["dbias"]) if "dbias" in shapes else None, _ptr(workspace), size, _stream())
+    if rc != 0:
+        raise AffmaeError("affmae_linear_bwd", rc)
+    return g
+
+
+def affmae_norm_fwd(x: torch.Tensor, gamma: Optional[torch.Tensor], beta: Optional[torch.Tensor], groups: int = 1,
+                    eps: float = 1e-5, act: str = "none", out: Optional[torch.Tensor] = None,
+                    mean: Optional[torch.Tensor] = None, rstd: Optional[torch.Tensor] = None,
+                    workspace: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+    """Group norm with an activation, channels last: x [B,N,C] -> (out [B,N,C] in x's dtype, mean [B,groups] fp32,
+    rstd [B,groups] fp32).  The layer norm of every token: x.view(-1, 1, C) with one group.  gamma, beta [C] or both None."""
+    lib = load_library()
+    code = _dtype_code(x)
+    _one_device(x, gamma, beta, out, mean, rstd, workspace)
+    _dev(x, "x")
+    if x.dim() != 3:
+        raise ValueError(f"x must be [B,N,C], got {tuple(x.shape)}")
+    B, N, C = x.shape
+    if (gamma is None) != (beta is None):
+        raise ValueError("gamma and beta are given together or not at all")
+    if gamma is not None:
+        _dev(gamma, "gamma", x.dtype, (C,))
+        _dev(beta, "beta", x.dtype, (C,))
+    if out is None:
+        out = torch.empty_like(x)
+    else:
+        _dev(out, "out", x.dtype, x.shape)
+    if mean is None:
+        mean = torch.empty((B, max(groups, 0)), dtype=torch.float32, device=x.device)
+    else:
+        _dev(mean, "mean", torch.float32, (B, groups))
+    if rstd is None:
+        rstd = torch.empty((B, max(groups, 0)), dtype=torch.float32, device=x.device)
+    else:
+        _dev(rstd, "rstd", torch.float32, (B, groups))
+    workspace, size = _own_workspace(workspace, lib.affmae_norm_fwd_workspace_bytes(B, N, C, groups, code), x.device)
+    rc = lib.affmae_norm_fwd(_ptr(x), _ptr(gamma), _ptr(beta), B, N, C, groups, float(eps), _act_code(act), code, _ptr(out), _ptr(mean),
+                             _ptr(rstd), _ptr(workspace), size, _stream())
+    if rc != 0:
+        raise AffmaeError("affmae_norm_fwd", rc)
+    return out, mean, rstd
+
+
+def affmae_norm_bwd(x: torch.Tensor, gamma: Optional[torch.Tensor], beta: Optional[torch.Tensor], mean: torch.Tensor,
+                    rstd: torch.Tensor, dout: torch.Tensor, groups: int = 1, act: str = "none",
+                    grads: Optional[Dict[str, torch.Tensor]] = None, workspace: Optional[torch.Tensor] = None
+                    ) -> Dict[str, torch.Tensor]:
+    """Gradients of affmae_norm_fwd -> dict(dx [B,N,C] in x's dtype[, dgamma, dbeta [C] fp32: with gamma])."""
+    lib = load_library()
+    code = _dtype_code(x)
+    g = dict(grads) if grads else {}
+    _one_device(x, gamma, beta, mean, rstd, dout, workspace, *g.values())
+    _dev(x, "x")
+    if x.dim() != 3:
+        raise ValueError(f"x must be [B,N,C], got {tuple(x.shape)}")
+    B, N, C = x.shape
+    if (gamma is None) != (beta is None):
+        raise ValueError("gamma and beta are given together or not at all")
+    shapes = {"dx": (x.shape, x.dtype)}
+    if gamma is not None:
+        _dev(gamma, "gamma", x.dtype, (C,))
+        _dev(beta, "beta", x.dtype, (C,))
+        shapes["dgamma"] = shapes["dbeta"] = ((C,), torch.float32)
+    _dev(mean, "mean", torch.float32, (B, groups))
+    _dev(rstd, "rstd", torch.float32, (B, groups))
+    _dev(dout, "dout", x.dtype, x.shape)
+    for name, (shape, dtype) in shapes.items():
+        if name not in g:
+            g[name] = torch.empty(shape, dtype=dtype, device=x.device)
+        else:
+            _dev(g[name], name, dtype, shape)
+    workspace, size = _own_workspace(workspace, lib.affmae_norm_bwd_workspace_bytes(B, N, C, groups, code), x.device)
+    rc = lib.affmae_norm_bwd(_ptr(x), _ptr(gamma), _ptr(beta), _ptr(mean), _ptr(rstd), _ptr(dout), B, N, C, groups, _act_code(act), code,
+                             _ptr(g["dx"]), _ptr(g["dgamma"]) if gamma is not None else None,
+                             _ptr(g["dbeta"]) if gamma is not None else None, _ptr(workspace), size, _stream())
+    if rc != 0:
+        raise AffmaeError("affmae_norm_bwd", rc)
+    return g
+
+
+def affmae_dropout_fwd(x: torch.Tensor, p: float, rng: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None,
+                       out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """out = residual + dropout(x), any shape; rng [2] int64 on the device (seed, call number), not needed where p is 0.
+    out may be x or residual."""
+    lib = load_library()
+    code = _dtype_code(x)
+    _one_device(x, rng, residual, out)
+    _dev(x, "x")
+    if residual is not None:
+        _dev(residual, "residual", x.dtype, x.shape)
+    if out is None:
+        out = torch.empty_like(x)
+    else:
+        _dev(out, "out", x.dtype, x.shape)
+    rc = lib.affmae_dropout_fwd(_ptr(x), _ptr(residual), x.numel(), float(p), _rng_ptr(rng, p), code, _ptr(out), _stream())
+    if rc != 0:
+        raise AffmaeError("affmae_dropout_fwd", rc)
+    return out
+
+
+def affmae_dropout_bwd(dout: torch.Tensor, p: float, rng: Optional[torch.Tensor] = None, dx: Optional[torch.Tensor] = None
+                       ) -> torch.Tensor:
+    """Gradient of affmae_dropout_fwd in x, with the same p and rng; dx may be dout.  (The gradient in residual is dout.)"""
+    lib = load_library()
+    code = _dtype_code(dout)
+    _one_device(dout, rng, dx)
+    _dev(dout, "dout")
+    if dx is None:
+        dx = torch.empty_like(dout)
+    else:
+        _dev(dx, "dx", dout.dtype, dout.shape)
+    rc = lib.affmae_dropout_bwd(_ptr(dout), dout.numel(), float(p), _rng_ptr(rng, p), code, _ptr(dx), _stream())
+    if rc != 0:
+        raise AffmaeError("affmae_dropout_bwd", rc)
+    return dx
 
 
 def timing_enable(on: bool) -> None:

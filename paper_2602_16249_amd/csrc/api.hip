@@ -79,7 +79,7 @@ const char* affmae_status_string(int status) {
   }
 }
 
-int affmae_version(void) { return 200; }
+int affmae_version(void) { return 300; }
 
 #ifndef AFFMAE_BUILD_ID
 #define AFFMAE_BUILD_ID "unstamped"

@@ -1,0 +1,166 @@
+// What the dense operators share (linear.hip, norm.hip, dropout.hip): storage of 16-byte pieces, activations, and the
+// counter-based generator behind dropout.
+#pragma once
+
+#include "device_util.h"
+
+#include <type_traits>
+
+namespace affmae {
+
+enum Act { kActNone = 0, kActRelu = 1, kActGelu = 2, kActSilu = 3 };
+
+// Phi(z) and phi(z) of the normal distribution.  erf by Abramowitz and Stegun, Handbook of Mathematical Functions, 7.1.26:
+// 1 - (a1 t + ... + a5 t^5) exp(-x^2), t = 1 / (1 + p x), off by at most 1.5e-7 - half of that in Phi, about one rounding of
+// fp32 - with the exponential that the derivative needs anyway; no branch, a third of the instructions of a library erf.
+__device__ __forceinline__ void normal_cdf(float z, float& cdf, float& density) {
+  const float x = fabsf(z) * 0.70710678118654752f;
+  const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.3275911f, x, 1.f));
+  const float e = __expf(-0.5f * z * z);
+  float s = __builtin_fmaf(1.061405429f, t, -1.453152027f);
+  s = __builtin_fmaf(s, t, 1.421413741f);
+  s = __builtin_fmaf(s, t, -0.284496736f);
+  s = __builtin_fmaf(s, t, 0.254829592f);
+  const float tail = 0.5f * (s * t) * e;
+  cdf = z < 0.f ? tail : 1.f - tail;
+  density = 0.39894228040143268f * e;
+}
+__device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.f + __expf(-z)); }
+
+__device__ __forceinline__ float act_value(float z, int act) {
+  if (act == kActRelu) return z < 0.f ? 0.f : z;  // (a NaN stays one)
+  if (act == kActGelu) {
+    float cdf, density;
+    normal_cdf(z, cdf, density);
+    return z * cdf;
+  }
+  if (act == kActSilu) return z * sigmoid(z);
+  return z;
+}
+__device__ __forceinline__ float act_slope(float z, int act) {
+  if (act == kActRelu) return z > 0.f ? 1.f : 0.f;
+  if (act == kActGelu) {
+    float cdf, density;
+    normal_cdf(z, cdf, density);
+    return __builtin_fmaf(z, density, cdf);
+  }
+  if (act == kActSilu) {
+    const float s = sigmoid(z);
+    return s * __builtin_fmaf(z, 1.f - s, 1.f);
+  }
+  return 1.f;
+}
+
+// Dropout of probability p.  Element i stays where word i % 4 of the generator's block i / 4 is at least `least` = floor(p 2^32);
+// kept values are multiplied by `factor` = 1 / (1 - p), dropped ones are replaced by 0, whatever they were.
+struct Dropout {
+  const int64_t* rng;  // device memory: seed, call number; null: nothing is dropped
+  uint32_t least;
+  float factor;
+};
+inline Dropout make_dropout(float p, const int64_t* rng) {
+  Dropout d = {nullptr, 0u, 1.f};
+  if (p > 0.f) {
+    d.rng = rng;
+    d.least = (uint32_t)((double)p * 4294967296.0);
+    d.factor = (float)(1.0 / (1.0 - (double)p));
+  }
+  return d;
+}
+
+struct RngKey {
+  uint32_t k0, k1, c2, c3;
+};
+__device__ __forceinline__ RngKey rng_key(const int64_t* rng) {
+  const uint64_t seed = (uint64_t)rng[0], call = (uint64_t)rng[1];
+  return {(uint32_t)seed, (uint32_t)(seed >> 32), (uint32_t)call, (uint32_t)(call >> 32)};
+}
+// Philox 4x32 with ten rounds (Salmon, Moraes, Dror, Shaw, "Parallel random numbers: as easy as 1, 2, 3", 2011): key = the seed,
+// counter = (block, call number).  A pure function of the element's place: forward and backward work it out again instead of
+// storing a mask, and any kernel may take any part of a tensor.
+__device__ __forceinline__ uint4 rng_words(const RngKey& key, uint64_t block) {
+  uint32_t c0 = (uint32_t)block, c1 = (uint32_t)(block >> 32), c2 = key.c2, c3 = key.c3, k0 = key.k0, k1 = key.k1;
+#pragma unroll
+  for (int r = 0; r < 10; ++r) {
+    const uint64_t a = (uint64_t)c0 * 0xD2511F53u, b = (uint64_t)c2 * 0xCD9E8D57u;
+    c0 = (uint32_t)(b >> 32) ^ c1 ^ k0;
+    c1 = (uint32_t)b;
+    c2 = (uint32_t)(a >> 32) ^ c3 ^ k1;
+    c3 = (uint32_t)a;
+    k0 += 0x9E3779B9u;
+    k1 += 0xBB67AE85u;
+  }
+  return make_uint4(c0, c1, c2, c3);
+}
+__device__ __forceinline__ uint32_t rng_word(const RngKey& key, uint64_t element) {
+  const uint4 w = rng_words(key, element >> 2);
+  const int i = (int)(element & 3);
+  return i == 0 ? w.x : i == 1 ? w.y : i == 2 ? w.z : w.w;
+}
+// v[0..E) are elements first .. first + E - 1; first and E are multiples of 4, or E is 1.
+template <int E>
+__device__ __forceinline__ void drop(float (&v)[E], const Dropout& d, const RngKey& key, uint64_t first) {
+  if constexpr (E % 4 == 0) {
+#pragma unroll
+    for (int q = 0; q < E / 4; ++q) {
+      const uint4 w = rng_words(key, (first >> 2) + q);
+      v[4 * q + 0] = w.x >= d.least ? v[4 * q + 0] * d.factor : 0.f;
+      v[4 * q + 1] = w.y >= d.least ? v[4 * q + 1] * d.factor : 0.f;
+      v[4 * q + 2] = w.z >= d.least ? v[4 * q + 2] * d.factor : 0.f;
+      v[4 * q + 3] = w.w >= d.least ? v[4 * q + 3] * d.factor : 0.f;
+    }
+  } else {
+    static_assert(E == 1);
+    v[0] = rng_word(key, first) >= d.least ? v[0] * d.factor : 0.f;
+  }
+}
+
+// A piece of E consecutive values: 16 bytes (E = 4 for fp32, 8 for bf16; 16-byte aligned), or one value.
+template <typename T>
+constexpr int kPiece = 16 / (int)sizeof(T);
+
+template <int E>
+__device__ __forceinline__ void load_piece(const float* p, float (&v)[E]) {
+  if constexpr (E == 1)
+    v[0] = *p;
+  else
+    load_row<E>(p, v);
+}
+template <int E>
+__device__ __forceinline__ void load_piece(const bf16_t* p, float (&v)[E]) {
+  if constexpr (E == 1)
+    v[0] = bf16_to_f32(*p);
+  else
+    load_row<E>(p, v);
+}
+__device__ __forceinline__ uint32_t pack2_bf16(float lo, float hi) {
+  typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+  typedef __attribute__((ext_vector_type(2))) float f32x2;
+  const f32x2 f = {lo, hi};
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f, bf16x2));
+}
+template <int E>
+__device__ __forceinline__ void store_piece(float* p, const float (&v)[E]) {
+  if constexpr (E == 1) {
+    *p = v[0];
+  } else {
+#pragma unroll
+    for (int t = 0; t < E / 4; ++t)
+      reinterpret_cast<float4*>(p)[t] = make_float4(v[4 * t], v[4 * t + 1], v[4 * t + 2], v[4 * t + 3]);
+  }
+}
+template <int E>
+__device__ __forceinline__ void store_piece(bf16_t* p, const float (&v)[E]) {
+  if constexpr (E == 1) {
+    *p = f32_to_bf16(v[0]);
+  } else {
+#pragma unroll
+    for (int t = 0; t < E / 8; ++t)
+      reinterpret_cast<uint4*>(p)[t] = make_uint4(pack2_bf16(v[8 * t], v[8 * t + 1]), pack2_bf16(v[8 * t + 2], v[8 * t + 3]),
+                                                  pack2_bf16(v[8 * t + 4], v[8 * t + 5]), pack2_bf16(v[8 * t + 6], v[8 * t + 7]));
+  }
+}
+
+inline bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }  // (a null pointer is)
+
+}  // namespace affmae

@@ -191,4 +191,57 @@ bool pla_bwd_wide_supported(const PlaArgs& a, const void* plan);
 hipError_t launch_pla_fwd_wide(const PlaArgs& a, const void* plan, hipStream_t stream);
 hipError_t launch_pla_bwd_wide(const PlaArgs& a, const void* plan, hipStream_t stream);
 
+// Dense layer of the tokens with its epilogue, and its gradients (linear.hip).
+struct LinearArgs {
+  const void* x;       // [rows,Cin]
+  const void* weight;  // [Cout,Cin]
+  int rows, Cin, Cout, act, dtype;
+  float p;
+  const int64_t* rng;  // device [2], not read where p is 0
+  // forward
+  const void* bias;      // [Cout] or nullptr
+  const void* residual;  // [rows,Cout] or nullptr
+  void* out;             // [rows,Cout]
+  void* pre_out;         // [rows,Cout] or nullptr
+  // backward
+  const void* pre;   // [rows,Cout], not read without an activation
+  const void* dout;  // [rows,Cout]
+  void* dx;          // [rows,Cin] or nullptr
+  void* dweight;     // [Cout,Cin] or nullptr
+  void* dbias;       // [Cout] or nullptr
+  void* workspace;
+};
+hipError_t launch_linear_fwd(const LinearArgs& a, hipStream_t stream);
+size_t linear_bwd_workspace_bytes(int rows, int Cin, int Cout, int act, bool drops, int dtype, bool want_dx, bool want_dweight);
+hipError_t launch_linear_bwd(const LinearArgs& a, hipStream_t stream);
+
+// Group norm with an activation, channels last (norm.hip).
+struct NormArgs {
+  const void* x;             // [B,N,C]
+  const void *gamma, *beta;  // [C], or both nullptr
+  int B, N, C, G, act, dtype;
+  float eps;
+  float *mean, *rstd;  // [B,G], written by the forward pass
+  void* out;           // [B,N,C]
+  const void* dout;    // [B,N,C]
+  void* dx;            // [B,N,C]
+  float *dgamma, *dbeta;  // [C], or both nullptr
+  void* workspace;
+};
+size_t norm_fwd_workspace_bytes(int B, int N, int C, int G, int dtype);
+hipError_t launch_norm_fwd(const NormArgs& a, hipStream_t stream);
+size_t norm_bwd_workspace_bytes(int B, int N, int C, int G, int dtype);
+hipError_t launch_norm_bwd(const NormArgs& a, hipStream_t stream);
+
+// Dropout, forward and backward (dropout.hip): out = residual + dropout(x).
+struct DropoutArgs {
+  const void *x, *residual;  // residual: nullptr for none
+  long long n;
+  float p;
+  const int64_t* rng;
+  int dtype;
+  void* out;
+};
+hipError_t launch_dropout(const DropoutArgs& a, hipStream_t stream);
+
 }  // namespace affmae
