@@ -1,7 +1,14 @@
-// Dense layer of the tokens: out = residual + dropout(act(x W^T + bias)), and its gradients.
+// Dense layer of the tokens: out = residual + dropout(act(x W^T + bias)), and its gradients dx = dz W, dW = dz^T x,
+// dbias = sum of dz, with dz = dropout(dout) act'(pre).
+//
+// All three are products c[m][n] = sum_k a(m, k) b(n, k) of one tiled kernel; they differ in which operands lie along k in memory:
+//   forward  a = x  [rows,Cin]  (along k)     b = W [Cout,Cin] (along k)
+//   dx       a = dz [rows,Cout] (along k)     b = W [Cout,Cin] (across: a row of W is one k)
+//   dW       a = dz [rows,Cout] (across)      b = x [rows,Cin] (across), k = rows: split over workgroups, parts added by a second launch
 #include "launch.h"
 #include "timing.h"
 
+#include "cluster_common.h"
 #include "dense_common.h"
 
 #include <algorithm>
@@ -9,13 +16,188 @@
 namespace affmae {
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kTile = 64, kDepth = 16;
+typedef __attribute__((ext_vector_type(4))) int i32x4;
 
-struct Product {  // c[m][n] = sum_k a(m, k) b(n, k), element (m, k) of a at a + m a_m + k a_k, likewise b
-  const void *a, *b;
-  size_t a_m, a_k, b_n, b_k;
-  long long M, N, K;
+constexpr uint32_t kNowhere = 0x80000000u;  // beyond every buffer: such loads bring 0
+
+// A buffer of at most 2^31 - 1 bytes from `base` on: what lies beyond reads as 0.
+__device__ __forceinline__ i32x4 buffer_of(const char* base, long long bytes) {
+  const uint64_t p = (uint64_t)base;
+  const int n = (int)(bytes < 0 ? 0 : bytes < 0x7fffffffll ? bytes : 0x7fffffffll);
+  return i32x4{(int)(uint32_t)p, (int)((uint32_t)(p >> 32) & 0xffffu), n, 0x00020000};
+}
+__device__ __forceinline__ i32x4 uniform(i32x4 v) {
+  return i32x4{__builtin_amdgcn_readfirstlane(v.x), __builtin_amdgcn_readfirstlane(v.y), __builtin_amdgcn_readfirstlane(v.z), __builtin_amdgcn_readfirstlane(v.w)};
+}
+
+// From a buffer straight into LDS (lane l's bytes land at dst + W l).  By hand: for the compiler every LDS read might read what
+// such a load still writes, and it would wait for what is on its way before it reads what is there.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"  // (m0 is reserved: written only for the next instruction, never held)
+template <int W>
+__device__ __forceinline__ void lds_load(uint32_t dst, i32x4 rsrc, uint32_t off) {
+  if constexpr (W == 16)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(dst), "v"(off), "s"(rsrc) : "m0", "memory");
+  else
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(dst), "v"(off), "s"(rsrc) : "m0", "memory");
+}
+#pragma clang diagnostic pop
+__device__ __forceinline__ uint32_t lds_at(const void* p) { return (uint32_t)(size_t)(__attribute__((address_space(3))) const char*)p; }
+
+// Slices are 128 bytes of k deep: 64 values of bf16, 32 of fp32, two steps of the matrix instruction's 32 / four times 4.
+constexpr int kSliceBytes = 128;
+template <typename T>
+constexpr int kSlice = kSliceBytes / (int)sizeof(T);
+
+// An operand's slice of BX rows in LDS, 16-byte pieces.  ALONG: BX lines of 128 bytes, a line per row; else a line of BX values per k.
+// A piece's place in its line is XORed with bits of the line's number, so that the lanes of a read, which take the same piece of
+// several lines, meet different banks.
+template <typename T, bool ALONG, int BX>
+struct SliceLayout {
+  static constexpr int kLine = ALONG ? kSliceBytes : BX * (int)sizeof(T);
+  static constexpr int kLines = ALONG ? BX : kSlice<T>;
+  static constexpr int kBytes = BX * kSliceBytes;
+  static __device__ __forceinline__ int mix(int line) {
+    if constexpr (ALONG)
+      return line & 7;  // a read takes one piece of 8 lines at a time
+    else if constexpr (sizeof(T) == 4)
+      return ((line >> 2) & 3) << 2;  // 64 bytes of each of the lines 4 g + j, g = 0..3
+    else if constexpr (kLine % 256 == 0)
+      return ((line & 3) | ((line >> 3) & 1) << 2) << 1;  // 32 bytes of each of four lines, of lines 8 apart beside them
+    else
+      return (((line >> 1) & 1) | ((line >> 3) & 1) << 1) << 1;  // (lines of 128 bytes: odd ones are in the other half of the banks)
+  }
+};
+
+// Brings slices of an operand into LDS.  W: bytes a lane brings at a time.  Rows beyond the operand's and k beyond the last read as 0.
+template <typename T, bool ALONG, int BX, int W, int THREADS>
+struct Stager {
+  using L = SliceLayout<T, ALONG, BX>;
+  static constexpr int kTurns = L::kBytes / (W < 4 ? 16 : W) / THREADS;
+  static_assert(kTurns * THREADS * (W < 4 ? 16 : W) == L::kBytes);
+  const char* first;  // of the tile, k = 0
+  long long bytes;    // from there to the end of the operand
+  uint32_t ld;
+  int x_left;  // rows of the operand from the tile's first on
+  uint32_t off[kTurns];
+
+  // which bytes of its line the thread's turn brings, and the line
+  static __device__ __forceinline__ void place(int turn, int& line, int& in_line) {
+    constexpr int U = W < 4 ? 16 : W;
+    const int at = (turn * THREADS + (int)threadIdx.x) * U;
+    line = at / L::kLine;
+    const int rest = at - line * L::kLine;
+    in_line = (((rest >> 4) ^ L::mix(line)) << 4) | (rest & 15);
+  }
+  __device__ __forceinline__ Stager(const void* p, uint32_t ld_, long long total, int x0, int X) : ld(ld_) {
+    const long long skip = ALONG ? (long long)x0 * ld : (long long)x0 * sizeof(T);
+    first = (const char*)p + skip;
+    bytes = total - skip;
+    x_left = X - x0;
+#pragma unroll
+    for (int t = 0; t < kTurns; ++t) {
+      int line, in_line;
+      place(t, line, in_line);
+      const bool there = ALONG ? line < x_left : in_line < x_left * (int)sizeof(T);
+      off[t] = there ? (uint32_t)line * ld + in_line : kNowhere;
+    }
+  }
+  __device__ __forceinline__ long long skip(int k0) const { return ALONG ? (long long)k0 * sizeof(T) : (long long)k0 * ld; }
+  // slice of k0 .. k0 + kSlice - 1, `left` of them there, into `dst`
+  __device__ __forceinline__ void load(char* dst, int k0, int left) const {
+    const i32x4 rsrc = uniform(buffer_of(first + skip(k0), bytes - skip(k0)));
+    const uint32_t base = lds_at(dst) + (uint32_t)(__builtin_amdgcn_readfirstlane(threadIdx.x / kWave) * kWave * W);
+    if (left >= kSlice<T>) {
+#pragma unroll
+      for (int t = 0; t < kTurns; ++t) lds_load<W>(base + t * THREADS * W, rsrc, off[t]);
+    } else {
+#pragma unroll
+      for (int t = 0; t < kTurns; ++t) {
+        int line, in_line;
+        place(t, line, in_line);
+        const bool there = ALONG ? in_line < left * (int)sizeof(T) : line < left;
+        lds_load<W>(base + t * THREADS * W, rsrc, there ? off[t] : kNowhere);
+      }
+    }
+  }
+  // the same value by value, for operands whose rows do not start on 4 bytes
+  __device__ __forceinline__ void load_values(char* dst, int k0, int left) const {
+    const char* from = first + skip(k0);
+#pragma unroll 1
+    for (int t = 0; t < kTurns; ++t) {
+      int line, in_line;
+      place(t, line, in_line);
+      T v[kPiece<T>];
+#pragma unroll
+      for (int e = 0; e < kPiece<T>; ++e) {
+        const int at = in_line + e * (int)sizeof(T);
+        const bool there = ALONG ? line < x_left && at < left * (int)sizeof(T) : line < left && at < x_left * (int)sizeof(T);
+        v[e] = there ? *reinterpret_cast<const T*>(from + (size_t)line * ld + at) : T(0);
+      }
+      *reinterpret_cast<uint4*>(dst + (t * THREADS + threadIdx.x) * 16) = *reinterpret_cast<const uint4*>(v);
+    }
+  }
+};
+
+// What lane (r = lane % 16, g = lane / 16) hands to the matrix instruction for row r of 16: bf16 k = 8 g .. 8 g + 7 of a step of 32;
+// fp32 k = 4 g .. 4 g + 3 of a step of 16, value j to the j-th of four instructions (which k meets which instruction is free as long
+// as both operands agree).
+template <typename T>
+struct Frag;
+template <>
+struct Frag<bf16_t> {
+  union {
+    uint4 u4;
+    uint2 u2[2];
+    bf16x8 v;
+  };
+};
+template <>
+struct Frag<float> {
+  union {
+    uint4 u4;
+    float f[4];
+  };
+};
+__device__ __forceinline__ f32x4 multiply(const Frag<bf16_t>& a, const Frag<bf16_t>& b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v, b.v, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 multiply(const Frag<float>& a, const Frag<float>& b, f32x4 c) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.f[j], b.f[j], c, 0, 0, 0);
+  return c;
+}
+template <typename T, bool ALONG, int BX>
+__device__ __forceinline__ Frag<T> read_frag(const char* slice, int row0, int step, int r, int g) {
+  using L = SliceLayout<T, ALONG, BX>;
+  Frag<T> f;
+  if constexpr (ALONG) {
+    f.u4 = *reinterpret_cast<const uint4*>(slice + (row0 + r) * kSliceBytes + (((4 * step + g) ^ (r & 7)) << 4));
+  } else if constexpr (sizeof(T) == 4) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int k = 16 * step + 4 * g + j;
+      f.f[j] = *reinterpret_cast<const float*>(slice + k * L::kLine + ((((row0 + r) >> 2) ^ (g << 2)) << 4) + (r & 3) * 4);
+    }
+  } else {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int k = 32 * step + 8 * g + 4 * h + (r >> 2);
+      f.u2[h] = lds_read_tr(slice + k * L::kLine + ((((row0 >> 3) + ((r & 3) >> 1)) ^ L::mix(k)) << 4) + (r & 1) * 8);
+    }
+  }
+  return f;
+}
+
+struct Operand {
+  const void* p;
+  uint32_t ld;      // bytes between its lines
+  long long bytes;  // of the whole operand
+};
+struct Product {
+  Operand a, b;
+  int M, N, K;
+  int tiles_n, tiles, splits, split_slices;  // tiles of c; workgroups that share a tile's k, slices of each
 };
 struct Epilogue {
   const void *bias, *residual;
@@ -23,116 +205,349 @@ struct Epilogue {
   int act;
   Dropout d;
 };
+struct GradEpilogue {
+  void* out;      // [M,N], times alpha
+  void* bias;     // [M]: alpha times the sums of a over k, or null
+  float* part;    // with splits: [splits][M][part_ld] fp32 instead of out, [splits][M] behind it instead of bias
+  int part_ld;
+  float alpha;
+};
 
-// 64 x 64 values of c by 256 threads, 4 x 4 each, 16 deep slices of both operands in LDS
-template <typename T>
-__global__ __launch_bounds__(kThreads) void linear_kernel(Product p, Epilogue e) {
-  __shared__ float as[kDepth][kTile + 1], bs[kDepth][kTile + 1];
-  const long long tiles_n = (p.N + kTile - 1) / kTile;
-  const long long m0 = (long long)blockIdx.x / tiles_n * kTile, n0 = (long long)blockIdx.x % tiles_n * kTile;
-  const T *a = (const T*)p.a, *b = (const T*)p.b;
-  const int tm = threadIdx.x / 16 * 4, tn = threadIdx.x % 16 * 4;
-  float c[4][4] = {};
-  for (long long k0 = 0; k0 < p.K; k0 += kDepth) {
-    for (int i = threadIdx.x; i < kTile * kDepth; i += kThreads) {
-      const int r = i / kDepth, k = i % kDepth;
-      as[k][r] = m0 + r < p.M && k0 + k < p.K ? Elem<T>::load(a + (m0 + r) * p.a_m + (k0 + k) * p.a_k) : 0.f;
-      bs[k][r] = n0 + r < p.N && k0 + k < p.K ? Elem<T>::load(b + (n0 + r) * p.b_n + (k0 + k) * p.b_k) : 0.f;
-    }
-    __syncthreads();
-    for (int k = 0; k < kDepth; ++k)
-      for (int i = 0; i < 4; ++i)
-        for (int j = 0; j < 4; ++j) c[i][j] += as[k][tm + i] * bs[k][tn + j];
-    __syncthreads();
+// E values of row m from column n on, `at` = m N + n
+template <typename T, int E>
+__device__ __forceinline__ void finish(const Epilogue& e, const RngKey& key, float (&v)[E], int n, size_t at) {
+  if (e.bias) {
+    float b[E];
+    load_piece<E>((const T*)e.bias + n, b);
+#pragma unroll
+    for (int i = 0; i < E; ++i) v[i] += b[i];
   }
-  RngKey key = {};
-  if (e.d.rng) key = rng_key(e.d.rng);
-  for (int i = 0; i < 4; ++i)
-    for (int j = 0; j < 4; ++j) {
-      const long long m = m0 + tm + i, n = n0 + tn + j;
-      if (m >= p.M || n >= p.N) continue;
-      const size_t at = (size_t)m * p.N + n;
-      float v[1] = {c[i][j]};
-      if (e.bias) v[0] += Elem<T>::load((const T*)e.bias + n);
-      if (e.pre) Elem<T>::store((T*)e.pre + at, v[0]);
-      v[0] = act_value(v[0], e.act);
-      if (e.d.rng) drop<1>(v, e.d, key, at);
-      if (e.residual) v[0] += Elem<T>::load((const T*)e.residual + at);
-      Elem<T>::store((T*)e.out + at, v[0]);
-    }
+  if (e.pre) store_piece<E>((T*)e.pre + at, v);
+  if (e.act != kActNone) {
+#pragma unroll
+    for (int i = 0; i < E; ++i) v[i] = act_value(v[i], e.act);
+  }
+  if (e.d.rng) drop<E>(v, e.d, key, at);
+  if (e.residual) {
+    float r[E];
+    load_piece<E>((const T*)e.residual + at, r);
+#pragma unroll
+    for (int i = 0; i < E; ++i) v[i] += r[i];
+  }
+  store_piece<E>((T*)e.out + at, v);
 }
 
-// dz = dropout(dout) act'(pre)
+// 16 rows x TNW columns of a wave's products, from the strip in LDS, as pieces of E values in the order of memory
+template <typename T, int E, int TNW, typename F>
+__device__ __forceinline__ void strip_pieces(const float* strip, int lane, int m0, int n0, int M, int N, F f) {
+  constexpr int kRow = TNW / E, kAll = 16 * kRow;
+#pragma unroll
+  for (int i = 0; i < (kAll + kWave - 1) / kWave; ++i) {
+    const int q = i * kWave + lane, row = q / kRow, col = q % kRow * E;
+    if (kAll % kWave != 0 && q >= kAll) break;
+    if (m0 + row >= M || n0 + col >= N) continue;
+    float v[E];
+    load_piece<E>(strip + row * (TNW + 4) + col, v);
+    f(v, m0 + row, n0 + col);
+  }
+}
+
+template <int BM, int BN>
+constexpr int kStageBytes = (BM + BN) * kSliceBytes;
+
+// BM x BN values of c by WM x WN waves.  Two slices of both operands in LDS: one is multiplied while the next one is on its way.
+// The products are c^T tiles (b's rows along the instruction's rows), so that a lane holds four consecutive columns of c.
+template <typename T, bool AA, bool BA, int W, int BM, int BN, int WM, int WN, typename Ep>
+__global__ __launch_bounds__(WM* WN* kWave) void linear_kernel(Product p, Ep e) {
+  extern __shared__ __align__(16) char lds[];
+  constexpr int kThreads = WM * WN * kWave, TM = BM / WM, TN = BN / WN, IM = TM / 16, IN = TN / 16;
+  constexpr bool kGrad = std::is_same_v<Ep, GradEpilogue>;
+  const int work = xcd_contiguous_block(blockIdx.x, gridDim.x);
+  if (work >= p.tiles * p.splits) return;
+  const int split = work / p.tiles, tile = work - split * p.tiles;
+  const int mt = tile / p.tiles_n, nt = tile - mt * p.tiles_n;
+  const int m0 = mt * BM, n0 = nt * BN;
+  const int k_begin = split * p.split_slices * kSlice<T>;
+  const int k_end = min(p.K, k_begin + p.split_slices * kSlice<T>);
+  const int slices = (k_end - k_begin + kSlice<T> - 1) / kSlice<T>;
+  const int lane = threadIdx.x & (kWave - 1), r = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), wm = wave / WN, wn = wave % WN;
+  const Stager<T, AA, BM, W, kThreads> sa(p.a.p, p.a.ld, p.a.bytes, m0, p.M);
+  const Stager<T, BA, BN, W, kThreads> sb(p.b.p, p.b.ld, p.b.bytes, n0, p.N);
+  const auto stage = [&](int s) {
+    char* dst = lds + (s & 1) * kStageBytes<BM, BN>;
+    const int k0 = k_begin + s * kSlice<T>;
+    if constexpr (W >= 4) {
+      sa.load(dst, k0, k_end - k0);
+      sb.load(dst + BM * kSliceBytes, k0, k_end - k0);
+    } else {
+      sa.load_values(dst, k0, k_end - k0);
+      sb.load_values(dst + BM * kSliceBytes, k0, k_end - k0);
+    }
+  };
+  f32x4 c[IM][IN] = {}, sums[IM] = {};
+  bool want_sums = false;
+  if constexpr (kGrad) want_sums = e.bias && nt == 0 && wn == 0;
+  stage(0);
+  for (int s = 0; s < slices; ++s) {
+    // slice s has arrived, and every wave has read what the next one will be written over
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    if (s + 1 < slices) stage(s + 1);
+    const char* as = lds + (s & 1) * kStageBytes<BM, BN>;
+    const char* bs = as + BM * kSliceBytes;
+#pragma unroll
+    for (int step = 0; step < 2; ++step) {
+      Frag<T> a[IM], b[IN];
+#pragma unroll
+      for (int i = 0; i < IM; ++i) a[i] = read_frag<T, AA, BM>(as, wm * TM + 16 * i, step, r, g);
+#pragma unroll
+      for (int j = 0; j < IN; ++j) b[j] = read_frag<T, BA, BN>(bs, wn * TN + 16 * j, step, r, g);
+#pragma unroll
+      for (int i = 0; i < IM; ++i)
+#pragma unroll
+        for (int j = 0; j < IN; ++j) c[i][j] = multiply(b[j], a[i], c[i][j]);
+      if constexpr (kGrad) {
+        if (want_sums) {  // a's sums over k: its products with ones
+          Frag<T> ones;
+          ones.u4 = sizeof(T) == 2 ? make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u)
+                                   : make_uint4(0x3f800000u, 0x3f800000u, 0x3f800000u, 0x3f800000u);
+#pragma unroll
+          for (int i = 0; i < IM; ++i) sums[i] = multiply(ones, a[i], sums[i]);
+        }
+      }
+    }
+  }
+  __syncthreads();
+  float* strip = reinterpret_cast<float*>(lds) + wave * 16 * (TN + 4);
+  static_assert(WM * WN * 16 * (TN + 4) * 4 <= kStageBytes<BM, BN>);
+  RngKey key = {};
+  bool pieces = false;
+  if constexpr (kGrad) {
+    pieces = p.N % kPiece<T> == 0 && ((uintptr_t)e.out & 15) == 0;
+  } else {
+    if (e.d.rng) key = rng_key(e.d.rng);
+    pieces = p.N % kPiece<T> == 0 && (((uintptr_t)e.out | (uintptr_t)e.pre | (uintptr_t)e.bias | (uintptr_t)e.residual) & 15) == 0;
+  }
+#pragma unroll
+  for (int i = 0; i < IM; ++i) {
+    const int m = m0 + wm * TM + 16 * i, n = n0 + wn * TN;
+    if (m >= p.M) break;
+#pragma unroll
+    for (int j = 0; j < IN; ++j) *reinterpret_cast<f32x4*>(strip + r * (TN + 4) + 16 * j + 4 * g) = c[i][j];
+    wave_lds_sync();
+    if constexpr (kGrad) {
+      if (e.part) {
+        float* part = e.part + (size_t)split * p.M * e.part_ld;
+        strip_pieces<float, 4, TN>(strip, lane, m, n, p.M, e.part_ld, [&](float(&v)[4], int row, int col) { store_piece<4>(part + (size_t)row * e.part_ld + col, v); });
+      } else {
+        const auto put = [&](auto& v, int row, int col) {
+          for (float& x : v) x *= e.alpha;
+          store_piece<sizeof(v) / sizeof(float)>((T*)e.out + (size_t)row * p.N + col, v);
+        };
+        if (pieces)
+          strip_pieces<T, kPiece<T>, TN>(strip, lane, m, n, p.M, p.N, put);
+        else
+          strip_pieces<T, 1, TN>(strip, lane, m, n, p.M, p.N, put);
+      }
+      if (want_sums && g == 0 && m + r < p.M) {
+        if (e.part)
+          e.part[(size_t)p.splits * p.M * e.part_ld + (size_t)split * p.M + m + r] = sums[i][0];
+        else
+          Elem<T>::store((T*)e.bias + m + r, sums[i][0] * e.alpha);
+      }
+    } else {
+      const auto put = [&](auto& v, int row, int col) { finish<T, sizeof(v) / sizeof(float)>(e, key, v, col, (size_t)row * p.N + col); };
+      if (pieces)
+        strip_pieces<T, kPiece<T>, TN>(strip, lane, m, n, p.M, p.N, put);
+      else
+        strip_pieces<T, 1, TN>(strip, lane, m, n, p.M, p.N, put);
+    }
+    wave_lds_sync();
+  }
+}
+
+// out[i] = alpha * (part[0][i] + part[1][i] + ...), rows of N in part_ld; the last workgroups: bias likewise
 template <typename T>
-__global__ __launch_bounds__(kThreads) void linear_dz_kernel(const T* __restrict__ dout, const T* __restrict__ pre, long long n, int act, Dropout d, T* __restrict__ dz) {
+__global__ __launch_bounds__(256) void linear_join_kernel(GradEpilogue e, int M, int N, int splits, int bias_blocks) {
+  const int blocks = gridDim.x - bias_blocks;
+  if ((int)blockIdx.x >= blocks) {
+    const int m = (blockIdx.x - blocks) * 256 + threadIdx.x;
+    if (m >= M) return;
+    const float* part = e.part + (size_t)splits * M * e.part_ld;
+    float s = 0.f;
+    for (int k = 0; k < splits; ++k) s += part[(size_t)k * M + m];
+    Elem<T>::store((T*)e.bias + m, s * e.alpha);
+    return;
+  }
+  const size_t all = (size_t)M * e.part_ld;
+  for (size_t i = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4; i < all; i += (size_t)blocks * 1024) {
+    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int k = 0; k < splits; ++k) {
+      const float4 v = *reinterpret_cast<const float4*>(e.part + k * all + i);
+      s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+    }
+    const size_t m = i / (unsigned)e.part_ld;
+    const int n = (int)(i - m * e.part_ld);
+    T* out = (T*)e.out + m * N + n;
+    const float v[4] = {s.x * e.alpha, s.y * e.alpha, s.z * e.alpha, s.w * e.alpha};
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (n + j < N) Elem<T>::store(out + j, v[j]);
+  }
+}
+
+// dz / factor = (kept? dout : 0) act'(pre), rows of C in lines of `ld` values whose rest is 0.  E > 1: C and ld are multiples of E.
+template <typename T, int E>
+__global__ __launch_bounds__(256) void linear_dz_kernel(const T* __restrict__ dout, const T* __restrict__ pre, int rows, int C, int ld, uint32_t ld_magic, int act,
+                                                        Dropout d, T* __restrict__ dz) {
   RngKey key = {};
   if (d.rng) key = rng_key(d.rng);
-  for (long long i = (long long)blockIdx.x * kThreads + threadIdx.x; i < n; i += (long long)gridDim.x * kThreads) {
-    float v[1] = {Elem<T>::load(dout + i)};
-    if (d.rng) drop<1>(v, d, key, (uint64_t)i);
-    if (pre) v[0] *= act_slope(Elem<T>::load(pre + i), act);
-    Elem<T>::store(dz + i, v[0]);
+  d.factor = 1.f;
+  const int line = ld / E;
+  // 256 rows at a time: places in them are 28-bit numbers
+  for (int row0 = blockIdx.y * 256; row0 < rows; row0 += gridDim.y * 256) {
+    const int n = min(256, rows - row0) * line;
+    for (int i = blockIdx.x * 256 + threadIdx.x; i < n; i += gridDim.x * 256) {
+      const int row = exact_div(i, line, ld_magic), col = (i - row * line) * E;
+      const size_t at = (size_t)(row0 + row) * C + col;
+      float v[E];
+      if (E > 1 || col < C) {
+        load_piece<E>(dout + at, v);
+        if (d.rng) drop<E>(v, d, key, at);
+        if (pre) {
+          float z[E];
+          load_piece<E>(pre + at, z);
+#pragma unroll
+          for (int j = 0; j < E; ++j) v[j] *= act_slope(z[j], act);
+        }
+      } else {
+        v[0] = 0.f;
+      }
+      store_piece<E>(dz + (size_t)(row0 + row) * ld + col, v);
+    }
   }
 }
 
-template <typename T>
-__global__ __launch_bounds__(kThreads) void linear_dbias_kernel(const T* __restrict__ dz, long long rows, int C, T* __restrict__ dbias) {
-  __shared__ float acc[4];
-  float s = 0.f;
-  for (long long i = threadIdx.x; i < rows; i += kThreads) s += Elem<T>::load(dz + (size_t)i * C + blockIdx.x);
-  s = wave_sum(s);
-  if ((threadIdx.x & (kWave - 1)) == 0) acc[threadIdx.x / kWave] = s;
-  __syncthreads();
-  if (threadIdx.x == 0) Elem<T>::store(dbias + blockIdx.x, (acc[0] + acc[1]) + (acc[2] + acc[3]));
+int cdiv(long long a, long long b) { return (int)((a + b - 1) / b); }
+
+// what a lane may bring at a time, by where an operand's lines start
+int line_bytes(const Operand& o) {
+  const uintptr_t all = reinterpret_cast<uintptr_t>(o.p) | o.ld;
+  return all % 16 == 0 ? 16 : all % 4 == 0 ? 4 : 2;
 }
 
+template <typename T, bool AA, bool BA, int W, int BM, int BN, int WM, int WN, typename Ep>
+hipError_t run_tiles(Product p, const Ep& e, hipStream_t stream) {
+  p.tiles_n = cdiv(p.N, BN);
+  p.tiles = cdiv(p.M, BM) * p.tiles_n;
+  const int slices = cdiv(p.K, kSlice<T>);
+  p.split_slices = cdiv(slices, p.splits);
+  const int stages = W >= 4 && p.split_slices > 1 ? 2 : W >= 4 ? 1 : 2;
+  const auto kernel = linear_kernel<T, AA, BA, W, BM, BN, WM, WN, Ep>;
+  const size_t lds = (size_t)stages * kStageBytes<BM, BN>;
+  if (lds > 64 * 1024) {
+    const hipError_t rc = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    if (rc != hipSuccess) return rc;
+  }
+  const unsigned grid = (unsigned)cdiv((long long)p.tiles * p.splits, 8) * 8;
+  [[maybe_unused]] constexpr const char* name = std::is_same_v<Ep, Epilogue> ? "linear_fwd_kernel" : AA ? "linear_dx_kernel" : "linear_dweight_kernel";
+  AFFMAE_LAUNCH(name, stream, kernel, dim3(grid), dim3(WM * WN * kWave), lds, stream, p, e);
+  return hipGetLastError();
+}
+
+template <typename T, bool AA, bool BA, typename Ep>
+hipError_t run_product(const Product& p, const Ep& e, hipStream_t stream) {
+  const int w = std::min(line_bytes(p.a), line_bytes(p.b));
+  if (w == 16) return run_tiles<T, AA, BA, 16, 128, 128, 2, 2>(p, e, stream);
+  if (w == 4) return run_tiles<T, AA, BA, 4, 128, 128, 2, 2>(p, e, stream);
+  if constexpr (sizeof(T) == 2) return run_tiles<T, AA, BA, 2, 128, 128, 2, 2>(p, e, stream);
+  return hipErrorInvalidValue;
+}
+
+// Workgroups that share a tile's k, where the tiles alone would leave the chip half empty: at least four slices each.
+int splits_of(long long M, long long N, long long K, int slice) {
+  const long long tiles = (long long)cdiv(M, 128) * cdiv(N, 128);
+  const long long slices = cdiv(K, slice);
+  const long long want = 512 / tiles;
+  const int most = (int)std::max(1ll, std::min(want, slices / 4));
+  return cdiv(slices, cdiv(slices, most));  // (no split without slices)
+}
+int part_ld(int N) { return cdiv(N, 4) * 4; }
+size_t part_bytes(int splits, int M, int N, bool bias) {
+  return splits > 1 ? ((size_t)splits * M * part_ld(N) + (bias ? (size_t)splits * M : 0)) * sizeof(float) : 0;
+}
+size_t up256(size_t n) { return (n + 255) / 256 * 256; }
+
 template <typename T>
-hipError_t product(const Product& p, const Epilogue& e, hipStream_t stream) {
-  const long long tiles = (p.M + kTile - 1) / kTile * ((p.N + kTile - 1) / kTile);
-  AFFMAE_LAUNCH("linear_kernel", stream, linear_kernel<T>, dim3((unsigned)tiles), dim3(kThreads), 0, stream, p, e);
+hipError_t gradient(bool dx, Operand a, Operand b, int M, int N, int K, void* out, void* bias, float alpha, float* part, hipStream_t stream) {
+  Product p = {};
+  p.a = a; p.b = b; p.M = M; p.N = N; p.K = K;
+  p.splits = splits_of(M, N, K, kSlice<T>);
+  const GradEpilogue e = {out, bias, p.splits > 1 ? part : nullptr, part_ld(N), alpha};
+  hipError_t rc = dx ? run_product<T, true, false>(p, e, stream) : run_product<T, false, false>(p, e, stream);
+  if (rc != hipSuccess || p.splits == 1) return rc;
+  const int bias_blocks = bias ? cdiv(M, 256) : 0;
+  const int blocks = (int)std::min<long long>(cdiv((long long)M * part_ld(N), 1024), 4096);
+  AFFMAE_LAUNCH("linear_join_kernel", stream, linear_join_kernel<T>, dim3(blocks + bias_blocks), dim3(256), 0, stream, e, M, N, p.splits, bias_blocks);
   return hipGetLastError();
 }
 
 template <typename T>
 hipError_t fwd(const LinearArgs& a, hipStream_t stream) {
-  const Product p = {a.x, a.weight, (size_t)a.Cin, 1, (size_t)a.Cin, 1, a.rows, a.Cout, a.Cin};
+  const uint32_t ld = (uint32_t)a.Cin * sizeof(T);
+  Product p = {};
+  p.a = {a.x, ld, (long long)a.rows * ld};
+  p.b = {a.weight, ld, (long long)a.Cout * ld};
+  p.M = a.rows; p.N = a.Cout; p.K = a.Cin; p.splits = 1;
   const Epilogue e = {a.bias, a.residual, a.out, a.pre_out, a.act, make_dropout(a.p, a.rng)};
-  return product<T>(p, e, stream);
+  return run_product<T, true, true>(p, e, stream);
 }
+
+int dz_ld(int Cout, int el) { return cdiv(Cout * el, 16) * 16 / el; }
 
 template <typename T>
 hipError_t bwd(const LinearArgs& a, hipStream_t stream) {
-  const void* dz = a.dout;
   const Dropout d = make_dropout(a.p, a.rng);
+  const uint32_t out_ld = (uint32_t)a.Cout * sizeof(T), in_ld = (uint32_t)a.Cin * sizeof(T);
+  Operand dz = {a.dout, out_ld, (long long)a.rows * out_ld};
+  char* ws = static_cast<char*>(a.workspace);
   if (a.act != kActNone || d.rng) {
-    const long long n = (long long)a.rows * a.Cout;
-    AFFMAE_LAUNCH("linear_dz_kernel", stream, linear_dz_kernel<T>, dim3((unsigned)std::min((n + kThreads - 1) / kThreads, 1ll << 23)), dim3(kThreads), 0, stream,
-                  (const T*)a.dout, a.act != kActNone ? (const T*)a.pre : nullptr, n, a.act, d, (T*)a.workspace);
-    dz = a.workspace;
+    const int ld = dz_ld(a.Cout, sizeof(T));
+    const void* pre = a.act != kActNone ? a.pre : nullptr;
+    constexpr int E = kPiece<T>;
+    const bool whole = a.Cout % E == 0 && aligned16(a.dout) && aligned16(pre);
+    const int line = whole ? ld / E : ld;
+    const dim3 grid(cdiv(256ll * line, 256 * 4), std::min(cdiv(a.rows, 256), 32768));
+    const auto run = [&](auto kernel) {
+      AFFMAE_LAUNCH("linear_dz_kernel", stream, kernel, grid, dim3(256), 0, stream, (const T*)a.dout, (const T*)pre, a.rows, a.Cout, ld, div_magic(line), a.act, d, (T*)ws);
+    };
+    if (whole)
+      run(linear_dz_kernel<T, E>);
+    else
+      run(linear_dz_kernel<T, 1>);
+    const hipError_t rc = hipGetLastError();
+    if (rc != hipSuccess) return rc;
+    dz = {ws, (uint32_t)(ld * sizeof(T)), (long long)a.rows * ld * (long long)sizeof(T)};
+    ws += up256((size_t)dz.bytes);
   }
-  const Epilogue none = {nullptr, nullptr, nullptr, nullptr, kActNone, make_dropout(0.f, nullptr)};
-  hipError_t rc = hipSuccess;
+  float* part = reinterpret_cast<float*>(ws);
   if (a.dx) {
-    Epilogue e = none;
-    e.out = a.dx;
-    rc = product<T>({dz, a.weight, (size_t)a.Cout, 1, 1, (size_t)a.Cin, a.rows, a.Cin, a.Cout}, e, stream);
+    const hipError_t rc = gradient<T>(true, dz, {a.weight, in_ld, (long long)a.Cout * in_ld}, a.rows, a.Cin, a.Cout, a.dx, nullptr, d.factor, part, stream);
+    if (rc != hipSuccess) return rc;
   }
-  if (rc == hipSuccess && a.dweight) {
-    Epilogue e = none;
-    e.out = a.dweight;
-    rc = product<T>({dz, a.x, 1, (size_t)a.Cout, 1, (size_t)a.Cin, a.Cout, a.Cin, a.rows}, e, stream);
-  }
-  if (rc == hipSuccess && a.dbias) {
-    AFFMAE_LAUNCH("linear_dbias_kernel", stream, linear_dbias_kernel<T>, dim3(a.Cout), dim3(kThreads), 0, stream, (const T*)dz, (long long)a.rows, a.Cout, (T*)a.dbias);
-    rc = hipGetLastError();
-  }
-  return rc;
+  if (a.dweight)
+    return gradient<T>(false, dz, {a.x, in_ld, (long long)a.rows * in_ld}, a.Cout, a.Cin, a.rows, a.dweight, a.dbias, d.factor, part, stream);
+  return hipSuccess;
 }
 
 }  // namespace
 
-size_t linear_bwd_workspace_bytes(int rows, int, int Cout, int act, bool drops, int dtype, bool, bool) {
-  return act != kActNone || drops ? (size_t)rows * Cout * (dtype == 1 ? 2 : 4) : 0;
+size_t linear_bwd_workspace_bytes(int rows, int Cin, int Cout, int act, bool drops, int dtype, bool want_dx, bool want_dweight) {
+  const int el = dtype == 1 ? 2 : 4, slice = kSliceBytes / el;
+  const size_t dz = act != kActNone || drops ? up256((size_t)rows * dz_ld(Cout, el) * el) : 0;
+  const size_t dx = want_dx ? part_bytes(splits_of(rows, Cin, Cout, slice), rows, Cin, false) : 0;
+  const size_t dw = want_dweight ? part_bytes(splits_of(Cout, Cin, rows, slice), Cout, Cin, true) : 0;
+  return dz + std::max(dx, dw);  // (the parts of one are joined before the other's are written)
 }
 hipError_t launch_linear_fwd(const LinearArgs& a, hipStream_t stream) { return a.dtype == 1 ? fwd<bf16_t>(a, stream) : fwd<float>(a, stream); }
 hipError_t launch_linear_bwd(const LinearArgs& a, hipStream_t stream) { return a.dtype == 1 ? bwd<bf16_t>(a, stream) : bwd<float>(a, stream); }
