@@ -1,130 +1,835 @@
-// Group norm with an activation over token tensors [B,N,C], channels last: an image's group g of Cg = C / G channels has
-// mean and variance over its N x Cg values, z = gamma (x - mean) rstd + beta, out = act(z).  B tokens of N = 1 and one group are
-// the layer norm of every token.
+// Group norm with an activation over token tensors [B,N,C], channels last: an image's group of Cg = C / G channels has mean and
+// variance over its N x Cg values, z = gamma (x - mean) rstd + beta, out = act(z).  B tokens of N = 1 and one group are the layer
+// norm of every token.
+//
+// All of it is bound by memory: a few operations a value.  Two families:
+//   rows     N = 1, one group, rows that fit a wave's registers: 4 to 64 lanes hold a row, statistics and values from one reading.
+//   groups   everything else: a workgroup takes a run of an image's tokens times a block of at most 256 pieces of channels (whole
+//            groups, or a share of one), every thread one column of pieces; a first launch leaves per group and workgroup a mean and a
+//            sum of squares about it, a second one puts these together and makes the values.  An image that one workgroup holds needs one.
+// A variance is always the mean square about a mean: of a workgroup's own values in registers, and between workgroups by
+// M2 = sum of (M2_i + n_i (mean_i - mean)^2).  No difference of squares, so offsets and outliers cost no digits.
 #include "launch.h"
 #include "timing.h"
 
+#include "cluster_common.h"
 #include "dense_common.h"
+
+#include <algorithm>
 
 namespace affmae {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kWaves = kThreads / kWave;
 
-__device__ __forceinline__ float block_sum(float v, float* acc) {
-  v = wave_sum(v);
-  __syncthreads();
-  if ((threadIdx.x & (kWave - 1)) == 0) acc[threadIdx.x / kWave] = v;
-  __syncthreads();
-  return (acc[0] + acc[1]) + (acc[2] + acc[3]);
+int cdiv(long long a, long long b) { return (int)((a + b - 1) / b); }
+size_t up256(size_t n) { return (n + 255) / 256 * 256; }
+
+// z = xhat gamma + beta, out = act(z)
+template <int E>
+__device__ __forceinline__ void normalise(float (&v)[E], float mean, float rstd, bool affine, const float (&gm)[E], const float (&bt)[E], int act) {
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    v[e] = (v[e] - mean) * rstd;
+    if (affine) v[e] = __builtin_fmaf(v[e], gm[e], bt[e]);
+  }
+  if (act != kActNone) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) v[e] = act_value(v[e], act);
+  }
+}
+// x becomes xhat, g (dout) becomes dz = dout act'(z)
+template <int E>
+__device__ __forceinline__ void slopes(float (&x)[E], float (&g)[E], float mean, float rstd, bool affine, const float (&gm)[E], const float (&bt)[E], int act) {
+#pragma unroll
+  for (int e = 0; e < E; ++e) x[e] = (x[e] - mean) * rstd;
+  if (act != kActNone) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) g[e] *= act_slope(affine ? __builtin_fmaf(x[e], gm[e], bt[e]) : x[e], act);
+  }
 }
 
-// workgroup per (image, group): mean, then the variance about it, then the values
-template <typename T>
-__global__ __launch_bounds__(kThreads) void norm_fwd_kernel(const T* __restrict__ x, const T* __restrict__ gamma, const T* __restrict__ beta, int N, int C,
-                                                            int G, float eps, int act, T* __restrict__ out, float* __restrict__ mean, float* __restrict__ rstd) {
-  __shared__ float acc[4];
-  const int b = blockIdx.x / G, g = blockIdx.x % G, Cg = C / G;
-  const size_t base = (size_t)b * N * C + (size_t)g * Cg;
-  const long long n = (long long)N * Cg;
+// ------------------------------------------------------------------------------------------------------------------ rows
+
+// LANES lanes a row, PIECES pieces of E values a lane, TURNS rows of a lane group on their way at a time
+template <typename T, int E, int LANES, int PIECES, int TURNS>
+__global__ __launch_bounds__(kThreads) void norm_rows_fwd_kernel(const T* __restrict__ x, const T* __restrict__ gamma, const T* __restrict__ beta, int rows,
+                                                                 int C, float eps, int act, T* __restrict__ out, float* __restrict__ mean,
+                                                                 float* __restrict__ rstd) {
+  constexpr int kRows = kThreads / LANES;  // of a turn
+  const int lane = threadIdx.x & (kWave - 1), l = threadIdx.x % LANES, at = threadIdx.x / LANES;
+  const float inv = 1.f / (float)C;
+  float gm[PIECES][E], bt[PIECES][E];
+#pragma unroll
+  for (int p = 0; p < PIECES; ++p) {
+    const int c = (p * LANES + l) * E;
+    if (gamma && c < C) {
+      load_piece<E>(gamma + c, gm[p]);
+      load_piece<E>(beta + c, bt[p]);
+    }
+  }
+  for (long long first = (long long)blockIdx.x * kRows * TURNS; first < rows; first += (long long)gridDim.x * kRows * TURNS) {
+    float v[TURNS][PIECES][E];
+#pragma unroll
+    for (int t = 0; t < TURNS; ++t) {
+      const long long row = std::min<long long>(first + t * kRows + at, rows - 1);  // (further ones repeat the last: all lanes stay active)
+#pragma unroll
+      for (int p = 0; p < PIECES; ++p) {
+        const int c = (p * LANES + l) * E;
+        if (c < C) {
+          load_piece<E>(x + row * C + c, v[t][p]);
+        } else {
+#pragma unroll
+          for (int e = 0; e < E; ++e) v[t][p][e] = 0.f;
+        }
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < TURNS; ++t) {
+      const long long row = first + t * kRows + at;
+      float s = 0.f;
+#pragma unroll
+      for (int p = 0; p < PIECES; ++p)
+#pragma unroll
+        for (int e = 0; e < E; ++e) s += v[t][p][e];
+      const float m = lanes_sum<1, LANES / 2>(s, lane) * inv;
+      s = 0.f;
+#pragma unroll
+      for (int p = 0; p < PIECES; ++p)
+        if ((p * LANES + l) * E < C) {
+#pragma unroll
+          for (int e = 0; e < E; ++e) s = __builtin_fmaf(v[t][p][e] - m, v[t][p][e] - m, s);
+        }
+      const float r = 1.f / sqrtf(lanes_sum<1, LANES / 2>(s, lane) * inv + eps);
+      if (row >= rows) continue;
+      if (l == 0) {
+        mean[row] = m;
+        rstd[row] = r;
+      }
+#pragma unroll
+      for (int p = 0; p < PIECES; ++p) {
+        const int c = (p * LANES + l) * E;
+        if (c >= C) continue;
+        normalise<E>(v[t][p], m, r, gamma != nullptr, gm[p], bt[p], act);
+        store_piece<E>(out + row * C + c, v[t][p]);
+      }
+    }
+  }
+}
+
+// dx, and per workgroup the sums of dz xhat and dz of every channel: part [workgroups][2][C]
+template <typename T, int E, int LANES, int PIECES, int TURNS>
+__global__ __launch_bounds__(kThreads) void norm_rows_bwd_kernel(const T* __restrict__ x, const T* __restrict__ gamma, const T* __restrict__ beta,
+                                                                 const float* __restrict__ mean, const float* __restrict__ rstd, const T* __restrict__ dout,
+                                                                 int rows, int C, int act, T* __restrict__ dx, float* __restrict__ part) {
+  constexpr int kRows = kThreads / LANES;
+  __shared__ float sums[kRows > 1 ? kRows : 1][LANES * E];
+  const int lane = threadIdx.x & (kWave - 1), l = threadIdx.x % LANES, at = threadIdx.x / LANES;
+  const float inv = 1.f / (float)C;
+  float gm[PIECES][E], bt[PIECES][E], dg[PIECES][E], db[PIECES][E];
+#pragma unroll
+  for (int p = 0; p < PIECES; ++p) {
+    const int c = (p * LANES + l) * E;
+    if (gamma && c < C) {
+      load_piece<E>(gamma + c, gm[p]);
+      load_piece<E>(beta + c, bt[p]);
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e) dg[p][e] = db[p][e] = 0.f;
+  }
+  for (long long first = (long long)blockIdx.x * kRows * TURNS; first < rows; first += (long long)gridDim.x * kRows * TURNS) {
+    float v[TURNS][PIECES][E], g[TURNS][PIECES][E], m[TURNS], r[TURNS];
+#pragma unroll
+    for (int t = 0; t < TURNS; ++t) {
+      const long long row = std::min<long long>(first + t * kRows + at, rows - 1);
+      m[t] = mean[row];
+      r[t] = rstd[row];
+#pragma unroll
+      for (int p = 0; p < PIECES; ++p) {
+        const int c = (p * LANES + l) * E;
+        if (c < C) {
+          load_piece<E>(x + row * C + c, v[t][p]);
+          load_piece<E>(dout + row * C + c, g[t][p]);
+        }
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < TURNS; ++t) {
+      const long long row = first + t * kRows + at;
+      float s1 = 0.f, s2 = 0.f;
+#pragma unroll
+      for (int p = 0; p < PIECES; ++p) {
+        if ((p * LANES + l) * E >= C) continue;
+        slopes<E>(v[t][p], g[t][p], m[t], r[t], gamma != nullptr, gm[p], bt[p], act);
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          if (row < rows) {
+            dg[p][e] = __builtin_fmaf(g[t][p][e], v[t][p][e], dg[p][e]);
+            db[p][e] += g[t][p][e];
+          }
+          if (gamma) g[t][p][e] *= gm[p][e];
+          s1 += g[t][p][e];
+          s2 = __builtin_fmaf(g[t][p][e], v[t][p][e], s2);
+        }
+      }
+      s1 = lanes_sum<1, LANES / 2>(s1, lane) * inv;
+      s2 = lanes_sum<1, LANES / 2>(s2, lane) * inv;
+      if (row >= rows) continue;
+#pragma unroll
+      for (int p = 0; p < PIECES; ++p) {
+        const int c = (p * LANES + l) * E;
+        if (c >= C) continue;
+#pragma unroll
+        for (int e = 0; e < E; ++e) g[t][p][e] = r[t] * (g[t][p][e] - s1 - v[t][p][e] * s2);
+        store_piece<E>(dx + row * C + c, g[t][p]);
+      }
+    }
+  }
+  if (!part) return;
+  // the lane groups' sums, one piece of columns after another
+#pragma unroll
+  for (int which = 0; which < 2; ++which)
+#pragma unroll
+    for (int p = 0; p < PIECES; ++p) {
+      __syncthreads();
+#pragma unroll
+      for (int e = 0; e < E; ++e) sums[at][l * E + e] = which ? db[p][e] : dg[p][e];
+      __syncthreads();
+      for (int i = threadIdx.x; i < LANES * E; i += kThreads) {
+        float s = 0.f;
+#pragma unroll
+        for (int k = 0; k < kRows; ++k) s += sums[k][i];
+        const int c = p * LANES * E + i;
+        if (c < C) part[((size_t)blockIdx.x * 2 + which) * C + c] = s;
+      }
+    }
+}
+
+// out[which][c] = sum over i < n of part[i][which][c]: 32 channels a workgroup, 32 runs of parts beside each other
+__global__ __launch_bounds__(1024) void norm_channel_sums_kernel(const float* __restrict__ part, int n, int C, float* __restrict__ dgamma, float* __restrict__ dbeta) {
+  __shared__ float sums[32][33];
+  const int c = blockIdx.x * 32 + (threadIdx.x & 31), run = threadIdx.x >> 5;
+  const float* from = part + (size_t)blockIdx.y * C + std::min(c, C - 1);
   float s = 0.f;
-  for (long long i = threadIdx.x; i < n; i += kThreads) s += Elem<T>::load(x + base + (size_t)(i / Cg) * C + i % Cg);
-  const float m = block_sum(s, acc) / (float)n;
+#pragma unroll 8
+  for (int i = run; i < n; i += 32) s += from[(size_t)i * 2 * C];
+  sums[run][threadIdx.x & 31] = s;
+  __syncthreads();
+  if (run == 0 && c < C) {
+    float t = 0.f;
+#pragma unroll
+    for (int k = 0; k < 32; ++k) t += sums[k][threadIdx.x];
+    (blockIdx.y ? dbeta : dgamma)[c] = t;
+  }
+}
+
+// ---------------------------------------------------------------------------------------------------------------- groups
+
+// How an image is cut: columns are pieces of E channels.
+struct Cut {
+  int E;
+  int group_cols;  // of a group
+  int shares;      // blocks of columns that share a group, 1 where blocks hold whole groups
+  int block_cols;  // columns of a block
+  int block_groups;
+  int blocks;      // of an image's columns
+  int lanes;       // threads over each other in a column: kThreads / block_cols
+  int rows;        // tokens of a workgroup
+  int slabs;       // workgroups over an image's tokens
+  uint32_t cols_magic, group_magic;
+  __host__ __device__ int parts() const { return slabs * shares; }  // of a group
+};
+
+struct Groups {  // what the kernels take
+  const void *x, *gamma, *beta, *dout;
+  int N, C, G;
+  Cut k;
+  unsigned first;  // workgroup of the launch
+  float eps;
+  int act;
+  void* out;            // out, or dx
+  float *mean, *rstd;   // [B,G]
+  float2* group_part;   // [B][G][parts]: mean and M2, or the sums of dh and dh xhat
+  float2* totals;       // [B][G]: these sums of the whole group, where a launch of its own adds them up
+  float* channel_part;  // [B][slabs][2][C]
+};
+
+// a thread's place: column of the block, its group in the block, first channel; the workgroup's tokens
+struct Place {
+  int b, block, slab;
+  int col, q, lane_row;
+  int c, group, groups, cols, group_cols;
+  bool active;
+  int row0, row1;
+  size_t base;
+  __device__ __forceinline__ Place(const Groups& a, unsigned work) {
+    const Cut& k = a.k;
+    const unsigned per_image = (unsigned)k.blocks * k.slabs;
+    b = work / per_image;
+    const unsigned rest = work - b * per_image;
+    slab = rest / k.blocks;
+    block = rest - slab * k.blocks;
+    lane_row = exact_div(threadIdx.x, k.block_cols, k.cols_magic);
+    col = threadIdx.x - lane_row * k.block_cols;
+    int first_col;
+    if (k.shares > 1) {  // a share of one group
+      group = block / k.shares;
+      const int share = block - group * k.shares;
+      first_col = group * k.group_cols + share * k.block_cols;
+      cols = std::min(k.block_cols, k.group_cols - share * k.block_cols);
+      groups = 1;
+      group_cols = cols;
+      q = 0;
+    } else {
+      group = block * k.block_groups;
+      first_col = group * k.group_cols;
+      groups = std::min(k.block_groups, a.G - group);
+      cols = groups * k.group_cols;
+      group_cols = k.group_cols;
+      q = exact_div(col, k.group_cols, k.group_magic);
+    }
+    active = lane_row < k.lanes && col < cols;
+    c = (first_col + (active ? col : 0)) * k.E;
+    row0 = slab * k.rows;
+    row1 = std::min(row0 + k.rows, a.N);
+    base = (size_t)b * a.N * a.C + c;
+    if (!active) q = 0;
+  }
+  __device__ __forceinline__ int part(const Groups& a) const { return a.k.shares > 1 ? slab * a.k.shares + block % a.k.shares : slab; }
+};
+
+// per group of the block, the sums over its threads of v: result[q], read by all threads afterwards
+__device__ __forceinline__ void group_sums(const Groups& a, const Place& w, float v, float (&values)[kThreads], float (&result)[kThreads]) {
+  const Cut& k = a.k;
+  __syncthreads();
+  values[threadIdx.x] = v;
+  __syncthreads();
+  const int lane = threadIdx.x & (kWave - 1), n = k.lanes * w.group_cols;
+  const uint32_t magic = k.shares > 1 ? 0u : k.group_magic;
+  for (int q = threadIdx.x / kWave; q < w.groups; q += kWaves) {
+    float s = 0.f;
+    for (int i = lane; i < n; i += kWave) {
+      const int row = k.shares > 1 ? i / w.group_cols : exact_div(i, w.group_cols, magic);
+      s += values[row * k.block_cols + q * w.group_cols + i - row * w.group_cols];
+    }
+    s = wave_sum(s);
+    if (lane == 0) result[q] = s;
+  }
+  __syncthreads();
+}
+
+// values of a group's part i
+__device__ __forceinline__ float part_count(const Groups& a, int i) {
+  const Cut& k = a.k;
+  const int slab = i / k.shares, share = i - slab * k.shares;
+  const int cols = k.shares > 1 ? std::min(k.block_cols, k.group_cols - share * k.block_cols) : k.group_cols;
+  return (float)(std::min(k.rows, a.N - slab * k.rows)) * (float)(cols * k.E);
+}
+// mean and rstd of a whole group from its parts, by a wave
+__device__ __forceinline__ void join_statistics(const Groups& a, size_t bg, int lane, float& mean, float& rstd) {
+  const int parts = a.k.parts();
+  const float2* from = a.group_part + bg * parts;
+  const float n = (float)a.N * (float)(a.k.group_cols * a.k.E);
+  float s = 0.f;
+  for (int i = lane; i < parts; i += kWave) s += from[i].x * (part_count(a, i) / n);
+  mean = wave_sum(s);
   s = 0.f;
-  for (long long i = threadIdx.x; i < n; i += kThreads) {
-    const float d = Elem<T>::load(x + base + (size_t)(i / Cg) * C + i % Cg) - m;
-    s += d * d;
+  for (int i = lane; i < parts; i += kWave) {
+    const float2 v = from[i];
+    s += v.y + part_count(a, i) * (v.x - mean) * (v.x - mean);
   }
-  const float r = 1.f / sqrtf(block_sum(s, acc) / (float)n + eps);
-  if (threadIdx.x == 0) {
-    mean[blockIdx.x] = m;
-    rstd[blockIdx.x] = r;
+  rstd = 1.f / sqrtf(wave_sum(s) / n + a.eps);
+}
+__device__ __forceinline__ float2 join_sums(const Groups& a, size_t bg, int lane) {
+  const int parts = a.k.parts();
+  const float2* from = a.group_part + bg * parts;
+  float s1 = 0.f, s2 = 0.f;
+  for (int i = lane; i < parts; i += kWave) {
+    const float2 v = from[i];
+    s1 += v.x;
+    s2 += v.y;
   }
-  for (long long i = threadIdx.x; i < n; i += kThreads) {
-    const int c = (int)(i % Cg);
-    const size_t at = base + (size_t)(i / Cg) * C + c;
-    float z = (Elem<T>::load(x + at) - m) * r;
-    if (gamma) z = z * Elem<T>::load(gamma + g * Cg + c) + Elem<T>::load(beta + g * Cg + c);
-    Elem<T>::store(out + at, act_value(z, act));
+  return make_float2(wave_sum(s1), wave_sum(s2));
+}
+
+// WHOLE: the workgroup holds all of its groups' values: statistics and output in one launch
+template <typename T, int E, int V, bool WHOLE>
+__global__ __launch_bounds__(kThreads) void norm_stats_kernel(Groups a) {
+  __shared__ float values[kThreads], result[kThreads];
+  const Place w(a, a.first + blockIdx.x);
+  const Cut& k = a.k;
+  float v[V][E];
+  float s = 0.f;
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    const int row = w.row0 + i * k.lanes + w.lane_row;
+    if (w.active && row < w.row1) {
+      load_piece<E>((const T*)a.x + w.base + (size_t)row * a.C, v[i]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < E; ++e) v[i][e] = 0.f;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < V; ++i)
+#pragma unroll
+    for (int e = 0; e < E; ++e) s += v[i][e];
+  group_sums(a, w, s, values, result);
+  const float n = (float)(w.row1 - w.row0) * (float)(w.group_cols * E);
+  const float mean = result[w.q] / n;
+  s = 0.f;
+#pragma unroll
+  for (int i = 0; i < V; ++i)
+    if (w.active && w.row0 + i * k.lanes + w.lane_row < w.row1) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) s = __builtin_fmaf(v[i][e] - mean, v[i][e] - mean, s);
+    }
+  const float m_first = (int)threadIdx.x < w.groups ? result[threadIdx.x] / n : 0.f;
+  group_sums(a, w, s, values, result);
+  const size_t bg = (size_t)w.b * a.G + w.group;
+  if constexpr (WHOLE) {
+    if ((int)threadIdx.x < w.groups) {
+      a.mean[bg + threadIdx.x] = m_first;
+      a.rstd[bg + threadIdx.x] = 1.f / sqrtf(result[threadIdx.x] / n + a.eps);
+    }
+    if (!w.active) return;
+    const float rstd = 1.f / sqrtf(result[w.q] / n + a.eps);
+    float gm[E], bt[E];
+    if (a.gamma) {
+      load_piece<E>((const T*)a.gamma + w.c, gm);
+      load_piece<E>((const T*)a.beta + w.c, bt);
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const int row = w.row0 + i * k.lanes + w.lane_row;
+      if (row >= w.row1) continue;
+      normalise<E>(v[i], mean, rstd, a.gamma != nullptr, gm, bt, a.act);
+      store_piece<E>((T*)a.out + w.base + (size_t)row * a.C, v[i]);
+    }
+  } else {
+    if ((int)threadIdx.x < w.groups) a.group_part[(bg + threadIdx.x) * k.parts() + w.part(a)] = make_float2(m_first, result[threadIdx.x]);
   }
 }
 
-template <typename T>
-__device__ __forceinline__ void norm_terms(const T* x, const T* dout, const T* gamma, const T* beta, size_t at, int c, float m, float r, int act,
-                                           float& xhat, float& dz, float& gm) {
-  xhat = (Elem<T>::load(x + at) - m) * r;
-  gm = gamma ? Elem<T>::load(gamma + c) : 1.f;
-  const float z = gamma ? xhat * gm + Elem<T>::load(beta + c) : xhat;
-  dz = Elem<T>::load(dout + at) * act_slope(z, act);
-}
-
-template <typename T>
-__global__ __launch_bounds__(kThreads) void norm_bwd_kernel(const T* __restrict__ x, const T* __restrict__ gamma, const T* __restrict__ beta,
-                                                            const float* __restrict__ mean, const float* __restrict__ rstd, const T* __restrict__ dout, int N,
-                                                            int C, int G, int act, T* __restrict__ dx) {
-  __shared__ float acc[4];
-  const int b = blockIdx.x / G, g = blockIdx.x % G, Cg = C / G;
-  const size_t base = (size_t)b * N * C + (size_t)g * Cg;
-  const long long n = (long long)N * Cg;
-  const float m = mean[blockIdx.x], r = rstd[blockIdx.x];
-  float s1 = 0.f, s2 = 0.f, xhat, dz, gm;
-  for (long long i = threadIdx.x; i < n; i += kThreads) {
-    norm_terms(x, dout, gamma, beta, base + (size_t)(i / Cg) * C + i % Cg, g * Cg + (int)(i % Cg), m, r, act, xhat, dz, gm);
-    s1 += dz * gm;
-    s2 += dz * gm * xhat;
-  }
-  s1 = block_sum(s1, acc) / (float)n;
-  s2 = block_sum(s2, acc) / (float)n;
-  for (long long i = threadIdx.x; i < n; i += kThreads) {
-    const size_t at = base + (size_t)(i / Cg) * C + i % Cg;
-    norm_terms(x, dout, gamma, beta, at, g * Cg + (int)(i % Cg), m, r, act, xhat, dz, gm);
-    Elem<T>::store(dx + at, r * (dz * gm - s1 - xhat * s2));
+// the parts of a group put together by a launch of its own, a wave a group: statistics, or with BWD the sums
+template <bool BWD>
+__global__ __launch_bounds__(kThreads) void norm_join_kernel(Groups a, int groups) {
+  const int bg = blockIdx.x * kWaves + threadIdx.x / kWave, lane = threadIdx.x & (kWave - 1);
+  if (bg >= groups) return;
+  if constexpr (BWD) {
+    const float2 s = join_sums(a, bg, lane);
+    if (lane == 0) a.totals[bg] = s;
+  } else {
+    float m, r;
+    join_statistics(a, bg, lane, m, r);
+    if (lane == 0) {
+      a.mean[bg] = m;
+      a.rstd[bg] = r;
+    }
   }
 }
 
-// workgroup per channel
-template <typename T>
-__global__ __launch_bounds__(kThreads) void norm_affine_kernel(const T* __restrict__ x, const T* __restrict__ gamma, const T* __restrict__ beta,
-                                                               const float* __restrict__ mean, const float* __restrict__ rstd, const T* __restrict__ dout,
-                                                               int B, int N, int C, int G, int act, float* __restrict__ dgamma, float* __restrict__ dbeta) {
-  __shared__ float acc[4];
-  const int c = blockIdx.x, g = c / (C / G);
-  float sg = 0.f, sb = 0.f, xhat, dz, gm;
-  for (long long i = threadIdx.x; i < (long long)B * N; i += kThreads) {
-    const size_t bg = (size_t)(i / N) * G + g;
-    norm_terms(x, dout, gamma, beta, (size_t)i * C + c, c, mean[bg], rstd[bg], act, xhat, dz, gm);
-    sg += dz * xhat;
-    sb += dz;
+// JOIN: the workgroup puts its groups' parts together itself
+template <typename T, int E, int V, bool JOIN>
+__global__ __launch_bounds__(kThreads) void norm_apply_kernel(Groups a) {
+  __shared__ float means[kThreads], rstds[kThreads];
+  const Place w(a, a.first + blockIdx.x);
+  const Cut& k = a.k;
+  float v[V][E];
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    const int row = w.row0 + i * k.lanes + w.lane_row;
+    if (w.active && row < w.row1) load_piece<E>((const T*)a.x + w.base + (size_t)row * a.C, v[i]);
   }
-  sg = block_sum(sg, acc);
-  sb = block_sum(sb, acc);
-  if (threadIdx.x == 0) {
-    dgamma[c] = sg;
-    dbeta[c] = sb;
+  float gm[E], bt[E];
+  if (a.gamma) {
+    load_piece<E>((const T*)a.gamma + w.c, gm);
+    load_piece<E>((const T*)a.beta + w.c, bt);
+  }
+  const size_t bg = (size_t)w.b * a.G + w.group;
+  float mean, rstd;
+  if constexpr (JOIN) {
+    const int lane = threadIdx.x & (kWave - 1);
+    for (int q = threadIdx.x / kWave; q < w.groups; q += kWaves) {
+      float m, r;
+      join_statistics(a, bg + q, lane, m, r);
+      if (lane == 0) {
+        means[q] = m;
+        rstds[q] = r;
+        if (w.slab == 0 && (k.shares == 1 || w.block % k.shares == 0)) {
+          a.mean[bg + q] = m;
+          a.rstd[bg + q] = r;
+        }
+      }
+    }
+    __syncthreads();
+    mean = means[w.q];
+    rstd = rstds[w.q];
+  } else {
+    mean = a.mean[bg + w.q];
+    rstd = a.rstd[bg + w.q];
+  }
+  if (!w.active) return;
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    const int row = w.row0 + i * k.lanes + w.lane_row;
+    if (row >= w.row1) continue;
+    normalise<E>(v[i], mean, rstd, a.gamma != nullptr, gm, bt, a.act);
+    store_piece<E>((T*)a.out + w.base + (size_t)row * a.C, v[i]);
   }
 }
 
+// per workgroup: the sums of dz xhat and dz of its channels, and of dh xhat and dh of its groups
+template <typename T, int E>
+__global__ __launch_bounds__(kThreads) void norm_bwd_sums_kernel(Groups a) {
+  __shared__ float values[kThreads], result[kThreads];
+  __shared__ float sums[kThreads * E];
+  const Place w(a, a.first + blockIdx.x);
+  const Cut& k = a.k;
+  const size_t bg = (size_t)w.b * a.G + w.group;
+  const float mean = a.mean[bg + w.q], rstd = a.rstd[bg + w.q];
+  float gm[E], bt[E], dg[E], db[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    gm[e] = 1.f;
+    bt[e] = dg[e] = db[e] = 0.f;
+  }
+  if (a.gamma) {
+    load_piece<E>((const T*)a.gamma + w.c, gm);
+    load_piece<E>((const T*)a.beta + w.c, bt);
+  }
+  if (w.active) {
+#pragma unroll 4
+    for (int row = w.row0 + w.lane_row; row < w.row1; row += k.lanes) {
+      float x[E], g[E];
+      load_piece<E>((const T*)a.x + w.base + (size_t)row * a.C, x);
+      load_piece<E>((const T*)a.dout + w.base + (size_t)row * a.C, g);
+      slopes<E>(x, g, mean, rstd, a.gamma != nullptr, gm, bt, a.act);
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        dg[e] = __builtin_fmaf(g[e], x[e], dg[e]);
+        db[e] += g[e];
+      }
+    }
+  }
+  float s1 = 0.f, s2 = 0.f;
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    s1 = __builtin_fmaf(gm[e], db[e], s1);
+    s2 = __builtin_fmaf(gm[e], dg[e], s2);
+  }
+  group_sums(a, w, s1, values, result);
+  const float t1 = (int)threadIdx.x < w.groups ? result[threadIdx.x] : 0.f;
+  group_sums(a, w, s2, values, result);
+  if ((int)threadIdx.x < w.groups) a.group_part[(bg + threadIdx.x) * k.parts() + w.part(a)] = make_float2(t1, result[threadIdx.x]);
+  if (!a.channel_part) return;
+  // (the block's first channel: w.c of a thread without a column)
+  const int c0 = w.c - (w.active ? w.col : 0) * E;
+  for (int which = 0; which < 2; ++which) {
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < E; ++e) sums[(w.lane_row * k.block_cols + w.col) * E + e] = which ? db[e] : dg[e];
+    __syncthreads();
+    float* to = a.channel_part + (((size_t)w.b * k.slabs + w.slab) * 2 + which) * a.C + c0;
+    for (int i = threadIdx.x; i < w.cols * E; i += kThreads) {
+      float s = 0.f;
+      for (int j = 0; j < k.lanes; ++j) s += sums[j * k.block_cols * E + i];
+      to[i] = s;
+    }
+  }
+}
+
+template <typename T, int E, int V, bool JOIN>
+__global__ __launch_bounds__(kThreads) void norm_bwd_apply_kernel(Groups a, Cut parts_cut) {
+  __shared__ float2 totals[kThreads];
+  const Place w(a, a.first + blockIdx.x);
+  const Cut& k = a.k;
+  const size_t bg = (size_t)w.b * a.G + w.group;
+  float x[V][E], g[V][E];
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    const int row = w.row0 + i * k.lanes + w.lane_row;
+    if (w.active && row < w.row1) {
+      load_piece<E>((const T*)a.x + w.base + (size_t)row * a.C, x[i]);
+      load_piece<E>((const T*)a.dout + w.base + (size_t)row * a.C, g[i]);
+    }
+  }
+  const float mean = a.mean[bg + w.q], rstd = a.rstd[bg + w.q];
+  float gm[E], bt[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    gm[e] = 1.f;
+    bt[e] = 0.f;
+  }
+  if (a.gamma) {
+    load_piece<E>((const T*)a.gamma + w.c, gm);
+    load_piece<E>((const T*)a.beta + w.c, bt);
+  }
+  const float inv = 1.f / ((float)a.N * (float)(k.group_cols * E));
+  float2 s;
+  if constexpr (JOIN) {
+    Groups p = a;
+    p.k = parts_cut;
+    const int lane = threadIdx.x & (kWave - 1);
+    for (int q = threadIdx.x / kWave; q < w.groups; q += kWaves) {
+      const float2 t = join_sums(p, bg + q, lane);
+      if (lane == 0) totals[q] = t;
+    }
+    __syncthreads();
+    s = totals[w.q];
+  } else {
+    s = a.totals[bg + w.q];
+  }
+  if (!w.active) return;
+  const float s1 = s.x * inv, s2 = s.y * inv;
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    const int row = w.row0 + i * k.lanes + w.lane_row;
+    if (row >= w.row1) continue;
+    slopes<E>(x[i], g[i], mean, rstd, a.gamma != nullptr, gm, bt, a.act);
+#pragma unroll
+    for (int e = 0; e < E; ++e) g[i][e] = rstd * (g[i][e] * gm[e] - s1 - x[i][e] * s2);
+    store_piece<E>((T*)a.out + w.base + (size_t)row * a.C, g[i]);
+  }
+}
+
+// ------------------------------------------------------------------------------------------------------------------ host
+
+constexpr int kHeld = 64;      // values of a thread that holds its run of tokens in registers
+constexpr int kHeldFew = 16;   // ... where that leaves fewer than kFullGrid workgroups
+constexpr long long kFullGrid = 512;
+constexpr int kJoinParts = 256;  // more parts of a group than this are put together by a launch of its own
+
+Cut cut_columns(int C, int G, int E) {
+  Cut k = {};
+  k.E = E;
+  k.group_cols = C / G / E;
+  if (k.group_cols > kThreads) {
+    k.shares = cdiv(k.group_cols, kThreads);
+    k.block_cols = cdiv(k.group_cols, k.shares);
+    k.shares = cdiv(k.group_cols, k.block_cols);
+    k.block_groups = 1;
+    k.blocks = G * k.shares;
+  } else {
+    k.shares = 1;
+    k.blocks = cdiv(G, kThreads / k.group_cols);
+    k.block_groups = cdiv(G, k.blocks);
+    k.blocks = cdiv(G, k.block_groups);
+    k.block_cols = k.block_groups * k.group_cols;
+  }
+  k.lanes = kThreads / k.block_cols;
+  k.cols_magic = div_magic(k.block_cols);
+  k.group_magic = div_magic(k.group_cols);
+  return k;
+}
+void cut_rows(Cut& k, int N, long long rows) {
+  k.rows = (int)std::min<long long>(rows, N);
+  k.slabs = cdiv(N, k.rows);
+}
+// threads hold `held` values each
+Cut cut_held(int B, int N, int C, int G, int E, int* held) {
+  Cut k = cut_columns(C, G, E);
+  for (int h : {kHeld, kHeldFew}) {
+    *held = h;
+    cut_rows(k, N, (long long)h / E * k.lanes);
+    if ((long long)B * k.blocks * k.slabs >= kFullGrid || k.slabs == 1) break;
+  }
+  return k;
+}
+// for sums: about 1024 workgroups, of at least four turns
+Cut cut_sums(int B, int N, int C, int G, int E) {
+  Cut k = cut_columns(C, G, E);
+  const long long slabs = std::max(1ll, 1024 / ((long long)B * k.blocks));
+  cut_rows(k, N, std::max<long long>(4 * k.lanes, cdiv(N, slabs)));
+  return k;
+}
+
+// pieces of 16 bytes, or single values
 template <typename T>
-hipError_t fwd(const NormArgs& a, hipStream_t stream) {
-  AFFMAE_LAUNCH("norm_fwd_kernel", stream, norm_fwd_kernel<T>, dim3(a.B * a.G), dim3(kThreads), 0, stream, (const T*)a.x, (const T*)a.gamma, (const T*)a.beta, a.N,
-                a.C, a.G, a.eps, a.act, (T*)a.out, a.mean, a.rstd);
+int piece_of(const NormArgs& a, const void* y, const void* z) {
+  const int E = kPiece<T>;
+  return a.C / a.G % E == 0 && aligned16(a.x) && aligned16(a.gamma) && aligned16(a.beta) && aligned16(y) && aligned16(z) ? E : 1;
+}
+
+// Rows that the row kernels hold: LANES x PIECES pieces, at most 16 pieces of single values and 4 of 16 bytes a lane.
+bool rows_fit(int N, int C, int G, int E) { return N == 1 && G == 1 && cdiv(C, E) <= kWave * (E == 1 ? 16 : 4); }
+int row_lanes(int C, int E) {
+  int lanes = 4;
+  while (lanes < kWave && lanes * E < C) lanes *= 2;
+  return lanes;
+}
+int rows_bwd_blocks(int rows) { return std::min(cdiv(rows, 16), 1024); }
+
+template <typename F>
+hipError_t for_row_shape(int C, int E, F f) {
+  const int lanes = row_lanes(C, E), pieces = cdiv(cdiv(C, E), lanes);
+  using std::integral_constant;
+  if (lanes == 4) return f(integral_constant<int, 4>(), integral_constant<int, 1>());
+  if (lanes == 8) return f(integral_constant<int, 8>(), integral_constant<int, 1>());
+  if (lanes == 16) return f(integral_constant<int, 16>(), integral_constant<int, 1>());
+  if (lanes == 32) return f(integral_constant<int, 32>(), integral_constant<int, 1>());
+  if (pieces == 1) return f(integral_constant<int, 64>(), integral_constant<int, 1>());
+  if (pieces == 2) return f(integral_constant<int, 64>(), integral_constant<int, 2>());
+  if (pieces <= 4) return f(integral_constant<int, 64>(), integral_constant<int, 4>());
+  return f(integral_constant<int, 64>(), integral_constant<int, 16>());
+}
+constexpr int turns_of(int pieces) { return pieces == 1 ? 4 : pieces == 2 ? 2 : 1; }
+
+template <typename T, int E>
+hipError_t rows_fwd(const NormArgs& a, hipStream_t stream) {
+  return for_row_shape(a.C, E, [&](auto lanes, auto pieces) {
+    constexpr int L = lanes, P = pieces, U = turns_of(P);
+    if constexpr (P == 16 && E > 1) {
+      return hipErrorInvalidValue;
+    } else {
+      const unsigned grid = (unsigned)std::min(cdiv(a.B, kThreads / L * U), 4096);
+      AFFMAE_LAUNCH("norm_rows_fwd_kernel", stream, (norm_rows_fwd_kernel<T, E, L, P, U>), dim3(grid), dim3(kThreads), 0, stream, (const T*)a.x, (const T*)a.gamma,
+                    (const T*)a.beta, a.B, a.C, a.eps, a.act, (T*)a.out, a.mean, a.rstd);
+      return hipGetLastError();
+    }
+  });
+}
+template <typename T, int E>
+hipError_t rows_bwd(const NormArgs& a, hipStream_t stream) {
+  const int blocks = rows_bwd_blocks(a.B);
+  float* part = a.dgamma ? static_cast<float*>(a.workspace) : nullptr;
+  const hipError_t rc = for_row_shape(a.C, E, [&](auto lanes, auto pieces) {
+    constexpr int L = lanes, P = pieces, U = turns_of(P) > 2 ? 2 : turns_of(P);
+    if constexpr (P == 16 && E > 1) {
+      return hipErrorInvalidValue;
+    } else {
+      AFFMAE_LAUNCH("norm_rows_bwd_kernel", stream, (norm_rows_bwd_kernel<T, E, L, P, U>), dim3(blocks), dim3(kThreads), 0, stream, (const T*)a.x, (const T*)a.gamma,
+                    (const T*)a.beta, a.mean, a.rstd, (const T*)a.dout, a.B, a.C, a.act, (T*)a.dx, part);
+      return hipGetLastError();
+    }
+  });
+  if (rc != hipSuccess || !part) return rc;
+  AFFMAE_LAUNCH("norm_channel_sums_kernel", stream, norm_channel_sums_kernel, dim3(cdiv(a.C, 32), 2), dim3(1024), 0, stream, part, blocks, a.C, a.dgamma, a.dbeta);
   return hipGetLastError();
 }
-template <typename T>
-hipError_t bwd(const NormArgs& a, hipStream_t stream) {
-  AFFMAE_LAUNCH("norm_bwd_kernel", stream, norm_bwd_kernel<T>, dim3(a.B * a.G), dim3(kThreads), 0, stream, (const T*)a.x, (const T*)a.gamma, (const T*)a.beta,
-                a.mean, a.rstd, (const T*)a.dout, a.N, a.C, a.G, a.act, (T*)a.dx);
+
+Groups groups_of(const NormArgs& a, const Cut& k) {
+  Groups g = {};
+  g.x = a.x; g.gamma = a.gamma; g.beta = a.beta; g.dout = a.dout;
+  g.N = a.N; g.C = a.C; g.G = a.G; g.k = k; g.eps = a.eps; g.act = a.act;
+  g.mean = a.mean; g.rstd = a.rstd;
+  return g;
+}
+
+// f(workgroups) for all of a cut's, in launches of as many as the runtime takes
+template <typename F>
+void for_workgroups(Groups& g, int B, F f) {
+  const long long all = (long long)B * g.k.blocks * g.k.slabs;
+  for (long long first = 0; first < all; first += kMaxBlocks) {
+    g.first = (unsigned)first;
+    f(dim3((unsigned)std::min(all - first, kMaxBlocks)));
+  }
+}
+
+template <typename T, int E>
+hipError_t groups_fwd(const NormArgs& a, hipStream_t stream) {
+  int held;
+  const Cut k = cut_held(a.B, a.N, a.C, a.G, E, &held);
+  Groups g = groups_of(a, k);
+  g.out = a.out;
+  g.group_part = static_cast<float2*>(a.workspace);
+  const dim3 threads(kThreads);
+  const auto run = [&](auto values) {
+    constexpr int V = decltype(values)::value / E;
+    const auto all = [&](const char* name, auto kernel) {
+      (void)name;
+      for_workgroups(g, a.B, [&](dim3 grid) { AFFMAE_LAUNCH(name, stream, kernel, grid, threads, 0, stream, g); });
+    };
+    if (k.parts() == 1) return all("norm_stats_kernel", norm_stats_kernel<T, E, V, true>);
+    all("norm_stats_kernel", norm_stats_kernel<T, E, V, false>);
+    if (k.parts() <= kJoinParts) return all("norm_apply_kernel", norm_apply_kernel<T, E, V, true>);
+    AFFMAE_LAUNCH("norm_join_kernel", stream, norm_join_kernel<false>, dim3(cdiv((long long)a.B * a.G, kWaves)), threads, 0, stream, g, a.B * a.G);
+    all("norm_apply_kernel", norm_apply_kernel<T, E, V, false>);
+  };
+  if (held == kHeld)
+    run(std::integral_constant<int, kHeld>());
+  else
+    run(std::integral_constant<int, kHeldFew>());
+  return hipGetLastError();
+}
+
+struct BwdSpace {
+  size_t totals, channels, all;
+};
+BwdSpace bwd_space(int B, int C, int G, const Cut& k) {
+  BwdSpace s;
+  s.totals = up256((size_t)B * G * k.parts() * sizeof(float2));
+  s.channels = s.totals + up256((size_t)B * G * sizeof(float2));
+  s.all = s.channels + (size_t)B * k.slabs * 2 * C * sizeof(float);
+  return s;
+}
+
+template <typename T, int E>
+hipError_t groups_bwd(const NormArgs& a, hipStream_t stream) {
+  const Cut sums = cut_sums(a.B, a.N, a.C, a.G, E);
+  const BwdSpace at = bwd_space(a.B, a.C, a.G, sums);
+  char* ws = static_cast<char*>(a.workspace);
+  Groups g = groups_of(a, sums);
+  g.out = a.dx;
+  g.group_part = reinterpret_cast<float2*>(ws);
+  g.totals = reinterpret_cast<float2*>(ws + at.totals);
+  g.channel_part = a.dgamma ? reinterpret_cast<float*>(ws + at.channels) : nullptr;
+  const dim3 threads(kThreads);
+  for_workgroups(g, a.B, [&](dim3 grid) { AFFMAE_LAUNCH("norm_bwd_sums_kernel", stream, (norm_bwd_sums_kernel<T, E>), grid, threads, 0, stream, g); });
+  const bool join = sums.parts() <= kJoinParts;
+  if (!join) AFFMAE_LAUNCH("norm_join_kernel", stream, norm_join_kernel<true>, dim3(cdiv((long long)a.B * a.G, kWaves)), threads, 0, stream, g, a.B * a.G);
+  constexpr int V = std::max(kHeldFew * 2 / E, 1);
+  Cut k = cut_columns(a.C, a.G, E);
+  cut_rows(k, a.N, (long long)V * k.lanes);
+  g.k = k;
+  const auto kernel = join ? norm_bwd_apply_kernel<T, E, V, true> : norm_bwd_apply_kernel<T, E, V, false>;
+  for_workgroups(g, a.B, [&](dim3 grid) { AFFMAE_LAUNCH("norm_bwd_apply_kernel", stream, kernel, grid, threads, 0, stream, g, sums); });
   if (a.dgamma)
-    AFFMAE_LAUNCH("norm_affine_kernel", stream, norm_affine_kernel<T>, dim3(a.C), dim3(kThreads), 0, stream, (const T*)a.x, (const T*)a.gamma,
-                  (const T*)a.beta, a.mean, a.rstd, (const T*)a.dout, a.B, a.N, a.C, a.G, a.act, a.dgamma, a.dbeta);
+    AFFMAE_LAUNCH("norm_channel_sums_kernel", stream, norm_channel_sums_kernel, dim3(cdiv(a.C, 32), 2), dim3(1024), 0, stream, g.channel_part, a.B * sums.slabs,
+                  a.C, a.dgamma, a.dbeta);
   return hipGetLastError();
+}
+
+template <typename T, int E>
+hipError_t fwd(const NormArgs& a, hipStream_t stream) {
+  return rows_fit(a.N, a.C, a.G, E) ? rows_fwd<T, E>(a, stream) : groups_fwd<T, E>(a, stream);
+}
+template <typename T, int E>
+hipError_t bwd(const NormArgs& a, hipStream_t stream) {
+  return rows_fit(a.N, a.C, a.G, E) ? rows_bwd<T, E>(a, stream) : groups_bwd<T, E>(a, stream);
+}
+
+// the larger need of pieces of 16 bytes and of single values: which of them a call takes depends on its tensors' alignment
+template <typename F>
+size_t either(int C, int G, int dtype, F f) {
+  const int E = dtype == 1 ? 8 : 4;
+  return std::max(f(1), C / G % E == 0 ? f(E) : size_t(0));
 }
 
 }  // namespace
 
-size_t norm_fwd_workspace_bytes(int, int, int, int, int) { return 0; }
-size_t norm_bwd_workspace_bytes(int, int, int, int, int) { return 0; }
-hipError_t launch_norm_fwd(const NormArgs& a, hipStream_t stream) { return a.dtype == 1 ? fwd<bf16_t>(a, stream) : fwd<float>(a, stream); }
-hipError_t launch_norm_bwd(const NormArgs& a, hipStream_t stream) { return a.dtype == 1 ? bwd<bf16_t>(a, stream) : bwd<float>(a, stream); }
+size_t norm_fwd_workspace_bytes(int B, int N, int C, int G, int dtype) {
+  return either(C, G, dtype, [&](int E) -> size_t {
+    if (rows_fit(N, C, G, E)) return 0;
+    int held;
+    const Cut k = cut_held(B, N, C, G, E, &held);
+    return k.parts() > 1 ? (size_t)B * G * k.parts() * sizeof(float2) : 0;
+  });
+}
+size_t norm_bwd_workspace_bytes(int B, int N, int C, int G, int dtype) {
+  return either(C, G, dtype, [&](int E) -> size_t {
+    if (rows_fit(N, C, G, E)) return (size_t)rows_bwd_blocks(B) * 2 * C * sizeof(float);
+    return bwd_space(B, C, G, cut_sums(B, N, C, G, E)).all;
+  });
+}
+hipError_t launch_norm_fwd(const NormArgs& a, hipStream_t stream) {
+  if (a.dtype == 1) return piece_of<bf16_t>(a, a.out, nullptr) > 1 ? fwd<bf16_t, 8>(a, stream) : fwd<bf16_t, 1>(a, stream);
+  return piece_of<float>(a, a.out, nullptr) > 1 ? fwd<float, 4>(a, stream) : fwd<float, 1>(a, stream);
+}
+hipError_t launch_norm_bwd(const NormArgs& a, hipStream_t stream) {
+  if (a.dtype == 1) return piece_of<bf16_t>(a, a.dout, a.dx) > 1 ? bwd<bf16_t, 8>(a, stream) : bwd<bf16_t, 1>(a, stream);
+  return piece_of<float>(a, a.dout, a.dx) > 1 ? bwd<float, 4>(a, stream) : bwd<float, 1>(a, stream);
+}
 
 }  // namespace affmae

@@ -518,7 +518,7 @@ def _block(t, nbr, H, scale, p, rng):
     norm1 = aff.affmae_norm_bwd(one(x), t["g1"], t["b1"], m1, r1, one(dn1))
     g.update(x=dh + norm1["dx"].view(B, N, C), g1=norm1["dgamma"], b1=norm1["dbeta"], g2=norm2["dgamma"], b2=norm2["dbeta"], wo=o["dweight"], co=o["dbias"],
              wu=up["dweight"], cu=up["dbias"], wd=down["dweight"], cd=down["dbias"])
-    return y, g
+    return y, g, a["dk"]
 
 
 def _block_reference(v, nbr, H, scale, p, rng):
@@ -571,7 +571,7 @@ def test_block_forward_and_backward(dtype, tol):
     B, N, C, H, p = 2, 150, 64, 2, 0.2
     t, v, nbr = _block_inputs(dtype, B, N, C)
     rng = torch.tensor([[5, 1], [5, 2]], dtype=torch.int64, device="cuda")
-    y, g = _block(t, torch.from_numpy(nbr).cuda(), H, 0.18, p, rng)
+    y, g, _ = _block(t, torch.from_numpy(nbr).cuda(), H, 0.18, p, rng)
     ry, rg = _block_reference(v, nbr, H, 0.18, p, [(5, 1), (5, 2)])
     errs = {"y": np.abs(y.double().cpu().numpy() - ry).max() / np.abs(ry).max()}
     for k in rg:
@@ -596,12 +596,12 @@ def test_block_replayed_from_a_graph_on_another_stream():
     torch.cuda.synchronize()
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph, stream=side):
-        y, g = _block(t, nbr, H, 0.18, p, rng)
+        y, g, _ = _block(t, nbr, H, 0.18, p, rng)
     seen = []
     for rep in range(4):
         rng[:, 1] += 2
         t["x"].add_(0.125)
-        ey, eg = _block(t, nbr, H, 0.18, p, rng)
+        ey, eg, edk = _block(t, nbr, H, 0.18, p, rng)
         torch.cuda.synchronize()
         graph.replay()
         torch.cuda.synchronize()
@@ -609,7 +609,14 @@ def test_block_replayed_from_a_graph_on_another_stream():
         for k in ("wd", "cd", "wu", "cu", "g2", "b2"):  # in front of the attention's backward, whose sums may change in the last bits
             assert torch.equal(g[k], eg[k]), f"replay {rep}: {k}"
         for k in eg:
-            assert torch.allclose(g[k].float(), eg[k].float(), rtol=2e-2, atol=2e-2 * float(eg[k].float().abs().max())), f"replay {rep}: {k}"
+            atol = 2e-2 * float(eg[k].float().abs().max())
+            if k == "ck":
+                # The key's bias moves all logits of a query alike: its gradient is 0, and what is left of the sum over 400 tokens is
+                # their rounding.  dk is added up in an order that changes by 2^-22 of the terms or so, and a value as near to the middle
+                # of a step of bf16 as that (one in 2^13) is rounded the other way: by 2^-7 of the value.  Four in a channel's 400 are a bound
+                # that 64 channels x 4 replays exceed once in 1e6 runs (Poisson with mean 400 / 2^13 = 0.05: 256 x 0.05^5 / 5! = 7e-7).
+                atol = 4 * 2.0 ** -7 * float(edk.float().abs().max())
+            assert torch.allclose(g[k].float(), eg[k].float(), rtol=2e-2, atol=atol), f"replay {rep}: {k}"
         seen.append(y.clone())
     assert all(not torch.equal(a, b) for a, b in zip(seen, seen[1:]))
 
