@@ -18,6 +18,8 @@ namespace {
 
 typedef __attribute__((ext_vector_type(4))) int i32x4;
 
+__host__ __device__ __forceinline__ int cdiv(long long a, long long b) { return (int)((a + b - 1) / b); }
+
 constexpr uint32_t kNowhere = 0x80000000u;  // beyond every buffer: such loads bring 0
 
 // A buffer of at most 2^31 - 1 bytes from `base` on: what lies beyond reads as 0.
@@ -159,13 +161,14 @@ struct Frag<float> {
     float f[4];
   };
 };
-__device__ __forceinline__ f32x4 multiply(const Frag<bf16_t>& a, const Frag<bf16_t>& b, f32x4 c) {
+__device__ __forceinline__ f32x4 multiply(const Frag<bf16_t>& a, const Frag<bf16_t>& b, f32x4 c, int) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v, b.v, c, 0, 0, 0);
 }
-__device__ __forceinline__ f32x4 multiply(const Frag<float>& a, const Frag<float>& b, f32x4 c) {
-#pragma unroll
-  for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.f[j], b.f[j], c, 0, 0, 0);
-  return c;
+// the h-th of the instructions of a step
+template <typename T>
+constexpr int kStepParts = sizeof(T) == 2 ? 1 : 4;
+__device__ __forceinline__ f32x4 multiply(const Frag<float>& a, const Frag<float>& b, f32x4 c, int h) {
+  return __builtin_amdgcn_mfma_f32_16x16x4f32(a.f[h], b.f[h], c, 0, 0, 0);
 }
 template <typename T, bool ALONG, int BX>
 __device__ __forceinline__ Frag<T> read_frag(const char* slice, int row0, int step, int r, int g) {
@@ -213,9 +216,9 @@ struct GradEpilogue {
   float alpha;
 };
 
-// E values of row m from column n on, `at` = m N + n
+// E values of row m from column n on, `at` = m N + n, r: the residual's
 template <typename T, int E>
-__device__ __forceinline__ void finish(const Epilogue& e, const RngKey& key, float (&v)[E], int n, size_t at) {
+__device__ __forceinline__ void finish(const Epilogue& e, const RngKey& key, float (&v)[E], const float (&r)[E], int n, size_t at) {
   if (e.bias) {
     float b[E];
     load_piece<E>((const T*)e.bias + n, b);
@@ -229,28 +232,26 @@ __device__ __forceinline__ void finish(const Epilogue& e, const RngKey& key, flo
   }
   if (e.d.rng) drop<E>(v, e.d, key, at);
   if (e.residual) {
-    float r[E];
-    load_piece<E>((const T*)e.residual + at, r);
 #pragma unroll
     for (int i = 0; i < E; ++i) v[i] += r[i];
   }
   store_piece<E>((T*)e.out + at, v);
 }
 
-// 16 rows x TNW columns of a wave's products, from the strip in LDS, as pieces of E values in the order of memory
-template <typename T, int E, int TNW, typename F>
-__device__ __forceinline__ void strip_pieces(const float* strip, int lane, int m0, int n0, int M, int N, F f) {
-  constexpr int kRow = TNW / E, kAll = 16 * kRow;
-#pragma unroll
-  for (int i = 0; i < (kAll + kWave - 1) / kWave; ++i) {
-    const int q = i * kWave + lane, row = q / kRow, col = q % kRow * E;
-    if (kAll % kWave != 0 && q >= kAll) break;
-    if (m0 + row >= M || n0 + col >= N) continue;
-    float v[E];
-    load_piece<E>(strip + row * (TNW + 4) + col, v);
-    f(v, m0 + row, n0 + col);
+// The 16 x TNW products of a strip in LDS as pieces of E values in the order of memory: the lane's i-th piece, if it has one there.
+template <int E, int TNW>
+struct Strip {
+  static constexpr int kRow = TNW / E, kAll = 16 * kRow, kTurns = (kAll + kWave - 1) / kWave;
+  static constexpr int kLd = TNW + 4;
+  int row, col;
+  bool there;
+  __device__ __forceinline__ Strip(int i, int lane, int m, int n, int M, int N) {
+    const int q = i * kWave + lane;
+    row = q / kRow;
+    col = q % kRow * E;
+    there = (kAll % kWave == 0 || q < kAll) && m + row < M && n + col < N;
   }
-}
+};
 
 template <int BM, int BN>
 constexpr int kStageBytes = (BM + BN) * kSliceBytes;
@@ -258,10 +259,10 @@ constexpr int kStageBytes = (BM + BN) * kSliceBytes;
 // BM x BN values of c by WM x WN waves.  Two slices of both operands in LDS: one is multiplied while the next one is on its way.
 // The products are c^T tiles (b's rows along the instruction's rows), so that a lane holds four consecutive columns of c.
 template <typename T, bool AA, bool BA, int W, int BM, int BN, int WM, int WN, typename Ep>
-__global__ __launch_bounds__(WM* WN* kWave) void linear_kernel(Product p, Ep e) {
+__global__ __launch_bounds__(WM* WN* kWave, 2) void linear_kernel(Product p, Ep e) {
   extern __shared__ __align__(16) char lds[];
   constexpr int kThreads = WM * WN * kWave, TM = BM / WM, TN = BN / WN, IM = TM / 16, IN = TN / 16;
-  constexpr bool kGrad = std::is_same_v<Ep, GradEpilogue>;
+  constexpr bool kGrad = std::is_same_v<Ep, GradEpilogue>, kSums = kGrad && !AA;  // (a's sums: the weights' gradient)
   const int work = xcd_contiguous_block(blockIdx.x, gridDim.x);
   if (work >= p.tiles * p.splits) return;
   const int split = work / p.tiles, tile = work - split * p.tiles;
@@ -285,9 +286,9 @@ __global__ __launch_bounds__(WM* WN* kWave) void linear_kernel(Product p, Ep e) 
       sb.load_values(dst + BM * kSliceBytes, k0, k_end - k0);
     }
   };
-  f32x4 c[IM][IN] = {}, sums[IM] = {};
+  f32x4 c[IM][IN] = {}, sums[kSums ? IM : 1] = {};
   bool want_sums = false;
-  if constexpr (kGrad) want_sums = e.bias && nt == 0 && wn == 0;
+  if constexpr (kSums) want_sums = e.bias && nt == 0 && wn == 0;
   stage(0);
   for (int s = 0; s < slices; ++s) {
     // slice s has arrived, and every wave has read what the next one will be written over
@@ -303,16 +304,20 @@ __global__ __launch_bounds__(WM* WN* kWave) void linear_kernel(Product p, Ep e) 
 #pragma unroll
       for (int j = 0; j < IN; ++j) b[j] = read_frag<T, BA, BN>(bs, wn * TN + 16 * j, step, r, g);
 #pragma unroll
-      for (int i = 0; i < IM; ++i)
+      for (int h = 0; h < kStepParts<T>; ++h)  // (instructions that add to the same registers far from each other)
 #pragma unroll
-        for (int j = 0; j < IN; ++j) c[i][j] = multiply(b[j], a[i], c[i][j]);
-      if constexpr (kGrad) {
+        for (int i = 0; i < IM; ++i)
+#pragma unroll
+          for (int j = 0; j < IN; ++j) c[i][j] = multiply(b[j], a[i], c[i][j], h);
+      if constexpr (kSums) {
         if (want_sums) {  // a's sums over k: its products with ones
           Frag<T> ones;
           ones.u4 = sizeof(T) == 2 ? make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u)
                                    : make_uint4(0x3f800000u, 0x3f800000u, 0x3f800000u, 0x3f800000u);
 #pragma unroll
-          for (int i = 0; i < IM; ++i) sums[i] = multiply(ones, a[i], sums[i]);
+          for (int h = 0; h < kStepParts<T>; ++h)
+#pragma unroll
+            for (int i = 0; i < IM; ++i) sums[i] = multiply(ones, a[i], sums[i], h);
         }
       }
     }
@@ -320,76 +325,199 @@ __global__ __launch_bounds__(WM* WN* kWave) void linear_kernel(Product p, Ep e) 
   __syncthreads();
   float* strip = reinterpret_cast<float*>(lds) + wave * 16 * (TN + 4);
   static_assert(WM * WN * 16 * (TN + 4) * 4 <= kStageBytes<BM, BN>);
-  RngKey key = {};
-  bool pieces = false;
-  if constexpr (kGrad) {
-    pieces = p.N % kPiece<T> == 0 && ((uintptr_t)e.out & 15) == 0;
-  } else {
-    if (e.d.rng) key = rng_key(e.d.rng);
-    pieces = p.N % kPiece<T> == 0 && (((uintptr_t)e.out | (uintptr_t)e.pre | (uintptr_t)e.bias | (uintptr_t)e.residual) & 15) == 0;
-  }
-#pragma unroll
-  for (int i = 0; i < IM; ++i) {
-    const int m = m0 + wm * TM + 16 * i, n = n0 + wn * TN;
-    if (m >= p.M) break;
+  const int n = n0 + wn * TN;
+  const auto to_strip = [&](int i) __attribute__((always_inline)) {
+    wave_lds_sync();
 #pragma unroll
     for (int j = 0; j < IN; ++j) *reinterpret_cast<f32x4*>(strip + r * (TN + 4) + 16 * j + 4 * g) = c[i][j];
     wave_lds_sync();
-    if constexpr (kGrad) {
-      if (e.part) {
-        float* part = e.part + (size_t)split * p.M * e.part_ld;
-        strip_pieces<float, 4, TN>(strip, lane, m, n, p.M, e.part_ld, [&](float(&v)[4], int row, int col) { store_piece<4>(part + (size_t)row * e.part_ld + col, v); });
-      } else {
-        const auto put = [&](auto& v, int row, int col) {
-          for (float& x : v) x *= e.alpha;
-          store_piece<sizeof(v) / sizeof(float)>((T*)e.out + (size_t)row * p.N + col, v);
-        };
-        if (pieces)
-          strip_pieces<T, kPiece<T>, TN>(strip, lane, m, n, p.M, p.N, put);
-        else
-          strip_pieces<T, 1, TN>(strip, lane, m, n, p.M, p.N, put);
-      }
-      if (want_sums && g == 0 && m + r < p.M) {
+  };
+  const int strips = min(IM, (p.M - m0 - wm * TM + 15) >> 4);  // (none or fewer where the tile is cut off)
+  if constexpr (kSums) {
+    if (want_sums) {
+#pragma unroll
+      for (int i = 0; i < IM; ++i) {
+        const int m = m0 + wm * TM + 16 * i + r;
+        if (g != 0 || m >= p.M) continue;
         if (e.part)
-          e.part[(size_t)p.splits * p.M * e.part_ld + (size_t)split * p.M + m + r] = sums[i][0];
+          e.part[(size_t)p.splits * p.M * e.part_ld + (size_t)split * p.M + m] = sums[i][0];
         else
-          Elem<T>::store((T*)e.bias + m + r, sums[i][0] * e.alpha);
+          Elem<T>::store((T*)e.bias + m, sums[i][0] * e.alpha);
       }
-    } else {
-      const auto put = [&](auto& v, int row, int col) { finish<T, sizeof(v) / sizeof(float)>(e, key, v, col, (size_t)row * p.N + col); };
-      if (pieces)
-        strip_pieces<T, kPiece<T>, TN>(strip, lane, m, n, p.M, p.N, put);
-      else
-        strip_pieces<T, 1, TN>(strip, lane, m, n, p.M, p.N, put);
     }
-    wave_lds_sync();
+  }
+  if constexpr (kGrad) {
+    const auto run = [&](auto out, auto piece, int N) __attribute__((always_inline)) {
+      constexpr int E = decltype(piece)::value;
+      using S = Strip<E, TN>;
+#pragma unroll
+      for (int i = 0; i < IM; ++i) {
+        if (i >= strips) break;
+        const int m = m0 + wm * TM + 16 * i;
+        to_strip(i);
+#pragma unroll
+        for (int t = 0; t < S::kTurns; ++t) {
+          const S q(t, lane, m, n, p.M, N);
+          if (!q.there) continue;
+          float v[E];
+          load_piece<E>(strip + q.row * S::kLd + q.col, v);
+#pragma unroll
+          for (int x = 0; x < E; ++x) v[x] *= e.alpha;
+          store_piece<E>(out + (size_t)(m + q.row) * N + n + q.col, v);
+        }
+      }
+    };
+    using std::integral_constant;
+    if (e.part)  // (alpha is 1)
+      run(e.part + (size_t)split * p.M * e.part_ld, integral_constant<int, 4>(), e.part_ld);
+    else if (p.N % kPiece<T> == 0 && ((uintptr_t)e.out & 15) == 0)
+      run((T*)e.out, integral_constant<int, kPiece<T>>(), p.N);
+    else
+      run((T*)e.out, integral_constant<int, 1>(), p.N);
+  } else {
+    RngKey key = {};
+    if (e.d.rng) key = rng_key(e.d.rng);
+    const auto run = [&](auto piece) __attribute__((always_inline)) {
+      constexpr int E = decltype(piece)::value;
+      using S = Strip<E, TN>;
+      float next[S::kTurns][E];  // the residual's values are on their way a strip ahead
+      const auto fetch = [&](int i) __attribute__((always_inline)) {
+#pragma unroll
+        for (int t = 0; t < S::kTurns; ++t) {
+          const int m = m0 + wm * TM + 16 * i;
+          const S q(t, lane, m, n, p.M, p.N);
+          if (q.there) load_piece<E>((const T*)e.residual + (size_t)(m + q.row) * p.N + n + q.col, next[t]);
+        }
+      };
+      if (e.residual && strips > 0) fetch(0);
+#pragma unroll
+      for (int i = 0; i < IM; ++i) {
+        if (i >= strips) break;
+        const int m = m0 + wm * TM + 16 * i;
+        to_strip(i);
+        float res[S::kTurns][E];
+#pragma unroll
+        for (int t = 0; t < S::kTurns; ++t)
+#pragma unroll
+          for (int x = 0; x < E; ++x) res[t][x] = next[t][x];
+        if (e.residual && i + 1 < strips) fetch(i + 1);
+#pragma unroll
+        for (int t = 0; t < S::kTurns; ++t) {
+          const S q(t, lane, m, n, p.M, p.N);
+          if (!q.there) continue;
+          float v[E];
+          load_piece<E>(strip + q.row * S::kLd + q.col, v);
+          finish<T, E>(e, key, v, res[t], n + q.col, (size_t)(m + q.row) * p.N + n + q.col);
+        }
+      }
+    };
+    if (p.N % kPiece<T> == 0 && (((uintptr_t)e.out | (uintptr_t)e.pre | (uintptr_t)e.bias | (uintptr_t)e.residual) & 15) == 0)
+      run(std::integral_constant<int, kPiece<T>>());
+    else
+      run(std::integral_constant<int, 1>());
   }
 }
 
-// out[i] = alpha * (part[0][i] + part[1][i] + ...), rows of N in part_ld; the last workgroups: bias likewise
+// Forward products of few rows and columns: 16 x 16 values of c a workgroup, the waves share k between them, operands straight from
+// memory into registers.  A tile of 64 x 64 would leave most of the chip without work and walk k alone, one round trip to memory per
+// slice: 64 rows, 2304 -> 768, 27.6 us with tiles of 128 x 128.
+constexpr int kSlim = 16, kSlimWaves = 8;
 template <typename T>
-__global__ __launch_bounds__(256) void linear_join_kernel(GradEpilogue e, int M, int N, int splits, int bias_blocks) {
+__global__ __launch_bounds__(kSlimWaves* kWave) void linear_slim_kernel(Product p, Epilogue e) {
+  __shared__ __align__(16) float parts[kSlimWaves][kSlim * kSlim];
+  constexpr int kStep = kSlice<T> / 2;
+  const int mt = blockIdx.x / p.tiles_n, nt = blockIdx.x - mt * p.tiles_n;
+  const int lane = threadIdx.x & (kWave - 1), r = lane & 15, g = lane >> 4, wave = threadIdx.x / kWave;
+  // (rows beyond the last repeat it: their values go nowhere)
+  const char* a = (const char*)p.a.p + (size_t)min(mt * kSlim + r, p.M - 1) * p.a.ld;
+  const char* b = (const char*)p.b.p + (size_t)min(nt * kSlim + r, p.N - 1) * p.b.ld;
+  const int begin = min(p.K, wave * p.split_slices * kStep), end = min(p.K, begin + p.split_slices * kStep);
+  f32x4 c = {};
+  constexpr int kAhead = 6;  // steps on their way at a time
+  for (int k0 = begin; k0 < end; k0 += kAhead * kStep) {
+    Frag<T> fa[kAhead], fb[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const int k = k0 + i * kStep + g * kPiece<T>;
+      fa[i].u4 = fb[i].u4 = make_uint4(0u, 0u, 0u, 0u);
+      if (k < end) {  // (lines are whole pieces)
+        fa[i].u4 = *reinterpret_cast<const uint4*>(a + (size_t)k * sizeof(T));
+        fb[i].u4 = *reinterpret_cast<const uint4*>(b + (size_t)k * sizeof(T));
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i)
+#pragma unroll
+      for (int h = 0; h < kStepParts<T>; ++h) c = multiply(fb[i], fa[i], c, h);
+  }
+  *reinterpret_cast<f32x4*>(&parts[wave][r * kSlim + 4 * g]) = c;
+  __syncthreads();
+  if (threadIdx.x >= kSlim * kSlim) return;
+  float v[1] = {0.f};
+#pragma unroll
+  for (int w = 0; w < kSlimWaves; ++w) v[0] += parts[w][threadIdx.x];
+  const int m = mt * kSlim + threadIdx.x / kSlim, n = nt * kSlim + threadIdx.x % kSlim;
+  if (m >= p.M || n >= p.N) return;
+  const size_t at = (size_t)m * p.N + n;
+  RngKey key = {};
+  if (e.d.rng) key = rng_key(e.d.rng);
+  float res[1] = {0.f};
+  if (e.residual) load_piece<1>((const T*)e.residual + at, res);
+  finish<T, 1>(e, key, v, res, n, at);
+}
+
+// out[i] = alpha * (part[0][i] + part[1][i] + ...), rows of N in part_ld, LANES threads a piece of four; the last workgroups: bias
+// likewise.  (A thread that adds all parts of its piece waits for them one after another where there are many: 94 parts of 301 x 100 took
+// 27 us.)
+template <typename T, int LANES>
+__global__ __launch_bounds__(256) void linear_join_kernel(GradEpilogue e, int M, int N, int splits, float alpha, int bias_blocks) {
+  constexpr int kPieces = 256 / LANES;
+  __shared__ float4 sums[LANES > 1 ? 256 : 1];
   const int blocks = gridDim.x - bias_blocks;
-  if ((int)blockIdx.x >= blocks) {
-    const int m = (blockIdx.x - blocks) * 256 + threadIdx.x;
-    if (m >= M) return;
+  if ((int)blockIdx.x >= blocks) {  // 16 values a workgroup, 16 threads each
+    const int m = (blockIdx.x - blocks) * 16 + (threadIdx.x & 15), run = threadIdx.x >> 4;
     const float* part = e.part + (size_t)splits * M * e.part_ld;
     float s = 0.f;
-    for (int k = 0; k < splits; ++k) s += part[(size_t)k * M + m];
-    Elem<T>::store((T*)e.bias + m, s * e.alpha);
+    if (m < M)
+      for (int k = run; k < splits; k += 16) s += part[(size_t)k * M + m];
+    __shared__ float all[16][17];
+    all[run][threadIdx.x & 15] = s;
+    __syncthreads();
+    if (run != 0 || m >= M) return;
+    s = 0.f;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) s += all[k][threadIdx.x];
+    Elem<T>::store((T*)e.bias + m, s * alpha);
     return;
   }
   const size_t all = (size_t)M * e.part_ld;
-  for (size_t i = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4; i < all; i += (size_t)blocks * 1024) {
+  const int run = threadIdx.x / kPieces;
+  for (size_t first = (size_t)blockIdx.x * kPieces * 4; first < all; first += (size_t)blocks * kPieces * 4) {
+    const size_t i = first + threadIdx.x % kPieces * 4;
     float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int k = 0; k < splits; ++k) {
-      const float4 v = *reinterpret_cast<const float4*>(e.part + k * all + i);
-      s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+    if (i < all) {
+#pragma unroll 4
+      for (int k = run; k < splits; k += LANES) {
+        const float4 v = *reinterpret_cast<const float4*>(e.part + k * all + i);
+        s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+      }
     }
+    if constexpr (LANES > 1) {
+      __syncthreads();
+      sums[threadIdx.x] = s;
+      __syncthreads();
+      if (run != 0) continue;
+#pragma unroll
+      for (int k = 1; k < LANES; ++k) {
+        const float4 v = sums[k * kPieces + threadIdx.x];
+        s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+      }
+    }
+    if (i >= all) continue;
     const size_t m = i / (unsigned)e.part_ld;
     const int n = (int)(i - m * e.part_ld);
     T* out = (T*)e.out + m * N + n;
-    const float v[4] = {s.x * e.alpha, s.y * e.alpha, s.z * e.alpha, s.w * e.alpha};
+    const float v[4] = {s.x * alpha, s.y * alpha, s.z * alpha, s.w * alpha};
 #pragma unroll
     for (int j = 0; j < 4; ++j)
       if (n + j < N) Elem<T>::store(out + j, v[j]);
@@ -428,8 +556,6 @@ __global__ __launch_bounds__(256) void linear_dz_kernel(const T* __restrict__ do
   }
 }
 
-int cdiv(long long a, long long b) { return (int)((a + b - 1) / b); }
-
 // what a lane may bring at a time, by where an operand's lines start
 int line_bytes(const Operand& o) {
   const uintptr_t all = reinterpret_cast<uintptr_t>(o.p) | o.ld;
@@ -455,23 +581,85 @@ hipError_t run_tiles(Product p, const Ep& e, hipStream_t stream) {
   return hipGetLastError();
 }
 
+template <typename T>
+hipError_t run_slim(Product p, const Epilogue& e, hipStream_t stream) {
+  p.tiles_n = cdiv(p.N, kSlim);
+  p.split_slices = cdiv(cdiv(p.K, kSlice<T> / 2), kSlimWaves);  // (steps of a wave)
+  AFFMAE_LAUNCH("linear_slim_kernel", stream, linear_slim_kernel<T>, dim3(cdiv(p.M, kSlim) * p.tiles_n), dim3(kSlimWaves * kWave), 0, stream, p, e);
+  return hipGetLastError();
+}
+
+// What a workgroup's tile costs, in us: a slice while a CU is full of such workgroups (per workgroup), a slice of one that has its CU
+// to itself, and everything but the slices.  Measured on products of 16384 to 32768 rows, 256 to 2304 deep; large tiles read less of LDS
+// per product (128 x 192 reaches 1.0 to 1.1 PFLOP/s in bf16), small ones fill the chip and hide their ends behind each other.
+struct Shape {
+  int bm, bn, resident;
+  float slice, alone, end;
+};
+enum { k64x64, k128x64, k128x128, k128x192, kSlimTile };
+constexpr Shape kShapes16[] = {{64, 64, 4, .183f, .55f, .57f}, {128, 64, 3, .283f, .58f, 1.2f}, {128, 128, 2, .546f, .85f, 2.2f}, {128, 192, 2, .70f, 1.1f, 3.7f}, {16, 16, 4, .112f, .11f, .4f}};
+constexpr Shape kShapes32[] = {{64, 64, 4, .66f, .78f, .4f}, {128, 64, 3, 1.17f, 1.22f, 1.4f}, {}, {}, {16, 16, 4, .116f, .11f, .4f}};
+constexpr int kCus = 256;
+
+struct Plan {
+  int shape, splits;
+};
+float plan_cost(const Shape& h, long long M, long long N, int slices, int splits) {
+  const long long work = (long long)cdiv(M, h.bm) * cdiv(N, h.bn) * splits, turn = (long long)kCus * h.resident;
+  const int deep = cdiv(slices, splits), rest = cdiv(work % turn, kCus);
+  float t = (float)(work / turn) * ((float)deep * std::max(h.alone, h.resident * h.slice) + h.resident * h.end);
+  if (rest) t += (float)deep * std::max(h.alone, rest * h.slice) + rest * h.end;
+  // parts are written and read once (4 TB/s), by one more launch
+  if (splits > 1) t += 4.f + (float)splits * (float)M * (float)N * 8.f / 4e6f;
+  return t;
+}
+// The cheapest tile; gradients also share a tile's k between workgroups, as many as make one or two full turns of the chip.
+Plan plan_product(long long M, long long N, int K, int el, int line, bool forward) {
+  const Shape* shapes = el == 2 ? kShapes16 : kShapes32;
+  const int slices = cdiv(K, kSliceBytes / el);
+  Plan best = {k64x64, 1};
+  float least = 3e38f;
+  for (int i = 0; i <= kSlimTile; ++i) {
+    const Shape& h = shapes[i];
+    if (!h.bm || (i > k128x64 && line < 16) || (i == kSlimTile && !forward)) continue;
+    const long long tiles = (long long)cdiv(M, h.bm) * cdiv(N, h.bn);
+    if (i == kSlimTile && tiles > 1 << 20) continue;
+    for (int turns = 0; turns <= 2; ++turns) {
+      if (turns && forward) break;
+      const int most = turns ? (int)std::min<long long>((long long)kCus * h.resident * turns / tiles, slices / 2) : 1;
+      if (most < 1) continue;
+      const int splits = cdiv(slices, cdiv(slices, most));  // (none without slices)
+      const float t = plan_cost(h, M, N, slices, splits);
+      if (t < least) {
+        least = t;
+        best = {i, splits};
+      }
+    }
+  }
+  return best;
+}
+
 template <typename T, bool AA, bool BA, typename Ep>
-hipError_t run_product(const Product& p, const Ep& e, hipStream_t stream) {
+hipError_t run_product(Product p, int shape, const Ep& e, hipStream_t stream) {
   const int w = std::min(line_bytes(p.a), line_bytes(p.b));
-  if (w == 16) return run_tiles<T, AA, BA, 16, 128, 128, 2, 2>(p, e, stream);
-  if (w == 4) return run_tiles<T, AA, BA, 4, 128, 128, 2, 2>(p, e, stream);
-  if constexpr (sizeof(T) == 2) return run_tiles<T, AA, BA, 2, 128, 128, 2, 2>(p, e, stream);
+  if (w == 16) {
+    if constexpr (std::is_same_v<Ep, Epilogue>) {
+      if (shape == kSlimTile) return run_slim<T>(p, e, stream);
+    }
+    if constexpr (sizeof(T) == 2) {
+      if (shape == k128x192) return run_tiles<T, AA, BA, 16, 128, 192, 2, 2>(p, e, stream);
+      if (shape == k128x128) return run_tiles<T, AA, BA, 16, 128, 128, 2, 2>(p, e, stream);
+    }
+    if (shape == k128x64) return run_tiles<T, AA, BA, 16, 128, 64, 2, 2>(p, e, stream);
+    return run_tiles<T, AA, BA, 16, 64, 64, 2, 2>(p, e, stream);
+  }
+  if (sizeof(T) == 4 || w == 4)
+    return shape == k128x64 ? run_tiles<T, AA, BA, 4, 128, 64, 2, 2>(p, e, stream) : run_tiles<T, AA, BA, 4, 64, 64, 2, 2>(p, e, stream);
+  if constexpr (sizeof(T) == 2)
+    return shape == k128x64 ? run_tiles<T, AA, BA, 2, 128, 64, 2, 2>(p, e, stream) : run_tiles<T, AA, BA, 2, 64, 64, 2, 2>(p, e, stream);
   return hipErrorInvalidValue;
 }
 
-// Workgroups that share a tile's k, where the tiles alone would leave the chip half empty: at least four slices each.
-int splits_of(long long M, long long N, long long K, int slice) {
-  const long long tiles = (long long)cdiv(M, 128) * cdiv(N, 128);
-  const long long slices = cdiv(K, slice);
-  const long long want = 512 / tiles;
-  const int most = (int)std::max(1ll, std::min(want, slices / 4));
-  return cdiv(slices, cdiv(slices, most));  // (no split without slices)
-}
 int part_ld(int N) { return cdiv(N, 4) * 4; }
 size_t part_bytes(int splits, int M, int N, bool bias) {
   return splits > 1 ? ((size_t)splits * M * part_ld(N) + (bias ? (size_t)splits * M : 0)) * sizeof(float) : 0;
@@ -480,15 +668,25 @@ size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 
 template <typename T>
 hipError_t gradient(bool dx, Operand a, Operand b, int M, int N, int K, void* out, void* bias, float alpha, float* part, hipStream_t stream) {
+  const Plan plan = plan_product(M, N, K, sizeof(T), std::min(line_bytes(a), line_bytes(b)), false);
   Product p = {};
-  p.a = a; p.b = b; p.M = M; p.N = N; p.K = K;
-  p.splits = splits_of(M, N, K, kSlice<T>);
-  const GradEpilogue e = {out, bias, p.splits > 1 ? part : nullptr, part_ld(N), alpha};
-  hipError_t rc = dx ? run_product<T, true, false>(p, e, stream) : run_product<T, false, false>(p, e, stream);
+  p.a = a; p.b = b; p.M = M; p.N = N; p.K = K; p.splits = plan.splits;
+  const GradEpilogue e = {out, bias, p.splits > 1 ? part : nullptr, part_ld(N), p.splits > 1 ? 1.f : alpha};
+  hipError_t rc = dx ? run_product<T, true, false>(p, plan.shape, e, stream) : run_product<T, false, false>(p, plan.shape, e, stream);
   if (rc != hipSuccess || p.splits == 1) return rc;
-  const int bias_blocks = bias ? cdiv(M, 256) : 0;
-  const int blocks = (int)std::min<long long>(cdiv((long long)M * part_ld(N), 1024), 4096);
-  AFFMAE_LAUNCH("linear_join_kernel", stream, linear_join_kernel<T>, dim3(blocks + bias_blocks), dim3(256), 0, stream, e, M, N, p.splits, bias_blocks);
+  const int bias_blocks = bias ? cdiv(M, 16) : 0;
+  const long long pieces = (long long)M * (part_ld(N) / 4);
+  const auto join = [&](auto lanes) {
+    constexpr int L = decltype(lanes)::value;
+    const int blocks = (int)std::min<long long>(cdiv(pieces * L, 256), 4096);
+    AFFMAE_LAUNCH("linear_join_kernel", stream, (linear_join_kernel<T, L>), dim3(blocks + bias_blocks), dim3(256), 0, stream, e, M, N, p.splits, alpha, bias_blocks);
+  };
+  if (pieces <= 8192 && p.splits > 16)
+    join(std::integral_constant<int, 16>());
+  else if (pieces <= 32768 && p.splits > 4)
+    join(std::integral_constant<int, 4>());
+  else
+    join(std::integral_constant<int, 1>());
   return hipGetLastError();
 }
 
@@ -500,7 +698,8 @@ hipError_t fwd(const LinearArgs& a, hipStream_t stream) {
   p.b = {a.weight, ld, (long long)a.Cout * ld};
   p.M = a.rows; p.N = a.Cout; p.K = a.Cin; p.splits = 1;
   const Epilogue e = {a.bias, a.residual, a.out, a.pre_out, a.act, make_dropout(a.p, a.rng)};
-  return run_product<T, true, true>(p, e, stream);
+  const Plan plan = plan_product(p.M, p.N, p.K, sizeof(T), std::min(line_bytes(p.a), line_bytes(p.b)), true);
+  return run_product<T, true, true>(p, plan.shape, e, stream);
 }
 
 int dz_ld(int Cout, int el) { return cdiv(Cout * el, 16) * 16 / el; }
@@ -543,10 +742,14 @@ hipError_t bwd(const LinearArgs& a, hipStream_t stream) {
 }  // namespace
 
 size_t linear_bwd_workspace_bytes(int rows, int Cin, int Cout, int act, bool drops, int dtype, bool want_dx, bool want_dweight) {
-  const int el = dtype == 1 ? 2 : 4, slice = kSliceBytes / el;
+  const int el = dtype == 1 ? 2 : 4;
   const size_t dz = act != kActNone || drops ? up256((size_t)rows * dz_ld(Cout, el) * el) : 0;
-  const size_t dx = want_dx ? part_bytes(splits_of(rows, Cin, Cout, slice), rows, Cin, false) : 0;
-  const size_t dw = want_dweight ? part_bytes(splits_of(Cout, Cin, rows, slice), Cout, Cin, true) : 0;
+  // (which tile a call takes, hence how it splits, depends on its tensors' alignment)
+  const auto parts = [&](int M, int N, int K, bool bias) {
+    return std::max(part_bytes(plan_product(M, N, K, el, 16, false).splits, M, N, bias), part_bytes(plan_product(M, N, K, el, 2, false).splits, M, N, bias));
+  };
+  const size_t dx = want_dx ? parts(rows, Cin, Cout, false) : 0;
+  const size_t dw = want_dweight ? parts(Cout, Cin, rows, true) : 0;
   return dz + std::max(dx, dw);  // (the parts of one are joined before the other's are written)
 }
 hipError_t launch_linear_fwd(const LinearArgs& a, hipStream_t stream) { return a.dtype == 1 ? fwd<bf16_t>(a, stream) : fwd<float>(a, stream); }
