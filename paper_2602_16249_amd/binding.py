@@ -686,7 +686,7 @@ def affmae_linear_fwd(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torc
     if pre is not None:
         _dev(pre, "pre", x.dtype, shape)
     elif want_pre:
-        pre = torch.empty(shape, dtype=x.dtype, device=x.device)
+        pre = torch.empty_like(out)
     rc = lib.affmae_linear_fwd(_ptr(x), _ptr(weight), _ptr(bias), _ptr(residual), x.numel() // max(Cin, 1), Cin, Cout,
                                _act_code(act), float(p), _rng_ptr(rng, p), code, _ptr(out), _ptr(pre), _stream())
     if rc != 0:

@@ -78,14 +78,15 @@ __device__ __forceinline__ RngKey rng_key(const int64_t* rng) {
 // Philox 4x32 with ten rounds (Salmon, Moraes, Dror, Shaw, "Parallel random numbers: as easy as 1, 2, 3", 2011): key = the seed,
 // counter = (block, call number).  A pure function of the element's place: forward and backward work it out again instead of
 // storing a mask, and any kernel may take any part of a tensor.
+__device__ __forceinline__ uint32_t xor3(uint32_t a, uint32_t b, uint32_t c) { return __builtin_amdgcn_bitop3_b32(a, b, c, 0x96); }
 __device__ __forceinline__ uint4 rng_words(const RngKey& key, uint64_t block) {
   uint32_t c0 = (uint32_t)block, c1 = (uint32_t)(block >> 32), c2 = key.c2, c3 = key.c3, k0 = key.k0, k1 = key.k1;
 #pragma unroll
   for (int r = 0; r < 10; ++r) {
     const uint64_t a = (uint64_t)c0 * 0xD2511F53u, b = (uint64_t)c2 * 0xCD9E8D57u;
-    c0 = (uint32_t)(b >> 32) ^ c1 ^ k0;
+    c0 = xor3((uint32_t)(b >> 32), c1, k0);
     c1 = (uint32_t)b;
-    c2 = (uint32_t)(a >> 32) ^ c3 ^ k1;
+    c2 = xor3((uint32_t)(a >> 32), c3, k1);
     c3 = (uint32_t)a;
     k0 += 0x9E3779B9u;
     k1 += 0xBB67AE85u;
@@ -100,7 +101,10 @@ __device__ __forceinline__ uint32_t rng_word(const RngKey& key, uint64_t element
 // v[0..E) are elements first .. first + E - 1; first and E are multiples of 4, or E is 1.
 template <int E>
 __device__ __forceinline__ void drop(float (&v)[E], const Dropout& d, const RngKey& key, uint64_t first) {
-  if constexpr (E % 4 == 0) {
+  if constexpr (E == 1) {
+    v[0] = rng_word(key, first) >= d.least ? v[0] * d.factor : 0.f;
+  } else {
+    static_assert(E % 4 == 0);
 #pragma unroll
     for (int q = 0; q < E / 4; ++q) {
       const uint4 w = rng_words(key, (first >> 2) + q);
@@ -109,9 +113,6 @@ __device__ __forceinline__ void drop(float (&v)[E], const Dropout& d, const RngK
       v[4 * q + 2] = w.z >= d.least ? v[4 * q + 2] * d.factor : 0.f;
       v[4 * q + 3] = w.w >= d.least ? v[4 * q + 3] * d.factor : 0.f;
     }
-  } else {
-    static_assert(E == 1);
-    v[0] = rng_word(key, first) >= d.least ? v[0] * d.factor : 0.f;
   }
 }
 
@@ -158,6 +159,27 @@ __device__ __forceinline__ void store_piece(bf16_t* p, const float (&v)[E]) {
     for (int t = 0; t < E / 8; ++t)
       reinterpret_cast<uint4*>(p)[t] = make_uint4(pack2_bf16(v[8 * t], v[8 * t + 1]), pack2_bf16(v[8 * t + 2], v[8 * t + 3]),
                                                   pack2_bf16(v[8 * t + 4], v[8 * t + 5]), pack2_bf16(v[8 * t + 6], v[8 * t + 7]));
+  }
+}
+
+// The first n of a piece's values, whole and aligned (`whole`) or one by one.
+template <int E, typename T>
+__device__ __forceinline__ void load_some(const T* p, int n, bool whole, float (&v)[E]) {
+  if (whole && n >= E) {
+    load_piece<E>(p, v);
+  } else {
+#pragma unroll
+    for (int e = 0; e < E; ++e) v[e] = e < n ? Elem<T>::load(p + e) : 0.f;
+  }
+}
+template <int E, typename T>
+__device__ __forceinline__ void store_some(T* p, int n, bool whole, const float (&v)[E]) {
+  if (whole && n >= E) {
+    store_piece<E>(p, v);
+  } else {
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+      if (e < n) Elem<T>::store(p + e, v[e]);
   }
 }
 

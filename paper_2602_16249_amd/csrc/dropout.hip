@@ -13,34 +13,33 @@ namespace {
 constexpr int kThreads = 256;
 constexpr long long kMaxBlocks = 1ll << 23;  // (the runtime counts the threads of a launch in 32 bits; further elements in further turns)
 
-template <typename T, int E>
-__global__ __launch_bounds__(kThreads) void dropout_kernel(const T* x, const T* residual, long long n, Dropout d, T* out) {
+// A thread takes a piece of 16 bytes, the generator's words for it in one or two blocks; in tensors that do not start on 16 bytes
+// (`whole` false) and in the last piece, value by value.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void dropout_kernel(const T* x, const T* residual, long long n, bool whole, Dropout d, T* out) {
+  constexpr int E = kPiece<T>;
   RngKey key = {};
   if (d.rng) key = rng_key(d.rng);
   for (long long i = ((long long)blockIdx.x * kThreads + threadIdx.x) * E; i < n; i += (long long)gridDim.x * kThreads * E) {
-    float v[E];
-    load_piece<E>(x + i, v);
+    const int some = (int)std::min<long long>(n - i, E);
+    float v[E], r[E];
+    load_some<E>(x + i, some, whole, v);
+    if (residual) load_some<E>(residual + i, some, whole, r);
     if (d.rng) drop<E>(v, d, key, (uint64_t)i);
     if (residual) {
-      float r[E];
-      load_piece<E>(residual + i, r);
 #pragma unroll
       for (int e = 0; e < E; ++e) v[e] += r[e];
     }
-    store_piece<E>(out + i, v);
+    store_some<E>(out + i, some, whole, v);
   }
 }
 
 template <typename T>
 hipError_t launch(const void* x, const void* residual, long long n, const Dropout& d, void* out, hipStream_t stream) {
-  constexpr int E = kPiece<T>;
-  const bool whole = n % E == 0 && aligned16(x) && aligned16(residual) && aligned16(out);
-  const long long per = (long long)kThreads * (whole ? E : 1);
+  const bool whole = aligned16(x) && aligned16(residual) && aligned16(out);
+  const long long per = (long long)kThreads * kPiece<T>;
   const dim3 grid((unsigned)std::min((n + per - 1) / per, kMaxBlocks));
-  if (whole)
-    AFFMAE_LAUNCH("dropout_kernel", stream, (dropout_kernel<T, E>), grid, dim3(kThreads), 0, stream, (const T*)x, (const T*)residual, n, d, (T*)out);
-  else
-    AFFMAE_LAUNCH("dropout_kernel", stream, (dropout_kernel<T, 1>), grid, dim3(kThreads), 0, stream, (const T*)x, (const T*)residual, n, d, (T*)out);
+  AFFMAE_LAUNCH("dropout_kernel", stream, dropout_kernel<T>, grid, dim3(kThreads), 0, stream, (const T*)x, (const T*)residual, n, whole, d, (T*)out);
   return hipGetLastError();
 }
 

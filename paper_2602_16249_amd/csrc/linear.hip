@@ -524,34 +524,46 @@ __global__ __launch_bounds__(256) void linear_join_kernel(GradEpilogue e, int M,
   }
 }
 
-// dz / factor = (kept? dout : 0) act'(pre), rows of C in lines of `ld` values whose rest is 0.  E > 1: C and ld are multiples of E.
-template <typename T, int E>
-__global__ __launch_bounds__(256) void linear_dz_kernel(const T* __restrict__ dout, const T* __restrict__ pre, int rows, int C, int ld, uint32_t ld_magic, int act,
+// dz / factor = (kept? dout : 0) act'(pre), rows of C in lines of `ld` values whose rest is 0.  A thread takes a piece of dout in the
+// order of memory, whatever rows it is part of, so that odd rows cost neither wide loads nor blocks of the generator.  EVEN: C is a
+// multiple of a piece, hence ld.
+template <typename T, bool EVEN>
+__global__ __launch_bounds__(256) void linear_dz_kernel(const T* __restrict__ dout, const T* __restrict__ pre, int rows, int C, int ld, uint32_t magic, bool whole, int act,
                                                         Dropout d, T* __restrict__ dz) {
+  constexpr int E = kPiece<T>;
   RngKey key = {};
   if (d.rng) key = rng_key(d.rng);
   d.factor = 1.f;
-  const int line = ld / E;
-  // 256 rows at a time: places in them are 28-bit numbers
-  for (int row0 = blockIdx.y * 256; row0 < rows; row0 += gridDim.y * 256) {
-    const int n = min(256, rows - row0) * line;
-    for (int i = blockIdx.x * 256 + threadIdx.x; i < n; i += gridDim.x * 256) {
-      const int row = exact_div(i, line, ld_magic), col = (i - row * line) * E;
-      const size_t at = (size_t)(row0 + row) * C + col;
-      float v[E];
-      if (E > 1 || col < C) {
-        load_piece<E>(dout + at, v);
-        if (d.rng) drop<E>(v, d, key, at);
-        if (pre) {
-          float z[E];
-          load_piece<E>(pre + at, z);
+  const long long all = (long long)rows * C;
+  for (long long first = (long long)blockIdx.x * 256 * E; first < all; first += (long long)gridDim.x * 256 * E) {
+    const long long i = first + threadIdx.x * E;
+    const int n = (int)std::min<long long>(all - i, E);
+    if (n <= 0) break;
+    float v[E], z[E];
+    load_some<E>(dout + i, n, whole, v);
+    if (pre) load_some<E>(pre + i, n, whole, z);
+    if (d.rng) drop<E>(v, d, key, (uint64_t)i);
+    if (pre) {
 #pragma unroll
-          for (int j = 0; j < E; ++j) v[j] *= act_slope(z[j], act);
+      for (int e = 0; e < E; ++e) v[e] *= act_slope(z[e], act);
+    }
+    if constexpr (EVEN) {
+      store_piece<E>(dz + i, v);
+    } else {
+      const long long row0 = first / C;  // (of the workgroup: one long division, short ones from there)
+      const int from = (int)(first - row0 * C) + (int)threadIdx.x * E;
+      int row = exact_div(from, C, magic), col = from - row * C;
+      T* to = dz + (size_t)(row0 + row) * ld;
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        if (e >= n) break;
+        Elem<T>::store(to + col, v[e]);
+        if (++col == C) {
+          for (int x = C; x < ld; ++x) Elem<T>::store(to + x, 0.f);
+          to += ld;
+          col = 0;
         }
-      } else {
-        v[0] = 0.f;
       }
-      store_piece<E>(dz + (size_t)(row0 + row) * ld + col, v);
     }
   }
 }
@@ -591,24 +603,27 @@ hipError_t run_slim(Product p, const Epilogue& e, hipStream_t stream) {
 
 // What a workgroup's tile costs, in us: a slice while a CU is full of such workgroups (per workgroup), a slice of one that has its CU
 // to itself, and everything but the slices.  Measured on products of 16384 to 32768 rows, 256 to 2304 deep; large tiles read less of LDS
-// per product (128 x 192 reaches 1.0 to 1.1 PFLOP/s in bf16), small ones fill the chip and hide their ends behind each other.
+// per product (128 x 192 reaches 1.0 to 1.1 PFLOP/s in bf16), small ones fill the chip and hide their ends behind each other; `epilogue`:
+// what the forward's longer end takes beyond that.
 struct Shape {
   int bm, bn, resident;
-  float slice, alone, end;
+  float slice, alone, end, epilogue;
 };
 enum { k64x64, k128x64, k128x128, k128x192, kSlimTile };
-constexpr Shape kShapes16[] = {{64, 64, 4, .183f, .55f, .57f}, {128, 64, 3, .283f, .58f, 1.2f}, {128, 128, 2, .546f, .85f, 2.2f}, {128, 192, 2, .70f, 1.1f, 3.7f}, {16, 16, 4, .112f, .11f, .4f}};
-constexpr Shape kShapes32[] = {{64, 64, 4, .66f, .78f, .4f}, {128, 64, 3, 1.17f, 1.22f, 1.4f}, {}, {}, {16, 16, 4, .116f, .11f, .4f}};
+constexpr Shape kShapes16[] = {{64, 64, 4, .183f, .55f, .57f, 0.f}, {128, 64, 3, .283f, .58f, 1.2f, 0.f}, {128, 128, 2, .546f, .85f, 2.2f, .6f},
+                               {128, 192, 2, .70f, 1.1f, 3.7f, .6f}, {16, 16, 4, .112f, .11f, .4f, 0.f}};
+constexpr Shape kShapes32[] = {{64, 64, 4, .66f, .78f, .4f, 0.f}, {128, 64, 3, 1.17f, 1.22f, 1.4f, 0.f}, {}, {}, {16, 16, 4, .116f, .11f, .4f, 0.f}};
 constexpr int kCus = 256;
 
 struct Plan {
   int shape, splits;
 };
-float plan_cost(const Shape& h, long long M, long long N, int slices, int splits) {
+float plan_cost(const Shape& h, long long M, long long N, int slices, int splits, bool forward) {
+  const float end = h.end + (forward ? h.epilogue : 0.f);
   const long long work = (long long)cdiv(M, h.bm) * cdiv(N, h.bn) * splits, turn = (long long)kCus * h.resident;
   const int deep = cdiv(slices, splits), rest = cdiv(work % turn, kCus);
-  float t = (float)(work / turn) * ((float)deep * std::max(h.alone, h.resident * h.slice) + h.resident * h.end);
-  if (rest) t += (float)deep * std::max(h.alone, rest * h.slice) + rest * h.end;
+  float t = (float)(work / turn) * ((float)deep * std::max(h.alone, h.resident * h.slice) + h.resident * end);
+  if (rest) t += (float)deep * std::max(h.alone, rest * h.slice) + rest * end;
   // parts are written and read once (4 TB/s), by one more launch
   if (splits > 1) t += 4.f + (float)splits * (float)M * (float)N * 8.f / 4e6f;
   return t;
@@ -629,7 +644,7 @@ Plan plan_product(long long M, long long N, int K, int el, int line, bool forwar
       const int most = turns ? (int)std::min<long long>((long long)kCus * h.resident * turns / tiles, slices / 2) : 1;
       if (most < 1) continue;
       const int splits = cdiv(slices, cdiv(slices, most));  // (none without slices)
-      const float t = plan_cost(h, M, N, slices, splits);
+      const float t = plan_cost(h, M, N, slices, splits, forward);
       if (t < least) {
         least = t;
         best = {i, splits};
@@ -714,16 +729,10 @@ hipError_t bwd(const LinearArgs& a, hipStream_t stream) {
     const int ld = dz_ld(a.Cout, sizeof(T));
     const void* pre = a.act != kActNone ? a.pre : nullptr;
     constexpr int E = kPiece<T>;
-    const bool whole = a.Cout % E == 0 && aligned16(a.dout) && aligned16(pre);
-    const int line = whole ? ld / E : ld;
-    const dim3 grid(cdiv(256ll * line, 256 * 4), std::min(cdiv(a.rows, 256), 32768));
-    const auto run = [&](auto kernel) {
-      AFFMAE_LAUNCH("linear_dz_kernel", stream, kernel, grid, dim3(256), 0, stream, (const T*)a.dout, (const T*)pre, a.rows, a.Cout, ld, div_magic(line), a.act, d, (T*)ws);
-    };
-    if (whole)
-      run(linear_dz_kernel<T, E>);
-    else
-      run(linear_dz_kernel<T, 1>);
+    const auto kernel = a.Cout % E == 0 ? linear_dz_kernel<T, true> : linear_dz_kernel<T, false>;
+    const dim3 grid((unsigned)std::min<long long>(cdiv((long long)a.rows * a.Cout, 256 * E), kMaxBlocks));
+    AFFMAE_LAUNCH("linear_dz_kernel", stream, kernel, grid, dim3(256), 0, stream, (const T*)a.dout, (const T*)pre, a.rows, a.Cout, ld, div_magic(a.Cout),
+                  aligned16(a.dout) && aligned16(pre), a.act, d, (T*)ws);
     const hipError_t rc = hipGetLastError();
     if (rc != hipSuccess) return rc;
     dz = {ws, (uint32_t)(ld * sizeof(T)), (long long)a.rows * ld * (long long)sizeof(T)};

@@ -206,22 +206,33 @@ __global__ __launch_bounds__(kThreads) void norm_rows_bwd_kernel(const T* __rest
     }
 }
 
-// out[which][c] = sum over i < n of part[i][which][c]: 32 channels a workgroup, 32 runs of parts beside each other
-__global__ __launch_bounds__(1024) void norm_channel_sums_kernel(const float* __restrict__ part, int n, int C, float* __restrict__ dgamma, float* __restrict__ dbeta) {
-  __shared__ float sums[32][33];
-  const int c = blockIdx.x * 32 + (threadIdx.x & 31), run = threadIdx.x >> 5;
-  const float* from = part + (size_t)blockIdx.y * C + std::min(c, C - 1);
-  float s = 0.f;
+// The sums over i < n of part[i][which][c], which = 0 into dgamma, 1 into dbeta: RUNS runs of parts beside each other, as many channels
+// a workgroup as that leaves threads; the i-th workgroup of channel_blocks(C).
+template <int THREADS, int RUNS>
+struct ChannelSums {
+  static constexpr int kChannels = THREADS / RUNS;
+  static int blocks(int C) { return 2 * cdiv(C, kChannels); }
+  static __device__ __forceinline__ void run(const float* __restrict__ part, int n, int C, int block, float* sums, float* __restrict__ dgamma, float* __restrict__ dbeta) {
+    const int which = block & 1, c = (block >> 1) * kChannels + (int)threadIdx.x % kChannels, run = threadIdx.x / kChannels;
+    const float* from = part + (size_t)which * C + std::min(c, C - 1);
+    float s = 0.f;
 #pragma unroll 8
-  for (int i = run; i < n; i += 32) s += from[(size_t)i * 2 * C];
-  sums[run][threadIdx.x & 31] = s;
-  __syncthreads();
-  if (run == 0 && c < C) {
-    float t = 0.f;
+    for (int i = run; i < n; i += RUNS) s += from[(size_t)i * 2 * C];
+    sums[threadIdx.x] = s;
+    __syncthreads();
+    if (run != 0 || c >= C) return;
+    s = 0.f;
 #pragma unroll
-    for (int k = 0; k < 32; ++k) t += sums[k][threadIdx.x];
-    (blockIdx.y ? dbeta : dgamma)[c] = t;
+    for (int k = 0; k < RUNS; ++k) s += sums[k * kChannels + threadIdx.x];
+    (which ? dbeta : dgamma)[c] = s;
   }
+};
+using RowSums = ChannelSums<1024, 32>;    // a launch of its own
+using GroupSums = ChannelSums<kThreads, 16>;  // beside the workgroups that write dx
+
+__global__ __launch_bounds__(1024) void norm_channel_sums_kernel(const float* __restrict__ part, int n, int C, float* __restrict__ dgamma, float* __restrict__ dbeta) {
+  __shared__ float sums[1024];
+  RowSums::run(part, n, C, blockIdx.x, sums, dgamma, dbeta);
 }
 
 // ---------------------------------------------------------------------------------------------------------------- groups
@@ -253,6 +264,8 @@ struct Groups {  // what the kernels take
   float2* group_part;   // [B][G][parts]: mean and M2, or the sums of dh and dh xhat
   float2* totals;       // [B][G]: these sums of the whole group, where a launch of its own adds them up
   float* channel_part;  // [B][slabs][2][C]
+  float *dgamma, *dbeta;
+  int sums;  // workgroups in front of the others that add up channel_part
 };
 
 // a thread's place: column of the block, its group in the block, first channel; the workgroup's tokens
@@ -299,8 +312,16 @@ struct Place {
   __device__ __forceinline__ int part(const Groups& a) const { return a.k.shares > 1 ? slab * a.k.shares + block % a.k.shares : slab; }
 };
 
-// per group of the block, the sums over its threads of v: result[q], read by all threads afterwards
-__device__ __forceinline__ void group_sums(const Groups& a, const Place& w, float v, float (&values)[kThreads], float (&result)[kThreads]) {
+__device__ __forceinline__ float wave_total(float v) { return wave_sum(v); }
+__device__ __forceinline__ float2 wave_total(float2 v) { return make_float2(wave_sum(v.x), wave_sum(v.y)); }
+__device__ __forceinline__ void add(float& s, float v) { s += v; }
+__device__ __forceinline__ void add(float2& s, float2 v) {
+  s.x += v.x;
+  s.y += v.y;
+}
+// per group of the block, the sums over its threads of v (a value or two): result[q], read by all threads afterwards
+template <typename V>
+__device__ __forceinline__ void group_sums(const Groups& a, const Place& w, V v, V (&values)[kThreads], V (&result)[kThreads]) {
   const Cut& k = a.k;
   __syncthreads();
   values[threadIdx.x] = v;
@@ -308,12 +329,12 @@ __device__ __forceinline__ void group_sums(const Groups& a, const Place& w, floa
   const int lane = threadIdx.x & (kWave - 1), n = k.lanes * w.group_cols;
   const uint32_t magic = k.shares > 1 ? 0u : k.group_magic;
   for (int q = threadIdx.x / kWave; q < w.groups; q += kWaves) {
-    float s = 0.f;
+    V s = {};
     for (int i = lane; i < n; i += kWave) {
       const int row = k.shares > 1 ? i / w.group_cols : exact_div(i, w.group_cols, magic);
-      s += values[row * k.block_cols + q * w.group_cols + i - row * w.group_cols];
+      add(s, values[row * k.block_cols + q * w.group_cols + i - row * w.group_cols]);
     }
-    s = wave_sum(s);
+    s = wave_total(s);
     if (lane == 0) result[q] = s;
   }
   __syncthreads();
@@ -483,8 +504,8 @@ __global__ __launch_bounds__(kThreads) void norm_apply_kernel(Groups a) {
 // per workgroup: the sums of dz xhat and dz of its channels, and of dh xhat and dh of its groups
 template <typename T, int E>
 __global__ __launch_bounds__(kThreads) void norm_bwd_sums_kernel(Groups a) {
-  __shared__ float values[kThreads], result[kThreads];
-  __shared__ float sums[kThreads * E];
+  __shared__ float2 values[kThreads], result[kThreads];
+  __shared__ float2 sums[kThreads * E];
   const Place w(a, a.first + blockIdx.x);
   const Cut& k = a.k;
   const size_t bg = (size_t)w.b * a.G + w.group;
@@ -513,37 +534,34 @@ __global__ __launch_bounds__(kThreads) void norm_bwd_sums_kernel(Groups a) {
       }
     }
   }
-  float s1 = 0.f, s2 = 0.f;
+  float2 s = make_float2(0.f, 0.f);
 #pragma unroll
   for (int e = 0; e < E; ++e) {
-    s1 = __builtin_fmaf(gm[e], db[e], s1);
-    s2 = __builtin_fmaf(gm[e], dg[e], s2);
+    s.x = __builtin_fmaf(gm[e], db[e], s.x);
+    s.y = __builtin_fmaf(gm[e], dg[e], s.y);
   }
-  group_sums(a, w, s1, values, result);
-  const float t1 = (int)threadIdx.x < w.groups ? result[threadIdx.x] : 0.f;
-  group_sums(a, w, s2, values, result);
-  if ((int)threadIdx.x < w.groups) a.group_part[(bg + threadIdx.x) * k.parts() + w.part(a)] = make_float2(t1, result[threadIdx.x]);
+  group_sums(a, w, s, values, result);
+  if ((int)threadIdx.x < w.groups) a.group_part[(bg + threadIdx.x) * k.parts() + w.part(a)] = result[threadIdx.x];
   if (!a.channel_part) return;
   // (the block's first channel: w.c of a thread without a column)
   const int c0 = w.c - (w.active ? w.col : 0) * E;
-  for (int which = 0; which < 2; ++which) {
-    __syncthreads();
 #pragma unroll
-    for (int e = 0; e < E; ++e) sums[(w.lane_row * k.block_cols + w.col) * E + e] = which ? db[e] : dg[e];
-    __syncthreads();
-    float* to = a.channel_part + (((size_t)w.b * k.slabs + w.slab) * 2 + which) * a.C + c0;
-    for (int i = threadIdx.x; i < w.cols * E; i += kThreads) {
-      float s = 0.f;
-      for (int j = 0; j < k.lanes; ++j) s += sums[j * k.block_cols * E + i];
-      to[i] = s;
-    }
+  for (int e = 0; e < E; ++e) sums[threadIdx.x * E + e] = make_float2(dg[e], db[e]);
+  __syncthreads();
+  float* to = a.channel_part + ((size_t)w.b * k.slabs + w.slab) * 2 * a.C + c0;
+  for (int i = threadIdx.x; i < w.cols * E; i += kThreads) {
+    float2 t = make_float2(0.f, 0.f);
+    for (int j = 0; j < k.lanes; ++j) add(t, sums[j * k.block_cols * E + i]);
+    to[i] = t.x;
+    to[a.C + i] = t.y;
   }
 }
 
 template <typename T, int E, int V, bool JOIN>
-__global__ __launch_bounds__(kThreads) void norm_bwd_apply_kernel(Groups a, Cut parts_cut) {
+__global__ __launch_bounds__(kThreads) void norm_bwd_apply_kernel(Groups a, Cut parts_cut, int B) {
   __shared__ float2 totals[kThreads];
-  const Place w(a, a.first + blockIdx.x);
+  if ((int)blockIdx.x < a.sums) return GroupSums::run(a.channel_part, B * parts_cut.slabs, a.C, blockIdx.x, &totals[0].x, a.dgamma, a.dbeta);
+  const Place w(a, a.first + blockIdx.x - a.sums);
   const Cut& k = a.k;
   const size_t bg = (size_t)w.b * a.G + w.group;
   float x[V][E], g[V][E];
@@ -705,7 +723,7 @@ hipError_t rows_bwd(const NormArgs& a, hipStream_t stream) {
     }
   });
   if (rc != hipSuccess || !part) return rc;
-  AFFMAE_LAUNCH("norm_channel_sums_kernel", stream, norm_channel_sums_kernel, dim3(cdiv(a.C, 32), 2), dim3(1024), 0, stream, part, blocks, a.C, a.dgamma, a.dbeta);
+  AFFMAE_LAUNCH("norm_channel_sums_kernel", stream, norm_channel_sums_kernel, dim3(RowSums::blocks(a.C)), dim3(1024), 0, stream, part, blocks, a.C, a.dgamma, a.dbeta);
   return hipGetLastError();
 }
 
@@ -717,13 +735,15 @@ Groups groups_of(const NormArgs& a, const Cut& k) {
   return g;
 }
 
-// f(workgroups) for all of a cut's, in launches of as many as the runtime takes
+// f(workgroups) for all of a cut's, in launches of as many as the runtime takes, g.sums more beside them
 template <typename F>
 void for_workgroups(Groups& g, int B, F f) {
   const long long all = (long long)B * g.k.blocks * g.k.slabs;
-  for (long long first = 0; first < all; first += kMaxBlocks) {
+  for (long long first = 0; first < all;) {
+    const long long n = std::min(all - first, kMaxBlocks - g.sums);
     g.first = (unsigned)first;
-    f(dim3((unsigned)std::min(all - first, kMaxBlocks)));
+    f(dim3((unsigned)n));
+    first += n;
   }
 }
 
@@ -784,10 +804,13 @@ hipError_t groups_bwd(const NormArgs& a, hipStream_t stream) {
   cut_rows(k, a.N, (long long)V * k.lanes);
   g.k = k;
   const auto kernel = join ? norm_bwd_apply_kernel<T, E, V, true> : norm_bwd_apply_kernel<T, E, V, false>;
-  for_workgroups(g, a.B, [&](dim3 grid) { AFFMAE_LAUNCH("norm_bwd_apply_kernel", stream, kernel, grid, threads, 0, stream, g, sums); });
-  if (a.dgamma)
-    AFFMAE_LAUNCH("norm_channel_sums_kernel", stream, norm_channel_sums_kernel, dim3(cdiv(a.C, 32), 2), dim3(1024), 0, stream, g.channel_part, a.B * sums.slabs,
-                  a.C, a.dgamma, a.dbeta);
+  g.dgamma = a.dgamma;
+  g.dbeta = a.dbeta;
+  g.sums = a.dgamma ? GroupSums::blocks(a.C) : 0;
+  for_workgroups(g, a.B, [&](dim3 grid) {
+    AFFMAE_LAUNCH("norm_bwd_apply_kernel", stream, kernel, dim3(grid.x + g.sums), threads, 0, stream, g, sums, a.B);
+    g.sums = 0;
+  });
   return hipGetLastError();
 }
 
