@@ -27,28 +27,44 @@ __device__ __forceinline__ void normal_cdf(float z, float& cdf, float& density) 
 }
 __device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.f + __expf(-z)); }
 
-__device__ __forceinline__ float act_value(float z, int act) {
-  if (act == kActRelu) return z < 0.f ? 0.f : z;  // (a NaN stays one)
-  if (act == kActGelu) {
-    float cdf, density;
-    normal_cdf(z, cdf, density);
-    return z * cdf;
+// z becomes its activation (one branch for all of them, not one for each)
+template <int E>
+__device__ __forceinline__ void act_values(float (&z)[E], int act) {
+  if (act == kActRelu) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) z[e] = z[e] < 0.f ? 0.f : z[e];  // (a NaN stays one)
+  } else if (act == kActGelu) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      float cdf, density;
+      normal_cdf(z[e], cdf, density);
+      z[e] *= cdf;
+    }
+  } else if (act == kActSilu) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) z[e] *= sigmoid(z[e]);
   }
-  if (act == kActSilu) return z * sigmoid(z);
-  return z;
 }
-__device__ __forceinline__ float act_slope(float z, int act) {
-  if (act == kActRelu) return z > 0.f ? 1.f : 0.f;
-  if (act == kActGelu) {
-    float cdf, density;
-    normal_cdf(z, cdf, density);
-    return __builtin_fmaf(z, density, cdf);
+// g becomes g act'(z)
+template <int E>
+__device__ __forceinline__ void act_slopes(float (&g)[E], const float (&z)[E], int act) {
+  if (act == kActRelu) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) g[e] = z[e] > 0.f ? g[e] : 0.f;
+  } else if (act == kActGelu) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      float cdf, density;
+      normal_cdf(z[e], cdf, density);
+      g[e] *= __builtin_fmaf(z[e], density, cdf);
+    }
+  } else if (act == kActSilu) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const float s = sigmoid(z[e]);
+      g[e] *= s * __builtin_fmaf(z[e], 1.f - s, 1.f);
+    }
   }
-  if (act == kActSilu) {
-    const float s = sigmoid(z);
-    return s * __builtin_fmaf(z, 1.f - s, 1.f);
-  }
-  return 1.f;
 }
 
 // Dropout of probability p.  Element i stays where word i % 4 of the generator's block i / 4 is at least `least` = floor(p 2^32);

@@ -201,6 +201,7 @@ struct Product {
   Operand a, b;
   int M, N, K;
   int tiles_n, tiles, splits, split_slices;  // tiles of c; workgroups that share a tile's k, slices of each
+  int buffers;  // 1: a slice's place in LDS besides the one that is multiplied, 0: none
 };
 struct Epilogue {
   const void *bias, *residual;
@@ -226,10 +227,7 @@ __device__ __forceinline__ void finish(const Epilogue& e, const RngKey& key, flo
     for (int i = 0; i < E; ++i) v[i] += b[i];
   }
   if (e.pre) store_piece<E>((T*)e.pre + at, v);
-  if (e.act != kActNone) {
-#pragma unroll
-    for (int i = 0; i < E; ++i) v[i] = act_value(v[i], e.act);
-  }
+  act_values<E>(v, e.act);
   if (e.d.rng) drop<E>(v, e.d, key, at);
   if (e.residual) {
 #pragma unroll
@@ -238,23 +236,17 @@ __device__ __forceinline__ void finish(const Epilogue& e, const RngKey& key, flo
   store_piece<E>((T*)e.out + at, v);
 }
 
-// The 16 x TNW products of a strip in LDS as pieces of E values in the order of memory: the lane's i-th piece, if it has one there.
-template <int E, int TNW>
-struct Strip {
-  static constexpr int kRow = TNW / E, kAll = 16 * kRow, kTurns = (kAll + kWave - 1) / kWave;
-  static constexpr int kLd = TNW + 4;
-  int row, col;
-  bool there;
-  __device__ __forceinline__ Strip(int i, int lane, int m, int n, int M, int N) {
-    const int q = i * kWave + lane;
-    row = q / kRow;
-    col = q % kRow * E;
-    there = (kAll % kWave == 0 || q < kAll) && m + row < M && n + col < N;
-  }
-};
-
 template <int BM, int BN>
 constexpr int kStageBytes = (BM + BN) * kSliceBytes;
+
+// What a wave puts into LDS at a tile's end: strips of 16 rows, all or half of them.
+template <int BM, int BN, int WM, int WN>
+struct Batch {
+  static constexpr int kLd = BN / WN + 4, kAll = BM / WM / 16;
+  static constexpr int kStrips = WM * WN * kAll * 16 * kLd * 4 <= 40 * 1024 ? kAll : kAll / 2;
+  static constexpr int kFloats = kStrips * 16 * kLd;
+  static constexpr int kBytes = WM * WN * kFloats * 4;
+};
 
 // BM x BN values of c by WM x WN waves.  Two slices of both operands in LDS: one is multiplied while the next one is on its way.
 // The products are c^T tiles (b's rows along the instruction's rows), so that a lane holds four consecutive columns of c.
@@ -276,7 +268,7 @@ __global__ __launch_bounds__(WM* WN* kWave, 2) void linear_kernel(Product p, Ep 
   const Stager<T, AA, BM, W, kThreads> sa(p.a.p, p.a.ld, p.a.bytes, m0, p.M);
   const Stager<T, BA, BN, W, kThreads> sb(p.b.p, p.b.ld, p.b.bytes, n0, p.N);
   const auto stage = [&](int s) {
-    char* dst = lds + (s & 1) * kStageBytes<BM, BN>;
+    char* dst = lds + (s & p.buffers) * kStageBytes<BM, BN>;
     const int k0 = k_begin + s * kSlice<T>;
     if constexpr (W >= 4) {
       sa.load(dst, k0, k_end - k0);
@@ -293,8 +285,8 @@ __global__ __launch_bounds__(WM* WN* kWave, 2) void linear_kernel(Product p, Ep 
   for (int s = 0; s < slices; ++s) {
     // slice s has arrived, and every wave has read what the next one will be written over
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    if (s + 1 < slices) stage(s + 1);
-    const char* as = lds + (s & 1) * kStageBytes<BM, BN>;
+    if (p.buffers && s + 1 < slices) stage(s + 1);
+    const char* as = lds + (s & p.buffers) * kStageBytes<BM, BN>;
     const char* bs = as + BM * kSliceBytes;
 #pragma unroll
     for (int step = 0; step < 2; ++step) {
@@ -321,18 +313,17 @@ __global__ __launch_bounds__(WM* WN* kWave, 2) void linear_kernel(Product p, Ep 
         }
       }
     }
+    if (!p.buffers && s + 1 < slices) {
+      asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+      stage(s + 1);
+    }
   }
+  // A wave's values go through LDS, a batch of strips of 16 rows at a time, and leave as pieces in the order of memory, by a loop that is
+  // not unrolled: with the epilogue's code once for every strip, a tile's end took a quarter longer (131072 x 64 -> 192, gelu, 26.3 us
+  // against 21).
   __syncthreads();
-  float* strip = reinterpret_cast<float*>(lds) + wave * 16 * (TN + 4);
-  static_assert(WM * WN * 16 * (TN + 4) * 4 <= kStageBytes<BM, BN>);
-  const int n = n0 + wn * TN;
-  const auto to_strip = [&](int i) __attribute__((always_inline)) {
-    wave_lds_sync();
-#pragma unroll
-    for (int j = 0; j < IN; ++j) *reinterpret_cast<f32x4*>(strip + r * (TN + 4) + 16 * j + 4 * g) = c[i][j];
-    wave_lds_sync();
-  };
-  const int strips = min(IM, (p.M - m0 - wm * TM + 15) >> 4);  // (none or fewer where the tile is cut off)
+  using B = Batch<BM, BN, WM, WN>;
+  float* batch = reinterpret_cast<float*>(lds) + wave * B::kFloats;
   if constexpr (kSums) {
     if (want_sums) {
 #pragma unroll
@@ -346,75 +337,62 @@ __global__ __launch_bounds__(WM* WN* kWave, 2) void linear_kernel(Product p, Ep 
       }
     }
   }
-  if constexpr (kGrad) {
-    const auto run = [&](auto out, auto piece, int N) __attribute__((always_inline)) {
-      constexpr int E = decltype(piece)::value;
-      using S = Strip<E, TN>;
 #pragma unroll
-      for (int i = 0; i < IM; ++i) {
-        if (i >= strips) break;
-        const int m = m0 + wm * TM + 16 * i;
-        to_strip(i);
+  for (int first = 0; first < IM; first += B::kStrips) {
+    const int m = m0 + wm * TM + 16 * first, n = n0 + wn * TN;
+    if (m >= p.M || n >= p.N) break;
+    wave_lds_sync();
 #pragma unroll
-        for (int t = 0; t < S::kTurns; ++t) {
-          const S q(t, lane, m, n, p.M, N);
-          if (!q.there) continue;
-          float v[E];
-          load_piece<E>(strip + q.row * S::kLd + q.col, v);
+    for (int i = 0; i < B::kStrips; ++i)
 #pragma unroll
-          for (int x = 0; x < E; ++x) v[x] *= e.alpha;
-          store_piece<E>(out + (size_t)(m + q.row) * N + n + q.col, v);
-        }
+      for (int j = 0; j < IN; ++j) *reinterpret_cast<f32x4*>(batch + (16 * i + r) * B::kLd + 16 * j + 4 * g) = c[first + i][j];
+    wave_lds_sync();
+    // f(piece number, its row and column in the batch) for the lane's pieces of E values inside M x N
+    const auto pieces = [&](auto piece, int N, auto f) __attribute__((always_inline)) {
+      constexpr int E = decltype(piece)::value, kRow = TN / E;
+      const int all = min(16 * B::kStrips, p.M - m) * kRow;
+#pragma unroll 1
+      for (int q = lane; q < all; q += kWave) {
+        const int row = q / kRow, col = q % kRow * E;
+        if (n + col < N) f(row, col);
       }
     };
     using std::integral_constant;
-    if (e.part)  // (alpha is 1)
-      run(e.part + (size_t)split * p.M * e.part_ld, integral_constant<int, 4>(), e.part_ld);
-    else if (p.N % kPiece<T> == 0 && ((uintptr_t)e.out & 15) == 0)
-      run((T*)e.out, integral_constant<int, kPiece<T>>(), p.N);
-    else
-      run((T*)e.out, integral_constant<int, 1>(), p.N);
-  } else {
-    RngKey key = {};
-    if (e.d.rng) key = rng_key(e.d.rng);
-    const auto run = [&](auto piece) __attribute__((always_inline)) {
-      constexpr int E = decltype(piece)::value;
-      using S = Strip<E, TN>;
-      float next[S::kTurns][E];  // the residual's values are on their way a strip ahead
-      const auto fetch = [&](int i) __attribute__((always_inline)) {
-#pragma unroll
-        for (int t = 0; t < S::kTurns; ++t) {
-          const int m = m0 + wm * TM + 16 * i;
-          const S q(t, lane, m, n, p.M, p.N);
-          if (q.there) load_piece<E>((const T*)e.residual + (size_t)(m + q.row) * p.N + n + q.col, next[t]);
-        }
-      };
-      if (e.residual && strips > 0) fetch(0);
-#pragma unroll
-      for (int i = 0; i < IM; ++i) {
-        if (i >= strips) break;
-        const int m = m0 + wm * TM + 16 * i;
-        to_strip(i);
-        float res[S::kTurns][E];
-#pragma unroll
-        for (int t = 0; t < S::kTurns; ++t)
-#pragma unroll
-          for (int x = 0; x < E; ++x) res[t][x] = next[t][x];
-        if (e.residual && i + 1 < strips) fetch(i + 1);
-#pragma unroll
-        for (int t = 0; t < S::kTurns; ++t) {
-          const S q(t, lane, m, n, p.M, p.N);
-          if (!q.there) continue;
+    if constexpr (kGrad) {
+      const auto put = [&](auto* out, auto piece, int N) __attribute__((always_inline)) {
+        constexpr int E = decltype(piece)::value;
+        pieces(piece, N, [&](int row, int col) {
           float v[E];
-          load_piece<E>(strip + q.row * S::kLd + q.col, v);
-          finish<T, E>(e, key, v, res[t], n + q.col, (size_t)(m + q.row) * p.N + n + q.col);
-        }
-      }
-    };
-    if (p.N % kPiece<T> == 0 && (((uintptr_t)e.out | (uintptr_t)e.pre | (uintptr_t)e.bias | (uintptr_t)e.residual) & 15) == 0)
-      run(std::integral_constant<int, kPiece<T>>());
-    else
-      run(std::integral_constant<int, 1>());
+          load_piece<E>(batch + row * B::kLd + col, v);
+#pragma unroll
+          for (int x = 0; x < E; ++x) v[x] *= e.alpha;
+          store_piece<E>(out + (size_t)(m + row) * N + n + col, v);
+        });
+      };
+      if (e.part)  // (alpha is 1)
+        put(e.part + (size_t)split * p.M * e.part_ld, integral_constant<int, 4>(), e.part_ld);
+      else if (p.N % kPiece<T> == 0 && ((uintptr_t)e.out & 15) == 0)
+        put((T*)e.out, integral_constant<int, kPiece<T>>(), p.N);
+      else
+        put((T*)e.out, integral_constant<int, 1>(), p.N);
+    } else {
+      RngKey key = {};
+      if (e.d.rng) key = rng_key(e.d.rng);
+      const auto put = [&](auto piece) __attribute__((always_inline)) {
+        constexpr int E = decltype(piece)::value;
+        pieces(piece, p.N, [&](int row, int col) {
+          const size_t at = (size_t)(m + row) * p.N + n + col;
+          float v[E], res[E];
+          if (e.residual) load_piece<E>((const T*)e.residual + at, res);
+          load_piece<E>(batch + row * B::kLd + col, v);
+          finish<T, E>(e, key, v, res, n + col, at);
+        });
+      };
+      if (p.N % kPiece<T> == 0 && (((uintptr_t)e.out | (uintptr_t)e.pre | (uintptr_t)e.bias | (uintptr_t)e.residual) & 15) == 0)
+        put(integral_constant<int, kPiece<T>>());
+      else
+        put(integral_constant<int, 1>());
+    }
   }
 }
 
@@ -543,10 +521,7 @@ __global__ __launch_bounds__(256) void linear_dz_kernel(const T* __restrict__ do
     load_some<E>(dout + i, n, whole, v);
     if (pre) load_some<E>(pre + i, n, whole, z);
     if (d.rng) drop<E>(v, d, key, (uint64_t)i);
-    if (pre) {
-#pragma unroll
-      for (int e = 0; e < E; ++e) v[e] *= act_slope(z[e], act);
-    }
+    if (pre) act_slopes<E>(v, z, act);
     if constexpr (EVEN) {
       store_piece<E>(dz + i, v);
     } else {
@@ -568,6 +543,8 @@ __global__ __launch_bounds__(256) void linear_dz_kernel(const T* __restrict__ do
   }
 }
 
+constexpr int kCus = 256;
+
 // what a lane may bring at a time, by where an operand's lines start
 int line_bytes(const Operand& o) {
   const uintptr_t all = reinterpret_cast<uintptr_t>(o.p) | o.ld;
@@ -580,9 +557,13 @@ hipError_t run_tiles(Product p, const Ep& e, hipStream_t stream) {
   p.tiles = cdiv(p.M, BM) * p.tiles_n;
   const int slices = cdiv(p.K, kSlice<T>);
   p.split_slices = cdiv(slices, p.splits);
-  const int stages = W >= 4 && p.split_slices > 1 ? 2 : W >= 4 ? 1 : 2;
+  // A second place for a slice hides its way from memory; without it twice the workgroups fit a CU and hide each other's.  The latter
+  // pays in forward products that have several for every CU and are not deep: 65536 x 256 -> 256 20.0 us against 23.1, 16384 x 768 -> 2304
+  // 67 against 74, but 16384 x 2304 -> 768 63 against 61, 4096 x 768 -> 768 13.5 against 12.5, dx of 16384 x 768 -> 2304 59 against 55; fp32: no difference.
+  const bool crowded = std::is_same_v<Ep, Epilogue> && sizeof(T) == 2 && p.split_slices <= 16 && p.tiles >= 2 * kCus;
+  p.buffers = p.split_slices > 1 && (!crowded || W < 4);
   const auto kernel = linear_kernel<T, AA, BA, W, BM, BN, WM, WN, Ep>;
-  const size_t lds = (size_t)stages * kStageBytes<BM, BN>;
+  const size_t lds = (size_t)std::max((1 + p.buffers) * kStageBytes<BM, BN>, Batch<BM, BN, WM, WN>::kBytes);
   if (lds > 64 * 1024) {
     const hipError_t rc = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
     if (rc != hipSuccess) return rc;
@@ -602,41 +583,39 @@ hipError_t run_slim(Product p, const Epilogue& e, hipStream_t stream) {
 }
 
 // What a workgroup's tile costs, in us: a slice while a CU is full of such workgroups (per workgroup), a slice of one that has its CU
-// to itself, and everything but the slices.  Measured on products of 16384 to 32768 rows, 256 to 2304 deep; large tiles read less of LDS
-// per product (128 x 192 reaches 1.0 to 1.1 PFLOP/s in bf16), small ones fill the chip and hide their ends behind each other; `epilogue`:
-// what the forward's longer end takes beyond that.
+// to itself, and everything but the slices.  Measured on products of 16384 to 131072 rows, 64 to 2304 deep; large tiles read less of LDS
+// per product (128 x 192 reaches 1.0 to 1.1 PFLOP/s in bf16), small ones fill the chip and hide their ends behind each other.
 struct Shape {
   int bm, bn, resident;
-  float slice, alone, end, epilogue;
+  float slice, alone, end;
 };
 enum { k64x64, k128x64, k128x128, k128x192, kSlimTile };
-constexpr Shape kShapes16[] = {{64, 64, 4, .183f, .55f, .57f, 0.f}, {128, 64, 3, .283f, .58f, 1.2f, 0.f}, {128, 128, 2, .546f, .85f, 2.2f, .6f},
-                               {128, 192, 2, .70f, 1.1f, 3.7f, .6f}, {16, 16, 4, .112f, .11f, .4f, 0.f}};
-constexpr Shape kShapes32[] = {{64, 64, 4, .66f, .78f, .4f, 0.f}, {128, 64, 3, 1.17f, 1.22f, 1.4f, 0.f}, {}, {}, {16, 16, 4, .116f, .11f, .4f, 0.f}};
-constexpr int kCus = 256;
+constexpr Shape kForward16[] = {{64, 64, 4, .19f, .55f, .45f}, {128, 64, 4, .31f, .58f, 1.1f}, {128, 128, 4, .47f, .85f, 2.1f}, {128, 192, 3, .60f, 1.1f, 4.0f}, {16, 16, 4, .112f, .11f, .4f}};
+constexpr Shape kGradient16[] = {{64, 64, 4, .183f, .55f, .57f}, {128, 64, 3, .283f, .58f, 1.2f}, {128, 128, 2, .546f, .85f, 2.2f}, {128, 192, 2, .70f, 1.1f, 3.7f}};
+constexpr Shape kForward32[] = {{64, 64, 4, .66f, .78f, .4f}, {128, 64, 3, 1.17f, 1.22f, 1.4f}, {}, {}, {16, 16, 4, .116f, .11f, .4f}};
+constexpr Shape kGradient32[] = {{64, 64, 4, .66f, .78f, .4f}, {128, 64, 3, 1.17f, 1.22f, 1.4f}, {}, {}};
 
 struct Plan {
   int shape, splits;
 };
-float plan_cost(const Shape& h, long long M, long long N, int slices, int splits, bool forward) {
-  const float end = h.end + (forward ? h.epilogue : 0.f);
+float plan_cost(const Shape& h, long long M, long long N, int slices, int splits) {
   const long long work = (long long)cdiv(M, h.bm) * cdiv(N, h.bn) * splits, turn = (long long)kCus * h.resident;
   const int deep = cdiv(slices, splits), rest = cdiv(work % turn, kCus);
-  float t = (float)(work / turn) * ((float)deep * std::max(h.alone, h.resident * h.slice) + h.resident * end);
-  if (rest) t += (float)deep * std::max(h.alone, rest * h.slice) + rest * end;
+  float t = (float)(work / turn) * ((float)deep * std::max(h.alone, h.resident * h.slice) + h.resident * h.end);
+  if (rest) t += (float)deep * std::max(h.alone, rest * h.slice) + rest * h.end;
   // parts are written and read once (4 TB/s), by one more launch
   if (splits > 1) t += 4.f + (float)splits * (float)M * (float)N * 8.f / 4e6f;
   return t;
 }
 // The cheapest tile; gradients also share a tile's k between workgroups, as many as make one or two full turns of the chip.
 Plan plan_product(long long M, long long N, int K, int el, int line, bool forward) {
-  const Shape* shapes = el == 2 ? kShapes16 : kShapes32;
+  const Shape* shapes = forward ? el == 2 ? kForward16 : kForward32 : el == 2 ? kGradient16 : kGradient32;
   const int slices = cdiv(K, kSliceBytes / el);
   Plan best = {k64x64, 1};
   float least = 3e38f;
-  for (int i = 0; i <= kSlimTile; ++i) {
+  for (int i = 0; i < (forward ? kSlimTile + 1 : kSlimTile); ++i) {
     const Shape& h = shapes[i];
-    if (!h.bm || (i > k128x64 && line < 16) || (i == kSlimTile && !forward)) continue;
+    if (!h.bm || (i > k128x64 && line < 16)) continue;
     const long long tiles = (long long)cdiv(M, h.bm) * cdiv(N, h.bn);
     if (i == kSlimTile && tiles > 1 << 20) continue;
     for (int turns = 0; turns <= 2; ++turns) {
@@ -644,7 +623,7 @@ Plan plan_product(long long M, long long N, int K, int el, int line, bool forwar
       const int most = turns ? (int)std::min<long long>((long long)kCus * h.resident * turns / tiles, slices / 2) : 1;
       if (most < 1) continue;
       const int splits = cdiv(slices, cdiv(slices, most));  // (none without slices)
-      const float t = plan_cost(h, M, N, slices, splits, forward);
+      const float t = plan_cost(h, M, N, slices, splits);
       if (t < least) {
         least = t;
         best = {i, splits};

@@ -34,10 +34,7 @@ __device__ __forceinline__ void normalise(float (&v)[E], float mean, float rstd,
     v[e] = (v[e] - mean) * rstd;
     if (affine) v[e] = __builtin_fmaf(v[e], gm[e], bt[e]);
   }
-  if (act != kActNone) {
-#pragma unroll
-    for (int e = 0; e < E; ++e) v[e] = act_value(v[e], act);
-  }
+  act_values<E>(v, act);
 }
 // x becomes xhat, g (dout) becomes dz = dout act'(z)
 template <int E>
@@ -45,8 +42,10 @@ __device__ __forceinline__ void slopes(float (&x)[E], float (&g)[E], float mean,
 #pragma unroll
   for (int e = 0; e < E; ++e) x[e] = (x[e] - mean) * rstd;
   if (act != kActNone) {
+    float z[E];
 #pragma unroll
-    for (int e = 0; e < E; ++e) g[e] *= act_slope(affine ? __builtin_fmaf(x[e], gm[e], bt[e]) : x[e], act);
+    for (int e = 0; e < E; ++e) z[e] = affine ? __builtin_fmaf(x[e], gm[e], bt[e]) : x[e];
+    act_slopes<E>(g, z, act);
   }
 }
 
