@@ -720,25 +720,20 @@ def affmae_linear_bwd(x: Optional[torch.Tensor], weight: Optional[torch.Tensor],
         _dev(pre, "pre", dout.dtype, dout.shape)
     elif act != "none":
         raise ValueError("an activation's backward needs pre")
-    shapes = {}
-    if want_dx:
-        shapes["dx"] = dout.shape[:-1] + (Cin,)
-    if want_dweight:
-        shapes["dweight"] = (Cout, Cin)
-        if want_dbias:
-            shapes["dbias"] = (Cout,)
-    for name, shape in shapes.items():
-        if name not in g:
-            g[name] = torch.empty(shape, dtype=dout.dtype, device=dout.device)
-        else:
-            _dev(g[name], name, dout.dtype, shape)
+    want_dbias = want_dbias and want_dweight
+    for name, shape, wanted in (("dx", dout.shape[:-1] + (Cin,), want_dx), ("dweight", (Cout, Cin), want_dweight), ("dbias", (Cout,), want_dbias)):
+        if wanted:
+            if name not in g:
+                g[name] = torch.empty(shape, dtype=dout.dtype, device=dout.device)
+            else:
+                _dev(g[name], name, dout.dtype, shape)
     rows = dout.numel() // max(Cout, 1)
     a = _act_code(act)
     need = lib.affmae_linear_bwd_workspace_bytes(rows, Cin, Cout, a, float(p), code, int(want_dx), int(want_dweight))
     workspace, size = _own_workspace(workspace, need, dout.device)
     rc = lib.affmae_linear_bwd(_ptr(x), _ptr(weight), _ptr(pre), _ptr(dout), rows, Cin, Cout, a, float(p), _rng_ptr(rng, p), code,
                                _ptr(g["dx"]) if want_dx else None, _ptr(g["dweight"]) if want_dweight else None,
-                               _ptr(g["dbias"]) if "dbias" in shapes else None, _ptr(workspace), size, _stream())
+                               _ptr(g["dbias"]) if want_dbias else None, _ptr(workspace), size, _stream())
     if rc != 0:
         raise AffmaeError("affmae_linear_bwd", rc)
     return g

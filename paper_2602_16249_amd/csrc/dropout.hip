@@ -21,16 +21,21 @@ __global__ __launch_bounds__(kThreads) void dropout_kernel(const T* x, const T* 
   RngKey key = {};
   if (d.rng) key = rng_key(d.rng);
   for (long long i = ((long long)blockIdx.x * kThreads + threadIdx.x) * E; i < n; i += (long long)gridDim.x * kThreads * E) {
-    const int some = (int)std::min<long long>(n - i, E);
-    float v[E], r[E];
-    load_some<E>(x + i, some, whole, v);
-    if (residual) load_some<E>(residual + i, some, whole, r);
-    if (d.rng) drop<E>(v, d, key, (uint64_t)i);
-    if (residual) {
+    const auto piece = [&](bool all, int some) __attribute__((always_inline)) {
+      float v[E], r[E];
+      load_some<E>(x + i, some, all, v);
+      if (residual) load_some<E>(residual + i, some, all, r);
+      if (d.rng) drop<E>(v, d, key, (uint64_t)i);
+      if (residual) {
 #pragma unroll
-      for (int e = 0; e < E; ++e) v[e] += r[e];
-    }
-    store_some<E>(out + i, some, whole, v);
+        for (int e = 0; e < E; ++e) v[e] += r[e];
+      }
+      store_some<E>(out + i, some, all, v);
+    };
+    if (whole && n - i >= E)
+      piece(true, E);
+    else
+      piece(false, (int)std::min<long long>(n - i, E));
   }
 }
 

@@ -12,6 +12,7 @@
 #include "dense_common.h"
 
 #include <algorithm>
+#include <cmath>
 
 namespace affmae {
 namespace {
@@ -598,35 +599,40 @@ constexpr Shape kGradient32[] = {{64, 64, 4, .66f, .78f, .4f}, {128, 64, 3, 1.17
 struct Plan {
   int shape, splits;
 };
-float plan_cost(const Shape& h, long long M, long long N, int slices, int splits) {
-  const long long work = (long long)cdiv(M, h.bm) * cdiv(N, h.bn) * splits, turn = (long long)kCus * h.resident;
-  const int deep = cdiv(slices, splits), rest = cdiv(work % turn, kCus);
-  float t = (float)(work / turn) * ((float)deep * std::max(h.alone, h.resident * h.slice) + h.resident * h.end);
-  if (rest) t += (float)deep * std::max(h.alone, rest * h.slice) + rest * h.end;
+// (floats: this is worked out for every call, several times)
+float plan_cost(const Shape& h, float tiles, float values, uint32_t slices, uint32_t splits) {
+  const float work = tiles * (float)splits, turn = (float)(kCus * h.resident), deep = (float)((slices + splits - 1) / splits);
+  const float full = std::floor(work / turn), rest = std::ceil((work - full * turn) * (1.f / kCus));
+  float t = full * (deep * std::max(h.alone, h.resident * h.slice) + h.resident * h.end);
+  if (rest > 0.f) t += deep * std::max(h.alone, rest * h.slice) + rest * h.end;
   // parts are written and read once (4 TB/s), by one more launch
-  if (splits > 1) t += 4.f + (float)splits * (float)M * (float)N * 8.f / 4e6f;
+  if (splits > 1) t += 4.f + (float)splits * values * (8.f / 4e6f);
   return t;
 }
 // The cheapest tile; gradients also share a tile's k between workgroups, as many as make one or two full turns of the chip.
-Plan plan_product(long long M, long long N, int K, int el, int line, bool forward) {
+Plan plan_product(uint32_t M, uint32_t N, uint32_t K, int el, int line, bool forward) {
   const Shape* shapes = forward ? el == 2 ? kForward16 : kForward32 : el == 2 ? kGradient16 : kGradient32;
-  const int slices = cdiv(K, kSliceBytes / el);
+  const uint32_t deep = kSliceBytes / el, slices = (K + deep - 1) / deep;
+  const float values = (float)M * (float)N;
   Plan best = {k64x64, 1};
   float least = 3e38f;
   for (int i = 0; i < (forward ? kSlimTile + 1 : kSlimTile); ++i) {
     const Shape& h = shapes[i];
     if (!h.bm || (i > k128x64 && line < 16)) continue;
-    const long long tiles = (long long)cdiv(M, h.bm) * cdiv(N, h.bn);
-    if (i == kSlimTile && tiles > 1 << 20) continue;
-    for (int turns = 0; turns <= 2; ++turns) {
-      if (turns && forward) break;
-      const int most = turns ? (int)std::min<long long>((long long)kCus * h.resident * turns / tiles, slices / 2) : 1;
-      if (most < 1) continue;
-      const int splits = cdiv(slices, cdiv(slices, most));  // (none without slices)
-      const float t = plan_cost(h, M, N, slices, splits);
+    const float tiles = (float)((M + h.bm - 1) / h.bm) * (float)((N + h.bn - 1) / h.bn);
+    if (i == kSlimTile && tiles > 1e6f) continue;
+    for (int turns = 0; turns <= (forward ? 0 : 2); ++turns) {
+      uint32_t splits = 1;
+      if (turns) {
+        const uint32_t most = (uint32_t)std::min((float)(kCus * h.resident * turns) / tiles, (float)(slices / 2));
+        if (most < 2) continue;
+        const uint32_t each = (slices + most - 1) / most;
+        splits = (slices + each - 1) / each;  // (none without slices)
+      }
+      const float t = plan_cost(h, tiles, values, slices, splits);
       if (t < least) {
         least = t;
-        best = {i, splits};
+        best = {i, (int)splits};
       }
     }
   }
