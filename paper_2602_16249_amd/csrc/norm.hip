@@ -21,6 +21,7 @@ namespace affmae {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kHeldParts = 4;
 constexpr int kWaves = kThreads / kWave;
 
 int cdiv(long long a, long long b) { return (int)((a + b - 1) / b); }
@@ -51,12 +52,28 @@ __device__ __forceinline__ void slopes(float (&x)[E], float (&g)[E], float mean,
 
 // ------------------------------------------------------------------------------------------------------------------ rows
 
+// the sum over the LANES lanes that hold a row, received by all of them: part of a wave, or the workgroup
+template <int LANES>
+__device__ __forceinline__ float row_sum(float v, int lane, float (&acc)[kWaves]) {
+  if constexpr (LANES <= kWave) {
+    return lanes_sum<1, LANES / 2>(v, lane);
+  } else {
+    static_assert(LANES == kThreads);
+    v = wave_sum(v);
+    __syncthreads();
+    if (lane == 0) acc[threadIdx.x / kWave] = v;
+    __syncthreads();
+    return (acc[0] + acc[1]) + (acc[2] + acc[3]);
+  }
+}
+
 // LANES lanes a row, PIECES pieces of E values a lane, TURNS rows of a lane group on their way at a time
 template <typename T, int E, int LANES, int PIECES, int TURNS>
 __global__ __launch_bounds__(kThreads) void norm_rows_fwd_kernel(const T* __restrict__ x, const T* __restrict__ gamma, const T* __restrict__ beta, int rows,
                                                                  int C, float eps, int act, T* __restrict__ out, float* __restrict__ mean,
                                                                  float* __restrict__ rstd) {
   constexpr int kRows = kThreads / LANES;  // of a turn
+  __shared__ float acc[kWaves];
   const int lane = threadIdx.x & (kWave - 1), l = threadIdx.x % LANES, at = threadIdx.x / LANES;
   const float inv = 1.f / (float)C;
   float gm[PIECES][E], bt[PIECES][E];
@@ -92,7 +109,7 @@ __global__ __launch_bounds__(kThreads) void norm_rows_fwd_kernel(const T* __rest
       for (int p = 0; p < PIECES; ++p)
 #pragma unroll
         for (int e = 0; e < E; ++e) s += v[t][p][e];
-      const float m = lanes_sum<1, LANES / 2>(s, lane) * inv;
+      const float m = row_sum<LANES>(s, lane, acc) * inv;
       s = 0.f;
 #pragma unroll
       for (int p = 0; p < PIECES; ++p)
@@ -100,7 +117,7 @@ __global__ __launch_bounds__(kThreads) void norm_rows_fwd_kernel(const T* __rest
 #pragma unroll
           for (int e = 0; e < E; ++e) s = __builtin_fmaf(v[t][p][e] - m, v[t][p][e] - m, s);
         }
-      const float r = 1.f / sqrtf(lanes_sum<1, LANES / 2>(s, lane) * inv + eps);
+      const float r = 1.f / sqrtf(row_sum<LANES>(s, lane, acc) * inv + eps);
       if (row >= rows) continue;
       if (l == 0) {
         mean[row] = m;
@@ -123,7 +140,8 @@ __global__ __launch_bounds__(kThreads) void norm_rows_bwd_kernel(const T* __rest
                                                                  const float* __restrict__ mean, const float* __restrict__ rstd, const T* __restrict__ dout,
                                                                  int rows, int C, int act, T* __restrict__ dx, float* __restrict__ part) {
   constexpr int kRows = kThreads / LANES;
-  __shared__ float sums[kRows > 1 ? kRows : 1][LANES * E];
+  __shared__ float sums[kRows][LANES * E];
+  __shared__ float acc[kWaves];
   const int lane = threadIdx.x & (kWave - 1), l = threadIdx.x % LANES, at = threadIdx.x / LANES;
   const float inv = 1.f / (float)C;
   float gm[PIECES][E], bt[PIECES][E], dg[PIECES][E], db[PIECES][E];
@@ -172,8 +190,8 @@ __global__ __launch_bounds__(kThreads) void norm_rows_bwd_kernel(const T* __rest
           s2 = __builtin_fmaf(g[t][p][e], v[t][p][e], s2);
         }
       }
-      s1 = lanes_sum<1, LANES / 2>(s1, lane) * inv;
-      s2 = lanes_sum<1, LANES / 2>(s2, lane) * inv;
+      s1 = row_sum<LANES>(s1, lane, acc) * inv;
+      s2 = row_sum<LANES>(s2, lane, acc) * inv;
       if (row >= rows) continue;
 #pragma unroll
       for (int p = 0; p < PIECES; ++p) {
@@ -247,6 +265,8 @@ struct Cut {
   int lanes;       // threads over each other in a column: kThreads / block_cols
   int rows;        // tokens of a workgroup
   int slabs;       // workgroups over an image's tokens
+  int team;       // lanes that add up a group's values of a workgroup
+  int join_team;  // lanes that put a group's parts together, kHeldParts each
   uint32_t cols_magic, group_magic;
   __host__ __device__ int parts() const { return slabs * shares; }  // of a group
 };
@@ -311,13 +331,26 @@ struct Place {
   __device__ __forceinline__ int part(const Groups& a) const { return a.k.shares > 1 ? slab * a.k.shares + block % a.k.shares : slab; }
 };
 
-__device__ __forceinline__ float wave_total(float v) { return wave_sum(v); }
-__device__ __forceinline__ float2 wave_total(float2 v) { return make_float2(wave_sum(v.x), wave_sum(v.y)); }
 __device__ __forceinline__ void add(float& s, float v) { s += v; }
 __device__ __forceinline__ void add(float2& s, float2 v) {
   s.x += v.x;
   s.y += v.y;
 }
+// the sum over `width` lanes (a power of two) next to each other, received by all of them
+__device__ __forceinline__ float sum_over(float v, int width) {
+  for (int o = width >> 1; o > 0; o >>= 1) v += __shfl_xor(v, o);
+  return v;
+}
+__device__ __forceinline__ float2 sum_over(float2 v, int width) { return make_float2(sum_over(v.x, width), sum_over(v.y, width)); }
+
+// f(group of the block, lane in its team) for all groups, by teams of `width` lanes; teams without one repeat the last (`there` false).
+// (By whole waves one group after another waited for LDS or memory once per group: 8 us of the 14 that 32 groups took.)
+template <typename F>
+__device__ __forceinline__ void for_groups(int groups, int width, F f) {
+  const int teams = kThreads / width, team = threadIdx.x / width, l = threadIdx.x & (width - 1);
+  for (int first = 0; first < groups; first += teams) f(std::min(first + team, groups - 1), l, first + team < groups);
+}
+
 // per group of the block, the sums over its threads of v (a value or two): result[q], read by all threads afterwards
 template <typename V>
 __device__ __forceinline__ void group_sums(const Groups& a, const Place& w, V v, V (&values)[kThreads], V (&result)[kThreads]) {
@@ -325,17 +358,17 @@ __device__ __forceinline__ void group_sums(const Groups& a, const Place& w, V v,
   __syncthreads();
   values[threadIdx.x] = v;
   __syncthreads();
-  const int lane = threadIdx.x & (kWave - 1), n = k.lanes * w.group_cols;
+  const int n = k.lanes * w.group_cols;
   const uint32_t magic = k.shares > 1 ? 0u : k.group_magic;
-  for (int q = threadIdx.x / kWave; q < w.groups; q += kWaves) {
+  for_groups(w.groups, k.team, [&](int q, int l, bool there) {
     V s = {};
-    for (int i = lane; i < n; i += kWave) {
+    for (int i = l; i < n; i += k.team) {
       const int row = k.shares > 1 ? i / w.group_cols : exact_div(i, w.group_cols, magic);
       add(s, values[row * k.block_cols + q * w.group_cols + i - row * w.group_cols]);
     }
-    s = wave_total(s);
-    if (lane == 0) result[q] = s;
-  }
+    s = sum_over(s, k.team);
+    if (l == 0 && there) result[q] = s;
+  });
   __syncthreads();
 }
 
@@ -346,31 +379,36 @@ __device__ __forceinline__ float part_count(const Groups& a, int i) {
   const int cols = k.shares > 1 ? std::min(k.block_cols, k.group_cols - share * k.block_cols) : k.group_cols;
   return (float)(std::min(k.rows, a.N - slab * k.rows)) * (float)(cols * k.E);
 }
-// mean and rstd of a whole group from its parts, by a wave
-__device__ __forceinline__ void join_statistics(const Groups& a, size_t bg, int lane, float& mean, float& rstd) {
+// mean and rstd of a whole group from its parts, by a team whose l-th lane this is; parts that a lane holds are read once
+__device__ __forceinline__ void join_statistics(const Groups& a, size_t bg, int l, int team, float& mean, float& rstd) {
   const int parts = a.k.parts();
   const float2* from = a.group_part + bg * parts;
   const float n = (float)a.N * (float)(a.k.group_cols * a.k.E);
+  float2 held[kHeldParts];
+#pragma unroll
+  for (int i = 0; i < kHeldParts; ++i) held[i] = l + i * team < parts ? from[l + i * team] : make_float2(0.f, 0.f);
   float s = 0.f;
-  for (int i = lane; i < parts; i += kWave) s += from[i].x * (part_count(a, i) / n);
-  mean = wave_sum(s);
+  const auto each = [&](auto f) {
+#pragma unroll
+    for (int i = 0; i < kHeldParts; ++i) {
+      const int at = l + i * team;
+      if (at < parts) f(held[i], part_count(a, at));
+    }
+    for (int at = l + kHeldParts * team; at < parts; at += team) f(from[at], part_count(a, at));
+  };
+  each([&](float2 v, float count) { s += v.x * (count / n); });
+  mean = sum_over(s, team);
   s = 0.f;
-  for (int i = lane; i < parts; i += kWave) {
-    const float2 v = from[i];
-    s += v.y + part_count(a, i) * (v.x - mean) * (v.x - mean);
-  }
-  rstd = 1.f / sqrtf(wave_sum(s) / n + a.eps);
+  each([&](float2 v, float count) { s += v.y + count * (v.x - mean) * (v.x - mean); });
+  rstd = 1.f / sqrtf(sum_over(s, team) / n + a.eps);
 }
-__device__ __forceinline__ float2 join_sums(const Groups& a, size_t bg, int lane) {
+__device__ __forceinline__ float2 join_sums(const Groups& a, size_t bg, int l, int team) {
   const int parts = a.k.parts();
   const float2* from = a.group_part + bg * parts;
-  float s1 = 0.f, s2 = 0.f;
-  for (int i = lane; i < parts; i += kWave) {
-    const float2 v = from[i];
-    s1 += v.x;
-    s2 += v.y;
-  }
-  return make_float2(wave_sum(s1), wave_sum(s2));
+  float2 s = make_float2(0.f, 0.f);
+#pragma unroll 4
+  for (int i = l; i < parts; i += team) add(s, from[i]);
+  return sum_over(s, team);
 }
 
 // WHOLE: the workgroup holds all of its groups' values: statistics and output in one launch
@@ -438,11 +476,11 @@ __global__ __launch_bounds__(kThreads) void norm_join_kernel(Groups a, int group
   const int bg = blockIdx.x * kWaves + threadIdx.x / kWave, lane = threadIdx.x & (kWave - 1);
   if (bg >= groups) return;
   if constexpr (BWD) {
-    const float2 s = join_sums(a, bg, lane);
+    const float2 s = join_sums(a, bg, lane, kWave);
     if (lane == 0) a.totals[bg] = s;
   } else {
     float m, r;
-    join_statistics(a, bg, lane, m, r);
+    join_statistics(a, bg, lane, kWave, m, r);
     if (lane == 0) {
       a.mean[bg] = m;
       a.rstd[bg] = r;
@@ -470,11 +508,10 @@ __global__ __launch_bounds__(kThreads) void norm_apply_kernel(Groups a) {
   const size_t bg = (size_t)w.b * a.G + w.group;
   float mean, rstd;
   if constexpr (JOIN) {
-    const int lane = threadIdx.x & (kWave - 1);
-    for (int q = threadIdx.x / kWave; q < w.groups; q += kWaves) {
+    for_groups(w.groups, k.join_team, [&](int q, int l, bool there) {
       float m, r;
-      join_statistics(a, bg + q, lane, m, r);
-      if (lane == 0) {
+      join_statistics(a, bg + q, l, k.join_team, m, r);
+      if (l == 0 && there) {
         means[q] = m;
         rstds[q] = r;
         if (w.slab == 0 && (k.shares == 1 || w.block % k.shares == 0)) {
@@ -482,7 +519,7 @@ __global__ __launch_bounds__(kThreads) void norm_apply_kernel(Groups a) {
           a.rstd[bg + q] = r;
         }
       }
-    }
+    });
     __syncthreads();
     mean = means[w.q];
     rstd = rstds[w.q];
@@ -588,11 +625,10 @@ __global__ __launch_bounds__(kThreads) void norm_bwd_apply_kernel(Groups a, Cut 
   if constexpr (JOIN) {
     Groups p = a;
     p.k = parts_cut;
-    const int lane = threadIdx.x & (kWave - 1);
-    for (int q = threadIdx.x / kWave; q < w.groups; q += kWaves) {
-      const float2 t = join_sums(p, bg + q, lane);
-      if (lane == 0) totals[q] = t;
-    }
+    for_groups(w.groups, parts_cut.join_team, [&](int q, int l, bool there) {
+      const float2 t = join_sums(p, bg + q, l, parts_cut.join_team);
+      if (l == 0 && there) totals[q] = t;
+    });
     __syncthreads();
     s = totals[w.q];
   } else {
@@ -618,7 +654,13 @@ constexpr int kHeldFew = 16;   // ... where that leaves fewer than kFullGrid wor
 constexpr long long kFullGrid = 512;
 constexpr int kJoinParts = 256;  // more parts of a group than this are put together by a launch of its own
 
-Cut cut_columns(int C, int G, int E) {
+int power_of_two(int n) {  // at least n, at most a wave
+  int p = 1;
+  while (p < n && p < kWave) p *= 2;
+  return p;
+}
+// blocks of at most `most` groups, or shares of one
+Cut cut_columns(int C, int G, int E, int most = kThreads) {
   Cut k = {};
   k.E = E;
   k.group_cols = C / G / E;
@@ -630,12 +672,13 @@ Cut cut_columns(int C, int G, int E) {
     k.blocks = G * k.shares;
   } else {
     k.shares = 1;
-    k.blocks = cdiv(G, kThreads / k.group_cols);
+    k.blocks = cdiv(G, std::min(most, kThreads / k.group_cols));
     k.block_groups = cdiv(G, k.blocks);
     k.blocks = cdiv(G, k.block_groups);
     k.block_cols = k.block_groups * k.group_cols;
   }
   k.lanes = kThreads / k.block_cols;
+  k.team = power_of_two(k.lanes * (k.block_cols / k.block_groups));
   k.cols_magic = div_magic(k.block_cols);
   k.group_magic = div_magic(k.group_cols);
   return k;
@@ -643,14 +686,27 @@ Cut cut_columns(int C, int G, int E) {
 void cut_rows(Cut& k, int N, long long rows) {
   k.rows = (int)std::min<long long>(rows, N);
   k.slabs = cdiv(N, k.rows);
+  k.join_team = power_of_two(cdiv(k.parts(), kHeldParts));
 }
 // threads hold `held` values each
 Cut cut_held(int B, int N, int C, int G, int E, int* held) {
+  // Groups that fit a workgroup's registers: as many of them as fit, fewer where that leaves CUs without a workgroup and the pieces of a
+  // token's row that it reads are not short.  One launch instead of two: 64 x 49 x 768 in 32 groups, bf16, 20.8 -> 9 us.
+  *held = kHeld;
+  const int V = kHeld / E;
+  const long long cols = C / G / E;
+  if (cols <= kThreads && cdiv(N, kThreads / cols) <= V) {
+    int most = (int)std::min<long long>(G, kThreads / cols);
+    while (most > 1 && (cdiv(N, kThreads / (int)(most * cols)) > V || ((long long)B * cdiv(G, most) < kFullGrid && most * cols > 4))) most = (most + 1) / 2;
+    Cut k = cut_columns(C, G, E, most);
+    cut_rows(k, N, (long long)V * k.lanes);
+    if (k.slabs == 1) return k;
+  }
   Cut k = cut_columns(C, G, E);
   for (int h : {kHeld, kHeldFew}) {
     *held = h;
     cut_rows(k, N, (long long)h / E * k.lanes);
-    if ((long long)B * k.blocks * k.slabs >= kFullGrid || k.slabs == 1) break;
+    if ((long long)B * k.blocks * k.slabs >= kFullGrid) break;
   }
   return k;
 }
@@ -669,11 +725,14 @@ int piece_of(const NormArgs& a, const void* y, const void* z) {
   return a.C / a.G % E == 0 && aligned16(a.x) && aligned16(a.gamma) && aligned16(a.beta) && aligned16(y) && aligned16(z) ? E : 1;
 }
 
-// Rows that the row kernels hold: LANES x PIECES pieces, at most 16 pieces of single values and 4 of 16 bytes a lane.
-bool rows_fit(int N, int C, int G, int E) { return N == 1 && G == 1 && cdiv(C, E) <= kWave * (E == 1 ? 16 : 4); }
+// Rows that the row kernels hold: at most 4 pieces of 16 bytes or 16 single values a lane; by a wave as long as that is enough.
+int most_pieces(int E) { return E == 1 ? 16 : 4; }
+bool rows_fit(int N, int C, int G, int E) { return N == 1 && G == 1 && cdiv(C, E) <= kThreads * most_pieces(E); }
 int row_lanes(int C, int E) {
+  const int pieces = cdiv(C, E);
+  if (pieces > kWave * most_pieces(E)) return kThreads;
   int lanes = 4;
-  while (lanes < kWave && lanes * E < C) lanes *= 2;
+  while (lanes < kWave && lanes < pieces) lanes *= 2;
   return lanes;
 }
 int rows_bwd_blocks(int rows) { return std::min(cdiv(rows, 16), 1024); }
@@ -686,6 +745,7 @@ hipError_t for_row_shape(int C, int E, F f) {
   if (lanes == 8) return f(integral_constant<int, 8>(), integral_constant<int, 1>());
   if (lanes == 16) return f(integral_constant<int, 16>(), integral_constant<int, 1>());
   if (lanes == 32) return f(integral_constant<int, 32>(), integral_constant<int, 1>());
+  if (lanes == kThreads) return pieces <= 2 ? f(integral_constant<int, kThreads>(), integral_constant<int, 2>()) : pieces <= 4 ? f(integral_constant<int, kThreads>(), integral_constant<int, 4>()) : f(integral_constant<int, kThreads>(), integral_constant<int, 16>());
   if (pieces == 1) return f(integral_constant<int, 64>(), integral_constant<int, 1>());
   if (pieces == 2) return f(integral_constant<int, 64>(), integral_constant<int, 2>());
   if (pieces <= 4) return f(integral_constant<int, 64>(), integral_constant<int, 4>());

@@ -240,7 +240,8 @@ def test_linear_leading_dimensions_and_values_that_are_not_finite():
 NORM = [  # B, N, C, groups
     (1, 1, 1, 1), (3, 1, 8, 1), (5, 1, 64, 1), (130, 1, 256, 1), (7, 1, 100, 1), (33, 1, 768, 1), (9, 1, 2304, 1), (2, 1, 5000, 1), (4, 1, 96, 4),
     (2, 1, 20000, 1), (2, 17, 24, 3), (3, 50, 33, 11), (2, 1000, 64, 8), (1, 4097, 96, 12), (2, 300, 40, 1), (1, 70, 2056, 1), (65, 2, 16, 16),
-    (3, 700, 12, 12), (1, 9, 4112, 257), (2, 2, 48, 3), (300, 3, 64, 1), (1, 33000, 16, 2),
+    (3, 700, 12, 12), (1, 9, 4112, 257), (2, 2, 48, 3), (300, 3, 64, 1), (1, 33000, 16, 2), (300, 1, 2047, 1), (2100, 1, 1030, 1), (17, 1, 4096, 1),
+    (4, 49, 768, 32), (3, 500, 64, 8), (1, 20000, 24, 3), (2, 2500, 256, 32),
 ]
 
 
