@@ -629,32 +629,38 @@ def _act_code(act: str) -> int:
     return code
 
 
-def _one_device(first: torch.Tensor, *others: Optional[torch.Tensor]) -> None:
-    """All tensors on the current device, whose current stream the call runs on."""
-    if not first.is_cuda:
+def _current(t: torch.Tensor) -> int:
+    """The current device, on whose current stream a call runs and where all of its tensors have to be."""
+    if not t.is_cuda:
         raise ValueError("tensors must be device tensors")
-    index = first.get_device()
-    current = torch.cuda.current_device() if _raw_device is None else _raw_device()
-    if index != current:
-        raise ValueError(f"tensors are on device {index}, but device {current} is current")
-    for t in others:
-        if t is not None and t.get_device() != index:
-            raise ValueError(f"tensors must share one device, got {index} and {t.get_device()}")
+    return torch.cuda.current_device() if _raw_device is None else _raw_device()
 
 
-def _rng_ptr(rng: Optional[torch.Tensor], p: float):
+def _on(index: int, t: torch.Tensor, name: str, dtype, shape=None) -> int:
+    """t's address, t being contiguous, on device `index`, of this type and shape."""
+    if t.get_device() == index and t.dtype == dtype and (shape is None or t.shape == shape) and t.is_contiguous():
+        return t.data_ptr()
+    _dev(t, name, dtype, shape)
+    raise ValueError(f"{name} is on device {t.get_device()}, but device {index} is current")
+
+
+def _rng_on(index: int, rng: Optional[torch.Tensor], p: float) -> Optional[int]:
     """The generator's state, (seed, call number) in device memory; not needed where p is 0."""
-    if rng is None:
-        if p:
-            raise ValueError("dropout needs rng, [2] int64 on the device: seed, call number")
-        return None
-    return _dev(rng, "rng", torch.int64, (2,)).data_ptr()
+    if rng is not None:
+        return _on(index, rng, "rng", torch.int64, (2,))
+    if p:
+        raise ValueError("dropout needs rng, [2] int64 on the device: seed, call number")
+    return None
 
 
-def _own_workspace(workspace: Optional[torch.Tensor], need: int, device) -> Tuple[Optional[torch.Tensor], int]:
+def _workspace_on(index: int, workspace: Optional[torch.Tensor], need: int, device) -> Tuple[Optional[torch.Tensor], Optional[int], int]:
+    """The given workspace or one of the call's own (which the caller of this holds on to), its address and size."""
     if workspace is None:
-        workspace = _workspace(need, device)
-    return workspace, 0 if workspace is None else workspace.numel() * workspace.element_size()
+        if need == 0:
+            return None, None, 0
+        workspace = torch.empty(need, dtype=torch.uint8, device=device)
+        return workspace, workspace.data_ptr(), need
+    return workspace, _on(index, workspace, "workspace", workspace.dtype), workspace.numel() * workspace.element_size()
 
 
 def affmae_linear_fwd(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] = None,
@@ -665,30 +671,32 @@ def affmae_linear_fwd(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torc
     which the backward of an activation needs, or None unless asked for).
 
     x [..., Cin], weight [Cout,Cin], bias [Cout], residual [..., Cout] in one dtype; act "none", "relu", "gelu" (exact) or
-    "silu"; p: probability of dropout, with rng [2] int64 on the device (seed, call number)."""
+    "silu"; p: probability of dropout, with rng [2] int64 on the device (seed, call number).  out may be residual."""
     lib = load_library()
+    dtype = x.dtype
     code = _dtype_code(x)
-    _one_device(x, weight, bias, residual, rng, out, pre)
-    _dev(x, "x")
-    _dev(weight, "weight", x.dtype)
+    dev = _current(x)
     if x.dim() < 1 or weight.dim() != 2 or x.shape[-1] != weight.shape[1]:
         raise ValueError(f"x must be [..., Cin] and weight [Cout, Cin], got {tuple(x.shape)} and {tuple(weight.shape)}")
     Cout, Cin = weight.shape
     shape = x.shape[:-1] + (Cout,)
-    if bias is not None:
-        _dev(bias, "bias", x.dtype, (Cout,))
-    if residual is not None:
-        _dev(residual, "residual", x.dtype, shape)
+    x_at = _on(dev, x, "x", dtype)
+    w_at = _on(dev, weight, "weight", dtype)
+    bias_at = None if bias is None else _on(dev, bias, "bias", dtype, (Cout,))
+    res_at = None if residual is None else _on(dev, residual, "residual", dtype, shape)
     if out is None:
-        out = torch.empty(shape, dtype=x.dtype, device=x.device)
+        out = x.new_empty(shape)
+        out_at = out.data_ptr()
     else:
-        _dev(out, "out", x.dtype, shape)
+        out_at = _on(dev, out, "out", dtype, shape)
+    pre_at = None
     if pre is not None:
-        _dev(pre, "pre", x.dtype, shape)
+        pre_at = _on(dev, pre, "pre", dtype, shape)
     elif want_pre:
         pre = torch.empty_like(out)
-    rc = lib.affmae_linear_fwd(_ptr(x), _ptr(weight), _ptr(bias), _ptr(residual), x.numel() // max(Cin, 1), Cin, Cout,
-                               _act_code(act), float(p), _rng_ptr(rng, p), code, _ptr(out), _ptr(pre), _stream())
+        pre_at = pre.data_ptr()
+    rc = lib.affmae_linear_fwd(x_at, w_at, bias_at, res_at, x.numel() // max(Cin, 1), Cin, Cout, _act_code(act), float(p),
+                               _rng_on(dev, rng, p), code, out_at, pre_at, _stream())
     if rc != 0:
         raise AffmaeError("affmae_linear_fwd", rc)
     return out, pre
@@ -702,38 +710,40 @@ def affmae_linear_bwd(x: Optional[torch.Tensor], weight: Optional[torch.Tensor],
     """Gradients of affmae_linear_fwd -> dict(dx [..., Cin], dweight [Cout,Cin], dbias [Cout]), those asked for, in dout's dtype
     (dbias comes with dweight only).  weight is needed for dx, x for dweight, pre with an activation; p and rng as in the forward."""
     lib = load_library()
+    dtype = dout.dtype
     code = _dtype_code(dout)
-    g = dict(grads) if grads else {}
-    _one_device(dout, x, weight, pre, rng, workspace, *g.values())
-    _dev(dout, "dout")
+    dev = _current(dout)
     if (x is None and want_dweight) or (weight is None and want_dx) or not (want_dx or want_dweight):
         raise ValueError("dweight needs x, dx needs weight, and one of them must be asked for")
     if dout.dim() < 1:
         raise ValueError("dout must be [..., Cout]")
+    rows = dout.shape[:-1]
     Cout = dout.shape[-1]
     Cin = weight.shape[-1] if x is None else x.shape[-1]
-    if x is not None:
-        _dev(x, "x", dout.dtype, dout.shape[:-1] + (Cin,))
-    if weight is not None:
-        _dev(weight, "weight", dout.dtype, (Cout, Cin))
-    if pre is not None:
-        _dev(pre, "pre", dout.dtype, dout.shape)
-    elif act != "none":
+    dout_at = _on(dev, dout, "dout", dtype)
+    x_at = None if x is None else _on(dev, x, "x", dtype, rows + (Cin,))
+    w_at = None if weight is None else _on(dev, weight, "weight", dtype, (Cout, Cin))
+    if pre is None and act != "none":
         raise ValueError("an activation's backward needs pre")
-    want_dbias = want_dbias and want_dweight
-    for name, shape, wanted in (("dx", dout.shape[:-1] + (Cin,), want_dx), ("dweight", (Cout, Cin), want_dweight), ("dbias", (Cout,), want_dbias)):
-        if wanted:
-            if name not in g:
-                g[name] = torch.empty(shape, dtype=dout.dtype, device=dout.device)
-            else:
-                _dev(g[name], name, dout.dtype, shape)
-    rows = dout.numel() // max(Cout, 1)
+    pre_at = None if pre is None else _on(dev, pre, "pre", dtype, dout.shape)
+    g = dict(grads) if grads else {}
+
+    def grad(name, shape):
+        if name in g:
+            return _on(dev, g[name], name, dtype, shape)
+        t = g[name] = dout.new_empty(shape)
+        return t.data_ptr()
+
+    dx_at = grad("dx", rows + (Cin,)) if want_dx else None
+    dw_at = grad("dweight", (Cout, Cin)) if want_dweight else None
+    db_at = grad("dbias", (Cout,)) if want_dweight and want_dbias else None
+    n = dout.numel() // max(Cout, 1)
     a = _act_code(act)
-    need = lib.affmae_linear_bwd_workspace_bytes(rows, Cin, Cout, a, float(p), code, int(want_dx), int(want_dweight))
-    workspace, size = _own_workspace(workspace, need, dout.device)
-    rc = lib.affmae_linear_bwd(_ptr(x), _ptr(weight), _ptr(pre), _ptr(dout), rows, Cin, Cout, a, float(p), _rng_ptr(rng, p), code,
-                               _ptr(g["dx"]) if want_dx else None, _ptr(g["dweight"]) if want_dweight else None,
-                               _ptr(g["dbias"]) if want_dbias else None, _ptr(workspace), size, _stream())
+    p = float(p)
+    need = lib.affmae_linear_bwd_workspace_bytes(n, Cin, Cout, a, p, code, want_dx, want_dweight)
+    workspace, ws_at, size = _workspace_on(dev, workspace, need, dout.device)
+    rc = lib.affmae_linear_bwd(x_at, w_at, pre_at, dout_at, n, Cin, Cout, a, p, _rng_on(dev, rng, p), code, dx_at, dw_at, db_at,
+                               ws_at, size, _stream())
     if rc != 0:
         raise AffmaeError("affmae_linear_bwd", rc)
     return g
@@ -746,32 +756,33 @@ def affmae_norm_fwd(x: torch.Tensor, gamma: Optional[torch.Tensor], beta: Option
     """Group norm with an activation, channels last: x [B,N,C] -> (out [B,N,C] in x's dtype, mean [B,groups] fp32,
     rstd [B,groups] fp32).  The layer norm of every token: x.view(-1, 1, C) with one group.  gamma, beta [C] or both None."""
     lib = load_library()
+    dtype = x.dtype
     code = _dtype_code(x)
-    _one_device(x, gamma, beta, out, mean, rstd, workspace)
-    _dev(x, "x")
+    dev = _current(x)
     if x.dim() != 3:
         raise ValueError(f"x must be [B,N,C], got {tuple(x.shape)}")
     B, N, C = x.shape
     if (gamma is None) != (beta is None):
         raise ValueError("gamma and beta are given together or not at all")
-    if gamma is not None:
-        _dev(gamma, "gamma", x.dtype, (C,))
-        _dev(beta, "beta", x.dtype, (C,))
+    x_at = _on(dev, x, "x", dtype)
+    gamma_at = None if gamma is None else _on(dev, gamma, "gamma", dtype, (C,))
+    beta_at = None if beta is None else _on(dev, beta, "beta", dtype, (C,))
     if out is None:
         out = torch.empty_like(x)
+        out_at = out.data_ptr()
     else:
-        _dev(out, "out", x.dtype, x.shape)
+        out_at = _on(dev, out, "out", dtype, x.shape)
+    shape = (B, max(groups, 0))
     if mean is None:
-        mean = torch.empty((B, max(groups, 0)), dtype=torch.float32, device=x.device)
-    else:
-        _dev(mean, "mean", torch.float32, (B, groups))
+        mean = torch.empty(shape, dtype=torch.float32, device=x.device)
     if rstd is None:
-        rstd = torch.empty((B, max(groups, 0)), dtype=torch.float32, device=x.device)
-    else:
-        _dev(rstd, "rstd", torch.float32, (B, groups))
-    workspace, size = _own_workspace(workspace, lib.affmae_norm_fwd_workspace_bytes(B, N, C, groups, code), x.device)
-    rc = lib.affmae_norm_fwd(_ptr(x), _ptr(gamma), _ptr(beta), B, N, C, groups, float(eps), _act_code(act), code, _ptr(out), _ptr(mean),
-                             _ptr(rstd), _ptr(workspace), size, _stream())
+        rstd = torch.empty_like(mean)
+    mean_at = _on(dev, mean, "mean", torch.float32, shape)
+    rstd_at = _on(dev, rstd, "rstd", torch.float32, shape)
+    need = lib.affmae_norm_fwd_workspace_bytes(B, N, C, groups, code)
+    workspace, ws_at, size = _workspace_on(dev, workspace, need, x.device)
+    rc = lib.affmae_norm_fwd(x_at, gamma_at, beta_at, B, N, C, groups, float(eps), _act_code(act), code, out_at, mean_at, rstd_at,
+                             ws_at, size, _stream())
     if rc != 0:
         raise AffmaeError("affmae_norm_fwd", rc)
     return out, mean, rstd
@@ -783,32 +794,35 @@ def affmae_norm_bwd(x: torch.Tensor, gamma: Optional[torch.Tensor], beta: Option
                     ) -> Dict[str, torch.Tensor]:
     """Gradients of affmae_norm_fwd -> dict(dx [B,N,C] in x's dtype[, dgamma, dbeta [C] fp32: with gamma])."""
     lib = load_library()
+    dtype = x.dtype
     code = _dtype_code(x)
-    g = dict(grads) if grads else {}
-    _one_device(x, gamma, beta, mean, rstd, dout, workspace, *g.values())
-    _dev(x, "x")
+    dev = _current(x)
     if x.dim() != 3:
         raise ValueError(f"x must be [B,N,C], got {tuple(x.shape)}")
     B, N, C = x.shape
     if (gamma is None) != (beta is None):
         raise ValueError("gamma and beta are given together or not at all")
-    shapes = {"dx": (x.shape, x.dtype)}
-    if gamma is not None:
-        _dev(gamma, "gamma", x.dtype, (C,))
-        _dev(beta, "beta", x.dtype, (C,))
-        shapes["dgamma"] = shapes["dbeta"] = ((C,), torch.float32)
-    _dev(mean, "mean", torch.float32, (B, groups))
-    _dev(rstd, "rstd", torch.float32, (B, groups))
-    _dev(dout, "dout", x.dtype, x.shape)
-    for name, (shape, dtype) in shapes.items():
-        if name not in g:
-            g[name] = torch.empty(shape, dtype=dtype, device=x.device)
-        else:
-            _dev(g[name], name, dtype, shape)
-    workspace, size = _own_workspace(workspace, lib.affmae_norm_bwd_workspace_bytes(B, N, C, groups, code), x.device)
-    rc = lib.affmae_norm_bwd(_ptr(x), _ptr(gamma), _ptr(beta), _ptr(mean), _ptr(rstd), _ptr(dout), B, N, C, groups, _act_code(act), code,
-                             _ptr(g["dx"]), _ptr(g["dgamma"]) if gamma is not None else None,
-                             _ptr(g["dbeta"]) if gamma is not None else None, _ptr(workspace), size, _stream())
+    x_at = _on(dev, x, "x", dtype)
+    gamma_at = None if gamma is None else _on(dev, gamma, "gamma", dtype, (C,))
+    beta_at = None if beta is None else _on(dev, beta, "beta", dtype, (C,))
+    mean_at = _on(dev, mean, "mean", torch.float32, (B, groups))
+    rstd_at = _on(dev, rstd, "rstd", torch.float32, (B, groups))
+    dout_at = _on(dev, dout, "dout", dtype, x.shape)
+    g = dict(grads) if grads else {}
+
+    def grad(name, like, shape, type_):
+        if name in g:
+            return _on(dev, g[name], name, type_, shape)
+        t = g[name] = torch.empty_like(like, dtype=type_)
+        return t.data_ptr()
+
+    dx_at = grad("dx", x, x.shape, dtype)
+    dgamma_at = None if gamma is None else grad("dgamma", gamma, (C,), torch.float32)
+    dbeta_at = None if gamma is None else grad("dbeta", beta, (C,), torch.float32)
+    need = lib.affmae_norm_bwd_workspace_bytes(B, N, C, groups, code)
+    workspace, ws_at, size = _workspace_on(dev, workspace, need, x.device)
+    rc = lib.affmae_norm_bwd(x_at, gamma_at, beta_at, mean_at, rstd_at, dout_at, B, N, C, groups, _act_code(act), code, dx_at,
+                             dgamma_at, dbeta_at, ws_at, size, _stream())
     if rc != 0:
         raise AffmaeError("affmae_norm_bwd", rc)
     return g
@@ -820,15 +834,13 @@ def affmae_dropout_fwd(x: torch.Tensor, p: float, rng: Optional[torch.Tensor] = 
     out may be x or residual."""
     lib = load_library()
     code = _dtype_code(x)
-    _one_device(x, rng, residual, out)
-    _dev(x, "x")
-    if residual is not None:
-        _dev(residual, "residual", x.dtype, x.shape)
+    dev = _current(x)
+    x_at = _on(dev, x, "x", x.dtype)
+    res_at = None if residual is None else _on(dev, residual, "residual", x.dtype, x.shape)
     if out is None:
         out = torch.empty_like(x)
-    else:
-        _dev(out, "out", x.dtype, x.shape)
-    rc = lib.affmae_dropout_fwd(_ptr(x), _ptr(residual), x.numel(), float(p), _rng_ptr(rng, p), code, _ptr(out), _stream())
+    out_at = _on(dev, out, "out", x.dtype, x.shape)
+    rc = lib.affmae_dropout_fwd(x_at, res_at, x.numel(), float(p), _rng_on(dev, rng, p), code, out_at, _stream())
     if rc != 0:
         raise AffmaeError("affmae_dropout_fwd", rc)
     return out
@@ -839,13 +851,12 @@ def affmae_dropout_bwd(dout: torch.Tensor, p: float, rng: Optional[torch.Tensor]
     """Gradient of affmae_dropout_fwd in x, with the same p and rng; dx may be dout.  (The gradient in residual is dout.)"""
     lib = load_library()
     code = _dtype_code(dout)
-    _one_device(dout, rng, dx)
-    _dev(dout, "dout")
+    dev = _current(dout)
+    dout_at = _on(dev, dout, "dout", dout.dtype)
     if dx is None:
         dx = torch.empty_like(dout)
-    else:
-        _dev(dx, "dx", dout.dtype, dout.shape)
-    rc = lib.affmae_dropout_bwd(_ptr(dout), dout.numel(), float(p), _rng_ptr(rng, p), code, _ptr(dx), _stream())
+    dx_at = _on(dev, dx, "dx", dout.dtype, dout.shape)
+    rc = lib.affmae_dropout_bwd(dout_at, dout.numel(), float(p), _rng_on(dev, rng, p), code, dx_at, _stream())
     if rc != 0:
         raise AffmaeError("affmae_dropout_bwd", rc)
     return dx

@@ -690,17 +690,22 @@ void cut_rows(Cut& k, int N, long long rows) {
 }
 // threads hold `held` values each
 Cut cut_held(int B, int N, int C, int G, int E, int* held) {
-  // Groups that fit a workgroup's registers: as many of them as fit, fewer where that leaves CUs without a workgroup and the pieces of a
-  // token's row that it reads are not short.  One launch instead of two: 64 x 49 x 768 in 32 groups, bf16, 20.8 -> 9 us.
+  // Groups that fit a workgroup's registers: one launch instead of two (64 x 49 x 768 in 32 groups, bf16: 9.5 us instead of 20.8).  As many
+  // of them as fit, fewer where that leaves CUs without a workgroup, but no less than 8 pieces of a token's row: 64 x 1024 x 256 in 32
+  // groups, bf16, two pieces a workgroup, takes 31.6 us.
   *held = kHeld;
   const int V = kHeld / E;
   const long long cols = C / G / E;
-  if (cols <= kThreads && cdiv(N, kThreads / cols) <= V) {
+  if (cols <= kThreads) {
+    const int least = (int)std::min<long long>(G, cdiv(8, cols));
     int most = (int)std::min<long long>(G, kThreads / cols);
-    while (most > 1 && (cdiv(N, kThreads / (int)(most * cols)) > V || ((long long)B * cdiv(G, most) < kFullGrid && most * cols > 4))) most = (most + 1) / 2;
-    Cut k = cut_columns(C, G, E, most);
-    cut_rows(k, N, (long long)V * k.lanes);
-    if (k.slabs == 1) return k;
+    const auto fits = [&](int groups) { return cdiv(N, kThreads / (int)(groups * cols)) <= V; };
+    while (most > least && (!fits(most) || (long long)B * cdiv(G, most) < kFullGrid)) most = std::max(least, (most + 1) / 2);
+    if (most >= least && fits(most)) {
+      Cut k = cut_columns(C, G, E, most);
+      cut_rows(k, N, (long long)V * k.lanes);
+      if (k.slabs == 1) return k;
+    }
   }
   Cut k = cut_columns(C, G, E);
   for (int h : {kHeld, kHeldFew}) {
