@@ -487,8 +487,8 @@ int affmae_dropout_bwd(const void* dout, int64_t n, float p, const int64_t* rng,
  *   may be NULL otherwise.
  *   workspace  affmae_linear_bwd_workspace_bytes(...) bytes, may be 0
  *
- * Limits: rows <= 2^30, Cin, Cout <= 2^20, rows * Cin and rows * Cout <= 2^35
- * (AFFMAE_ERR_UNSUPPORTED beyond).  Any sizes and any alignment (to the element) run;
+ * Limits: rows <= 2^29, Cin, Cout <= 2^20, rows * Cin, rows * Cout and Cin * Cout
+ * <= 2^35 (AFFMAE_ERR_UNSUPPORTED beyond).  Any sizes and any alignment (to the element) run;
  * rows of whole 16-byte pieces in 16-byte aligned tensors are the fastest.
  * Errors: AFFMAE_ERR_NULL, AFFMAE_ERR_DTYPE, AFFMAE_ERR_SHAPE (sizes < 1, unknown act,
  * p outside [0, 1), misaligned tensors), AFFMAE_ERR_UNSUPPORTED, AFFMAE_ERR_WORKSPACE.
@@ -524,7 +524,7 @@ int affmae_linear_bwd(const void* x, const void* weight, const void* pre, const 
  * Statistics and sums are fp32, added in a fixed order; a variance is the mean square
  * about the mean (never a difference of squares), so that offsets large against the
  * spread cost no digits.
- * Limits: groups divides C <= 2^20, B*N below 2^31 - 8, B*groups <= 2^24
+ * Limits: groups divides C <= 2^20, B*N below 2^31 - 8, B*groups <= 2^24, B*N*C <= 2^38
  * (AFFMAE_ERR_UNSUPPORTED beyond).  Any sizes and any alignment (to the element) run;
  * C / groups a multiple of 8 (bf16) or 4 (fp32) in 16-byte aligned tensors runs the
  * fastest kernels.

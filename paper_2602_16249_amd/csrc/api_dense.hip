@@ -28,8 +28,8 @@ int check_linear_shape(int rows, int Cin, int Cout, int act, int dtype) {
   if (rc != AFFMAE_OK) return rc;
   if (rows < 1 || Cin < 1 || Cout < 1 || bad_act(act)) return AFFMAE_ERR_SHAPE;
   // a tile's rows are addressed from its first one with 32-bit offsets; the runtime counts the threads of a launch in 32 bits
-  if (rows > (1 << 30) || Cin > (1 << 20) || Cout > (1 << 20)) return AFFMAE_ERR_UNSUPPORTED;
-  if ((long long)rows * Cin > (1ll << 35) || (long long)rows * Cout > (1ll << 35)) return AFFMAE_ERR_UNSUPPORTED;
+  if (rows > (1 << 29) || Cin > (1 << 20) || Cout > (1 << 20)) return AFFMAE_ERR_UNSUPPORTED;
+  if ((long long)rows * Cin > (1ll << 35) || (long long)rows * Cout > (1ll << 35) || (long long)Cin * Cout > (1ll << 35)) return AFFMAE_ERR_UNSUPPORTED;
   return AFFMAE_OK;
 }
 

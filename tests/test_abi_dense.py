@@ -26,8 +26,9 @@ def test_linear_forward_refuses():
         assert fwd(**{name: P + 1}) == -2, name
         assert fwd(dtype=0, **{name: P + 2}) == -2, name
     assert fwd(dtype=2) == -3
-    assert fwd(Cin=(1 << 20) + 1) == -5 and fwd(Cout=(1 << 20) + 1) == -5 and fwd(rows=(1 << 30) + 1) == -5
-    assert fwd(rows=1 << 30, Cin=64) == -5 and fwd(rows=1 << 30, Cout=64) == -5
+    assert fwd(Cin=(1 << 20) + 1) == -5 and fwd(Cout=(1 << 20) + 1) == -5 and fwd(rows=(1 << 29) + 1) == -5
+    assert fwd(rows=1 << 29, Cin=65) == -5 and fwd(rows=1 << 29, Cout=65) == -5
+    assert fwd(Cin=1 << 18, Cout=(1 << 17) + 1) == -5
 
 
 def test_linear_backward_refuses():

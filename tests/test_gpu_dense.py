@@ -213,6 +213,45 @@ def test_linear_of_many_rows(dtype):
     assert all(torch.equal(got[k], again[k]) for k in got)
 
 
+@pytest.mark.parametrize("rows,cin,cout", [(16400, 776, 2312), (65552, 264, 264), (8200, 392, 1160), (20008, 264, 136)])
+def test_linear_of_large_tiles(rows, cin, cout):
+    """Sizes at which the larger tiles are taken, a little beyond whole tiles and slices, against products in 64 bits on the device."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(rows)
+    normal = lambda *shape, std=1.0: (torch.randn(*shape, generator=g, device="cuda") * std).bfloat16()
+    x, w, b, r, dout, pre = (normal(rows, cin), normal(cout, cin, std=cin ** -0.5), normal(cout, std=0.3), normal(rows, cout), normal(rows, cout),
+                             normal(rows, cout, std=1.5))
+    p, f = 0.2, 1.0 / (1.0 - float(np.float32(0.2)))
+    keep = torch.from_numpy(dense.keep((rows, cout), p, *SEED)).cuda()
+    cdf = lambda z: 0.5 * torch.special.erfc(-z * 2 ** -0.5)
+    half = HALF["bf16"]
+
+    def close(got, ref, tol, what):
+        over = ~((got.double() - ref).abs() <= tol + half * (ref.abs() + tol))
+        assert not bool(over.any()), f"{what}: {int(over.sum())} of {over.numel()} off, first at {over.nonzero()[0].tolist()}"
+
+    out, z = aff.affmae_linear_fwd(x, w, b, r, act="gelu", p=p, rng=_rng(), want_pre=True)
+    xd, wt = x.double(), w.double().t().contiguous()
+    rz = xd @ wt + b.double()
+    dz = 2 * U * (cin + 5) * (xd.abs() @ wt.abs() + b.double().abs())
+    close(z, rz, dz, "pre")
+    branch = torch.where(keep, rz * cdf(rz) * f, 0.0)
+    d = f * (SLOPE * dz + 8 * U * (1 + rz.abs())) + 4 * U * f * rz.abs() + U * (r.double().abs() + (r.double() + branch).abs())
+    close(out, r.double() + branch, d, "out")
+    del xd, wt, rz, dz, branch, d
+    got = aff.affmae_linear_bwd(x, w, dout, pre, act="gelu", p=p, rng=_rng())
+    pd = pre.double()
+    z = torch.where(keep, dout.double() * f, 0.0) * (cdf(pd) + pd * torch.exp(-0.5 * pd * pd) * (2 * np.pi) ** -0.5)
+    e = 4 * U * z.abs() + 8 * U * f * dout.double().abs() * (1 + pd.abs())
+    e = e + half * (z.abs() + e)
+    a = z.abs() + e
+    wd, xd = w.double(), x.double()
+    close(got["dx"], z @ wd, e @ wd.abs() + 2 * U * (cout + 5) * (a @ wd.abs()), "dx")
+    zt, et, at = z.t().contiguous(), e.t().contiguous(), a.t().contiguous()
+    close(got["dweight"], zt @ xd, et @ xd.abs() + 2 * U * (rows + 5) * (at @ xd.abs()), "dweight")
+    close(got["dbias"], zt.sum(1), et.sum(1) + 2 * U * (rows + 5) * at.sum(1), "dbias")
+
+
 def test_linear_leading_dimensions_and_values_that_are_not_finite():
     d = _linear_inputs("f32", 24, 16, 20, 6)
     x, w, b = (d[k][0] for k in "xwb")
@@ -463,6 +502,51 @@ def test_dropout_of_more_than_2_32_elements():
     assert np.array_equal(x[:1000].float().cpu().numpy() != 0, words >= np.uint64(2 ** 31))
 
 
+def test_linear_beyond_2_31_values():
+    """Tensors of more than 2^31 values.  Whole numbers of at most two digits: every sum is exact, whatever its order."""
+    rows, cin, cout = 33_600_005, 64, 72
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    small = lambda *shape: torch.randint(-1, 2, shape, generator=g, device="cuda", dtype=torch.int8).bfloat16()
+    x, w, dout = small(rows, cin), small(cout, cin), small(rows, cout)
+    out, _ = aff.affmae_linear_fwd(x, w)
+    for lo in (0, rows // 2, rows - 4099):
+        assert torch.equal(out[lo:lo + 4099].float(), x[lo:lo + 4099].float() @ w.float().t())
+    del out
+    got = aff.affmae_linear_bwd(x, w, dout, dout, act="relu")  # dz: dout where it is 1
+    for lo in (0, rows // 2, rows - 4099):
+        assert torch.equal(got["dx"][lo:lo + 4099].float(), (dout[lo:lo + 4099] > 0).float() @ w.float())
+    dw, db = torch.zeros(cout, cin, dtype=torch.float64, device="cuda"), torch.zeros(cout, dtype=torch.float64, device="cuda")
+    for lo in range(0, rows, 1 << 22):
+        z = (dout[lo:lo + (1 << 22)] > 0).double()
+        dw += z.t().contiguous() @ x[lo:lo + (1 << 22)].double()
+        db += z.sum(0)
+    assert float(dw.abs().max()) < 2 ** 24 and float(db.max()) < 2 ** 24
+    assert torch.equal(got["dweight"], dw.bfloat16()) and torch.equal(got["dbias"], db.bfloat16())
+
+
+def test_norm_beyond_2_31_values():
+    """-1, 1, -1, ... in tensors of more than 2^31 values: mean 0 and variance 1, exactly."""
+    for B, N, C, G in ((2, 9_000_005, 128, 4), (16_777_215, 1, 136, 1)):
+        x = torch.ones(B, N, C, dtype=torch.bfloat16, device="cuda")
+        x[..., ::2] = -1
+        gamma, beta = torch.full((C,), 3.0, device="cuda").bfloat16(), torch.zeros(C, device="cuda").bfloat16()
+        out, mean, rstd = aff.affmae_norm_fwd(x, gamma, beta, G, eps=1e-5)
+        assert bool((mean == 0).all()) and bool(((rstd - (1 + 1e-5) ** -0.5).abs() < 4 * U).all())
+        want = x.view(-1)[:C] * 3
+        for lo in (0, B * N // 2, B * N - 5000):
+            assert torch.equal(out.view(-1, C)[lo:lo + 5000], want.expand(5000, C))
+        del out
+        # dout = x: dh = 3 x = 3 xhat (up to eps), so dx is 3 x (1 - 1 / (1 + eps)) rstd; dgamma counts the tokens, dbeta too, with signs
+        got = aff.affmae_norm_bwd(x, gamma, beta, mean, rstd, x, G)
+        for lo in (0, B * N // 2, B * N - 5000):
+            assert float(got["dx"].view(-1, C)[lo:lo + 5000].float().abs().max()) < 1e-4
+        tokens = float(B * N)
+        assert float((got["dgamma"].double() / tokens - (1 + 1e-5) ** -0.5).abs().max()) < _sum_error(B * N)
+        assert float((got["dbeta"].double() / tokens - x.view(-1)[:C].double()).abs().max()) < _sum_error(B * N)
+        del got, x
+
+
 # -------------------------------------------------------------------------------------------------------------- refusals
 
 def test_binding_refuses():
@@ -620,6 +704,40 @@ def test_block_replayed_from_a_graph_on_another_stream():
             assert torch.allclose(g[k].float(), eg[k].float(), rtol=2e-2, atol=atol), f"replay {rep}: {k}"
         seen.append(y.clone())
     assert all(not torch.equal(a, b) for a, b in zip(seen, seen[1:]))
+
+
+def test_large_products_replayed_from_a_graph():
+    """Tiles of more than 64 KB of LDS, k split over workgroups, statistics of several launches: replays with new inputs, eager work of the
+    same calls between them."""
+    rows, cin, cout = 16400, 776, 2312
+    x, w, dout, pre = (torch.randn(*s, device="cuda").bfloat16() for s in ((rows, cin), (cout, cin), (rows, cout), (rows, cout)))
+    nx, nd, gamma, beta = (torch.randn(*s, device="cuda") for s in ((2, 9000, 48), (2, 9000, 48), (48,), (48,)))
+    rng = _rng()
+
+    def run():
+        out, _ = aff.affmae_linear_fwd(x, w, act="silu", p=0.5, rng=rng)
+        g = aff.affmae_linear_bwd(x, w, dout, pre, act="silu", p=0.5, rng=rng)
+        y, m, r = aff.affmae_norm_fwd(nx, gamma, beta, 6, act="gelu")
+        h = aff.affmae_norm_bwd(nx, gamma, beta, m, r, nd, 6, act="gelu")
+        return [out, y, m, r, aff.affmae_dropout_fwd(nx, 0.3, rng), *g.values(), *h.values()]
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        run()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        got = run()
+    for rep in range(3):
+        rng[1] += 1
+        x.mul_(0.5)
+        nx.add_(1.0)
+        ref = run()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, ref)), f"replay {rep}"
 
 
 def test_calls_on_two_streams_at_once():
