@@ -34,15 +34,16 @@ __device__ __forceinline__ i32x4 uniform(i32x4 v) {
 }
 
 // From a buffer straight into LDS (lane l's bytes land at dst + W l).  By hand: for the compiler every LDS read might read what
-// such a load still writes, and it would wait for what is on its way before it reads what is there.
+// such a load still writes, and it would wait for what is on its way before it reads what is there.  (The waits: m0 for the load, and five
+// states between a vector instruction that writes a scalar of `rsrc` and the load, which the compiler does not see in here.)
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"  // (m0 is reserved: written only for the next instruction, never held)
 template <int W>
 __device__ __forceinline__ void lds_load(uint32_t dst, i32x4 rsrc, uint32_t off) {
   if constexpr (W == 16)
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(dst), "v"(off), "s"(rsrc) : "m0", "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(dst), "v"(off), "s"(rsrc) : "m0", "memory");
   else
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(dst), "v"(off), "s"(rsrc) : "m0", "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(dst), "v"(off), "s"(rsrc) : "m0", "memory");
 }
 #pragma clang diagnostic pop
 __device__ __forceinline__ uint32_t lds_at(const void* p) { return (uint32_t)(size_t)(__attribute__((address_space(3))) const char*)p; }
