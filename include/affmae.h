@@ -454,8 +454,7 @@ int affmae_pla_bwd_relpos(const void* q, const void* k, const void* v, const flo
  *   x, residual, out, dout, dx  [n] dtype; residual NULL = 0; out may be x or residual,
  *              dx may be dout
  *
- * Any n and alignment (to the element); n a multiple of 8 (bf16) or 4 (fp32) in 16-byte
- * aligned tensors runs the fast kernel, others a slower one, same results.
+ * Any n and any alignment (to the element), same kernel.
  * Errors: AFFMAE_ERR_NULL (x, out; rng with p > 0), AFFMAE_ERR_DTYPE, AFFMAE_ERR_SHAPE
  * (n < 1, p outside [0, 1), misaligned tensors).
  */
@@ -526,8 +525,8 @@ int affmae_linear_bwd(const void* x, const void* weight, const void* pre, const 
  * spread cost no digits.
  * Limits: groups divides C <= 2^20, B*N below 2^31 - 8, B*groups <= 2^24, B*N*C <= 2^38
  * (AFFMAE_ERR_UNSUPPORTED beyond).  Any sizes and any alignment (to the element) run;
- * C / groups a multiple of 8 (bf16) or 4 (fp32) in 16-byte aligned tensors runs the
- * fastest kernels.
+ * layer norms of up to 8192 (bf16) or 4096 (fp32) channels and groups of a multiple of
+ * 8 (bf16) or 4 (fp32) channels are the fastest.
  * Errors: AFFMAE_ERR_NULL, AFFMAE_ERR_DTYPE, AFFMAE_ERR_SHAPE (sizes < 1, C % groups,
  * unknown act, eps not positive and finite, misaligned tensors), AFFMAE_ERR_UNSUPPORTED,
  * AFFMAE_ERR_WORKSPACE.

@@ -114,42 +114,47 @@ __device__ __forceinline__ uint32_t rng_word(const RngKey& key, uint64_t element
   const int i = (int)(element & 3);
   return i == 0 ? w.x : i == 1 ? w.y : i == 2 ? w.z : w.w;
 }
-// v[0..E) are elements first .. first + E - 1; first and E are multiples of 4, or E is 1.
+// v[0..E) are elements first .. first + E - 1; `even`: first is a multiple of 4, that is, of the generator's blocks.
 template <int E>
-__device__ __forceinline__ void drop(float (&v)[E], const Dropout& d, const RngKey& key, uint64_t first) {
+__device__ __forceinline__ void drop(float (&v)[E], const Dropout& d, const RngKey& key, uint64_t first, bool even) {
   if constexpr (E == 1) {
     v[0] = rng_word(key, first) >= d.least ? v[0] * d.factor : 0.f;
   } else {
     static_assert(E % 4 == 0);
+    const uint64_t block = first >> 2;
+    uint4 w[E / 4 + 1];
 #pragma unroll
-    for (int q = 0; q < E / 4; ++q) {
-      const uint4 w = rng_words(key, (first >> 2) + q);
-      v[4 * q + 0] = w.x >= d.least ? v[4 * q + 0] * d.factor : 0.f;
-      v[4 * q + 1] = w.y >= d.least ? v[4 * q + 1] * d.factor : 0.f;
-      v[4 * q + 2] = w.z >= d.least ? v[4 * q + 2] * d.factor : 0.f;
-      v[4 * q + 3] = w.w >= d.least ? v[4 * q + 3] * d.factor : 0.f;
+    for (int q = 0; q < E / 4; ++q) w[q] = rng_words(key, block + q);
+    const auto keep = [&](float& x, uint32_t word) __attribute__((always_inline)) { x = word >= d.least ? x * d.factor : 0.f; };
+    if (even) {
+#pragma unroll
+      for (int q = 0; q < E / 4; ++q) {
+        keep(v[4 * q], w[q].x);
+        keep(v[4 * q + 1], w[q].y);
+        keep(v[4 * q + 2], w[q].z);
+        keep(v[4 * q + 3], w[q].w);
+      }
+    } else {  // one block more, and the words from where the piece begins
+      w[E / 4] = rng_words(key, block + E / 4);
+      const bool odd = first & 1, two = first & 2;
+#pragma unroll
+      for (int q = 0; q < E / 4; ++q) {
+        const uint32_t a = two ? w[q].z : w[q].x, b = two ? w[q].w : w[q].y, c = two ? w[q + 1].x : w[q].z, e = two ? w[q + 1].y : w[q].w,
+                       f = two ? w[q + 1].z : w[q + 1].x;
+        keep(v[4 * q], odd ? b : a);
+        keep(v[4 * q + 1], odd ? c : b);
+        keep(v[4 * q + 2], odd ? e : c);
+        keep(v[4 * q + 3], odd ? f : e);
+      }
     }
   }
 }
 
-// A piece of E consecutive values: 16 bytes (E = 4 for fp32, 8 for bf16; 16-byte aligned), or one value.
+// A piece of E consecutive values in memory: 16 bytes (E = 4 for fp32, 8 for bf16), wherever a value may start, or one value.  (Loads and
+// stores of 16 bytes need no alignment on this hardware; a piece that crosses a line takes two.)
 template <typename T>
 constexpr int kPiece = 16 / (int)sizeof(T);
 
-template <int E>
-__device__ __forceinline__ void load_piece(const float* p, float (&v)[E]) {
-  if constexpr (E == 1)
-    v[0] = *p;
-  else
-    load_row<E>(p, v);
-}
-template <int E>
-__device__ __forceinline__ void load_piece(const bf16_t* p, float (&v)[E]) {
-  if constexpr (E == 1)
-    v[0] = bf16_to_f32(*p);
-  else
-    load_row<E>(p, v);
-}
 __device__ __forceinline__ uint32_t pack2_bf16(float lo, float hi) {
   typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
   typedef __attribute__((ext_vector_type(2))) float f32x2;
@@ -157,31 +162,42 @@ __device__ __forceinline__ uint32_t pack2_bf16(float lo, float hi) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(f, bf16x2));
 }
 template <int E>
-__device__ __forceinline__ void store_piece(float* p, const float (&v)[E]) {
+__device__ __forceinline__ void load_piece(const float* p, float (&v)[E]) {
+  __builtin_memcpy(v, p, sizeof(v));
+}
+template <int E>
+__device__ __forceinline__ void load_piece(const bf16_t* p, float (&v)[E]) {
   if constexpr (E == 1) {
-    *p = v[0];
+    v[0] = bf16_to_f32(*p);
   } else {
+    uint32_t w[E / 2];
+    __builtin_memcpy(w, p, sizeof(w));
 #pragma unroll
-    for (int t = 0; t < E / 4; ++t)
-      reinterpret_cast<float4*>(p)[t] = make_float4(v[4 * t], v[4 * t + 1], v[4 * t + 2], v[4 * t + 3]);
+    for (int e = 0; e < E / 2; ++e) {
+      v[2 * e] = __uint_as_float(w[e] << 16);
+      v[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
+    }
   }
+}
+template <int E>
+__device__ __forceinline__ void store_piece(float* p, const float (&v)[E]) {
+  __builtin_memcpy(p, v, sizeof(v));
 }
 template <int E>
 __device__ __forceinline__ void store_piece(bf16_t* p, const float (&v)[E]) {
   if constexpr (E == 1) {
     *p = f32_to_bf16(v[0]);
   } else {
+    uint32_t w[E / 2];
 #pragma unroll
-    for (int t = 0; t < E / 8; ++t)
-      reinterpret_cast<uint4*>(p)[t] = make_uint4(pack2_bf16(v[8 * t], v[8 * t + 1]), pack2_bf16(v[8 * t + 2], v[8 * t + 3]),
-                                                  pack2_bf16(v[8 * t + 4], v[8 * t + 5]), pack2_bf16(v[8 * t + 6], v[8 * t + 7]));
+    for (int e = 0; e < E / 2; ++e) w[e] = pack2_bf16(v[2 * e], v[2 * e + 1]);
+    __builtin_memcpy(p, w, sizeof(w));
   }
 }
-
-// The first n of a piece's values, whole and aligned (`whole`) or one by one.
+// the first n of a piece's values (the others read as 0)
 template <int E, typename T>
-__device__ __forceinline__ void load_some(const T* p, int n, bool whole, float (&v)[E]) {
-  if (whole && n >= E) {
+__device__ __forceinline__ void load_some(const T* p, int n, float (&v)[E]) {
+  if (n >= E) {
     load_piece<E>(p, v);
   } else {
 #pragma unroll
@@ -189,8 +205,8 @@ __device__ __forceinline__ void load_some(const T* p, int n, bool whole, float (
   }
 }
 template <int E, typename T>
-__device__ __forceinline__ void store_some(T* p, int n, bool whole, const float (&v)[E]) {
-  if (whole && n >= E) {
+__device__ __forceinline__ void store_some(T* p, int n, const float (&v)[E]) {
+  if (n >= E) {
     store_piece<E>(p, v);
   } else {
 #pragma unroll
@@ -198,7 +214,5 @@ __device__ __forceinline__ void store_some(T* p, int n, bool whole, const float 
       if (e < n) Elem<T>::store(p + e, v[e]);
   }
 }
-
-inline bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }  // (a null pointer is)
 
 }  // namespace affmae

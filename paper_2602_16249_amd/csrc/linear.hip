@@ -124,22 +124,30 @@ struct Stager {
       }
     }
   }
-  // the same value by value, for operands whose rows do not start on 4 bytes
+  // the same through registers, for operands whose rows do not start on 4 bytes: whole pieces wherever they start, value by value where a
+  // piece is cut off
   __device__ __forceinline__ void load_values(char* dst, int k0, int left) const {
     const char* from = first + skip(k0);
-#pragma unroll 1
+    uint4 v[kTurns];
+#pragma unroll
     for (int t = 0; t < kTurns; ++t) {
       int line, in_line;
       place(t, line, in_line);
-      T v[kPiece<T>];
+      const int lines = ALONG ? x_left : left, row = (ALONG ? left : x_left) * (int)sizeof(T);  // there: lines, bytes of each
+      v[t] = make_uint4(0u, 0u, 0u, 0u);
+      if (line >= lines || in_line >= row) continue;
+      const char* at = from + (size_t)line * ld + in_line;
+      if (in_line + 16 <= row) {
+        __builtin_memcpy(&v[t], at, 16);
+      } else {
+        T some[kPiece<T>];
 #pragma unroll
-      for (int e = 0; e < kPiece<T>; ++e) {
-        const int at = in_line + e * (int)sizeof(T);
-        const bool there = ALONG ? line < x_left && at < left * (int)sizeof(T) : line < left && at < x_left * (int)sizeof(T);
-        v[e] = there ? *reinterpret_cast<const T*>(from + (size_t)line * ld + at) : T(0);
+        for (int e = 0; e < kPiece<T>; ++e) some[e] = in_line + e * (int)sizeof(T) < row ? reinterpret_cast<const T*>(at)[e] : T(0);
+        __builtin_memcpy(&v[t], some, 16);
       }
-      *reinterpret_cast<uint4*>(dst + (t * THREADS + threadIdx.x) * 16) = *reinterpret_cast<const uint4*>(v);
     }
+#pragma unroll
+    for (int t = 0; t < kTurns; ++t) *reinterpret_cast<uint4*>(dst + (t * THREADS + threadIdx.x) * 16) = v[t];
   }
 };
 
@@ -219,23 +227,25 @@ struct GradEpilogue {
   float alpha;
 };
 
-// E values of row m from column n on, `at` = m N + n, r: the residual's
+// the first `some` of E values from column n on of a row, the first of them value `at` of the tensor; `even`: rows are whole blocks of 4
 template <typename T, int E>
-__device__ __forceinline__ void finish(const Epilogue& e, const RngKey& key, float (&v)[E], const float (&r)[E], int n, size_t at) {
+__device__ __forceinline__ void finish(const Epilogue& e, const RngKey& key, float (&v)[E], int some, int n, size_t at, bool even) {
+  float r[E];
+  if (e.residual) load_some<E>((const T*)e.residual + at, some, r);
   if (e.bias) {
     float b[E];
-    load_piece<E>((const T*)e.bias + n, b);
+    load_some<E>((const T*)e.bias + n, some, b);
 #pragma unroll
     for (int i = 0; i < E; ++i) v[i] += b[i];
   }
-  if (e.pre) store_piece<E>((T*)e.pre + at, v);
+  if (e.pre) store_some<E>((T*)e.pre + at, some, v);
   act_values<E>(v, e.act);
-  if (e.d.rng) drop<E>(v, e.d, key, at);
+  if (e.d.rng) drop<E>(v, e.d, key, at, even);
   if (e.residual) {
 #pragma unroll
     for (int i = 0; i < E; ++i) v[i] += r[i];
   }
-  store_piece<E>((T*)e.out + at, v);
+  store_some<E>((T*)e.out + at, some, v);
 }
 
 template <int BM, int BN>
@@ -349,7 +359,7 @@ __global__ __launch_bounds__(WM* WN* kWave, 2) void linear_kernel(Product p, Ep 
 #pragma unroll
       for (int j = 0; j < IN; ++j) *reinterpret_cast<f32x4*>(batch + (16 * i + r) * B::kLd + 16 * j + 4 * g) = c[first + i][j];
     wave_lds_sync();
-    // f(piece number, its row and column in the batch) for the lane's pieces of E values inside M x N
+    // f(row and column in the batch, values) for the lane's pieces of E values inside M x N
     const auto pieces = [&](auto piece, int N, auto f) __attribute__((always_inline)) {
       constexpr int E = decltype(piece)::value, kRow = TN / E;
       const int all = min(16 * B::kStrips, p.M - m) * kRow;
@@ -360,40 +370,39 @@ __global__ __launch_bounds__(WM* WN* kWave, 2) void linear_kernel(Product p, Ep 
       }
     };
     using std::integral_constant;
+    constexpr int E = kPiece<T>;
     if constexpr (kGrad) {
-      const auto put = [&](auto* out, auto piece, int N) __attribute__((always_inline)) {
+      // `whole`: rows are whole pieces
+      const auto put = [&](auto* out, auto piece, int N, auto whole) __attribute__((always_inline)) {
         constexpr int E = decltype(piece)::value;
         pieces(piece, N, [&](int row, int col) {
           float v[E];
-          load_piece<E>(batch + row * B::kLd + col, v);
+          load_row<E>(batch + row * B::kLd + col, v);
 #pragma unroll
           for (int x = 0; x < E; ++x) v[x] *= e.alpha;
-          store_piece<E>(out + (size_t)(m + row) * N + n + col, v);
+          store_some<E>(out + (size_t)(m + row) * N + n + col, whole ? E : min(E, N - n - col), v);
         });
       };
       if (e.part)  // (alpha is 1)
-        put(e.part + (size_t)split * p.M * e.part_ld, integral_constant<int, 4>(), e.part_ld);
-      else if (p.N % kPiece<T> == 0 && ((uintptr_t)e.out & 15) == 0)
-        put((T*)e.out, integral_constant<int, kPiece<T>>(), p.N);
+        put(e.part + (size_t)split * p.M * e.part_ld, integral_constant<int, 4>(), e.part_ld, std::true_type());
+      else if (p.N % E == 0)
+        put((T*)e.out, integral_constant<int, E>(), p.N, std::true_type());
       else
-        put((T*)e.out, integral_constant<int, 1>(), p.N);
+        put((T*)e.out, integral_constant<int, E>(), p.N, std::false_type());
     } else {
       RngKey key = {};
       if (e.d.rng) key = rng_key(e.d.rng);
-      const auto put = [&](auto piece) __attribute__((always_inline)) {
-        constexpr int E = decltype(piece)::value;
-        pieces(piece, p.N, [&](int row, int col) {
-          const size_t at = (size_t)(m + row) * p.N + n + col;
-          float v[E], res[E];
-          if (e.residual) load_piece<E>((const T*)e.residual + at, res);
-          load_piece<E>(batch + row * B::kLd + col, v);
-          finish<T, E>(e, key, v, res, n + col, at);
+      const auto put = [&](auto whole) __attribute__((always_inline)) {
+        pieces(integral_constant<int, E>(), p.N, [&](int row, int col) {
+          float v[E];
+          load_row<E>(batch + row * B::kLd + col, v);
+          finish<T, E>(e, key, v, whole ? E : min(E, p.N - n - col), n + col, (size_t)(m + row) * p.N + n + col, whole || p.N % 4 == 0);
         });
       };
-      if (p.N % kPiece<T> == 0 && (((uintptr_t)e.out | (uintptr_t)e.pre | (uintptr_t)e.bias | (uintptr_t)e.residual) & 15) == 0)
-        put(integral_constant<int, kPiece<T>>());
+      if (p.N % E == 0)
+        put(std::true_type());
       else
-        put(integral_constant<int, 1>());
+        put(std::false_type());
     }
   }
 }
@@ -441,9 +450,7 @@ __global__ __launch_bounds__(kSlimWaves* kWave) void linear_slim_kernel(Product 
   const size_t at = (size_t)m * p.N + n;
   RngKey key = {};
   if (e.d.rng) key = rng_key(e.d.rng);
-  float res[1] = {0.f};
-  if (e.residual) load_piece<1>((const T*)e.residual + at, res);
-  finish<T, 1>(e, key, v, res, n, at);
+  finish<T, 1>(e, key, v, 1, n, at, true);
 }
 
 // out[i] = alpha * (part[0][i] + part[1][i] + ...), rows of N in part_ld, LANES threads a piece of four; the last workgroups: bias
@@ -508,7 +515,7 @@ __global__ __launch_bounds__(256) void linear_join_kernel(GradEpilogue e, int M,
 // order of memory, whatever rows it is part of, so that odd rows cost neither wide loads nor blocks of the generator.  EVEN: C is a
 // multiple of a piece, hence ld.
 template <typename T, bool EVEN>
-__global__ __launch_bounds__(256) void linear_dz_kernel(const T* __restrict__ dout, const T* __restrict__ pre, int rows, int C, int ld, uint32_t magic, bool whole, int act,
+__global__ __launch_bounds__(256) void linear_dz_kernel(const T* __restrict__ dout, const T* __restrict__ pre, int rows, int C, int ld, uint32_t magic, int act,
                                                         Dropout d, T* __restrict__ dz) {
   constexpr int E = kPiece<T>;
   RngKey key = {};
@@ -520,9 +527,9 @@ __global__ __launch_bounds__(256) void linear_dz_kernel(const T* __restrict__ do
     const int n = (int)std::min<long long>(all - i, E);
     if (n <= 0) break;
     float v[E], z[E];
-    load_some<E>(dout + i, n, whole, v);
-    if (pre) load_some<E>(pre + i, n, whole, z);
-    if (d.rng) drop<E>(v, d, key, (uint64_t)i);
+    load_some<E>(dout + i, n, v);
+    if (pre) load_some<E>(pre + i, n, z);
+    if (d.rng) drop<E>(v, d, key, (uint64_t)i, true);
     if (pre) act_slopes<E>(v, z, act);
     if constexpr (EVEN) {
       store_piece<E>(dz + i, v);
@@ -718,7 +725,7 @@ hipError_t bwd(const LinearArgs& a, hipStream_t stream) {
     const auto kernel = a.Cout % E == 0 ? linear_dz_kernel<T, true> : linear_dz_kernel<T, false>;
     const dim3 grid((unsigned)std::min<long long>(cdiv((long long)a.rows * a.Cout, 256 * E), kMaxBlocks));
     AFFMAE_LAUNCH("linear_dz_kernel", stream, kernel, grid, dim3(256), 0, stream, (const T*)a.dout, (const T*)pre, a.rows, a.Cout, ld, div_magic(a.Cout),
-                  aligned16(a.dout) && aligned16(pre), a.act, d, (T*)ws);
+                  a.act, d, (T*)ws);
     const hipError_t rc = hipGetLastError();
     if (rc != hipSuccess) return rc;
     dz = {ws, (uint32_t)(ld * sizeof(T)), (long long)a.rows * ld * (long long)sizeof(T)};

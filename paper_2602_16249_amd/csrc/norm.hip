@@ -67,22 +67,23 @@ __device__ __forceinline__ float row_sum(float v, int lane, float (&acc)[kWaves]
   }
 }
 
-// LANES lanes a row, PIECES pieces of E values a lane, TURNS rows of a lane group on their way at a time
-template <typename T, int E, int LANES, int PIECES, int TURNS>
+// LANES lanes a row, PIECES pieces of E values a lane, TURNS rows of a lane group on their way at a time; TAIL: rows end inside a piece
+template <typename T, int LANES, int PIECES, int TURNS, bool TAIL>
 __global__ __launch_bounds__(kThreads) void norm_rows_fwd_kernel(const T* __restrict__ x, const T* __restrict__ gamma, const T* __restrict__ beta, int rows,
                                                                  int C, float eps, int act, T* __restrict__ out, float* __restrict__ mean,
                                                                  float* __restrict__ rstd) {
-  constexpr int kRows = kThreads / LANES;  // of a turn
+  constexpr int E = kPiece<T>, kRows = kThreads / LANES;  // of a turn
   __shared__ float acc[kWaves];
   const int lane = threadIdx.x & (kWave - 1), l = threadIdx.x % LANES, at = threadIdx.x / LANES;
   const float inv = 1.f / (float)C;
+  const auto there = [&](int c) { return TAIL ? C - c : E; };  // values from c on, if fewer than a piece
   float gm[PIECES][E], bt[PIECES][E];
 #pragma unroll
   for (int p = 0; p < PIECES; ++p) {
     const int c = (p * LANES + l) * E;
     if (gamma && c < C) {
-      load_piece<E>(gamma + c, gm[p]);
-      load_piece<E>(beta + c, bt[p]);
+      load_some<E>(gamma + c, there(c), gm[p]);
+      load_some<E>(beta + c, there(c), bt[p]);
     }
   }
   for (long long first = (long long)blockIdx.x * kRows * TURNS; first < rows; first += (long long)gridDim.x * kRows * TURNS) {
@@ -94,7 +95,7 @@ __global__ __launch_bounds__(kThreads) void norm_rows_fwd_kernel(const T* __rest
       for (int p = 0; p < PIECES; ++p) {
         const int c = (p * LANES + l) * E;
         if (c < C) {
-          load_piece<E>(x + row * C + c, v[t][p]);
+          load_some<E>(x + row * C + c, there(c), v[t][p]);
         } else {
 #pragma unroll
           for (int e = 0; e < E; ++e) v[t][p][e] = 0.f;
@@ -115,7 +116,8 @@ __global__ __launch_bounds__(kThreads) void norm_rows_fwd_kernel(const T* __rest
       for (int p = 0; p < PIECES; ++p)
         if ((p * LANES + l) * E < C) {
 #pragma unroll
-          for (int e = 0; e < E; ++e) s = __builtin_fmaf(v[t][p][e] - m, v[t][p][e] - m, s);
+          for (int e = 0; e < E; ++e)
+            if (!TAIL || (p * LANES + l) * E + e < C) s = __builtin_fmaf(v[t][p][e] - m, v[t][p][e] - m, s);
         }
       const float r = 1.f / sqrtf(row_sum<LANES>(s, lane, acc) * inv + eps);
       if (row >= rows) continue;
@@ -128,29 +130,30 @@ __global__ __launch_bounds__(kThreads) void norm_rows_fwd_kernel(const T* __rest
         const int c = (p * LANES + l) * E;
         if (c >= C) continue;
         normalise<E>(v[t][p], m, r, gamma != nullptr, gm[p], bt[p], act);
-        store_piece<E>(out + row * C + c, v[t][p]);
+        store_some<E>(out + row * C + c, there(c), v[t][p]);
       }
     }
   }
 }
 
 // dx, and per workgroup the sums of dz xhat and dz of every channel: part [workgroups][2][C]
-template <typename T, int E, int LANES, int PIECES, int TURNS>
+template <typename T, int LANES, int PIECES, int TURNS, bool TAIL>
 __global__ __launch_bounds__(kThreads) void norm_rows_bwd_kernel(const T* __restrict__ x, const T* __restrict__ gamma, const T* __restrict__ beta,
                                                                  const float* __restrict__ mean, const float* __restrict__ rstd, const T* __restrict__ dout,
                                                                  int rows, int C, int act, T* __restrict__ dx, float* __restrict__ part) {
-  constexpr int kRows = kThreads / LANES;
+  constexpr int E = kPiece<T>, kRows = kThreads / LANES;
   __shared__ float sums[kRows][LANES * E];
   __shared__ float acc[kWaves];
   const int lane = threadIdx.x & (kWave - 1), l = threadIdx.x % LANES, at = threadIdx.x / LANES;
   const float inv = 1.f / (float)C;
+  const auto there = [&](int c) { return TAIL ? C - c : E; };  // values from c on, if fewer than a piece
   float gm[PIECES][E], bt[PIECES][E], dg[PIECES][E], db[PIECES][E];
 #pragma unroll
   for (int p = 0; p < PIECES; ++p) {
     const int c = (p * LANES + l) * E;
     if (gamma && c < C) {
-      load_piece<E>(gamma + c, gm[p]);
-      load_piece<E>(beta + c, bt[p]);
+      load_some<E>(gamma + c, there(c), gm[p]);
+      load_some<E>(beta + c, there(c), bt[p]);
     }
 #pragma unroll
     for (int e = 0; e < E; ++e) dg[p][e] = db[p][e] = 0.f;
@@ -166,8 +169,8 @@ __global__ __launch_bounds__(kThreads) void norm_rows_bwd_kernel(const T* __rest
       for (int p = 0; p < PIECES; ++p) {
         const int c = (p * LANES + l) * E;
         if (c < C) {
-          load_piece<E>(x + row * C + c, v[t][p]);
-          load_piece<E>(dout + row * C + c, g[t][p]);
+          load_some<E>(x + row * C + c, there(c), v[t][p]);
+          load_some<E>(dout + row * C + c, there(c), g[t][p]);
         }
       }
     }
@@ -199,7 +202,7 @@ __global__ __launch_bounds__(kThreads) void norm_rows_bwd_kernel(const T* __rest
         if (c >= C) continue;
 #pragma unroll
         for (int e = 0; e < E; ++e) g[t][p][e] = r[t] * (g[t][p][e] - s1 - v[t][p][e] * s2);
-        store_piece<E>(dx + row * C + c, g[t][p]);
+        store_some<E>(dx + row * C + c, there(c), g[t][p]);
       }
     }
   }
@@ -723,68 +726,53 @@ Cut cut_sums(int B, int N, int C, int G, int E) {
   return k;
 }
 
-// pieces of 16 bytes, or single values
-template <typename T>
-int piece_of(const NormArgs& a, const void* y, const void* z) {
-  const int E = kPiece<T>;
-  return a.C / a.G % E == 0 && aligned16(a.x) && aligned16(a.gamma) && aligned16(a.beta) && aligned16(y) && aligned16(z) ? E : 1;
-}
-
-// Rows that the row kernels hold: at most 4 pieces of 16 bytes or 16 single values a lane; by a wave as long as that is enough.
-int most_pieces(int E) { return E == 1 ? 16 : 4; }
-bool rows_fit(int N, int C, int G, int E) { return N == 1 && G == 1 && cdiv(C, E) <= kThreads * most_pieces(E); }
-int row_lanes(int C, int E) {
-  const int pieces = cdiv(C, E);
-  if (pieces > kWave * most_pieces(E)) return kThreads;
+// Rows that the row kernels hold: at most 4 pieces a lane, by a wave as long as that is enough, else by the workgroup.
+constexpr int kMostPieces = 4;
+bool rows_fit(int N, int C, int G, int E) { return N == 1 && G == 1 && cdiv(C, E) <= kThreads * kMostPieces; }
+int row_lanes(int pieces) {
+  if (pieces > kWave * kMostPieces) return kThreads;
   int lanes = 4;
   while (lanes < kWave && lanes < pieces) lanes *= 2;
   return lanes;
 }
 int rows_bwd_blocks(int rows) { return std::min(cdiv(rows, 16), 1024); }
 
+// f(lanes, pieces, whether rows end inside a piece)
 template <typename F>
 hipError_t for_row_shape(int C, int E, F f) {
-  const int lanes = row_lanes(C, E), pieces = cdiv(cdiv(C, E), lanes);
+  const int all = cdiv(C, E), lanes = row_lanes(all), pieces = cdiv(all, lanes);
+  const auto shape = [&](auto lanes_, auto pieces_) { return C % E ? f(lanes_, pieces_, std::true_type()) : f(lanes_, pieces_, std::false_type()); };
   using std::integral_constant;
-  if (lanes == 4) return f(integral_constant<int, 4>(), integral_constant<int, 1>());
-  if (lanes == 8) return f(integral_constant<int, 8>(), integral_constant<int, 1>());
-  if (lanes == 16) return f(integral_constant<int, 16>(), integral_constant<int, 1>());
-  if (lanes == 32) return f(integral_constant<int, 32>(), integral_constant<int, 1>());
-  if (lanes == kThreads) return pieces <= 2 ? f(integral_constant<int, kThreads>(), integral_constant<int, 2>()) : pieces <= 4 ? f(integral_constant<int, kThreads>(), integral_constant<int, 4>()) : f(integral_constant<int, kThreads>(), integral_constant<int, 16>());
-  if (pieces == 1) return f(integral_constant<int, 64>(), integral_constant<int, 1>());
-  if (pieces == 2) return f(integral_constant<int, 64>(), integral_constant<int, 2>());
-  if (pieces <= 4) return f(integral_constant<int, 64>(), integral_constant<int, 4>());
-  return f(integral_constant<int, 64>(), integral_constant<int, 16>());
+  if (lanes == 4) return shape(integral_constant<int, 4>(), integral_constant<int, 1>());
+  if (lanes == 8) return shape(integral_constant<int, 8>(), integral_constant<int, 1>());
+  if (lanes == 16) return shape(integral_constant<int, 16>(), integral_constant<int, 1>());
+  if (lanes == 32) return shape(integral_constant<int, 32>(), integral_constant<int, 1>());
+  if (lanes == kThreads) return pieces <= 2 ? shape(integral_constant<int, kThreads>(), integral_constant<int, 2>()) : shape(integral_constant<int, kThreads>(), integral_constant<int, 4>());
+  if (pieces == 1) return shape(integral_constant<int, 64>(), integral_constant<int, 1>());
+  if (pieces == 2) return shape(integral_constant<int, 64>(), integral_constant<int, 2>());
+  return shape(integral_constant<int, 64>(), integral_constant<int, 4>());
 }
 constexpr int turns_of(int pieces) { return pieces == 1 ? 4 : pieces == 2 ? 2 : 1; }
 
-template <typename T, int E>
+template <typename T>
 hipError_t rows_fwd(const NormArgs& a, hipStream_t stream) {
-  return for_row_shape(a.C, E, [&](auto lanes, auto pieces) {
+  return for_row_shape(a.C, kPiece<T>, [&](auto lanes, auto pieces, auto tail) {
     constexpr int L = lanes, P = pieces, U = turns_of(P);
-    if constexpr (P == 16 && E > 1) {
-      return hipErrorInvalidValue;
-    } else {
-      const unsigned grid = (unsigned)std::min(cdiv(a.B, kThreads / L * U), 4096);
-      AFFMAE_LAUNCH("norm_rows_fwd_kernel", stream, (norm_rows_fwd_kernel<T, E, L, P, U>), dim3(grid), dim3(kThreads), 0, stream, (const T*)a.x, (const T*)a.gamma,
-                    (const T*)a.beta, a.B, a.C, a.eps, a.act, (T*)a.out, a.mean, a.rstd);
-      return hipGetLastError();
-    }
+    const unsigned grid = (unsigned)std::min(cdiv(a.B, kThreads / L * U), 4096);
+    AFFMAE_LAUNCH("norm_rows_fwd_kernel", stream, (norm_rows_fwd_kernel<T, L, P, U, tail>), dim3(grid), dim3(kThreads), 0, stream, (const T*)a.x, (const T*)a.gamma,
+                  (const T*)a.beta, a.B, a.C, a.eps, a.act, (T*)a.out, a.mean, a.rstd);
+    return hipGetLastError();
   });
 }
-template <typename T, int E>
+template <typename T>
 hipError_t rows_bwd(const NormArgs& a, hipStream_t stream) {
   const int blocks = rows_bwd_blocks(a.B);
   float* part = a.dgamma ? static_cast<float*>(a.workspace) : nullptr;
-  const hipError_t rc = for_row_shape(a.C, E, [&](auto lanes, auto pieces) {
+  const hipError_t rc = for_row_shape(a.C, kPiece<T>, [&](auto lanes, auto pieces, auto tail) {
     constexpr int L = lanes, P = pieces, U = turns_of(P) > 2 ? 2 : turns_of(P);
-    if constexpr (P == 16 && E > 1) {
-      return hipErrorInvalidValue;
-    } else {
-      AFFMAE_LAUNCH("norm_rows_bwd_kernel", stream, (norm_rows_bwd_kernel<T, E, L, P, U>), dim3(blocks), dim3(kThreads), 0, stream, (const T*)a.x, (const T*)a.gamma,
-                    (const T*)a.beta, a.mean, a.rstd, (const T*)a.dout, a.B, a.C, a.act, (T*)a.dx, part);
-      return hipGetLastError();
-    }
+    AFFMAE_LAUNCH("norm_rows_bwd_kernel", stream, (norm_rows_bwd_kernel<T, L, P, U, tail>), dim3(blocks), dim3(kThreads), 0, stream, (const T*)a.x, (const T*)a.gamma,
+                  (const T*)a.beta, a.mean, a.rstd, (const T*)a.dout, a.B, a.C, a.act, (T*)a.dx, part);
+    return hipGetLastError();
   });
   if (rc != hipSuccess || !part) return rc;
   AFFMAE_LAUNCH("norm_channel_sums_kernel", stream, norm_channel_sums_kernel, dim3(RowSums::blocks(a.C)), dim3(1024), 0, stream, part, blocks, a.C, a.dgamma, a.dbeta);
@@ -878,45 +866,35 @@ hipError_t groups_bwd(const NormArgs& a, hipStream_t stream) {
   return hipGetLastError();
 }
 
-template <typename T, int E>
-hipError_t fwd(const NormArgs& a, hipStream_t stream) {
-  return rows_fit(a.N, a.C, a.G, E) ? rows_fwd<T, E>(a, stream) : groups_fwd<T, E>(a, stream);
-}
-template <typename T, int E>
-hipError_t bwd(const NormArgs& a, hipStream_t stream) {
-  return rows_fit(a.N, a.C, a.G, E) ? rows_bwd<T, E>(a, stream) : groups_bwd<T, E>(a, stream);
-}
-
-// the larger need of pieces of 16 bytes and of single values: which of them a call takes depends on its tensors' alignment
-template <typename F>
-size_t either(int C, int G, int dtype, F f) {
+// What the group kernels move at a time: pieces, or single values where a group ends inside a piece.
+int group_piece(int C, int G, int dtype) {
   const int E = dtype == 1 ? 8 : 4;
-  return std::max(f(1), C / G % E == 0 ? f(E) : size_t(0));
+  return C / G % E == 0 ? E : 1;
+}
+template <typename T>
+hipError_t fwd(const NormArgs& a, hipStream_t stream) {
+  if (rows_fit(a.N, a.C, a.G, kPiece<T>)) return rows_fwd<T>(a, stream);
+  return group_piece(a.C, a.G, a.dtype) > 1 ? groups_fwd<T, kPiece<T>>(a, stream) : groups_fwd<T, 1>(a, stream);
+}
+template <typename T>
+hipError_t bwd(const NormArgs& a, hipStream_t stream) {
+  if (rows_fit(a.N, a.C, a.G, kPiece<T>)) return rows_bwd<T>(a, stream);
+  return group_piece(a.C, a.G, a.dtype) > 1 ? groups_bwd<T, kPiece<T>>(a, stream) : groups_bwd<T, 1>(a, stream);
 }
 
 }  // namespace
 
 size_t norm_fwd_workspace_bytes(int B, int N, int C, int G, int dtype) {
-  return either(C, G, dtype, [&](int E) -> size_t {
-    if (rows_fit(N, C, G, E)) return 0;
-    int held;
-    const Cut k = cut_held(B, N, C, G, E, &held);
-    return k.parts() > 1 ? (size_t)B * G * k.parts() * sizeof(float2) : 0;
-  });
+  if (rows_fit(N, C, G, dtype == 1 ? 8 : 4)) return 0;
+  int held;
+  const Cut k = cut_held(B, N, C, G, group_piece(C, G, dtype), &held);
+  return k.parts() > 1 ? (size_t)B * G * k.parts() * sizeof(float2) : 0;
 }
 size_t norm_bwd_workspace_bytes(int B, int N, int C, int G, int dtype) {
-  return either(C, G, dtype, [&](int E) -> size_t {
-    if (rows_fit(N, C, G, E)) return (size_t)rows_bwd_blocks(B) * 2 * C * sizeof(float);
-    return bwd_space(B, C, G, cut_sums(B, N, C, G, E)).all;
-  });
+  if (rows_fit(N, C, G, dtype == 1 ? 8 : 4)) return (size_t)rows_bwd_blocks(B) * 2 * C * sizeof(float);
+  return bwd_space(B, C, G, cut_sums(B, N, C, G, group_piece(C, G, dtype))).all;
 }
-hipError_t launch_norm_fwd(const NormArgs& a, hipStream_t stream) {
-  if (a.dtype == 1) return piece_of<bf16_t>(a, a.out, nullptr) > 1 ? fwd<bf16_t, 8>(a, stream) : fwd<bf16_t, 1>(a, stream);
-  return piece_of<float>(a, a.out, nullptr) > 1 ? fwd<float, 4>(a, stream) : fwd<float, 1>(a, stream);
-}
-hipError_t launch_norm_bwd(const NormArgs& a, hipStream_t stream) {
-  if (a.dtype == 1) return piece_of<bf16_t>(a, a.dout, a.dx) > 1 ? bwd<bf16_t, 8>(a, stream) : bwd<bf16_t, 1>(a, stream);
-  return piece_of<float>(a, a.dout, a.dx) > 1 ? bwd<float, 4>(a, stream) : bwd<float, 1>(a, stream);
-}
+hipError_t launch_norm_fwd(const NormArgs& a, hipStream_t stream) { return a.dtype == 1 ? fwd<bf16_t>(a, stream) : fwd<float>(a, stream); }
+hipError_t launch_norm_bwd(const NormArgs& a, hipStream_t stream) { return a.dtype == 1 ? bwd<bf16_t>(a, stream) : bwd<float>(a, stream); }
 
 }  // namespace affmae
