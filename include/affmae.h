@@ -487,8 +487,10 @@ int affmae_dropout_bwd(const void* dout, int64_t n, float p, const int64_t* rng,
  *   workspace  affmae_linear_bwd_workspace_bytes(...) bytes, may be 0
  *
  * Limits: rows <= 2^29, Cin, Cout <= 2^20, rows * Cin, rows * Cout and Cin * Cout
- * <= 2^35 (AFFMAE_ERR_UNSUPPORTED beyond).  Any sizes and any alignment (to the element) run;
- * rows of whole 16-byte pieces in 16-byte aligned tensors are the fastest.
+ * <= 2^35 (AFFMAE_ERR_UNSUPPORTED beyond).  Outputs must not overlap inputs, but for
+ * what is said above.  Any sizes and any alignment (to the element) run, same results;
+ * x, weight and dout with rows of whole 16-byte pieces in 16-byte aligned memory are the
+ * fastest, rows of whole 4-byte words come next.
  * Errors: AFFMAE_ERR_NULL, AFFMAE_ERR_DTYPE, AFFMAE_ERR_SHAPE (sizes < 1, unknown act,
  * p outside [0, 1), misaligned tensors), AFFMAE_ERR_UNSUPPORTED, AFFMAE_ERR_WORKSPACE.
  */
@@ -523,7 +525,7 @@ int affmae_linear_bwd(const void* x, const void* weight, const void* pre, const 
  * Statistics and sums are fp32, added in a fixed order; a variance is the mean square
  * about the mean (never a difference of squares), so that offsets large against the
  * spread cost no digits.
- * Limits: groups divides C <= 2^20, B*N below 2^31 - 8, B*groups <= 2^24, B*N*C <= 2^38
+ * Limits: groups divides C <= 2^20, B*N <= 2^31 - 2^16, B*groups <= 2^24, B*N*C <= 2^38
  * (AFFMAE_ERR_UNSUPPORTED beyond).  Any sizes and any alignment (to the element) run;
  * layer norms of up to 8192 (bf16) or 4096 (fp32) channels and groups of a multiple of
  * 8 (bf16) or 4 (fp32) channels are the fastest.

@@ -547,6 +547,21 @@ def test_norm_beyond_2_31_values():
         del got, x
 
 
+def test_norm_of_as_many_tokens_as_there_may_be():
+    """One image of 2^31 - 2^16 tokens of one channel, -1, 1, -1, ...: mean 0 and variance 1, exactly."""
+    N = 2 ** 31 - 2 ** 16
+    x = torch.ones(1, N, 1, dtype=torch.bfloat16, device="cuda")
+    x[:, ::2] = -1
+    gamma, beta = torch.full((1,), 3.0, device="cuda").bfloat16(), torch.zeros(1, device="cuda").bfloat16()
+    out, mean, rstd = aff.affmae_norm_fwd(x, gamma, beta, 1, eps=1e-5)
+    assert float(mean) == 0 and abs(float(rstd) - (1 + 1e-5) ** -0.5) < 4 * U
+    for lo in (0, N // 2, N - 5000):
+        assert torch.equal(out[:, lo:lo + 5000], x[:, lo:lo + 5000] * 3)
+    got = aff.affmae_norm_bwd(x, gamma, beta, mean, rstd, x, 1, grads={"dx": out})
+    assert float(got["dx"][:, -5000:].float().abs().max()) < 1e-4
+    assert abs(float(got["dgamma"]) / N - (1 + 1e-5) ** -0.5) < _sum_error(N) and abs(float(got["dbeta"])) <= _sum_error(N) * N
+
+
 # -------------------------------------------------------------------------------------------------------------- refusals
 
 def test_binding_refuses():
