@@ -48,7 +48,8 @@ __device__ __forceinline__ void lds_load(uint32_t dst, i32x4 rsrc, uint32_t off)
 #pragma clang diagnostic pop
 __device__ __forceinline__ uint32_t lds_at(const void* p) { return (uint32_t)(size_t)(__attribute__((address_space(3))) const char*)p; }
 
-// Slices are 128 bytes of k deep: 64 values of bf16, 32 of fp32, two steps of the matrix instruction's 32 / four times 4.
+// Slices are 128 bytes of k deep: 64 values of bf16, 32 of fp32, two steps of one instruction of
+// 32 of them / of four instructions of 4.
 constexpr int kSliceBytes = 128;
 template <typename T>
 constexpr int kSlice = kSliceBytes / (int)sizeof(T);
@@ -59,7 +60,6 @@ constexpr int kSlice = kSliceBytes / (int)sizeof(T);
 template <typename T, bool ALONG, int BX>
 struct SliceLayout {
   static constexpr int kLine = ALONG ? kSliceBytes : BX * (int)sizeof(T);
-  static constexpr int kLines = ALONG ? BX : kSlice<T>;
   static constexpr int kBytes = BX * kSliceBytes;
   static __device__ __forceinline__ int mix(int line) {
     if constexpr (ALONG)
@@ -153,7 +153,8 @@ struct Stager {
 
 // What lane (r = lane % 16, g = lane / 16) hands to the matrix instruction for row r of 16: bf16 k = 8 g .. 8 g + 7 of a step of 32;
 // fp32 k = 4 g .. 4 g + 3 of a step of 16, value j to the j-th of four instructions (which k meets which instruction is free as long
-// as both operands agree).
+// as both operands agree).  (The instructions of 32 x 32 values are faster alone, 2.0 PFLOP/s against 1.26 in bf16, 152 TFLOP/s against 139
+// in fp32, but not in these tiles: 16384 x 768 -> 2304 75 us against 67, dx 57 against 55, dW of 16384 x 256 -> 768 in fp32 81 against 73.)
 template <typename T>
 struct Frag;
 template <>
@@ -211,7 +212,7 @@ struct Product {
   Operand a, b;
   int M, N, K;
   int tiles_n, tiles, splits, split_slices;  // tiles of c; workgroups that share a tile's k, slices of each
-  int buffers;  // 1: a slice's place in LDS besides the one that is multiplied, 0: none
+  int buffers;  // 1: the next slice comes into a second place in LDS while one is multiplied, 0: into the same, afterwards
 };
 struct Epilogue {
   const void *bias, *residual;
@@ -260,7 +261,7 @@ struct Batch {
   static constexpr int kBytes = WM * WN * kFloats * 4;
 };
 
-// BM x BN values of c by WM x WN waves.  Two slices of both operands in LDS: one is multiplied while the next one is on its way.
+// BM x BN values of c by WM x WN waves, a slice of both operands in LDS at a time, with p.buffers the next one on its way beside it.
 // The products are c^T tiles (b's rows along the instruction's rows), so that a lane holds four consecutive columns of c.
 template <typename T, bool AA, bool BA, int W, int BM, int BN, int WM, int WN, typename Ep>
 __global__ __launch_bounds__(WM* WN* kWave, 2) void linear_kernel(Product p, Ep e) {
@@ -331,8 +332,8 @@ __global__ __launch_bounds__(WM* WN* kWave, 2) void linear_kernel(Product p, Ep 
     }
   }
   // A wave's values go through LDS, a batch of strips of 16 rows at a time, and leave as pieces in the order of memory, by a loop that is
-  // not unrolled: with the epilogue's code once for every strip, a tile's end took a quarter longer (131072 x 64 -> 192, gelu, 26.3 us
-  // against 21).
+  // not unrolled: with the epilogue's code once for every strip, 65536 x 256 -> 256 took 30.6 us with gelu and 24.8 with relu, so it takes
+  // 27.4 and 23.1.
   __syncthreads();
   using B = Batch<BM, BN, WM, WN>;
   float* batch = reinterpret_cast<float*>(lds) + wave * B::kFloats;
@@ -359,7 +360,7 @@ __global__ __launch_bounds__(WM* WN* kWave, 2) void linear_kernel(Product p, Ep 
 #pragma unroll
       for (int j = 0; j < IN; ++j) *reinterpret_cast<f32x4*>(batch + (16 * i + r) * B::kLd + 16 * j + 4 * g) = c[first + i][j];
     wave_lds_sync();
-    // f(row and column in the batch, values) for the lane's pieces of E values inside M x N
+    // f(row and column in the batch) for the lane's pieces of E values inside M x N
     const auto pieces = [&](auto piece, int N, auto f) __attribute__((always_inline)) {
       constexpr int E = decltype(piece)::value, kRow = TN / E;
       const int all = min(16 * B::kStrips, p.M - m) * kRow;
@@ -409,7 +410,7 @@ __global__ __launch_bounds__(WM* WN* kWave, 2) void linear_kernel(Product p, Ep 
 
 // Forward products of few rows and columns: 16 x 16 values of c a workgroup, the waves share k between them, operands straight from
 // memory into registers.  A tile of 64 x 64 would leave most of the chip without work and walk k alone, one round trip to memory per
-// slice: 64 rows, 2304 -> 768, 27.6 us with tiles of 128 x 128.
+// slice: 64 rows, 2304 -> 768 in bf16, 27.6 us with tiles of 128 x 128, 7.3 so.
 constexpr int kSlim = 16, kSlimWaves = 8;
 template <typename T>
 __global__ __launch_bounds__(kSlimWaves* kWave) void linear_slim_kernel(Product p, Epilogue e) {
