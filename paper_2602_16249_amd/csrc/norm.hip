@@ -6,7 +6,8 @@
 //   rows     N = 1, one group, rows that fit a wave's registers: 4 to 64 lanes hold a row, statistics and values from one reading.
 //   groups   everything else: a workgroup takes a run of an image's tokens times a block of at most 256 pieces of channels (whole
 //            groups, or a share of one), every thread one column of pieces; a first launch leaves per group and workgroup a mean and a
-//            sum of squares about it, a second one puts these together and makes the values.  An image that one workgroup holds needs one.
+//            sum of squares about it, a second one puts these together and makes the values.  Groups that one workgroup holds need one
+//            launch, and it takes as many images as fit: 131072 x 1 x 64 in 4 groups, bf16, with an image each took 491 us, backward 910.
 // A variance is always the mean square about a mean: of a workgroup's own values in registers, and between workgroups by
 // M2 = sum of (M2_i + n_i (mean_i - mean)^2).  No difference of squares, so offsets and outliers cost no digits.
 #include "launch.h"
@@ -262,20 +263,22 @@ struct Cut {
   int block_cols;  // columns of a block
   int block_groups;
   int blocks;      // of an image's columns
-  int lanes;       // threads over each other in a column: kThreads / block_cols
+  int images;      // of a workgroup
+  int lanes;       // threads over each other in a column of an image
   int rows;        // tokens of a workgroup
   int slabs;       // workgroups over an image's tokens
   int team;       // lanes that add up a group's values of a workgroup
   int join_team;  // lanes that put a group's parts together, kHeldParts each
-  uint32_t cols_magic, group_magic;
+  uint32_t cols_magic, lanes_magic, group_magic;
   __host__ __device__ int parts() const { return slabs * shares; }  // of a group
 };
 
 struct Groups {  // what the kernels take
   const void *x, *gamma, *beta, *dout;
-  int N, C, G;
+  int B, N, C, G;
   Cut k;
   unsigned first;  // workgroup of the launch
+  unsigned work;   // workgroups of the launch, the grid filled up to a multiple of 8
   float eps;
   int act;
   void* out;            // out, or dx
@@ -287,10 +290,11 @@ struct Groups {  // what the kernels take
   int sums;  // workgroups in front of the others that add up channel_part
 };
 
-// a thread's place: column of the block, its group in the block, first channel; the workgroup's tokens
+// a thread's place: column of the block, its group among all of the workgroup's, first channel; the workgroup's images and tokens
 struct Place {
-  int b, block, slab;
-  int col, q, lane_row;
+  int b, block, slab;  // b: the thread's image
+  int b0, images;      // the workgroup's
+  int col, q, im, lane_row;
   int c, group, groups, cols, group_cols;
   bool active;
   int row0, row1;
@@ -298,12 +302,13 @@ struct Place {
   __device__ __forceinline__ Place(const Groups& a, unsigned work) {
     const Cut& k = a.k;
     const unsigned per_image = (unsigned)k.blocks * k.slabs;
-    b = work / per_image;
-    const unsigned rest = work - b * per_image;
+    const unsigned batch = work / per_image, rest = work - batch * per_image;
     slab = rest / k.blocks;
     block = rest - slab * k.blocks;
-    lane_row = exact_div(threadIdx.x, k.block_cols, k.cols_magic);
-    col = threadIdx.x - lane_row * k.block_cols;
+    const int row = exact_div(threadIdx.x, k.block_cols, k.cols_magic);
+    col = threadIdx.x - row * k.block_cols;
+    im = exact_div(row, k.lanes, k.lanes_magic);
+    lane_row = row - im * k.lanes;
     int first_col;
     if (k.shares > 1) {  // a share of one group
       group = block / k.shares;
@@ -312,21 +317,33 @@ struct Place {
       cols = std::min(k.block_cols, k.group_cols - share * k.block_cols);
       groups = 1;
       group_cols = cols;
-      q = 0;
     } else {
       group = block * k.block_groups;
       first_col = group * k.group_cols;
       groups = std::min(k.block_groups, a.G - group);
       cols = groups * k.group_cols;
       group_cols = k.group_cols;
-      q = exact_div(col, k.group_cols, k.group_magic);
     }
-    active = lane_row < k.lanes && col < cols;
-    c = (first_col + (active ? col : 0)) * k.E;
+    c = (first_col + (col < cols ? col : 0)) * k.E;
     row0 = slab * k.rows;
     row1 = std::min(row0 + k.rows, a.N);
+    take(a, batch);
+  }
+  // the images of the batch-th workgroup of a block and slab
+  __device__ __forceinline__ void take(const Groups& a, unsigned batch) {
+    const Cut& k = a.k;
+    b0 = batch * k.images;
+    images = std::min(k.images, a.B - b0);
+    active = im < images && col < cols;
+    b = b0 + (active ? im : 0);
+    q = active ? im * groups + (k.shares > 1 ? 0 : exact_div(col, k.group_cols, k.group_magic)) : 0;
     base = (size_t)b * a.N * a.C + c;
-    if (!active) q = 0;
+  }
+  __device__ __forceinline__ int sets() const { return images * groups; }
+  // the q-th of the workgroup's groups among all
+  __device__ __forceinline__ size_t set(const Groups& a, int q) const {
+    const int im = a.k.images > 1 ? q / groups : 0;
+    return (size_t)(b0 + im) * a.G + group + q - im * groups;
   }
   __device__ __forceinline__ int part(const Groups& a) const { return a.k.shares > 1 ? slab * a.k.shares + block % a.k.shares : slab; }
 };
@@ -343,7 +360,7 @@ __device__ __forceinline__ float sum_over(float v, int width) {
 }
 __device__ __forceinline__ float2 sum_over(float2 v, int width) { return make_float2(sum_over(v.x, width), sum_over(v.y, width)); }
 
-// f(group of the block, lane in its team) for all groups, by teams of `width` lanes; teams without one repeat the last (`there` false).
+// f(group of the workgroup's, lane in its team) for all groups, by teams of `width` lanes; teams without one repeat the last (`there` false).
 // (By whole waves one group after another waited for LDS or memory once per group: 8 us of the 14 that 32 groups took.)
 template <typename F>
 __device__ __forceinline__ void for_groups(int groups, int width, F f) {
@@ -351,7 +368,7 @@ __device__ __forceinline__ void for_groups(int groups, int width, F f) {
   for (int first = 0; first < groups; first += teams) f(std::min(first + team, groups - 1), l, first + team < groups);
 }
 
-// per group of the block, the sums over its threads of v (a value or two): result[q], read by all threads afterwards
+// per group of the workgroup's, the sums over its threads of v (a value or two): result[q], read by all threads afterwards
 template <typename V>
 __device__ __forceinline__ void group_sums(const Groups& a, const Place& w, V v, V (&values)[kThreads], V (&result)[kThreads]) {
   const Cut& k = a.k;
@@ -360,11 +377,13 @@ __device__ __forceinline__ void group_sums(const Groups& a, const Place& w, V v,
   __syncthreads();
   const int n = k.lanes * w.group_cols;
   const uint32_t magic = k.shares > 1 ? 0u : k.group_magic;
-  for_groups(w.groups, k.team, [&](int q, int l, bool there) {
+  for_groups(w.sets(), k.team, [&](int q, int l, bool there) {
+    const int im = k.images > 1 ? q / w.groups : 0;
+    const V* from = values + im * k.lanes * k.block_cols + (q - im * w.groups) * w.group_cols;
     V s = {};
     for (int i = l; i < n; i += k.team) {
       const int row = k.shares > 1 ? i / w.group_cols : exact_div(i, w.group_cols, magic);
-      add(s, values[row * k.block_cols + q * w.group_cols + i - row * w.group_cols]);
+      add(s, from[row * k.block_cols + i - row * w.group_cols]);
     }
     s = sum_over(s, k.team);
     if (l == 0 && there) result[q] = s;
@@ -415,7 +434,9 @@ __device__ __forceinline__ float2 join_sums(const Groups& a, size_t bg, int l, i
 template <typename T, int E, int V, bool WHOLE>
 __global__ __launch_bounds__(kThreads) void norm_stats_kernel(Groups a) {
   __shared__ float values[kThreads], result[kThreads];
-  const Place w(a, a.first + blockIdx.x);
+  const unsigned work = WHOLE ? xcd_contiguous_block(blockIdx.x, gridDim.x) : blockIdx.x;
+  if (WHOLE && work >= a.work) return;
+  const Place w(a, a.first + work);
   const Cut& k = a.k;
   float v[V][E];
   float s = 0.f;
@@ -443,13 +464,13 @@ __global__ __launch_bounds__(kThreads) void norm_stats_kernel(Groups a) {
 #pragma unroll
       for (int e = 0; e < E; ++e) s = __builtin_fmaf(v[i][e] - mean, v[i][e] - mean, s);
     }
-  const float m_first = (int)threadIdx.x < w.groups ? result[threadIdx.x] / n : 0.f;
+  const float m_first = (int)threadIdx.x < w.sets() ? result[threadIdx.x] / n : 0.f;
   group_sums(a, w, s, values, result);
-  const size_t bg = (size_t)w.b * a.G + w.group;
+  const size_t set = (int)threadIdx.x < w.sets() ? w.set(a, threadIdx.x) : 0;
   if constexpr (WHOLE) {
-    if ((int)threadIdx.x < w.groups) {
-      a.mean[bg + threadIdx.x] = m_first;
-      a.rstd[bg + threadIdx.x] = 1.f / sqrtf(result[threadIdx.x] / n + a.eps);
+    if ((int)threadIdx.x < w.sets()) {
+      a.mean[set] = m_first;
+      a.rstd[set] = 1.f / sqrtf(result[threadIdx.x] / n + a.eps);
     }
     if (!w.active) return;
     const float rstd = 1.f / sqrtf(result[w.q] / n + a.eps);
@@ -466,7 +487,7 @@ __global__ __launch_bounds__(kThreads) void norm_stats_kernel(Groups a) {
       store_piece<E>((T*)a.out + w.base + (size_t)row * a.C, v[i]);
     }
   } else {
-    if ((int)threadIdx.x < w.groups) a.group_part[(bg + threadIdx.x) * k.parts() + w.part(a)] = make_float2(m_first, result[threadIdx.x]);
+    if ((int)threadIdx.x < w.sets()) a.group_part[set * k.parts() + w.part(a)] = make_float2(m_first, result[threadIdx.x]);
   }
 }
 
@@ -537,6 +558,86 @@ __global__ __launch_bounds__(kThreads) void norm_apply_kernel(Groups a) {
   }
 }
 
+// the workgroup's sums of dg and db of its channels, into part `to` of channel_part
+template <int E>
+__device__ __forceinline__ void channel_sums(const Groups& a, const Place& w, const float (&dg)[E], const float (&db)[E], float2 (&sums)[kThreads * E], size_t to) {
+  const Cut& k = a.k;
+  const int c0 = w.c - (w.col < w.cols ? w.col : 0) * E;  // the block's first channel
+#pragma unroll
+  for (int e = 0; e < E; ++e) sums[threadIdx.x * E + e] = make_float2(dg[e], db[e]);
+  __syncthreads();
+  float* part = a.channel_part + to * 2 * a.C + c0;
+  for (int i = threadIdx.x; i < w.cols * E; i += kThreads) {
+    float2 t = make_float2(0.f, 0.f);
+    for (int j = 0; j < k.images * k.lanes; ++j) add(t, sums[j * k.block_cols * E + i]);
+    part[i] = t.x;
+    part[a.C + i] = t.y;
+  }
+}
+
+// Groups that one workgroup holds: their sums and dx in one launch, from one reading, further images in further turns; channel_part
+// [workgroups of a block][2][C].
+template <typename T, int E, int V>
+__global__ __launch_bounds__(kThreads) void norm_bwd_whole_kernel(Groups a, int batches) {
+  __shared__ float2 values[kThreads], result[kThreads];
+  __shared__ float2 sums[kThreads * E];
+  const unsigned work = xcd_contiguous_block(blockIdx.x, gridDim.x);
+  if (work >= a.work) return;
+  Place w(a, work);
+  const Cut& k = a.k;
+  const unsigned first = work / k.blocks, all = a.work / k.blocks;
+  float gm[E], bt[E], dg[E], db[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    gm[e] = 1.f;
+    bt[e] = dg[e] = db[e] = 0.f;
+  }
+  if (a.gamma) {
+    load_piece<E>((const T*)a.gamma + w.c, gm);
+    load_piece<E>((const T*)a.beta + w.c, bt);
+  }
+  const float inv = 1.f / ((float)a.N * (float)(k.group_cols * E));
+  for (unsigned batch = first; batch < (unsigned)batches; batch += all) {
+    w.take(a, batch);
+    float x[V][E], g[V][E];
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const int row = i * k.lanes + w.lane_row;
+      if (w.active && row < a.N) {
+        load_piece<E>((const T*)a.x + w.base + (size_t)row * a.C, x[i]);
+        load_piece<E>((const T*)a.dout + w.base + (size_t)row * a.C, g[i]);
+      }
+    }
+    const size_t set = w.set(a, w.q);
+    const float mean = a.mean[set], rstd = a.rstd[set];
+    float2 s = make_float2(0.f, 0.f);
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      if (!w.active || i * k.lanes + w.lane_row >= a.N) continue;
+      slopes<E>(x[i], g[i], mean, rstd, a.gamma != nullptr, gm, bt, a.act);
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        dg[e] = __builtin_fmaf(g[i][e], x[i][e], dg[e]);
+        db[e] += g[i][e];
+        g[i][e] *= gm[e];
+        s.x += g[i][e];
+        s.y = __builtin_fmaf(g[i][e], x[i][e], s.y);
+      }
+    }
+    group_sums(a, w, s, values, result);
+    const float s1 = result[w.q].x * inv, s2 = result[w.q].y * inv;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const int row = i * k.lanes + w.lane_row;
+      if (!w.active || row >= a.N) continue;
+#pragma unroll
+      for (int e = 0; e < E; ++e) g[i][e] = rstd * (g[i][e] - s1 - x[i][e] * s2);
+      store_piece<E>((T*)a.out + w.base + (size_t)row * a.C, g[i]);
+    }
+  }
+  if (a.channel_part) channel_sums<E>(a, w, dg, db, sums, first);
+}
+
 // per workgroup: the sums of dz xhat and dz of its channels, and of dh xhat and dh of its groups
 template <typename T, int E>
 __global__ __launch_bounds__(kThreads) void norm_bwd_sums_kernel(Groups a) {
@@ -578,19 +679,7 @@ __global__ __launch_bounds__(kThreads) void norm_bwd_sums_kernel(Groups a) {
   }
   group_sums(a, w, s, values, result);
   if ((int)threadIdx.x < w.groups) a.group_part[(bg + threadIdx.x) * k.parts() + w.part(a)] = result[threadIdx.x];
-  if (!a.channel_part) return;
-  // (the block's first channel: w.c of a thread without a column)
-  const int c0 = w.c - (w.active ? w.col : 0) * E;
-#pragma unroll
-  for (int e = 0; e < E; ++e) sums[threadIdx.x * E + e] = make_float2(dg[e], db[e]);
-  __syncthreads();
-  float* to = a.channel_part + ((size_t)w.b * k.slabs + w.slab) * 2 * a.C + c0;
-  for (int i = threadIdx.x; i < w.cols * E; i += kThreads) {
-    float2 t = make_float2(0.f, 0.f);
-    for (int j = 0; j < k.lanes; ++j) add(t, sums[j * k.block_cols * E + i]);
-    to[i] = t.x;
-    to[a.C + i] = t.y;
-  }
+  if (a.channel_part) channel_sums<E>(a, w, dg, db, sums, (size_t)w.b0 * k.slabs + w.slab);
 }
 
 template <typename T, int E, int V, bool JOIN>
@@ -659,6 +748,12 @@ int power_of_two(int n) {  // at least n, at most a wave
   while (p < n && p < kWave) p *= 2;
   return p;
 }
+void cut_images(Cut& k, int images, int lanes) {
+  k.images = images;
+  k.lanes = lanes;
+  k.lanes_magic = div_magic(lanes);
+  k.team = power_of_two(lanes * (k.block_cols / k.block_groups));
+}
 // blocks of at most `most` groups, or shares of one
 Cut cut_columns(int C, int G, int E, int most = kThreads) {
   Cut k = {};
@@ -677,10 +772,9 @@ Cut cut_columns(int C, int G, int E, int most = kThreads) {
     k.blocks = cdiv(G, k.block_groups);
     k.block_cols = k.block_groups * k.group_cols;
   }
-  k.lanes = kThreads / k.block_cols;
-  k.team = power_of_two(k.lanes * (k.block_cols / k.block_groups));
   k.cols_magic = div_magic(k.block_cols);
   k.group_magic = div_magic(k.group_cols);
+  cut_images(k, 1, kThreads / k.block_cols);
   return k;
 }
 void cut_rows(Cut& k, int N, long long rows) {
@@ -688,32 +782,57 @@ void cut_rows(Cut& k, int N, long long rows) {
   k.slabs = cdiv(N, k.rows);
   k.join_team = power_of_two(cdiv(k.parts(), kHeldParts));
 }
-// threads hold `held` values each
+// Groups that fit a workgroup whose threads hold V pieces each: one launch instead of two (64 x 49 x 768 in 32 groups, bf16: 7.9 us instead
+// of 20.8).  As many of them as fit, fewer where that leaves CUs without a workgroup, but no less than 8 pieces of a token's row:
+// 64 x 1024 x 256 in 32 groups, bf16, two pieces a workgroup, takes 31.6 us.  Then as many images as fit, with the same proviso; with
+// `several`, narrower blocks until there are four of them (32768 x 1 x 768 in 12 groups, fp32: 70 us instead of 148).
+bool cut_whole(int B, int N, int C, int G, int E, int V, Cut* k, bool several = false) {
+  const long long cols = C / G / E, lanes = cdiv(N, V);  // of a group, of an image
+  if (cols > kThreads || lanes * cols > kThreads) return false;
+  const int least = (int)std::min<long long>(G, cdiv(8, cols));
+  int most = (int)std::min<long long>(G, kThreads / (lanes * cols));
+  if (most < least) return false;
+  const auto images_of = [&](int groups) { return std::min<long long>(kThreads / (groups * cols) / lanes, (long long)B * cdiv(G, groups) / kFullGrid); };
+  const auto fewer = [&] { return most = std::max(least, (most + 1) / 2); };
+  while (most > least && (long long)B * cdiv(G, most) < kFullGrid) fewer();
+  while (several && most > least && images_of(most) < 4 && (long long)B * cdiv(G, most) >= 2 * kFullGrid) fewer();
+  *k = cut_columns(C, G, E, most);
+  const long long images = images_of(k->block_groups);
+  if (images > 1) cut_images(*k, (int)images, k->lanes / (int)images);
+  cut_rows(*k, N, N);
+  return true;
+}
+// Threads hold `held` values each: few where images have fewer tokens than a thread would hold pieces (4096 x 16 x 256 in 32 groups, bf16:
+// 19.3 us with few, 15.4 so; 131072 x 1 x 64 in 4 groups, fp32: 24.5 with few).
 Cut cut_held(int B, int N, int C, int G, int E, int* held) {
-  // Groups that fit a workgroup's registers: one launch instead of two (64 x 49 x 768 in 32 groups, bf16: 9.5 us instead of 20.8).  As many
-  // of them as fit, fewer where that leaves CUs without a workgroup, but no less than 8 pieces of a token's row: 64 x 1024 x 256 in 32
-  // groups, bf16, two pieces a workgroup, takes 31.6 us.
+  Cut k;
+  *held = kHeldFew;
+  if (N < kHeld / E && cut_whole(B, N, C, G, E, kHeldFew / E, &k, true) && k.images > 1) return k;
   *held = kHeld;
-  const int V = kHeld / E;
-  const long long cols = C / G / E;
-  if (cols <= kThreads) {
-    const int least = (int)std::min<long long>(G, cdiv(8, cols));
-    int most = (int)std::min<long long>(G, kThreads / cols);
-    const auto fits = [&](int groups) { return cdiv(N, kThreads / (int)(groups * cols)) <= V; };
-    while (most > least && (!fits(most) || (long long)B * cdiv(G, most) < kFullGrid)) most = std::max(least, (most + 1) / 2);
-    if (most >= least && fits(most)) {
-      Cut k = cut_columns(C, G, E, most);
-      cut_rows(k, N, (long long)V * k.lanes);
-      if (k.slabs == 1) return k;
-    }
-  }
-  Cut k = cut_columns(C, G, E);
+  if (cut_whole(B, N, C, G, E, kHeld / E, &k)) return k;
+  k = cut_columns(C, G, E);
   for (int h : {kHeld, kHeldFew}) {
     *held = h;
     cut_rows(k, N, (long long)h / E * k.lanes);
     if ((long long)B * k.blocks * k.slabs >= kFullGrid) break;
   }
   return k;
+}
+// Backward of groups that fit a workgroup: few values a thread where that takes several images (131072 x 1 x 64 in 4 groups, bf16: 19 us, with
+// kHeldBwd 26).  Single values are read twice instead, unless several images fit: 2048 x 49 x 765 in 15 groups, bf16, 459 us against 691.
+constexpr int kHeldBwd = 32;  // values of x, and of dout
+bool cut_bwd_whole(int B, int N, int C, int G, int E, Cut* k, int* held, int* batches, int* workgroups) {
+  *held = kHeldFew;
+  if (!(cut_whole(B, N, C, G, E, kHeldFew / E, k, true) && k->images > 1)) {
+    *held = kHeldBwd;
+    if (!cut_whole(B, N, C, G, E, kHeldBwd / E, k)) return false;
+    if (E == 1 && k->images == 1) return false;
+  }
+  *batches = cdiv(B, k->images);
+  // (of a block: as many as are on the chip at a time, by the registers that the kernel takes; 2048 x 49 x 768 in 32 groups, bf16: 156 us,
+  // with 1024 workgroups 209)
+  *workgroups = std::min(*batches, std::max(1, (*held == kHeldFew ? 1024 : 768) / k->blocks));
+  return true;
 }
 // for sums: about 1024 workgroups, of at least four turns
 Cut cut_sums(int B, int N, int C, int G, int E) {
@@ -778,18 +897,20 @@ hipError_t rows_bwd(const NormArgs& a, hipStream_t stream) {
 Groups groups_of(const NormArgs& a, const Cut& k) {
   Groups g = {};
   g.x = a.x; g.gamma = a.gamma; g.beta = a.beta; g.dout = a.dout;
-  g.N = a.N; g.C = a.C; g.G = a.G; g.k = k; g.eps = a.eps; g.act = a.act;
+  g.B = a.B; g.N = a.N; g.C = a.C; g.G = a.G; g.k = k; g.eps = a.eps; g.act = a.act;
   g.mean = a.mean; g.rstd = a.rstd;
   return g;
 }
 
+dim3 eights(unsigned n) { return dim3((n + 7) / 8 * 8); }
 // f(workgroups) for all of a cut's, in launches of as many as the runtime takes, g.sums more beside them
 template <typename F>
 void for_workgroups(Groups& g, int B, F f) {
-  const long long all = (long long)B * g.k.blocks * g.k.slabs;
+  const long long all = (long long)cdiv(B, g.k.images) * g.k.blocks * g.k.slabs;
   for (long long first = 0; first < all;) {
     const long long n = std::min(all - first, kMaxBlocks - g.sums);
     g.first = (unsigned)first;
+    g.work = (unsigned)n;
     f(dim3((unsigned)n));
     first += n;
   }
@@ -809,7 +930,10 @@ hipError_t groups_fwd(const NormArgs& a, hipStream_t stream) {
       (void)name;
       for_workgroups(g, a.B, [&](dim3 grid) { AFFMAE_LAUNCH(name, stream, kernel, grid, threads, 0, stream, g); });
     };
-    if (k.parts() == 1) return all("norm_stats_kernel", norm_stats_kernel<T, E, V, true>);
+    if (k.parts() == 1)
+      return for_workgroups(g, a.B, [&](dim3 grid) {
+        AFFMAE_LAUNCH("norm_stats_kernel", stream, (norm_stats_kernel<T, E, V, true>), eights(grid.x), threads, 0, stream, g);
+      });
     all("norm_stats_kernel", norm_stats_kernel<T, E, V, false>);
     if (k.parts() <= kJoinParts) return all("norm_apply_kernel", norm_apply_kernel<T, E, V, true>);
     AFFMAE_LAUNCH("norm_join_kernel", stream, norm_join_kernel<false>, dim3(cdiv((long long)a.B * a.G, kWaves)), threads, 0, stream, g, a.B * a.G);
@@ -835,6 +959,20 @@ BwdSpace bwd_space(int B, int C, int G, const Cut& k) {
 
 template <typename T, int E>
 hipError_t groups_bwd(const NormArgs& a, hipStream_t stream) {
+  Cut whole;
+  int held, batches, workgroups;
+  if (cut_bwd_whole(a.B, a.N, a.C, a.G, E, &whole, &held, &batches, &workgroups)) {
+    Groups g = groups_of(a, whole);
+    g.out = a.dx;
+    g.channel_part = a.dgamma ? static_cast<float*>(a.workspace) : nullptr;
+    g.work = (unsigned)workgroups * whole.blocks;
+    const auto kernel = held == kHeldFew ? norm_bwd_whole_kernel<T, E, kHeldFew / E> : norm_bwd_whole_kernel<T, E, kHeldBwd / E>;
+    AFFMAE_LAUNCH("norm_bwd_whole_kernel", stream, kernel, eights(g.work), dim3(kThreads), 0, stream, g, batches);
+    if (a.dgamma)
+      AFFMAE_LAUNCH("norm_channel_sums_kernel", stream, norm_channel_sums_kernel, dim3(RowSums::blocks(a.C)), dim3(1024), 0, stream, g.channel_part, workgroups, a.C, a.dgamma,
+                    a.dbeta);
+    return hipGetLastError();
+  }
   const Cut sums = cut_sums(a.B, a.N, a.C, a.G, E);
   const BwdSpace at = bwd_space(a.B, a.C, a.G, sums);
   char* ws = static_cast<char*>(a.workspace);
@@ -847,7 +985,7 @@ hipError_t groups_bwd(const NormArgs& a, hipStream_t stream) {
   for_workgroups(g, a.B, [&](dim3 grid) { AFFMAE_LAUNCH("norm_bwd_sums_kernel", stream, (norm_bwd_sums_kernel<T, E>), grid, threads, 0, stream, g); });
   const bool join = sums.parts() <= kJoinParts;
   if (!join) AFFMAE_LAUNCH("norm_join_kernel", stream, norm_join_kernel<true>, dim3(cdiv((long long)a.B * a.G, kWaves)), threads, 0, stream, g, a.B * a.G);
-  constexpr int V = std::max(kHeldFew * 2 / E, 1);
+  constexpr int V = kHeldBwd / E;
   Cut k = cut_columns(a.C, a.G, E);
   cut_rows(k, a.N, (long long)V * k.lanes);
   g.k = k;
@@ -888,7 +1026,11 @@ size_t norm_fwd_workspace_bytes(int B, int N, int C, int G, int dtype) {
 }
 size_t norm_bwd_workspace_bytes(int B, int N, int C, int G, int dtype) {
   if (rows_fit(N, C, G, dtype == 1 ? 8 : 4)) return (size_t)rows_bwd_blocks(B) * 2 * C * sizeof(float);
-  return bwd_space(B, C, G, cut_sums(B, N, C, G, group_piece(C, G, dtype))).all;
+  const int E = group_piece(C, G, dtype);
+  Cut whole;
+  int held, batches, workgroups;
+  if (cut_bwd_whole(B, N, C, G, E, &whole, &held, &batches, &workgroups)) return (size_t)workgroups * 2 * C * sizeof(float);
+  return bwd_space(B, C, G, cut_sums(B, N, C, G, E)).all;
 }
 hipError_t launch_norm_fwd(const NormArgs& a, hipStream_t stream) { return a.dtype == 1 ? fwd<bf16_t>(a, stream) : fwd<float>(a, stream); }
 hipError_t launch_norm_bwd(const NormArgs& a, hipStream_t stream) { return a.dtype == 1 ? bwd<bf16_t>(a, stream) : bwd<float>(a, stream); }

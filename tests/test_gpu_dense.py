@@ -281,6 +281,8 @@ NORM = [  # B, N, C, groups
     (2, 1, 20000, 1), (2, 17, 24, 3), (3, 50, 33, 11), (2, 1000, 64, 8), (1, 4097, 96, 12), (2, 300, 40, 1), (1, 70, 2056, 1), (65, 2, 16, 16),
     (3, 700, 12, 12), (1, 9, 4112, 257), (2, 2, 48, 3), (300, 3, 64, 1), (1, 33000, 16, 2), (300, 1, 2047, 1), (2100, 1, 1030, 1), (17, 1, 4096, 1),
     (4, 49, 768, 32), (3, 500, 64, 8), (1, 20000, 24, 3), (2, 2500, 256, 32),
+    # many small images, several a workgroup
+    (2101, 1, 64, 4), (4099, 1, 24, 3), (3001, 2, 40, 5), (1025, 9, 64, 8), (1537, 4, 256, 32), (5003, 1, 6, 3), (1300, 7, 10, 2), (1027, 33, 16, 1),
 ]
 
 
@@ -433,14 +435,19 @@ def test_norm_of_constant_values():
         assert all(bool(torch.isfinite(t).all()) for t in g.values())
 
 
-def test_norm_keeps_what_is_not_finite_in_its_group():
-    x = torch.randn(3, 40, 32, device="cuda")
-    x[1, 7, 9] = float("nan")
+@pytest.mark.parametrize("B,N", [(3, 40), (3000, 2)])
+def test_norm_keeps_what_is_not_finite_in_its_group(B, N):
+    x = torch.randn(B, N, 32, device="cuda")
+    x[1, N // 2, 9] = float("nan")
     out, mean, rstd = aff.affmae_norm_fwd(x, None, None, 4)
-    bad = torch.zeros(3, 4, dtype=torch.bool, device="cuda")
+    bad = torch.zeros(B, 4, dtype=torch.bool, device="cuda")
     bad[1, 1] = True
     assert torch.equal(torch.isnan(mean), bad) and torch.equal(torch.isnan(rstd), bad)
-    assert torch.equal(torch.isnan(out), bad[:, None, :, None].expand(3, 40, 4, 8).reshape(3, 40, 32))
+    wide = bad[:, None, :, None].expand(B, N, 4, 8).reshape(B, N, 32)
+    assert torch.equal(torch.isnan(out), wide)
+    good = torch.randn(B, 4, device="cuda").abs() + 0.5
+    dx = aff.affmae_norm_bwd(torch.nan_to_num(x), None, None, torch.where(bad, mean, good), good, torch.ones_like(x), 4)["dx"]
+    assert torch.equal(torch.isnan(dx), wide)
 
 
 # --------------------------------------------------------------------------------------------------------------- dropout
