@@ -783,13 +783,13 @@ void cut_rows(Cut& k, int N, long long rows) {
   k.join_team = power_of_two(cdiv(k.parts(), kHeldParts));
 }
 // Groups that fit a workgroup whose threads hold V pieces each: one launch instead of two (64 x 49 x 768 in 32 groups, bf16: 7.9 us instead
-// of 20.8).  As many of them as fit, fewer where that leaves CUs without a workgroup, but no less than 8 pieces of a token's row:
-// 64 x 1024 x 256 in 32 groups, bf16, two pieces a workgroup, takes 31.6 us.  Then as many images as fit, with the same proviso; with
+// of 20.8).  As many of them as fit, fewer where that leaves CUs without a workgroup, but no less than 128 bytes of a token's row:
+// 64 x 1024 x 256 in 32 groups, bf16, 32 bytes a workgroup, takes 31.6 us.  Then as many images as fit, with the same proviso; with
 // `several`, narrower blocks until there are four of them (32768 x 1 x 768 in 12 groups, fp32: 70 us instead of 148).
-bool cut_whole(int B, int N, int C, int G, int E, int V, Cut* k, bool several = false) {
+bool cut_whole(int B, int N, int C, int G, int E, int el, int V, Cut* k, bool several = false) {
   const long long cols = C / G / E, lanes = cdiv(N, V);  // of a group, of an image
   if (cols > kThreads || lanes * cols > kThreads) return false;
-  const int least = (int)std::min<long long>(G, cdiv(8, cols));
+  const int least = (int)std::min<long long>(G, cdiv(128 / (E * el), cols));
   int most = (int)std::min<long long>(G, kThreads / (lanes * cols));
   if (most < least) return false;
   const auto images_of = [&](int groups) { return std::min<long long>(kThreads / (groups * cols) / lanes, (long long)B * cdiv(G, groups) / kFullGrid); };
@@ -804,12 +804,12 @@ bool cut_whole(int B, int N, int C, int G, int E, int V, Cut* k, bool several = 
 }
 // Threads hold `held` values each: few where images have fewer tokens than a thread would hold pieces (4096 x 16 x 256 in 32 groups, bf16:
 // 19.3 us with few, 15.4 so; 131072 x 1 x 64 in 4 groups, fp32: 24.5 with few).
-Cut cut_held(int B, int N, int C, int G, int E, int* held) {
+Cut cut_held(int B, int N, int C, int G, int E, int el, int* held) {
   Cut k;
   *held = kHeldFew;
-  if (N < kHeld / E && cut_whole(B, N, C, G, E, kHeldFew / E, &k, true) && k.images > 1) return k;
+  if (N < kHeld / E && cut_whole(B, N, C, G, E, el, kHeldFew / E, &k, true) && k.images > 1) return k;
   *held = kHeld;
-  if (cut_whole(B, N, C, G, E, kHeld / E, &k)) return k;
+  if (cut_whole(B, N, C, G, E, el, kHeld / E, &k)) return k;
   k = cut_columns(C, G, E);
   for (int h : {kHeld, kHeldFew}) {
     *held = h;
@@ -821,11 +821,11 @@ Cut cut_held(int B, int N, int C, int G, int E, int* held) {
 // Backward of groups that fit a workgroup: few values a thread where that takes several images (131072 x 1 x 64 in 4 groups, bf16: 19 us, with
 // kHeldBwd 26).  Single values are read twice instead, unless several images fit: 2048 x 49 x 765 in 15 groups, bf16, 459 us against 691.
 constexpr int kHeldBwd = 32;  // values of x, and of dout
-bool cut_bwd_whole(int B, int N, int C, int G, int E, Cut* k, int* held, int* batches, int* workgroups) {
+bool cut_bwd_whole(int B, int N, int C, int G, int E, int el, Cut* k, int* held, int* batches, int* workgroups) {
   *held = kHeldFew;
-  if (!(cut_whole(B, N, C, G, E, kHeldFew / E, k, true) && k->images > 1)) {
+  if (!(cut_whole(B, N, C, G, E, el, kHeldFew / E, k, true) && k->images > 1)) {
     *held = kHeldBwd;
-    if (!cut_whole(B, N, C, G, E, kHeldBwd / E, k)) return false;
+    if (!cut_whole(B, N, C, G, E, el, kHeldBwd / E, k)) return false;
     if (E == 1 && k->images == 1) return false;
   }
   *batches = cdiv(B, k->images);
@@ -919,7 +919,7 @@ void for_workgroups(Groups& g, int B, F f) {
 template <typename T, int E>
 hipError_t groups_fwd(const NormArgs& a, hipStream_t stream) {
   int held;
-  const Cut k = cut_held(a.B, a.N, a.C, a.G, E, &held);
+  const Cut k = cut_held(a.B, a.N, a.C, a.G, E, sizeof(T), &held);
   Groups g = groups_of(a, k);
   g.out = a.out;
   g.group_part = static_cast<float2*>(a.workspace);
@@ -961,7 +961,7 @@ template <typename T, int E>
 hipError_t groups_bwd(const NormArgs& a, hipStream_t stream) {
   Cut whole;
   int held, batches, workgroups;
-  if (cut_bwd_whole(a.B, a.N, a.C, a.G, E, &whole, &held, &batches, &workgroups)) {
+  if (cut_bwd_whole(a.B, a.N, a.C, a.G, E, sizeof(T), &whole, &held, &batches, &workgroups)) {
     Groups g = groups_of(a, whole);
     g.out = a.dx;
     g.channel_part = a.dgamma ? static_cast<float*>(a.workspace) : nullptr;
@@ -1000,20 +1000,33 @@ hipError_t groups_bwd(const NormArgs& a, hipStream_t stream) {
   return hipGetLastError();
 }
 
-// What the group kernels move at a time: pieces, or single values where a group ends inside a piece.
+// What the group kernels move at a time: 16 bytes, or less where a group ends inside that, down to single values (2048 x 49 x 768
+// in 32, 64 and 128 groups, bf16, pieces of 16, 8 and 4 bytes: 88, 117 and 213 us, 159, 183 and 280 backward; x 765 in 15, single values:
+// 399 and 458).
 int group_piece(int C, int G, int dtype) {
-  const int E = dtype == 1 ? 8 : 4;
-  return C / G % E == 0 ? E : 1;
+  int E = dtype == 1 ? 8 : 4;
+  while (C / G % E) E /= 2;
+  return E;
+}
+// f(values of a piece)
+template <typename T, typename F>
+hipError_t for_group_piece(const NormArgs& a, F f) {
+  using std::integral_constant;
+  const int E = group_piece(a.C, a.G, a.dtype);
+  if constexpr (sizeof(T) == 2) {
+    if (E == 8) return f(integral_constant<int, 8>());
+  }
+  return E == 4 ? f(integral_constant<int, 4>()) : E == 2 ? f(integral_constant<int, 2>()) : f(integral_constant<int, 1>());
 }
 template <typename T>
 hipError_t fwd(const NormArgs& a, hipStream_t stream) {
   if (rows_fit(a.N, a.C, a.G, kPiece<T>)) return rows_fwd<T>(a, stream);
-  return group_piece(a.C, a.G, a.dtype) > 1 ? groups_fwd<T, kPiece<T>>(a, stream) : groups_fwd<T, 1>(a, stream);
+  return for_group_piece<T>(a, [&](auto piece) { return groups_fwd<T, decltype(piece)::value>(a, stream); });
 }
 template <typename T>
 hipError_t bwd(const NormArgs& a, hipStream_t stream) {
   if (rows_fit(a.N, a.C, a.G, kPiece<T>)) return rows_bwd<T>(a, stream);
-  return group_piece(a.C, a.G, a.dtype) > 1 ? groups_bwd<T, kPiece<T>>(a, stream) : groups_bwd<T, 1>(a, stream);
+  return for_group_piece<T>(a, [&](auto piece) { return groups_bwd<T, decltype(piece)::value>(a, stream); });
 }
 
 }  // namespace
@@ -1021,7 +1034,7 @@ hipError_t bwd(const NormArgs& a, hipStream_t stream) {
 size_t norm_fwd_workspace_bytes(int B, int N, int C, int G, int dtype) {
   if (rows_fit(N, C, G, dtype == 1 ? 8 : 4)) return 0;
   int held;
-  const Cut k = cut_held(B, N, C, G, group_piece(C, G, dtype), &held);
+  const Cut k = cut_held(B, N, C, G, group_piece(C, G, dtype), dtype == 1 ? 2 : 4, &held);
   return k.parts() > 1 ? (size_t)B * G * k.parts() * sizeof(float2) : 0;
 }
 size_t norm_bwd_workspace_bytes(int B, int N, int C, int G, int dtype) {
@@ -1029,7 +1042,7 @@ size_t norm_bwd_workspace_bytes(int B, int N, int C, int G, int dtype) {
   const int E = group_piece(C, G, dtype);
   Cut whole;
   int held, batches, workgroups;
-  if (cut_bwd_whole(B, N, C, G, E, &whole, &held, &batches, &workgroups)) return (size_t)workgroups * 2 * C * sizeof(float);
+  if (cut_bwd_whole(B, N, C, G, E, dtype == 1 ? 2 : 4, &whole, &held, &batches, &workgroups)) return (size_t)workgroups * 2 * C * sizeof(float);
   return bwd_space(B, C, G, cut_sums(B, N, C, G, E)).all;
 }
 hipError_t launch_norm_fwd(const NormArgs& a, hipStream_t stream) { return a.dtype == 1 ? fwd<bf16_t>(a, stream) : fwd<float>(a, stream); }

@@ -283,6 +283,8 @@ NORM = [  # B, N, C, groups
     (4, 49, 768, 32), (3, 500, 64, 8), (1, 20000, 24, 3), (2, 2500, 256, 32),
     # many small images, several a workgroup
     (2101, 1, 64, 4), (4099, 1, 24, 3), (3001, 2, 40, 5), (1025, 9, 64, 8), (1537, 4, 256, 32), (5003, 1, 6, 3), (1300, 7, 10, 2), (1027, 33, 16, 1),
+    # groups of 4 and 2 values at a time
+    (3, 500, 36, 3), (2, 1700, 30, 3), (1100, 3, 24, 4), (1, 9001, 84, 7), (2, 300, 1036, 1), (6, 49, 770, 77),
 ]
 
 
