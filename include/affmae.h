@@ -171,7 +171,7 @@ int affmae_vts_bwd(const float* query_xy, const float* vis_xy, const void* feat,
  * differentiable, location-aware aggregation; supplement "AFF architecture": a
  * linear projection follows every merging block).  The paper leaves the operator
  * to the AFF paper; this library takes the following form.  The score layer and
- * the projection are the caller's dense layers.
+ * the projection are dense layers of their own (affmae_linear_fwd).
  *
  * affmae_merge_select  anchors of every image: the n_keep (= d_s N) tokens with the
  *                      largest score, equal scores (-0 and +0 are equal) going to
@@ -488,9 +488,9 @@ int affmae_dropout_bwd(const void* dout, int64_t n, float p, const int64_t* rng,
  *
  * Limits: rows <= 2^29, Cin, Cout <= 2^20, rows * Cin, rows * Cout and Cin * Cout
  * <= 2^35 (AFFMAE_ERR_UNSUPPORTED beyond).  Outputs must not overlap inputs, but for
- * what is said above.  Any sizes and any alignment (to the element) run, same results;
- * x, weight and dout with rows of whole 16-byte pieces in 16-byte aligned memory are the
- * fastest, rows of whole 4-byte words come next.
+ * what is said above.  Any sizes and any alignment (to the element) run; x, weight and
+ * dout with rows of whole 16-byte pieces in 16-byte aligned memory are the fastest, rows
+ * of whole 4-byte words come next.  (The order of the sums depends on both.)
  * Errors: AFFMAE_ERR_NULL, AFFMAE_ERR_DTYPE, AFFMAE_ERR_SHAPE (sizes < 1, unknown act,
  * p outside [0, 1), misaligned tensors), AFFMAE_ERR_UNSUPPORTED, AFFMAE_ERR_WORKSPACE.
  */
@@ -528,7 +528,7 @@ int affmae_linear_bwd(const void* x, const void* weight, const void* pre, const 
  * Limits: groups divides C <= 2^20, B*N <= 2^31 - 2^16, B*groups <= 2^24, B*N*C <= 2^38
  * (AFFMAE_ERR_UNSUPPORTED beyond).  Any sizes and any alignment (to the element) run;
  * layer norms of up to 8192 (bf16) or 4096 (fp32) channels and groups of a multiple of
- * 8 (bf16) or 4 (fp32) channels are the fastest.
+ * 8 (bf16) or 4 (fp32) channels are the fastest, then groups of a multiple of 4 or 2.
  * Errors: AFFMAE_ERR_NULL, AFFMAE_ERR_DTYPE, AFFMAE_ERR_SHAPE (sizes < 1, C % groups,
  * unknown act, eps not positive and finite, misaligned tensors), AFFMAE_ERR_UNSUPPORTED,
  * AFFMAE_ERR_WORKSPACE.

@@ -2,7 +2,7 @@
 dropout from the Philox generator.
 
 TEST INFRASTRUCTURE ONLY, like the rest of this package: written from the definitions, sharing no code with the product.  Every
-function takes and returns float64 arrays that hold the stored values exactly; `err` functions bound what fp32 sums may differ by.
+function takes and returns float64 arrays that hold the stored values exactly.
 """
 from __future__ import annotations
 

@@ -774,11 +774,15 @@ def affmae_norm_fwd(x: torch.Tensor, gamma: Optional[torch.Tensor], beta: Option
         out_at = _on(dev, out, "out", dtype, x.shape)
     shape = (B, max(groups, 0))
     if mean is None:
-        mean = torch.empty(shape, dtype=torch.float32, device=x.device)
+        mean = x.new_empty(shape, dtype=torch.float32)
+        mean_at = mean.data_ptr()
+    else:
+        mean_at = _on(dev, mean, "mean", torch.float32, shape)
     if rstd is None:
         rstd = torch.empty_like(mean)
-    mean_at = _on(dev, mean, "mean", torch.float32, shape)
-    rstd_at = _on(dev, rstd, "rstd", torch.float32, shape)
+        rstd_at = rstd.data_ptr()
+    else:
+        rstd_at = _on(dev, rstd, "rstd", torch.float32, shape)
     need = lib.affmae_norm_fwd_workspace_bytes(B, N, C, groups, code)
     workspace, ws_at, size = _workspace_on(dev, workspace, need, x.device)
     rc = lib.affmae_norm_fwd(x_at, gamma_at, beta_at, B, N, C, groups, float(eps), _act_code(act), code, out_at, mean_at, rstd_at,
