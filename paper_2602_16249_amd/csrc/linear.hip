@@ -603,7 +603,7 @@ enum { k64x64, k128x64, k128x128, k128x192, kSlimTile };
 constexpr Shape kForward16[] = {{64, 64, 4, .19f, .55f, .45f}, {128, 64, 4, .31f, .58f, 1.1f}, {128, 128, 4, .47f, .85f, 2.1f}, {128, 192, 3, .60f, 1.1f, 4.0f}, {16, 16, 4, .112f, .11f, .4f}};
 constexpr Shape kGradient16[] = {{64, 64, 4, .183f, .55f, .57f}, {128, 64, 3, .283f, .58f, 1.2f}, {128, 128, 2, .546f, .85f, 2.2f}, {128, 192, 2, .70f, 1.1f, 3.7f}};
 constexpr Shape kForward32[] = {{64, 64, 4, .66f, .78f, .4f}, {128, 64, 3, 1.17f, 1.22f, 1.4f}, {}, {}, {16, 16, 4, .116f, .11f, .4f}};
-constexpr Shape kGradient32[] = {{64, 64, 4, .66f, .78f, .4f}, {128, 64, 3, 1.17f, 1.22f, 1.4f}, {}, {}};
+constexpr Shape kGradient32[] = {{64, 64, 4, .66f, 1.04f, .4f}, {128, 64, 3, 1.17f, 1.5f, 1.4f}, {}, {}};
 
 struct Plan {
   int shape, splits;
@@ -618,7 +618,7 @@ float plan_cost(const Shape& h, float tiles, float values, uint32_t slices, uint
   if (splits > 1) t += 4.f + (float)splits * values * (8.f / 4e6f);
   return t;
 }
-// The cheapest tile; gradients also share a tile's k between workgroups, as many as make one or two full turns of the chip.
+// The cheapest tile; gradients also share a tile's k between workgroups: as many as make one or two full turns of the chip.
 Plan plan_product(uint32_t M, uint32_t N, uint32_t K, int el, int line, bool forward) {
   const Shape* shapes = forward ? el == 2 ? kForward16 : kForward32 : el == 2 ? kGradient16 : kGradient32;
   const uint32_t deep = kSliceBytes / el, slices = (K + deep - 1) / deep;
