@@ -642,7 +642,7 @@ Plan plan_product(uint32_t M, uint32_t N, uint32_t K, int el, int line, bool for
   float least = 3e38f;
   for (int i = 0; i < (forward ? kSlimTile + 1 : kSlimTile); ++i) {
     const Shape& h = shapes[i];
-    if (!h.bm || (i > k128x64 && line < 16)) continue;
+    if (!h.bm || (i > k128x128 && line < 16)) continue;
     const float tiles = (float)((M + h.bm - 1) / h.bm) * (float)((N + h.bn - 1) / h.bn);
     if (i == kSlimTile && tiles > 1e6f) continue;
     for (int turns = 0; turns <= (forward ? 0 : 2); ++turns) {
@@ -677,11 +677,14 @@ hipError_t run_product(Product p, int shape, const Ep& e, hipStream_t stream) {
     if (shape == k128x64) return run_tiles<T, AA, BA, 16, 128, 64, 2, 2>(p, e, stream);
     return run_tiles<T, AA, BA, 16, 64, 64, 2, 2>(p, e, stream);
   }
-  if (sizeof(T) == 4 || w == 4)
-    return shape == k128x64 ? run_tiles<T, AA, BA, 4, 128, 64, 2, 2>(p, e, stream) : run_tiles<T, AA, BA, 4, 64, 64, 2, 2>(p, e, stream);
-  if constexpr (sizeof(T) == 2)
-    return shape == k128x64 ? run_tiles<T, AA, BA, 2, 128, 64, 2, 2>(p, e, stream) : run_tiles<T, AA, BA, 2, 64, 64, 2, 2>(p, e, stream);
-  return hipErrorInvalidValue;
+  if constexpr (sizeof(T) == 2) {
+    if (w == 4 && shape == k128x128) return run_tiles<T, AA, BA, 4, 128, 128, 2, 2>(p, e, stream);
+    if (w == 2) {
+      if (shape == k128x128) return run_tiles<T, AA, BA, 2, 128, 128, 2, 2>(p, e, stream);
+      return shape == k128x64 ? run_tiles<T, AA, BA, 2, 128, 64, 2, 2>(p, e, stream) : run_tiles<T, AA, BA, 2, 64, 64, 2, 2>(p, e, stream);
+    }
+  }
+  return shape == k128x64 ? run_tiles<T, AA, BA, 4, 128, 64, 2, 2>(p, e, stream) : run_tiles<T, AA, BA, 4, 64, 64, 2, 2>(p, e, stream);
 }
 
 int part_ld(int N) { return cdiv(N, 4) * 4; }
