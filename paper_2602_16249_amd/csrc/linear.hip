@@ -529,7 +529,7 @@ __global__ __launch_bounds__(256) void linear_join_kernel(GradEpilogue e, int M,
 
 // dz / factor = (kept? dout : 0) act'(pre), rows of C in lines of `ld` values whose rest is 0.  A thread takes a piece of dout in the
 // order of memory, whatever rows it is part of, so that odd rows cost neither wide loads nor blocks of the generator.  EVEN: C is a
-// multiple of a piece, hence ld.
+// multiple of a piece, hence ld.  (Without pre and mask: a copy in such lines.)
 template <typename T, bool EVEN>
 __global__ __launch_bounds__(256) void linear_dz_kernel(const T* __restrict__ dout, const T* __restrict__ pre, int rows, int C, int ld, uint32_t magic, int act,
                                                         Dropout d, T* __restrict__ dz) {
@@ -729,34 +729,55 @@ hipError_t fwd(const LinearArgs& a, hipStream_t stream) {
   return run_product<T, true, true>(p, plan.shape, e, stream);
 }
 
-int dz_ld(int Cout, int el) { return cdiv(Cout * el, 16) * 16 / el; }
+int padded(int C, int el) { return cdiv(C * el, 16) * 16 / el; }
+
+// What of the backward's operands is written anew, in rows of whole pieces.
+struct Copies {
+  bool dz, x, weight;
+};
+// dz with an activation or dropout anyway.  Else bf16 operands whose rows are no whole pieces, all or none, whichever gradients are asked for:
+// with copies a product saves at least 4 us per 10^9 multiplications where rows are odd and 1 us where they are whole words, a copy costs 1.2 us
+// per 10^6 values and its launch (dx and dW of 16384 x 767 -> 2303: 198 us instead of 498, of 16384 x 768 -> 2300 163 instead of 199; but
+// 65536 x 255 -> 255, with copies of 34 million values, 109 instead of 99).
+Copies copies(int rows, int Cin, int Cout, bool made, bool want_dx, bool want_dweight, int el) {
+  const Copies c = {made, false, false};
+  if (el == 4) return c;
+  const bool in = Cin % 8, out = Cout % 8 && !made, odd = (in && Cin & 1) || (out && Cout & 1);
+  const double macs = (double)rows * Cin * Cout, values = (out ? (double)rows * Cout : 0.) + (in ? ((double)rows + Cout) * Cin : 0.);
+  if (!(in || out) || 2. * (odd ? 4e-9 : 1e-9) * macs <= 1.2e-6 * values + 8. * (out + 2 * in)) return c;
+  return {made || out, in && want_dweight, in && want_dx};
+}
+size_t copy_bytes(int rows, int C, int el) { return up256((size_t)rows * padded(C, el) * el); }
 
 template <typename T>
 hipError_t bwd(const LinearArgs& a, hipStream_t stream) {
   const Dropout d = make_dropout(a.p, a.rng);
-  const uint32_t out_ld = (uint32_t)a.Cout * sizeof(T), in_ld = (uint32_t)a.Cin * sizeof(T);
-  Operand dz = {a.dout, out_ld, (long long)a.rows * out_ld};
+  constexpr int el = sizeof(T), E = kPiece<T>;
+  const auto operand = [](const void* p, int rows, int ld) { return Operand{p, (uint32_t)ld * el, (long long)rows * ld * el}; };
+  Operand dz = operand(a.dout, a.rows, a.Cout), x = operand(a.x, a.rows, a.Cin), weight = operand(a.weight, a.Cout, a.Cin);
   char* ws = static_cast<char*>(a.workspace);
-  if (a.act != kActNone || d.rng) {
-    const int ld = dz_ld(a.Cout, sizeof(T));
-    const void* pre = a.act != kActNone ? a.pre : nullptr;
-    constexpr int E = kPiece<T>;
-    const auto kernel = a.Cout % E == 0 ? linear_dz_kernel<T, true> : linear_dz_kernel<T, false>;
-    const dim3 grid((unsigned)std::min<long long>(cdiv((long long)a.rows * a.Cout, 256 * E), kMaxBlocks));
-    AFFMAE_LAUNCH("linear_dz_kernel", stream, kernel, grid, dim3(256), 0, stream, (const T*)a.dout, (const T*)pre, a.rows, a.Cout, ld, div_magic(a.Cout),
-                  a.act, d, (T*)ws);
-    const hipError_t rc = hipGetLastError();
-    if (rc != hipSuccess) return rc;
-    dz = {ws, (uint32_t)(ld * sizeof(T)), (long long)a.rows * ld * (long long)sizeof(T)};
-    ws += up256((size_t)dz.bytes);
-  }
+  const auto write = [&](Operand& o, const void* from, const void* pre, int rows, int C, int act, Dropout drop) {
+    const int ld = padded(C, el);
+    const auto kernel = C % E == 0 ? linear_dz_kernel<T, true> : linear_dz_kernel<T, false>;
+    const dim3 grid((unsigned)std::min<long long>(cdiv((long long)rows * C, 256 * E), kMaxBlocks));
+    AFFMAE_LAUNCH("linear_dz_kernel", stream, kernel, grid, dim3(256), 0, stream, (const T*)from, (const T*)pre, rows, C, ld, div_magic(C), act, drop, (T*)ws);
+    o = operand(ws, rows, ld);
+    ws += copy_bytes(rows, C, el);
+  };
+  const Copies c = copies(a.rows, a.Cin, a.Cout, a.act != kActNone || d.rng, a.dx != nullptr, a.dweight != nullptr, el);
+  const Dropout none = make_dropout(0.f, nullptr);
+  if (c.dz) write(dz, a.dout, a.act != kActNone ? a.pre : nullptr, a.rows, a.Cout, a.act, d);
+  if (c.x) write(x, a.x, nullptr, a.rows, a.Cin, kActNone, none);
+  if (c.weight) write(weight, a.weight, nullptr, a.Cout, a.Cin, kActNone, none);
+  const hipError_t launched = hipGetLastError();
+  if (launched != hipSuccess) return launched;
   float* part = reinterpret_cast<float*>(ws);
   if (a.dx) {
-    const hipError_t rc = gradient<T>(true, dz, {a.weight, in_ld, (long long)a.Cout * in_ld}, a.rows, a.Cin, a.Cout, a.dx, nullptr, d.factor, part, stream);
+    const hipError_t rc = gradient<T>(true, dz, weight, a.rows, a.Cin, a.Cout, a.dx, nullptr, d.factor, part, stream);
     if (rc != hipSuccess) return rc;
   }
   if (a.dweight)
-    return gradient<T>(false, dz, {a.x, in_ld, (long long)a.rows * in_ld}, a.Cout, a.Cin, a.rows, a.dweight, a.dbias, d.factor, part, stream);
+    return gradient<T>(false, dz, x, a.Cout, a.Cin, a.rows, a.dweight, a.dbias, d.factor, part, stream);
   return hipSuccess;
 }
 
@@ -764,14 +785,15 @@ hipError_t bwd(const LinearArgs& a, hipStream_t stream) {
 
 size_t linear_bwd_workspace_bytes(int rows, int Cin, int Cout, int act, bool drops, int dtype, bool want_dx, bool want_dweight) {
   const int el = dtype == 1 ? 2 : 4;
-  const size_t dz = act != kActNone || drops ? up256((size_t)rows * dz_ld(Cout, el) * el) : 0;
+  const Copies c = copies(rows, Cin, Cout, act != kActNone || drops, want_dx, want_dweight, el);
+  const size_t written = (c.dz ? copy_bytes(rows, Cout, el) : 0) + (c.x ? copy_bytes(rows, Cin, el) : 0) + (c.weight ? copy_bytes(Cout, Cin, el) : 0);
   // (which tile a call takes, hence how it splits, depends on its tensors' alignment)
   const auto parts = [&](int M, int N, int K, bool bias) {
     return std::max(part_bytes(plan_product(M, N, K, el, 16, false).splits, M, N, bias), part_bytes(plan_product(M, N, K, el, 2, false).splits, M, N, bias));
   };
   const size_t dx = want_dx ? parts(rows, Cin, Cout, false) : 0;
   const size_t dw = want_dweight ? parts(Cout, Cin, rows, true) : 0;
-  return dz + std::max(dx, dw);  // (the parts of one are joined before the other's are written)
+  return written + std::max(dx, dw);  // (the parts of one are joined before the other's are written)
 }
 hipError_t launch_linear_fwd(const LinearArgs& a, hipStream_t stream) { return a.dtype == 1 ? fwd<bf16_t>(a, stream) : fwd<float>(a, stream); }
 hipError_t launch_linear_bwd(const LinearArgs& a, hipStream_t stream) { return a.dtype == 1 ? bwd<bf16_t>(a, stream) : bwd<float>(a, stream); }

@@ -213,7 +213,7 @@ def test_linear_of_many_rows(dtype):
     assert all(torch.equal(got[k], again[k]) for k in got)
 
 
-@pytest.mark.parametrize("rows,cin,cout", [(16400, 776, 2312), (65552, 264, 264), (8200, 392, 1160), (20008, 264, 136)])
+@pytest.mark.parametrize("rows,cin,cout", [(16400, 776, 2312), (65552, 264, 264), (8200, 392, 1160), (20008, 264, 136), (8201, 767, 1023), (9000, 520, 1157), (16400, 2300, 1000)])
 def test_linear_of_large_tiles(rows, cin, cout):
     """Sizes at which the larger tiles are taken, a little beyond whole tiles and slices, against products in 64 bits on the device."""
     g = torch.Generator(device="cuda")
@@ -250,6 +250,27 @@ def test_linear_of_large_tiles(rows, cin, cout):
     zt, et, at = z.t().contiguous(), e.t().contiguous(), a.t().contiguous()
     close(got["dweight"], zt @ xd, et @ xd.abs() + 2 * U * (rows + 5) * (at @ xd.abs()), "dweight")
     close(got["dbias"], zt.sum(1), et.sum(1) + 2 * U * (rows + 5) * at.sum(1), "dbias")
+
+
+@pytest.mark.parametrize("rows,cin,cout", [(3001, 1281, 1283), (3000, 1024, 1537), (2500, 1281, 1152), (20001, 65, 191)])
+def test_linear_backward_of_odd_rows(rows, cin, cout):
+    """bf16 rows of an odd length, of which large calls write copies: nothing but the gradients and the workspace is written."""
+    d = _linear_inputs("bf16", rows, cin, cout, 7)
+    ref, bounds = _linear_bwd_bounds({k: a[1] for k, a in d.items()}, "none", 0.0, "bf16")
+    g = {"dx": Guarded((rows, cin), torch.bfloat16), "dweight": Guarded((cout, cin), torch.bfloat16), "dbias": Guarded((cout,), torch.bfloat16)}
+    need = aff.load_library().affmae_linear_bwd_workspace_bytes(rows, cin, cout, 0, 0.0, 1, 1, 1)
+    space = torch.full((need + 512,), 77, dtype=torch.uint8, device="cuda")  # 256 bytes around it
+    x, w, dout = (d[k][0] for k in ("x", "w", "dout"))
+    before = [t.clone() for t in (x, w, dout)]
+    aff.affmae_linear_bwd(x, w, dout, grads={k: o.t for k, o in g.items()}, workspace=space[256:256 + need])
+    for k in g:
+        _close(g[k].t, ref[k], bounds[k], k)
+        g[k].check()
+    assert bool((space[:256] == 77).all()) and bool((space[256 + need:] == 77).all())
+    assert all(torch.equal(a, b) for a, b in zip(before, (x, w, dout)))
+    one = aff.affmae_linear_bwd(None, w, dout, want_dweight=False)
+    other = aff.affmae_linear_bwd(x, None, dout, want_dx=False)
+    assert all(torch.equal(t, g[k].t) for k, t in (*one.items(), *other.items()))
 
 
 def test_linear_leading_dimensions_and_values_that_are_not_finite():
