@@ -480,8 +480,8 @@ int affmae_dropout_bwd(const void* dout, int64_t n, float p, const int64_t* rng,
  *   dweight  out [Cout,Cin]  = dz^T x        or NULL (not both NULL)
  *   dbias    out [Cout]      = sum of dz     or NULL (only with dweight)
  *   all in `dtype` like the tensors that they belong to, sums in fp32 in a fixed order.
- *   (The gradient of residual is dout itself.)  For bf16 dz is rounded to bf16: it is
- *   an operand of both products.  relu's slope at 0 is 0.
+ *   (The gradient of residual is dout itself.)  For bf16 dz is rounded to bf16 as the
+ *   operand of both products, not for dbias.  relu's slope at 0 is 0.
  *   weight is read for dx only, x for dweight only, pre with an activation only: each
  *   may be NULL otherwise.
  *   workspace  affmae_linear_bwd_workspace_bytes(...) bytes, may be 0

@@ -5,6 +5,8 @@
 //   forward  a = x  [rows,Cin]  (along k)     b = W [Cout,Cin] (along k)
 //   dx       a = dz [rows,Cout] (along k)     b = W [Cout,Cin] (across: a row of W is one k)
 //   dW       a = dz [rows,Cout] (across)      b = x [rows,Cin] (across), k = rows: split over workgroups, parts added by a second launch
+// dz is written once, rounded to the tensors' type: bf16 operands are what the matrix instructions take, and an operand in two bf16 parts
+// would double both products.  dbias adds the values before they are rounded.
 #include "launch.h"
 #include "timing.h"
 
@@ -470,19 +472,21 @@ __global__ __launch_bounds__(kSlimWaves* kWave) void linear_slim_kernel(Product 
 }
 
 // out[i] = alpha * (part[0][i] + part[1][i] + ...), rows of N in part_ld, LANES threads a piece of four; the last workgroups: bias
-// likewise.  (A thread that adds all parts of its piece waits for them one after another where there are many: 94 parts of 301 x 100 took
+// likewise, of bias_part.  (A thread that adds all parts of its piece waits for them one after another where there are many: 94 parts of 301 x 100 took
 // 27 us.)
 template <typename T, int LANES>
-__global__ __launch_bounds__(256) void linear_join_kernel(GradEpilogue e, int M, int N, int splits, float alpha, int bias_blocks) {
+__global__ __launch_bounds__(256) void linear_join_kernel(GradEpilogue e, int M, int N, int splits, float alpha, int bias_blocks, const float* bias_part,
+                                                          int bias_parts) {
   constexpr int kPieces = 256 / LANES;
   __shared__ float4 sums[LANES > 1 ? 256 : 1];
   const int blocks = gridDim.x - bias_blocks;
   if ((int)blockIdx.x >= blocks) {  // 16 values a workgroup, 16 threads each
     const int m = (blockIdx.x - blocks) * 16 + (threadIdx.x & 15), run = threadIdx.x >> 4;
-    const float* part = e.part + (size_t)splits * M * e.part_ld;
     float s = 0.f;
-    if (m < M)
-      for (int k = run; k < splits; k += 16) s += part[(size_t)k * M + m];
+    if (m < M) {
+#pragma unroll 8
+      for (int k = run; k < bias_parts; k += 16) s += bias_part[(size_t)k * M + m];
+    }
     __shared__ float all[16][17];
     all[run][threadIdx.x & 15] = s;
     __syncthreads();
@@ -566,6 +570,63 @@ __global__ __launch_bounds__(256) void linear_dz_kernel(const T* __restrict__ do
       }
     }
   }
+}
+
+// The same for bf16 with the sums of dz over a run of rows, part [runs][C]: of the values before they are rounded for the products, since the
+// bias' gradient is the only one that adds them up bare (1024 x 64 -> 192: off by 0.0029 of its size with rounded ones, by 0.0017 so).  A
+// thread takes one column of pieces, `lanes` of them over each other, every lanes-th row.
+struct Runs {
+  int cols, lanes, blocks;  // columns of a workgroup, threads of one, workgroups of a row
+  int rows, count;          // of a run, runs
+};
+template <bool EVEN>
+__global__ __launch_bounds__(256) void linear_dz_sums_kernel(const bf16_t* __restrict__ dout, const bf16_t* __restrict__ pre, int rows, int C, int ld, Runs k,
+                                                             uint32_t cols_magic, int act, Dropout d, bf16_t* __restrict__ dz, float* __restrict__ part) {
+  constexpr int E = kPiece<bf16_t>;
+  __shared__ float sums[256 * E];
+  RngKey key = {};
+  if (d.rng) key = rng_key(d.rng);
+  d.factor = 1.f;
+  const int run = blockIdx.x / k.blocks, block = blockIdx.x - run * k.blocks;
+  const int lane = exact_div(threadIdx.x, k.cols, cols_magic), col = threadIdx.x - lane * k.cols;
+  const int c0 = block * k.cols * E, c = c0 + col * E, n = C - c, some = EVEN ? E : n;
+  const int end = std::min(rows, (run + 1) * k.rows);
+  float db[E] = {};
+  if (lane < k.lanes && n > 0) {
+#pragma unroll 4
+    for (int row = run * k.rows + lane; row < end; row += k.lanes) {
+      const long long at = (long long)row * C + c;
+      float v[E], z[E];
+      load_some<E>(dout + at, some, v);
+      if (pre) load_some<E>(pre + at, some, z);
+      if (d.rng) drop<E>(v, d, key, (uint64_t)at, EVEN || C % 4 == 0);
+      if (pre) act_slopes<E>(v, z, act);
+#pragma unroll
+      for (int e = 0; e < E; ++e) db[e] += v[e];
+      store_piece<E>(dz + (size_t)row * ld + c, v);
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < E; ++e) sums[threadIdx.x * E + e] = db[e];
+  __syncthreads();
+  for (int i = threadIdx.x; i < k.cols * E && c0 + i < C; i += 256) {
+    float s = 0.f;
+    for (int l = 0; l < k.lanes; ++l) s += sums[l * k.cols * E + i];
+    part[(size_t)run * C + c0 + i] = s;
+  }
+}
+// Columns in blocks of at most 32 pieces, which fill a workgroup (blocks of 144, of 256 threads 112 idle: 63 us of 16384 x 2304 instead of 45);
+// about 6144 workgroups, of at least four turns.
+Runs runs_of(int rows, int C) {
+  Runs k;
+  const int pieces = cdiv(C, kPiece<bf16_t>);
+  k.blocks = cdiv(pieces, 32);
+  k.cols = cdiv(pieces, k.blocks);
+  k.blocks = cdiv(pieces, k.cols);
+  k.lanes = 256 / k.cols;
+  k.rows = std::max(4 * k.lanes, cdiv(rows, std::max(1, 6144 / k.blocks)));
+  k.count = cdiv(rows, k.rows);
+  return k;
 }
 
 constexpr int kCus = 256;
@@ -694,19 +755,26 @@ size_t part_bytes(int splits, int M, int N, bool bias) {
 size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 
 template <typename T>
-hipError_t gradient(bool dx, Operand a, Operand b, int M, int N, int K, void* out, void* bias, float alpha, float* part, hipStream_t stream) {
+hipError_t gradient(bool dx, Operand a, Operand b, int M, int N, int K, void* out, void* bias, const float* bias_part, int bias_parts, float alpha,
+                    float* part, hipStream_t stream) {
   const Plan plan = plan_product(M, N, K, sizeof(T), std::min(line_bytes(a), line_bytes(b)), false);
   Product p = {};
   p.a = a; p.b = b; p.M = M; p.N = N; p.K = K; p.splits = plan.splits;
-  const GradEpilogue e = {out, bias, p.splits > 1 ? part : nullptr, part_ld(N), p.splits > 1 ? 1.f : alpha};
+  GradEpilogue e = {out, bias_part ? nullptr : bias, p.splits > 1 ? part : nullptr, part_ld(N), p.splits > 1 ? 1.f : alpha};
   hipError_t rc = dx ? run_product<T, true, false>(p, plan.shape, e, stream) : run_product<T, false, false>(p, plan.shape, e, stream);
-  if (rc != hipSuccess || p.splits == 1) return rc;
+  if (rc != hipSuccess || (p.splits == 1 && !bias_part)) return rc;
   const int bias_blocks = bias ? cdiv(M, 16) : 0;
-  const long long pieces = (long long)M * (part_ld(N) / 4);
+  if (!bias_part) {
+    bias_part = part + (size_t)p.splits * M * e.part_ld;
+    bias_parts = p.splits;
+  }
+  e.bias = bias;
+  const long long pieces = p.splits > 1 ? (long long)M * (part_ld(N) / 4) : 0;
   const auto join = [&](auto lanes) {
     constexpr int L = decltype(lanes)::value;
     const int blocks = (int)std::min<long long>(cdiv(pieces * L, 256), 4096);
-    AFFMAE_LAUNCH("linear_join_kernel", stream, (linear_join_kernel<T, L>), dim3(blocks + bias_blocks), dim3(256), 0, stream, e, M, N, p.splits, alpha, bias_blocks);
+    AFFMAE_LAUNCH("linear_join_kernel", stream, (linear_join_kernel<T, L>), dim3(blocks + bias_blocks), dim3(256), 0, stream, e, M, N, p.splits, alpha, bias_blocks,
+                  bias_part, bias_parts);
   };
   if (pieces <= 8192 && p.splits > 16)
     join(std::integral_constant<int, 16>());
@@ -766,18 +834,34 @@ hipError_t bwd(const LinearArgs& a, hipStream_t stream) {
   };
   const Copies c = copies(a.rows, a.Cin, a.Cout, a.act != kActNone || d.rng, a.dx != nullptr, a.dweight != nullptr, el);
   const Dropout none = make_dropout(0.f, nullptr);
-  if (c.dz) write(dz, a.dout, a.act != kActNone ? a.pre : nullptr, a.rows, a.Cout, a.act, d);
+  const void* pre = a.act != kActNone ? a.pre : nullptr;
+  const float* sums = nullptr;
+  int runs = 0;
+  if (sizeof(T) == 2 && (pre || d.rng) && a.dbias) {
+    const Runs k = runs_of(a.rows, a.Cout);
+    const int ld = padded(a.Cout, el);
+    float* to = reinterpret_cast<float*>(ws + copy_bytes(a.rows, a.Cout, el));
+    const auto kernel = a.Cout % E == 0 ? linear_dz_sums_kernel<true> : linear_dz_sums_kernel<false>;
+    AFFMAE_LAUNCH("linear_dz_kernel", stream, kernel, dim3((unsigned)k.count * k.blocks), dim3(256), 0, stream, (const bf16_t*)a.dout,
+                  (const bf16_t*)pre, a.rows, a.Cout, ld, k, div_magic(k.cols), a.act, d, (bf16_t*)ws, to);
+    dz = operand(ws, a.rows, ld);
+    sums = to;
+    runs = k.count;
+    ws += copy_bytes(a.rows, a.Cout, el) + up256((size_t)runs * a.Cout * sizeof(float));
+  } else if (c.dz) {
+    write(dz, a.dout, pre, a.rows, a.Cout, a.act, d);
+  }
   if (c.x) write(x, a.x, nullptr, a.rows, a.Cin, kActNone, none);
   if (c.weight) write(weight, a.weight, nullptr, a.Cout, a.Cin, kActNone, none);
   const hipError_t launched = hipGetLastError();
   if (launched != hipSuccess) return launched;
   float* part = reinterpret_cast<float*>(ws);
   if (a.dx) {
-    const hipError_t rc = gradient<T>(true, dz, weight, a.rows, a.Cin, a.Cout, a.dx, nullptr, d.factor, part, stream);
+    const hipError_t rc = gradient<T>(true, dz, weight, a.rows, a.Cin, a.Cout, a.dx, nullptr, nullptr, 0, d.factor, part, stream);
     if (rc != hipSuccess) return rc;
   }
   if (a.dweight)
-    return gradient<T>(false, dz, x, a.Cout, a.Cin, a.rows, a.dweight, a.dbias, d.factor, part, stream);
+    return gradient<T>(false, dz, x, a.Cout, a.Cin, a.rows, a.dweight, a.dbias, sums, runs, d.factor, part, stream);
   return hipSuccess;
 }
 
@@ -785,8 +869,10 @@ hipError_t bwd(const LinearArgs& a, hipStream_t stream) {
 
 size_t linear_bwd_workspace_bytes(int rows, int Cin, int Cout, int act, bool drops, int dtype, bool want_dx, bool want_dweight) {
   const int el = dtype == 1 ? 2 : 4;
-  const Copies c = copies(rows, Cin, Cout, act != kActNone || drops, want_dx, want_dweight, el);
-  const size_t written = (c.dz ? copy_bytes(rows, Cout, el) : 0) + (c.x ? copy_bytes(rows, Cin, el) : 0) + (c.weight ? copy_bytes(Cout, Cin, el) : 0);
+  const bool made = act != kActNone || drops;
+  const Copies c = copies(rows, Cin, Cout, made, want_dx, want_dweight, el);
+  const size_t sums = el == 2 && made && want_dweight ? up256((size_t)runs_of(rows, Cout).count * Cout * sizeof(float)) : 0;
+  const size_t written = sums + (c.dz ? copy_bytes(rows, Cout, el) : 0) + (c.x ? copy_bytes(rows, Cin, el) : 0) + (c.weight ? copy_bytes(Cout, Cin, el) : 0);
   // (which tile a call takes, hence how it splits, depends on its tensors' alignment)
   const auto parts = [&](int M, int N, int K, bool bias) {
     return std::max(part_bytes(plan_product(M, N, K, el, 16, false).splits, M, N, bias), part_bytes(plan_product(M, N, K, el, 2, false).splits, M, N, bias));
