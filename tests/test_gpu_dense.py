@@ -785,6 +785,36 @@ def test_large_products_replayed_from_a_graph():
         assert all(torch.equal(a, b) for a, b in zip(got, ref)), f"replay {rep}"
 
 
+def test_copies_and_small_images_replayed_from_a_graph():
+    """Gradients that write copies of odd rows, and norms of several images a workgroup, forward and backward."""
+    rows, cin, cout = 3001, 1281, 1283
+    x, w, dout = (torch.randn(*s, device="cuda").bfloat16() for s in ((rows, cin), (cout, cin), (rows, cout)))
+    nx, nd, gamma, beta = (torch.randn(*s, device="cuda").bfloat16() for s in ((3001, 3, 64), (3001, 3, 64), (64,), (64,)))
+
+    def run():
+        g = aff.affmae_linear_bwd(x, w, dout)
+        y, m, r = aff.affmae_norm_fwd(nx, gamma, beta, 4, act="silu")
+        h = aff.affmae_norm_bwd(nx, gamma, beta, m, r, nd, 4, act="silu")
+        return [y, m, r, *g.values(), *h.values()]
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        run()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        got = run()
+    for rep in range(3):
+        x.mul_(0.5)
+        nx.add_(1.0)
+        ref = run()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, ref)), f"replay {rep}"
+
+
 def test_calls_on_two_streams_at_once():
     d = _linear_inputs("bf16", 20000, 64, 192, 8)
     x, w, b, dout, pre = (d[k][0] for k in ("x", "w", "b", "dout", "pre"))
