@@ -257,7 +257,7 @@ __device__ __forceinline__ void finish(const Epilogue& e, const RngKey& key, flo
     for (int i = 0; i < E; ++i) v[i] += b[i];
   }
   if (e.pre) store_some<E>((T*)e.pre + at, some, v);
-  act_values<E>(v, e.act);
+  act_values<sizeof(T) == 2, E>(v, e.act);
   if (e.d.rng) drop<E>(v, e.d, key, at, even);
   if (e.residual) {
 #pragma unroll
@@ -550,7 +550,7 @@ __global__ __launch_bounds__(256) void linear_dz_kernel(const T* __restrict__ do
     load_some<E>(dout + i, n, v);
     if (pre) load_some<E>(pre + i, n, z);
     if (d.rng) drop<E>(v, d, key, (uint64_t)i, true);
-    if (pre) act_slopes<E>(v, z, act);
+    if (pre) act_slopes<sizeof(T) == 2, E>(v, z, act);
     if constexpr (EVEN) {
       store_piece<E>(dz + i, v);
     } else {
@@ -600,7 +600,7 @@ __global__ __launch_bounds__(256) void linear_dz_sums_kernel(const bf16_t* __res
       load_some<E>(dout + at, some, v);
       if (pre) load_some<E>(pre + at, some, z);
       if (d.rng) drop<E>(v, d, key, (uint64_t)at, EVEN || C % 4 == 0);
-      if (pre) act_slopes<E>(v, z, act);
+      if (pre) act_slopes<true, E>(v, z, act);
 #pragma unroll
       for (int e = 0; e < E; ++e) db[e] += v[e];
       store_piece<E>(dz + (size_t)row * ld + c, v);

@@ -36,7 +36,7 @@ __device__ __forceinline__ void normalise(float (&v)[E], float mean, float rstd,
     v[e] = (v[e] - mean) * rstd;
     if (affine) v[e] = __builtin_fmaf(v[e], gm[e], bt[e]);
   }
-  act_values<E>(v, act);
+  act_values<false, E>(v, act);
 }
 // x becomes xhat, g (dout) becomes dz = dout act'(z)
 template <int E>
@@ -47,7 +47,7 @@ __device__ __forceinline__ void slopes(float (&x)[E], float (&g)[E], float mean,
     float z[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) z[e] = affine ? __builtin_fmaf(x[e], gm[e], bt[e]) : x[e];
-    act_slopes<E>(g, z, act);
+    act_slopes<false, E>(g, z, act);  // (dgamma and dbeta leave as fp32)
   }
 }
 

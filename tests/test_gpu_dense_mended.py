@@ -1,0 +1,81 @@
+"""GPU tests of the dense operators at the places where they were mended: each failed before, or compares what nothing else does.
+
+U: half a step of fp32, relative to the value; HALF: half a step of the output's type."""
+import numpy as np
+import pytest
+import torch
+from scipy import special
+
+import paper_2602_16249_amd as aff
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+HALF = {"f32": 2.0 ** -24, "bf16": 2.0 ** -8}
+
+
+# ------------------------------------------------------------------------------------------------------------------ gelu
+
+def _gelu_points(dtype):
+    z = torch.cat([torch.linspace(-12, 12, 48001), torch.linspace(-0.01, 0.01, 2001)]).to(TYPES[dtype])
+    return z.cuda().view(-1, 1), z.double().numpy()
+
+
+# Relative errors in units of U.  The exponent z^2 / 2: z z and its product with -1/2 log2(e) are rounded once each, 2 U (z^2 / 2) = z^2 U of
+# the result together; the hardware's exponential is off by 2 U (one step); the polynomial's fit by 0.7 (fp32) or 4 (bf16); t by 2, which counts
+# 2.1 times (4.2), or uncorrected and 2.7 times (5.4); the last of the sum's roundings, sum of |terms| / value 3.6 at t = 1, count 7; s t, its
+# product with e, 1 - tail and z cdf one each.  In all z^2 + 18 in fp32, z^2 + 22.4 in bf16: z^2 + 24 is taken.
+ROUNDINGS = 24
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_gelu_to_the_last_digits(dtype):
+    """Far into the negative tail, where gelu is small: relative to its own size."""
+    t, z = _gelu_points(dtype)
+    got, _ = aff.affmae_linear_fwd(t, torch.ones(1, 1, dtype=t.dtype, device="cuda"), act="gelu")
+    ref = z * special.ndtr(z)
+    tol = (z * z + ROUNDINGS) * U * np.abs(ref)
+    off = np.abs(got.double().cpu().numpy()[:, 0] - ref)
+    over = off > tol + HALF[dtype] * (np.abs(ref) + tol)
+    assert not over.any(), (int(over.sum()), z[over][0], off[over][0] / abs(ref[over][0]))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_slope_of_gelu_to_the_last_digits(dtype):
+    """The slope is cdf + z density, two terms of either sign: relative to the sum of their sizes."""
+    t, z = _gelu_points(dtype)
+    one = torch.ones(1, 1, dtype=t.dtype, device="cuda")
+    got = aff.affmae_linear_bwd(None, one, torch.ones_like(t), t, act="gelu", want_dweight=False)["dx"]
+    cdf, part = special.ndtr(z), z * np.exp(-0.5 * z * z) / np.sqrt(2 * np.pi)
+    ref = cdf + part
+    tol = (z * z + ROUNDINGS) * U * (cdf + np.abs(part))
+    half = HALF[dtype] if dtype == "f32" else 2 * HALF[dtype] + HALF[dtype] ** 2  # (bf16: dz and the gradient, one rounding each)
+    off = np.abs(got.double().cpu().numpy()[:, 0] - ref)
+    over = off > tol + half * (np.abs(ref) + tol)
+    assert not over.any(), (int(over.sum()), z[over][0], off[over][0])
+
+
+@pytest.mark.parametrize("G", [1, 4])
+def test_gelu_behind_a_norm(G):
+    """The norm's own activation: constant channels of +-1 make xhat +-1 (eps 1e-12), gamma carries the value."""
+    z = np.linspace(-9, 9, 64).astype(np.float32)
+    x = torch.ones(40, 1, 64, device="cuda")
+    x[..., 1::2] = -1
+    sign = x[0, 0].cpu().numpy()
+    gamma = torch.from_numpy(z * sign).cuda()
+    out, mean, rstd = aff.affmae_norm_fwd(x, gamma, torch.zeros(64, device="cuda"), G, 1e-12, act="gelu")
+    zd = z.astype(np.float64)
+    ref = zd * special.ndtr(zd)
+    # xhat is off by 4 U, z then by as much: z |slope| / |gelu| <= 1 + z^2 for z < 0
+    tol = ((1 + zd * zd) * 5 + zd * zd + ROUNDINGS) * U * np.abs(ref)
+    assert bool((mean == 0).all()) and (np.abs(out.double().cpu().numpy()[:, 0] - ref) <= tol + U * np.abs(ref)).all()
+
+
+def test_gelu_of_infinities():
+    z = torch.tensor([[float("inf")], [float("nan")], [3e38], [-3e38], [0.0]], device="cuda")
+    one = torch.ones(1, 1, device="cuda")
+    got, _ = aff.affmae_linear_fwd(z, one, act="gelu")
+    assert got[0, 0] == float("inf") and bool(torch.isnan(got[1, 0])) and got[2, 0] == z[2, 0] and got[3, 0] == 0 and got[4, 0] == 0
+    g = aff.affmae_linear_bwd(None, one, torch.ones_like(z), z, act="gelu", want_dweight=False)["dx"]
+    assert bool(torch.isnan(g[1, 0])) and g[2, 0] == 1 and g[3, 0] == 0 and g[4, 0] == 0.5
