@@ -6,7 +6,8 @@
 //   dx       a = dz [rows,Cout] (along k)     b = W [Cout,Cin] (across: a row of W is one k)
 //   dW       a = dz [rows,Cout] (across)      b = x [rows,Cin] (across), k = rows: split over workgroups, parts added by a second launch
 // dz is written once, rounded to the tensors' type: bf16 operands are what the matrix instructions take, and an operand in two bf16 parts
-// would double both products.  dbias adds the values before they are rounded.
+// would double both products (16384 x 768 -> 2304 behind gelu: dx and dW 112 of 167 us).  What that costs there: dx and dW are off by 0.00235 of
+// their size, with dz unrounded by 0.00166, the rounding of the results.  dbias adds the values before they are rounded.
 #include "launch.h"
 #include "timing.h"
 

@@ -1,4 +1,5 @@
-"""GPU tests of the dense operators at the places where they were mended: each failed before, or compares what nothing else does.
+"""GPU tests of the dense operators where errors hide: the last digits of gelu, the one rounding of dz, every tile of the products, layer
+norms wider than the row kernels, sums over as many tokens as there may be.
 
 U: half a step of fp32, relative to the value; HALF: half a step of the output's type."""
 import numpy as np
@@ -7,6 +8,7 @@ import torch
 from scipy import special
 
 import paper_2602_16249_amd as aff
+from oracle import dense
 
 pytestmark = pytest.mark.gpu
 
@@ -79,3 +81,37 @@ def test_gelu_of_infinities():
     assert got[0, 0] == float("inf") and bool(torch.isnan(got[1, 0])) and got[2, 0] == z[2, 0] and got[3, 0] == 0 and got[4, 0] == 0
     g = aff.affmae_linear_bwd(None, one, torch.ones_like(z), z, act="gelu", want_dweight=False)["dx"]
     assert bool(torch.isnan(g[1, 0])) and g[2, 0] == 1 and g[3, 0] == 0 and g[4, 0] == 0.5
+
+
+# ---------------------------------------------------------------------------------------------- one rounding of dz, no other
+
+@pytest.mark.parametrize("rows,cin,cout", [(1030, 136, 264), (700, 65, 191), (16400, 776, 2312)])
+@pytest.mark.parametrize("p", [0.0, 0.25])
+def test_bf16_gradients_are_the_products_of_dz_rounded_once(rows, cin, cout, p):
+    """dx and dweight against products in 64 bits of dz rounded to bf16, dbias against the sum of dz as it is.  dz (in front of the mask's
+    factor, which the sums are multiplied by) is off by (z^2 + 24) U of the sum of the slope's two terms; where that spans a border of the
+    rounding, by the step between the two."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(rows)
+    normal = lambda *shape, std=1.0: (torch.randn(*shape, generator=g, device="cuda") * std).bfloat16()
+    x, w, dout, pre = normal(rows, cin), normal(cout, cin, std=cin ** -0.5), normal(rows, cout), normal(rows, cout, std=1.1)
+    rng = torch.tensor([77, 5], dtype=torch.int64, device="cuda")
+    got = aff.affmae_linear_bwd(x, w, dout, pre, act="gelu", p=p, rng=rng)
+    z, d = pre.double(), dout.double()
+    if p:
+        d = torch.where(torch.from_numpy(dense.keep((rows, cout), p, 77, 5)).cuda(), d, 0.0)
+    f = 1.0 / (1.0 - float(np.float32(p)))
+    cdf, part = 0.5 * torch.special.erfc(-z * 2 ** -0.5), z * torch.exp(-0.5 * z * z) * (2 * np.pi) ** -0.5
+    dz = d * (cdf + part)
+    e = (z * z + 25) * U * d.abs() * (cdf + part.abs())
+    lo, hi = (dz - e).float().bfloat16().double(), (dz + e).float().bfloat16().double()
+    r, step = dz.float().bfloat16().double(), (hi - lo).abs()
+    assert float((step > 0).double().mean()) < 0.01  # (so that nearly every value's rounding is known)
+    a = r.abs() + step
+    wd, xd = w.double(), x.double()
+    rt, st, at = r.t().contiguous(), step.t().contiguous(), a.t().contiguous()
+    for k, ref, tol in (("dx", f * (r @ wd), f * (step @ wd.abs() + 2 * U * (cout + 6) * (a @ wd.abs()))),
+                        ("dweight", f * (rt @ xd), f * (st @ xd.abs() + 2 * U * (rows + 6) * (at @ xd.abs()))),
+                        ("dbias", f * dz.sum(0), f * (e.sum(0) + 2 * U * (rows + 6) * dz.abs().sum(0)))):
+        over = (got[k].double() - ref).abs() > tol + HALF["bf16"] * (ref.abs() + tol)
+        assert not bool(over.any()), f"{k}: {int(over.sum())} of {over.numel()} off"
