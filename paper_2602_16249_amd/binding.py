@@ -20,6 +20,7 @@ _libs = {}         # path -> loaded library
 
 AFFMAE_F32 = 0
 AFFMAE_BF16 = 1
+AFFMAE_ERR_UNSUPPORTED = -5
 _ACTS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
 
 _c_int = ctypes.c_int
@@ -644,6 +645,15 @@ def _on(index: int, t: torch.Tensor, name: str, dtype, shape=None) -> int:
     raise ValueError(f"{name} is on device {t.get_device()}, but device {index} is current")
 
 
+_INT_MAX = 2 ** 31 - 1
+
+
+def _ints(call: str, *sizes: int) -> None:
+    """Refuses sizes that a C int does not hold: ctypes would pass their low 32 bits, which the library cannot tell from a call of that size."""
+    if max(sizes) > _INT_MAX or min(sizes) < -_INT_MAX:
+        raise AffmaeError(call, AFFMAE_ERR_UNSUPPORTED)
+
+
 def _rng_on(index: int, rng: Optional[torch.Tensor], p: float) -> Optional[int]:
     """The generator's state, (seed, call number) in device memory; not needed where p is 0."""
     if rng is not None:
@@ -679,6 +689,8 @@ def affmae_linear_fwd(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torc
     if x.dim() < 1 or weight.dim() != 2 or x.shape[-1] != weight.shape[1]:
         raise ValueError(f"x must be [..., Cin] and weight [Cout, Cin], got {tuple(x.shape)} and {tuple(weight.shape)}")
     Cout, Cin = weight.shape
+    rows = x.numel() // max(Cin, 1)
+    _ints("affmae_linear_fwd", rows, Cin, Cout)
     shape = x.shape[:-1] + (Cout,)
     x_at = _on(dev, x, "x", dtype)
     w_at = _on(dev, weight, "weight", dtype)
@@ -695,7 +707,7 @@ def affmae_linear_fwd(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torc
     elif want_pre:
         pre = torch.empty_like(out)
         pre_at = pre.data_ptr()
-    rc = lib.affmae_linear_fwd(x_at, w_at, bias_at, res_at, x.numel() // max(Cin, 1), Cin, Cout, _act_code(act), float(p),
+    rc = lib.affmae_linear_fwd(x_at, w_at, bias_at, res_at, rows, Cin, Cout, _act_code(act), float(p),
                                _rng_on(dev, rng, p), code, out_at, pre_at, _stream())
     if rc != 0:
         raise AffmaeError("affmae_linear_fwd", rc)
@@ -720,6 +732,8 @@ def affmae_linear_bwd(x: Optional[torch.Tensor], weight: Optional[torch.Tensor],
     rows = dout.shape[:-1]
     Cout = dout.shape[-1]
     Cin = weight.shape[-1] if x is None else x.shape[-1]
+    n = dout.numel() // max(Cout, 1)
+    _ints("affmae_linear_bwd", n, Cin, Cout)
     dout_at = _on(dev, dout, "dout", dtype)
     x_at = None if x is None else _on(dev, x, "x", dtype, rows + (Cin,))
     w_at = None if weight is None else _on(dev, weight, "weight", dtype, (Cout, Cin))
@@ -737,7 +751,6 @@ def affmae_linear_bwd(x: Optional[torch.Tensor], weight: Optional[torch.Tensor],
     dx_at = grad("dx", rows + (Cin,)) if want_dx else None
     dw_at = grad("dweight", (Cout, Cin)) if want_dweight else None
     db_at = grad("dbias", (Cout,)) if want_dweight and want_dbias else None
-    n = dout.numel() // max(Cout, 1)
     a = _act_code(act)
     p = float(p)
     need = lib.affmae_linear_bwd_workspace_bytes(n, Cin, Cout, a, p, code, want_dx, want_dweight)
@@ -762,6 +775,7 @@ def affmae_norm_fwd(x: torch.Tensor, gamma: Optional[torch.Tensor], beta: Option
     if x.dim() != 3:
         raise ValueError(f"x must be [B,N,C], got {tuple(x.shape)}")
     B, N, C = x.shape
+    _ints("affmae_norm_fwd", B, N, C, groups)
     if (gamma is None) != (beta is None):
         raise ValueError("gamma and beta are given together or not at all")
     x_at = _on(dev, x, "x", dtype)
@@ -804,6 +818,7 @@ def affmae_norm_bwd(x: torch.Tensor, gamma: Optional[torch.Tensor], beta: Option
     if x.dim() != 3:
         raise ValueError(f"x must be [B,N,C], got {tuple(x.shape)}")
     B, N, C = x.shape
+    _ints("affmae_norm_bwd", B, N, C, groups)
     if (gamma is None) != (beta is None):
         raise ValueError("gamma and beta are given together or not at all")
     x_at = _on(dev, x, "x", dtype)
