@@ -285,7 +285,8 @@ struct Groups {  // what the kernels take
   float *mean, *rstd;   // [B,G]
   float2* group_part;   // [B][G][parts]: mean and M2, or the sums of dh and dh xhat
   float2* totals;       // [B][G]: these sums of the whole group, where a launch of its own adds them up
-  float* channel_part;  // [B][slabs][2][C]
+  float* channel_part;  // [runs][slabs][2][C]
+  int run;              // images of a workgroup of the sums, one after another
   float *dgamma, *dbeta;
   int sums;  // workgroups in front of the others that add up channel_part
 };
@@ -638,15 +639,17 @@ __global__ __launch_bounds__(kThreads) void norm_bwd_whole_kernel(Groups a, int 
   if (a.channel_part) channel_sums<E>(a, w, dg, db, sums, first);
 }
 
-// per workgroup: the sums of dz xhat and dz of its channels, and of dh xhat and dh of its groups
-template <typename T, int E>
+// per workgroup: the sums of dz xhat and dz of its channels over a run of images, and per image those of dh xhat and dh of its groups.
+// RUN: the run may be longer than an image.  (One kernel for both would hold twice the sums: 16 x 4096 x 384, one group, bf16: 58.6 us backward
+// instead of 53.3.)
+template <typename T, int E, bool RUN>
 __global__ __launch_bounds__(kThreads) void norm_bwd_sums_kernel(Groups a) {
   __shared__ float2 values[kThreads], result[kThreads];
   __shared__ float2 sums[kThreads * E];
-  const Place w(a, a.first + blockIdx.x);
+  constexpr int kAhead = RUN ? 1 : 4;  // tokens on their way (runs are of short images: 16384 x 8200 in bf16 601 us, with four 818)
+  Place w(a, a.first + blockIdx.x);
   const Cut& k = a.k;
-  const size_t bg = (size_t)w.b * a.G + w.group;
-  const float mean = a.mean[bg + w.q], rstd = a.rstd[bg + w.q];
+  const int run = w.b0, first = RUN ? run * a.run : run, last = RUN ? std::min(a.B, first + a.run) : run + 1;  // (the launch counts runs in the place of images)
   float gm[E], bt[E], dg[E], db[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) {
@@ -657,35 +660,46 @@ __global__ __launch_bounds__(kThreads) void norm_bwd_sums_kernel(Groups a) {
     load_piece<E>((const T*)a.gamma + w.c, gm);
     load_piece<E>((const T*)a.beta + w.c, bt);
   }
-  if (w.active) {
-#pragma unroll 4
-    for (int row = w.row0 + w.lane_row; row < w.row1; row += k.lanes) {
-      float x[E], g[E];
-      load_piece<E>((const T*)a.x + w.base + (size_t)row * a.C, x);
-      load_piece<E>((const T*)a.dout + w.base + (size_t)row * a.C, g);
-      slopes<E>(x, g, mean, rstd, a.gamma != nullptr, gm, bt, a.act);
+  for (int image = first; image < last; ++image) {
+    if constexpr (RUN) w.take(a, image);
+    const size_t bg = (size_t)image * a.G + w.group;
+    const float mean = a.mean[bg + w.q], rstd = a.rstd[bg + w.q];
+    float own[2][E] = {};  // of the image
+    float(&ig)[E] = RUN ? own[0] : dg, (&ib)[E] = RUN ? own[1] : db;
+    if (w.active) {
+#pragma unroll kAhead
+      for (int row = w.row0 + w.lane_row; row < w.row1; row += k.lanes) {
+        float x[E], g[E];
+        load_piece<E>((const T*)a.x + w.base + (size_t)row * a.C, x);
+        load_piece<E>((const T*)a.dout + w.base + (size_t)row * a.C, g);
+        slopes<E>(x, g, mean, rstd, a.gamma != nullptr, gm, bt, a.act);
 #pragma unroll
-      for (int e = 0; e < E; ++e) {
-        dg[e] = __builtin_fmaf(g[e], x[e], dg[e]);
-        db[e] += g[e];
+        for (int e = 0; e < E; ++e) {
+          ig[e] = __builtin_fmaf(g[e], x[e], ig[e]);
+          ib[e] += g[e];
+        }
       }
     }
-  }
-  float2 s = make_float2(0.f, 0.f);
+    float2 s = make_float2(0.f, 0.f);
 #pragma unroll
-  for (int e = 0; e < E; ++e) {
-    s.x = __builtin_fmaf(gm[e], db[e], s.x);
-    s.y = __builtin_fmaf(gm[e], dg[e], s.y);
+    for (int e = 0; e < E; ++e) {
+      s.x = __builtin_fmaf(gm[e], ib[e], s.x);
+      s.y = __builtin_fmaf(gm[e], ig[e], s.y);
+      if constexpr (RUN) {
+        dg[e] += ig[e];
+        db[e] += ib[e];
+      }
+    }
+    group_sums(a, w, s, values, result);
+    if ((int)threadIdx.x < w.groups) a.group_part[(bg + threadIdx.x) * k.parts() + w.part(a)] = result[threadIdx.x];
   }
-  group_sums(a, w, s, values, result);
-  if ((int)threadIdx.x < w.groups) a.group_part[(bg + threadIdx.x) * k.parts() + w.part(a)] = result[threadIdx.x];
-  if (a.channel_part) channel_sums<E>(a, w, dg, db, sums, (size_t)w.b0 * k.slabs + w.slab);
+  if (a.channel_part) channel_sums<E>(a, w, dg, db, sums, (size_t)run * k.slabs + w.slab);
 }
 
 template <typename T, int E, int V, bool JOIN>
-__global__ __launch_bounds__(kThreads) void norm_bwd_apply_kernel(Groups a, Cut parts_cut, int B) {
+__global__ __launch_bounds__(kThreads) void norm_bwd_apply_kernel(Groups a, Cut parts_cut, int channel_parts) {
   __shared__ float2 totals[kThreads];
-  if ((int)blockIdx.x < a.sums) return GroupSums::run(a.channel_part, B * parts_cut.slabs, a.C, blockIdx.x, &totals[0].x, a.dgamma, a.dbeta);
+  if ((int)blockIdx.x < a.sums) return GroupSums::run(a.channel_part, channel_parts, a.C, blockIdx.x, &totals[0].x, a.dgamma, a.dbeta);
   const Place w(a, a.first + blockIdx.x - a.sums);
   const Cut& k = a.k;
   const size_t bg = (size_t)w.b * a.G + w.group;
@@ -841,6 +855,13 @@ Cut cut_sums(int B, int N, int C, int G, int E) {
   cut_rows(k, N, std::max<long long>(4 * k.lanes, cdiv(N, slabs)));
   return k;
 }
+// Images of a workgroup of the sums.  A workgroup leaves sums of its channels, 8 bytes a channel, written and read once: at most 2048 of them, however many
+// images there are, and where images are short as many together as make that a quarter of what is read of x and dout, if it leaves 1024
+// workgroups.  (Layer norm of 65536 x 4100 in fp32, one row a workgroup: 2714 us and 2.15 GB of workspace; so 1482 us and 70 MB.)
+int run_of(int B, int N, const Cut& k, int el) {
+  const long long most = std::min<long long>(cdiv(16, (long long)el * N), (long long)B * k.blocks / 1024);
+  return (int)std::max<long long>(cdiv(B, 2048), k.slabs > 1 ? 1 : most);
+}
 
 // Rows that the row kernels hold: at most 4 pieces a lane, by a wave as long as that is enough, else by the workgroup.
 constexpr int kMostPieces = 4;
@@ -949,11 +970,11 @@ hipError_t groups_fwd(const NormArgs& a, hipStream_t stream) {
 struct BwdSpace {
   size_t totals, channels, all;
 };
-BwdSpace bwd_space(int B, int C, int G, const Cut& k) {
+BwdSpace bwd_space(int B, int C, int G, const Cut& k, int run) {
   BwdSpace s;
   s.totals = up256((size_t)B * G * k.parts() * sizeof(float2));
   s.channels = s.totals + up256((size_t)B * G * sizeof(float2));
-  s.all = s.channels + (size_t)B * k.slabs * 2 * C * sizeof(float);
+  s.all = s.channels + (size_t)cdiv(B, run) * k.slabs * 2 * C * sizeof(float);
   return s;
 }
 
@@ -974,15 +995,18 @@ hipError_t groups_bwd(const NormArgs& a, hipStream_t stream) {
     return hipGetLastError();
   }
   const Cut sums = cut_sums(a.B, a.N, a.C, a.G, E);
-  const BwdSpace at = bwd_space(a.B, a.C, a.G, sums);
+  const int run = run_of(a.B, a.N, sums, sizeof(T)), runs = cdiv(a.B, run);
+  const BwdSpace at = bwd_space(a.B, a.C, a.G, sums, run);
   char* ws = static_cast<char*>(a.workspace);
   Groups g = groups_of(a, sums);
   g.out = a.dx;
   g.group_part = reinterpret_cast<float2*>(ws);
   g.totals = reinterpret_cast<float2*>(ws + at.totals);
   g.channel_part = a.dgamma ? reinterpret_cast<float*>(ws + at.channels) : nullptr;
+  g.run = run;
   const dim3 threads(kThreads);
-  for_workgroups(g, a.B, [&](dim3 grid) { AFFMAE_LAUNCH("norm_bwd_sums_kernel", stream, (norm_bwd_sums_kernel<T, E>), grid, threads, 0, stream, g); });
+  const auto sums_kernel = run > 1 ? norm_bwd_sums_kernel<T, E, true> : norm_bwd_sums_kernel<T, E, false>;
+  for_workgroups(g, runs, [&](dim3 grid) { AFFMAE_LAUNCH("norm_bwd_sums_kernel", stream, sums_kernel, grid, threads, 0, stream, g); });
   const bool join = sums.parts() <= kJoinParts;
   if (!join) AFFMAE_LAUNCH("norm_join_kernel", stream, norm_join_kernel<true>, dim3(cdiv((long long)a.B * a.G, kWaves)), threads, 0, stream, g, a.B * a.G);
   constexpr int V = kHeldBwd / E;
@@ -994,7 +1018,7 @@ hipError_t groups_bwd(const NormArgs& a, hipStream_t stream) {
   g.dbeta = a.dbeta;
   g.sums = a.dgamma ? GroupSums::blocks(a.C) : 0;
   for_workgroups(g, a.B, [&](dim3 grid) {
-    AFFMAE_LAUNCH("norm_bwd_apply_kernel", stream, kernel, dim3(grid.x + g.sums), threads, 0, stream, g, sums, a.B);
+    AFFMAE_LAUNCH("norm_bwd_apply_kernel", stream, kernel, dim3(grid.x + g.sums), threads, 0, stream, g, sums, runs * sums.slabs);
     g.sums = 0;
   });
   return hipGetLastError();
@@ -1043,7 +1067,8 @@ size_t norm_bwd_workspace_bytes(int B, int N, int C, int G, int dtype) {
   Cut whole;
   int held, batches, workgroups;
   if (cut_bwd_whole(B, N, C, G, E, dtype == 1 ? 2 : 4, &whole, &held, &batches, &workgroups)) return (size_t)workgroups * 2 * C * sizeof(float);
-  return bwd_space(B, C, G, cut_sums(B, N, C, G, E)).all;
+  const Cut sums = cut_sums(B, N, C, G, E);
+  return bwd_space(B, C, G, sums, run_of(B, N, sums, dtype == 1 ? 2 : 4)).all;
 }
 hipError_t launch_norm_fwd(const NormArgs& a, hipStream_t stream) { return a.dtype == 1 ? fwd<bf16_t>(a, stream) : fwd<float>(a, stream); }
 hipError_t launch_norm_bwd(const NormArgs& a, hipStream_t stream) { return a.dtype == 1 ? bwd<bf16_t>(a, stream) : bwd<float>(a, stream); }

@@ -9,6 +9,7 @@ from scipy import special
 
 import paper_2602_16249_amd as aff
 from oracle import dense
+from test_gpu_dense import Guarded, _close, _norm_bwd_bounds, _norm_inputs, _stored
 
 pytestmark = pytest.mark.gpu
 
@@ -115,3 +116,35 @@ def test_bf16_gradients_are_the_products_of_dz_rounded_once(rows, cin, cout, p):
                         ("dbias", f * dz.sum(0), f * (e.sum(0) + 2 * U * (rows + 6) * dz.abs().sum(0)))):
         over = (got[k].double() - ref).abs() > tol + HALF["bf16"] * (ref.abs() + tol)
         assert not bool(over.any()), f"{k}: {int(over.sum())} of {over.numel()} off"
+
+
+# ------------------------------------------------------------ norms whose channels' sums are taken over runs of images, backward
+
+WIDE = [  # dtype, B, N, C, groups: pieces of 16 bytes down to single values, shares of a group, whole groups beside each other
+    ("bf16", 2100, 1, 8200, 1), ("bf16", 2100, 1, 8196, 1), ("bf16", 1030, 1, 8198, 1), ("bf16", 1030, 1, 8201, 1), ("f32", 2100, 1, 4100, 1),
+    ("f32", 1030, 1, 4098, 1), ("f32", 4100, 1, 4097, 1), ("bf16", 300, 1, 20000, 1), ("bf16", 2300, 3, 2600, 1), ("bf16", 2100, 3, 302, 2),
+    ("f32", 6200, 2, 302, 2), ("bf16", 2049, 2, 4112, 2),
+]
+
+
+@pytest.mark.parametrize("dtype,B,N,C,G", WIDE)
+def test_norm_backward_over_runs_of_images(dtype, B, N, C, G):
+    name = ["silu", "none", "relu"][(B + N + C) % 3]
+    d = _norm_inputs(dtype, B, N, C, seed=11)
+    v = {k: a[1] for k, a in d.items()}
+    _, mean, rstd = dense.norm_fwd(v["x"], v["gamma"], v["beta"], G, 1e-5)
+    (tm, mean), (tr, rstd) = _stored(mean, "f32"), _stored(rstd, "f32")
+    ref, bounds = _norm_bwd_bounds(v, mean, rstd, G, name, True, dtype)
+    g = {"dx": Guarded((B, N, C), TYPES[dtype]), "dgamma": Guarded((C,), torch.float32), "dbeta": Guarded((C,), torch.float32)}
+    args = (d["x"][0], d["gamma"][0], d["beta"][0], tm, tr, d["dout"][0], G)
+    need = aff.load_library().affmae_norm_bwd_workspace_bytes(B, N, C, G, 1 if dtype == "bf16" else 0)
+    space = torch.full((need + 512,), 77, dtype=torch.uint8, device="cuda")
+    aff.affmae_norm_bwd(*args, act=name, grads={k: o.t for k, o in g.items()}, workspace=space[256:256 + need])
+    for k in g:
+        _close(g[k].t, ref[k], bounds[k], k)
+        g[k].check()
+    assert bool((space[:256] == 77).all()) and bool((space[256 + need:] == 77).all())
+    again = aff.affmae_norm_bwd(*args, act=name)
+    assert all(torch.equal(again[k], g[k].t) for k in g)
+    bare = aff.affmae_norm_bwd(args[0], None, None, *args[3:])  # (no gamma: no sums of channels)
+    assert set(bare) == {"dx"} and bool(torch.isfinite(bare["dx"]).all())
