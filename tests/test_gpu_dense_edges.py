@@ -9,7 +9,8 @@ from scipy import special
 
 import paper_2602_16249_amd as aff
 from oracle import dense
-from test_gpu_dense import Guarded, _close, _norm_bwd_bounds, _norm_inputs, _stored
+from product_sizes import SIZES
+from test_gpu_dense import Guarded, _close, _norm_bwd_bounds, _norm_inputs, _shifted, _stored
 
 pytestmark = pytest.mark.gpu
 
@@ -148,3 +149,65 @@ def test_norm_backward_over_runs_of_images(dtype, B, N, C, G):
     assert all(torch.equal(again[k], g[k].t) for k in g)
     bare = aff.affmae_norm_bwd(args[0], None, None, *args[3:])  # (no gamma: no sums of channels)
     assert set(bare) == {"dx"} and bool(torch.isfinite(bare["dx"]).all())
+
+
+# ------------------------------------------------------------------------------------------------ every tile of the products
+
+@pytest.mark.parametrize("dtype,rows,cin,cout,made,shift", SIZES)
+def test_every_tile_of_the_products(dtype, rows, cin, cout, made, shift):
+    """Forward and gradients against products in 64 bits on the device, value by value, in outputs with guards around them.  gelu is off by
+    (z^2 + 24) U of |z| Phi(-|z|) and 3 U |z| of what is left, its slope by as much of Phi(-|z|) + |z| phi(z) and 2 U; a sum of n terms by 2 U (n + 5)
+    of their sizes."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(rows + cin)
+    normal = lambda *shape, std=1.0: _shifted((torch.randn(*shape, generator=g, device="cuda") * std).to(TYPES[dtype]), shift)
+    x, w, b, r, dout, pre = (normal(rows, cin), normal(cout, cin, std=cin ** -0.5), normal(cout, std=0.3), normal(rows, cout), normal(rows, cout),
+                             normal(rows, cout, std=1.5))
+    act, p = ("gelu", 0.2) if made else ("none", 0.0)
+    rng = torch.tensor([2602, 41], dtype=torch.int64, device="cuda")
+    f = 1.0 / (1.0 - float(np.float32(p)))
+    keep = torch.from_numpy(dense.keep((rows, cout), p, 2602, 41)).cuda() if made else None
+    half = HALF[dtype]
+
+    def close(got, ref, tol, what):
+        got.check()
+        over = ~((got.t.double() - ref).abs() <= tol + half * (ref.abs() + tol))
+        assert not bool(over.any()), f"{what}: {int(over.sum())} of {over.numel()} off, first at {over.nonzero()[0].tolist()}"
+
+    tail = lambda z: 0.5 * torch.special.erfc(z.abs() * 2 ** -0.5)
+    cdf = lambda z: 0.5 * torch.special.erfc(-z * 2 ** -0.5)
+    density = lambda z: torch.exp(-0.5 * z * z) * (2 * np.pi) ** -0.5
+    guarded = lambda *shape: Guarded(shape, TYPES[dtype], shift)
+
+    out, zo = guarded(rows, cout), guarded(rows, cout)
+    aff.affmae_linear_fwd(x, w, b, r, act=act, p=p, rng=rng, out=out.t, pre=zo.t)
+    xd, wt = x.double(), w.double().t().contiguous()
+    z = xd @ wt + b.double()
+    e = 2 * U * (cin + 5) * (xd.abs() @ wt.abs() + b.double().abs())
+    close(zo, z, e, "pre")
+    if made:
+        branch = torch.where(keep, z * cdf(z) * f, 0.0)
+        e = f * (1.13 * e + U * ((z * z + 24) * z.abs() * tail(z) + 3 * z.abs())) + 4 * U * f * z.abs()
+    else:
+        branch = z
+    ref = r.double() + branch
+    close(out, ref, e + U * (r.double().abs() + ref.abs()), "out")
+    del out, zo, xd, wt, z, e, branch, ref
+
+    dx, dw, db = guarded(rows, cin), guarded(cout, cin), guarded(cout)
+    aff.affmae_linear_bwd(x, w, dout, pre if made else None, act=act, p=p, rng=rng, grads={"dx": dx.t, "dweight": dw.t, "dbias": db.t})
+    d, z = dout.double(), pre.double()
+    if made:
+        d = torch.where(keep, d * f, 0.0)
+        e = U * d.abs() * ((z * z + 24) * (tail(z) + z.abs() * density(z)) + 2) + 4 * U * d.abs()
+        dz = d * (cdf(z) + z * density(z))
+        e0, e = e, e + (half * (dz.abs() + e) if dtype == "bf16" else 0.0)  # dz rounded once as an operand, not for dbias
+    else:
+        dz, e = d, torch.zeros_like(d)
+        e0 = e
+    a = dz.abs() + e
+    wd, xd = w.double(), x.double()
+    close(dx, dz @ wd, e @ wd.abs() + 2 * U * (cout + 6) * (a @ wd.abs()), "dx")
+    zt, et, at = dz.t().contiguous(), e.t().contiguous(), a.t().contiguous()
+    close(dw, zt @ xd, et @ xd.abs() + 2 * U * (rows + 6) * (at @ xd.abs()), "dweight")
+    close(db, dz.sum(0), e0.sum(0) + 2 * U * (rows + 6) * (dz.abs() + e0).sum(0), "dbias")
