@@ -211,3 +211,29 @@ def test_every_tile_of_the_products(dtype, rows, cin, cout, made, shift):
     zt, et, at = dz.t().contiguous(), e.t().contiguous(), a.t().contiguous()
     close(dw, zt @ xd, et @ xd.abs() + 2 * U * (rows + 6) * (at @ xd.abs()), "dweight")
     close(db, dz.sum(0), e0.sum(0) + 2 * U * (rows + 6) * (dz.abs() + e0).sum(0), "dbias")
+
+
+# -------------------------------------------------------------------------------- sums over as many tokens as there may be
+
+@pytest.mark.parametrize("B,N,C,G,serial", [
+    # terms that a sum adds one after another: by a thread, over the threads of a column, over a run of parts and over the runs.  What a launch does:
+    (1, 2 ** 31 - 2 ** 16, 1, 1, 2 ** 13 + 256 + 64 + 16),  # 1024 workgroups of 2097088 tokens, 256 threads a column; 16 runs of 64 parts
+    (2, 9_000_005, 128, 4, 1099 + 16 + 64 + 16),            # 2 x 512 workgroups of 17579 tokens, 16 threads a column; the same
+    (16_777_215, 1, 136, 1, 2048 + 8 + 32 + 32),            # 1024 workgroups, 8 rows at a time; 32 runs of 32 parts
+])
+def test_channel_sums_of_very_many_tokens(B, N, C, G, serial):
+    """-1, 1, -1, ... and dout = x: the terms of dgamma are all rstd, so that it is tokens x rstd up to `serial` roundings (a part of the
+    thousand that went missing would be 1e-3 of it); dbeta's are whole numbers, exact up to 2^24 and then off by one an addition."""
+    x = torch.ones(B, N, C, dtype=torch.bfloat16, device="cuda")
+    flat = x.view(-1)
+    flat[::2] = -1
+    gamma, beta = torch.full((C,), 3.0, device="cuda").bfloat16(), torch.zeros(C, device="cuda").bfloat16()
+    out, mean, rstd = aff.affmae_norm_fwd(x, gamma, beta, G, eps=1e-5)
+    assert bool((mean == 0).all()) and bool((rstd == rstd.view(-1)[0]).all())
+    got = aff.affmae_norm_bwd(x, gamma, beta, mean, rstd, x, G, grads={"dx": out})
+    tokens = B * N
+    r = float(rstd.view(-1)[0])
+    assert float((got["dgamma"].double() / (tokens * r) - 1).abs().max()) <= (serial + 8) * U
+    # (an odd number of channels: a channel's signs alternate from token to token; an even one: they are the same in all)
+    want = torch.zeros(C) if C % 2 else torch.where(torch.arange(C) % 2 == 0, -tokens, tokens)
+    assert float((got["dbeta"].double().cpu() - want.double()).abs().max()) <= (0 if tokens % 2 == 0 and C % 2 else 4)
