@@ -470,7 +470,7 @@ int affmae_dropout_bwd(const void* dout, int64_t n, float p, const int64_t* rng,
  *                      the activation and the mask in one kernel
  *   x        in  [rows,Cin]    weight  in  [Cout,Cin]    bias  in  [Cout] or NULL
  *   residual in  [rows,Cout] or NULL
- *   out      out [rows,Cout]; may be residual
+ *   out      out [rows,Cout]; may be residual (unless that shares memory with x)
  *   pre      out [rows,Cout] or NULL: z, which the backward of an activation needs
  *   all in `dtype`, sums in fp32, one rounding (to nearest even) of each output; act,
  *   p, rng: affmae_act and the dropout above, over the elements of out.
@@ -522,6 +522,7 @@ int affmae_linear_bwd(const void* x, const void* weight, const void* pre, const 
  *   dgamma, dbeta out [C] fp32: sums of dz (x - mean) rstd and of dz; or both NULL
  *   workspace     affmae_norm_bwd_workspace_bytes(...) bytes, may be 0
  *
+ * Outputs must not overlap inputs or each other.
  * Statistics and sums are fp32, added in a fixed order; a variance is the mean square
  * about the mean (never a difference of squares), so that offsets large against the
  * spread cost no digits.
