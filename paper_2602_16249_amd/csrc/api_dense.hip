@@ -37,7 +37,8 @@ int check_norm_shape(int B, int N, int C, int groups, int dtype) {
   const int rc = check_type(dtype);
   if (rc != AFFMAE_OK) return rc;
   if (B < 1 || N < 1 || C < 1 || groups < 1 || C % groups) return AFFMAE_ERR_SHAPE;
-  // tokens are counted in 31 bits, a workgroup's run of them (at most 2^14) beyond the last among them
+  // tokens are counted in 31 bits, and those beyond the last that a workgroup's threads look at: up to 64 times 256 where they hold its run
+  // in registers, up to 255 where they walk it
   if ((long long)B * N > (1ll << 31) - (1 << 16) || (long long)B * groups > (1ll << 24)) return AFFMAE_ERR_UNSUPPORTED;
   if (C > (1 << 20) || (long long)B * N * C > (1ll << 38)) return AFFMAE_ERR_UNSUPPORTED;
   return AFFMAE_OK;

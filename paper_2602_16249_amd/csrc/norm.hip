@@ -327,7 +327,7 @@ struct Place {
     }
     c = (first_col + (col < cols ? col : 0)) * k.E;
     row0 = slab * k.rows;
-    row1 = std::min(row0 + k.rows, a.N);
+    row1 = row0 + std::min(k.rows, a.N - row0);  // (row0 + k.rows may be beyond 31 bits)
     take(a, batch);
   }
   // the images of the batch-th workgroup of a block and slab
