@@ -648,10 +648,9 @@ def _on(index: int, t: torch.Tensor, name: str, dtype, shape=None) -> int:
 _INT_MAX = 2 ** 31 - 1
 
 
-def _ints(call: str, *sizes: int) -> None:
-    """Refuses sizes that a C int does not hold: ctypes would pass their low 32 bits, which the library cannot tell from a call of that size."""
-    if max(sizes) > _INT_MAX or min(sizes) < -_INT_MAX:
-        raise AffmaeError(call, AFFMAE_ERR_UNSUPPORTED)
+def _beyond_int(call: str):
+    """Of sizes that a C int does not hold: ctypes would pass their low 32 bits, which the library cannot tell from a call of that size."""
+    raise AffmaeError(call, AFFMAE_ERR_UNSUPPORTED)
 
 
 def _rng_on(index: int, rng: Optional[torch.Tensor], p: float) -> Optional[int]:
@@ -690,7 +689,8 @@ def affmae_linear_fwd(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torc
         raise ValueError(f"x must be [..., Cin] and weight [Cout, Cin], got {tuple(x.shape)} and {tuple(weight.shape)}")
     Cout, Cin = weight.shape
     rows = x.numel() // max(Cin, 1)
-    _ints("affmae_linear_fwd", rows, Cin, Cout)
+    if rows > _INT_MAX or Cin > _INT_MAX or Cout > _INT_MAX:
+        _beyond_int("affmae_linear_fwd")
     shape = x.shape[:-1] + (Cout,)
     x_at = _on(dev, x, "x", dtype)
     w_at = _on(dev, weight, "weight", dtype)
@@ -733,7 +733,8 @@ def affmae_linear_bwd(x: Optional[torch.Tensor], weight: Optional[torch.Tensor],
     Cout = dout.shape[-1]
     Cin = weight.shape[-1] if x is None else x.shape[-1]
     n = dout.numel() // max(Cout, 1)
-    _ints("affmae_linear_bwd", n, Cin, Cout)
+    if n > _INT_MAX or Cin > _INT_MAX or Cout > _INT_MAX:
+        _beyond_int("affmae_linear_bwd")
     dout_at = _on(dev, dout, "dout", dtype)
     x_at = None if x is None else _on(dev, x, "x", dtype, rows + (Cin,))
     w_at = None if weight is None else _on(dev, weight, "weight", dtype, (Cout, Cin))
@@ -775,7 +776,8 @@ def affmae_norm_fwd(x: torch.Tensor, gamma: Optional[torch.Tensor], beta: Option
     if x.dim() != 3:
         raise ValueError(f"x must be [B,N,C], got {tuple(x.shape)}")
     B, N, C = x.shape
-    _ints("affmae_norm_fwd", B, N, C, groups)
+    if B > _INT_MAX or N > _INT_MAX or C > _INT_MAX or not -_INT_MAX <= groups <= _INT_MAX:
+        _beyond_int("affmae_norm_fwd")
     if (gamma is None) != (beta is None):
         raise ValueError("gamma and beta are given together or not at all")
     x_at = _on(dev, x, "x", dtype)
@@ -818,7 +820,8 @@ def affmae_norm_bwd(x: torch.Tensor, gamma: Optional[torch.Tensor], beta: Option
     if x.dim() != 3:
         raise ValueError(f"x must be [B,N,C], got {tuple(x.shape)}")
     B, N, C = x.shape
-    _ints("affmae_norm_bwd", B, N, C, groups)
+    if B > _INT_MAX or N > _INT_MAX or C > _INT_MAX or not -_INT_MAX <= groups <= _INT_MAX:
+        _beyond_int("affmae_norm_bwd")
     if (gamma is None) != (beta is None):
         raise ValueError("gamma and beta are given together or not at all")
     x_at = _on(dev, x, "x", dtype)
