@@ -14,16 +14,16 @@ enum Act { kActNone = 0, kActRelu = 1, kActGelu = 2, kActSilu = 3 };
 // polynomial in t, fitted by least squares weighted towards the largest relative error up to |z| = 14.5, where exp(-z^2 / 2) is below the
 // least fp32.  The error is relative, also in the tail, where the published short forms of erf have an absolute one (1.5e-7: gelu(-5)
 // off by 1.6e-3 of itself).
-//   ten terms (c = 3/8): 4e-8 with coefficients of fp32, an error of t counting 2.1 times near 0, hence the reciprocal's correction.  Against 64
-//   bits, z of spread 1.1, root mean square: gelu 3.5e-8, its slope 5.0e-8 (a library's erf: 3.8e-8 and 4.1e-8).
-//   BRIEF, eight terms (c = 5/16): 2.3e-7, for values that leave as bf16 (half a step: 3.9e-3).  131072 x 64 -> 192 with gelu, bf16: 27.0 us, with
-//   ten terms 29.7.
+//   ten terms (c = 3/8): 4e-8 with coefficients of fp32; an error of t counts 2.1 times near 0.  Against 64 bits, z of spread 1.1, root mean square:
+//   gelu 3.5e-8, its slope 5.1e-8 (a library's erf: 3.8e-8 and 4.1e-8).  A second step of the reciprocal changes neither.
+//   BRIEF, eight terms (c = 5/16): 2.3e-7, for bf16 tensors (half a step: 3.9e-3).  131072 x 64 -> 192 with gelu 26.9 us, with ten terms 27.5; layer
+//   norm of 65536 x 256 with gelu 21.2 and 21.7, backward 31.2 and 32.1 (dgamma off by 1.9e-7 either way, from its sums).
 template <bool BRIEF>
 __device__ __forceinline__ void normal_cdf(float z, float& cdf, float& density) {
   const float e = __expf(-0.5f * z * z);
-  float t, s;
+  const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(BRIEF ? 0.3125f : 0.375f, fabsf(z), 1.f));
+  float s;
   if constexpr (BRIEF) {
-    t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.3125f, fabsf(z), 1.f));
     s = __builtin_fmaf(0.035328057f, t, -0.1358021f);
     s = __builtin_fmaf(s, t, 0.14035626f);
     s = __builtin_fmaf(s, t, -0.004521572f);
@@ -32,9 +32,6 @@ __device__ __forceinline__ void normal_cdf(float z, float& cdf, float& density) 
     s = __builtin_fmaf(s, t, 0.1249033f);
     s = __builtin_fmaf(s, t, 0.12466235f);
   } else {
-    const float d = __builtin_fmaf(0.375f, fminf(fabsf(z), 64.f), 1.f);  // (a finite one for infinities: the correction is inf * 0 there)
-    t = __builtin_amdgcn_rcpf(d);
-    t = __builtin_fmaf(__builtin_fmaf(-d, t, 1.f), t, t);
     s = __builtin_fmaf(0.02089967f, t, -0.13400264f);
     s = __builtin_fmaf(s, t, 0.3448391f);
     s = __builtin_fmaf(s, t, -0.42401287f);
@@ -51,7 +48,7 @@ __device__ __forceinline__ void normal_cdf(float z, float& cdf, float& density) 
 }
 __device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.f + __expf(-z)); }
 
-// z becomes its activation (one branch for all of them, not one for each); BRIEF: it leaves as bf16 only
+// z becomes its activation (one branch for all of them, not one for each); BRIEF: of bf16 tensors
 template <bool BRIEF, int E>
 __device__ __forceinline__ void act_values(float (&z)[E], int act) {
   if (act == kActRelu) {
@@ -69,7 +66,7 @@ __device__ __forceinline__ void act_values(float (&z)[E], int act) {
     for (int e = 0; e < E; ++e) z[e] *= sigmoid(z[e]);
   }
 }
-// g becomes g act'(z); BRIEF likewise
+// g becomes g act'(z)
 template <bool BRIEF, int E>
 __device__ __forceinline__ void act_slopes(float (&g)[E], const float (&z)[E], int act) {
   if (act == kActRelu) {

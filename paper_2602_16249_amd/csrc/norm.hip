@@ -28,18 +28,18 @@ constexpr int kWaves = kThreads / kWave;
 int cdiv(long long a, long long b) { return (int)((a + b - 1) / b); }
 size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 
-// z = xhat gamma + beta, out = act(z)
-template <int E>
+// z = xhat gamma + beta, out = act(z); BRIEF: see normal_cdf
+template <bool BRIEF, int E>
 __device__ __forceinline__ void normalise(float (&v)[E], float mean, float rstd, bool affine, const float (&gm)[E], const float (&bt)[E], int act) {
 #pragma unroll
   for (int e = 0; e < E; ++e) {
     v[e] = (v[e] - mean) * rstd;
     if (affine) v[e] = __builtin_fmaf(v[e], gm[e], bt[e]);
   }
-  act_values<false, E>(v, act);
+  act_values<BRIEF, E>(v, act);
 }
 // x becomes xhat, g (dout) becomes dz = dout act'(z)
-template <int E>
+template <bool BRIEF, int E>
 __device__ __forceinline__ void slopes(float (&x)[E], float (&g)[E], float mean, float rstd, bool affine, const float (&gm)[E], const float (&bt)[E], int act) {
 #pragma unroll
   for (int e = 0; e < E; ++e) x[e] = (x[e] - mean) * rstd;
@@ -47,7 +47,7 @@ __device__ __forceinline__ void slopes(float (&x)[E], float (&g)[E], float mean,
     float z[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) z[e] = affine ? __builtin_fmaf(x[e], gm[e], bt[e]) : x[e];
-    act_slopes<false, E>(g, z, act);  // (dgamma and dbeta leave as fp32)
+    act_slopes<BRIEF, E>(g, z, act);
   }
 }
 
@@ -127,7 +127,7 @@ __global__ __launch_bounds__(kThreads) void norm_rows_fwd_kernel(const T* __rest
     for (int p = 0; p < PIECES; ++p) {
       const int c = (p * LANES + l) * E;
       if (c >= C) continue;
-      normalise<E>(v[p], m, r, gamma != nullptr, gm[p], bt[p], act);
+      normalise<sizeof(T) == 2, E>(v[p], m, r, gamma != nullptr, gm[p], bt[p], act);
       store_some<E>(out + row * C + c, there(c), v[p]);
     }
   }
@@ -179,7 +179,7 @@ __global__ __launch_bounds__(kThreads) void norm_rows_bwd_kernel(const T* __rest
 #pragma unroll
       for (int p = 0; p < PIECES; ++p) {
         if ((p * LANES + l) * E >= C) continue;
-        slopes<E>(v[t][p], g[t][p], m[t], r[t], gamma != nullptr, gm[p], bt[p], act);
+        slopes<sizeof(T) == 2, E>(v[t][p], g[t][p], m[t], r[t], gamma != nullptr, gm[p], bt[p], act);
 #pragma unroll
         for (int e = 0; e < E; ++e) {
           if (row < rows) {
@@ -484,7 +484,7 @@ __global__ __launch_bounds__(kThreads) void norm_stats_kernel(Groups a) {
     for (int i = 0; i < V; ++i) {
       const int row = w.row0 + i * k.lanes + w.lane_row;
       if (row >= w.row1) continue;
-      normalise<E>(v[i], mean, rstd, a.gamma != nullptr, gm, bt, a.act);
+      normalise<sizeof(T) == 2, E>(v[i], mean, rstd, a.gamma != nullptr, gm, bt, a.act);
       store_piece<E>((T*)a.out + w.base + (size_t)row * a.C, v[i]);
     }
   } else {
@@ -554,7 +554,7 @@ __global__ __launch_bounds__(kThreads) void norm_apply_kernel(Groups a) {
   for (int i = 0; i < V; ++i) {
     const int row = w.row0 + i * k.lanes + w.lane_row;
     if (row >= w.row1) continue;
-    normalise<E>(v[i], mean, rstd, a.gamma != nullptr, gm, bt, a.act);
+    normalise<sizeof(T) == 2, E>(v[i], mean, rstd, a.gamma != nullptr, gm, bt, a.act);
     store_piece<E>((T*)a.out + w.base + (size_t)row * a.C, v[i]);
   }
 }
@@ -615,7 +615,7 @@ __global__ __launch_bounds__(kThreads) void norm_bwd_whole_kernel(Groups a, int 
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       if (!w.active || i * k.lanes + w.lane_row >= a.N) continue;
-      slopes<E>(x[i], g[i], mean, rstd, a.gamma != nullptr, gm, bt, a.act);
+      slopes<sizeof(T) == 2, E>(x[i], g[i], mean, rstd, a.gamma != nullptr, gm, bt, a.act);
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         dg[e] = __builtin_fmaf(g[i][e], x[i][e], dg[e]);
@@ -672,7 +672,7 @@ __global__ __launch_bounds__(kThreads) void norm_bwd_sums_kernel(Groups a) {
         float x[E], g[E];
         load_piece<E>((const T*)a.x + w.base + (size_t)row * a.C, x);
         load_piece<E>((const T*)a.dout + w.base + (size_t)row * a.C, g);
-        slopes<E>(x, g, mean, rstd, a.gamma != nullptr, gm, bt, a.act);
+        slopes<sizeof(T) == 2, E>(x, g, mean, rstd, a.gamma != nullptr, gm, bt, a.act);
 #pragma unroll
         for (int e = 0; e < E; ++e) {
           ig[e] = __builtin_fmaf(g[e], x[e], ig[e]);
@@ -743,7 +743,7 @@ __global__ __launch_bounds__(kThreads) void norm_bwd_apply_kernel(Groups a, Cut 
   for (int i = 0; i < V; ++i) {
     const int row = w.row0 + i * k.lanes + w.lane_row;
     if (row >= w.row1) continue;
-    slopes<E>(x[i], g[i], mean, rstd, a.gamma != nullptr, gm, bt, a.act);
+    slopes<sizeof(T) == 2, E>(x[i], g[i], mean, rstd, a.gamma != nullptr, gm, bt, a.act);
 #pragma unroll
     for (int e = 0; e < E; ++e) g[i][e] = rstd * (g[i][e] * gm[e] - s1 - x[i][e] * s2);
     store_piece<E>((T*)a.out + w.base + (size_t)row * a.C, g[i]);

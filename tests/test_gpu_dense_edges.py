@@ -27,9 +27,9 @@ def _gelu_points(dtype):
 
 
 # Relative errors in units of U.  The exponent z^2 / 2: z z and its product with -1/2 log2(e) are rounded once each, 2 U (z^2 / 2) = z^2 U of
-# the result together; the hardware's exponential is off by 2 U (one step); the polynomial's fit by 0.7 (fp32) or 4 (bf16); t by 2, which counts
-# 2.1 times (4.2), or uncorrected and 2.7 times (5.4); the last of the sum's roundings, sum of |terms| / value 3.6 at t = 1, count 7; s t, its
-# product with e, 1 - tail and z cdf one each.  In all z^2 + 18 in fp32, z^2 + 22.4 in bf16: z^2 + 24 is taken.
+# the result together; the hardware's exponential is off by 2 U (one step); the polynomial's fit by 0.7 (fp32) or 4 (bf16); t = 1 / (1 + c |z|) by
+# the hardware's reciprocal, 2 U, which counts 2.1 (fp32) or 2.7 times (bf16), 4.2 or 5.4; the last of the sum's roundings, sum of |terms| / value
+# 3.6 at t = 1, count 7; s t, its product with e, 1 - tail and z cdf one each.  In all z^2 + 18 in fp32, z^2 + 22.4 in bf16: z^2 + 24 is taken.
 ROUNDINGS = 24
 
 
