@@ -857,10 +857,11 @@ Cut cut_sums(int B, int N, int C, int G, int E) {
 }
 // Images of a workgroup of the sums.  A workgroup leaves sums of its channels, 8 bytes a channel, written and read once: at most 2048 of them, however many
 // images there are, and where images are short as many together as make that a quarter of what is read of x and dout, if it leaves 1024
-// workgroups.  (Layer norm of 65536 x 4100 in fp32, one row a workgroup: 2714 us and 2.15 GB of workspace; so 1482 us and 70 MB.)
+// workgroups.  (Layer norm of 65536 x 4100 in fp32, one row a workgroup: 2714 us and 2.15 GB of workspace; so 1490 us and 70 MB.)  Beside images of 64
+// bytes a channel and more they are little: at most 8192 of them (2500 x 400 x 256, one group, bf16: 528 us with one image a workgroup, 556 with two).
 int run_of(int B, int N, const Cut& k, int el) {
-  const long long most = std::min<long long>(cdiv(16, (long long)el * N), (long long)B * k.blocks / 1024);
-  return (int)std::max<long long>(cdiv(B, 2048), k.slabs > 1 ? 1 : most);
+  const long long image = (long long)el * N, together = std::min<long long>(cdiv(16, image), (long long)B * k.blocks / 1024);
+  return (int)std::max<long long>(cdiv(B, image < 64 ? 2048 : 8192), k.slabs > 1 ? 1 : together);
 }
 
 // Rows that the row kernels hold: at most 4 pieces a lane, by a wave as long as that is enough, else by the workgroup.

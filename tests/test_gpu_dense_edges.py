@@ -124,7 +124,7 @@ def test_bf16_gradients_are_the_products_of_dz_rounded_once(rows, cin, cout, p):
 WIDE = [  # dtype, B, N, C, groups: pieces of 16 bytes down to single values, shares of a group, whole groups beside each other
     ("bf16", 2100, 1, 8200, 1), ("bf16", 2100, 1, 8196, 1), ("bf16", 1030, 1, 8198, 1), ("bf16", 1030, 1, 8201, 1), ("f32", 2100, 1, 4100, 1),
     ("f32", 1030, 1, 4098, 1), ("f32", 4100, 1, 4097, 1), ("bf16", 300, 1, 20000, 1), ("bf16", 2300, 3, 2600, 1), ("bf16", 2100, 3, 302, 2),
-    ("f32", 6200, 2, 302, 2), ("bf16", 2049, 2, 4112, 2),
+    ("f32", 6200, 2, 302, 2), ("bf16", 2049, 2, 4112, 2), ("bf16", 8200, 33, 65, 1),
 ]
 
 

@@ -1,4 +1,5 @@
-"""The workspace of the norms' backward on the CPU: the sums of the channels take at most 2048 parts, however many images there are."""
+"""The workspace of the norms' backward on the CPU: the sums of the channels take at most 2048 parts, however many images there are (8192 of
+long ones)."""
 import pytest
 
 import paper_2602_16249_amd as aff
@@ -23,3 +24,9 @@ def test_layer_norms_on_both_sides_of_the_row_kernels_limit(dtype, el, limit):
 def test_many_short_images(B, N, C, G):
     for dtype in (0, 1):
         assert _need(B, N, C, G, dtype) <= 2048 * 2 * C * 4 + 8 * B * G * (-(-C // G // 256) + 2) + 1024
+
+
+@pytest.mark.parametrize("B,N,C,G", [(8192, 400, 256, 1), (8193, 400, 256, 1), (1 << 20, 64, 96, 3), (1 << 20, 33, 400, 1)])
+def test_many_long_images(B, N, C, G):
+    for dtype in (0, 1):
+        assert _need(B, N, C, G, dtype) <= 8192 * 2 * C * 4 + 8 * B * G * 3 + 1024
