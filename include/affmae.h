@@ -8,7 +8,8 @@
  * each token's K neighbours, the neighbourhood merging that downsamples the token
  * set between stages, and the point decoder's virtual sampled tokens; and the dense
  * operators of a block around them: matrix products with their epilogue, group and
- * layer norm with an activation, dropout.
+ * layer norm with an activation, dropout; and attention between all tokens with the
+ * rotary positions of its queries and keys.
  *
  * Conventions for every entry point
  *   - All tensor pointers are DEVICE pointers owned by the caller; the library
@@ -541,6 +542,92 @@ size_t affmae_norm_bwd_workspace_bytes(int B, int N, int C, int groups, int dtyp
 int affmae_norm_bwd(const void* x, const void* gamma, const void* beta, const float* mean, const float* rstd,
                     const void* dout, int B, int N, int C, int groups, int act, int dtype, void* dx, float* dgamma,
                     float* dbeta, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Rotary positions of queries and keys from the tokens' coordinates, on one to three
+ * axes (a token's x and y; time, height and width of a video's tokens), for dot products that
+ * depend on where two tokens lie from each other.  The d channels of a head are d / 2
+ * pairs; pair c of every head turns by the angle
+ *     t = sum_a coords[b,n,a] freq[c,a]
+ *     (x0, x1) -> (x0 cos t - x1 sin t, x0 sin t + x1 cos t)
+ * so that freq says which axis, or which direction of several, a pair follows, and how
+ * fast; a row of zeros leaves its pair as it is.  Angles are 64-bit up to the sine: an
+ * angle t is off by at most |t| 2^-52, sine and cosine by 2^-22 besides, for |t| < 2^40.
+ *
+ * affmae_rotary_fwd
+ *   q, q_out  [B,N,H,d] dtype     k, k_out  [B,N,Hk,d] dtype, or both NULL with Hk = 0:
+ *             keys of the same tokens, turned in the same launch
+ *   coords    in  [B,N,axes] fp32, finite     freq  in  [d/2,axes] fp32, finite
+ *   layout    pair c is channels 2c and 2c + 1 (AFFMAE_ROTARY_PAIRS), or c and c + d/2
+ *             (AFFMAE_ROTARY_HALVES)
+ *
+ * affmae_rotary_bwd   gradients of L = <dq_out, q_out> + <dk_out, k_out>
+ *   dq, dk    out, turned back: shapes of q and k
+ *   dcoords   out [B,N,axes] fp32 or NULL: sum over pairs of freq[c,a] times the sum over
+ *             heads of y0 dy1 - y1 dy0, fp32 sums in a fixed order; needs
+ *   q_out, k_out  in  what the forward call wrote (NULL without dcoords)
+ *   (freq is taken as given: it has no gradient.)
+ *
+ * q_out may be q and k_out k, dq may be dq_out and dk dk_out; outputs must not overlap
+ * anything else.  Any alignment (to the element); d / 2 a multiple of 4 (bf16 pairs) or 8
+ * (bf16 halves), of 2 or 4 for fp32, is the fastest.
+ * Limits: d <= 512, axes <= 3, H, Hk <= 4096, B*N <= 2^31 - 2^16, B*N*(H+Hk)*d <= 2^38.
+ * Errors: AFFMAE_ERR_NULL, AFFMAE_ERR_DTYPE, AFFMAE_ERR_SHAPE (sizes < 1, odd d, unknown
+ * layout, misaligned tensors), AFFMAE_ERR_UNSUPPORTED.
+ */
+typedef enum { AFFMAE_ROTARY_PAIRS = 0, AFFMAE_ROTARY_HALVES = 1 } affmae_rotary_layout;
+int affmae_rotary_fwd(const void* q, const void* k, const float* coords, const float* freq, int B, int N, int H, int Hk, int d,
+                      int axes, int layout, int dtype, void* q_out, void* k_out, void* stream);
+int affmae_rotary_bwd(const void* dq_out, const void* dk_out, const void* q_out, const void* k_out, const float* coords,
+                      const float* freq, int B, int N, int H, int Hk, int d, int axes, int layout, int dtype, void* dq, void* dk,
+                      float* dcoords, void* stream);
+
+/*
+ * Attention between all tokens of an image: the point decoder's self- and cross-attention,
+ * and encoder stages short enough for it (paper, Sec. "AFFMAE": the decoder's blocks).
+ * For every image b, query i and head h, with key head hk = h / (H / Hk),
+ *     z_j = scale <q[b,i,h,:], k[b,j,hk,:]>
+ *     z_j = cap tanh(z_j / cap)                                if cap > 0
+ *     z_j = z_j - slope[h] |q_xy[b,i] - k_xy[b,j]|             if slope is given
+ *     j is hidden unless q_doc[b,i] == k_doc[b,j] >= 0         if q_doc is given
+ *     out[b,i,h,:] = sum_j softmax(z)_j v[b,j,hk,:],   lse[b,i,h] = log(sum_j exp(z_j))
+ * without storing the scores, with fp32 statistics and sums whatever the storage type.  A
+ * query that sees no key gets out = 0 and lse = -infinity.
+ *
+ *   q            in  [B,Nq,H,d] dtype    k, v  in  [B,Nk,Hk,d] dtype, Hk a divisor of H
+ *   q_xy, k_xy   in  [B,Nq,2], [B,Nk,2] fp32, finite, and slope in [H] fp32: all or none
+ *   q_doc, k_doc in  [B,Nq], [B,Nk] int32 or both NULL: images that share a row (what masks
+ *                leave of them has different lengths).  Any ids in any order; tokens of
+ *                an image lying together are what lets whole tiles be skipped.  A negative
+ *                id is padding, whose vectors and places may hold anything; elsewhere
+ *                tensors must be finite, also where a pair is hidden.
+ *   out          out [B,Nq,H,d] dtype    lse  out [B,Nq,H] fp32
+ *   workspace    affmae_attn_fwd_workspace_bytes(...) bytes, may be 0
+ *
+ * affmae_attn_bwd   gradients of L = <dout, out>, from the forward call's out and lse:
+ *   dq [B,Nq,H,d], dk, dv [B,Nk,Hk,d] out dtype (of padding: zeros), dslope out [H] fp32 or
+ *   NULL.  fp32 sums in a fixed order.  For bf16 the operands p and dS of the products are
+ *   rounded to bf16.
+ *   workspace    affmae_attn_bwd_workspace_bytes(...) bytes
+ *
+ * Outputs must not overlap inputs or each other.  q, k, v, out, dout and gradients are
+ * 16-byte aligned, q_xy and k_xy 8-byte.
+ * Limits: d a multiple of 8 up to 128, H <= 4096, Nq, Nk <= 2^24, Nq * H / Hk <= 2^30,
+ * B * Hk * ceil(Nq * H / Hk / 128) and B * Hk * ceil(Nk / 128) <= 2^24 - 8
+ * (AFFMAE_ERR_UNSUPPORTED otherwise).
+ * Errors: AFFMAE_ERR_NULL, AFFMAE_ERR_DTYPE, AFFMAE_ERR_SHAPE (sizes < 1, H % Hk, a scale
+ * or cap that is not finite, cap < 0, misaligned tensors), AFFMAE_ERR_UNSUPPORTED,
+ * AFFMAE_ERR_WORKSPACE.
+ */
+size_t affmae_attn_fwd_workspace_bytes(int B, int Nq, int Nk, int H, int Hk, int d, int dtype, int docs);
+int affmae_attn_fwd(const void* q, const void* k, const void* v, const float* q_xy, const float* k_xy, const float* slope,
+                    const int32_t* q_doc, const int32_t* k_doc, int B, int Nq, int Nk, int H, int Hk, int d, float scale, float cap,
+                    int dtype, void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+size_t affmae_attn_bwd_workspace_bytes(int B, int Nq, int Nk, int H, int Hk, int d, int dtype, int docs, int want_dslope);
+int affmae_attn_bwd(const void* q, const void* k, const void* v, const float* q_xy, const float* k_xy, const float* slope,
+                    const int32_t* q_doc, const int32_t* k_doc, const void* out, const float* lse, const void* dout, int B, int Nq,
+                    int Nk, int H, int Hk, int d, float scale, float cap, int dtype, void* dq, void* dk, void* dv, float* dslope,
+                    void* workspace, size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

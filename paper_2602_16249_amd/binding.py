@@ -21,6 +21,7 @@ _libs = {}         # path -> loaded library
 AFFMAE_F32 = 0
 AFFMAE_BF16 = 1
 AFFMAE_ERR_UNSUPPORTED = -5
+_ROTARY_LAYOUTS = {"pairs": 0, "halves": 1}
 _ACTS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
 
 _c_int = ctypes.c_int
@@ -141,6 +142,20 @@ def _load(path: str):
     lib.affmae_dropout_fwd.argtypes = [_c_void_p, _c_void_p, ctypes.c_int64, _c_float, _c_void_p, _c_int, _c_void_p, _c_void_p]
     lib.affmae_dropout_bwd.restype = _c_int
     lib.affmae_dropout_bwd.argtypes = [_c_void_p, ctypes.c_int64, _c_float, _c_void_p, _c_int, _c_void_p, _c_void_p]
+    lib.affmae_rotary_fwd.restype = _c_int
+    lib.affmae_rotary_fwd.argtypes = [_c_void_p] * 4 + [_c_int] * 8 + [_c_void_p] * 3
+    lib.affmae_rotary_bwd.restype = _c_int
+    lib.affmae_rotary_bwd.argtypes = [_c_void_p] * 6 + [_c_int] * 8 + [_c_void_p] * 4
+    lib.affmae_attn_fwd_workspace_bytes.restype = _c_size_t
+    lib.affmae_attn_fwd_workspace_bytes.argtypes = [_c_int] * 8
+    lib.affmae_attn_fwd.restype = _c_int
+    lib.affmae_attn_fwd.argtypes = ([_c_void_p] * 8 + [_c_int] * 6 + [_c_float] * 2 + [_c_int] + [_c_void_p] * 3
+                                    + [_c_size_t, _c_void_p])
+    lib.affmae_attn_bwd_workspace_bytes.restype = _c_size_t
+    lib.affmae_attn_bwd_workspace_bytes.argtypes = [_c_int] * 9
+    lib.affmae_attn_bwd.restype = _c_int
+    lib.affmae_attn_bwd.argtypes = ([_c_void_p] * 11 + [_c_int] * 6 + [_c_float] * 2 + [_c_int] + [_c_void_p] * 5
+                                    + [_c_size_t, _c_void_p])
     _libs[path] = lib
     return lib
 
@@ -882,6 +897,173 @@ def affmae_dropout_bwd(dout: torch.Tensor, p: float, rng: Optional[torch.Tensor]
     if rc != 0:
         raise AffmaeError("affmae_dropout_bwd", rc)
     return dx
+
+
+def _rotary_args(call: str, dev: int, q: torch.Tensor, k: Optional[torch.Tensor], coords: torch.Tensor, freq: torch.Tensor,
+                 layout: str):
+    """Sizes, addresses and codes that both directions check and pass alike."""
+    code = _ROTARY_LAYOUTS.get(layout)
+    if code is None:
+        raise ValueError(f"layout must be one of {', '.join(_ROTARY_LAYOUTS)}, got {layout!r}")
+    if q.dim() != 4 or (k is not None and k.dim() != 4) or coords.dim() != 3:
+        raise ValueError("queries and keys must be [B,N,H,d] and coords [B,N,axes]")
+    B, N, H, d = q.shape
+    Hk = 0 if k is None else k.shape[2]
+    axes = coords.shape[2]
+    if max(B, N, H, d, Hk, axes) > _INT_MAX:
+        _beyond_int(call)
+    if k is not None and Hk < 1:
+        raise ValueError("keys need a head")
+    coords_at = _on(dev, coords, "coords", torch.float32, (B, N, axes))
+    freq_at = _on(dev, freq, "freq", torch.float32, (d // 2, axes))
+    return (B, N, H, Hk, d, axes, code), coords_at, freq_at, (B, N, Hk, d)
+
+
+def affmae_rotary_fwd(q: torch.Tensor, coords: torch.Tensor, freq: torch.Tensor, k: Optional[torch.Tensor] = None,
+                      layout: str = "pairs", q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None
+                      ) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
+    """Rotary positions: q [B,N,H,d] and, if given, k [B,N,Hk,d] of the same tokens -> (q_out, k_out or None), pair c of every head
+    turned by coords [B,N,axes] . freq [d/2,axes], both fp32.  layout: pair c is channels 2c, 2c + 1 ("pairs") or c, c + d/2
+    ("halves").  q_out may be q, k_out may be k."""
+    lib = load_library()
+    code = _dtype_code(q)
+    dev = _current(q)
+    sizes, coords_at, freq_at, k_shape = _rotary_args("affmae_rotary_fwd", dev, q, k, coords, freq, layout)
+    q_at = _on(dev, q, "q", q.dtype)
+    k_at = None if k is None else _on(dev, k, "k", q.dtype, k_shape)
+    if q_out is None:
+        q_out = torch.empty_like(q)
+    to_q = _on(dev, q_out, "q_out", q.dtype, q.shape)
+    to_k = None
+    if k is not None:
+        if k_out is None:
+            k_out = torch.empty_like(k)
+        to_k = _on(dev, k_out, "k_out", q.dtype, k_shape)
+    elif k_out is not None:
+        raise ValueError("k_out without k")
+    rc = lib.affmae_rotary_fwd(q_at, k_at, coords_at, freq_at, *sizes, code, to_q, to_k, _stream())
+    if rc != 0:
+        raise AffmaeError("affmae_rotary_fwd", rc)
+    return q_out, k_out
+
+
+def affmae_rotary_bwd(dq_out: torch.Tensor, coords: torch.Tensor, freq: torch.Tensor, dk_out: Optional[torch.Tensor] = None,
+                      layout: str = "pairs", q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None,
+                      want_dcoords: bool = False, grads: Optional[Dict[str, torch.Tensor]] = None) -> Dict[str, torch.Tensor]:
+    """Gradients of affmae_rotary_fwd -> dict(dq[, dk: with dk_out][, dcoords [B,N,axes] fp32: if asked for, from the forward's
+    q_out and k_out]).  dq may be dq_out, dk may be dk_out."""
+    lib = load_library()
+    code = _dtype_code(dq_out)
+    dev = _current(dq_out)
+    dtype = dq_out.dtype
+    sizes, coords_at, freq_at, k_shape = _rotary_args("affmae_rotary_bwd", dev, dq_out, dk_out, coords, freq, layout)
+    dq_out_at = _on(dev, dq_out, "dq_out", dtype)
+    dk_out_at = None if dk_out is None else _on(dev, dk_out, "dk_out", dtype, k_shape)
+    q_at = k_at = None
+    if want_dcoords:
+        if q_out is None or (dk_out is not None and k_out is None):
+            raise ValueError("dcoords needs the forward's q_out, and with dk_out its k_out")
+        q_at = _on(dev, q_out, "q_out", dtype, dq_out.shape)
+        k_at = None if dk_out is None else _on(dev, k_out, "k_out", dtype, k_shape)
+    g = dict(grads) if grads else {}
+
+    def grad(name, shape, type_):
+        if name in g:
+            return _on(dev, g[name], name, type_, shape)
+        t = g[name] = dq_out.new_empty(shape, dtype=type_)
+        return t.data_ptr()
+
+    dq_at = grad("dq", dq_out.shape, dtype)
+    dk_at = None if dk_out is None else grad("dk", k_shape, dtype)
+    dc_at = grad("dcoords", coords.shape, torch.float32) if want_dcoords else None
+    rc = lib.affmae_rotary_bwd(dq_out_at, dk_out_at, q_at, k_at, coords_at, freq_at, *sizes, code, dq_at, dk_at, dc_at, _stream())
+    if rc != 0:
+        raise AffmaeError("affmae_rotary_bwd", rc)
+    return g
+
+
+def _attn_args(call: str, dev: int, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_xy, k_xy, slope, q_doc, k_doc):
+    """Sizes and addresses that both directions check and pass alike."""
+    if q.dim() != 4 or k.dim() != 4:
+        raise ValueError(f"q must be [B,Nq,H,d] and k [B,Nk,Hk,d], got {tuple(q.shape)} and {tuple(k.shape)}")
+    B, Nq, H, d = q.shape
+    Nk, Hk = k.shape[1], k.shape[2]
+    if max(B, Nq, Nk, H, Hk, d) > _INT_MAX:
+        _beyond_int(call)
+    if (q_xy is None) != (slope is None) or (k_xy is None) != (slope is None):
+        raise ValueError("q_xy, k_xy and slope are given together or not at all")
+    if (q_doc is None) != (k_doc is None):
+        raise ValueError("q_doc and k_doc are given together or not at all")
+    kv = (B, Nk, Hk, d)
+    at = [_on(dev, q, "q", q.dtype), _on(dev, k, "k", q.dtype, kv), _on(dev, v, "v", q.dtype, kv)]
+    at += [None] * 3 if slope is None else [_on(dev, q_xy, "q_xy", torch.float32, (B, Nq, 2)),
+                                            _on(dev, k_xy, "k_xy", torch.float32, (B, Nk, 2)), _on(dev, slope, "slope", torch.float32, (H,))]
+    at += [None] * 2 if q_doc is None else [_on(dev, q_doc, "q_doc", torch.int32, (B, Nq)), _on(dev, k_doc, "k_doc", torch.int32, (B, Nk))]
+    return (B, Nq, Nk, H, Hk, d), at
+
+
+def affmae_attn_fwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, scale: float, cap: float = 0.0,
+                    q_xy: Optional[torch.Tensor] = None, k_xy: Optional[torch.Tensor] = None, slope: Optional[torch.Tensor] = None,
+                    q_doc: Optional[torch.Tensor] = None, k_doc: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                    lse: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None
+                    ) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Attention between all tokens: q [B,Nq,H,d], k and v [B,Nk,Hk,d] -> (out [B,Nq,H,d] in q's dtype, lse [B,Nq,H] fp32).
+
+    Scores are scale <q, k>, bent to cap tanh(. / cap) if cap > 0, less slope[h] |q_xy - k_xy| if slope [H] fp32 is given
+    (q_xy [B,Nq,2], k_xy [B,Nk,2] fp32), and hidden unless q_doc [B,Nq] == k_doc [B,Nk] >= 0 (int32) if these are given."""
+    lib = load_library()
+    code = _dtype_code(q)
+    dev = _current(q)
+    sizes, at = _attn_args("affmae_attn_fwd", dev, q, k, v, q_xy, k_xy, slope, q_doc, k_doc)
+    B, Nq, _, H, _, _ = sizes
+    if out is None:
+        out = torch.empty_like(q)
+        out_at = out.data_ptr()
+    else:
+        out_at = _on(dev, out, "out", q.dtype, q.shape)
+    if lse is None:
+        lse = q.new_empty((B, Nq, H), dtype=torch.float32)
+        lse_at = lse.data_ptr()
+    else:
+        lse_at = _on(dev, lse, "lse", torch.float32, (B, Nq, H))
+    need = lib.affmae_attn_fwd_workspace_bytes(*sizes, code, q_doc is not None)
+    workspace, ws_at, size = _workspace_on(dev, workspace, need, q.device)
+    rc = lib.affmae_attn_fwd(*at, *sizes, float(scale), float(cap), code, out_at, lse_at, ws_at, size, _stream())
+    if rc != 0:
+        raise AffmaeError("affmae_attn_fwd", rc)
+    return out, lse
+
+
+def affmae_attn_bwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor, lse: torch.Tensor, dout: torch.Tensor,
+                    scale: float, cap: float = 0.0, q_xy: Optional[torch.Tensor] = None, k_xy: Optional[torch.Tensor] = None,
+                    slope: Optional[torch.Tensor] = None, q_doc: Optional[torch.Tensor] = None, k_doc: Optional[torch.Tensor] = None,
+                    want_dslope: bool = True, grads: Optional[Dict[str, torch.Tensor]] = None,
+                    workspace: Optional[torch.Tensor] = None) -> Dict[str, torch.Tensor]:
+    """Gradients of affmae_attn_fwd, whose out and lse it takes -> dict(dq, dk, dv[, dslope [H] fp32: with slope])."""
+    lib = load_library()
+    code = _dtype_code(q)
+    dev = _current(q)
+    sizes, at = _attn_args("affmae_attn_bwd", dev, q, k, v, q_xy, k_xy, slope, q_doc, k_doc)
+    B, Nq, _, H, _, _ = sizes
+    at += [_on(dev, out, "out", q.dtype, q.shape), _on(dev, lse, "lse", torch.float32, (B, Nq, H)),
+           _on(dev, dout, "dout", q.dtype, q.shape)]
+    g = dict(grads) if grads else {}
+
+    def grad(name, like, type_):
+        if name in g:
+            return _on(dev, g[name], name, type_, like.shape)
+        t = g[name] = torch.empty_like(like)
+        return t.data_ptr()
+
+    to = [grad("dq", q, q.dtype), grad("dk", k, q.dtype), grad("dv", v, q.dtype)]
+    sloped = slope is not None and want_dslope
+    to.append(grad("dslope", slope, torch.float32) if sloped else None)
+    need = lib.affmae_attn_bwd_workspace_bytes(*sizes, code, q_doc is not None, sloped)
+    workspace, ws_at, size = _workspace_on(dev, workspace, need, q.device)
+    rc = lib.affmae_attn_bwd(*at, *sizes, float(scale), float(cap), code, *to, ws_at, size, _stream())
+    if rc != 0:
+        raise AffmaeError("affmae_attn_bwd", rc)
+    return g
 
 
 def timing_enable(on: bool) -> None:

@@ -1,0 +1,412 @@
+// What the kernels of attention between all tokens share (attn_fwd.hip, attn_bwd.hip).
+//
+// With G = H / Hk query heads to a key head, the Nq G (query, head) pairs that meet the same keys are the rows of one problem, row r =
+// query r / G, head hk G + r % G, so that grouped heads share the keys on the chip and small calls of many heads fill their tiles.
+// A workgroup of four waves keeps 128 rows (or keys) in registers, 32 to a wave, and lets tiles of the other side come through LDS.
+//
+// Products are matrix instructions of 32 x 32.  The side in registers lies along the columns (a lane's column is lane % 32, in both
+// halves), the side in LDS along the rows: a lane then holds 16 scores of one row of the softmax, whose sums need one exchange with
+// the other half, and the scores are at once the second operand of the next product.  For that LDS rows are taken in the order
+// that puts 8 consecutive ones into the lane's first 8 registers: place m of an instruction is row perm(m), bits 2 and 3 swapped.
+#pragma once
+
+#include "launch.h"
+
+#include "cluster_common.h"
+#include "dense_common.h"
+#include "direct_lds.h"
+
+namespace affmae {
+
+typedef __attribute__((ext_vector_type(16))) float f32x16;
+
+constexpr int kAttnThreads = 256;
+constexpr int kAttnRows = 128;  // of a workgroup
+constexpr int kSpan = 64;       // tokens whose images are summed up beforehand
+constexpr float kLog2e = 1.44269504f, kLn2 = 0.693147181f;
+
+// Images of kSpan consecutive tokens: the lowest and highest one, and whether there is padding (id < 0) among them; lo > hi: nothing else.
+struct Span {
+  int lo, hi, pad, unused;
+};
+
+struct AttnParams {
+  const void *q, *k, *v, *out, *dout;
+  const float* lse;
+  const float *q_xy, *k_xy, *slope;
+  const int32_t *q_doc, *k_doc;
+  const Span *q_span, *k_span;  // [B][spans of Nq], [B][spans of Nk], null without images
+  int B, Nq, Nk, H, Hk, G, d, rows;
+  uint32_t g_magic;
+  float scale;   // at least 0: a negative one is taken off the queries
+  bool negate;
+  float cap;
+  // workgroups: `blocks` of rows (or keys), `splits` of the other side, `split_tiles` tiles each
+  int blocks, splits, split_tiles, work;
+  uint32_t blocks_magic;
+  // forward
+  void* o;
+  float* lse_out;
+  float* part;      // [splits][B,Nq,H][d + 1], the last one lse; null: no splits
+  // backward
+  float* rowsum;    // [B,Nq,H] <dout, out>
+  float* rowslope;  // [splits][3][H][B,Nq] parts of dslope, or null
+  float* part_v;    // (part: dq, or dk: [splits][...][d])
+  float grad_scale; // scale, sign and all
+  void *dq, *dk, *dv;
+};
+
+// A tile's rows in LDS, 16-byte pieces.  A piece's place is XORed with bits of its row so that the lanes of a read meet different
+// banks: 16 consecutive rows at the same piece, and (bf16) 64 bytes of each of four consecutive rows.
+template <typename T, int D>
+struct TileRows {
+  static constexpr int E = sizeof(T), RB = D * E, PR = RB / 16;
+  static constexpr int BN = D * E > 256 ? 32 : 64;  // rows of a tile
+  static constexpr int kBytes = BN * RB;
+  static constexpr int kTurns = kBytes / 16 / kAttnThreads;
+  static constexpr int kSteps = PR / 2;  // pairs of pieces of a row: a product's steps over channels
+  static constexpr int kBlocks = BN / 32;
+  static_assert(kTurns * 16 * kAttnThreads == kBytes);
+  static __device__ __forceinline__ int mix(int row) {
+    if constexpr (E == 4) return (RB == 128 ? row >> 1 : row) & (PR - 1) & 31;
+    else if constexpr (RB == 64) return (row >> 2) & 3;
+    else if constexpr (RB == 128) return ((row >> 1) & 1) << 2 | ((row >> 2) & 3);
+    else return (row & 3) << 2 | ((row >> 2) & 3);
+  }
+};
+
+__device__ __forceinline__ int swap23(int m) { return (m & ~12) | (m & 4) << 1 | (m & 8) >> 1; }
+
+// One side's tensor [B,N,heads,d] as the rows of an image and key head.  KEYS: a row is a token; else a (query, head) pair.
+template <typename T, int D, bool KEYS>
+struct Source {
+  using R = TileRows<T, D>;
+  const char* first;  // row 0, channel 0
+  long long bytes;    // from there to the tensor's end
+  uint32_t stride;    // bytes from token to token
+  int rows, G, row_bytes;
+  uint32_t g_magic;
+  const int32_t* doc;  // of the image, or null
+
+  __device__ __forceinline__ Source(const AttnParams& p, const void* tensor, int b, int hk) {
+    const int N = KEYS ? p.Nk : p.Nq, heads = KEYS ? p.Hk : p.H, head = KEYS ? hk : hk * p.G;
+    const long long skip = (((long long)b * N) * heads + head) * p.d * R::E;
+    first = (const char*)tensor + skip;
+    bytes = (long long)p.B * N * heads * p.d * R::E - skip;
+    stride = (uint32_t)heads * p.d * R::E;
+    rows = KEYS ? p.Nk : p.rows;
+    G = KEYS ? 1 : p.G;
+    g_magic = KEYS ? 0u : p.g_magic;
+    row_bytes = p.d * R::E;
+    const int32_t* ids = KEYS ? p.k_doc : p.q_doc;
+    doc = ids ? ids + (long long)b * N : nullptr;
+  }
+  __device__ __forceinline__ int token(int r) const { return KEYS ? r : exact_div(r, G, g_magic); }
+  __device__ __forceinline__ long long offset(int r) const {
+    const int i = token(r);
+    return (long long)i * stride + (KEYS ? 0 : (r - i * G) * row_bytes);
+  }
+  // rows r0 .. r0 + BN - 1 into LDS at `dst`; what is not there, and with `pads` rows of padding, as zeros
+  __device__ __forceinline__ void load(char* dst, int r0, bool pads) const {
+    const int i0 = token(r0);
+    const long long skip = (long long)i0 * stride;
+    const i32x4 rsrc = uniform(buffer_of(first + skip, bytes - skip));
+    const uint32_t at0 = lds_at(dst) + (uint32_t)(__builtin_amdgcn_readfirstlane(threadIdx.x / kWave) * kWave * 16);
+    uint32_t off[R::kTurns];
+#pragma unroll
+    for (int t = 0; t < R::kTurns; ++t) {
+      const int at = t * kAttnThreads + (int)threadIdx.x, row = at / R::PR, piece = (at % R::PR) ^ R::mix(row);
+      const int r = r0 + row, i = token(r);
+      bool there = r < rows && piece * 16 < row_bytes;
+      if (pads && there) there = doc[i] >= 0;
+      off[t] = there ? (uint32_t)(i - i0) * stride + (uint32_t)((KEYS ? 0 : r - i * G) * row_bytes + piece * 16) : kNowhere;
+    }
+#pragma unroll
+    for (int t = 0; t < R::kTurns; ++t) lds_load<16>(at0 + t * kAttnThreads * 16, rsrc, off[t]);
+  }
+};
+
+// 16 bytes of a row: an operand of kSteps steps of a product over channels
+template <typename T>
+struct Piece;
+template <>
+struct Piece<bf16_t> {
+  bf16x8 x;
+  __device__ __forceinline__ void zero() { x = bf16x8{}; }
+  __device__ __forceinline__ void negate() {
+    u32x4 u = __builtin_bit_cast(u32x4, x);
+    u ^= 0x80008000u;
+    x = __builtin_bit_cast(bf16x8, u);
+  }
+  static __device__ __forceinline__ float dot(const Piece& a, const Piece& b) {
+    float s = 0.f;
+    const u32x4 u = __builtin_bit_cast(u32x4, a.x), w = __builtin_bit_cast(u32x4, b.x);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      s = __builtin_fmaf(__uint_as_float(u[e] << 16), __uint_as_float(w[e] << 16), s);
+      s = __builtin_fmaf(__uint_as_float(u[e] & 0xffff0000u), __uint_as_float(w[e] & 0xffff0000u), s);
+    }
+    return s;
+  }
+};
+template <>
+struct Piece<float> {
+  f32x4 x;
+  __device__ __forceinline__ void zero() { x = f32x4{}; }
+  __device__ __forceinline__ void negate() { x = -x; }
+  static __device__ __forceinline__ float dot(const Piece& a, const Piece& b) {
+    float s = 0.f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) s = __builtin_fmaf(a.x[e], b.x[e], s);
+    return s;
+  }
+};
+__device__ __forceinline__ f32x16 multiply(const Piece<bf16_t>& a, const Piece<bf16_t>& b, f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.x, b.x, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16 multiply(const Piece<float>& a, const Piece<float>& b, f32x16 c) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.x[e], b.x[e], c, 0, 0, 0);
+  return c;
+}
+
+// The lane's row of the side in registers: piece 2 s + half of step s.
+template <typename T, int D>
+struct Fixed {
+  using R = TileRows<T, D>;
+  Piece<T> x[R::kSteps];
+  __device__ __forceinline__ void load(const char* row, int half, int row_bytes, bool there) {
+#pragma unroll
+    for (int s = 0; s < R::kSteps; ++s) {
+      x[s].zero();
+      const int at = (2 * s + half) * 16;
+      if (there && at < row_bytes) __builtin_memcpy(&x[s], row + at, 16);
+    }
+  }
+};
+
+// s[m][n] = <row perm(m) of block `block` in LDS, column n's row>
+template <typename T, int D>
+__device__ __forceinline__ f32x16 row_products(const char* tile, int block, const Fixed<T, D>& fixed, int lane) {
+  using R = TileRows<T, D>;
+  const int row = swap23(lane & 31);
+  const char* at = tile + block * 32 * R::RB + row * R::RB;
+  const int m = (R::mix(row) ^ (lane >> 5)) << 4;
+  f32x16 c = {};
+#pragma unroll
+  for (int s = 0; s < R::kSteps; ++s) {
+    Piece<T> a;
+    __builtin_memcpy(&a, at + (m ^ (s << 5)), 16);
+    c = multiply(a, fixed.x[s], c);
+  }
+  return c;
+}
+
+// c[ch][n] += sum over the block's rows of tile[row][ch] w[row][n], with w as row_products leaves it: a lane's registers are the
+// weights of rows 16 (i / 8) + 8 (lane / 32) + i % 8.
+template <int D>
+__device__ __forceinline__ void column_products(const char* tile, int block, const f32x16& w, f32x16 (&c)[D / 32], int lane, bf16_t) {
+  using R = TileRows<bf16_t, D>;
+  const int r = lane & 15, half = lane >> 5;
+  // (bf16 weights: off by at most 2^-8 of each; products are exact and sums 32-bit)
+  Frag8 p[2];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) p[i >> 2].u[i & 3] = pack_bf16x2(w[2 * i], w[2 * i + 1]);
+  const int row = 8 * half + (r >> 2);  // + 4 e + 16 t
+  const char* at = tile + (block * 32 + row) * R::RB + (r & 1) * 8;
+  const int m = (R::mix(row) ^ (2 * ((lane >> 4) & 1) + ((r & 3) >> 1))) << 4;
+#pragma unroll
+  for (int t = 0; t < 2; ++t)
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db) {
+      Frag8 a;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) a.u2[e] = lds_read_tr(at + (16 * t + 4 * e) * R::RB + (m ^ (db << 6) ^ (e << 4)));  // (mix has bit 2 of the row in bit 0)
+      c[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.v, p[t].v, c[db], 0, 0, 0);
+    }
+}
+template <int D>
+__device__ __forceinline__ void column_products(const char* tile, int block, const f32x16& w, f32x16 (&c)[D / 32], int lane, float) {
+  using R = TileRows<float, D>;
+  const int ch = lane & 31, half = lane >> 5;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const int row = 16 * (i >> 3) + 8 * half + (i & 7);
+    const char* at = tile + (block * 32 + row) * R::RB + (ch & 3) * 4;
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db) {
+      const float a = *reinterpret_cast<const float*>(at + (((8 * db + (ch >> 2)) ^ R::mix(row)) << 4));
+      c[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, w[i], c[db], 0, 0, 0);
+    }
+  }
+}
+
+// tanh.  fp32: below 0.55 x times a polynomial of x^2, fitted by least squares to a relative error of 3e-9, beyond it 1 - 2 / (exp(2 x) + 1),
+// of which the 1 is most.  bf16 tensors (EXACT false) take the second form everywhere: its error of 1e-7 of the cap is far below
+// what a rounded query moves the score.
+template <bool EXACT>
+__device__ __forceinline__ float bent(float x) {
+  const float far = 1.f - 2.f * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * (2.f * kLog2e)));
+  if constexpr (!EXACT) return far;
+  const float z = x * x;
+  float s = __builtin_fmaf(z, -0.0062211f, 0.02103814f);
+  s = __builtin_fmaf(z, s, -0.05384533f);
+  s = __builtin_fmaf(z, s, 0.13332534f);
+  s = __builtin_fmaf(z, s, -0.33333316f);
+  return fabsf(x) < 0.55f ? __builtin_fmaf(x * z, s, x) : far;
+}
+
+// Score in units of log 2 from a product s, with the terms that the call has; t: the bent score, which its slope needs.
+template <bool EXACT>
+__device__ __forceinline__ float score(float s, const AttnParams& p, float factor, float dx, float dy, float slope, float& t, float& distance) {
+  float z;
+  if (p.cap > 0.f) {
+    t = bent<EXACT>(s * factor);  // factor = scale / cap
+    z = t * (p.cap * kLog2e);
+  } else {
+    z = s * factor;  // factor = scale log2 e
+  }
+  if (p.slope) {
+    distance = __builtin_amdgcn_sqrtf(__builtin_fmaf(dx, dx, dy * dy));
+    z = __builtin_fmaf(-slope, distance, z);  // slope in units of log 2
+  }
+  return z;
+}
+
+__device__ __forceinline__ float other_half_max(float x) { return fmaxf(x, __uint_as_float(lane_xor_u32<32>(__float_as_uint(x), threadIdx.x & 63))); }
+__device__ __forceinline__ float other_half_sum(float x) { return x + __uint_as_float(lane_xor_u32<32>(__float_as_uint(x), threadIdx.x & 63)); }
+
+// What a workgroup's own rows (or keys) see of the other side's tiles: all of them, or those that hold a token of one of its images.
+struct Walk {
+  const Span* spans;  // of the other side's image
+  int lo, hi;         // own images
+  bool mixed;         // own tokens are not all of one image
+  int end, tile_rows, G;
+  uint32_t g_magic;
+  uint64_t bits;
+  int base;
+
+  // own tokens i0 .. i1
+  __device__ __forceinline__ void own(const Span* s, int i0, int i1) {
+    lo = 0x7fffffff; hi = -1;
+    int pad = 0;
+    for (int t = i0 / kSpan; t <= i1 / kSpan; ++t) {
+      const Span x = s[t];
+      lo = min(lo, x.lo);
+      hi = max(hi, x.hi);
+      pad |= x.pad;
+    }
+    lo = __builtin_amdgcn_readfirstlane(lo);
+    hi = __builtin_amdgcn_readfirstlane(hi);
+    mixed = __builtin_amdgcn_readfirstlane((lo != hi || pad) ? 1 : 0);
+  }
+  // the images of tile t's tokens, rows t tile_rows ... (a tile of 64 rows lies in at most two spans)
+  __device__ __forceinline__ Span of(int t, int rows) const {
+    const int r0 = t * tile_rows, r1 = min(r0 + tile_rows, rows) - 1;
+    const int a = exact_div(r0, G, g_magic) / kSpan, b = exact_div(r1, G, g_magic) / kSpan;
+    Span x = spans[a];
+    if (b != a) {
+      const Span y = spans[b];
+      x.lo = min(x.lo, y.lo);
+      x.hi = max(x.hi, y.hi);
+      x.pad |= y.pad;
+    }
+    return x;
+  }
+  __device__ __forceinline__ void start(int t) {
+    bits = 0;
+    base = t - 64;
+  }
+  // the next tile that matters, after the one that it gave last; `end`: none
+  __device__ __forceinline__ int next(int rows) {
+    while (!bits) {
+      base += 64;
+      if (base >= end) return end;
+      const int t = base + (int)(threadIdx.x & 63);
+      bool hit = t < end;
+      if (hit && spans) {
+        const Span x = of(t, rows);
+        hit = x.lo <= hi && x.hi >= lo;
+      }
+      bits = __ballot(hit);
+    }
+    const int at = __builtin_ctzll(bits);
+    bits &= bits - 1;
+    return base + at;
+  }
+};
+
+// A wave's 32 rows of the image's problem, one to a lane of either half.
+struct Row {
+  int r, i, head;   // clamped to the last one
+  bool there;
+  size_t at;        // (query, head) in [B,Nq,H]
+  float x, y, slope;  // slope in units of log 2
+  int doc;          // -1: padding
+};
+__device__ __forceinline__ Row own_row(const AttnParams& p, int b, int hk, int r0) {
+  Row w;
+  const int r = r0 + (int)(threadIdx.x & 31);
+  w.there = r < p.rows;
+  w.r = min(r, p.rows - 1);
+  w.i = exact_div(w.r, p.G, p.g_magic);
+  w.head = hk * p.G + (w.r - w.i * p.G);
+  const size_t token = (size_t)b * p.Nq + w.i;
+  w.at = token * p.H + w.head;
+  w.x = w.y = w.slope = 0.f;
+  if (p.slope) {
+    const float2 xy = reinterpret_cast<const float2*>(p.q_xy)[token];
+    w.x = xy.x;
+    w.y = xy.y;
+    w.slope = p.slope[w.head] * kLog2e;
+  }
+  w.doc = p.q_doc ? max(p.q_doc[token], -1) : 0;
+  return w;
+}
+
+// Of a tile's keys: places and images (-2: padding, or behind the last key).
+template <int BN>
+struct KeyNotes {
+  float x[BN], y[BN];
+  int doc[BN];
+};
+template <int BN>
+struct KeyNote {
+  float x, y;
+  int doc;
+  __device__ __forceinline__ void fetch(const AttnParams& p, int b, int k0) {
+    const int j = k0 + (int)threadIdx.x;
+    x = y = 0.f;
+    doc = -2;
+    if ((int)threadIdx.x < BN && j < p.Nk) {
+      const size_t token = (size_t)b * p.Nk + j;
+      doc = 0;
+      if (p.k_doc) {
+        doc = p.k_doc[token];
+        if (doc < 0) doc = -2;
+      }
+      if (p.slope && doc >= 0) {  // (padding may have any place, none at all too)
+        const float2 xy = reinterpret_cast<const float2*>(p.k_xy)[token];
+        x = xy.x;
+        y = xy.y;
+      }
+    }
+  }
+  __device__ __forceinline__ void keep(KeyNotes<BN>& n) const {
+    if ((int)threadIdx.x < BN) {
+      n.x[threadIdx.x] = x;
+      n.y[threadIdx.x] = y;
+      n.doc[threadIdx.x] = doc;
+    }
+  }
+};
+
+hipError_t launch_attn_spans(const AttnArgs& a, Span* q_span, Span* k_span, hipStream_t stream);
+
+inline int attn_spans(int N) { return (N + kSpan - 1) / kSpan; }
+inline size_t attn_align(size_t n) { return (n + 255) / 256 * 256; }
+inline size_t attn_span_bytes(int B, int Nq, int Nk) { return attn_align((size_t)B * attn_spans(Nq) * sizeof(Span)) + attn_align((size_t)B * attn_spans(Nk) * sizeof(Span)); }
+
+AttnParams attn_params(const AttnArgs& a, Span* spans);
+
+}  // namespace affmae

@@ -1,0 +1,303 @@
+// Attention between all tokens, forward: per image, head h and query i
+//     z_j = scale <q_i, k_j>,  z_j = cap tanh(z_j / cap),  z_j -= slope_h |x_i - y_j|,  hidden where the images of i and j differ,
+//     out_i = sum_j p_j v_j,  p = softmax(z),  lse_i = log sum_j exp z_j,
+// in one pass over the keys with the running maximum and sum of every row (attn_common.h: the tiles and their layout).
+#include "attn_common.h"
+#include "timing.h"
+
+#include <algorithm>
+
+namespace affmae {
+namespace {
+
+template <typename T, int D, bool TERMS>
+__global__ __launch_bounds__(kAttnThreads, 2) void attn_fwd_kernel(AttnParams p) {
+  using R = TileRows<T, D>;
+  constexpr int BN = R::BN;
+  extern __shared__ __align__(16) char lds[];
+  __shared__ KeyNotes<BN> notes[2];
+  const int work = xcd_contiguous_block(blockIdx.x, gridDim.x);
+  if (work >= p.work) return;
+  const int group = exact_div(work, p.blocks, p.blocks_magic), block = work - group * p.blocks;  // group: (split, image, key head)
+  const int split = group / (p.B * p.Hk), bh = group - split * p.B * p.Hk, b = bh / p.Hk, hk = bh - b * p.Hk;
+  const int lane = threadIdx.x & 63, half = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int block0 = block * kAttnRows, r0 = block0 + wave * 32;
+  const bool busy = r0 < p.rows;
+  const Row own = own_row(p, b, hk, r0);
+  const Source<T, D, true> keys(p, p.k, b, hk), values(p, p.v, b, hk);
+  Fixed<T, D> q;
+  q.load((const char*)p.q + own.at * p.d * R::E, half, p.d * R::E, own.there);
+  if (p.negate) {
+#pragma unroll
+    for (int s = 0; s < R::kSteps; ++s) q.x[s].negate();
+  }
+  const float factor = TERMS && p.cap > 0.f ? p.scale / p.cap : p.scale * kLog2e;
+
+  const int tiles = (p.Nk + BN - 1) / BN;
+  Walk walk;
+  walk.spans = nullptr;
+  walk.mixed = false;
+  walk.end = min(tiles, (split + 1) * p.split_tiles);
+  walk.tile_rows = BN; walk.G = 1; walk.g_magic = 0u;
+  if (p.q_doc) {
+    walk.spans = p.k_span + (size_t)b * ((p.Nk + kSpan - 1) / kSpan);
+    walk.own(p.q_span + (size_t)b * ((p.Nq + kSpan - 1) / kSpan), exact_div(block0, p.G, p.g_magic), exact_div(min(block0 + kAttnRows, p.rows) - 1, p.G, p.g_magic));
+  }
+  walk.start(split * p.split_tiles);
+
+  const auto fetch = [&](int t, int buffer, KeyNote<BN>& note, bool& masked) __attribute__((always_inline)) {
+    char* dst = lds + buffer * 2 * R::kBytes;
+    bool pads = false;
+    masked = t * BN + BN > p.Nk;
+    if (walk.spans) {
+      const Span x = walk.of(t, p.Nk);
+      pads = __builtin_amdgcn_readfirstlane(x.pad);
+      masked = masked || walk.mixed || pads || __builtin_amdgcn_readfirstlane(x.lo) != walk.lo || __builtin_amdgcn_readfirstlane(x.hi) != walk.lo;
+    }
+    keys.load(dst, t * BN, pads);
+    values.load(dst + R::kBytes, t * BN, pads);
+    if (masked || (TERMS && p.slope)) note.fetch(p, b, t * BN);
+  };
+
+  f32x16 o[D / 32] = {};
+  float m = -__builtin_inff(), l = 0.f;
+  KeyNote<BN> note = {};
+  bool masked = false;
+  int t = walk.next(p.Nk);
+  if (t < walk.end) {
+    fetch(t, 0, note, masked);
+    note.keep(notes[0]);
+  }
+  for (int buffer = 0; t < walk.end; buffer ^= 1) {
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    const int following = walk.next(p.Nk);
+    bool next_masked = false;
+    if (following < walk.end) fetch(following, buffer ^ 1, note, next_masked);
+    const char* kt = lds + buffer * 2 * R::kBytes;
+    const char* vt = kt + R::kBytes;
+    if (busy) {
+      f32x16 s[R::kBlocks];
+#pragma unroll
+      for (int kb = 0; kb < R::kBlocks; ++kb) s[kb] = row_products<T, D>(kt, kb, q, lane);
+      const bool plain = !TERMS && !masked;
+      float top;
+      if (plain) {
+        top = s[0][0];
+#pragma unroll
+        for (int kb = 0; kb < R::kBlocks; ++kb)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) top = fmaxf(top, s[kb][i]);
+        top *= factor;
+      } else {
+        top = -__builtin_inff();
+        const KeyNotes<BN>& n = notes[buffer];
+#pragma unroll
+        for (int kb = 0; kb < R::kBlocks; ++kb)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int j = 32 * kb + 16 * (i >> 3) + 8 * half + (i & 7);
+            float bend, distance;
+            float z;
+            if constexpr (TERMS) z = score<sizeof(T) == 4>(s[kb][i], p, factor, own.x - n.x[j], own.y - n.y[j], own.slope, bend, distance);
+            else z = s[kb][i] * factor;
+            if (masked && n.doc[j] != own.doc) z = -__builtin_inff();
+            s[kb][i] = z;
+            top = fmaxf(top, z);
+          }
+      }
+      top = other_half_max(top);
+      if (__any(top > m)) {
+        const float before = m;
+        m = fmaxf(m, top);
+        const float shrink = m == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f(before - m);
+        l *= shrink;
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db) o[db] *= shrink;
+      }
+      const float from = m == -__builtin_inff() ? 0.f : m;
+#pragma unroll
+      for (int kb = 0; kb < R::kBlocks; ++kb) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          s[kb][i] = __builtin_amdgcn_exp2f(plain ? __builtin_fmaf(s[kb][i], factor, -from) : s[kb][i] - from);
+          l += s[kb][i];
+        }
+        column_products<D>(vt, kb, s[kb], o, lane, T{});
+      }
+    }
+    if (following < walk.end) note.keep(notes[buffer ^ 1]);
+    t = following;
+    masked = next_masked;
+  }
+
+  if (!busy) return;
+  l = other_half_sum(l);
+  const float part = l > 0.f ? 1.f / l : (l == l ? 0.f : l);  // (no key: zeros; a NaN stays one)
+  const float lse = l > 0.f ? __builtin_fmaf(m, kLn2, __logf(l)) : (l == l ? -__builtin_inff() : l);
+  if (!own.there) return;
+  if (p.part) {
+    const size_t all = (size_t)p.B * p.Nq * p.H;
+    float* to = p.part + ((size_t)split * all + own.at) * p.d;
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const int ch = 32 * db + 8 * g + 4 * half;
+        if (ch < p.d) {
+          const float v[4] = {o[db][4 * g] * part, o[db][4 * g + 1] * part, o[db][4 * g + 2] * part, o[db][4 * g + 3] * part};
+          store_piece<4>(to + ch, v);
+        }
+      }
+    if (half == 0) p.part[(size_t)p.splits * all * p.d + (size_t)split * all + own.at] = lse;
+    return;
+  }
+  T* to = (T*)p.o + own.at * p.d;
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const int ch = 32 * db + 8 * g + 4 * half;
+      if (ch < p.d) {
+        const float v[4] = {o[db][4 * g] * part, o[db][4 * g + 1] * part, o[db][4 * g + 2] * part, o[db][4 * g + 3] * part};
+        store_piece<4>(to + ch, v);
+      }
+    }
+  if (half == 0) p.lse_out[own.at] = lse;
+}
+
+// out = sum over splits of exp(lse_s - lse) out_s, lse = log sum exp lse_s: a thread for four channels of a (query, head)
+template <typename T>
+__global__ __launch_bounds__(256) void attn_join_kernel(const float* part, int splits, size_t all, int d, T* out, float* lse) {
+  const int quarters = d / 4;
+  const size_t at = (size_t)blockIdx.x * 256 + threadIdx.x;
+  if (at >= all * quarters) return;
+  const size_t row = at / quarters;
+  const int ch = (int)(at - row * quarters) * 4;
+  const float* ls = part + (size_t)splits * all * d + row;
+  float top = -__builtin_inff();
+  for (int s = 0; s < splits; ++s) top = fmaxf(top, ls[s * all]);
+  const float from = top == -__builtin_inff() ? 0.f : top;
+  float sum = 0.f, v[4] = {};
+  for (int s = 0; s < splits; ++s) {
+    const float w = __expf(ls[s * all] - from);
+    float x[4];
+    load_piece<4>(part + (s * all + row) * d + ch, x);
+    sum += w;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = __builtin_fmaf(w, x[e], v[e]);
+  }
+  const float inv = sum > 0.f ? 1.f / sum : (sum == sum ? 0.f : sum);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) v[e] *= inv;
+  store_piece<4>(out + row * d + ch, v);
+  if (ch == 0) lse[row] = sum > 0.f ? from + __logf(sum) : (sum == sum ? -__builtin_inff() : sum);
+}
+
+__global__ __launch_bounds__(256) void attn_spans_kernel(const int32_t* q_doc, const int32_t* k_doc, int Nq, int Nk, int q_spans, int k_spans, int images, Span* to_q, Span* to_k) {
+  const int at = (int)blockIdx.x * 4 + (int)(threadIdx.x / kWave), lane = threadIdx.x & 63;
+  const int of_q = images * q_spans;
+  if (at >= of_q + images * k_spans) return;
+  const bool q = at < of_q;
+  const int n = q ? at : at - of_q, spans = q ? q_spans : k_spans, N = q ? Nq : Nk;
+  const int b = n / spans, i = (n - b * spans) * kSpan + lane;
+  int lo = 0x7fffffff, hi = -1, pad = 0;
+  if (i < N) {
+    const int id = (q ? q_doc : k_doc)[(size_t)b * N + i];
+    if (id < 0) pad = 1;
+    else lo = hi = id;
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    lo = min(lo, __shfl_xor(lo, o));
+    hi = max(hi, __shfl_xor(hi, o));
+  }
+  pad = __any(pad);
+  if (lane == 0) (q ? to_q : to_k)[n] = Span{lo, hi, pad, 0};
+}
+
+// Splits of the keys: where the rows alone do not fill the chip's 256 CUs twice, as many as do, of at least kLeastKeys keys.
+constexpr int kLeastKeys = 256;
+void plan(int B, int Nq, int Nk, int H, int Hk, int D, int el, int& blocks, int& splits, int& split_tiles) {
+  const int BN = D * el > 256 ? 32 : 64;
+  const long long rows = (long long)Nq * (H / Hk);
+  blocks = (int)((rows + kAttnRows - 1) / kAttnRows);
+  const int tiles = (Nk + BN - 1) / BN;
+  const long long groups = (long long)B * Hk * blocks;
+  long long want = std::min<long long>((512 + groups - 1) / groups, std::max(1, Nk / kLeastKeys));
+  split_tiles = (int)((tiles + want - 1) / want);
+  splits = (tiles + split_tiles - 1) / split_tiles;
+}
+int width(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : 128; }
+
+template <typename T, int D, bool TERMS>
+hipError_t launch(const AttnParams& p, hipStream_t stream) {
+  const size_t lds = 4 * TileRows<T, D>::kBytes;
+  const hipError_t e = hipFuncSetAttribute((const void*)attn_fwd_kernel<T, D, TERMS>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+  if (e != hipSuccess) return e;
+  AFFMAE_LAUNCH("attn_fwd_kernel", stream, (attn_fwd_kernel<T, D, TERMS>), dim3((p.work + 7) / 8 * 8), dim3(kAttnThreads), lds, stream, p);
+  if (p.part) {
+    const size_t all = (size_t)p.B * p.Nq * p.H;
+    AFFMAE_LAUNCH("attn_join_kernel", stream, attn_join_kernel<T>, dim3((unsigned)((all * (p.d / 4) + 255) / 256)), dim3(256), 0, stream, p.part, p.splits, all, p.d, (T*)p.o, p.lse_out);
+  }
+  return hipGetLastError();
+}
+template <typename T, bool TERMS>
+hipError_t launch_width(const AttnParams& p, hipStream_t stream) {
+  switch (width(p.d)) {
+    case 32: return launch<T, 32, TERMS>(p, stream);
+    case 64: return launch<T, 64, TERMS>(p, stream);
+    default: return launch<T, 128, TERMS>(p, stream);
+  }
+}
+
+}  // namespace
+
+AttnParams attn_params(const AttnArgs& a, Span* spans) {
+  AttnParams p = {};
+  p.q = a.q; p.k = a.k; p.v = a.v; p.out = a.out; p.dout = a.dout; p.lse = a.lse;
+  p.q_xy = a.q_xy; p.k_xy = a.k_xy; p.slope = a.slope; p.q_doc = a.q_doc; p.k_doc = a.k_doc;
+  if (a.q_doc) {
+    p.q_span = spans;
+    p.k_span = spans + attn_align((size_t)a.B * attn_spans(a.Nq) * sizeof(Span)) / sizeof(Span);
+  }
+  p.B = a.B; p.Nq = a.Nq; p.Nk = a.Nk; p.H = a.H; p.Hk = a.Hk; p.G = a.H / a.Hk; p.d = a.d;
+  p.rows = a.Nq * p.G;
+  p.g_magic = div_magic(p.G);
+  p.negate = a.scale < 0.f;
+  p.scale = p.negate ? -a.scale : a.scale;
+  p.cap = a.cap;
+  return p;
+}
+
+hipError_t launch_attn_spans(const AttnArgs& a, Span* q_span, Span* k_span, hipStream_t stream) {
+  const int qs = attn_spans(a.Nq), ks = attn_spans(a.Nk);
+  AFFMAE_LAUNCH("attn_spans_kernel", stream, attn_spans_kernel, dim3((unsigned)(((long long)a.B * (qs + ks) + 3) / 4)), dim3(256), 0, stream, a.q_doc, a.k_doc, a.Nq, a.Nk, qs, ks, a.B,
+                q_span, k_span);
+  return hipGetLastError();
+}
+
+size_t attn_fwd_workspace_bytes(int B, int Nq, int Nk, int H, int Hk, int d, int dtype, bool docs) {
+  int blocks, splits, split_tiles;
+  plan(B, Nq, Nk, H, Hk, width(d), dtype == 1 ? 2 : 4, blocks, splits, split_tiles);
+  return (docs ? attn_span_bytes(B, Nq, Nk) : 0) + (splits > 1 ? (size_t)splits * B * Nq * H * (d + 1) * sizeof(float) : 0);
+}
+
+hipError_t launch_attn_fwd(const AttnArgs& a, hipStream_t stream) {
+  AttnParams p = attn_params(a, static_cast<Span*>(a.workspace));
+  p.o = a.out;
+  p.lse_out = a.lse;
+  plan(a.B, a.Nq, a.Nk, a.H, a.Hk, width(a.d), a.dtype == 1 ? 2 : 4, p.blocks, p.splits, p.split_tiles);
+  if (p.splits > 1) p.part = reinterpret_cast<float*>(static_cast<char*>(a.workspace) + (a.q_doc ? attn_span_bytes(a.B, a.Nq, a.Nk) : 0));
+  p.blocks_magic = div_magic(p.blocks);
+  p.work = a.B * a.Hk * p.blocks * p.splits;
+  if (a.q_doc) {
+    const hipError_t e = launch_attn_spans(a, const_cast<Span*>(p.q_span), const_cast<Span*>(p.k_span), stream);
+    if (e != hipSuccess) return e;
+  }
+  const bool terms = a.cap > 0.f || a.slope;
+  if (a.dtype == 1) return terms ? launch_width<bf16_t, true>(p, stream) : launch_width<bf16_t, false>(p, stream);
+  return terms ? launch_width<float, true>(p, stream) : launch_width<float, false>(p, stream);
+}
+
+}  // namespace affmae

@@ -244,4 +244,36 @@ struct DropoutArgs {
 };
 hipError_t launch_dropout(const DropoutArgs& a, hipStream_t stream);
 
+// Rotary positions, forward and backward (rotary.hip).
+struct RotaryArgs {
+  const void *q, *k;  // [B,N,H,d], [B,N,Hk,d] or nullptr with Hk = 0: inputs, backward the gradients of the outputs
+  const void *q_out, *k_out;  // backward with dcoords: outputs of the forward pass
+  const float *coords, *freq;  // [B,N,axes], [d/2,axes]
+  int B, N, H, Hk, d, axes, dtype;
+  bool halves, backward;
+  void *to_q, *to_k;
+  float* dcoords;  // [B,N,axes] or nullptr
+};
+hipError_t launch_rotary(const RotaryArgs& a, hipStream_t stream);
+
+// Attention between all tokens, forward (attn_fwd.hip) and backward (attn_bwd.hip).
+struct AttnArgs {
+  const void *q, *k, *v;  // [B,Nq,H,d], [B,Nk,Hk,d] twice
+  const float *q_xy, *k_xy, *slope;  // [B,Nq,2], [B,Nk,2], [H], or all nullptr
+  const int32_t *q_doc, *k_doc;      // [B,Nq], [B,Nk], or both nullptr
+  int B, Nq, Nk, H, Hk, d, dtype;
+  float scale, cap;
+  void* out;   // [B,Nq,H,d], written by the forward pass
+  float* lse;  // [B,Nq,H], written by the forward pass
+  // backward
+  const void* dout;
+  void *dq, *dk, *dv;
+  float* dslope;  // [H] or nullptr
+  void* workspace;
+};
+size_t attn_fwd_workspace_bytes(int B, int Nq, int Nk, int H, int Hk, int d, int dtype, bool docs);
+hipError_t launch_attn_fwd(const AttnArgs& a, hipStream_t stream);
+size_t attn_bwd_workspace_bytes(int B, int Nq, int Nk, int H, int Hk, int d, int dtype, bool docs, bool want_dslope);
+hipError_t launch_attn_bwd(const AttnArgs& a, hipStream_t stream);
+
 }  // namespace affmae

@@ -1,0 +1,85 @@
+"""Pins of the plain implementations of attention between all tokens and of rotary positions: a dense formula written apart, hand
+values, and gradients against central differences."""
+import numpy as np
+import pytest
+
+from oracle import attn as oa
+
+
+def _inputs(B=2, Nq=5, Nk=7, H=4, Hk=2, d=8, seed=0):
+    g = np.random.default_rng(seed)
+    a = {"q": g.normal(size=(B, Nq, H, d)), "k": g.normal(size=(B, Nk, Hk, d)), "v": g.normal(size=(B, Nk, Hk, d))}
+    t = {"q_xy": g.uniform(0, 10, (B, Nq, 2)), "k_xy": g.uniform(0, 10, (B, Nk, 2)), "slope": g.uniform(0.1, 0.5, H),
+         "q_doc": np.array([[0, 0, 1, 2, -1], [3, 3, 3, 9, 3]])[:, :Nq], "k_doc": np.array([[0, 1, 1, 0, -1, 1, 0], [3, 3, 4, 3, -1, 3, 3]])[:, :Nk]}
+    return a, t
+
+
+def test_attention_of_hand_values():
+    q, k, v = np.zeros((1, 1, 1, 8)), np.zeros((1, 2, 1, 8)), np.zeros((1, 2, 1, 8))
+    q[..., 0], k[0, :, 0, 0], v[0, :, 0, 0] = 2.0, [0.0, np.log(3.0)], [1.0, 5.0]
+    r = oa.attn(q, k, v, 0.5)
+    assert np.isclose(r["out"][0][0, 0, 0, 0], 0.25 * 1 + 0.75 * 5) and np.isclose(r["lse"][0][0, 0, 0], np.log(4.0))
+    xy = np.zeros((1, 1, 2)), np.array([[[3.0, 4.0], [0.0, 0.0]]])
+    r = oa.attn(q * 0, k, v, 1.0, q_xy=xy[0], k_xy=xy[1], slope=np.array([np.log(3.0) / 5]))  # 5 away: a third
+    assert np.isclose(r["out"][0][0, 0, 0, 0], 0.25 * 1 + 0.75 * 5)
+    r = oa.attn(q, k, v, 0.5, q_doc=np.array([[4]]), k_doc=np.array([[4, 5]]))
+    assert r["out"][0][0, 0, 0, 0] == 1.0 and r["lse"][0][0, 0, 0] == 0.0
+    for doc in (7, -1):
+        r = oa.attn(q, k, v, 0.5, q_doc=np.array([[doc]]), k_doc=np.array([[4, -1]]))
+        assert (r["out"][0] == 0).all() and r["lse"][0][0, 0, 0] == -np.inf
+
+
+@pytest.mark.parametrize("cap", [0.0, 1.5])
+@pytest.mark.parametrize("distance", [False, True])
+@pytest.mark.parametrize("docs", [False, True])
+def test_attention_gradients_against_differences(cap, distance, docs):
+    a, t = _inputs()
+    terms = {n: t[n] for n in (["q_xy", "k_xy", "slope"] if distance else []) + (["q_doc", "k_doc"] if docs else [])}
+    dout = np.random.default_rng(1).normal(size=a["q"].shape)
+    f = lambda **kw: (oa.attn(**{**a, **terms, **kw}, scale=0.4, cap=cap)["out"][0] * dout).sum()  # noqa: E731
+    r = oa.attn(**a, scale=0.4, cap=cap, dout=dout, **terms)
+    step = 1e-5
+    for name in ("q", "k", "v") + (("slope",) if distance else ()):
+        x = {**a, **terms}[name]
+        for i in list(np.ndindex(x.shape))[::3]:
+            up, down = x.copy(), x.copy()
+            up[i] += step
+            down[i] -= step
+            want = (f(**{name: up}) - f(**{name: down})) / (2 * step)
+            assert abs(r["d" + name][0][i] - want) < 1e-7 * max(1.0, abs(want)), (name, i)
+
+
+def test_attention_of_one_image_is_that_of_the_image_alone():
+    a, t = _inputs()
+    r = oa.attn(**a, scale=0.3, q_doc=t["q_doc"], k_doc=t["k_doc"])
+    qi, ki = np.flatnonzero(t["q_doc"][0] == 0), np.flatnonzero(t["k_doc"][0] == 0)
+    alone = oa.attn(a["q"][:1, qi], a["k"][:1, ki], a["v"][:1, ki], 0.3)
+    assert np.allclose(r["out"][0][0, qi], alone["out"][0][0], rtol=0, atol=1e-14)
+
+
+@pytest.mark.parametrize("layout", ["pairs", "halves"])
+def test_rotary(layout):
+    g = np.random.default_rng(3)
+    x, y = g.normal(size=(1, 4, 2, 6)), g.normal(size=(1, 4, 2, 6))
+    coords, freq = g.uniform(-5, 5, (1, 4, 2)), g.normal(size=(3, 2))
+    r = oa.rotary(x, coords, freq, layout)
+    assert np.allclose(oa.rotary(r, coords, freq, layout, back=True), x, atol=1e-14)
+    # dot products depend on the difference of the places only
+    s = oa.rotary(y, coords[:, ::-1], freq, layout)
+    away = coords + np.array([3.0, -7.0])
+    r2, s2 = oa.rotary(x, away, freq, layout), oa.rotary(y, away[:, ::-1], freq, layout)
+    assert np.allclose((r * s).sum(-1), (r2 * s2).sum(-1), atol=1e-12)
+    # a quarter turn of the first pair
+    first = (0, 1) if layout == "pairs" else (0, 3)
+    q = oa.rotary(np.eye(6)[None, None, :1], np.full((1, 1, 1), 0.5), np.array([[np.pi], [0.0], [0.0]]), layout)
+    assert np.allclose(q[0, 0, 0, list(first)], [0.0, 1.0], atol=1e-15)
+    # places' gradient against differences
+    dout = g.normal(size=x.shape)
+    spin, _ = oa.rotary_spin(r, dout, layout)
+    got = spin @ freq
+    for i in np.ndindex(coords.shape):
+        up, down = coords.copy(), coords.copy()
+        up[i] += 1e-6
+        down[i] -= 1e-6
+        want = ((oa.rotary(x, up, freq, layout) - oa.rotary(x, down, freq, layout)) * dout).sum() / 2e-6
+        assert abs(got[i] - want) < 1e-7
