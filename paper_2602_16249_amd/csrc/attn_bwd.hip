@@ -1,9 +1,13 @@
 // Attention between all tokens, backward.  With p = exp(z - lse) worked out again and g = dout, per image and head (attn_fwd.hip has z):
 //     dP_ij = <g_i, v_j>,  D_i = <g_i, out_i>,  dZ_ij = p_ij (dP_ij - D_i),  dS_ij = dZ_ij (1 - tanh^2),
 //     dq_i = scale sum_j dS_ij k_j,  dk_j = scale sum_i dS_ij q_i,  dv_j = sum_i p_ij g_i,  dslope_h = -sum_ij dZ_ij |x_i - y_j|.
-// Two kernels, one that keeps queries and lets keys come by (dq, D, dslope) and one the other way round (dk, dv): seven products of
-// two of a pair's vectors instead of five, and nothing is added up by atomics: the results are the same in every run, and grouped
-// heads' gradients add up in registers.
+// Two kernels, one that keeps queries and lets keys come by (dq, D, dslope; this file) and one the other way round (dk, dv; attn_bwd_key.hip):
+// seven products of two of a pair's vectors instead of five, and nothing is added up by atomics: the results are the same in every
+// run, and grouped heads' gradients add up in registers.
+//
+// D from the bf16 out is off by what out was rounded by, as much as a hundredth of dZ where few keys share a row's weight (two keys of 64
+// channels: dq and dk off by 0.8 % of their size).  The row's dZ sum to 0 if D is right, so their sum is what D lacks: the key
+// kernel gets it, and dq is put right at the end by as much of sum_j p_ij k_j, one more product.
 #include "attn_common.h"
 #include "timing.h"
 
@@ -12,8 +16,10 @@
 namespace affmae {
 namespace {
 
-template <typename T, int D, bool TERMS>
-__global__ __launch_bounds__(kAttnThreads, 2) void attn_bwd_query_kernel(AttnParams p) {
+int width(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : 128; }
+
+template <typename T, int D, int TERMS, bool REST>
+__global__ __launch_bounds__(kAttnThreads, D == 128 && (REST || sizeof(T) == 4) ? 1 : 2) void attn_bwd_query_kernel(AttnParams p) {
   using R = TileRows<T, D>;
   constexpr int BN = R::BN;
   extern __shared__ __align__(16) char lds[];
@@ -28,9 +34,9 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_bwd_query_kernel(AttnPar
   const bool busy = r0 < p.rows;
   const Row own = own_row(p, b, hk, r0);
   const Source<T, D, true> keys(p, p.k, b, hk), values(p, p.v, b, hk);
-  Fixed<T, D> q, g;
-  q.load((const char*)p.q + own.at * p.d * R::E, half, p.d * R::E, own.there);
-  g.load((const char*)p.dout + own.at * p.d * R::E, half, p.d * R::E, own.there);
+  Fixed<T, D> q[1], g[1];
+  q[0].load((const char*)p.q + own.at * p.d * R::E, half, p.d * R::E, own.there);
+  g[0].load((const char*)p.dout + own.at * p.d * R::E, half, p.d * R::E, own.there);
   float sum = 0.f;  // D
 #pragma unroll
   for (int s = 0; s < R::kSteps; ++s) {
@@ -38,15 +44,14 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_bwd_query_kernel(AttnPar
     Piece<T> o;
     o.zero();
     if (own.there && at < p.d * R::E) __builtin_memcpy(&o, (const char*)p.out + own.at * p.d * R::E + at, 16);
-    sum += Piece<T>::dot(g.x[s], o);
-    if (p.negate) q.x[s].negate();
+    sum += Piece<T>::dot(g[0].x[s], o);
+    if (p.negate) q[0].x[s].negate();
   }
   sum = other_half_sum(sum);
   if (own.there && half == 0 && split == 0) p.rowsum[own.at] = sum;
   const float seen = own.there ? p.lse[own.at] : 0.f;
   const float lse = seen == -__builtin_inff() ? __builtin_inff() : seen * kLog2e;  // (no key: every p is 0)
-  const bool capped = TERMS && p.cap > 0.f;
-  const float factor = capped ? p.scale / p.cap : p.scale * kLog2e;
+  const float factor = TERMS & kCap ? p.scale / p.cap : p.scale * kLog2e, cap = p.cap * kLog2e;
 
   const int tiles = (p.Nk + BN - 1) / BN;
   Walk walk;
@@ -71,10 +76,10 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_bwd_query_kernel(AttnPar
     }
     keys.load(dst, t * BN, pads);
     values.load(dst + R::kBytes, t * BN, pads);
-    if (masked || (TERMS && p.slope)) note.fetch(p, b, t * BN);
+    if (masked || (TERMS & kDistance)) note.fetch(p, b, t * BN);
   };
 
-  f32x16 dq[D / 32] = {};
+  f32x16 dq[D / 32] = {}, keys_seen[REST ? D / 32 : 1] = {};  // sums of dS k, and of what multiplies D in dS
   float by_distance = 0.f, rest = 0.f, distances = 0.f;  // sums of dZ |x - y|, of dZ, of p |x - y|
   KeyNote<BN> note = {};
   bool masked = false;
@@ -94,28 +99,55 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_bwd_query_kernel(AttnPar
       const KeyNotes<BN>& n = notes[buffer];
 #pragma unroll
       for (int kb = 0; kb < R::kBlocks; ++kb) {
-        f32x16 s = row_products<T, D>(kt, kb, q, lane);
-        const f32x16 dp = row_products<T, D>(vt, kb, g, lane);
+        f32x16 s[1], dp[1];
+        row_products<T, D, 1>(kt, kb, q, s, lane);
+        row_products<T, D, 1>(vt, kb, g, dp, lane);
+        const auto slopes = [&](auto near, auto hides) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int j = 32 * kb + 16 * (i >> 3) + 8 * half + (i & 7);
-          if constexpr (TERMS) {
-            float bend = 0.f, distance = 0.f;
-            const float z = score<sizeof(T) == 4>(s[i], p, factor, own.x - n.x[j], own.y - n.y[j], own.slope, bend, distance);
-            float pr = __builtin_amdgcn_exp2f(z - lse), dz = pr * (dp[i] - sum);
-            if (masked && n.doc[j] != own.doc) pr = dz = 0.f;
-            if (p.rowslope) {
+          for (int i = 0; i < 16; ++i) {
+            const int j = 32 * kb + 16 * (i >> 3) + 8 * half + (i & 7);
+            float bend, distance, z;
+            if constexpr (TERMS == 0) z = __builtin_fmaf(s[0][i], factor, -lse);
+            else if constexpr (TERMS & kDistance) z = score<TERMS, near>(s[0][i], factor, cap, own.x - n.x[j], own.y - n.y[j], own.slope, bend, distance) - lse;
+            else z = score<TERMS, near>(s[0][i], factor, cap, 0.f, 0.f, 0.f, bend, distance) - lse;
+            float pr = __builtin_amdgcn_exp2f(z), dz = pr * (dp[0][i] - sum);
+            if constexpr (hides) {
+              const bool off = n.doc[j] != own.doc;
+              pr = off ? 0.f : pr;
+              dz = off ? 0.f : dz;
+            }
+            if constexpr (REST || (TERMS & kDistance)) rest += dz;
+            if constexpr (TERMS & kDistance) {
               by_distance = __builtin_fmaf(dz, distance, by_distance);
               distances = __builtin_fmaf(pr, distance, distances);
-              rest += dz;
             }
-            s[i] = capped ? dz * __builtin_fmaf(-bend, bend, 1.f) : dz;
-          } else {
-            s[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], factor, -lse)) * (dp[i] - sum);
-            if (masked && n.doc[j] != own.doc) s[i] = 0.f;
+            if constexpr (TERMS & kCap) {
+              const float bends = __builtin_fmaf(-bend, bend, 1.f);
+              dz *= bends;
+              if constexpr (REST) pr *= bends;
+            }
+            s[0][i] = dz;
+            dp[0][i] = pr;
           }
+        };
+        using yes = std::true_type;
+        using no = std::false_type;
+        bool near = false;
+        if constexpr (TERMS & kCap) near = all_near(s[0], factor);
+        if (masked) {
+          if (near) slopes(yes{}, yes{});
+          else slopes(no{}, yes{});
+        } else {
+          if (near) slopes(yes{}, no{});
+          else slopes(no{}, no{});
         }
-        column_products<D>(kt, kb, s, dq, lane, T{});
+        const Weights<T> w(s[0]);
+        if constexpr (REST) {
+          const Weights<T> wp(dp[0]);
+          column_products<D, 2>(kt, kb, {&w, &wp}, {dq, keys_seen}, lane);
+        } else {
+          column_products<D, 1>(kt, kb, {&w}, {dq}, lane);
+        }
       }
     }
     if (following < walk.end) note.keep(notes[buffer ^ 1]);
@@ -124,14 +156,15 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_bwd_query_kernel(AttnPar
   }
 
   if (!busy) return;
-  if (TERMS && p.rowslope) {
+  const bool pad = own.doc < 0;
+  rest = other_half_sum(rest);
+  if (REST && own.there && half == 0) p.rowrest[(size_t)split * p.B * p.Nq * p.H + own.at] = pad ? 0.f : rest;
+  if constexpr (TERMS & kDistance) {
     by_distance = other_half_sum(by_distance);
-    rest = other_half_sum(rest);
     distances = other_half_sum(distances);
-    if (own.there && half == 0) {
+    if (p.rowslope && own.there && half == 0) {
       const size_t tokens = (size_t)p.B * p.Nq, plane = (size_t)p.H * tokens;
       float* to = p.rowslope + (size_t)split * 3 * plane + (size_t)own.head * tokens + (size_t)b * p.Nq + own.i;
-      const bool pad = own.doc < 0;
       to[0] = pad ? 0.f : by_distance;
       to[plane] = pad ? 0.f : rest;
       to[2 * plane] = pad ? 0.f : distances;
@@ -144,221 +177,84 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_bwd_query_kernel(AttnPar
     for (int e = 0; e < 4; ++e) {
       const int ch = 32 * db + 8 * e + 4 * half;
       if (ch < p.d) {
-        float v[4];
+        float v[4], u[4];
 #pragma unroll
-        for (int c = 0; c < 4; ++c) v[c] = own.doc < 0 ? 0.f : dq[db][4 * e + c] * p.grad_scale;
-        if (p.part) store_piece<4>(p.part + ((size_t)split * p.B * p.Nq * p.H + own.at) * p.d + ch, v);
-        else store_piece<4>((T*)p.dq + own.at * p.d + ch, v);
-      }
-    }
-}
-
-// Of a tile's rows: lse in units of log 2 (infinity for rows that are not there, see no key or are padding: their p is 0) and <dout,
-// out>; place, slope and image.
-template <int BN>
-struct RowNotes {
-  float lse[BN], sum[BN], x[BN], y[BN], slope[BN];
-  int doc[BN];
-};
-template <int BN>
-struct RowNote {
-  float lse, sum, x, y, slope;
-  int doc;
-  __device__ __forceinline__ void fetch(const AttnParams& p, int b, int hk, int r0) {
-    const int r = r0 + (int)threadIdx.x;
-    lse = __builtin_inff();
-    sum = x = y = slope = 0.f;
-    doc = -2;
-    if ((int)threadIdx.x < BN && r < p.rows) {
-      const int i = exact_div(r, p.G, p.g_magic), head = hk * p.G + (r - i * p.G);
-      const size_t token = (size_t)b * p.Nq + i, at = token * p.H + head;
-      doc = 0;
-      if (p.q_doc) {
-        doc = p.q_doc[token];
-        if (doc < 0) doc = -2;
-      }
-      if (p.slope && doc >= 0) {
-        const float2 xy = reinterpret_cast<const float2*>(p.q_xy)[token];
-        x = xy.x;
-        y = xy.y;
-        slope = p.slope[head] * kLog2e;
-      }
-      const float seen = p.lse[at];
-      if (doc >= 0 && seen != -__builtin_inff()) {
-        lse = seen * kLog2e;
-        sum = p.rowsum[at];
-      }
-    }
-  }
-  __device__ __forceinline__ void keep(RowNotes<BN>& n, bool terms) const {
-    if ((int)threadIdx.x < BN) {
-      n.lse[threadIdx.x] = lse;
-      n.sum[threadIdx.x] = sum;
-      n.doc[threadIdx.x] = doc;
-      if (terms) {
-        n.x[threadIdx.x] = x;
-        n.y[threadIdx.x] = y;
-        n.slope[threadIdx.x] = slope;
-      }
-    }
-  }
-};
-
-template <typename T, int D, bool TERMS>
-__global__ __launch_bounds__(kAttnThreads, D == 128 || sizeof(T) == 4 ? 1 : 2) void attn_bwd_key_kernel(AttnParams p) {
-  using R = TileRows<T, D>;
-  constexpr int BN = R::BN;
-  extern __shared__ __align__(16) char lds[];
-  __shared__ RowNotes<BN> notes[2];
-  const int work = xcd_contiguous_block(blockIdx.x, gridDim.x);
-  if (work >= p.work) return;
-  const int group = exact_div(work, p.blocks, p.blocks_magic), block = work - group * p.blocks;
-  const int split = group / (p.B * p.Hk), bh = group - split * p.B * p.Hk, b = bh / p.Hk, hk = bh - b * p.Hk;
-  const int lane = threadIdx.x & 63, half = lane >> 5;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  const int block0 = block * kAttnRows, j0 = block0 + wave * 32;
-  const bool busy = j0 < p.Nk;
-  const int j = min(j0 + (lane & 31), p.Nk - 1);
-  const bool there = j0 + (lane & 31) < p.Nk;
-  const size_t token = (size_t)b * p.Nk + j, own_at = token * p.Hk + hk;
-  float own_x = 0.f, own_y = 0.f;
-  if (p.slope) {
-    const float2 xy = reinterpret_cast<const float2*>(p.k_xy)[token];
-    own_x = xy.x;
-    own_y = xy.y;
-  }
-  const int own_doc = p.k_doc ? max(p.k_doc[token], -1) : 0;
-  const Source<T, D, false> queries(p, p.q, b, hk), douts(p, p.dout, b, hk);
-  Fixed<T, D> k, v;
-  k.load((const char*)p.k + own_at * p.d * R::E, half, p.d * R::E, there);
-  v.load((const char*)p.v + own_at * p.d * R::E, half, p.d * R::E, there);
-  if (p.negate) {
-#pragma unroll
-    for (int s = 0; s < R::kSteps; ++s) k.x[s].negate();
-  }
-  const bool capped = TERMS && p.cap > 0.f;
-  const float factor = capped ? p.scale / p.cap : p.scale * kLog2e;
-
-  const int tiles = (p.rows + BN - 1) / BN;
-  Walk walk;
-  walk.spans = nullptr;
-  walk.mixed = false;
-  walk.end = min(tiles, (split + 1) * p.split_tiles);
-  walk.tile_rows = BN; walk.G = p.G; walk.g_magic = p.g_magic;
-  if (p.q_doc) {
-    walk.spans = p.q_span + (size_t)b * ((p.Nq + kSpan - 1) / kSpan);
-    walk.own(p.k_span + (size_t)b * ((p.Nk + kSpan - 1) / kSpan), block0, min(block0 + kAttnRows, p.Nk) - 1);
-  }
-  walk.start(split * p.split_tiles);
-
-  const auto fetch = [&](int t, int buffer, RowNote<BN>& note, bool& masked) __attribute__((always_inline)) {
-    char* dst = lds + buffer * 2 * R::kBytes;
-    bool pads = false;
-    masked = false;
-    if (walk.spans) {
-      const Span x = walk.of(t, p.rows);
-      pads = __builtin_amdgcn_readfirstlane(x.pad);
-      masked = walk.mixed || pads || __builtin_amdgcn_readfirstlane(x.lo) != walk.lo || __builtin_amdgcn_readfirstlane(x.hi) != walk.lo;
-    }
-    queries.load(dst, t * BN, pads);
-    douts.load(dst + R::kBytes, t * BN, pads);
-    note.fetch(p, b, hk, t * BN);
-  };
-
-  f32x16 dk[D / 32] = {}, dv[D / 32] = {};
-  RowNote<BN> note = {};
-  bool masked = false;
-  int t = walk.next(p.rows);
-  if (t < walk.end) {
-    fetch(t, 0, note, masked);
-    note.keep(notes[0], TERMS);
-  }
-  for (int buffer = 0; t < walk.end; buffer ^= 1) {
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    const int following = walk.next(p.rows);
-    bool next_masked = false;
-    if (following < walk.end) fetch(following, buffer ^ 1, note, next_masked);
-    const char* qt = lds + buffer * 2 * R::kBytes;
-    const char* gt = qt + R::kBytes;
-    if (busy) {
-      const RowNotes<BN>& n = notes[buffer];
-#pragma unroll
-      for (int rb = 0; rb < R::kBlocks; ++rb) {
-        f32x16 s = row_products<T, D>(qt, rb, k, lane);
-        f32x16 dp = row_products<T, D>(gt, rb, v, lane);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int r = 32 * rb + 16 * (i >> 3) + 8 * half + (i & 7);
-          float pr, bend = 0.f;
-          if constexpr (TERMS) {
-            float distance;
-            pr = __builtin_amdgcn_exp2f(score<sizeof(T) == 4>(s[i], p, factor, n.x[r] - own_x, n.y[r] - own_y, n.slope[r], bend, distance) - n.lse[r]);
-          } else {
-            pr = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], factor, -n.lse[r]));
-          }
-          float ds = pr * (dp[i] - n.sum[r]);
-          if (capped) ds *= __builtin_fmaf(-bend, bend, 1.f);
-          if (masked && n.doc[r] != own_doc) pr = ds = 0.f;
-          s[i] = pr;
-          dp[i] = ds;
-        }
-        column_products<D>(gt, rb, s, dv, lane, T{});
-        column_products<D>(qt, rb, dp, dk, lane, T{});
-      }
-    }
-    if (following < walk.end) note.keep(notes[buffer ^ 1], TERMS);
-    t = following;
-    masked = next_masked;
-  }
-
-  if (!busy || !there) return;
-#pragma unroll
-  for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int ch = 32 * db + 8 * e + 4 * half;
-      if (ch < p.d) {
-        float a[4], c[4];
-#pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          a[x] = own_doc < 0 ? 0.f : dk[db][4 * e + x] * p.grad_scale;
-          c[x] = own_doc < 0 ? 0.f : dv[db][4 * e + x];
+        for (int c = 0; c < 4; ++c) {
+          v[c] = pad ? 0.f : dq[db][4 * e + c];
+          u[c] = !REST || pad ? 0.f : keys_seen[REST ? db : 0][4 * e + c];
         }
         if (p.part) {
-          const size_t to = ((size_t)split * p.B * p.Nk * p.Hk + own_at) * p.d + ch;
-          store_piece<4>(p.part + to, a);
-          store_piece<4>(p.part_v + to, c);
+          const size_t to = ((size_t)split * p.B * p.Nq * p.H + own.at) * p.d + ch;
+          store_piece<4>(p.part + to, v);
+          if (REST) store_piece<4>(p.part_v + to, u);
         } else {
-          store_piece<4>((T*)p.dk + own_at * p.d + ch, a);
-          store_piece<4>((T*)p.dv + own_at * p.d + ch, c);
+#pragma unroll
+          for (int c = 0; c < 4; ++c) v[c] = __builtin_fmaf(-rest, u[c], v[c]) * p.grad_scale;
+          store_piece<4>((T*)p.dq + own.at * p.d + ch, v);
         }
       }
     }
 }
 
-// Parts of splits added up, in their order: of dq, dk and dv, a blockIdx.y each
+template <typename T, int D, int TERMS, bool REST>
+hipError_t launch(const AttnParams& p, hipStream_t stream) {
+  const size_t lds = 4 * TileRows<T, D>::kBytes;
+  const hipError_t e = hipFuncSetAttribute((const void*)attn_bwd_query_kernel<T, D, TERMS, REST>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+  if (e != hipSuccess) return e;
+  AFFMAE_LAUNCH("attn_bwd_query_kernel", stream, (attn_bwd_query_kernel<T, D, TERMS, REST>), dim3((p.work + 7) / 8 * 8), dim3(kAttnThreads), lds, stream, p);
+  return hipGetLastError();
+}
+template <typename T, int TERMS>
+hipError_t launch_width(const AttnParams& p, hipStream_t stream) {
+  constexpr bool kBf16 = sizeof(T) == 2;
+  switch (width(p.d)) {
+    case 32: return launch<T, 32, TERMS, kBf16>(p, stream);
+    case 64: return launch<T, 64, TERMS, kBf16>(p, stream);
+    default:
+      if constexpr (kBf16 && !(TERMS & kDistance))
+        if (!p.rowrest) return launch<T, 128, TERMS, false>(p, stream);
+      return launch<T, 128, TERMS, kBf16>(p, stream);
+  }
+}
+template <typename T>
+hipError_t launch_query(const AttnParams& p, hipStream_t stream) {
+  if (p.cap > 0.f) return p.slope ? launch_width<T, kCap | kDistance>(p, stream) : launch_width<T, kCap>(p, stream);
+  return p.slope ? launch_width<T, kDistance>(p, stream) : launch_width<T, 0>(p, stream);
+}
+
+// Parts of splits added up, in their order: of dq, dk and dv, a blockIdx.y each.  With `rest`, whose sum is what D lacks in a row of d
+// values, as much of `seen` is taken off, and the whole times `scale`.
+struct Join {
+  const float *part, *seen, *rest;
+  void* out;
+  int splits, d;
+  size_t n;  // values, a multiple of 4
+  float scale;
+};
 struct Joins {
-  const float* part[3];
-  void* out[3];
-  int splits[3];
-  size_t n[3];  // values, a multiple of 4
+  Join of[3];
 };
 template <typename T>
-__global__ __launch_bounds__(256) void attn_bwd_join_kernel(Joins j) {
-  const int w = blockIdx.y;
-  const float* part = w == 0 ? j.part[0] : w == 1 ? j.part[1] : j.part[2];
-  T* out = (T*)(w == 0 ? j.out[0] : w == 1 ? j.out[1] : j.out[2]);
-  const int splits = w == 0 ? j.splits[0] : w == 1 ? j.splits[1] : j.splits[2];
-  const size_t n = w == 0 ? j.n[0] : w == 1 ? j.n[1] : j.n[2];
-  for (size_t at = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4; at < n; at += (size_t)gridDim.x * 1024) {
-    float v[4] = {};
-    for (int s = 0; s < splits; ++s) {
+__global__ __launch_bounds__(256) void attn_bwd_join_kernel(Joins all) {
+  const Join j = blockIdx.y == 0 ? all.of[0] : blockIdx.y == 1 ? all.of[1] : all.of[2];
+  for (size_t at = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4; at < j.n; at += (size_t)gridDim.x * 1024) {
+    float v[4] = {}, u[4] = {}, rest = 0.f;
+    const size_t rows = j.n / j.d, row = at / j.d;
+    for (int s = 0; s < j.splits; ++s) {
       float x[4];
-      load_piece<4>(part + s * n + at, x);
+      load_piece<4>(j.part + s * j.n + at, x);
 #pragma unroll
       for (int e = 0; e < 4; ++e) v[e] += x[e];
+      if (j.rest) {
+        load_piece<4>(j.seen + s * j.n + at, x);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) u[e] += x[e];
+        rest += j.rest[s * rows + row];
+      }
     }
-    store_piece<4>(out + at, v);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = __builtin_fmaf(-rest, u[e], v[e]) * j.scale;
+    store_piece<4>((T*)j.out + at, v);
   }
 }
 
@@ -405,13 +301,16 @@ Side side(long long own, long long other, long long groups, int D, int el) {
   s.splits = (tiles + s.split_tiles - 1) / s.split_tiles;
   return s;
 }
-int width(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : 128; }
-
 struct Layout {
   Side query, key;
-  size_t spans, rowsum, rowslope, part_q, part_k, part_v, total;  // places in the workspace
+  size_t spans, rowsum, rowrest, rowslope, part_q, seen_q, part_k, part_v, total;  // places in the workspace
+  bool rest;
 };
-Layout layout(int B, int Nq, int Nk, int H, int Hk, int d, int dtype, bool docs, bool want_dslope) {
+// Whether D is put right (attn_bwd.hip's head).  In heads of 32 and 64 channels the product that this takes is hidden behind the
+// exponentials; in wider ones it is not, and long rows without a term that makes them narrow go without.
+constexpr int kLongRow = 1024;
+bool puts_right(int Nk, int d, int dtype, bool docs, bool distance) { return dtype == 1 && (d <= 64 || Nk < kLongRow || docs || distance); }
+Layout layout(int B, int Nq, int Nk, int H, int Hk, int d, int dtype, bool docs, bool want_dslope, bool distance) {
   Layout l;
   const int D = width(d), el = dtype == 1 ? 2 : 4;
   const long long rows = (long long)Nq * (H / Hk);
@@ -425,47 +324,32 @@ Layout layout(int B, int Nq, int Nk, int H, int Hk, int d, int dtype, bool docs,
   };
   const size_t nq = (size_t)B * Nq * H, nk = (size_t)B * Nk * Hk;
   l.spans = take(docs ? attn_span_bytes(B, Nq, Nk) : 0);
+  l.rest = puts_right(Nk, d, dtype, docs, distance);
   l.rowsum = take(nq * 4);
+  l.rowrest = take(l.rest ? (size_t)l.query.splits * nq * 4 : 0);
   l.rowslope = take(want_dslope ? (size_t)l.query.splits * 3 * nq * 4 : 0);
   l.part_q = take(l.query.splits > 1 ? (size_t)l.query.splits * nq * d * 4 : 0);
+  l.seen_q = take(l.query.splits > 1 && l.rest ? (size_t)l.query.splits * nq * d * 4 : 0);
   l.part_k = take(l.key.splits > 1 ? (size_t)l.key.splits * nk * d * 4 : 0);
   l.part_v = take(l.key.splits > 1 ? (size_t)l.key.splits * nk * d * 4 : 0);
   l.total = off;
   return l;
 }
 
-template <typename T, int D, bool TERMS>
-hipError_t launch(const AttnParams& pq, const AttnParams& pk, hipStream_t stream) {
-  const size_t lds = 4 * TileRows<T, D>::kBytes;
-  hipError_t e = hipFuncSetAttribute((const void*)attn_bwd_query_kernel<T, D, TERMS>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-  if (e != hipSuccess) return e;
-  e = hipFuncSetAttribute((const void*)attn_bwd_key_kernel<T, D, TERMS>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-  if (e != hipSuccess) return e;
-  AFFMAE_LAUNCH("attn_bwd_query_kernel", stream, (attn_bwd_query_kernel<T, D, TERMS>), dim3((pq.work + 7) / 8 * 8), dim3(kAttnThreads), lds, stream, pq);
-  AFFMAE_LAUNCH("attn_bwd_key_kernel", stream, (attn_bwd_key_kernel<T, D, TERMS>), dim3((pk.work + 7) / 8 * 8), dim3(kAttnThreads), lds, stream, pk);
-  return hipGetLastError();
-}
-template <typename T, bool TERMS>
-hipError_t launch_width(const AttnParams& pq, const AttnParams& pk, hipStream_t stream) {
-  switch (width(pq.d)) {
-    case 32: return launch<T, 32, TERMS>(pq, pk, stream);
-    case 64: return launch<T, 64, TERMS>(pq, pk, stream);
-    default: return launch<T, 128, TERMS>(pq, pk, stream);
-  }
-}
-
 }  // namespace
 
 size_t attn_bwd_workspace_bytes(int B, int Nq, int Nk, int H, int Hk, int d, int dtype, bool docs, bool want_dslope) {
-  return layout(B, Nq, Nk, H, Hk, d, dtype, docs, want_dslope).total;
+  return layout(B, Nq, Nk, H, Hk, d, dtype, docs, want_dslope, true).total;  // (a few values more than a call without distances takes)
 }
 
 hipError_t launch_attn_bwd(const AttnArgs& a, hipStream_t stream) {
-  const Layout l = layout(a.B, a.Nq, a.Nk, a.H, a.Hk, a.d, a.dtype, a.q_doc != nullptr, a.dslope != nullptr);
+  const Layout l = layout(a.B, a.Nq, a.Nk, a.H, a.Hk, a.d, a.dtype, a.q_doc != nullptr, a.dslope != nullptr, a.slope != nullptr);
   char* ws = static_cast<char*>(a.workspace);
   AttnParams p = attn_params(a, reinterpret_cast<Span*>(ws + l.spans));
   p.rowsum = reinterpret_cast<float*>(ws + l.rowsum);
   p.rowslope = a.dslope ? reinterpret_cast<float*>(ws + l.rowslope) : nullptr;
+  p.rowrest = l.rest ? reinterpret_cast<float*>(ws + l.rowrest) : nullptr;
+  p.row_splits = l.query.splits;
   p.grad_scale = a.scale;
   p.dq = a.dq; p.dk = a.dk; p.dv = a.dv;
   AttnParams pq = p, pk = p;
@@ -475,28 +359,29 @@ hipError_t launch_attn_bwd(const AttnArgs& a, hipStream_t stream) {
     x->blocks_magic = div_magic(x->blocks);
     x->work = a.B * a.Hk * x->blocks * x->splits;
   }
-  if (pq.splits > 1) pq.part = reinterpret_cast<float*>(ws + l.part_q);
+  if (pq.splits > 1) pq.part = reinterpret_cast<float*>(ws + l.part_q), pq.part_v = reinterpret_cast<float*>(ws + l.seen_q);
   if (pk.splits > 1) pk.part = reinterpret_cast<float*>(ws + l.part_k), pk.part_v = reinterpret_cast<float*>(ws + l.part_v);
   hipError_t e = hipSuccess;
   if (a.q_doc) e = launch_attn_spans(a, const_cast<Span*>(p.q_span), const_cast<Span*>(p.k_span), stream);
   if (e != hipSuccess) return e;
-  const bool terms = a.cap > 0.f || a.slope;
-  if (a.dtype == 1) e = terms ? launch_width<bf16_t, true>(pq, pk, stream) : launch_width<bf16_t, false>(pq, pk, stream);
-  else e = terms ? launch_width<float, true>(pq, pk, stream) : launch_width<float, false>(pq, pk, stream);
+  e = a.dtype == 1 ? launch_query<bf16_t>(pq, stream) : launch_query<float>(pq, stream);
+  if (e != hipSuccess) return e;
+  e = launch_attn_bwd_key(pk, a.dtype, stream);
   if (e != hipSuccess) return e;
   Joins j = {};
   int parts = 0;
-  const auto join = [&](const float* part, void* out, int splits, size_t n) {
-    j.part[parts] = part; j.out[parts] = out; j.splits[parts] = splits; j.n[parts] = n;
-    ++parts;
+  size_t most = 0;
+  const auto join = [&](const float* part, const float* seen, const float* rest, void* out, int splits, size_t n, float scale) {
+    j.of[parts++] = {part, seen, rest, out, splits, a.d, n, scale};
+    most = std::max(most, n);
   };
-  if (pq.splits > 1) join(pq.part, a.dq, pq.splits, (size_t)a.B * a.Nq * a.H * a.d);
+  const size_t nq = (size_t)a.B * a.Nq * a.H * a.d, nk = (size_t)a.B * a.Nk * a.Hk * a.d;
+  if (pq.splits > 1) join(pq.part, pq.part_v, p.rowrest, a.dq, pq.splits, nq, a.scale);
   if (pk.splits > 1) {
-    join(pk.part, a.dk, pk.splits, (size_t)a.B * a.Nk * a.Hk * a.d);
-    join(pk.part_v, a.dv, pk.splits, (size_t)a.B * a.Nk * a.Hk * a.d);
+    join(pk.part, nullptr, nullptr, a.dk, pk.splits, nk, 1.f);
+    join(pk.part_v, nullptr, nullptr, a.dv, pk.splits, nk, 1.f);
   }
   if (parts) {
-    const size_t most = *std::max_element(j.n, j.n + parts);
     const dim3 grid((unsigned)std::min<size_t>((most / 4 + 255) / 256, 4096), parts);
     if (a.dtype == 1) AFFMAE_LAUNCH("attn_bwd_join_kernel", stream, attn_bwd_join_kernel<bf16_t>, grid, dim3(256), 0, stream, j);
     else AFFMAE_LAUNCH("attn_bwd_join_kernel", stream, attn_bwd_join_kernel<float>, grid, dim3(256), 0, stream, j);

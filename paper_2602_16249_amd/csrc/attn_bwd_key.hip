@@ -1,0 +1,235 @@
+// Attention between all tokens, backward by keys: dk and dv (attn_bwd.hip has the formulas).  A workgroup keeps 128 keys of an image and key
+// head with their values; the rows that may see them, of all the head's queries, come by with their dout, lse and D.
+#include "attn_common.h"
+#include "timing.h"
+
+namespace affmae {
+namespace {
+
+// Of a tile's rows: lse in units of log 2 (infinity for rows that are not there, see no key or are padding: their p is 0) and <dout,
+// out>; place, slope and image.
+template <int BN>
+struct RowNotes {
+  float lse[BN], sum[BN], x[BN], y[BN], slope[BN];
+  int doc[BN];
+};
+template <int BN>
+struct RowNote {
+  float lse, sum, x, y, slope;
+  int doc;
+  __device__ __forceinline__ void fetch(const AttnParams& p, int b, int hk, int r0) {
+    const int r = r0 + (int)threadIdx.x;
+    lse = __builtin_inff();
+    sum = x = y = slope = 0.f;
+    doc = -2;
+    if ((int)threadIdx.x < BN && r < p.rows) {
+      const int i = exact_div(r, p.G, p.g_magic), head = hk * p.G + (r - i * p.G);
+      const size_t token = (size_t)b * p.Nq + i, at = token * p.H + head;
+      doc = 0;
+      if (p.q_doc) {
+        doc = p.q_doc[token];
+        if (doc < 0) doc = -2;
+      }
+      if (p.slope && doc >= 0) {
+        const float2 xy = reinterpret_cast<const float2*>(p.q_xy)[token];
+        x = xy.x;
+        y = xy.y;
+        slope = p.slope[head] * kLog2e;
+      }
+      const float seen = p.lse[at];
+      if (doc >= 0 && seen != -__builtin_inff()) {
+        lse = seen * kLog2e;
+        sum = p.rowsum[at];
+        if (p.rowrest)
+          for (int s = 0; s < p.row_splits; ++s) sum += p.rowrest[(size_t)s * p.B * p.Nq * p.H + at];
+      }
+    }
+  }
+  __device__ __forceinline__ void keep(RowNotes<BN>& n, bool places) const {
+    if ((int)threadIdx.x < BN) {
+      n.lse[threadIdx.x] = lse;
+      n.sum[threadIdx.x] = sum;
+      n.doc[threadIdx.x] = doc;
+      if (places) {
+        n.x[threadIdx.x] = x;
+        n.y[threadIdx.x] = y;
+        n.slope[threadIdx.x] = slope;
+      }
+    }
+  }
+};
+
+template <typename T, int D, int TERMS>
+__global__ __launch_bounds__(kAttnThreads, sizeof(T) == 4 && D > 32 ? 1 : 2) void attn_bwd_key_kernel(AttnParams p) {
+  using R = TileRows<T, D>;
+  constexpr int BN = R::BN;
+  extern __shared__ __align__(16) char lds[];
+  __shared__ RowNotes<BN> notes[2];
+  const int work = xcd_contiguous_block(blockIdx.x, gridDim.x);
+  if (work >= p.work) return;
+  const int group = exact_div(work, p.blocks, p.blocks_magic), block = work - group * p.blocks;
+  const int split = group / (p.B * p.Hk), bh = group - split * p.B * p.Hk, b = bh / p.Hk, hk = bh - b * p.Hk;
+  const int lane = threadIdx.x & 63, half = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int block0 = block * kAttnRows, j0 = block0 + wave * 32;
+  const bool busy = j0 < p.Nk;
+  const int j = min(j0 + (lane & 31), p.Nk - 1);
+  const bool there = j0 + (lane & 31) < p.Nk;
+  const size_t token = (size_t)b * p.Nk + j, own_at = token * p.Hk + hk;
+  float own_x = 0.f, own_y = 0.f;
+  if (p.slope) {
+    const float2 xy = reinterpret_cast<const float2*>(p.k_xy)[token];
+    own_x = xy.x;
+    own_y = xy.y;
+  }
+  const int own_doc = p.k_doc ? max(p.k_doc[token], -1) : 0;
+  const Source<T, D, false> queries(p, p.q, b, hk), douts(p, p.dout, b, hk);
+  Fixed<T, D> k[1], v[1];
+  k[0].load((const char*)p.k + own_at * p.d * R::E, half, p.d * R::E, there);
+  v[0].load((const char*)p.v + own_at * p.d * R::E, half, p.d * R::E, there);
+  if (p.negate) {
+#pragma unroll
+    for (int s = 0; s < R::kSteps; ++s) k[0].x[s].negate();
+  }
+  const float factor = TERMS & kCap ? p.scale / p.cap : p.scale * kLog2e, cap = p.cap * kLog2e;
+
+  const int tiles = (p.rows + BN - 1) / BN;
+  Walk walk;
+  walk.spans = nullptr;
+  walk.mixed = false;
+  walk.end = min(tiles, (split + 1) * p.split_tiles);
+  walk.tile_rows = BN; walk.G = p.G; walk.g_magic = p.g_magic;
+  if (p.q_doc) {
+    walk.spans = p.q_span + (size_t)b * ((p.Nq + kSpan - 1) / kSpan);
+    walk.own(p.k_span + (size_t)b * ((p.Nk + kSpan - 1) / kSpan), block0, min(block0 + kAttnRows, p.Nk) - 1);
+  }
+  walk.start(split * p.split_tiles);
+
+  const auto fetch = [&](int t, int buffer, RowNote<BN>& note, bool& masked) __attribute__((always_inline)) {
+    char* dst = lds + buffer * 2 * R::kBytes;
+    bool pads = false;
+    masked = false;
+    if (walk.spans) {
+      const Span x = walk.of(t, p.rows);
+      pads = __builtin_amdgcn_readfirstlane(x.pad);
+      masked = walk.mixed || pads || __builtin_amdgcn_readfirstlane(x.lo) != walk.lo || __builtin_amdgcn_readfirstlane(x.hi) != walk.lo;
+    }
+    queries.load(dst, t * BN, pads);
+    douts.load(dst + R::kBytes, t * BN, pads);
+    note.fetch(p, b, hk, t * BN);
+  };
+
+  f32x16 dk[D / 32] = {}, dv[D / 32] = {};
+  RowNote<BN> note = {};
+  bool masked = false;
+  int t = walk.next(p.rows);
+  if (t < walk.end) {
+    fetch(t, 0, note, masked);
+    note.keep(notes[0], TERMS & kDistance);
+  }
+  for (int buffer = 0; t < walk.end; buffer ^= 1) {
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    const int following = walk.next(p.rows);
+    bool next_masked = false;
+    if (following < walk.end) fetch(following, buffer ^ 1, note, next_masked);
+    const char* qt = lds + buffer * 2 * R::kBytes;
+    const char* gt = qt + R::kBytes;
+    if (busy) {
+      const RowNotes<BN>& n = notes[buffer];
+#pragma unroll
+      for (int rb = 0; rb < R::kBlocks; ++rb) {
+        f32x16 s[1], dp[1];
+        row_products<T, D, 1>(qt, rb, k, s, lane);
+        row_products<T, D, 1>(gt, rb, v, dp, lane);
+        const auto slopes = [&](auto near, auto hides) __attribute__((always_inline)) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int r = 32 * rb + 16 * (i >> 3) + 8 * half + (i & 7);
+            float bend, distance, z;
+            if constexpr (TERMS == 0) z = __builtin_fmaf(s[0][i], factor, -n.lse[r]);
+            else if constexpr (TERMS & kDistance) z = score<TERMS, near>(s[0][i], factor, cap, n.x[r] - own_x, n.y[r] - own_y, n.slope[r], bend, distance) - n.lse[r];
+            else z = score<TERMS, near>(s[0][i], factor, cap, 0.f, 0.f, 0.f, bend, distance) - n.lse[r];
+            float pr = __builtin_amdgcn_exp2f(z), ds = pr * (dp[0][i] - n.sum[r]);
+            if constexpr (TERMS & kCap) ds *= __builtin_fmaf(-bend, bend, 1.f);
+            if constexpr (hides) {
+              const bool off = n.doc[r] != own_doc;
+              pr = off ? 0.f : pr;
+              ds = off ? 0.f : ds;
+            }
+            s[0][i] = pr;
+            dp[0][i] = ds;
+          }
+        };
+        using yes = std::true_type;
+        using no = std::false_type;
+        bool near = false;
+        if constexpr (TERMS & kCap) near = all_near(s[0], factor);
+        if (masked) {
+          if (near) slopes(yes{}, yes{});
+          else slopes(no{}, yes{});
+        } else {
+          if (near) slopes(yes{}, no{});
+          else slopes(no{}, no{});
+        }
+        const Weights<T> wp(s[0]), ws(dp[0]);
+        column_products<D, 1>(gt, rb, {&wp}, {dv}, lane);
+        column_products<D, 1>(qt, rb, {&ws}, {dk}, lane);
+      }
+    }
+    if (following < walk.end) note.keep(notes[buffer ^ 1], TERMS & kDistance);
+    t = following;
+    masked = next_masked;
+  }
+
+  if (!busy || !there) return;
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int ch = 32 * db + 8 * e + 4 * half;
+      if (ch < p.d) {
+        float a[4], c[4];
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          a[x] = own_doc < 0 ? 0.f : dk[db][4 * e + x] * p.grad_scale;
+          c[x] = own_doc < 0 ? 0.f : dv[db][4 * e + x];
+        }
+        if (p.part) {
+          const size_t to = ((size_t)split * p.B * p.Nk * p.Hk + own_at) * p.d + ch;
+          store_piece<4>(p.part + to, a);
+          store_piece<4>(p.part_v + to, c);
+        } else {
+          store_piece<4>((T*)p.dk + own_at * p.d + ch, a);
+          store_piece<4>((T*)p.dv + own_at * p.d + ch, c);
+        }
+      }
+    }
+}
+
+template <typename T, int D, int TERMS>
+hipError_t launch(const AttnParams& p, hipStream_t stream) {
+  const size_t lds = 4 * TileRows<T, D>::kBytes;
+  const hipError_t e = hipFuncSetAttribute((const void*)attn_bwd_key_kernel<T, D, TERMS>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+  if (e != hipSuccess) return e;
+  AFFMAE_LAUNCH("attn_bwd_key_kernel", stream, (attn_bwd_key_kernel<T, D, TERMS>), dim3((p.work + 7) / 8 * 8), dim3(kAttnThreads), lds, stream, p);
+  return hipGetLastError();
+}
+template <typename T, int TERMS>
+hipError_t launch_width(const AttnParams& p, hipStream_t stream) {
+  if (p.d <= 32) return launch<T, 32, TERMS>(p, stream);
+  if (p.d <= 64) return launch<T, 64, TERMS>(p, stream);
+  return launch<T, 128, TERMS>(p, stream);
+}
+template <typename T>
+hipError_t launch_terms(const AttnParams& p, hipStream_t stream) {
+  if (p.cap > 0.f) return p.slope ? launch_width<T, kCap | kDistance>(p, stream) : launch_width<T, kCap>(p, stream);
+  return p.slope ? launch_width<T, kDistance>(p, stream) : launch_width<T, 0>(p, stream);
+}
+
+}  // namespace
+
+hipError_t launch_attn_bwd_key(const AttnParams& p, int dtype, hipStream_t stream) {
+  return dtype == 1 ? launch_terms<bf16_t>(p, stream) : launch_terms<float>(p, stream);
+}
+
+}  // namespace affmae

@@ -50,8 +50,10 @@ struct AttnParams {
   float* part;      // [splits][B,Nq,H][d + 1], the last one lse; null: no splits
   // backward
   float* rowsum;    // [B,Nq,H] <dout, out>
+  float* rowrest;   // [row_splits][B,Nq,H] what it lacks of D, or null
+  int row_splits;
   float* rowslope;  // [splits][3][H][B,Nq] parts of dslope, or null
-  float* part_v;    // (part: dq, or dk: [splits][...][d])
+  float* part_v;    // (part: dq, or dk: [splits][...][d]; part_v: what D's rest takes from dq, or dv)
   float grad_scale; // scale, sign and all
   void *dq, *dk, *dv;
 };
@@ -185,33 +187,47 @@ struct Fixed {
   }
 };
 
-// s[m][n] = <row perm(m) of block `block` in LDS, column n's row>
-template <typename T, int D>
-__device__ __forceinline__ f32x16 row_products(const char* tile, int block, const Fixed<T, D>& fixed, int lane) {
+// s[n][m] = <row perm(m) of block `block` in LDS, the rows of column block n>
+template <typename T, int D, int NB>
+__device__ __forceinline__ void row_products(const char* tile, int block, const Fixed<T, D> (&fixed)[NB], f32x16 (&s)[NB], int lane) {
   using R = TileRows<T, D>;
   const int row = swap23(lane & 31);
   const char* at = tile + block * 32 * R::RB + row * R::RB;
   const int m = (R::mix(row) ^ (lane >> 5)) << 4;
-  f32x16 c = {};
 #pragma unroll
-  for (int s = 0; s < R::kSteps; ++s) {
+  for (int n = 0; n < NB; ++n) s[n] = f32x16{};
+#pragma unroll
+  for (int step = 0; step < R::kSteps; ++step) {
     Piece<T> a;
-    __builtin_memcpy(&a, at + (m ^ (s << 5)), 16);
-    c = multiply(a, fixed.x[s], c);
+    __builtin_memcpy(&a, at + (m ^ (step << 5)), 16);
+#pragma unroll
+    for (int n = 0; n < NB; ++n) s[n] = multiply(a, fixed[n].x[step], s[n]);
   }
-  return c;
 }
 
-// c[ch][n] += sum over the block's rows of tile[row][ch] w[row][n], with w as row_products leaves it: a lane's registers are the
-// weights of rows 16 (i / 8) + 8 (lane / 32) + i % 8.
-template <int D>
-__device__ __forceinline__ void column_products(const char* tile, int block, const f32x16& w, f32x16 (&c)[D / 32], int lane, bf16_t) {
+// Weights of a block's 32 rows by the lane's column as row_products leaves them (registers i: rows 16 (i / 8) + 8 (lane / 32) + i % 8), as
+// the second operand of a product over those rows.
+template <typename T>
+struct Weights;
+template <>
+struct Weights<bf16_t> {  // (off by at most 2^-8 of each; products of bf16 values are exact and sums 32-bit)
+  Frag8 w[2];
+  __device__ __forceinline__ Weights(const f32x16& x) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i >> 2].u[i & 3] = pack_bf16x2(x[2 * i], x[2 * i + 1]);
+  }
+};
+template <>
+struct Weights<float> {
+  f32x16 w;
+  __device__ __forceinline__ Weights(const f32x16& x) : w(x) {}
+};
+
+// c[j][n][ch] += sum over the block's rows of tile[row][ch] w[j * NB + n][row]: J sets of weights for each of NB column blocks
+template <int D, int M>
+__device__ __forceinline__ void column_products(const char* tile, int block, const Weights<bf16_t>* const (&w)[M], f32x16* const (&c)[M], int lane) {
   using R = TileRows<bf16_t, D>;
   const int r = lane & 15, half = lane >> 5;
-  // (bf16 weights: off by at most 2^-8 of each; products are exact and sums 32-bit)
-  Frag8 p[2];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) p[i >> 2].u[i & 3] = pack_bf16x2(w[2 * i], w[2 * i + 1]);
   const int row = 8 * half + (r >> 2);  // + 4 e + 16 t
   const char* at = tile + (block * 32 + row) * R::RB + (r & 1) * 8;
   const int m = (R::mix(row) ^ (2 * ((lane >> 4) & 1) + ((r & 3) >> 1))) << 4;
@@ -222,11 +238,12 @@ __device__ __forceinline__ void column_products(const char* tile, int block, con
       Frag8 a;
 #pragma unroll
       for (int e = 0; e < 2; ++e) a.u2[e] = lds_read_tr(at + (16 * t + 4 * e) * R::RB + (m ^ (db << 6) ^ (e << 4)));  // (mix has bit 2 of the row in bit 0)
-      c[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.v, p[t].v, c[db], 0, 0, 0);
+#pragma unroll
+      for (int j = 0; j < M; ++j) c[j][db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.v, w[j]->w[t].v, c[j][db], 0, 0, 0);
     }
 }
-template <int D>
-__device__ __forceinline__ void column_products(const char* tile, int block, const f32x16& w, f32x16 (&c)[D / 32], int lane, float) {
+template <int D, int M>
+__device__ __forceinline__ void column_products(const char* tile, int block, const Weights<float>* const (&w)[M], f32x16* const (&c)[M], int lane) {
   using R = TileRows<float, D>;
   const int ch = lane & 31, half = lane >> 5;
 #pragma unroll
@@ -236,39 +253,51 @@ __device__ __forceinline__ void column_products(const char* tile, int block, con
 #pragma unroll
     for (int db = 0; db < D / 32; ++db) {
       const float a = *reinterpret_cast<const float*>(at + (((8 * db + (ch >> 2)) ^ R::mix(row)) << 4));
-      c[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, w[i], c[db], 0, 0, 0);
+#pragma unroll
+      for (int j = 0; j < M; ++j) c[j][db] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, w[j]->w[i], c[j][db], 0, 0, 0);
     }
   }
 }
 
-// tanh.  fp32: below 0.55 x times a polynomial of x^2, fitted by least squares to a relative error of 3e-9, beyond it 1 - 2 / (exp(2 x) + 1),
-// of which the 1 is most.  bf16 tensors (EXACT false) take the second form everywhere: its error of 1e-7 of the cap is far below
-// what a rounded query moves the score.
-template <bool EXACT>
+// Terms of the scores that a kernel is built for.
+enum { kCap = 1, kDistance = 2 };
+constexpr float kNear = 0.55f;
+// tanh: up to kNear x times a polynomial of x^2, fitted by least squares to a relative error of 3e-9, beyond it 1 - 2 / (exp(2 x) + 1), of
+// which the 1 is most there (near 0 it would leave an error of 1e-7, times the cap).  NEAR: no lane of the wave is beyond, as
+// in most calls, whose caps are many times the usual score: six operations instead of twelve, two of them slow.
+template <bool NEAR>
 __device__ __forceinline__ float bent(float x) {
-  const float far = 1.f - 2.f * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * (2.f * kLog2e)));
-  if constexpr (!EXACT) return far;
   const float z = x * x;
   float s = __builtin_fmaf(z, -0.0062211f, 0.02103814f);
   s = __builtin_fmaf(z, s, -0.05384533f);
   s = __builtin_fmaf(z, s, 0.13332534f);
   s = __builtin_fmaf(z, s, -0.33333316f);
-  return fabsf(x) < 0.55f ? __builtin_fmaf(x * z, s, x) : far;
+  s = __builtin_fmaf(x * z, s, x);
+  if constexpr (NEAR) return s;
+  const float far = 1.f - 2.f * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * (2.f * kLog2e)));
+  return fabsf(x) < kNear ? s : far;
 }
-
-// Score in units of log 2 from a product s, with the terms that the call has; t: the bent score, which its slope needs.
-template <bool EXACT>
-__device__ __forceinline__ float score(float s, const AttnParams& p, float factor, float dx, float dy, float slope, float& t, float& distance) {
+// no lane has a product beyond kNear of the cap
+__device__ __forceinline__ bool all_near(const f32x16& s, float factor) {
+  float top = 0.f;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) top = fmaxf(top, fabsf(s[i]));
+  return !__any(!(top * factor < kNear));
+}
+// Score in units of log 2 from a product s.  factor: scale / cap, or without a cap scale log2 e; cap and slope in units of log 2.  bend is
+// tanh, distance |x_i - y_j|.
+template <int TERMS, bool NEAR>
+__device__ __forceinline__ float score(float s, float factor, float cap, float dx, float dy, float slope, float& bend, float& distance) {
   float z;
-  if (p.cap > 0.f) {
-    t = bent<EXACT>(s * factor);  // factor = scale / cap
-    z = t * (p.cap * kLog2e);
+  if constexpr (TERMS & kCap) {
+    bend = bent<NEAR>(s * factor);
+    z = bend * cap;
   } else {
-    z = s * factor;  // factor = scale log2 e
+    z = s * factor;
   }
-  if (p.slope) {
+  if constexpr (TERMS & kDistance) {
     distance = __builtin_amdgcn_sqrtf(__builtin_fmaf(dx, dx, dy * dy));
-    z = __builtin_fmaf(-slope, distance, z);  // slope in units of log 2
+    z = __builtin_fmaf(-slope, distance, z);
   }
   return z;
 }
@@ -408,5 +437,6 @@ inline size_t attn_align(size_t n) { return (n + 255) / 256 * 256; }
 inline size_t attn_span_bytes(int B, int Nq, int Nk) { return attn_align((size_t)B * attn_spans(Nq) * sizeof(Span)) + attn_align((size_t)B * attn_spans(Nk) * sizeof(Span)); }
 
 AttnParams attn_params(const AttnArgs& a, Span* spans);
+hipError_t launch_attn_bwd_key(const AttnParams& p, int dtype, hipStream_t stream);
 
 }  // namespace affmae

@@ -10,7 +10,7 @@
 namespace affmae {
 namespace {
 
-template <typename T, int D, bool TERMS>
+template <typename T, int D, int TERMS, int NB>
 __global__ __launch_bounds__(kAttnThreads, 2) void attn_fwd_kernel(AttnParams p) {
   using R = TileRows<T, D>;
   constexpr int BN = R::BN;
@@ -22,17 +22,22 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_fwd_kernel(AttnParams p)
   const int split = group / (p.B * p.Hk), bh = group - split * p.B * p.Hk, b = bh / p.Hk, hk = bh - b * p.Hk;
   const int lane = threadIdx.x & 63, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  const int block0 = block * kAttnRows, r0 = block0 + wave * 32;
+  constexpr int kRows = kAttnRows * NB;
+  const int block0 = block * kRows, r0 = block0 + wave * 32 * NB;
   const bool busy = r0 < p.rows;
-  const Row own = own_row(p, b, hk, r0);
   const Source<T, D, true> keys(p, p.k, b, hk), values(p, p.v, b, hk);
-  Fixed<T, D> q;
-  q.load((const char*)p.q + own.at * p.d * R::E, half, p.d * R::E, own.there);
-  if (p.negate) {
+  Row own[NB];
+  Fixed<T, D> q[NB];
 #pragma unroll
-    for (int s = 0; s < R::kSteps; ++s) q.x[s].negate();
+  for (int n = 0; n < NB; ++n) {
+    own[n] = own_row(p, b, hk, r0 + 32 * n);
+    q[n].load((const char*)p.q + own[n].at * p.d * R::E, half, p.d * R::E, own[n].there);
+    if (p.negate) {
+#pragma unroll
+      for (int s = 0; s < R::kSteps; ++s) q[n].x[s].negate();
+    }
   }
-  const float factor = TERMS && p.cap > 0.f ? p.scale / p.cap : p.scale * kLog2e;
+  const float factor = TERMS & kCap ? p.scale / p.cap : p.scale * kLog2e, cap = p.cap * kLog2e;
 
   const int tiles = (p.Nk + BN - 1) / BN;
   Walk walk;
@@ -42,7 +47,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_fwd_kernel(AttnParams p)
   walk.tile_rows = BN; walk.G = 1; walk.g_magic = 0u;
   if (p.q_doc) {
     walk.spans = p.k_span + (size_t)b * ((p.Nk + kSpan - 1) / kSpan);
-    walk.own(p.q_span + (size_t)b * ((p.Nq + kSpan - 1) / kSpan), exact_div(block0, p.G, p.g_magic), exact_div(min(block0 + kAttnRows, p.rows) - 1, p.G, p.g_magic));
+    walk.own(p.q_span + (size_t)b * ((p.Nq + kSpan - 1) / kSpan), exact_div(block0, p.G, p.g_magic), exact_div(min(block0 + kRows, p.rows) - 1, p.G, p.g_magic));
   }
   walk.start(split * p.split_tiles);
 
@@ -57,11 +62,13 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_fwd_kernel(AttnParams p)
     }
     keys.load(dst, t * BN, pads);
     values.load(dst + R::kBytes, t * BN, pads);
-    if (masked || (TERMS && p.slope)) note.fetch(p, b, t * BN);
+    if (masked || (TERMS & kDistance)) note.fetch(p, b, t * BN);
   };
 
-  f32x16 o[D / 32] = {};
-  float m = -__builtin_inff(), l = 0.f;
+  f32x16 o[NB][D / 32] = {};
+  float m[NB], l[NB];
+#pragma unroll
+  for (int n = 0; n < NB; ++n) m[n] = -__builtin_inff(), l[n] = 0.f;
   KeyNote<BN> note = {};
   bool masked = false;
   int t = walk.next(p.Nk);
@@ -77,53 +84,79 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_fwd_kernel(AttnParams p)
     const char* kt = lds + buffer * 2 * R::kBytes;
     const char* vt = kt + R::kBytes;
     if (busy) {
-      f32x16 s[R::kBlocks];
+      f32x16 s[R::kBlocks][NB];
 #pragma unroll
-      for (int kb = 0; kb < R::kBlocks; ++kb) s[kb] = row_products<T, D>(kt, kb, q, lane);
+      for (int kb = 0; kb < R::kBlocks; ++kb) row_products<T, D, NB>(kt, kb, q, s[kb], lane);
+      const KeyNotes<BN>& notes_ = notes[buffer];
       const bool plain = !TERMS && !masked;
-      float top;
-      if (plain) {
-        top = s[0][0];
+      const float times = plain ? factor : 1.f;
 #pragma unroll
-        for (int kb = 0; kb < R::kBlocks; ++kb)
+      for (int n = 0; n < NB; ++n) {
+        float top = -__builtin_inff();
+        const auto scores = [&](auto near, auto hides) __attribute__((always_inline)) {
 #pragma unroll
-          for (int i = 0; i < 16; ++i) top = fmaxf(top, s[kb][i]);
-        top *= factor;
-      } else {
-        top = -__builtin_inff();
-        const KeyNotes<BN>& n = notes[buffer];
+          for (int kb = 0; kb < R::kBlocks; ++kb)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              const int j = 32 * kb + 16 * (i >> 3) + 8 * half + (i & 7);
+              float bend, distance, z;
+              if constexpr (TERMS & kDistance) z = score<TERMS, near>(s[kb][n][i], factor, cap, own[n].x - notes_.x[j], own[n].y - notes_.y[j], own[n].slope, bend, distance);
+              else z = score<TERMS, near>(s[kb][n][i], factor, cap, 0.f, 0.f, 0.f, bend, distance);
+              if constexpr (hides) z = notes_.doc[j] != own[n].doc ? -__builtin_inff() : z;
+              s[kb][n][i] = z;
+              top = fmaxf(top, z);
+            }
+        };
+        using yes = std::true_type;
+        using no = std::false_type;
+        if (plain) {
+#pragma unroll
+          for (int kb = 0; kb < R::kBlocks; ++kb)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) top = fmaxf(top, s[kb][n][i]);
+          top *= factor;
+        } else {
+          bool near = false;
+          if constexpr (TERMS & kCap) {
+            near = true;
+#pragma unroll
+            for (int kb = 0; kb < R::kBlocks; ++kb) near = near && all_near(s[kb][n], factor);
+          }
+          if (masked) {
+            if (near) scores(yes{}, yes{});
+            else scores(no{}, yes{});
+          } else {
+            if (near) scores(yes{}, no{});
+            else scores(no{}, no{});
+          }
+        }
+        top = other_half_max(top);
+        if (__any(top > m[n])) {
+          const float before = m[n];
+          m[n] = fmaxf(m[n], top);
+          const float shrink = m[n] == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f(before - m[n]);
+          l[n] *= shrink;
+#pragma unroll
+          for (int db = 0; db < D / 32; ++db) o[n][db] *= shrink;
+        }
+        const float from = m[n] == -__builtin_inff() ? 0.f : m[n];
 #pragma unroll
         for (int kb = 0; kb < R::kBlocks; ++kb)
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
-            const int j = 32 * kb + 16 * (i >> 3) + 8 * half + (i & 7);
-            float bend, distance;
-            float z;
-            if constexpr (TERMS) z = score<sizeof(T) == 4>(s[kb][i], p, factor, own.x - n.x[j], own.y - n.y[j], own.slope, bend, distance);
-            else z = s[kb][i] * factor;
-            if (masked && n.doc[j] != own.doc) z = -__builtin_inff();
-            s[kb][i] = z;
-            top = fmaxf(top, z);
+            s[kb][n][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kb][n][i], times, -from));
+            l[n] += s[kb][n][i];
           }
       }
-      top = other_half_max(top);
-      if (__any(top > m)) {
-        const float before = m;
-        m = fmaxf(m, top);
-        const float shrink = m == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f(before - m);
-        l *= shrink;
-#pragma unroll
-        for (int db = 0; db < D / 32; ++db) o[db] *= shrink;
-      }
-      const float from = m == -__builtin_inff() ? 0.f : m;
 #pragma unroll
       for (int kb = 0; kb < R::kBlocks; ++kb) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          s[kb][i] = __builtin_amdgcn_exp2f(plain ? __builtin_fmaf(s[kb][i], factor, -from) : s[kb][i] - from);
-          l += s[kb][i];
+        if constexpr (NB == 1) {
+          const Weights<T> w(s[kb][0]);
+          column_products<D, 1>(vt, kb, {&w}, {o[0]}, lane);
+        } else {
+          const Weights<T> w0(s[kb][0]), w1(s[kb][1]);
+          column_products<D, 2>(vt, kb, {&w0, &w1}, {o[0], o[1]}, lane);
         }
-        column_products<D>(vt, kb, s[kb], o, lane, T{});
       }
     }
     if (following < walk.end) note.keep(notes[buffer ^ 1]);
@@ -132,38 +165,28 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_fwd_kernel(AttnParams p)
   }
 
   if (!busy) return;
-  l = other_half_sum(l);
-  const float part = l > 0.f ? 1.f / l : (l == l ? 0.f : l);  // (no key: zeros; a NaN stays one)
-  const float lse = l > 0.f ? __builtin_fmaf(m, kLn2, __logf(l)) : (l == l ? -__builtin_inff() : l);
-  if (!own.there) return;
-  if (p.part) {
+#pragma unroll
+  for (int n = 0; n < NB; ++n) {
+    const float sum = other_half_sum(l[n]);
+    const float part = sum > 0.f ? 1.f / sum : (sum == sum ? 0.f : sum);  // (no key: zeros; a NaN stays one)
+    const float lse = sum > 0.f ? __builtin_fmaf(m[n], kLn2, __logf(sum)) : (sum == sum ? -__builtin_inff() : sum);
+    if (!own[n].there) continue;
     const size_t all = (size_t)p.B * p.Nq * p.H;
-    float* to = p.part + ((size_t)split * all + own.at) * p.d;
 #pragma unroll
     for (int db = 0; db < D / 32; ++db)
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
         const int ch = 32 * db + 8 * g + 4 * half;
         if (ch < p.d) {
-          const float v[4] = {o[db][4 * g] * part, o[db][4 * g + 1] * part, o[db][4 * g + 2] * part, o[db][4 * g + 3] * part};
-          store_piece<4>(to + ch, v);
+          float v[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = o[n][db][4 * g + e] * part;
+          if (p.part) store_piece<4>(p.part + ((size_t)split * all + own[n].at) * p.d + ch, v);
+          else store_piece<4>((T*)p.o + own[n].at * p.d + ch, v);
         }
       }
-    if (half == 0) p.part[(size_t)p.splits * all * p.d + (size_t)split * all + own.at] = lse;
-    return;
+    if (half == 0) (p.part ? p.part + (size_t)p.splits * all * p.d + (size_t)split * all : p.lse_out)[own[n].at] = lse;
   }
-  T* to = (T*)p.o + own.at * p.d;
-#pragma unroll
-  for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      const int ch = 32 * db + 8 * g + 4 * half;
-      if (ch < p.d) {
-        const float v[4] = {o[db][4 * g] * part, o[db][4 * g + 1] * part, o[db][4 * g + 2] * part, o[db][4 * g + 3] * part};
-        store_piece<4>(to + ch, v);
-      }
-    }
-  if (half == 0) p.lse_out[own.at] = lse;
 }
 
 // out = sum over splits of exp(lse_s - lse) out_s, lse = log sum exp lse_s: a thread for four channels of a (query, head)
@@ -230,25 +253,30 @@ void plan(int B, int Nq, int Nk, int H, int Hk, int D, int el, int& blocks, int&
 }
 int width(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : 128; }
 
-template <typename T, int D, bool TERMS>
+template <typename T, int D, int TERMS, int NB>
 hipError_t launch(const AttnParams& p, hipStream_t stream) {
   const size_t lds = 4 * TileRows<T, D>::kBytes;
-  const hipError_t e = hipFuncSetAttribute((const void*)attn_fwd_kernel<T, D, TERMS>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+  const hipError_t e = hipFuncSetAttribute((const void*)attn_fwd_kernel<T, D, TERMS, NB>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
   if (e != hipSuccess) return e;
-  AFFMAE_LAUNCH("attn_fwd_kernel", stream, (attn_fwd_kernel<T, D, TERMS>), dim3((p.work + 7) / 8 * 8), dim3(kAttnThreads), lds, stream, p);
+  AFFMAE_LAUNCH("attn_fwd_kernel", stream, (attn_fwd_kernel<T, D, TERMS, NB>), dim3((p.work + 7) / 8 * 8), dim3(kAttnThreads), lds, stream, p);
   if (p.part) {
     const size_t all = (size_t)p.B * p.Nq * p.H;
     AFFMAE_LAUNCH("attn_join_kernel", stream, attn_join_kernel<T>, dim3((unsigned)((all * (p.d / 4) + 255) / 256)), dim3(256), 0, stream, p.part, p.splits, all, p.d, (T*)p.o, p.lse_out);
   }
   return hipGetLastError();
 }
-template <typename T, bool TERMS>
+template <typename T, int TERMS>
 hipError_t launch_width(const AttnParams& p, hipStream_t stream) {
   switch (width(p.d)) {
-    case 32: return launch<T, 32, TERMS>(p, stream);
-    case 64: return launch<T, 64, TERMS>(p, stream);
-    default: return launch<T, 128, TERMS>(p, stream);
+    case 32: return launch<T, 32, TERMS, 1>(p, stream);
+    case 64: return launch<T, 64, TERMS, 1>(p, stream);
+    default: return launch<T, 128, TERMS, 1>(p, stream);
   }
+}
+template <typename T>
+hipError_t launch_terms(const AttnParams& p, hipStream_t stream) {
+  if (p.cap > 0.f) return p.slope ? launch_width<T, kCap | kDistance>(p, stream) : launch_width<T, kCap>(p, stream);
+  return p.slope ? launch_width<T, kDistance>(p, stream) : launch_width<T, 0>(p, stream);
 }
 
 }  // namespace
@@ -295,9 +323,7 @@ hipError_t launch_attn_fwd(const AttnArgs& a, hipStream_t stream) {
     const hipError_t e = launch_attn_spans(a, const_cast<Span*>(p.q_span), const_cast<Span*>(p.k_span), stream);
     if (e != hipSuccess) return e;
   }
-  const bool terms = a.cap > 0.f || a.slope;
-  if (a.dtype == 1) return terms ? launch_width<bf16_t, true>(p, stream) : launch_width<bf16_t, false>(p, stream);
-  return terms ? launch_width<float, true>(p, stream) : launch_width<float, false>(p, stream);
+  return a.dtype == 1 ? launch_terms<bf16_t>(p, stream) : launch_terms<float>(p, stream);
 }
 
 }  // namespace affmae
