@@ -18,19 +18,20 @@ namespace {
 
 int width(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : 128; }
 
-template <typename T, int D, int TERMS, bool REST>
-__global__ __launch_bounds__(kAttnThreads, D == 128 && (REST || sizeof(T) == 4) ? 1 : 2) void attn_bwd_query_kernel(AttnParams p) {
-  using R = TileRows<T, D>;
-  constexpr int BN = R::BN;
+template <typename T, int D, int TERMS, bool REST, bool ALONE>
+__global__ __launch_bounds__(kAttnThreads, (kAttnWaves<T, D>)) void attn_bwd_query_kernel(AttnParams p) {
+  using R = TileRows<T, D, ALONE>;
+  constexpr int BN = R::BN, kTogether = D == 128 ? 1 : 2;  // blocks of a tile that are worked on together
   extern __shared__ __align__(16) char lds[];
-  __shared__ KeyNotes<BN> notes[2];
+  __shared__ KeyNotes<BN> notes[ALONE ? 4 : 2];
   const int work = xcd_contiguous_block(blockIdx.x, gridDim.x);
   if (work >= p.work) return;
   const int group = exact_div(work, p.blocks, p.blocks_magic), block = work - group * p.blocks;
   const int split = group / (p.B * p.Hk), bh = group - split * p.B * p.Hk, b = bh / p.Hk, hk = bh - b * p.Hk;
   const int lane = threadIdx.x & 63, half = lane >> 5;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  const int block0 = block * kAttnRows, r0 = block0 + wave * 32;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), tid = ALONE ? lane : (int)threadIdx.x;
+  constexpr int kRows = ALONE ? 32 : kAttnRows;
+  const int block0 = block * kRows, r0 = ALONE ? block0 : block0 + wave * 32;
   const bool busy = r0 < p.rows;
   const Row own = own_row(p, b, hk, r0);
   const Source<T, D, true> keys(p, p.k, b, hk), values(p, p.v, b, hk);
@@ -48,7 +49,7 @@ __global__ __launch_bounds__(kAttnThreads, D == 128 && (REST || sizeof(T) == 4) 
     if (p.negate) q[0].x[s].negate();
   }
   sum = other_half_sum(sum);
-  if (own.there && half == 0 && split == 0) p.rowsum[own.at] = sum;
+  if (own.there && half == 0 && split == 0 && (!ALONE || wave == 0)) p.rowsum[own.at] = sum;
   const float seen = own.there ? p.lse[own.at] : 0.f;
   const float lse = seen == -__builtin_inff() ? __builtin_inff() : seen * kLog2e;  // (no key: every p is 0)
   const float factor = TERMS & kCap ? p.scale / p.cap : p.scale * kLog2e, cap = p.cap * kLog2e;
@@ -61,12 +62,12 @@ __global__ __launch_bounds__(kAttnThreads, D == 128 && (REST || sizeof(T) == 4) 
   walk.tile_rows = BN; walk.G = 1; walk.g_magic = 0u;
   if (p.q_doc) {
     walk.spans = p.k_span + (size_t)b * ((p.Nk + kSpan - 1) / kSpan);
-    walk.own(p.q_span + (size_t)b * ((p.Nq + kSpan - 1) / kSpan), exact_div(block0, p.G, p.g_magic), exact_div(min(block0 + kAttnRows, p.rows) - 1, p.G, p.g_magic));
+    walk.own(p.q_span + (size_t)b * ((p.Nq + kSpan - 1) / kSpan), exact_div(block0, p.G, p.g_magic), exact_div(min(block0 + kRows, p.rows) - 1, p.G, p.g_magic));
   }
   walk.start(split * p.split_tiles);
 
   const auto fetch = [&](int t, int buffer, KeyNote<BN>& note, bool& masked) __attribute__((always_inline)) {
-    char* dst = lds + buffer * 2 * R::kBytes;
+    char* dst = lds + (ALONE ? wave : buffer) * 2 * R::kBytes;
     bool pads = false;
     masked = t * BN + BN > p.Nk;
     if (walk.spans) {
@@ -74,30 +75,32 @@ __global__ __launch_bounds__(kAttnThreads, D == 128 && (REST || sizeof(T) == 4) 
       pads = __builtin_amdgcn_readfirstlane(x.pad);
       masked = masked || walk.mixed || pads || __builtin_amdgcn_readfirstlane(x.lo) != walk.lo || __builtin_amdgcn_readfirstlane(x.hi) != walk.lo;
     }
-    keys.load(dst, t * BN, pads);
-    values.load(dst + R::kBytes, t * BN, pads);
-    if (masked || (TERMS & kDistance)) note.fetch(p, b, t * BN);
+    keys.template load<ALONE>(dst, t * BN, pads);
+    values.template load<ALONE>(dst + R::kBytes, t * BN, pads);
+    if (masked || (TERMS & kDistance) || (D == 128 && REST)) note.fetch(p, b, t * BN, tid);
   };
 
   f32x16 dq[D / 32] = {}, keys_seen[REST ? D / 32 : 1] = {};  // sums of dS k, and of what multiplies D in dS
   float by_distance = 0.f, rest = 0.f, distances = 0.f;  // sums of dZ |x - y|, of dZ, of p |x - y|
   KeyNote<BN> note = {};
   bool masked = false;
-  int t = walk.next(p.Nk);
+  int t = walk.skip(p.Nk, ALONE ? wave : 0);
   if (t < walk.end) {
     fetch(t, 0, note, masked);
-    note.keep(notes[0]);
+    note.keep(notes[ALONE ? wave : 0], tid);
   }
-  for (int buffer = 0; t < walk.end; buffer ^= 1) {
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    const int following = walk.next(p.Nk);
+  for (int buffer = 0; t < walk.end; buffer ^= ALONE ? 0 : 1) {
+    // the tile has arrived, and (with a barrier) every wave has read what the next one will be written over
+    if constexpr (ALONE) asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    const int following = walk.skip(p.Nk, ALONE ? 3 : 0);
     bool next_masked = false;
-    if (following < walk.end) fetch(following, buffer ^ 1, note, next_masked);
-    const char* kt = lds + buffer * 2 * R::kBytes;
+    if (!ALONE && following < walk.end) fetch(following, buffer ^ 1, note, next_masked);
+    const char* kt = lds + (ALONE ? wave : buffer) * 2 * R::kBytes;
     const char* vt = kt + R::kBytes;
     if (busy) {
-      const KeyNotes<BN>& n = notes[buffer];
-#pragma unroll
+      const KeyNotes<BN>& n = notes[ALONE ? wave : buffer];
+#pragma unroll kTogether
       for (int kb = 0; kb < R::kBlocks; ++kb) {
         f32x16 s[1], dp[1];
         row_products<T, D, 1>(kt, kb, q, s, lane);
@@ -133,8 +136,8 @@ __global__ __launch_bounds__(kAttnThreads, D == 128 && (REST || sizeof(T) == 4) 
         using yes = std::true_type;
         using no = std::false_type;
         bool near = false;
-        if constexpr (TERMS & kCap) near = all_near(s[0], factor);
-        if (masked) {
+        if constexpr ((TERMS & kCap) && D < 128) near = all_near(s[0], factor);
+        if (masked || (D == 128 && REST)) {
           if (near) slopes(yes{}, yes{});
           else slopes(no{}, yes{});
         } else {
@@ -150,19 +153,46 @@ __global__ __launch_bounds__(kAttnThreads, D == 128 && (REST || sizeof(T) == 4) 
         }
       }
     }
-    if (following < walk.end) note.keep(notes[buffer ^ 1]);
+    if (following < walk.end) {
+      if constexpr (ALONE) {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (the tile has been read)
+        fetch(following, buffer, note, next_masked);
+      }
+      note.keep(notes[ALONE ? wave : buffer ^ 1], tid);
+    }
     t = following;
     masked = next_masked;
   }
 
-  if (!busy) return;
-  const bool pad = own.doc < 0;
   rest = other_half_sum(rest);
-  if (REST && own.there && half == 0) p.rowrest[(size_t)split * p.B * p.Nq * p.H + own.at] = pad ? 0.f : rest;
   if constexpr (TERMS & kDistance) {
     by_distance = other_half_sum(by_distance);
     distances = other_half_sum(distances);
-    if (p.rowslope && own.there && half == 0) {
+  }
+  if constexpr (ALONE) {
+    __syncthreads();  // (the last tiles have been read)
+    add_waves<D>(lds, wave, lane, dq);
+    if constexpr (REST) {
+      __syncthreads();
+      add_waves<D>(lds, wave, lane, keys_seen);
+    }
+    if constexpr (REST || (TERMS & kDistance)) {
+      float* at = reinterpret_cast<float*>(lds) + lane;
+      __syncthreads();
+      at[wave * 64] = rest;
+      at[256 + wave * 64] = by_distance;
+      at[512 + wave * 64] = distances;
+      __syncthreads();
+      rest = (at[0] + at[64]) + (at[128] + at[192]);
+      by_distance = (at[256] + at[320]) + (at[384] + at[448]);
+      distances = (at[512] + at[576]) + (at[640] + at[704]);
+    }
+  }
+  if (!busy) return;
+  const bool pad = own.doc < 0, first = half == 0 && (!ALONE || wave == 0);
+  if (REST && own.there && first) p.rowrest[(size_t)split * p.B * p.Nq * p.H + own.at] = pad ? 0.f : rest;
+  if constexpr (TERMS & kDistance) {
+    if (p.rowslope && own.there && first) {
       const size_t tokens = (size_t)p.B * p.Nq, plane = (size_t)p.H * tokens;
       float* to = p.rowslope + (size_t)split * 3 * plane + (size_t)own.head * tokens + (size_t)b * p.Nq + own.i;
       to[0] = pad ? 0.f : by_distance;
@@ -176,7 +206,7 @@ __global__ __launch_bounds__(kAttnThreads, D == 128 && (REST || sizeof(T) == 4) 
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const int ch = 32 * db + 8 * e + 4 * half;
-      if (ch < p.d) {
+      if (ch < p.d && (!ALONE || e == wave)) {
         float v[4], u[4];
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
@@ -196,13 +226,17 @@ __global__ __launch_bounds__(kAttnThreads, D == 128 && (REST || sizeof(T) == 4) 
     }
 }
 
+template <typename T, int D, int TERMS, bool REST, bool ALONE>
+hipError_t launch_kernel(const AttnParams& p, hipStream_t stream) {
+  const size_t lds = (ALONE ? 8 : 4) * TileRows<T, D, ALONE>::kBytes;
+  const hipError_t e = hipFuncSetAttribute((const void*)attn_bwd_query_kernel<T, D, TERMS, REST, ALONE>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+  if (e != hipSuccess) return e;
+  AFFMAE_LAUNCH("attn_bwd_query_kernel", stream, (attn_bwd_query_kernel<T, D, TERMS, REST, ALONE>), dim3((p.work + 7) / 8 * 8), dim3(kAttnThreads), lds, stream, p);
+  return hipGetLastError();
+}
 template <typename T, int D, int TERMS, bool REST>
 hipError_t launch(const AttnParams& p, hipStream_t stream) {
-  const size_t lds = 4 * TileRows<T, D>::kBytes;
-  const hipError_t e = hipFuncSetAttribute((const void*)attn_bwd_query_kernel<T, D, TERMS, REST>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-  if (e != hipSuccess) return e;
-  AFFMAE_LAUNCH("attn_bwd_query_kernel", stream, (attn_bwd_query_kernel<T, D, TERMS, REST>), dim3((p.work + 7) / 8 * 8), dim3(kAttnThreads), lds, stream, p);
-  return hipGetLastError();
+  return p.alone ? launch_kernel<T, D, TERMS, REST, true>(p, stream) : launch_kernel<T, D, TERMS, REST, false>(p, stream);
 }
 template <typename T, int TERMS>
 hipError_t launch_width(const AttnParams& p, hipStream_t stream) {
@@ -285,22 +319,26 @@ __global__ __launch_bounds__(1024) void attn_bwd_slope_kernel(const float* rows,
   }
 }
 
-// Splits of the side that comes by: where the other one alone does not fill the chip, as many as do, of at least kLeast rows.
+// Blocks of 128 or of 32 rows (or keys) and splits of the other side, as in the forward.
 constexpr int kLeast = 256;
 struct Side {
+  bool alone;
   int blocks, splits, split_tiles;
 };
-Side side(long long own, long long other, long long groups, int D, int el) {
-  const int BN = D * el > 256 ? 32 : 64;
+Side side(long long own, long long other, long long heads, int D, int el) {
   Side s;
-  s.blocks = (int)((own + kAttnRows - 1) / kAttnRows);
+  s.alone = (own + kAttnRows - 1) / kAttnRows * heads < 512;
+  const int BN = attn_tile_rows(D, el, s.alone);
+  const int per = s.alone ? 32 : kAttnRows;
+  s.blocks = (int)((own + per - 1) / per);
   const int tiles = (int)((other + BN - 1) / BN);
-  groups *= s.blocks;
-  const long long want = std::min<long long>((512 + groups - 1) / groups, std::max<long long>(1, other / kLeast));
+  const long long groups = heads * s.blocks;
+  const long long want = std::max(1ll, std::min(512 / groups, other / kLeast));
   s.split_tiles = (int)((tiles + want - 1) / want);
   s.splits = (tiles + s.split_tiles - 1) / s.split_tiles;
   return s;
 }
+
 struct Layout {
   Side query, key;
   size_t spans, rowsum, rowrest, rowslope, part_q, seen_q, part_k, part_v, total;  // places in the workspace
@@ -353,8 +391,8 @@ hipError_t launch_attn_bwd(const AttnArgs& a, hipStream_t stream) {
   p.grad_scale = a.scale;
   p.dq = a.dq; p.dk = a.dk; p.dv = a.dv;
   AttnParams pq = p, pk = p;
-  pq.blocks = l.query.blocks; pq.splits = l.query.splits; pq.split_tiles = l.query.split_tiles;
-  pk.blocks = l.key.blocks; pk.splits = l.key.splits; pk.split_tiles = l.key.split_tiles;
+  pq.alone = l.query.alone; pq.blocks = l.query.blocks; pq.splits = l.query.splits; pq.split_tiles = l.query.split_tiles;
+  pk.alone = l.key.alone; pk.blocks = l.key.blocks; pk.splits = l.key.splits; pk.split_tiles = l.key.split_tiles;
   for (AttnParams* x : {&pq, &pk}) {
     x->blocks_magic = div_magic(x->blocks);
     x->work = a.B * a.Hk * x->blocks * x->splits;

@@ -17,12 +17,12 @@ template <int BN>
 struct RowNote {
   float lse, sum, x, y, slope;
   int doc;
-  __device__ __forceinline__ void fetch(const AttnParams& p, int b, int hk, int r0) {
-    const int r = r0 + (int)threadIdx.x;
+  __device__ __forceinline__ void fetch(const AttnParams& p, int b, int hk, int r0, int tid) {
+    const int r = r0 + tid;
     lse = __builtin_inff();
     sum = x = y = slope = 0.f;
     doc = -2;
-    if ((int)threadIdx.x < BN && r < p.rows) {
+    if (tid < BN && r < p.rows) {
       const int i = exact_div(r, p.G, p.g_magic), head = hk * p.G + (r - i * p.G);
       const size_t token = (size_t)b * p.Nq + i, at = token * p.H + head;
       doc = 0;
@@ -45,33 +45,34 @@ struct RowNote {
       }
     }
   }
-  __device__ __forceinline__ void keep(RowNotes<BN>& n, bool places) const {
-    if ((int)threadIdx.x < BN) {
-      n.lse[threadIdx.x] = lse;
-      n.sum[threadIdx.x] = sum;
-      n.doc[threadIdx.x] = doc;
+  __device__ __forceinline__ void keep(RowNotes<BN>& n, int tid, bool places) const {
+    if (tid < BN) {
+      n.lse[tid] = lse;
+      n.sum[tid] = sum;
+      n.doc[tid] = doc;
       if (places) {
-        n.x[threadIdx.x] = x;
-        n.y[threadIdx.x] = y;
-        n.slope[threadIdx.x] = slope;
+        n.x[tid] = x;
+        n.y[tid] = y;
+        n.slope[tid] = slope;
       }
     }
   }
 };
 
-template <typename T, int D, int TERMS>
-__global__ __launch_bounds__(kAttnThreads, sizeof(T) == 4 && D > 32 ? 1 : 2) void attn_bwd_key_kernel(AttnParams p) {
-  using R = TileRows<T, D>;
-  constexpr int BN = R::BN;
+template <typename T, int D, int TERMS, bool DOCS, bool ALONE>
+__global__ __launch_bounds__(kAttnThreads, (sizeof(T) == 4 && D > 32 ? 1 : 2)) void attn_bwd_key_kernel(AttnParams p) {
+  using R = TileRows<T, D, ALONE>;
+  constexpr int BN = R::BN, kTogether = D == 128 ? 1 : 2;  // blocks of a tile that are worked on together
   extern __shared__ __align__(16) char lds[];
-  __shared__ RowNotes<BN> notes[2];
+  __shared__ RowNotes<BN> notes[ALONE ? 4 : 2];
   const int work = xcd_contiguous_block(blockIdx.x, gridDim.x);
   if (work >= p.work) return;
   const int group = exact_div(work, p.blocks, p.blocks_magic), block = work - group * p.blocks;
   const int split = group / (p.B * p.Hk), bh = group - split * p.B * p.Hk, b = bh / p.Hk, hk = bh - b * p.Hk;
   const int lane = threadIdx.x & 63, half = lane >> 5;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  const int block0 = block * kAttnRows, j0 = block0 + wave * 32;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), tid = ALONE ? lane : (int)threadIdx.x;
+  constexpr int kRows = ALONE ? 32 : kAttnRows;
+  const int block0 = block * kRows, j0 = ALONE ? block0 : block0 + wave * 32;
   const bool busy = j0 < p.Nk;
   const int j = min(j0 + (lane & 31), p.Nk - 1);
   const bool there = j0 + (lane & 31) < p.Nk;
@@ -82,7 +83,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) == 4 && D > 32 ? 1 : 2) voi
     own_x = xy.x;
     own_y = xy.y;
   }
-  const int own_doc = p.k_doc ? max(p.k_doc[token], -1) : 0;
+  const int own_doc = DOCS ? max(p.k_doc[token], -1) : 0;
   const Source<T, D, false> queries(p, p.q, b, hk), douts(p, p.dout, b, hk);
   Fixed<T, D> k[1], v[1];
   k[0].load((const char*)p.k + own_at * p.d * R::E, half, p.d * R::E, there);
@@ -99,44 +100,46 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) == 4 && D > 32 ? 1 : 2) voi
   walk.mixed = false;
   walk.end = min(tiles, (split + 1) * p.split_tiles);
   walk.tile_rows = BN; walk.G = p.G; walk.g_magic = p.g_magic;
-  if (p.q_doc) {
+  if constexpr (DOCS) {
     walk.spans = p.q_span + (size_t)b * ((p.Nq + kSpan - 1) / kSpan);
-    walk.own(p.k_span + (size_t)b * ((p.Nk + kSpan - 1) / kSpan), block0, min(block0 + kAttnRows, p.Nk) - 1);
+    walk.own(p.k_span + (size_t)b * ((p.Nk + kSpan - 1) / kSpan), block0, min(block0 + kRows, p.Nk) - 1);
   }
   walk.start(split * p.split_tiles);
 
   const auto fetch = [&](int t, int buffer, RowNote<BN>& note, bool& masked) __attribute__((always_inline)) {
-    char* dst = lds + buffer * 2 * R::kBytes;
+    char* dst = lds + (ALONE ? wave : buffer) * 2 * R::kBytes;
     bool pads = false;
     masked = false;
-    if (walk.spans) {
+    if constexpr (DOCS) {
       const Span x = walk.of(t, p.rows);
       pads = __builtin_amdgcn_readfirstlane(x.pad);
       masked = walk.mixed || pads || __builtin_amdgcn_readfirstlane(x.lo) != walk.lo || __builtin_amdgcn_readfirstlane(x.hi) != walk.lo;
     }
-    queries.load(dst, t * BN, pads);
-    douts.load(dst + R::kBytes, t * BN, pads);
-    note.fetch(p, b, hk, t * BN);
+    queries.template load<ALONE>(dst, t * BN, pads);
+    douts.template load<ALONE>(dst + R::kBytes, t * BN, pads);
+    note.fetch(p, b, hk, t * BN, tid);
   };
 
   f32x16 dk[D / 32] = {}, dv[D / 32] = {};
   RowNote<BN> note = {};
   bool masked = false;
-  int t = walk.next(p.rows);
+  int t = walk.skip(p.rows, ALONE ? wave : 0);
   if (t < walk.end) {
     fetch(t, 0, note, masked);
-    note.keep(notes[0], TERMS & kDistance);
+    note.keep(notes[ALONE ? wave : 0], tid, TERMS & kDistance);
   }
-  for (int buffer = 0; t < walk.end; buffer ^= 1) {
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    const int following = walk.next(p.rows);
+  for (int buffer = 0; t < walk.end; buffer ^= ALONE ? 0 : 1) {
+    // the tile has arrived, and (with a barrier) every wave has read what the next one will be written over
+    if constexpr (ALONE) asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    const int following = walk.skip(p.rows, ALONE ? 3 : 0);
     bool next_masked = false;
-    if (following < walk.end) fetch(following, buffer ^ 1, note, next_masked);
-    const char* qt = lds + buffer * 2 * R::kBytes;
+    if (!ALONE && following < walk.end) fetch(following, buffer ^ 1, note, next_masked);
+    const char* qt = lds + (ALONE ? wave : buffer) * 2 * R::kBytes;
     const char* gt = qt + R::kBytes;
     if (busy) {
-      const RowNotes<BN>& n = notes[buffer];
-#pragma unroll
+      const RowNotes<BN>& n = notes[ALONE ? wave : buffer];
+#pragma unroll kTogether
       for (int rb = 0; rb < R::kBlocks; ++rb) {
         f32x16 s[1], dp[1];
         row_products<T, D, 1>(qt, rb, k, s, lane);
@@ -163,8 +166,8 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) == 4 && D > 32 ? 1 : 2) voi
         using yes = std::true_type;
         using no = std::false_type;
         bool near = false;
-        if constexpr (TERMS & kCap) near = all_near(s[0], factor);
-        if (masked) {
+        if constexpr ((TERMS & kCap) && D < 128) near = all_near(s[0], factor);
+        if (DOCS && (D == 128 || masked)) {  // (one way through where two would not fit the registers)
           if (near) slopes(yes{}, yes{});
           else slopes(no{}, yes{});
         } else {
@@ -176,18 +179,30 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) == 4 && D > 32 ? 1 : 2) voi
         column_products<D, 1>(qt, rb, {&ws}, {dk}, lane);
       }
     }
-    if (following < walk.end) note.keep(notes[buffer ^ 1], TERMS & kDistance);
+    if (following < walk.end) {
+      if constexpr (ALONE) {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (the tile has been read)
+        fetch(following, buffer, note, next_masked);
+      }
+      note.keep(notes[ALONE ? wave : buffer ^ 1], tid, TERMS & kDistance);
+    }
     t = following;
     masked = next_masked;
   }
 
+  if constexpr (ALONE) {
+    __syncthreads();  // (the last tiles have been read)
+    add_waves<D>(lds, wave, lane, dk);
+    __syncthreads();
+    add_waves<D>(lds, wave, lane, dv);
+  }
   if (!busy || !there) return;
 #pragma unroll
   for (int db = 0; db < D / 32; ++db)
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const int ch = 32 * db + 8 * e + 4 * half;
-      if (ch < p.d) {
+      if (ch < p.d && (!ALONE || e == wave)) {
         float a[4], c[4];
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
@@ -206,13 +221,21 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) == 4 && D > 32 ? 1 : 2) voi
     }
 }
 
+template <typename T, int D, int TERMS, bool DOCS, bool ALONE>
+hipError_t launch_kernel(const AttnParams& p, hipStream_t stream) {
+  const size_t lds = (ALONE ? 8 : 4) * TileRows<T, D, ALONE>::kBytes;
+  const hipError_t e = hipFuncSetAttribute((const void*)attn_bwd_key_kernel<T, D, TERMS, DOCS, ALONE>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+  if (e != hipSuccess) return e;
+  AFFMAE_LAUNCH("attn_bwd_key_kernel", stream, (attn_bwd_key_kernel<T, D, TERMS, DOCS, ALONE>), dim3((p.work + 7) / 8 * 8), dim3(kAttnThreads), lds, stream, p);
+  return hipGetLastError();
+}
+template <typename T, int D, int TERMS, bool DOCS>
+hipError_t launch_docs(const AttnParams& p, hipStream_t stream) {
+  return p.alone ? launch_kernel<T, D, TERMS, DOCS, true>(p, stream) : launch_kernel<T, D, TERMS, DOCS, false>(p, stream);
+}
 template <typename T, int D, int TERMS>
 hipError_t launch(const AttnParams& p, hipStream_t stream) {
-  const size_t lds = 4 * TileRows<T, D>::kBytes;
-  const hipError_t e = hipFuncSetAttribute((const void*)attn_bwd_key_kernel<T, D, TERMS>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-  if (e != hipSuccess) return e;
-  AFFMAE_LAUNCH("attn_bwd_key_kernel", stream, (attn_bwd_key_kernel<T, D, TERMS>), dim3((p.work + 7) / 8 * 8), dim3(kAttnThreads), lds, stream, p);
-  return hipGetLastError();
+  return p.q_doc ? launch_docs<T, D, TERMS, true>(p, stream) : launch_docs<T, D, TERMS, false>(p, stream);
 }
 template <typename T, int TERMS>
 hipError_t launch_width(const AttnParams& p, hipStream_t stream) {

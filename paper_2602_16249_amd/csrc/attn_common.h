@@ -2,7 +2,9 @@
 //
 // With G = H / Hk query heads to a key head, the Nq G (query, head) pairs that meet the same keys are the rows of one problem, row r =
 // query r / G, head hk G + r % G, so that grouped heads share the keys on the chip and small calls of many heads fill their tiles.
-// A workgroup of four waves keeps 128 rows (or keys) in registers, 32 to a wave, and lets tiles of the other side come through LDS.
+// A workgroup of four waves keeps 128 rows (or keys) in registers, 32 to a wave, and lets tiles of the other side come through LDS, the
+// next one on its way while one is used.  Where that makes too few workgroups (ALONE), it keeps 32 rows, the same in all four waves; each wave takes
+// every fourth tile, fetched by itself, and the waves' results are joined at the end.
 //
 // Products are matrix instructions of 32 x 32.  The side in registers lies along the columns (a lane's column is lane % 32, in both
 // halves), the side in LDS along the rows: a lane then holds 16 scores of one row of the softmax, whose sums need one exchange with
@@ -43,6 +45,7 @@ struct AttnParams {
   float cap;
   // workgroups: `blocks` of rows (or keys), `splits` of the other side, `split_tiles` tiles each
   int blocks, splits, split_tiles, work;
+  bool alone;
   uint32_t blocks_magic;
   // forward
   void* o;
@@ -60,15 +63,14 @@ struct AttnParams {
 
 // A tile's rows in LDS, 16-byte pieces.  A piece's place is XORed with bits of its row so that the lanes of a read meet different
 // banks: 16 consecutive rows at the same piece, and (bf16) 64 bytes of each of four consecutive rows.
-template <typename T, int D>
+template <typename T, int D, bool ALONE = false>
 struct TileRows {
   static constexpr int E = sizeof(T), RB = D * E, PR = RB / 16;
-  static constexpr int BN = D * E > 256 ? 32 : 64;  // rows of a tile
+  static constexpr int BN = RB > 256 || (ALONE && RB > 128) ? 32 : 64;  // rows of a tile (ALONE has four of each side in a CU's LDS at least twice)
   static constexpr int kBytes = BN * RB;
-  static constexpr int kTurns = kBytes / 16 / kAttnThreads;
   static constexpr int kSteps = PR / 2;  // pairs of pieces of a row: a product's steps over channels
   static constexpr int kBlocks = BN / 32;
-  static_assert(kTurns * 16 * kAttnThreads == kBytes);
+  static_assert(kBytes % (16 * kAttnThreads) == 0);
   static __device__ __forceinline__ int mix(int row) {
     if constexpr (E == 4) return (RB == 128 ? row >> 1 : row) & (PR - 1) & 31;
     else if constexpr (RB == 64) return (row >> 2) & 3;
@@ -76,6 +78,11 @@ struct TileRows {
     else return (row & 3) << 2 | ((row >> 2) & 3);
   }
 };
+
+// Waves that a kernel's registers are to leave room for on a SIMD: two, but where the vectors of a lane's row alone fill them.
+template <typename T, int D>
+constexpr int kAttnWaves = sizeof(T) == 4 && D == 128 ? 1 : 2;
+inline int attn_tile_rows(int D, int el, bool alone) { return D * el > 256 || (alone && D * el > 128) ? 32 : 64; }
 
 __device__ __forceinline__ int swap23(int m) { return (m & ~12) | (m & 4) << 1 | (m & 8) >> 1; }
 
@@ -108,23 +115,27 @@ struct Source {
     const int i = token(r);
     return (long long)i * stride + (KEYS ? 0 : (r - i * G) * row_bytes);
   }
-  // rows r0 .. r0 + BN - 1 into LDS at `dst`; what is not there, and with `pads` rows of padding, as zeros
+  // rows r0 .. r0 + BN - 1 into LDS at `dst`, by the workgroup or by a wave; what is not there, and with `pads` rows of padding, as
+  // zeros
+  template <bool ALONE>
   __device__ __forceinline__ void load(char* dst, int r0, bool pads) const {
+    constexpr int kThreads = ALONE ? kWave : kAttnThreads, kTurns = TileRows<T, D, ALONE>::kBytes / 16 / kThreads;
+    const int tid = ALONE ? (int)(threadIdx.x & 63) : (int)threadIdx.x;
     const int i0 = token(r0);
     const long long skip = (long long)i0 * stride;
     const i32x4 rsrc = uniform(buffer_of(first + skip, bytes - skip));
-    const uint32_t at0 = lds_at(dst) + (uint32_t)(__builtin_amdgcn_readfirstlane(threadIdx.x / kWave) * kWave * 16);
-    uint32_t off[R::kTurns];
+    const uint32_t at0 = lds_at(dst) + (ALONE ? 0u : (uint32_t)(__builtin_amdgcn_readfirstlane(threadIdx.x / kWave) * kWave * 16));
+    uint32_t off[kTurns];
 #pragma unroll
-    for (int t = 0; t < R::kTurns; ++t) {
-      const int at = t * kAttnThreads + (int)threadIdx.x, row = at / R::PR, piece = (at % R::PR) ^ R::mix(row);
+    for (int t = 0; t < kTurns; ++t) {
+      const int at = t * kThreads + tid, row = at / R::PR, piece = (at % R::PR) ^ R::mix(row);
       const int r = r0 + row, i = token(r);
       bool there = r < rows && piece * 16 < row_bytes;
       if (pads && there) there = doc[i] >= 0;
       off[t] = there ? (uint32_t)(i - i0) * stride + (uint32_t)((KEYS ? 0 : r - i * G) * row_bytes + piece * 16) : kNowhere;
     }
 #pragma unroll
-    for (int t = 0; t < R::kTurns; ++t) lds_load<16>(at0 + t * kAttnThreads * 16, rsrc, off[t]);
+    for (int t = 0; t < kTurns; ++t) lds_load<16>(at0 + t * kThreads * 16, rsrc, off[t]);
   }
 };
 
@@ -305,6 +316,29 @@ __device__ __forceinline__ float score(float s, float factor, float cap, float d
 __device__ __forceinline__ float other_half_max(float x) { return fmaxf(x, __uint_as_float(lane_xor_u32<32>(__float_as_uint(x), threadIdx.x & 63))); }
 __device__ __forceinline__ float other_half_sum(float x) { return x + __uint_as_float(lane_xor_u32<32>(__float_as_uint(x), threadIdx.x & 63)); }
 
+// Sums over the four waves: wave w gets those of registers 4 w .. 4 w + 3 of each block of channels.
+template <int D>
+__device__ __forceinline__ void add_waves(char* lds, int wave, int lane, f32x16 (&c)[D / 32]) {
+  f32x4* at = reinterpret_cast<f32x4*>(lds) + lane;  // [wave][block][4][64]
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) at[((wave * (D / 32) + db) * 4 + g) * 64] = f32x4{c[db][4 * g], c[db][4 * g + 1], c[db][4 * g + 2], c[db][4 * g + 3]};
+  __syncthreads();
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db) {
+    f32x4 s = {};
+#pragma unroll
+    for (int w = 0; w < 4; ++w) s += at[((w * (D / 32) + db) * 4 + wave) * 64];
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+      if (g == wave) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) c[db][4 * g + e] = s[e];
+      }
+  }
+}
+
 // What a workgroup's own rows (or keys) see of the other side's tiles: all of them, or those that hold a token of one of its images.
 struct Walk {
   const Span* spans;  // of the other side's image
@@ -329,7 +363,7 @@ struct Walk {
     hi = __builtin_amdgcn_readfirstlane(hi);
     mixed = __builtin_amdgcn_readfirstlane((lo != hi || pad) ? 1 : 0);
   }
-  // the images of tile t's tokens, rows t tile_rows ... (a tile of 64 rows lies in at most two spans)
+  // the images of tile t's tokens, rows t tile_rows ... (a tile of at most 64 rows lies in at most two spans)
   __device__ __forceinline__ Span of(int t, int rows) const {
     const int r0 = t * tile_rows, r1 = min(r0 + tile_rows, rows) - 1;
     const int a = exact_div(r0, G, g_magic) / kSpan, b = exact_div(r1, G, g_magic) / kSpan;
@@ -346,11 +380,17 @@ struct Walk {
     bits = 0;
     base = t - 64;
   }
+  // the tile that matters `more` after the next one
+  __device__ __forceinline__ int skip(int rows, int more) {
+    int t = next(rows);
+    for (int i = 0; i < more && t < end; ++i) t = next(rows);
+    return t;
+  }
   // the next tile that matters, after the one that it gave last; `end`: none
   __device__ __forceinline__ int next(int rows) {
     while (!bits) {
+      if (base + 64 >= end) return end;  // (asked again behind the last one, too)
       base += 64;
-      if (base >= end) return end;
       const int t = base + (int)(threadIdx.x & 63);
       bool hit = t < end;
       if (hit && spans) {
@@ -403,11 +443,11 @@ template <int BN>
 struct KeyNote {
   float x, y;
   int doc;
-  __device__ __forceinline__ void fetch(const AttnParams& p, int b, int k0) {
-    const int j = k0 + (int)threadIdx.x;
+  __device__ __forceinline__ void fetch(const AttnParams& p, int b, int k0, int tid) {
+    const int j = k0 + tid;
     x = y = 0.f;
     doc = -2;
-    if ((int)threadIdx.x < BN && j < p.Nk) {
+    if (tid < BN && j < p.Nk) {
       const size_t token = (size_t)b * p.Nk + j;
       doc = 0;
       if (p.k_doc) {
@@ -421,11 +461,11 @@ struct KeyNote {
       }
     }
   }
-  __device__ __forceinline__ void keep(KeyNotes<BN>& n) const {
-    if ((int)threadIdx.x < BN) {
-      n.x[threadIdx.x] = x;
-      n.y[threadIdx.x] = y;
-      n.doc[threadIdx.x] = doc;
+  __device__ __forceinline__ void keep(KeyNotes<BN>& n, int tid) const {
+    if (tid < BN) {
+      n.x[tid] = x;
+      n.y[tid] = y;
+      n.doc[tid] = doc;
     }
   }
 };

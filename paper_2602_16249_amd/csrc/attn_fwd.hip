@@ -10,20 +10,46 @@
 namespace affmae {
 namespace {
 
-template <typename T, int D, int TERMS, int NB>
-__global__ __launch_bounds__(kAttnThreads, 2) void attn_fwd_kernel(AttnParams p) {
-  using R = TileRows<T, D>;
+// The four waves' running maximum, sum and output of the same rows, joined: every wave gets the maximum and the sum (of both halves), and
+// wave w the sums of registers 4 w .. 4 w + 3 of each block of channels, which it stores.
+template <int D>
+__device__ __forceinline__ void join_waves(char* lds, int wave, int lane, f32x16 (&o)[D / 32], float& m, float& l) {
+  l = other_half_sum(l);
+  float* tops = reinterpret_cast<float*>(lds);
+  __syncthreads();  // (the last tiles have been read)
+  tops[wave * 64 + lane] = m;
+  tops[256 + wave * 64 + lane] = l;
+  __syncthreads();
+  float top = m;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) top = fmaxf(top, tops[w * 64 + lane]);
+  const float from = top == -__builtin_inff() ? 0.f : top;
+  float sum = 0.f;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) sum += tops[256 + w * 64 + lane] * __builtin_amdgcn_exp2f(tops[w * 64 + lane] - from);
+  const float mine = __builtin_amdgcn_exp2f(m - from);
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db) o[db] *= mine;
+  __syncthreads();
+  add_waves<D>(lds, wave, lane, o);
+  m = top;
+  l = sum;
+}
+
+template <typename T, int D, int TERMS, bool ALONE, int NB>
+__global__ __launch_bounds__(kAttnThreads, (kAttnWaves<T, D>)) void attn_fwd_kernel(AttnParams p) {
+  using R = TileRows<T, D, ALONE>;
   constexpr int BN = R::BN;
   extern __shared__ __align__(16) char lds[];
-  __shared__ KeyNotes<BN> notes[2];
+  __shared__ KeyNotes<BN> notes[ALONE ? 4 : 2];
   const int work = xcd_contiguous_block(blockIdx.x, gridDim.x);
   if (work >= p.work) return;
   const int group = exact_div(work, p.blocks, p.blocks_magic), block = work - group * p.blocks;  // group: (split, image, key head)
   const int split = group / (p.B * p.Hk), bh = group - split * p.B * p.Hk, b = bh / p.Hk, hk = bh - b * p.Hk;
   const int lane = threadIdx.x & 63, half = lane >> 5;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  constexpr int kRows = kAttnRows * NB;
-  const int block0 = block * kRows, r0 = block0 + wave * 32 * NB;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), tid = ALONE ? lane : (int)threadIdx.x;
+  constexpr int kRows = ALONE ? 32 : kAttnRows * NB;
+  const int block0 = block * kRows, r0 = ALONE ? block0 : block0 + wave * 32 * NB;
   const bool busy = r0 < p.rows;
   const Source<T, D, true> keys(p, p.k, b, hk), values(p, p.v, b, hk);
   Row own[NB];
@@ -52,7 +78,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_fwd_kernel(AttnParams p)
   walk.start(split * p.split_tiles);
 
   const auto fetch = [&](int t, int buffer, KeyNote<BN>& note, bool& masked) __attribute__((always_inline)) {
-    char* dst = lds + buffer * 2 * R::kBytes;
+    char* dst = lds + (ALONE ? wave : buffer) * 2 * R::kBytes;
     bool pads = false;
     masked = t * BN + BN > p.Nk;
     if (walk.spans) {
@@ -60,9 +86,9 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_fwd_kernel(AttnParams p)
       pads = __builtin_amdgcn_readfirstlane(x.pad);
       masked = masked || walk.mixed || pads || __builtin_amdgcn_readfirstlane(x.lo) != walk.lo || __builtin_amdgcn_readfirstlane(x.hi) != walk.lo;
     }
-    keys.load(dst, t * BN, pads);
-    values.load(dst + R::kBytes, t * BN, pads);
-    if (masked || (TERMS & kDistance)) note.fetch(p, b, t * BN);
+    keys.template load<ALONE>(dst, t * BN, pads);
+    values.template load<ALONE>(dst + R::kBytes, t * BN, pads);
+    if (masked || (TERMS & kDistance)) note.fetch(p, b, t * BN, tid);
   };
 
   f32x16 o[NB][D / 32] = {};
@@ -71,23 +97,25 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_fwd_kernel(AttnParams p)
   for (int n = 0; n < NB; ++n) m[n] = -__builtin_inff(), l[n] = 0.f;
   KeyNote<BN> note = {};
   bool masked = false;
-  int t = walk.next(p.Nk);
+  int t = walk.skip(p.Nk, ALONE ? wave : 0);
   if (t < walk.end) {
     fetch(t, 0, note, masked);
-    note.keep(notes[0]);
+    note.keep(notes[ALONE ? wave : 0], tid);
   }
-  for (int buffer = 0; t < walk.end; buffer ^= 1) {
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    const int following = walk.next(p.Nk);
+  for (int buffer = 0; t < walk.end; buffer ^= ALONE ? 0 : 1) {
+    // the tile has arrived, and (with a barrier) every wave has read what the next one will be written over
+    if constexpr (ALONE) asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    const int following = walk.skip(p.Nk, ALONE ? 3 : 0);
     bool next_masked = false;
-    if (following < walk.end) fetch(following, buffer ^ 1, note, next_masked);
-    const char* kt = lds + buffer * 2 * R::kBytes;
+    if (!ALONE && following < walk.end) fetch(following, buffer ^ 1, note, next_masked);
+    const char* kt = lds + (ALONE ? wave : buffer) * 2 * R::kBytes;
     const char* vt = kt + R::kBytes;
     if (busy) {
       f32x16 s[R::kBlocks][NB];
 #pragma unroll
       for (int kb = 0; kb < R::kBlocks; ++kb) row_products<T, D, NB>(kt, kb, q, s[kb], lane);
-      const KeyNotes<BN>& notes_ = notes[buffer];
+      const KeyNotes<BN>& notes_ = notes[ALONE ? wave : buffer];
       const bool plain = !TERMS && !masked;
       const float times = plain ? factor : 1.f;
 #pragma unroll
@@ -159,15 +187,22 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_fwd_kernel(AttnParams p)
         }
       }
     }
-    if (following < walk.end) note.keep(notes[buffer ^ 1]);
+    if (following < walk.end) {
+      if constexpr (ALONE) {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (the tile has been read)
+        fetch(following, buffer, note, next_masked);
+      }
+      note.keep(notes[ALONE ? wave : buffer ^ 1], tid);
+    }
     t = following;
     masked = next_masked;
   }
 
+  if constexpr (ALONE) join_waves<D>(lds, wave, lane, o[0], m[0], l[0]);
   if (!busy) return;
 #pragma unroll
   for (int n = 0; n < NB; ++n) {
-    const float sum = other_half_sum(l[n]);
+    const float sum = ALONE ? l[n] : other_half_sum(l[n]);
     const float part = sum > 0.f ? 1.f / sum : (sum == sum ? 0.f : sum);  // (no key: zeros; a NaN stays one)
     const float lse = sum > 0.f ? __builtin_fmaf(m[n], kLn2, __logf(sum)) : (sum == sum ? -__builtin_inff() : sum);
     if (!own[n].there) continue;
@@ -177,7 +212,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_fwd_kernel(AttnParams p)
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
         const int ch = 32 * db + 8 * g + 4 * half;
-        if (ch < p.d) {
+        if (ch < p.d && (!ALONE || g == wave)) {
           float v[4];
 #pragma unroll
           for (int e = 0; e < 4; ++e) v[e] = o[n][db][4 * g + e] * part;
@@ -185,36 +220,51 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_fwd_kernel(AttnParams p)
           else store_piece<4>((T*)p.o + own[n].at * p.d + ch, v);
         }
       }
-    if (half == 0) (p.part ? p.part + (size_t)p.splits * all * p.d + (size_t)split * all : p.lse_out)[own[n].at] = lse;
+    if (half == 0 && (!ALONE || wave == 0)) (p.part ? p.part + (size_t)p.splits * all * p.d + (size_t)split * all : p.lse_out)[own[n].at] = lse;
   }
 }
 
-// out = sum over splits of exp(lse_s - lse) out_s, lse = log sum exp lse_s: a thread for four channels of a (query, head)
+// out = sum over splits of exp(lse_s - lse) out_s, lse = log sum exp lse_s.  A thread takes four channels of a (query, head) for every `lanes`th
+// split, and the first of the lanes adds up, in their order.  (A thread for all splits waited for one after the other: 24 us for 43.)
 template <typename T>
-__global__ __launch_bounds__(256) void attn_join_kernel(const float* part, int splits, size_t all, int d, T* out, float* lse) {
-  const int quarters = d / 4;
-  const size_t at = (size_t)blockIdx.x * 256 + threadIdx.x;
-  if (at >= all * quarters) return;
-  const size_t row = at / quarters;
-  const int ch = (int)(at - row * quarters) * 4;
+__global__ __launch_bounds__(256) void attn_join_kernel(const float* part, int splits, int lanes, size_t all, int d, T* out, float* lse) {
+  __shared__ float sums[256][5];
+  const int quarters = d / 4, per = quarters * lanes, rows = 256 / per;
+  const int slot = (int)threadIdx.x / per, in_row = (int)threadIdx.x - slot * per, lane = in_row / quarters, ch = (in_row - lane * quarters) * 4;
+  const size_t row = (size_t)blockIdx.x * rows + slot;
+  const bool there = slot < rows && row < all;
   const float* ls = part + (size_t)splits * all * d + row;
-  float top = -__builtin_inff();
-  for (int s = 0; s < splits; ++s) top = fmaxf(top, ls[s * all]);
-  const float from = top == -__builtin_inff() ? 0.f : top;
-  float sum = 0.f, v[4] = {};
-  for (int s = 0; s < splits; ++s) {
-    const float w = __expf(ls[s * all] - from);
-    float x[4];
-    load_piece<4>(part + (s * all + row) * d + ch, x);
-    sum += w;
+  float top = -__builtin_inff(), sum = 0.f, v[4] = {};
+  if (there) {
+#pragma unroll 8
+    for (int s = 0; s < splits; ++s) top = fmaxf(top, ls[s * all]);
+    const float from = top == -__builtin_inff() ? 0.f : top;
+    for (int s = lane; s < splits; s += lanes) {
+      const float w = __expf(ls[s * all] - from);
+      float x[4];
+      load_piece<4>(part + (s * all + row) * d + ch, x);
+      sum += w;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = __builtin_fmaf(w, x[e], v[e]);
+      for (int e = 0; e < 4; ++e) v[e] = __builtin_fmaf(w, x[e], v[e]);
+    }
+    top = from;
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) sums[threadIdx.x][e] = v[e];
+  sums[threadIdx.x][4] = sum;
+  __syncthreads();
+  if (!there || lane > 0) return;
+  for (int i = 1; i < lanes; ++i) {
+    const float* x = sums[threadIdx.x + i * quarters];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] += x[e];
+    sum += x[4];
   }
   const float inv = sum > 0.f ? 1.f / sum : (sum == sum ? 0.f : sum);
 #pragma unroll
   for (int e = 0; e < 4; ++e) v[e] *= inv;
   store_piece<4>(out + row * d + ch, v);
-  if (ch == 0) lse[row] = sum > 0.f ? from + __logf(sum) : (sum == sum ? -__builtin_inff() : sum);
+  if (ch == 0) lse[row] = sum > 0.f ? top + __logf(sum) : (sum == sum ? -__builtin_inff() : sum);
 }
 
 __global__ __launch_bounds__(256) void attn_spans_kernel(const int32_t* q_doc, const int32_t* k_doc, int Nq, int Nk, int q_spans, int k_spans, int images, Span* to_q, Span* to_k) {
@@ -239,38 +289,53 @@ __global__ __launch_bounds__(256) void attn_spans_kernel(const int32_t* q_doc, c
   if (lane == 0) (q ? to_q : to_k)[n] = Span{lo, hi, pad, 0};
 }
 
-// Splits of the keys: where the rows alone do not fill the chip's 256 CUs twice, as many as do, of at least kLeastKeys keys.
+// Where blocks of 128 rows do not fill the chip's 256 CUs twice, blocks of 32 whose waves share the keys out; where these do not either,
+// the keys are split over workgroups too, kLeastKeys each at least.
 constexpr int kLeastKeys = 256;
-void plan(int B, int Nq, int Nk, int H, int Hk, int D, int el, int& blocks, int& splits, int& split_tiles) {
-  const int BN = D * el > 256 ? 32 : 64;
-  const long long rows = (long long)Nq * (H / Hk);
-  blocks = (int)((rows + kAttnRows - 1) / kAttnRows);
+struct Plan {
+  bool alone;
+  int blocks, splits, split_tiles;
+};
+Plan plan(int B, int Nq, int Nk, int H, int Hk, int D, int el) {
+  const long long rows = (long long)Nq * (H / Hk), heads = (long long)B * Hk;
+  Plan l;
+  l.alone = (rows + kAttnRows - 1) / kAttnRows * heads < 512;
+  const int BN = attn_tile_rows(D, el, l.alone);
+  const int per = l.alone ? 32 : kAttnRows;
+  l.blocks = (int)((rows + per - 1) / per);
   const int tiles = (Nk + BN - 1) / BN;
-  const long long groups = (long long)B * Hk * blocks;
-  long long want = std::min<long long>((512 + groups - 1) / groups, std::max(1, Nk / kLeastKeys));
-  split_tiles = (int)((tiles + want - 1) / want);
-  splits = (tiles + split_tiles - 1) / split_tiles;
+  const long long groups = heads * l.blocks;
+  const long long want = std::max(1ll, std::min<long long>(512 / groups, Nk / kLeastKeys));
+  l.split_tiles = (int)((tiles + want - 1) / want);
+  l.splits = (tiles + l.split_tiles - 1) / l.split_tiles;
+  return l;
 }
 int width(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : 128; }
 
-template <typename T, int D, int TERMS, int NB>
-hipError_t launch(const AttnParams& p, hipStream_t stream) {
-  const size_t lds = 4 * TileRows<T, D>::kBytes;
-  const hipError_t e = hipFuncSetAttribute((const void*)attn_fwd_kernel<T, D, TERMS, NB>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+template <typename T, int D, int TERMS, bool ALONE>
+hipError_t launch_kernel(const AttnParams& p, hipStream_t stream) {
+  constexpr int NB = 1;
+  const size_t lds = (ALONE ? 8 : 4) * TileRows<T, D, ALONE>::kBytes;
+  const hipError_t e = hipFuncSetAttribute((const void*)attn_fwd_kernel<T, D, TERMS, ALONE, NB>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
   if (e != hipSuccess) return e;
-  AFFMAE_LAUNCH("attn_fwd_kernel", stream, (attn_fwd_kernel<T, D, TERMS, NB>), dim3((p.work + 7) / 8 * 8), dim3(kAttnThreads), lds, stream, p);
-  if (p.part) {
-    const size_t all = (size_t)p.B * p.Nq * p.H;
-    AFFMAE_LAUNCH("attn_join_kernel", stream, attn_join_kernel<T>, dim3((unsigned)((all * (p.d / 4) + 255) / 256)), dim3(256), 0, stream, p.part, p.splits, all, p.d, (T*)p.o, p.lse_out);
-  }
+  AFFMAE_LAUNCH("attn_fwd_kernel", stream, (attn_fwd_kernel<T, D, TERMS, ALONE, NB>), dim3((p.work + 7) / 8 * 8), dim3(kAttnThreads), lds, stream, p);
+  return hipGetLastError();
+}
+template <typename T, int D, int TERMS>
+hipError_t launch(const AttnParams& p, hipStream_t stream) {
+  const hipError_t e = p.alone ? launch_kernel<T, D, TERMS, true>(p, stream) : launch_kernel<T, D, TERMS, false>(p, stream);
+  if (e != hipSuccess || !p.part) return e;
+  const size_t all = (size_t)p.B * p.Nq * p.H;
+  const int lanes = std::min(p.splits, 256 / (p.d / 4)), rows = 256 / (lanes * (p.d / 4));
+  AFFMAE_LAUNCH("attn_join_kernel", stream, attn_join_kernel<T>, dim3((unsigned)((all + rows - 1) / rows)), dim3(256), 0, stream, p.part, p.splits, lanes, all, p.d, (T*)p.o, p.lse_out);
   return hipGetLastError();
 }
 template <typename T, int TERMS>
 hipError_t launch_width(const AttnParams& p, hipStream_t stream) {
   switch (width(p.d)) {
-    case 32: return launch<T, 32, TERMS, 1>(p, stream);
-    case 64: return launch<T, 64, TERMS, 1>(p, stream);
-    default: return launch<T, 128, TERMS, 1>(p, stream);
+    case 32: return launch<T, 32, TERMS>(p, stream);
+    case 64: return launch<T, 64, TERMS>(p, stream);
+    default: return launch<T, 128, TERMS>(p, stream);
   }
 }
 template <typename T>
@@ -306,16 +371,16 @@ hipError_t launch_attn_spans(const AttnArgs& a, Span* q_span, Span* k_span, hipS
 }
 
 size_t attn_fwd_workspace_bytes(int B, int Nq, int Nk, int H, int Hk, int d, int dtype, bool docs) {
-  int blocks, splits, split_tiles;
-  plan(B, Nq, Nk, H, Hk, width(d), dtype == 1 ? 2 : 4, blocks, splits, split_tiles);
-  return (docs ? attn_span_bytes(B, Nq, Nk) : 0) + (splits > 1 ? (size_t)splits * B * Nq * H * (d + 1) * sizeof(float) : 0);
+  const Plan l = plan(B, Nq, Nk, H, Hk, width(d), dtype == 1 ? 2 : 4);
+  return (docs ? attn_span_bytes(B, Nq, Nk) : 0) + (l.splits > 1 ? (size_t)l.splits * B * Nq * H * (d + 1) * sizeof(float) : 0);
 }
 
 hipError_t launch_attn_fwd(const AttnArgs& a, hipStream_t stream) {
   AttnParams p = attn_params(a, static_cast<Span*>(a.workspace));
   p.o = a.out;
   p.lse_out = a.lse;
-  plan(a.B, a.Nq, a.Nk, a.H, a.Hk, width(a.d), a.dtype == 1 ? 2 : 4, p.blocks, p.splits, p.split_tiles);
+  const Plan l = plan(a.B, a.Nq, a.Nk, a.H, a.Hk, width(a.d), a.dtype == 1 ? 2 : 4);
+  p.alone = l.alone; p.blocks = l.blocks; p.splits = l.splits; p.split_tiles = l.split_tiles;
   if (p.splits > 1) p.part = reinterpret_cast<float*>(static_cast<char*>(a.workspace) + (a.q_doc ? attn_span_bytes(a.B, a.Nq, a.Nk) : 0));
   p.blocks_magic = div_magic(p.blocks);
   p.work = a.B * a.Hk * p.blocks * p.splits;
