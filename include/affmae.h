@@ -612,7 +612,7 @@ int affmae_rotary_bwd(const void* dq_out, const void* dk_out, const void* q_out,
  *
  * Outputs must not overlap inputs or each other.  q, k, v, out, dout and gradients are
  * 16-byte aligned, q_xy and k_xy 8-byte.
- * Limits: d a multiple of 8 up to 128, H <= 4096, Nq, Nk <= 2^24, Nq * H / Hk <= 2^30,
+ * Limits: d a multiple of 8 up to 128, H <= 4096, Nq, Nk <= 2^24, Nq * H / Hk <= 2^28,
  * B * Hk * ceil(Nq * H / Hk / 128) and B * Hk * ceil(Nk / 128) <= 2^24 - 8
  * (AFFMAE_ERR_UNSUPPORTED otherwise).
  * Errors: AFFMAE_ERR_NULL, AFFMAE_ERR_DTYPE, AFFMAE_ERR_SHAPE (sizes < 1, H % Hk, a scale

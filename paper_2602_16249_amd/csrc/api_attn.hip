@@ -28,7 +28,7 @@ int check_attn(int B, int Nq, int Nk, int H, int Hk, int d, int dtype) {
   if (d % 8 || d > 128 || H > 4096 || Nq > (1 << 24) || Nk > (1 << 24)) return AFFMAE_ERR_UNSUPPORTED;
   // (query, head) pairs of a key head are numbered in 31 bits; a launch has at most 2^24 workgroups of 128 of them, or of 128 keys
   const long long rows = (long long)Nq * (H / Hk), most = (1ll << 24) - 8;
-  if (rows > (1ll << 30) || (rows + 127) / 128 * B * Hk > most || ((long long)Nk + 127) / 128 * B * Hk > most) return AFFMAE_ERR_UNSUPPORTED;
+  if (rows > (1ll << 28) || (rows + 127) / 128 * B * Hk > most || ((long long)Nk + 127) / 128 * B * Hk > most) return AFFMAE_ERR_UNSUPPORTED;
   return AFFMAE_OK;
 }
 

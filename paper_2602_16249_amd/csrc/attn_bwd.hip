@@ -18,22 +18,22 @@ namespace {
 
 int width(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : 128; }
 
-template <typename T, int D, int TERMS, bool REST, bool ALONE>
+template <typename T, int D, int TERMS, bool REST, bool DOCS, bool ALONE>
 __global__ __launch_bounds__(kAttnThreads, (kAttnWaves<T, D>)) void attn_bwd_query_kernel(AttnParams p) {
   using R = TileRows<T, D, ALONE>;
   constexpr int BN = R::BN, kTogether = D == 128 ? 1 : 2;  // blocks of a tile that are worked on together
   extern __shared__ __align__(16) char lds[];
-  __shared__ KeyNotes<BN> notes[ALONE ? 4 : 2];
+  __shared__ KeyNotes notes[ALONE ? 4 : 2];
   const int work = xcd_contiguous_block(blockIdx.x, gridDim.x);
   if (work >= p.work) return;
   const int group = exact_div(work, p.blocks, p.blocks_magic), block = work - group * p.blocks;
   const int split = group / (p.B * p.Hk), bh = group - split * p.B * p.Hk, b = bh / p.Hk, hk = bh - b * p.Hk;
   const int lane = threadIdx.x & 63, half = lane >> 5;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), tid = ALONE ? lane : (int)threadIdx.x;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   constexpr int kRows = ALONE ? 32 : kAttnRows;
   const int block0 = block * kRows, r0 = ALONE ? block0 : block0 + wave * 32;
   const bool busy = r0 < p.rows;
-  const Row own = own_row(p, b, hk, r0);
+  Row own = own_row(p, b, hk, r0);
   const Source<T, D, true> keys(p, p.k, b, hk), values(p, p.v, b, hk);
   Fixed<T, D> q[1], g[1];
   q[0].load((const char*)p.q + own.at * p.d * R::E, half, p.d * R::E, own.there);
@@ -49,9 +49,8 @@ __global__ __launch_bounds__(kAttnThreads, (kAttnWaves<T, D>)) void attn_bwd_que
     if (p.negate) q[0].x[s].negate();
   }
   sum = other_half_sum(sum);
-  if (own.there && half == 0 && split == 0 && (!ALONE || wave == 0)) p.rowsum[own.at] = sum;
   const float seen = own.there ? p.lse[own.at] : 0.f;
-  const float lse = seen == -__builtin_inff() ? __builtin_inff() : seen * kLog2e;  // (no key: every p is 0)
+  float lse = seen == -__builtin_inff() ? __builtin_inff() : seen * kLog2e;  // (no key: every p is 0)
   const float factor = TERMS & kCap ? p.scale / p.cap : p.scale * kLog2e, cap = p.cap * kLog2e;
 
   const int tiles = (p.Nk + BN - 1) / BN;
@@ -60,46 +59,49 @@ __global__ __launch_bounds__(kAttnThreads, (kAttnWaves<T, D>)) void attn_bwd_que
   walk.mixed = false;
   walk.end = min(tiles, (split + 1) * p.split_tiles);
   walk.tile_rows = BN; walk.G = 1; walk.g_magic = 0u;
-  if (p.q_doc) {
+  if constexpr (DOCS) {
     walk.spans = p.k_span + (size_t)b * ((p.Nk + kSpan - 1) / kSpan);
     walk.own(p.q_span + (size_t)b * ((p.Nq + kSpan - 1) / kSpan), exact_div(block0, p.G, p.g_magic), exact_div(min(block0 + kRows, p.rows) - 1, p.G, p.g_magic));
   }
   walk.start(split * p.split_tiles);
 
-  const auto fetch = [&](int t, int buffer, KeyNote<BN>& note, bool& masked) __attribute__((always_inline)) {
+  const KeySource about(p, b, TERMS & kDistance, DOCS);
+  const auto fetch = [&](int t, int buffer, bool& masked) __attribute__((always_inline)) {
     char* dst = lds + (ALONE ? wave : buffer) * 2 * R::kBytes;
     bool pads = false;
     masked = t * BN + BN > p.Nk;
-    if (walk.spans) {
+    if constexpr (DOCS) {
       const Span x = walk.of(t, p.Nk);
       pads = __builtin_amdgcn_readfirstlane(x.pad);
       masked = masked || walk.mixed || pads || __builtin_amdgcn_readfirstlane(x.lo) != walk.lo || __builtin_amdgcn_readfirstlane(x.hi) != walk.lo;
     }
     keys.template load<ALONE>(dst, t * BN, pads);
     values.template load<ALONE>(dst + R::kBytes, t * BN, pads);
-    if (masked || (TERMS & kDistance) || (D == 128 && REST)) note.fetch(p, b, t * BN, tid);
+    about.load<TERMS, DOCS, ALONE, BN>(notes[ALONE ? wave : buffer], t * BN, wave, lane);
   };
 
+  q[0].arrive();
+  g[0].arrive();
+  arrive(own);
+  arrive(lse);
+  arrive(sum);
   f32x16 dq[D / 32] = {}, keys_seen[REST ? D / 32 : 1] = {};  // sums of dS k, and of what multiplies D in dS
   float by_distance = 0.f, rest = 0.f, distances = 0.f;  // sums of dZ |x - y|, of dZ, of p |x - y|
-  KeyNote<BN> note = {};
   bool masked = false;
   int t = walk.skip(p.Nk, ALONE ? wave : 0);
-  if (t < walk.end) {
-    fetch(t, 0, note, masked);
-    note.keep(notes[ALONE ? wave : 0], tid);
-  }
+  if (t < walk.end) fetch(t, 0, masked);
   for (int buffer = 0; t < walk.end; buffer ^= ALONE ? 0 : 1) {
     // the tile has arrived, and (with a barrier) every wave has read what the next one will be written over
     if constexpr (ALONE) asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
     const int following = walk.skip(p.Nk, ALONE ? 3 : 0);
     bool next_masked = false;
-    if (!ALONE && following < walk.end) fetch(following, buffer ^ 1, note, next_masked);
+    if (!ALONE && following < walk.end) fetch(following, buffer ^ 1, next_masked);
     const char* kt = lds + (ALONE ? wave : buffer) * 2 * R::kBytes;
     const char* vt = kt + R::kBytes;
     if (busy) {
-      const KeyNotes<BN>& n = notes[ALONE ? wave : buffer];
+      const int left = p.Nk - t * BN - 8 * half;  // keys of the tile that are there, from the lane's first one on
+      const KeyNotes& n = notes[ALONE ? wave : buffer];
 #pragma unroll kTogether
       for (int kb = 0; kb < R::kBlocks; ++kb) {
         f32x16 s[1], dp[1];
@@ -115,9 +117,10 @@ __global__ __launch_bounds__(kAttnThreads, (kAttnWaves<T, D>)) void attn_bwd_que
             else z = score<TERMS, near>(s[0][i], factor, cap, 0.f, 0.f, 0.f, bend, distance) - lse;
             float pr = __builtin_amdgcn_exp2f(z), dz = pr * (dp[0][i] - sum);
             if constexpr (hides) {
-              const bool off = n.doc[j] != own.doc;
+              const bool off = j - 8 * half >= left || (DOCS && n.doc[j] != own.doc);
               pr = off ? 0.f : pr;
               dz = off ? 0.f : dz;
+              if constexpr (DOCS && (TERMS & kDistance)) distance = off ? 0.f : distance;  // (padding may have any place)
             }
             if constexpr (REST || (TERMS & kDistance)) rest += dz;
             if constexpr (TERMS & kDistance) {
@@ -137,7 +140,9 @@ __global__ __launch_bounds__(kAttnThreads, (kAttnWaves<T, D>)) void attn_bwd_que
         using no = std::false_type;
         bool near = false;
         if constexpr ((TERMS & kCap) && D < 128) near = all_near(s[0], factor);
-        if (masked || (D == 128 && REST)) {
+        // keys that are not there have zeros for vectors, so that they add nothing to dq: without sums over p and dZ nothing is hidden
+        constexpr bool kHides = REST || (TERMS & kDistance) || DOCS;
+        if (kHides && (masked || D == 128)) {  // (one way through where two would not fit the registers)
           if (near) slopes(yes{}, yes{});
           else slopes(no{}, yes{});
         } else {
@@ -153,12 +158,9 @@ __global__ __launch_bounds__(kAttnThreads, (kAttnWaves<T, D>)) void attn_bwd_que
         }
       }
     }
-    if (following < walk.end) {
-      if constexpr (ALONE) {
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (the tile has been read)
-        fetch(following, buffer, note, next_masked);
-      }
-      note.keep(notes[ALONE ? wave : buffer ^ 1], tid);
+    if (ALONE && following < walk.end) {
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (the tile has been read)
+      fetch(following, buffer, next_masked);
     }
     t = following;
     masked = next_masked;
@@ -190,14 +192,23 @@ __global__ __launch_bounds__(kAttnThreads, (kAttnWaves<T, D>)) void attn_bwd_que
   }
   if (!busy) return;
   const bool pad = own.doc < 0, first = half == 0 && (!ALONE || wave == 0);
-  if (REST && own.there && first) p.rowrest[(size_t)split * p.B * p.Nq * p.H + own.at] = pad ? 0.f : rest;
+  if (pad) rest = by_distance = distances = 0.f;  // (padding may hold anything)
+  if (own.there && first) {
+    const size_t row = (size_t)bh * p.rows + own.r;
+    const bool none = pad || lse == __builtin_inff();
+    if (split == 0) {
+      p.rowlse[row] = none ? __builtin_inff() : lse;
+      p.rowsum[row] = none ? 0.f : sum + (REST && p.splits == 1 ? rest : 0.f);
+    }
+    if (REST && p.splits > 1) p.rowrest[(size_t)split * p.B * p.Nq * p.H + row] = none ? 0.f : rest;
+  }
   if constexpr (TERMS & kDistance) {
     if (p.rowslope && own.there && first) {
       const size_t tokens = (size_t)p.B * p.Nq, plane = (size_t)p.H * tokens;
       float* to = p.rowslope + (size_t)split * 3 * plane + (size_t)own.head * tokens + (size_t)b * p.Nq + own.i;
-      to[0] = pad ? 0.f : by_distance;
-      to[plane] = pad ? 0.f : rest;
-      to[2 * plane] = pad ? 0.f : distances;
+      to[0] = by_distance;
+      to[plane] = rest;
+      to[2 * plane] = distances;
     }
   }
   if (!own.there) return;
@@ -226,17 +237,22 @@ __global__ __launch_bounds__(kAttnThreads, (kAttnWaves<T, D>)) void attn_bwd_que
     }
 }
 
-template <typename T, int D, int TERMS, bool REST, bool ALONE>
+template <typename T, int D, int TERMS, bool REST, bool DOCS, bool ALONE>
 hipError_t launch_kernel(const AttnParams& p, hipStream_t stream) {
   const size_t lds = (ALONE ? 8 : 4) * TileRows<T, D, ALONE>::kBytes;
-  const hipError_t e = hipFuncSetAttribute((const void*)attn_bwd_query_kernel<T, D, TERMS, REST, ALONE>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+  const hipError_t e = hipFuncSetAttribute((const void*)attn_bwd_query_kernel<T, D, TERMS, REST, DOCS, ALONE>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
   if (e != hipSuccess) return e;
-  AFFMAE_LAUNCH("attn_bwd_query_kernel", stream, (attn_bwd_query_kernel<T, D, TERMS, REST, ALONE>), dim3((p.work + 7) / 8 * 8), dim3(kAttnThreads), lds, stream, p);
+  AFFMAE_LAUNCH("attn_bwd_query_kernel", stream, (attn_bwd_query_kernel<T, D, TERMS, REST, DOCS, ALONE>), dim3((p.work + 7) / 8 * 8), dim3(kAttnThreads), lds, stream, p);
   return hipGetLastError();
 }
 template <typename T, int D, int TERMS, bool REST>
 hipError_t launch(const AttnParams& p, hipStream_t stream) {
-  return p.alone ? launch_kernel<T, D, TERMS, REST, true>(p, stream) : launch_kernel<T, D, TERMS, REST, false>(p, stream);
+  if constexpr (D == 128 && sizeof(T) == 2 && !REST) {  // (with images D is always put right)
+    return p.alone ? launch_kernel<T, D, TERMS, REST, false, true>(p, stream) : launch_kernel<T, D, TERMS, REST, false, false>(p, stream);
+  } else {
+    if (p.q_doc) return p.alone ? launch_kernel<T, D, TERMS, REST, true, true>(p, stream) : launch_kernel<T, D, TERMS, REST, true, false>(p, stream);
+    return p.alone ? launch_kernel<T, D, TERMS, REST, false, true>(p, stream) : launch_kernel<T, D, TERMS, REST, false, false>(p, stream);
+  }
 }
 template <typename T, int TERMS>
 hipError_t launch_width(const AttnParams& p, hipStream_t stream) {
@@ -246,7 +262,7 @@ hipError_t launch_width(const AttnParams& p, hipStream_t stream) {
     case 64: return launch<T, 64, TERMS, kBf16>(p, stream);
     default:
       if constexpr (kBf16 && !(TERMS & kDistance))
-        if (!p.rowrest) return launch<T, 128, TERMS, false>(p, stream);
+        if (!p.puts_right) return launch<T, 128, TERMS, false>(p, stream);
       return launch<T, 128, TERMS, kBf16>(p, stream);
   }
 }
@@ -256,24 +272,32 @@ hipError_t launch_query(const AttnParams& p, hipStream_t stream) {
   return p.slope ? launch_width<T, kDistance>(p, stream) : launch_width<T, 0>(p, stream);
 }
 
-// Parts of splits added up, in their order: of dq, dk and dv, a blockIdx.y each.  With `rest`, whose sum is what D lacks in a row of d
-// values, as much of `seen` is taken off, and the whole times `scale`.
+// Parts of splits added up, in their order: of dq, or of dk and dv, a blockIdx.y each.  With `rest`, whose sum is what D lacks in a row of d
+// values, as much of `seen` is taken off, and D gets it; the whole times `scale`.
 struct Join {
   const float *part, *seen, *rest;
+  float* sum;  // with rest: D, which it is added to
   void* out;
   int splits, d;
   size_t n;  // values, a multiple of 4
   float scale;
+  int rows, H, G;  // with rest: part's rows are (query, head) in [B,Nq,H], rest's and sum's [B,Hk,rows]
 };
 struct Joins {
-  Join of[3];
+  Join of[2];
 };
 template <typename T>
 __global__ __launch_bounds__(256) void attn_bwd_join_kernel(Joins all) {
-  const Join j = blockIdx.y == 0 ? all.of[0] : blockIdx.y == 1 ? all.of[1] : all.of[2];
+  const Join j = blockIdx.y == 0 ? all.of[0] : all.of[1];
   for (size_t at = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4; at < j.n; at += (size_t)gridDim.x * 1024) {
     float v[4] = {}, u[4] = {}, rest = 0.f;
-    const size_t rows = j.n / j.d, row = at / j.d;
+    const size_t all_rows = j.n / j.d, at_row = at / j.d;
+    size_t row = 0;
+    if (j.rest) {
+      const int head = (int)(at_row % j.H), Nq = j.rows / j.G;
+      const size_t token = at_row / j.H, b = token / Nq, i = token - b * Nq;
+      row = (b * (j.H / j.G) + head / j.G) * j.rows + i * j.G + head % j.G;
+    }
     for (int s = 0; s < j.splits; ++s) {
       float x[4];
       load_piece<4>(j.part + s * j.n + at, x);
@@ -283,12 +307,13 @@ __global__ __launch_bounds__(256) void attn_bwd_join_kernel(Joins all) {
         load_piece<4>(j.seen + s * j.n + at, x);
 #pragma unroll
         for (int e = 0; e < 4; ++e) u[e] += x[e];
-        rest += j.rest[s * rows + row];
+        rest += j.rest[s * all_rows + row];
       }
     }
 #pragma unroll
     for (int e = 0; e < 4; ++e) v[e] = __builtin_fmaf(-rest, u[e], v[e]) * j.scale;
     store_piece<4>((T*)j.out + at, v);
+    if (j.rest && at % j.d == 0) j.sum[row] += rest;
   }
 }
 
@@ -341,7 +366,7 @@ Side side(long long own, long long other, long long heads, int D, int el) {
 
 struct Layout {
   Side query, key;
-  size_t spans, rowsum, rowrest, rowslope, part_q, seen_q, part_k, part_v, total;  // places in the workspace
+  size_t spans, rowsum, rowlse, rowrest, rowslope, part_q, seen_q, part_k, part_v, total;  // places in the workspace
   bool rest;
 };
 // Whether D is put right (attn_bwd.hip's head).  In heads of 32 and 64 channels the product that this takes is hidden behind the
@@ -364,7 +389,8 @@ Layout layout(int B, int Nq, int Nk, int H, int Hk, int d, int dtype, bool docs,
   l.spans = take(docs ? attn_span_bytes(B, Nq, Nk) : 0);
   l.rest = puts_right(Nk, d, dtype, docs, distance);
   l.rowsum = take(nq * 4);
-  l.rowrest = take(l.rest ? (size_t)l.query.splits * nq * 4 : 0);
+  l.rowlse = take(nq * 4);
+  l.rowrest = take(l.rest && l.query.splits > 1 ? (size_t)l.query.splits * nq * 4 : 0);
   l.rowslope = take(want_dslope ? (size_t)l.query.splits * 3 * nq * 4 : 0);
   l.part_q = take(l.query.splits > 1 ? (size_t)l.query.splits * nq * d * 4 : 0);
   l.seen_q = take(l.query.splits > 1 && l.rest ? (size_t)l.query.splits * nq * d * 4 : 0);
@@ -386,8 +412,9 @@ hipError_t launch_attn_bwd(const AttnArgs& a, hipStream_t stream) {
   AttnParams p = attn_params(a, reinterpret_cast<Span*>(ws + l.spans));
   p.rowsum = reinterpret_cast<float*>(ws + l.rowsum);
   p.rowslope = a.dslope ? reinterpret_cast<float*>(ws + l.rowslope) : nullptr;
-  p.rowrest = l.rest ? reinterpret_cast<float*>(ws + l.rowrest) : nullptr;
-  p.row_splits = l.query.splits;
+  p.rowlse = reinterpret_cast<float*>(ws + l.rowlse);
+  p.rowrest = reinterpret_cast<float*>(ws + l.rowrest);
+  p.puts_right = l.rest;
   p.grad_scale = a.scale;
   p.dq = a.dq; p.dk = a.dk; p.dv = a.dv;
   AttnParams pq = p, pk = p;
@@ -404,26 +431,17 @@ hipError_t launch_attn_bwd(const AttnArgs& a, hipStream_t stream) {
   if (e != hipSuccess) return e;
   e = a.dtype == 1 ? launch_query<bf16_t>(pq, stream) : launch_query<float>(pq, stream);
   if (e != hipSuccess) return e;
-  e = launch_attn_bwd_key(pk, a.dtype, stream);
-  if (e != hipSuccess) return e;
-  Joins j = {};
-  int parts = 0;
-  size_t most = 0;
-  const auto join = [&](const float* part, const float* seen, const float* rest, void* out, int splits, size_t n, float scale) {
-    j.of[parts++] = {part, seen, rest, out, splits, a.d, n, scale};
-    most = std::max(most, n);
-  };
   const size_t nq = (size_t)a.B * a.Nq * a.H * a.d, nk = (size_t)a.B * a.Nk * a.Hk * a.d;
-  if (pq.splits > 1) join(pq.part, pq.part_v, p.rowrest, a.dq, pq.splits, nq, a.scale);
-  if (pk.splits > 1) {
-    join(pk.part, nullptr, nullptr, a.dk, pk.splits, nk, 1.f);
-    join(pk.part_v, nullptr, nullptr, a.dv, pk.splits, nk, 1.f);
-  }
-  if (parts) {
-    const dim3 grid((unsigned)std::min<size_t>((most / 4 + 255) / 256, 4096), parts);
+  const auto join = [&](const Joins& j, int parts) {
+    const dim3 grid((unsigned)std::min<size_t>((j.of[0].n / 4 + 255) / 256, 4096), parts);
     if (a.dtype == 1) AFFMAE_LAUNCH("attn_bwd_join_kernel", stream, attn_bwd_join_kernel<bf16_t>, grid, dim3(256), 0, stream, j);
     else AFFMAE_LAUNCH("attn_bwd_join_kernel", stream, attn_bwd_join_kernel<float>, grid, dim3(256), 0, stream, j);
-  }
+  };
+  if (pq.splits > 1) join({{{pq.part, pq.part_v, l.rest ? p.rowrest : nullptr, p.rowsum, a.dq, pq.splits, a.d, nq, a.scale, p.rows, a.H, p.G}}}, 1);
+  e = launch_attn_bwd_key(pk, a.dtype, stream);
+  if (e != hipSuccess) return e;
+  if (pk.splits > 1)
+    join({{{pk.part, nullptr, nullptr, nullptr, a.dk, pk.splits, a.d, nk, 1.f}, {pk.part_v, nullptr, nullptr, nullptr, a.dv, pk.splits, a.d, nk, 1.f}}}, 2);
   if (a.dslope)
     AFFMAE_LAUNCH("attn_bwd_slope_kernel", stream, attn_bwd_slope_kernel, dim3(a.H), dim3(1024), 0, stream, p.rowslope, pq.splits, a.H, (size_t)a.B * a.Nq, a.dslope);
   return hipGetLastError();

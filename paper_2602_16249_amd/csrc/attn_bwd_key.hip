@@ -6,54 +6,45 @@
 namespace affmae {
 namespace {
 
-// Of a tile's rows: lse in units of log 2 (infinity for rows that are not there, see no key or are padding: their p is 0) and <dout,
-// out>; place, slope and image.
-template <int BN>
+// Rows of a tile, as they are in memory (attn_common.h: KeyNotes): lse and D (zeros behind the last one, whose vectors are zeros too), place,
+// slope and image.
 struct RowNotes {
-  float lse[BN], sum[BN], x[BN], y[BN], slope[BN];
-  int doc[BN];
+  float lse[64], sum[64], x[64], y[64], slope[64];
+  int doc[64];
 };
-template <int BN>
-struct RowNote {
-  float lse, sum, x, y, slope;
-  int doc;
-  __device__ __forceinline__ void fetch(const AttnParams& p, int b, int hk, int r0, int tid) {
-    const int r = r0 + tid;
-    lse = __builtin_inff();
-    sum = x = y = slope = 0.f;
-    doc = -2;
-    if (tid < BN && r < p.rows) {
-      const int i = exact_div(r, p.G, p.g_magic), head = hk * p.G + (r - i * p.G);
-      const size_t token = (size_t)b * p.Nq + i, at = token * p.H + head;
-      doc = 0;
-      if (p.q_doc) {
-        doc = p.q_doc[token];
-        if (doc < 0) doc = -2;
-      }
-      if (p.slope && doc >= 0) {
-        const float2 xy = reinterpret_cast<const float2*>(p.q_xy)[token];
-        x = xy.x;
-        y = xy.y;
-        slope = p.slope[head] * kLog2e;
-      }
-      const float seen = p.lse[at];
-      if (doc >= 0 && seen != -__builtin_inff()) {
-        lse = seen * kLog2e;
-        sum = p.rowsum[at];
-        if (p.rowrest)
-          for (int s = 0; s < p.row_splits; ++s) sum += p.rowrest[(size_t)s * p.B * p.Nq * p.H + at];
-      }
+struct RowSource {
+  i32x4 lse, sum, xy, slope, doc;
+  int rows, G;
+  uint32_t g_magic;
+  __device__ __forceinline__ RowSource(const AttnParams& p, int b, int hk, bool places, bool images) : rows(p.rows), G(p.G), g_magic(p.g_magic) {
+    const size_t at = ((size_t)b * p.Hk + hk) * p.rows;
+    lse = uniform(buffer_of((const char*)(p.rowlse + at), 4ll * p.rows));
+    sum = uniform(buffer_of((const char*)(p.rowsum + at), 4ll * p.rows));
+    if (places) {
+      xy = uniform(buffer_of((const char*)(p.q_xy + 2 * (size_t)b * p.Nq), 8ll * p.Nq));
+      slope = uniform(buffer_of((const char*)(p.slope + hk * p.G), 4ll * p.G));
     }
+    if (images) doc = uniform(buffer_of((const char*)(p.q_doc + (size_t)b * p.Nq), 4ll * p.Nq));
   }
-  __device__ __forceinline__ void keep(RowNotes<BN>& n, int tid, bool places) const {
-    if (tid < BN) {
-      n.lse[tid] = lse;
-      n.sum[tid] = sum;
-      n.doc[tid] = doc;
-      if (places) {
-        n.x[tid] = x;
-        n.y[tid] = y;
-        n.slope[tid] = slope;
+  template <int TERMS, bool DOCS, bool ALONE, int BN>
+  __device__ __forceinline__ void load(RowNotes& n, int r0, int wave, int lane) const {
+    const int r = r0 + lane;
+    if (lane < BN) {
+      const bool there = r < rows;
+      if (ALONE || wave == 0) lds_load<4>(lds_at(n.lse), lse, there ? (uint32_t)r * 4u : kNowhere);
+      if (ALONE || wave == 1) lds_load<4>(lds_at(n.sum), sum, there ? (uint32_t)r * 4u : kNowhere);
+      if constexpr (DOCS || (TERMS & kDistance)) {
+        const int i = exact_div(r, G, g_magic);
+        if constexpr (TERMS & kDistance) {
+          if (ALONE || wave == 2) {
+            const uint32_t at = there ? (uint32_t)i * 8u : kNowhere;
+            lds_load<4>(lds_at(n.x), xy, at);
+            lds_load<4>(lds_at(n.y), xy, at + 4);
+          }
+          if (ALONE || wave == 3) lds_load<4>(lds_at(n.slope), slope, there ? (uint32_t)(r - i * G) * 4u : kNowhere);
+        }
+        if constexpr (DOCS)
+          if (ALONE || wave == 0) lds_load<4>(lds_at(n.doc), doc, there ? (uint32_t)i * 4u : kNowhere);
       }
     }
   }
@@ -64,13 +55,13 @@ __global__ __launch_bounds__(kAttnThreads, (sizeof(T) == 4 && D > 32 ? 1 : 2)) v
   using R = TileRows<T, D, ALONE>;
   constexpr int BN = R::BN, kTogether = D == 128 ? 1 : 2;  // blocks of a tile that are worked on together
   extern __shared__ __align__(16) char lds[];
-  __shared__ RowNotes<BN> notes[ALONE ? 4 : 2];
+  __shared__ RowNotes notes[ALONE ? 4 : 2];
   const int work = xcd_contiguous_block(blockIdx.x, gridDim.x);
   if (work >= p.work) return;
   const int group = exact_div(work, p.blocks, p.blocks_magic), block = work - group * p.blocks;
   const int split = group / (p.B * p.Hk), bh = group - split * p.B * p.Hk, b = bh / p.Hk, hk = bh - b * p.Hk;
   const int lane = threadIdx.x & 63, half = lane >> 5;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), tid = ALONE ? lane : (int)threadIdx.x;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   constexpr int kRows = ALONE ? 32 : kAttnRows;
   const int block0 = block * kRows, j0 = ALONE ? block0 : block0 + wave * 32;
   const bool busy = j0 < p.Nk;
@@ -83,7 +74,7 @@ __global__ __launch_bounds__(kAttnThreads, (sizeof(T) == 4 && D > 32 ? 1 : 2)) v
     own_x = xy.x;
     own_y = xy.y;
   }
-  const int own_doc = DOCS ? max(p.k_doc[token], -1) : 0;
+  int own_doc = DOCS ? max(p.k_doc[token], -1) : 0;
   const Source<T, D, false> queries(p, p.q, b, hk), douts(p, p.dout, b, hk);
   Fixed<T, D> k[1], v[1];
   k[0].load((const char*)p.k + own_at * p.d * R::E, half, p.d * R::E, there);
@@ -106,7 +97,8 @@ __global__ __launch_bounds__(kAttnThreads, (sizeof(T) == 4 && D > 32 ? 1 : 2)) v
   }
   walk.start(split * p.split_tiles);
 
-  const auto fetch = [&](int t, int buffer, RowNote<BN>& note, bool& masked) __attribute__((always_inline)) {
+  const RowSource about(p, b, hk, TERMS & kDistance, DOCS);
+  const auto fetch = [&](int t, int buffer, bool& masked) __attribute__((always_inline)) {
     char* dst = lds + (ALONE ? wave : buffer) * 2 * R::kBytes;
     bool pads = false;
     masked = false;
@@ -117,28 +109,29 @@ __global__ __launch_bounds__(kAttnThreads, (sizeof(T) == 4 && D > 32 ? 1 : 2)) v
     }
     queries.template load<ALONE>(dst, t * BN, pads);
     douts.template load<ALONE>(dst + R::kBytes, t * BN, pads);
-    note.fetch(p, b, hk, t * BN, tid);
+    about.load<TERMS, DOCS, ALONE, BN>(notes[ALONE ? wave : buffer], t * BN, wave, lane);
   };
 
+  k[0].arrive();
+  v[0].arrive();
+  arrive(own_x);
+  arrive(own_y);
+  arrive(own_doc);
   f32x16 dk[D / 32] = {}, dv[D / 32] = {};
-  RowNote<BN> note = {};
   bool masked = false;
   int t = walk.skip(p.rows, ALONE ? wave : 0);
-  if (t < walk.end) {
-    fetch(t, 0, note, masked);
-    note.keep(notes[ALONE ? wave : 0], tid, TERMS & kDistance);
-  }
+  if (t < walk.end) fetch(t, 0, masked);
   for (int buffer = 0; t < walk.end; buffer ^= ALONE ? 0 : 1) {
     // the tile has arrived, and (with a barrier) every wave has read what the next one will be written over
     if constexpr (ALONE) asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
     const int following = walk.skip(p.rows, ALONE ? 3 : 0);
     bool next_masked = false;
-    if (!ALONE && following < walk.end) fetch(following, buffer ^ 1, note, next_masked);
+    if (!ALONE && following < walk.end) fetch(following, buffer ^ 1, next_masked);
     const char* qt = lds + (ALONE ? wave : buffer) * 2 * R::kBytes;
     const char* gt = qt + R::kBytes;
     if (busy) {
-      const RowNotes<BN>& n = notes[ALONE ? wave : buffer];
+      const RowNotes& n = notes[ALONE ? wave : buffer];
 #pragma unroll kTogether
       for (int rb = 0; rb < R::kBlocks; ++rb) {
         f32x16 s[1], dp[1];
@@ -150,7 +143,7 @@ __global__ __launch_bounds__(kAttnThreads, (sizeof(T) == 4 && D > 32 ? 1 : 2)) v
             const int r = 32 * rb + 16 * (i >> 3) + 8 * half + (i & 7);
             float bend, distance, z;
             if constexpr (TERMS == 0) z = __builtin_fmaf(s[0][i], factor, -n.lse[r]);
-            else if constexpr (TERMS & kDistance) z = score<TERMS, near>(s[0][i], factor, cap, n.x[r] - own_x, n.y[r] - own_y, n.slope[r], bend, distance) - n.lse[r];
+            else if constexpr (TERMS & kDistance) z = score<TERMS, near>(s[0][i], factor, cap, n.x[r] - own_x, n.y[r] - own_y, n.slope[r] * kLog2e, bend, distance) - n.lse[r];
             else z = score<TERMS, near>(s[0][i], factor, cap, 0.f, 0.f, 0.f, bend, distance) - n.lse[r];
             float pr = __builtin_amdgcn_exp2f(z), ds = pr * (dp[0][i] - n.sum[r]);
             if constexpr (TERMS & kCap) ds *= __builtin_fmaf(-bend, bend, 1.f);
@@ -179,12 +172,9 @@ __global__ __launch_bounds__(kAttnThreads, (sizeof(T) == 4 && D > 32 ? 1 : 2)) v
         column_products<D, 1>(qt, rb, {&ws}, {dk}, lane);
       }
     }
-    if (following < walk.end) {
-      if constexpr (ALONE) {
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (the tile has been read)
-        fetch(following, buffer, note, next_masked);
-      }
-      note.keep(notes[ALONE ? wave : buffer ^ 1], tid, TERMS & kDistance);
+    if (ALONE && following < walk.end) {
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (the tile has been read)
+      fetch(following, buffer, next_masked);
     }
     t = following;
     masked = next_masked;

@@ -52,9 +52,10 @@ struct AttnParams {
   float* lse_out;
   float* part;      // [splits][B,Nq,H][d + 1], the last one lse; null: no splits
   // backward
-  float* rowsum;    // [B,Nq,H] <dout, out>
-  float* rowrest;   // [row_splits][B,Nq,H] what it lacks of D, or null
-  int row_splits;
+  float* rowsum;    // [B,Hk,rows] D: <dout, out>, and what that lacks
+  float* rowlse;    // [B,Hk,rows] lse in units of log 2; infinity for rows that see no key or are padding: their p is 0
+  bool puts_right;  // (attn_bwd.hip)
+  float* rowrest;   // [splits][B,Hk,rows] what <dout, out> lacks of D, with splits
   float* rowslope;  // [splits][3][H][B,Nq] parts of dslope, or null
   float* part_v;    // (part: dq, or dk: [splits][...][d]; part_v: what D's rest takes from dq, or dv)
   float grad_scale; // scale, sign and all
@@ -195,6 +196,11 @@ struct Fixed {
       const int at = (2 * s + half) * 16;
       if (there && at < row_bytes) __builtin_memcpy(&x[s], row + at, 16);
     }
+  }
+  // Waits for them.  (The compiler would wait where they are first used, inside the loop, in every turn of it, and so for the next tile.)
+  __device__ __forceinline__ void arrive() {
+#pragma unroll
+    for (int s = 0; s < R::kSteps; ++s) asm volatile("" : "+v"(x[s].x));
   }
 };
 
@@ -433,39 +439,41 @@ __device__ __forceinline__ Row own_row(const AttnParams& p, int b, int hk, int r
   return w;
 }
 
-// Of a tile's keys: places and images (-2: padding, or behind the last key).
-template <int BN>
+__device__ __forceinline__ void arrive(float& x) { asm volatile("" : "+v"(x)); }
+__device__ __forceinline__ void arrive(int& x) { asm volatile("" : "+v"(x)); }
+__device__ __forceinline__ void arrive(Row& w) {
+  arrive(w.x);
+  arrive(w.y);
+  arrive(w.slope);
+  arrive(w.doc);
+}
+
+// Tokens of a tile: places and images, as they are in memory (zeros behind the last one).  They come by loads that the compiler does not
+// see, like the tile: behind a load that it sees it would wait for everything on its way, the next tile too, before it uses anything.
 struct KeyNotes {
-  float x[BN], y[BN];
-  int doc[BN];
+  float x[64], y[64];
+  int doc[64];
 };
-template <int BN>
-struct KeyNote {
-  float x, y;
-  int doc;
-  __device__ __forceinline__ void fetch(const AttnParams& p, int b, int k0, int tid) {
-    const int j = k0 + tid;
-    x = y = 0.f;
-    doc = -2;
-    if (tid < BN && j < p.Nk) {
-      const size_t token = (size_t)b * p.Nk + j;
-      doc = 0;
-      if (p.k_doc) {
-        doc = p.k_doc[token];
-        if (doc < 0) doc = -2;
-      }
-      if (p.slope && doc >= 0) {  // (padding may have any place, none at all too)
-        const float2 xy = reinterpret_cast<const float2*>(p.k_xy)[token];
-        x = xy.x;
-        y = xy.y;
-      }
-    }
+struct KeySource {
+  i32x4 xy, doc;
+  int rows;
+  __device__ __forceinline__ KeySource(const AttnParams& p, int b, bool places, bool images) : rows(p.Nk) {
+    if (places) xy = uniform(buffer_of((const char*)(p.k_xy + 2 * (size_t)b * p.Nk), 8ll * p.Nk));
+    if (images) doc = uniform(buffer_of((const char*)(p.k_doc + (size_t)b * p.Nk), 4ll * p.Nk));
   }
-  __device__ __forceinline__ void keep(KeyNotes<BN>& n, int tid) const {
-    if (tid < BN) {
-      n.x[tid] = x;
-      n.y[tid] = y;
-      n.doc[tid] = doc;
+  // by one wave, or by waves 0 (places) and 1 (images) of a workgroup
+  template <int TERMS, bool DOCS, bool ALONE, int BN>
+  __device__ __forceinline__ void load(KeyNotes& n, int k0, int wave, int lane) const {
+    const int j = k0 + lane;
+    if (lane < BN) {
+      if constexpr (TERMS & kDistance)
+        if (ALONE || wave == 0) {
+          const uint32_t at = j < rows ? (uint32_t)j * 8u : kNowhere;
+          lds_load<4>(lds_at(n.x), xy, at);
+          lds_load<4>(lds_at(n.y), xy, at + 4);
+        }
+      if constexpr (DOCS)
+        if (ALONE || wave == 1) lds_load<4>(lds_at(n.doc), doc, j < rows ? (uint32_t)j * 4u : kNowhere);
     }
   }
 };

@@ -36,18 +36,18 @@ __device__ __forceinline__ void join_waves(char* lds, int wave, int lane, f32x16
   l = sum;
 }
 
-template <typename T, int D, int TERMS, bool ALONE, int NB>
+template <typename T, int D, int TERMS, bool DOCS, bool ALONE>
 __global__ __launch_bounds__(kAttnThreads, (kAttnWaves<T, D>)) void attn_fwd_kernel(AttnParams p) {
   using R = TileRows<T, D, ALONE>;
-  constexpr int BN = R::BN;
+  constexpr int BN = R::BN, NB = 1;
   extern __shared__ __align__(16) char lds[];
-  __shared__ KeyNotes<BN> notes[ALONE ? 4 : 2];
+  __shared__ KeyNotes notes[ALONE ? 4 : 2];
   const int work = xcd_contiguous_block(blockIdx.x, gridDim.x);
   if (work >= p.work) return;
   const int group = exact_div(work, p.blocks, p.blocks_magic), block = work - group * p.blocks;  // group: (split, image, key head)
   const int split = group / (p.B * p.Hk), bh = group - split * p.B * p.Hk, b = bh / p.Hk, hk = bh - b * p.Hk;
   const int lane = threadIdx.x & 63, half = lane >> 5;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), tid = ALONE ? lane : (int)threadIdx.x;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   constexpr int kRows = ALONE ? 32 : kAttnRows * NB;
   const int block0 = block * kRows, r0 = ALONE ? block0 : block0 + wave * 32 * NB;
   const bool busy = r0 < p.rows;
@@ -71,52 +71,55 @@ __global__ __launch_bounds__(kAttnThreads, (kAttnWaves<T, D>)) void attn_fwd_ker
   walk.mixed = false;
   walk.end = min(tiles, (split + 1) * p.split_tiles);
   walk.tile_rows = BN; walk.G = 1; walk.g_magic = 0u;
-  if (p.q_doc) {
+  if constexpr (DOCS) {
     walk.spans = p.k_span + (size_t)b * ((p.Nk + kSpan - 1) / kSpan);
     walk.own(p.q_span + (size_t)b * ((p.Nq + kSpan - 1) / kSpan), exact_div(block0, p.G, p.g_magic), exact_div(min(block0 + kRows, p.rows) - 1, p.G, p.g_magic));
   }
   walk.start(split * p.split_tiles);
 
-  const auto fetch = [&](int t, int buffer, KeyNote<BN>& note, bool& masked) __attribute__((always_inline)) {
+  const KeySource about(p, b, TERMS & kDistance, DOCS);
+  const auto fetch = [&](int t, int buffer, bool& masked) __attribute__((always_inline)) {
     char* dst = lds + (ALONE ? wave : buffer) * 2 * R::kBytes;
     bool pads = false;
     masked = t * BN + BN > p.Nk;
-    if (walk.spans) {
+    if constexpr (DOCS) {
       const Span x = walk.of(t, p.Nk);
       pads = __builtin_amdgcn_readfirstlane(x.pad);
       masked = masked || walk.mixed || pads || __builtin_amdgcn_readfirstlane(x.lo) != walk.lo || __builtin_amdgcn_readfirstlane(x.hi) != walk.lo;
     }
     keys.template load<ALONE>(dst, t * BN, pads);
     values.template load<ALONE>(dst + R::kBytes, t * BN, pads);
-    if (masked || (TERMS & kDistance)) note.fetch(p, b, t * BN, tid);
+    about.load<TERMS, DOCS, ALONE, BN>(notes[ALONE ? wave : buffer], t * BN, wave, lane);
   };
 
+#pragma unroll
+  for (int n = 0; n < NB; ++n) {
+    q[n].arrive();
+    arrive(own[n]);
+  }
   f32x16 o[NB][D / 32] = {};
   float m[NB], l[NB];
 #pragma unroll
   for (int n = 0; n < NB; ++n) m[n] = -__builtin_inff(), l[n] = 0.f;
-  KeyNote<BN> note = {};
   bool masked = false;
   int t = walk.skip(p.Nk, ALONE ? wave : 0);
-  if (t < walk.end) {
-    fetch(t, 0, note, masked);
-    note.keep(notes[ALONE ? wave : 0], tid);
-  }
+  if (t < walk.end) fetch(t, 0, masked);
   for (int buffer = 0; t < walk.end; buffer ^= ALONE ? 0 : 1) {
     // the tile has arrived, and (with a barrier) every wave has read what the next one will be written over
     if constexpr (ALONE) asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
     const int following = walk.skip(p.Nk, ALONE ? 3 : 0);
     bool next_masked = false;
-    if (!ALONE && following < walk.end) fetch(following, buffer ^ 1, note, next_masked);
+    if (!ALONE && following < walk.end) fetch(following, buffer ^ 1, next_masked);
     const char* kt = lds + (ALONE ? wave : buffer) * 2 * R::kBytes;
     const char* vt = kt + R::kBytes;
     if (busy) {
       f32x16 s[R::kBlocks][NB];
 #pragma unroll
       for (int kb = 0; kb < R::kBlocks; ++kb) row_products<T, D, NB>(kt, kb, q, s[kb], lane);
-      const KeyNotes<BN>& notes_ = notes[ALONE ? wave : buffer];
+      const KeyNotes& notes_ = notes[ALONE ? wave : buffer];
       const bool plain = !TERMS && !masked;
+      const int left = p.Nk - t * BN - 8 * half;  // keys of the tile that are there, from the lane's first one on
       const float times = plain ? factor : 1.f;
 #pragma unroll
       for (int n = 0; n < NB; ++n) {
@@ -130,7 +133,7 @@ __global__ __launch_bounds__(kAttnThreads, (kAttnWaves<T, D>)) void attn_fwd_ker
               float bend, distance, z;
               if constexpr (TERMS & kDistance) z = score<TERMS, near>(s[kb][n][i], factor, cap, own[n].x - notes_.x[j], own[n].y - notes_.y[j], own[n].slope, bend, distance);
               else z = score<TERMS, near>(s[kb][n][i], factor, cap, 0.f, 0.f, 0.f, bend, distance);
-              if constexpr (hides) z = notes_.doc[j] != own[n].doc ? -__builtin_inff() : z;
+              if constexpr (hides) z = j - 8 * half >= left || (DOCS && notes_.doc[j] != own[n].doc) ? -__builtin_inff() : z;
               s[kb][n][i] = z;
               top = fmaxf(top, z);
             }
@@ -187,12 +190,9 @@ __global__ __launch_bounds__(kAttnThreads, (kAttnWaves<T, D>)) void attn_fwd_ker
         }
       }
     }
-    if (following < walk.end) {
-      if constexpr (ALONE) {
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (the tile has been read)
-        fetch(following, buffer, note, next_masked);
-      }
-      note.keep(notes[ALONE ? wave : buffer ^ 1], tid);
+    if (ALONE && following < walk.end) {
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (the tile has been read)
+      fetch(following, buffer, next_masked);
     }
     t = following;
     masked = next_masked;
@@ -202,9 +202,10 @@ __global__ __launch_bounds__(kAttnThreads, (kAttnWaves<T, D>)) void attn_fwd_ker
   if (!busy) return;
 #pragma unroll
   for (int n = 0; n < NB; ++n) {
-    const float sum = ALONE ? l[n] : other_half_sum(l[n]);
-    const float part = sum > 0.f ? 1.f / sum : (sum == sum ? 0.f : sum);  // (no key: zeros; a NaN stays one)
-    const float lse = sum > 0.f ? __builtin_fmaf(m[n], kLn2, __logf(sum)) : (sum == sum ? -__builtin_inff() : sum);
+    const float seen = ALONE ? l[n] : other_half_sum(l[n]), sum = DOCS && own[n].doc < 0 ? 0.f : seen;
+    const bool none = sum == 0.f;  // (a NaN stays one)
+    const float part = 1.f / sum;
+    const float lse = none ? -__builtin_inff() : __builtin_fmaf(m[n], kLn2, __logf(sum));
     if (!own[n].there) continue;
     const size_t all = (size_t)p.B * p.Nq * p.H;
 #pragma unroll
@@ -215,7 +216,7 @@ __global__ __launch_bounds__(kAttnThreads, (kAttnWaves<T, D>)) void attn_fwd_ker
         if (ch < p.d && (!ALONE || g == wave)) {
           float v[4];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) v[e] = o[n][db][4 * g + e] * part;
+          for (int e = 0; e < 4; ++e) v[e] = none ? 0.f : o[n][db][4 * g + e] * part;
           if (p.part) store_piece<4>(p.part + ((size_t)split * all + own[n].at) * p.d + ch, v);
           else store_piece<4>((T*)p.o + own[n].at * p.d + ch, v);
         }
@@ -312,18 +313,18 @@ Plan plan(int B, int Nq, int Nk, int H, int Hk, int D, int el) {
 }
 int width(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : 128; }
 
-template <typename T, int D, int TERMS, bool ALONE>
+template <typename T, int D, int TERMS, bool DOCS, bool ALONE>
 hipError_t launch_kernel(const AttnParams& p, hipStream_t stream) {
-  constexpr int NB = 1;
   const size_t lds = (ALONE ? 8 : 4) * TileRows<T, D, ALONE>::kBytes;
-  const hipError_t e = hipFuncSetAttribute((const void*)attn_fwd_kernel<T, D, TERMS, ALONE, NB>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+  const hipError_t e = hipFuncSetAttribute((const void*)attn_fwd_kernel<T, D, TERMS, DOCS, ALONE>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
   if (e != hipSuccess) return e;
-  AFFMAE_LAUNCH("attn_fwd_kernel", stream, (attn_fwd_kernel<T, D, TERMS, ALONE, NB>), dim3((p.work + 7) / 8 * 8), dim3(kAttnThreads), lds, stream, p);
+  AFFMAE_LAUNCH("attn_fwd_kernel", stream, (attn_fwd_kernel<T, D, TERMS, DOCS, ALONE>), dim3((p.work + 7) / 8 * 8), dim3(kAttnThreads), lds, stream, p);
   return hipGetLastError();
 }
 template <typename T, int D, int TERMS>
 hipError_t launch(const AttnParams& p, hipStream_t stream) {
-  const hipError_t e = p.alone ? launch_kernel<T, D, TERMS, true>(p, stream) : launch_kernel<T, D, TERMS, false>(p, stream);
+  const hipError_t e = p.q_doc ? (p.alone ? launch_kernel<T, D, TERMS, true, true>(p, stream) : launch_kernel<T, D, TERMS, true, false>(p, stream))
+                               : (p.alone ? launch_kernel<T, D, TERMS, false, true>(p, stream) : launch_kernel<T, D, TERMS, false, false>(p, stream));
   if (e != hipSuccess || !p.part) return e;
   const size_t all = (size_t)p.B * p.Nq * p.H;
   const int lanes = std::min(p.splits, 256 / (p.d / 4)), rows = 256 / (lanes * (p.d / 4));
