@@ -51,7 +51,6 @@ __global__ __launch_bounds__(kAttnThreads, (kAttnWaves<T, D>)) void attn_bwd_que
   sum = other_half_sum(sum);
   const float seen = own.there ? p.lse[own.at] : 0.f;
   float lse = seen == -__builtin_inff() ? __builtin_inff() : seen * kLog2e;  // (no key: every p is 0)
-  const float factor = TERMS & kCap ? p.scale / p.cap : p.scale * kLog2e, cap = p.cap * kLog2e;
 
   const int tiles = (p.Nk + BN - 1) / BN;
   Walk walk;
@@ -111,10 +110,9 @@ __global__ __launch_bounds__(kAttnThreads, (kAttnWaves<T, D>)) void attn_bwd_que
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
             const int j = 32 * kb + 16 * (i >> 3) + 8 * half + (i & 7);
-            float bend, distance, z;
-            if constexpr (TERMS == 0) z = __builtin_fmaf(s[0][i], factor, -lse);
-            else if constexpr (TERMS & kDistance) z = score<TERMS, near>(s[0][i], factor, cap, own.x - n.x[j], own.y - n.y[j], own.slope, bend, distance) - lse;
-            else z = score<TERMS, near>(s[0][i], factor, cap, 0.f, 0.f, 0.f, bend, distance) - lse;
+            float bend, distance, dx = 0.f, dy = 0.f;
+            if constexpr (TERMS & kDistance) dx = own.x - n.x[j], dy = own.y - n.y[j];
+            const float z = score<T, TERMS, near>(s[0][i], p, dx, dy, own.slope, lse, bend, distance);
             float pr = __builtin_amdgcn_exp2f(z), dz = pr * (dp[0][i] - sum);
             if constexpr (hides) {
               const bool off = j - 8 * half >= left || (DOCS && n.doc[j] != own.doc);
@@ -128,7 +126,7 @@ __global__ __launch_bounds__(kAttnThreads, (kAttnWaves<T, D>)) void attn_bwd_que
               distances = __builtin_fmaf(pr, distance, distances);
             }
             if constexpr (TERMS & kCap) {
-              const float bends = __builtin_fmaf(-bend, bend, 1.f);
+              const float bends = bend_slope(bend, p);
               dz *= bends;
               if constexpr (REST) pr *= bends;
             }
@@ -139,7 +137,7 @@ __global__ __launch_bounds__(kAttnThreads, (kAttnWaves<T, D>)) void attn_bwd_que
         using yes = std::true_type;
         using no = std::false_type;
         bool near = false;
-        if constexpr ((TERMS & kCap) && D < 128) near = all_near(s[0], factor);
+        if constexpr ((TERMS & kCap) && D < 128) near = all_near(s[0], p.near);
         // keys that are not there have zeros for vectors, so that they add nothing to dq: without sums over p and dZ nothing is hidden
         constexpr bool kHides = REST || (TERMS & kDistance) || DOCS;
         if (kHides && (masked || D == 128)) {  // (one way through where two would not fit the registers)

@@ -83,7 +83,6 @@ __global__ __launch_bounds__(kAttnThreads, (sizeof(T) == 4 && D > 32 ? 1 : 2)) v
 #pragma unroll
     for (int s = 0; s < R::kSteps; ++s) k[0].x[s].negate();
   }
-  const float factor = TERMS & kCap ? p.scale / p.cap : p.scale * kLog2e, cap = p.cap * kLog2e;
 
   const int tiles = (p.rows + BN - 1) / BN;
   Walk walk;
@@ -141,12 +140,11 @@ __global__ __launch_bounds__(kAttnThreads, (sizeof(T) == 4 && D > 32 ? 1 : 2)) v
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
             const int r = 32 * rb + 16 * (i >> 3) + 8 * half + (i & 7);
-            float bend, distance, z;
-            if constexpr (TERMS == 0) z = __builtin_fmaf(s[0][i], factor, -n.lse[r]);
-            else if constexpr (TERMS & kDistance) z = score<TERMS, near>(s[0][i], factor, cap, n.x[r] - own_x, n.y[r] - own_y, n.slope[r] * kLog2e, bend, distance) - n.lse[r];
-            else z = score<TERMS, near>(s[0][i], factor, cap, 0.f, 0.f, 0.f, bend, distance) - n.lse[r];
+            float bend, distance, dx = 0.f, dy = 0.f, slope = 0.f;
+            if constexpr (TERMS & kDistance) dx = n.x[r] - own_x, dy = n.y[r] - own_y, slope = n.slope[r] * kLog2e;
+            const float z = score<T, TERMS, near>(s[0][i], p, dx, dy, slope, n.lse[r], bend, distance);
             float pr = __builtin_amdgcn_exp2f(z), ds = pr * (dp[0][i] - n.sum[r]);
-            if constexpr (TERMS & kCap) ds *= __builtin_fmaf(-bend, bend, 1.f);
+            if constexpr (TERMS & kCap) ds *= bend_slope(bend, p);
             if constexpr (hides) {
               const bool off = n.doc[r] != own_doc;
               pr = off ? 0.f : pr;
@@ -159,7 +157,7 @@ __global__ __launch_bounds__(kAttnThreads, (sizeof(T) == 4 && D > 32 ? 1 : 2)) v
         using yes = std::true_type;
         using no = std::false_type;
         bool near = false;
-        if constexpr ((TERMS & kCap) && D < 128) near = all_near(s[0], factor);
+        if constexpr ((TERMS & kCap) && D < 128) near = all_near(s[0], p.near);
         if (DOCS && (D == 128 || masked)) {  // (one way through where two would not fit the registers)
           if (near) slopes(yes{}, yes{});
           else slopes(no{}, yes{});

@@ -43,6 +43,9 @@ struct AttnParams {
   float scale;   // at least 0: a negative one is taken off the queries
   bool negate;
   float cap;
+  float factor;             // scale / cap, without a cap scale log2 e
+  float cap2, cap2_inv;     // cap log2 e
+  float near, bend[6];      // products below `near` are bent by s q(s^2)
   // workgroups: `blocks` of rows (or keys), `splits` of the other side, `split_tiles` tiles each
   int blocks, splits, split_tiles, work;
   bool alone;
@@ -278,45 +281,53 @@ __device__ __forceinline__ void column_products(const char* tile, int block, con
 
 // Terms of the scores that a kernel is built for.
 enum { kCap = 1, kDistance = 2 };
+// tanh x up to |x| = kNear is x times a polynomial of x^2, fitted by least squares to a relative error of 5e-8 (2e-9 for fp32 tensors), beyond
+// it 1 - 2 / (exp(2 x) + 1), of which the 1 is most there (near 0 it would leave an error of 1e-7, times the cap).  Caps are many
+// times the usual score, so that as a rule no lane of a wave is beyond: then cap tanh(scale s / cap) log2 e is s q(s^2) with the constants
+// in q's coefficients, and the second form is not worked out.
 constexpr float kNear = 0.55f;
-// tanh: up to kNear x times a polynomial of x^2, fitted by least squares to a relative error of 3e-9, beyond it 1 - 2 / (exp(2 x) + 1), of
-// which the 1 is most there (near 0 it would leave an error of 1e-7, times the cap).  NEAR: no lane of the wave is beyond, as
-// in most calls, whose caps are many times the usual score: six operations instead of twelve, two of them slow.
-template <bool NEAR>
-__device__ __forceinline__ float bent(float x) {
-  const float z = x * x;
-  float s = __builtin_fmaf(z, -0.0062211f, 0.02103814f);
-  s = __builtin_fmaf(z, s, -0.05384533f);
-  s = __builtin_fmaf(z, s, 0.13332534f);
-  s = __builtin_fmaf(z, s, -0.33333316f);
-  s = __builtin_fmaf(x * z, s, x);
-  if constexpr (NEAR) return s;
-  const float far = 1.f - 2.f * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * (2.f * kLog2e)));
-  return fabsf(x) < kNear ? s : far;
+constexpr double kBend16[5] = {-0.33332926, 0.13320038, -0.05261931, 0.01632615, 0.0};
+constexpr double kBend32[5] = {-0.33333316, 0.13332534, -0.05384533, 0.02103814, -0.0062211};
+template <typename T>
+__device__ __forceinline__ float bent_near(float s, const float (&q)[6]) {  // q(s^2)
+  const float t = s * s;
+  float c = sizeof(T) == 4 ? __builtin_fmaf(t, q[5], q[4]) : q[4];
+  c = __builtin_fmaf(t, c, q[3]);
+  c = __builtin_fmaf(t, c, q[2]);
+  c = __builtin_fmaf(t, c, q[1]);
+  return __builtin_fmaf(t, c, q[0]);
 }
-// no lane has a product beyond kNear of the cap
-__device__ __forceinline__ bool all_near(const f32x16& s, float factor) {
+// no lane has a product of `limit` or more
+__device__ __forceinline__ bool all_near(const f32x16& s, float limit) {
   float top = 0.f;
 #pragma unroll
   for (int i = 0; i < 16; ++i) top = fmaxf(top, fabsf(s[i]));
-  return !__any(!(top * factor < kNear));
+  return !__any(!(top < limit));
 }
-// Score in units of log 2 from a product s.  factor: scale / cap, or without a cap scale log2 e; cap and slope in units of log 2.  bend is
-// tanh, distance |x_i - y_j|.
-template <int TERMS, bool NEAR>
-__device__ __forceinline__ float score(float s, float factor, float cap, float dx, float dy, float slope, float& bend, float& distance) {
-  float z;
-  if constexpr (TERMS & kCap) {
-    bend = bent<NEAR>(s * factor);
-    z = bend * cap;
-  } else {
-    z = s * factor;
-  }
+// Score in units of log 2 from a product s, less `from`; bend: the part of it that the cap bends (NEAR: no lane of the wave is beyond).
+template <typename T, int TERMS, bool NEAR>
+__device__ __forceinline__ float score(float s, const AttnParams& p, float dx, float dy, float slope, float from, float& bend, float& distance) {
+  float rest = -from;
   if constexpr (TERMS & kDistance) {
     distance = __builtin_amdgcn_sqrtf(__builtin_fmaf(dx, dx, dy * dy));
-    z = __builtin_fmaf(-slope, distance, z);
+    rest = __builtin_fmaf(-slope, distance, rest);
   }
-  return z;
+  if constexpr (!(TERMS & kCap)) return __builtin_fmaf(s, p.factor, rest);
+  const float near = bent_near<T>(s, p.bend);
+  if constexpr (NEAR) {
+    bend = s * near;
+    return __builtin_fmaf(s, near, rest);
+  } else {
+    const float x = s * p.factor;  // scale / cap
+    const float far = p.cap2 - 2.f * p.cap2 * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * (2.f * kLog2e)));
+    bend = fabsf(s) < p.near ? s * near : far;
+    return bend + rest;
+  }
+}
+// 1 - tanh^2, from the bent score
+__device__ __forceinline__ float bend_slope(float bend, const AttnParams& p) {
+  const float t = bend * p.cap2_inv;
+  return __builtin_fmaf(-t, t, 1.f);
 }
 
 __device__ __forceinline__ float other_half_max(float x) { return fmaxf(x, __uint_as_float(lane_xor_u32<32>(__float_as_uint(x), threadIdx.x & 63))); }

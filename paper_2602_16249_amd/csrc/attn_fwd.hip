@@ -37,7 +37,7 @@ __device__ __forceinline__ void join_waves(char* lds, int wave, int lane, f32x16
 }
 
 template <typename T, int D, int TERMS, bool DOCS, bool ALONE>
-__global__ __launch_bounds__(kAttnThreads, (kAttnWaves<T, D>)) void attn_fwd_kernel(AttnParams p) {
+__global__ __launch_bounds__(kAttnThreads, (sizeof(T) == 4 ? kAttnWaves<T, D> : D == 32 ? 4 : D == 64 ? 3 : 2)) void attn_fwd_kernel(AttnParams p) {
   using R = TileRows<T, D, ALONE>;
   constexpr int BN = R::BN, NB = 1;
   extern __shared__ __align__(16) char lds[];
@@ -63,7 +63,6 @@ __global__ __launch_bounds__(kAttnThreads, (kAttnWaves<T, D>)) void attn_fwd_ker
       for (int s = 0; s < R::kSteps; ++s) q[n].x[s].negate();
     }
   }
-  const float factor = TERMS & kCap ? p.scale / p.cap : p.scale * kLog2e, cap = p.cap * kLog2e;
 
   const int tiles = (p.Nk + BN - 1) / BN;
   Walk walk;
@@ -98,9 +97,11 @@ __global__ __launch_bounds__(kAttnThreads, (kAttnWaves<T, D>)) void attn_fwd_ker
     arrive(own[n]);
   }
   f32x16 o[NB][D / 32] = {};
-  float m[NB], l[NB];
-#pragma unroll
-  for (int n = 0; n < NB; ++n) m[n] = -__builtin_inff(), l[n] = 0.f;
+  // The exponentials are taken from a score of the row that lies within 2^12 of the largest one (in p) so far: m.  It is found in the row's
+  // first tile, and again where the sum over a tile says that a score lies above it, which hardly ever happens: floating
+  // values lose nothing by being larger than 1, and the maximum of every tile took a tenth of the vector instructions.
+  float m = -__builtin_inff(), l = 0.f;
+  if (DOCS && own[0].doc < 0) m = 0.f;  // (padding: nothing to find)
   bool masked = false;
   int t = walk.skip(p.Nk, ALONE ? wave : 0);
   if (t < walk.end) fetch(t, 0, masked);
@@ -114,80 +115,93 @@ __global__ __launch_bounds__(kAttnThreads, (kAttnWaves<T, D>)) void attn_fwd_ker
     const char* kt = lds + (ALONE ? wave : buffer) * 2 * R::kBytes;
     const char* vt = kt + R::kBytes;
     if (busy) {
-      f32x16 s[R::kBlocks][NB];
+      f32x16 s[R::kBlocks][1];
 #pragma unroll
-      for (int kb = 0; kb < R::kBlocks; ++kb) row_products<T, D, NB>(kt, kb, q, s[kb], lane);
-      const KeyNotes& notes_ = notes[ALONE ? wave : buffer];
-      const bool plain = !TERMS && !masked;
+      for (int kb = 0; kb < R::kBlocks; ++kb) row_products<T, D, 1>(kt, kb, q, s[kb], lane);
+      const KeyNotes& about_key = notes[ALONE ? wave : buffer];
       const int left = p.Nk - t * BN - 8 * half;  // keys of the tile that are there, from the lane's first one on
-      const float times = plain ? factor : 1.f;
-#pragma unroll
-      for (int n = 0; n < NB; ++n) {
-        float top = -__builtin_inff();
-        const auto scores = [&](auto near, auto hides) __attribute__((always_inline)) {
-#pragma unroll
-          for (int kb = 0; kb < R::kBlocks; ++kb)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              const int j = 32 * kb + 16 * (i >> 3) + 8 * half + (i & 7);
-              float bend, distance, z;
-              if constexpr (TERMS & kDistance) z = score<TERMS, near>(s[kb][n][i], factor, cap, own[n].x - notes_.x[j], own[n].y - notes_.y[j], own[n].slope, bend, distance);
-              else z = score<TERMS, near>(s[kb][n][i], factor, cap, 0.f, 0.f, 0.f, bend, distance);
-              if constexpr (hides) z = j - 8 * half >= left || (DOCS && notes_.doc[j] != own[n].doc) ? -__builtin_inff() : z;
-              s[kb][n][i] = z;
-              top = fmaxf(top, z);
-            }
-        };
-        using yes = std::true_type;
-        using no = std::false_type;
-        if (plain) {
-#pragma unroll
-          for (int kb = 0; kb < R::kBlocks; ++kb)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) top = fmaxf(top, s[kb][n][i]);
-          top *= factor;
-        } else {
-          bool near = false;
-          if constexpr (TERMS & kCap) {
-            near = true;
-#pragma unroll
-            for (int kb = 0; kb < R::kBlocks; ++kb) near = near && all_near(s[kb][n], factor);
-          }
-          if (masked) {
-            if (near) scores(yes{}, yes{});
-            else scores(no{}, yes{});
-          } else {
-            if (near) scores(yes{}, no{});
-            else scores(no{}, no{});
-          }
-        }
-        top = other_half_max(top);
-        if (__any(top > m[n])) {
-          const float before = m[n];
-          m[n] = fmaxf(m[n], top);
-          const float shrink = m[n] == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f(before - m[n]);
-          l[n] *= shrink;
-#pragma unroll
-          for (int db = 0; db < D / 32; ++db) o[n][db] *= shrink;
-        }
-        const float from = m[n] == -__builtin_inff() ? 0.f : m[n];
+      // s becomes score - from, hidden ones -infinity
+      const auto scores = [&](auto near, auto hides, float from) __attribute__((always_inline)) {
 #pragma unroll
         for (int kb = 0; kb < R::kBlocks; ++kb)
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
-            s[kb][n][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kb][n][i], times, -from));
-            l[n] += s[kb][n][i];
+            const int j = 32 * kb + 16 * (i >> 3) + 8 * half + (i & 7);
+            float bend, distance, dx = 0.f, dy = 0.f;
+            if constexpr (TERMS & kDistance) dx = own[0].x - about_key.x[j], dy = own[0].y - about_key.y[j];
+            float z = score<T, TERMS, near>(s[kb][0][i], p, dx, dy, own[0].slope, from, bend, distance);
+            if constexpr (hides) z = j - 8 * half >= left || (DOCS && about_key.doc[j] != own[0].doc) ? -__builtin_inff() : z;
+            s[kb][0][i] = z;
           }
+      };
+      const auto exponentials = [&]() __attribute__((always_inline)) {
+        float sum = 0.f;
+#pragma unroll
+        for (int kb = 0; kb < R::kBlocks; ++kb)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            s[kb][0][i] = __builtin_amdgcn_exp2f(s[kb][0][i]);
+            sum += s[kb][0][i];
+          }
+        return sum;
+      };
+      using yes = std::true_type;
+      using no = std::false_type;
+      const auto is_near = [&]() __attribute__((always_inline)) {
+        bool near = true;
+#pragma unroll
+        for (int kb = 0; kb < R::kBlocks; ++kb) near = near && all_near(s[kb][0], p.near);
+        return near;
+      };
+      bool search = masked || __any(m == -__builtin_inff()), near = false;
+      if constexpr (TERMS & kCap) {
+        near = is_near();
+        search = search || !near;
+      }
+      if (!search) {
+        scores(yes{}, no{}, m);
+        const float sum = exponentials();
+        search = __any(!(sum < 4096.f));
+        if (search) {
+#pragma unroll
+          for (int kb = 0; kb < R::kBlocks; ++kb) row_products<T, D, 1>(kt, kb, q, s[kb], lane);
+        } else {
+          l += sum;
+        }
+      }
+      if (search) {
+        if (masked) {
+          if (near) scores(yes{}, yes{}, 0.f);
+          else scores(no{}, yes{}, 0.f);
+        } else {
+          if (near) scores(yes{}, no{}, 0.f);
+          else scores(no{}, no{}, 0.f);
+        }
+        float top = -__builtin_inff();
+#pragma unroll
+        for (int kb = 0; kb < R::kBlocks; ++kb)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) top = fmaxf(top, s[kb][0][i]);
+        top = other_half_max(top);
+        if (__any(top > m)) {
+          const float before = m;
+          m = fmaxf(m, top);
+          const float shrink = m == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f(before - m);
+          l *= shrink;
+#pragma unroll
+          for (int db = 0; db < D / 32; ++db) o[0][db] *= shrink;
+        }
+        const float from = m == -__builtin_inff() ? 0.f : m;
+#pragma unroll
+        for (int kb = 0; kb < R::kBlocks; ++kb)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s[kb][0][i] -= from;
+        l += exponentials();
       }
 #pragma unroll
       for (int kb = 0; kb < R::kBlocks; ++kb) {
-        if constexpr (NB == 1) {
-          const Weights<T> w(s[kb][0]);
-          column_products<D, 1>(vt, kb, {&w}, {o[0]}, lane);
-        } else {
-          const Weights<T> w0(s[kb][0]), w1(s[kb][1]);
-          column_products<D, 2>(vt, kb, {&w0, &w1}, {o[0], o[1]}, lane);
-        }
+        const Weights<T> w(s[kb][0]);
+        column_products<D, 1>(vt, kb, {&w}, {o[0]}, lane);
       }
     }
     if (ALONE && following < walk.end) {
@@ -198,14 +212,14 @@ __global__ __launch_bounds__(kAttnThreads, (kAttnWaves<T, D>)) void attn_fwd_ker
     masked = next_masked;
   }
 
-  if constexpr (ALONE) join_waves<D>(lds, wave, lane, o[0], m[0], l[0]);
+  if constexpr (ALONE) join_waves<D>(lds, wave, lane, o[0], m, l);
   if (!busy) return;
 #pragma unroll
   for (int n = 0; n < NB; ++n) {
-    const float seen = ALONE ? l[n] : other_half_sum(l[n]), sum = DOCS && own[n].doc < 0 ? 0.f : seen;
+    const float seen = ALONE ? l : other_half_sum(l), sum = DOCS && own[n].doc < 0 ? 0.f : seen;
     const bool none = sum == 0.f;  // (a NaN stays one)
     const float part = 1.f / sum;
-    const float lse = none ? -__builtin_inff() : __builtin_fmaf(m[n], kLn2, __logf(sum));
+    const float lse = none ? -__builtin_inff() : __builtin_fmaf(m, kLn2, __logf(sum));
     if (!own[n].there) continue;
     const size_t all = (size_t)p.B * p.Nq * p.H;
 #pragma unroll
@@ -361,6 +375,22 @@ AttnParams attn_params(const AttnArgs& a, Span* spans) {
   p.negate = a.scale < 0.f;
   p.scale = p.negate ? -a.scale : a.scale;
   p.cap = a.cap;
+  const double log2e = 1.4426950408889634;
+  p.factor = (float)(a.cap > 0.f ? (double)p.scale / a.cap : p.scale * log2e);
+  if (a.cap > 0.f) {
+    const double f = (double)p.scale / a.cap, c = p.scale * log2e;
+    p.cap2 = (float)(a.cap * log2e);
+    p.cap2_inv = (float)(1.0 / (a.cap * log2e));
+    double power = c;
+    bool fits = true;
+    p.bend[0] = (float)c;
+    for (int k = 0; k < 5; ++k) {
+      power *= f * f;
+      p.bend[k + 1] = (float)(power * (a.dtype == 1 ? kBend16 : kBend32)[k]);
+      fits = fits && power < 1e30;
+    }
+    p.near = fits ? (float)(kNear / std::max(f, 1e-30)) : 0.f;
+  }
   return p;
 }
 
