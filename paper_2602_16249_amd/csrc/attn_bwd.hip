@@ -70,9 +70,8 @@ __global__ __launch_bounds__(kAttnThreads, (kAttnWaves<T, D>)) void attn_bwd_que
     bool pads = false;
     masked = t * BN + BN > p.Nk;
     if constexpr (DOCS) {
-      const Span x = walk.of(t, p.Nk);
-      pads = __builtin_amdgcn_readfirstlane(x.pad);
-      masked = masked || walk.mixed || pads || __builtin_amdgcn_readfirstlane(x.lo) != walk.lo || __builtin_amdgcn_readfirstlane(x.hi) != walk.lo;
+      pads = walk.padded(t);
+      masked = masked || walk.hides(t);
     }
     keys.template load<ALONE>(dst, t * BN, pads);
     values.template load<ALONE>(dst + R::kBytes, t * BN, pads);
@@ -104,8 +103,8 @@ __global__ __launch_bounds__(kAttnThreads, (kAttnWaves<T, D>)) void attn_bwd_que
 #pragma unroll kTogether
       for (int kb = 0; kb < R::kBlocks; ++kb) {
         f32x16 s[1], dp[1];
-        row_products<T, D, 1>(kt, kb, q, s, lane);
-        row_products<T, D, 1>(vt, kb, g, dp, lane);
+        row_products<T, D, 1>(kt, kb, q, s, lane, p.d);
+        row_products<T, D, 1>(vt, kb, g, dp, lane, p.d);
         const auto slopes = [&](auto near, auto hides) __attribute__((always_inline)) {
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
@@ -150,9 +149,9 @@ __global__ __launch_bounds__(kAttnThreads, (kAttnWaves<T, D>)) void attn_bwd_que
         const Weights<T> w(s[0]);
         if constexpr (REST) {
           const Weights<T> wp(dp[0]);
-          column_products<D, 2>(kt, kb, {&w, &wp}, {dq, keys_seen}, lane);
+          column_products<D, 2>(kt, kb, {&w, &wp}, {dq, keys_seen}, lane, p.d);
         } else {
-          column_products<D, 1>(kt, kb, {&w}, {dq}, lane);
+          column_products<D, 1>(kt, kb, {&w}, {dq}, lane, p.d);
         }
       }
     }

@@ -102,9 +102,8 @@ __global__ __launch_bounds__(kAttnThreads, (sizeof(T) == 4 && D > 32 ? 1 : 2)) v
     bool pads = false;
     masked = false;
     if constexpr (DOCS) {
-      const Span x = walk.of(t, p.rows);
-      pads = __builtin_amdgcn_readfirstlane(x.pad);
-      masked = walk.mixed || pads || __builtin_amdgcn_readfirstlane(x.lo) != walk.lo || __builtin_amdgcn_readfirstlane(x.hi) != walk.lo;
+      pads = walk.padded(t);
+      masked = walk.hides(t);
     }
     queries.template load<ALONE>(dst, t * BN, pads);
     douts.template load<ALONE>(dst + R::kBytes, t * BN, pads);
@@ -134,8 +133,8 @@ __global__ __launch_bounds__(kAttnThreads, (sizeof(T) == 4 && D > 32 ? 1 : 2)) v
 #pragma unroll kTogether
       for (int rb = 0; rb < R::kBlocks; ++rb) {
         f32x16 s[1], dp[1];
-        row_products<T, D, 1>(qt, rb, k, s, lane);
-        row_products<T, D, 1>(gt, rb, v, dp, lane);
+        row_products<T, D, 1>(qt, rb, k, s, lane, p.d);
+        row_products<T, D, 1>(gt, rb, v, dp, lane, p.d);
         const auto slopes = [&](auto near, auto hides) __attribute__((always_inline)) {
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
@@ -166,8 +165,8 @@ __global__ __launch_bounds__(kAttnThreads, (sizeof(T) == 4 && D > 32 ? 1 : 2)) v
           else slopes(no{}, no{});
         }
         const Weights<T> wp(s[0]), ws(dp[0]);
-        column_products<D, 1>(gt, rb, {&wp}, {dv}, lane);
-        column_products<D, 1>(qt, rb, {&ws}, {dk}, lane);
+        column_products<D, 1>(gt, rb, {&wp}, {dv}, lane, p.d);
+        column_products<D, 1>(qt, rb, {&ws}, {dk}, lane, p.d);
       }
     }
     if (ALONE && following < walk.end) {

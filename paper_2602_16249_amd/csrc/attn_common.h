@@ -209,7 +209,7 @@ struct Fixed {
 
 // s[n][m] = <row perm(m) of block `block` in LDS, the rows of column block n>
 template <typename T, int D, int NB>
-__device__ __forceinline__ void row_products(const char* tile, int block, const Fixed<T, D> (&fixed)[NB], f32x16 (&s)[NB], int lane) {
+__device__ __forceinline__ void row_products(const char* tile, int block, const Fixed<T, D> (&fixed)[NB], f32x16 (&s)[NB], int lane, int d) {
   using R = TileRows<T, D>;
   const int row = swap23(lane & 31);
   const char* at = tile + block * 32 * R::RB + row * R::RB;
@@ -218,6 +218,7 @@ __device__ __forceinline__ void row_products(const char* tile, int block, const 
   for (int n = 0; n < NB; ++n) s[n] = f32x16{};
 #pragma unroll
   for (int step = 0; step < R::kSteps; ++step) {
+    if (sizeof(T) == 4 && step > 0 && step * 8 >= d) break;  // (256 cycles a step; of bf16 it is 32, less than a branch between the reads costs)
     Piece<T> a;
     __builtin_memcpy(&a, at + (m ^ (step << 5)), 16);
 #pragma unroll
@@ -245,7 +246,7 @@ struct Weights<float> {
 
 // c[j][n][ch] += sum over the block's rows of tile[row][ch] w[j * NB + n][row]: J sets of weights for each of NB column blocks
 template <int D, int M>
-__device__ __forceinline__ void column_products(const char* tile, int block, const Weights<bf16_t>* const (&w)[M], f32x16* const (&c)[M], int lane) {
+__device__ __forceinline__ void column_products(const char* tile, int block, const Weights<bf16_t>* const (&w)[M], f32x16* const (&c)[M], int lane, int) {
   using R = TileRows<bf16_t, D>;
   const int r = lane & 15, half = lane >> 5;
   const int row = 8 * half + (r >> 2);  // + 4 e + 16 t
@@ -263,7 +264,7 @@ __device__ __forceinline__ void column_products(const char* tile, int block, con
     }
 }
 template <int D, int M>
-__device__ __forceinline__ void column_products(const char* tile, int block, const Weights<float>* const (&w)[M], f32x16* const (&c)[M], int lane) {
+__device__ __forceinline__ void column_products(const char* tile, int block, const Weights<float>* const (&w)[M], f32x16* const (&c)[M], int lane, int d) {
   using R = TileRows<float, D>;
   const int ch = lane & 31, half = lane >> 5;
 #pragma unroll
@@ -272,6 +273,7 @@ __device__ __forceinline__ void column_products(const char* tile, int block, con
     const char* at = tile + (block * 32 + row) * R::RB + (ch & 3) * 4;
 #pragma unroll
     for (int db = 0; db < D / 32; ++db) {
+      if (db > 0 && 32 * db >= d) break;
       const float a = *reinterpret_cast<const float*>(at + (((8 * db + (ch >> 2)) ^ R::mix(row)) << 4));
 #pragma unroll
       for (int j = 0; j < M; ++j) c[j][db] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, w[j]->w[i], c[j][db], 0, 0, 0);
@@ -310,6 +312,14 @@ __device__ __forceinline__ float score(float s, const AttnParams& p, float dx, f
   float rest = -from;
   if constexpr (TERMS & kDistance) {
     distance = __builtin_amdgcn_sqrtf(__builtin_fmaf(dx, dx, dy * dy));
+    if constexpr (sizeof(T) == 4) {  // (`from` last: it takes most of the value away, and what is left is exact)
+      float z = s * p.factor;
+      if constexpr (TERMS & kCap) {
+        score<T, kCap, NEAR>(s, p, 0.f, 0.f, 0.f, 0.f, bend, z);
+        z = bend;
+      }
+      return __builtin_fmaf(-slope, distance, z) - from;
+    }
     rest = __builtin_fmaf(-slope, distance, rest);
   }
   if constexpr (!(TERMS & kCap)) return __builtin_fmaf(s, p.factor, rest);
@@ -365,6 +375,7 @@ struct Walk {
   uint32_t g_magic;
   uint64_t bits;
   int base;
+  int tile_lo, tile_hi, tile_pad;  // of tile base + lane
 
   // own tokens i0 .. i1
   __device__ __forceinline__ void own(const Span* s, int i0, int i1) {
@@ -393,6 +404,11 @@ struct Walk {
     }
     return x;
   }
+  // whether the tile that next() gave last holds padding, and whether some of its tokens are hidden from some of the own ones
+  __device__ __forceinline__ bool padded(int t) const { return __builtin_amdgcn_readlane(tile_pad, t - base); }
+  __device__ __forceinline__ bool hides(int t) const {
+    return mixed || padded(t) || __builtin_amdgcn_readlane(tile_lo, t - base) != lo || __builtin_amdgcn_readlane(tile_hi, t - base) != lo;
+  }
   __device__ __forceinline__ void start(int t) {
     bits = 0;
     base = t - 64;
@@ -410,9 +426,17 @@ struct Walk {
       base += 64;
       const int t = base + (int)(threadIdx.x & 63);
       bool hit = t < end;
-      if (hit && spans) {
-        const Span x = of(t, rows);
-        hit = x.lo <= hi && x.hi >= lo;
+      if (spans) {
+        tile_lo = 0x7fffffff;
+        tile_hi = -1;
+        tile_pad = 0;
+        if (hit) {
+          const Span x = of(t, rows);
+          tile_lo = x.lo;
+          tile_hi = x.hi;
+          tile_pad = x.pad;
+          hit = x.lo <= hi && x.hi >= lo;
+        }
       }
       bits = __ballot(hit);
     }

@@ -37,7 +37,7 @@ __device__ __forceinline__ void join_waves(char* lds, int wave, int lane, f32x16
 }
 
 template <typename T, int D, int TERMS, bool DOCS, bool ALONE>
-__global__ __launch_bounds__(kAttnThreads, (sizeof(T) == 4 ? kAttnWaves<T, D> : D == 32 ? 4 : D == 64 ? 3 : 2)) void attn_fwd_kernel(AttnParams p) {
+__global__ __launch_bounds__(kAttnThreads, (sizeof(T) == 4 ? kAttnWaves<T, D> : D == 32 ? 4 : D == 64 && !ALONE ? 3 : 2)) void attn_fwd_kernel(AttnParams p) {
   using R = TileRows<T, D, ALONE>;
   constexpr int BN = R::BN, NB = 1;
   extern __shared__ __align__(16) char lds[];
@@ -82,9 +82,8 @@ __global__ __launch_bounds__(kAttnThreads, (sizeof(T) == 4 ? kAttnWaves<T, D> : 
     bool pads = false;
     masked = t * BN + BN > p.Nk;
     if constexpr (DOCS) {
-      const Span x = walk.of(t, p.Nk);
-      pads = __builtin_amdgcn_readfirstlane(x.pad);
-      masked = masked || walk.mixed || pads || __builtin_amdgcn_readfirstlane(x.lo) != walk.lo || __builtin_amdgcn_readfirstlane(x.hi) != walk.lo;
+      pads = walk.padded(t);
+      masked = masked || walk.hides(t);
     }
     keys.template load<ALONE>(dst, t * BN, pads);
     values.template load<ALONE>(dst + R::kBytes, t * BN, pads);
@@ -117,7 +116,7 @@ __global__ __launch_bounds__(kAttnThreads, (sizeof(T) == 4 ? kAttnWaves<T, D> : 
     if (busy) {
       f32x16 s[R::kBlocks][1];
 #pragma unroll
-      for (int kb = 0; kb < R::kBlocks; ++kb) row_products<T, D, 1>(kt, kb, q, s[kb], lane);
+      for (int kb = 0; kb < R::kBlocks; ++kb) row_products<T, D, 1>(kt, kb, q, s[kb], lane, p.d);
       const KeyNotes& about_key = notes[ALONE ? wave : buffer];
       const int left = p.Nk - t * BN - 8 * half;  // keys of the tile that are there, from the lane's first one on
       // s becomes score - from, hidden ones -infinity
@@ -164,7 +163,7 @@ __global__ __launch_bounds__(kAttnThreads, (sizeof(T) == 4 ? kAttnWaves<T, D> : 
         search = __any(!(sum < 4096.f));
         if (search) {
 #pragma unroll
-          for (int kb = 0; kb < R::kBlocks; ++kb) row_products<T, D, 1>(kt, kb, q, s[kb], lane);
+          for (int kb = 0; kb < R::kBlocks; ++kb) row_products<T, D, 1>(kt, kb, q, s[kb], lane, p.d);
         } else {
           l += sum;
         }
@@ -201,7 +200,7 @@ __global__ __launch_bounds__(kAttnThreads, (sizeof(T) == 4 ? kAttnWaves<T, D> : 
 #pragma unroll
       for (int kb = 0; kb < R::kBlocks; ++kb) {
         const Weights<T> w(s[kb][0]);
-        column_products<D, 1>(vt, kb, {&w}, {o[0]}, lane);
+        column_products<D, 1>(vt, kb, {&w}, {o[0]}, lane, p.d);
       }
     }
     if (ALONE && following < walk.end) {
