@@ -54,7 +54,7 @@ def test_attention_refuses():
     for name in ("B", "Nq", "Nk", "H", "Hk", "d"):
         assert fwd(**{name: 0}) == -2, name
     assert fwd(Hk=3) == -2 and fwd(Hk=8) == -2
-    assert fwd(scale=NAN) == -2 and fwd(scale=INF) == -2 and fwd(cap=-1.0) == -2 and fwd(cap=NAN) == -2 and fwd(cap=INF) == -2
+    assert fwd(scale=NAN) == -2 and fwd(scale=INF) == -2 and fwd(cap=-1.0) == -2 and fwd(cap=NAN) == -2 and fwd(cap=INF) == -2 and fwd(cap=1e-35) == -2 and fwd(scale=1e20, cap=1e-20) == -2
     assert fwd(dtype=2) == -3
     assert fwd(d=20) == -5 and fwd(d=136) == -5 and fwd(H=4098) == -5 and fwd(Nk=(1 << 24) + 1) == -5 and fwd(Nq=(1 << 24) + 1) == -5
     assert fwd(B=1 << 24) == -5 and fwd(Nq=1 << 24, H=256, Hk=2) == -5

@@ -134,10 +134,61 @@ def test_attention_terms(dtype, shape, cap, distance, docs):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [32, 64, 88, 128])
+@pytest.mark.parametrize("cap,distance,docs", [(0.0, False, None), (3.0, False, None), (0.0, True, None), (4.0, True, None), (0.0, False, "runs"), (5.0, False, "any"),
+                                               (0.0, True, "runs"), (4.0, True, "any")])
+def test_attention_of_many_images(dtype, d, cap, distance, docs):
+    """Enough blocks of 128 rows, and of 128 keys, for the kernels that work by these."""
+    _check(dtype, (130, 23, 70, 8, 4, d) if docs == "any" else (130, 37, 70, 4, 4, d), cap=cap, distance=distance, docs=docs, seed=2)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("images,d", [(1, 32), (1, 128), (66, 32), (66, 64), (66, 128)])
+@pytest.mark.parametrize("cap", [0.0, 150.0])
+def test_scores_that_rise_along_the_keys(dtype, images, d, cap):
+    """Scores that grow, or fall, by hundreds from the first keys to the last: what the exponentials are taken from has to follow."""
+    g = np.random.default_rng(6)
+    H, Nq, Nk = 8, 20, 400
+    for rise in (60.0, -60.0):
+        q = g.normal(size=(images, Nq, H, d)) * 0.3
+        k = g.normal(size=(images, Nk, H, d)) * 0.3
+        q[..., 0] = 1.0 + 0.5 * g.random((images, Nq, H))
+        k[..., 0] = (np.arange(Nk) / Nk * rise)[None, :, None]
+        val = {}
+        dev = {}
+        for n, x in (("q", q), ("k", k), ("v", g.normal(size=k.shape)), ("dout", g.normal(size=q.shape))):
+            dev[n], val[n] = _stored(x, dtype)
+        out, lse = aff.affmae_attn_fwd(dev["q"], dev["k"], dev["v"], 2.0, cap)
+        got = aff.affmae_attn_bwd(dev["q"], dev["k"], dev["v"], out, lse, dev["dout"], 2.0, cap)
+        some = slice(0, 2)
+        ref = oa.attn(val["q"][some], val["k"][some], val["v"][some], 2.0, cap, dout=val["dout"][some], half=HALF[dtype], given=out[some].double().cpu().numpy())
+        # what is below fp32's least normal value, 2^-126 = 1.2e-38, is 0 there: 1e3 terms of it times values of at most 1e3 are far below 1e-30
+        for n, t in (("out", out), ("lse", lse), *got.items()):
+            _close(t[some], ref[n][0], ref[n][1] + 1e-30, n)
+
+
+def test_keys_that_all_lie_far_below_zero():
+    """Scores near -1e4, and one image whose first tile is hidden from most."""
+    q = torch.full((1, 70, 1, 32), 1.0, device="cuda")
+    k = torch.full((1, 300, 1, 32), -312.5, device="cuda")
+    v = torch.randn(1, 300, 1, 32, device="cuda")
+    k[0, 200, 0, 0] += 2.0
+    out, lse = aff.affmae_attn_fwd(q, k, v, 1.0)
+    w = torch.ones(300, dtype=torch.float64, device="cuda")
+    w[200] = float(np.exp(2.0))
+    want = (w[:, None] * v[0, :, 0].double()).sum(0) / w.sum()
+    # a score of 1e4 is off by at most half a step of fp32 for each of its sums: 32 * 2^-24 * 1e4 = 0.02 at worst, the same for equal keys
+    assert float((out[0, :, 0].double() - want).abs().max()) < 0.04 * float(v.abs().max())
+    assert float((lse[0, :, 0].double() - (-1e4 + float(w.sum().log()))).abs().max()) < 0.04
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_attention_scales(dtype):
     for scale in (-0.3, 0.0, 1.5):
         _check(dtype, (1, 70, 90, 2, 2, 32), scale=scale)
         _check(dtype, (1, 70, 90, 2, 2, 32), scale=scale, cap=4.0, distance=True)
+    for cap in (0.05, 1.0, 1e6, 1e30):
+        _check(dtype, (1, 70, 90, 2, 2, 32), cap=cap)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
