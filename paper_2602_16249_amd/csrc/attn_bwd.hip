@@ -347,9 +347,9 @@ struct Side {
   bool alone;
   int blocks, splits, split_tiles;
 };
-Side side(long long own, long long other, long long heads, int D, int el) {
+Side side(long long own, long long other, long long heads, int D, int el, bool docs) {
   Side s;
-  s.alone = (own + kAttnRows - 1) / kAttnRows * heads < 512;
+  s.alone = attn_alone((own + kAttnRows - 1) / kAttnRows * heads, docs);
   const int BN = attn_tile_rows(D, el, s.alone);
   const int per = s.alone ? 32 : kAttnRows;
   s.blocks = (int)((own + per - 1) / per);
@@ -374,8 +374,8 @@ Layout layout(int B, int Nq, int Nk, int H, int Hk, int d, int dtype, bool docs,
   Layout l;
   const int D = width(d), el = dtype == 1 ? 2 : 4;
   const long long rows = (long long)Nq * (H / Hk);
-  l.query = side(rows, Nk, (long long)B * Hk, D, el);
-  l.key = side(Nk, rows, (long long)B * Hk, D, el);
+  l.query = side(rows, Nk, (long long)B * Hk, D, el, docs);
+  l.key = side(Nk, rows, (long long)B * Hk, D, el, docs);
   size_t off = 0;
   const auto take = [&](size_t bytes) {
     const size_t at = off;

@@ -86,6 +86,10 @@ struct TileRows {
 // Waves that a kernel's registers are to leave room for on a SIMD: two, but where the vectors of a lane's row alone fill them.
 template <typename T, int D>
 constexpr int kAttnWaves = sizeof(T) == 4 && D == 128 ? 1 : 2;
+// Whether `blocks` workgroups of 128 rows are too few: below one a CU, and with images, whose blocks see more or fewer tiles, below two.  us,
+// blocks of 128 / of 32: 4 x 2048 tokens, 6 heads of 64 (384 blocks) forward 61 / 77, backward 79 + 86 / 97 + 105; two rows of 8001 tokens
+// of 11 images each, 4 heads of 32 (504) 80 / 53.
+inline bool attn_alone(long long blocks, bool docs) { return blocks < (docs ? 512 : 256); }
 inline int attn_tile_rows(int D, int el, bool alone) { return D * el > 256 || (alone && D * el > 128) ? 32 : 64; }
 
 __device__ __forceinline__ int swap23(int m) { return (m & ~12) | (m & 4) << 1 | (m & 8) >> 1; }

@@ -303,17 +303,17 @@ __global__ __launch_bounds__(256) void attn_spans_kernel(const int32_t* q_doc, c
   if (lane == 0) (q ? to_q : to_k)[n] = Span{lo, hi, pad, 0};
 }
 
-// Where blocks of 128 rows do not fill the chip's 256 CUs twice, blocks of 32 whose waves share the keys out; where these do not either,
-// the keys are split over workgroups too, kLeastKeys each at least.
+// Blocks of 128 rows, or of 32 whose waves share the keys out (attn_alone); where these do not fill the chip's 256 CUs twice, the keys are split over
+// workgroups too, kLeastKeys each at least.
 constexpr int kLeastKeys = 256;
 struct Plan {
   bool alone;
   int blocks, splits, split_tiles;
 };
-Plan plan(int B, int Nq, int Nk, int H, int Hk, int D, int el) {
+Plan plan(int B, int Nq, int Nk, int H, int Hk, int D, int el, bool docs) {
   const long long rows = (long long)Nq * (H / Hk), heads = (long long)B * Hk;
   Plan l;
-  l.alone = (rows + kAttnRows - 1) / kAttnRows * heads < 512;
+  l.alone = attn_alone((rows + kAttnRows - 1) / kAttnRows * heads, docs);
   const int BN = attn_tile_rows(D, el, l.alone);
   const int per = l.alone ? 32 : kAttnRows;
   l.blocks = (int)((rows + per - 1) / per);
@@ -401,7 +401,7 @@ hipError_t launch_attn_spans(const AttnArgs& a, Span* q_span, Span* k_span, hipS
 }
 
 size_t attn_fwd_workspace_bytes(int B, int Nq, int Nk, int H, int Hk, int d, int dtype, bool docs) {
-  const Plan l = plan(B, Nq, Nk, H, Hk, width(d), dtype == 1 ? 2 : 4);
+  const Plan l = plan(B, Nq, Nk, H, Hk, width(d), dtype == 1 ? 2 : 4, docs);
   return (docs ? attn_span_bytes(B, Nq, Nk) : 0) + (l.splits > 1 ? (size_t)l.splits * B * Nq * H * (d + 1) * sizeof(float) : 0);
 }
 
@@ -409,7 +409,7 @@ hipError_t launch_attn_fwd(const AttnArgs& a, hipStream_t stream) {
   AttnParams p = attn_params(a, static_cast<Span*>(a.workspace));
   p.o = a.out;
   p.lse_out = a.lse;
-  const Plan l = plan(a.B, a.Nq, a.Nk, a.H, a.Hk, width(a.d), a.dtype == 1 ? 2 : 4);
+  const Plan l = plan(a.B, a.Nq, a.Nk, a.H, a.Hk, width(a.d), a.dtype == 1 ? 2 : 4, a.q_doc != nullptr);
   p.alone = l.alone; p.blocks = l.blocks; p.splits = l.splits; p.split_tiles = l.split_tiles;
   if (p.splits > 1) p.part = reinterpret_cast<float*>(static_cast<char*>(a.workspace) + (a.q_doc ? attn_span_bytes(a.B, a.Nq, a.Nk) : 0));
   p.blocks_magic = div_magic(p.blocks);
