@@ -5,6 +5,9 @@
 // seven products of two of a pair's vectors instead of five, and nothing is added up by atomics: the results are the same in every
 // run, and grouped heads' gradients add up in registers.
 //
+// Bound by the vector ALU with 32 channels (16 x 1024 tokens, 8 heads, distances: 90 us, key kernel 85), by matrix instructions with 128 (8 x 4096, 6
+// heads: 540 us, 1145 TFLOP/s, about the rate of a large library product; key kernel 806 us, 1023).
+//
 // D from the bf16 out is off by what out was rounded by, as much as a hundredth of dZ where few keys share a row's weight (two keys of 64
 // channels: dq and dk off by 0.8 % of their size).  The row's dZ sum to 0 if D is right, so their sum is what D lacks: the key
 // kernel gets it, and dq is put right at the end by as much of sum_j p_ij k_j, one more product.

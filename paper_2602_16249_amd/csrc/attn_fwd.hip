@@ -1,7 +1,12 @@
 // Attention between all tokens, forward: per image, head h and query i
 //     z_j = scale <q_i, k_j>,  z_j = cap tanh(z_j / cap),  z_j -= slope_h |x_i - y_j|,  hidden where the images of i and j differ,
 //     out_i = sum_j p_j v_j,  p = softmax(z),  lse_i = log sum_j exp z_j,
-// in one pass over the keys with the running maximum and sum of every row (attn_common.h: the tiles and their layout).
+// in one pass over the keys with a running reference and sum of every row (attn_common.h: the tiles and their layout).
+//
+// Bound by the vector ALU up to 64 channels (a product, an exponential that takes the time of two, a sum and half a conversion a
+// pair, beside 8 cycles of matrix instructions for 64 channels), by both with 128: 8 x 4096 tokens, 6 heads of 64 255 us (808 TFLOP/s; 306 while
+// a tile waited for the next one), of 128 409 us (1010); 16 x 1024, 8 heads of 32 with distances 68 us.  Two rows of 8001 tokens of 11 images
+// each, capped, 4 heads of 32: 50 us.  One query of 12 heads on 3, 4 x 16384 keys of 64: 14.5 us (3.5 TB/s) and 5.4 for the join.
 #include "attn_common.h"
 #include "timing.h"
 

@@ -4,7 +4,8 @@
 // and, backward, by -theta; d<dy, y> / d theta = y0 dy1 - y1 dy0, which summed over heads and pairs times freq gives dcoords.
 //
 // Bound by memory: three operations a value.  A thread holds P pairs of a token, works their sines and cosines out once and
-// turns those pairs of all the heads, of the queries and of the keys.
+// turns those pairs of all the heads, of the queries and of the keys.  131072 tokens of (2 + 2) x 32 bf16 12.1 us (68 MB, 5.6 TB/s, part of it in the
+// last-level cache), backward of 98304 x 6 x 64 with dcoords 44 us (228 MB, 5.2 TB/s).
 #include "launch.h"
 #include "timing.h"
 
