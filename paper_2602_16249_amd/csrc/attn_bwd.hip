@@ -140,9 +140,8 @@ __global__ __launch_bounds__(kAttnThreads, (kAttnWaves<T, D>)) void attn_bwd_que
         using no = std::false_type;
         bool near = false;
         if constexpr ((TERMS & kCap) && D < 128) near = all_near(s[0], p.near);
-        // keys that are not there have zeros for vectors, so that they add nothing to dq: without sums over p and dZ nothing is hidden
-        constexpr bool kHides = REST || (TERMS & kDistance) || DOCS;
-        if (kHides && (masked || D == 128)) {  // (one way through where two would not fit the registers)
+        // (keys that are not there have zeros for vectors, but exp(0 - lse) need not be finite)
+        if (masked || (D == 128 && REST)) {  // (one way through where two would not fit the registers)
           if (near) slopes(yes{}, yes{});
           else slopes(no{}, yes{});
         } else {

@@ -183,6 +183,28 @@ def test_keys_that_all_lie_far_below_zero():
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("images,Nk", [(1, 70), (130, 70), (1, 1030), (66, 1030)])
+@pytest.mark.parametrize("d", [32, 64, 128])
+@pytest.mark.parametrize("far", [-300.0, 300.0])
+def test_gradients_of_scores_far_from_zero(dtype, images, Nk, d, far):
+    """exp(0 - lse) of a key or query that is not there does not fit 32 bits."""
+    g = np.random.default_rng(8)
+    H, Nq = 4, 9
+    q, k = g.normal(size=(images, Nq, H, d)) * 0.3, g.normal(size=(images, Nk, H, d)) * 0.3
+    q[..., 0], k[..., 0] = 1.0, far
+    dev, val = {}, {}
+    for n, x in (("q", q), ("k", k), ("v", g.normal(size=k.shape)), ("dout", g.normal(size=q.shape))):
+        dev[n], val[n] = _stored(x, dtype)
+    out, lse = aff.affmae_attn_fwd(dev["q"], dev["k"], dev["v"], 1.0)
+    got = aff.affmae_attn_bwd(dev["q"], dev["k"], dev["v"], out, lse, dev["dout"], 1.0)
+    some = slice(0, 1)
+    ref = oa.attn(val["q"][some], val["k"][some], val["v"][some], 1.0, dout=val["dout"][some], half=HALF[dtype], given=out[some].double().cpu().numpy())
+    for n, t in (("out", out), ("lse", lse), *got.items()):
+        assert bool(torch.isfinite(t).all()), n
+        _close(t[some], *ref[n], n)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_attention_scales(dtype):
     for scale in (-0.3, 0.0, 1.5):
         _check(dtype, (1, 70, 90, 2, 2, 32), scale=scale)
