@@ -25,6 +25,9 @@ template <typename T, int D, int TERMS, bool REST, bool DOCS, bool ALONE>
 __global__ __launch_bounds__(kAttnThreads, (kAttnWaves<T, D>)) void attn_bwd_query_kernel(AttnParams p) {
   using R = TileRows<T, D, ALONE>;
   constexpr int BN = R::BN, kTogether = D == 128 ? 1 : 2;  // blocks of a tile that are worked on together
+  // Keys behind the last one have zeros for vectors, which keeps them out of dq if their p, exp(0 - lse), is kept finite: at most 1, as those of
+  // keys are anyway (a modifier of the exponential).  With sums over p and dZ they have to be hidden, like keys of other images.
+  constexpr bool kHides = REST || (TERMS & kDistance) || DOCS || sizeof(T) == 4;
   extern __shared__ __align__(16) char lds[];
   __shared__ KeyNotes notes[ALONE ? 4 : 2];
   const int work = xcd_contiguous_block(blockIdx.x, gridDim.x);
@@ -115,7 +118,9 @@ __global__ __launch_bounds__(kAttnThreads, (kAttnWaves<T, D>)) void attn_bwd_que
             float bend, distance, dx = 0.f, dy = 0.f;
             if constexpr (TERMS & kDistance) dx = own.x - n.x[j], dy = own.y - n.y[j];
             const float z = score<T, TERMS, near>(s[0][i], p, dx, dy, own.slope, lse, bend, distance);
-            float pr = __builtin_amdgcn_exp2f(z), dz = pr * (dp[0][i] - sum);
+            float pr = __builtin_amdgcn_exp2f(z);
+            if constexpr (!kHides) pr = __builtin_amdgcn_fmed3f(pr, 0.f, 1.f);
+            float dz = pr * (dp[0][i] - sum);
             if constexpr (hides) {
               const bool off = j - 8 * half >= left || (DOCS && n.doc[j] != own.doc);
               pr = off ? 0.f : pr;
@@ -140,8 +145,7 @@ __global__ __launch_bounds__(kAttnThreads, (kAttnWaves<T, D>)) void attn_bwd_que
         using no = std::false_type;
         bool near = false;
         if constexpr ((TERMS & kCap) && D < 128) near = all_near(s[0], p.near);
-        // (keys that are not there have zeros for vectors, but exp(0 - lse) need not be finite)
-        if (masked || (D == 128 && REST)) {  // (one way through where two would not fit the registers)
+        if (kHides && (masked || D == 128)) {  // (one way through where two would not fit the registers)
           if (near) slopes(yes{}, yes{});
           else slopes(no{}, yes{});
         } else {
