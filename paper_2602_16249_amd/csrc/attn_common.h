@@ -248,7 +248,7 @@ struct Weights<float> {
   __device__ __forceinline__ Weights(const f32x16& x) : w(x) {}
 };
 
-// c[j][n][ch] += sum over the block's rows of tile[row][ch] w[j * NB + n][row]: J sets of weights for each of NB column blocks
+// c[j][column][ch] += sum over the block's rows of tile[row][ch] w[j][column][row], for M sets of weights that share the reads of the tile
 template <int D, int M>
 __device__ __forceinline__ void column_products(const char* tile, int block, const Weights<bf16_t>* const (&w)[M], f32x16* const (&c)[M], int lane, int) {
   using R = TileRows<bf16_t, D>;
