@@ -37,10 +37,12 @@ def hidden(q_doc, k_doc):
     return (q_doc[:, :, None] != k_doc[:, None, :]) | (q_doc[:, :, None] < 0) | (k_doc[:, None, :] < 0)
 
 
-def attn(q, k, v, scale, cap=0.0, q_xy=None, k_xy=None, slope=None, q_doc=None, k_doc=None, dout=None, half=0.0, given=None):
+def attn(q, k, v, scale, cap=0.0, q_xy=None, k_xy=None, slope=None, q_doc=None, k_doc=None, dout=None, half=0.0, given=None, puts_right=False):
     """out, lse and, with dout, dq, dk, dv (and dslope): name -> (values, bound).  `half`: rounding of the storage type; what a bf16
     implementation rounds on the way (p, dS) is counted with it, U stands for a type that it need not round.
-    `given`: the stored output that the backward pass got, whose rounding goes into D."""
+    `given`: the stored output that the backward pass got, whose rounding goes into D.  `puts_right`: of an implementation that works out
+    what D lacks, r = sum_j p (dP - D), and takes r sum_j p (1 - tanh^2) k_j off dq and gives D + r to dk: then what `given` was rounded by
+    is left only where dS and p were rounded for dq's two products, at `on_way` each."""
     B, Nq, H, d = q.shape
     Nk, Hk = k.shape[1:3]
     G = H // Hk
@@ -100,7 +102,16 @@ def attn(q, k, v, scale, cap=0.0, q_xy=None, k_xy=None, slope=None, q_doc=None, 
             stored = tol if given is None else np.abs(np.where(sees[:, None], given[b, :, h], 0.0) - out)
             D_off = (np.abs(g) * stored).sum(1) + 2 * U * (d + 6) * (np.abs(g) * np.abs(out)).sum(1)
             dZ = p * (dP - D[:, None])
-            dZ_off = p * ((eps + 4 * U) * np.abs(dP - D[:, None]) + dP_off + D_off[:, None])
+            pair_off = (eps + 4 * U) * np.abs(dP - D[:, None]) + dP_off
+            gap = np.zeros(Nq)
+            if puts_right:
+                # with D - gap for D a row's dZ sum to gap (1 + a row's error of sum p) and the sum of what their own are off by
+                if given is not None:
+                    gap = np.abs((g * np.where(sees[:, None], given[b, :, h] - out, 0.0)).sum(1)) + 2 * U * (d + 6) * (np.abs(g) * np.abs(out)).sum(1)
+                gap_sum = n_sum * (p * (np.abs(dP - D[:, None]) + gap[:, None])).sum(1) + (np.where(gone, 0.0, eps).max(1) + 4 * U) * gap + 4 * U * np.abs(D)
+                dZ_off = p * (pair_off + ((p * pair_off).sum(1) + gap_sum + 4 * U * gap)[:, None])
+            else:
+                dZ_off = p * (pair_off + D_off[:, None])
             if slope is not None:
                 r["dslope"][0][h] -= (dZ * dist).sum()
                 # D enters as the sum of p dP, so its storage's rounding does not: only the sums that put it right
@@ -113,7 +124,8 @@ def attn(q, k, v, scale, cap=0.0, q_xy=None, k_xy=None, slope=None, q_doc=None, 
                 dS_off = dZ_off + np.abs(dZ) * (2 * np.abs(bend) * bend_off + bend_off ** 2 + 4 * U)
             dS_off = dS_off + on_way * (np.abs(dS) + dS_off)
             dq = scale * (dS @ K)
-            dq_off = abs(scale) * ((dS_off + n_sum * np.abs(dS)) @ np.abs(K))
+            twice = 2 * (on_way + n_sum + 4 * U) * p * gap[:, None]  # in dS and in p times what D lacks
+            dq_off = abs(scale) * ((dS_off + twice + n_sum * np.abs(dS)) @ np.abs(K))
             r["dq"][0][b, :, h], r["dq"][1][b, :, h] = dq, dq_off + max(half, U) * (np.abs(dq) + dq_off) + 4 * U * np.abs(dq)
             r_sum = 2 * U * (Nq * G + 16)
             p_off = p * (eps + on_way)
