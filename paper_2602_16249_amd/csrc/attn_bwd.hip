@@ -6,11 +6,14 @@
 // run, and grouped heads' gradients add up in registers.
 //
 // Bound by the vector ALU with 32 channels (16 x 1024 tokens, 8 heads, distances: 90 us, key kernel 85), by matrix instructions with 128 (8 x 4096, 6
-// heads: 540 us, 1145 TFLOP/s, about the rate of a large library product; key kernel 806 us, 1023).
+// heads: 769 us, 1073 TFLOP/s, near the rate of a large library product; key kernel 814 us, 1013).
 //
-// D from the bf16 out is off by what out was rounded by, as much as a hundredth of dZ where few keys share a row's weight (two keys of 64
-// channels: dq and dk off by 0.8 % of their size).  The row's dZ sum to 0 if D is right, so their sum is what D lacks: the key
-// kernel gets it, and dq is put right at the end by as much of sum_j p_ij k_j, one more product.
+// D from the bf16 out is off by what out was rounded by, which counts where few keys share a row's weight, in a row of any length (500
+// queries near the sum of two keys, of 2 of 64 channels or of 1024 of 128: dq off by 0.0049 and 0.0060 of its size, dk by 0.0029 and
+// 0.0055, rows with one key in front by all of their own).  The row's dZ sum to 0 if D is right, so their sum is what D lacks: the key kernel
+// gets it, and dq is put right at the end by as much of sum_j p_ij k_j, one more product (dq 0.0025, dk at most 0.0025).  How many keys
+// share a row's weight is not known beforehand, so every bf16 row has it.  With 128 channels that product is not hidden behind the
+// exponentials: 8 x 4096 tokens, 6 heads 769 us, 546 without it.
 #include "attn_common.h"
 #include "timing.h"
 
@@ -21,13 +24,11 @@ namespace {
 
 int width(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : 128; }
 
-template <typename T, int D, int TERMS, bool REST, bool DOCS, bool ALONE>
+template <typename T, int D, int TERMS, bool DOCS, bool ALONE>
 __global__ __launch_bounds__(kAttnThreads, (kAttnWaves<T, D>)) void attn_bwd_query_kernel(AttnParams p) {
   using R = TileRows<T, D, ALONE>;
   constexpr int BN = R::BN, kTogether = D == 128 ? 1 : 2;  // blocks of a tile that are worked on together
-  // Keys behind the last one have zeros for vectors, which keeps them out of dq if their p, exp(0 - lse), is kept finite: at most 1, as those of
-  // keys are anyway (a modifier of the exponential).  With sums over p and dZ they have to be hidden, like keys of other images.
-  constexpr bool kHides = REST || (TERMS & kDistance) || DOCS || sizeof(T) == 4;
+  constexpr bool REST = sizeof(T) == 2;  // D is put right
   extern __shared__ __align__(16) char lds[];
   __shared__ KeyNotes notes[ALONE ? 4 : 2];
   const int work = xcd_contiguous_block(blockIdx.x, gridDim.x);
@@ -119,9 +120,8 @@ __global__ __launch_bounds__(kAttnThreads, (kAttnWaves<T, D>)) void attn_bwd_que
             if constexpr (TERMS & kDistance) dx = own.x - n.x[j], dy = own.y - n.y[j];
             const float z = score<T, TERMS, near>(s[0][i], p, dx, dy, own.slope, lse, bend, distance);
             float pr = __builtin_amdgcn_exp2f(z);
-            if constexpr (!kHides) pr = __builtin_amdgcn_fmed3f(pr, 0.f, 1.f);
             float dz = pr * (dp[0][i] - sum);
-            if constexpr (hides) {
+            if constexpr (hides) {  // (keys behind the last one, too: their p, exp(0 - lse), may not fit 32 bits)
               const bool off = j - 8 * half >= left || (DOCS && n.doc[j] != own.doc);
               pr = off ? 0.f : pr;
               dz = off ? 0.f : dz;
@@ -145,7 +145,7 @@ __global__ __launch_bounds__(kAttnThreads, (kAttnWaves<T, D>)) void attn_bwd_que
         using no = std::false_type;
         bool near = false;
         if constexpr ((TERMS & kCap) && D < 128) near = all_near(s[0], p.near);
-        if (kHides && (masked || D == 128)) {  // (one way through where two would not fit the registers)
+        if (masked || D == 128) {  // (one way through where two would not fit the registers)
           if (near) slopes(yes{}, yes{});
           else slopes(no{}, yes{});
         } else {
@@ -240,33 +240,25 @@ __global__ __launch_bounds__(kAttnThreads, (kAttnWaves<T, D>)) void attn_bwd_que
     }
 }
 
-template <typename T, int D, int TERMS, bool REST, bool DOCS, bool ALONE>
+template <typename T, int D, int TERMS, bool DOCS, bool ALONE>
 hipError_t launch_kernel(const AttnParams& p, hipStream_t stream) {
   const size_t lds = (ALONE ? 8 : 4) * TileRows<T, D, ALONE>::kBytes;
-  const hipError_t e = hipFuncSetAttribute((const void*)attn_bwd_query_kernel<T, D, TERMS, REST, DOCS, ALONE>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+  const hipError_t e = hipFuncSetAttribute((const void*)attn_bwd_query_kernel<T, D, TERMS, DOCS, ALONE>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
   if (e != hipSuccess) return e;
-  AFFMAE_LAUNCH("attn_bwd_query_kernel", stream, (attn_bwd_query_kernel<T, D, TERMS, REST, DOCS, ALONE>), dim3((p.work + 7) / 8 * 8), dim3(kAttnThreads), lds, stream, p);
+  AFFMAE_LAUNCH("attn_bwd_query_kernel", stream, (attn_bwd_query_kernel<T, D, TERMS, DOCS, ALONE>), dim3((p.work + 7) / 8 * 8), dim3(kAttnThreads), lds, stream, p);
   return hipGetLastError();
 }
-template <typename T, int D, int TERMS, bool REST>
+template <typename T, int D, int TERMS>
 hipError_t launch(const AttnParams& p, hipStream_t stream) {
-  if constexpr (D == 128 && sizeof(T) == 2 && !REST) {  // (with images D is always put right)
-    return p.alone ? launch_kernel<T, D, TERMS, REST, false, true>(p, stream) : launch_kernel<T, D, TERMS, REST, false, false>(p, stream);
-  } else {
-    if (p.q_doc) return p.alone ? launch_kernel<T, D, TERMS, REST, true, true>(p, stream) : launch_kernel<T, D, TERMS, REST, true, false>(p, stream);
-    return p.alone ? launch_kernel<T, D, TERMS, REST, false, true>(p, stream) : launch_kernel<T, D, TERMS, REST, false, false>(p, stream);
-  }
+  if (p.q_doc) return p.alone ? launch_kernel<T, D, TERMS, true, true>(p, stream) : launch_kernel<T, D, TERMS, true, false>(p, stream);
+  return p.alone ? launch_kernel<T, D, TERMS, false, true>(p, stream) : launch_kernel<T, D, TERMS, false, false>(p, stream);
 }
 template <typename T, int TERMS>
 hipError_t launch_width(const AttnParams& p, hipStream_t stream) {
-  constexpr bool kBf16 = sizeof(T) == 2;
   switch (width(p.d)) {
-    case 32: return launch<T, 32, TERMS, kBf16>(p, stream);
-    case 64: return launch<T, 64, TERMS, kBf16>(p, stream);
-    default:
-      if constexpr (kBf16 && !(TERMS & kDistance))
-        if (!p.puts_right) return launch<T, 128, TERMS, false>(p, stream);
-      return launch<T, 128, TERMS, kBf16>(p, stream);
+    case 32: return launch<T, 32, TERMS>(p, stream);
+    case 64: return launch<T, 64, TERMS>(p, stream);
+    default: return launch<T, 128, TERMS>(p, stream);
   }
 }
 template <typename T>
@@ -370,13 +362,9 @@ Side side(long long own, long long other, long long heads, int D, int el, bool d
 struct Layout {
   Side query, key;
   size_t spans, rowsum, rowlse, rowrest, rowslope, part_q, seen_q, part_k, part_v, total;  // places in the workspace
-  bool rest;
+  bool rest;  // D is put right
 };
-// Whether D is put right (attn_bwd.hip's head).  In heads of 32 and 64 channels the product that this takes is hidden behind the
-// exponentials; in wider ones it is not, and long rows without a term that makes them narrow go without.
-constexpr int kLongRow = 1024;
-bool puts_right(int Nk, int d, int dtype, bool docs, bool distance) { return dtype == 1 && (d <= 64 || Nk < kLongRow || docs || distance); }
-Layout layout(int B, int Nq, int Nk, int H, int Hk, int d, int dtype, bool docs, bool want_dslope, bool distance) {
+Layout layout(int B, int Nq, int Nk, int H, int Hk, int d, int dtype, bool docs, bool want_dslope) {
   Layout l;
   const int D = width(d), el = dtype == 1 ? 2 : 4;
   const long long rows = (long long)Nq * (H / Hk);
@@ -390,7 +378,7 @@ Layout layout(int B, int Nq, int Nk, int H, int Hk, int d, int dtype, bool docs,
   };
   const size_t nq = (size_t)B * Nq * H, nk = (size_t)B * Nk * Hk;
   l.spans = take(docs ? attn_span_bytes(B, Nq, Nk) : 0);
-  l.rest = puts_right(Nk, d, dtype, docs, distance);
+  l.rest = dtype == 1;
   l.rowsum = take(nq * 4);
   l.rowlse = take(nq * 4);
   l.rowrest = take(l.rest && l.query.splits > 1 ? (size_t)l.query.splits * nq * 4 : 0);
@@ -406,18 +394,17 @@ Layout layout(int B, int Nq, int Nk, int H, int Hk, int d, int dtype, bool docs,
 }  // namespace
 
 size_t attn_bwd_workspace_bytes(int B, int Nq, int Nk, int H, int Hk, int d, int dtype, bool docs, bool want_dslope) {
-  return layout(B, Nq, Nk, H, Hk, d, dtype, docs, want_dslope, true).total;  // (a few values more than a call without distances takes)
+  return layout(B, Nq, Nk, H, Hk, d, dtype, docs, want_dslope).total;
 }
 
 hipError_t launch_attn_bwd(const AttnArgs& a, hipStream_t stream) {
-  const Layout l = layout(a.B, a.Nq, a.Nk, a.H, a.Hk, a.d, a.dtype, a.q_doc != nullptr, a.dslope != nullptr, a.slope != nullptr);
+  const Layout l = layout(a.B, a.Nq, a.Nk, a.H, a.Hk, a.d, a.dtype, a.q_doc != nullptr, a.dslope != nullptr);
   char* ws = static_cast<char*>(a.workspace);
   AttnParams p = attn_params(a, reinterpret_cast<Span*>(ws + l.spans));
   p.rowsum = reinterpret_cast<float*>(ws + l.rowsum);
   p.rowslope = a.dslope ? reinterpret_cast<float*>(ws + l.rowslope) : nullptr;
   p.rowlse = reinterpret_cast<float*>(ws + l.rowlse);
   p.rowrest = reinterpret_cast<float*>(ws + l.rowrest);
-  p.puts_right = l.rest;
   p.grad_scale = a.scale;
   p.dq = a.dq; p.dk = a.dk; p.dv = a.dv;
   AttnParams pq = p, pk = p;

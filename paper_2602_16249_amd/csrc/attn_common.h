@@ -57,7 +57,6 @@ struct AttnParams {
   // backward
   float* rowsum;    // [B,Hk,rows] D: <dout, out>, and what that lacks
   float* rowlse;    // [B,Hk,rows] lse in units of log 2; infinity for rows that see no key or are padding: their p is 0
-  bool puts_right;  // (attn_bwd.hip)
   float* rowrest;   // [splits][B,Hk,rows] what <dout, out> lacks of D, with splits
   float* rowslope;  // [splits][3][H][B,Nq] parts of dslope, or null
   float* part_v;    // (part: dq, or dk: [splits][...][d]; part_v: what D's rest takes from dq, or dv)

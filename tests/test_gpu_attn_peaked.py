@@ -78,3 +78,23 @@ def test_two_keys_share_the_weight_with_terms(dtype, d, Nq, Nk, cap, distance, d
 def test_two_keys_share_the_weight_in_many_images(d, cap, docs):
     """Enough blocks of 128 rows, and of 128 keys, for the kernels that work by these."""
     _check("bf16", 130, 23, 150, 4, 4, d, cap, False, docs, images=2)
+
+
+@pytest.mark.parametrize("d", [72, 104, 128])
+@pytest.mark.parametrize("Nk", [2, 1023, 1024, 4097])
+def test_two_keys_share_the_weight_in_wide_heads(d, Nk):
+    """D is put right whatever the row's length."""
+    _check("bf16", 1, 70, Nk, 4, 2, d)
+
+
+@pytest.mark.parametrize("d", [72, 128])
+@pytest.mark.parametrize("Nq,Nk", [(70, 1025), (9, 2999)])
+@pytest.mark.parametrize("cap,distance,docs", [(30.0, False, False), (0.0, True, False), (0.0, False, True), (25.0, True, True)])
+def test_long_rows_of_wide_heads_with_terms(d, Nq, Nk, cap, distance, docs):
+    _check("bf16", 2, Nq, Nk, 4, 2, d, cap, distance, docs)
+
+
+@pytest.mark.parametrize("d", [72, 128])
+@pytest.mark.parametrize("cap,docs", [(0.0, False), (30.0, False), (0.0, True)])
+def test_long_rows_of_wide_heads_in_many_images(d, cap, docs):
+    _check("bf16", 66, 20, 1030, 4, 4, d, cap, False, docs, images=1)
