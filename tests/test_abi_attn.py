@@ -137,3 +137,15 @@ def test_rotary_layouts_of_header_and_binding():
     import re
     text = open(os.path.join(os.path.dirname(aff.library_path()), "..", "include", "affmae.h")).read()
     assert {n.lower(): int(v) for n, v in re.findall(r"AFFMAE_ROTARY_([A-Z]+) = (\d)", text)} == binding._ROTARY_LAYOUTS
+
+
+def test_binding_refuses_gradients_that_a_call_does_not_write(no_library):
+    """A buffer that stays as it was would come back as if it held a gradient."""
+    x, xy, s, freq = _meta(1, 4, 2, 8), _meta(1, 4, 2, dtype=torch.float32), _meta(2, dtype=torch.float32), _meta(4, 2, dtype=torch.float32)
+    where = dict(q_xy=xy, k_xy=xy, slope=s)
+    for grads, more in ((dict(dslope=s), {}), (dict(dslope=s), dict(want_dslope=False, **where)), (dict(dq=x, dkey=x), {}), (dict(dbias=x), where)):
+        with pytest.raises(ValueError, match="not written"):
+            aff.affmae_attn_bwd(x, x, x, x, x, x, 1.0, grads=grads, **more)
+    for grads, more in ((dict(dcoords=xy), {}), (dict(dq=x, dk=x), {}), (dict(dcoords=xy), dict(dk_out=x)), (dict(dfreq=freq), dict(q_out=x, want_dcoords=True))):
+        with pytest.raises(ValueError, match="not written"):
+            aff.affmae_rotary_bwd(x, xy, freq, grads=grads, **more)
