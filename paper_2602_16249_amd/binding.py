@@ -899,6 +899,15 @@ def affmae_dropout_bwd(dout: torch.Tensor, p: float, rng: Optional[torch.Tensor]
     return dx
 
 
+def _given_grads(grads: Optional[Dict[str, torch.Tensor]], *written: str) -> Dict[str, torch.Tensor]:
+    """The caller's buffers for gradients: none but for those that the call writes, as others would come back as they were."""
+    g = dict(grads) if grads else {}
+    for name in g:
+        if name not in written:
+            raise ValueError(f"grads has {name!r}, which is not written by this call ({', '.join(written)} are)")
+    return g
+
+
 def _rotary_args(call: str, dev: int, q: torch.Tensor, k: Optional[torch.Tensor], coords: torch.Tensor, freq: torch.Tensor,
                  layout: str):
     """Sizes, addresses and codes that both directions check and pass alike."""
@@ -951,7 +960,7 @@ def affmae_rotary_bwd(dq_out: torch.Tensor, coords: torch.Tensor, freq: torch.Te
                       layout: str = "pairs", q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None,
                       want_dcoords: bool = False, grads: Optional[Dict[str, torch.Tensor]] = None) -> Dict[str, torch.Tensor]:
     """Gradients of affmae_rotary_fwd -> dict(dq[, dk: with dk_out][, dcoords [B,N,axes] fp32: if asked for, from the forward's
-    q_out and k_out]).  dq may be dq_out, dk may be dk_out."""
+    q_out and k_out]).  dq may be dq_out, dk may be dk_out.  grads: buffers for any of these and nothing else."""
     lib = load_library()
     code = _dtype_code(dq_out)
     dev = _current(dq_out)
@@ -965,7 +974,7 @@ def affmae_rotary_bwd(dq_out: torch.Tensor, coords: torch.Tensor, freq: torch.Te
             raise ValueError("dcoords needs the forward's q_out, and with dk_out its k_out")
         q_at = _on(dev, q_out, "q_out", dtype, dq_out.shape)
         k_at = None if dk_out is None else _on(dev, k_out, "k_out", dtype, k_shape)
-    g = dict(grads) if grads else {}
+    g = _given_grads(grads, "dq", *(("dk",) if dk_out is not None else ()), *(("dcoords",) if want_dcoords else ()))
 
     def grad(name, shape, type_):
         if name in g:
@@ -1039,7 +1048,8 @@ def affmae_attn_bwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torc
                     slope: Optional[torch.Tensor] = None, q_doc: Optional[torch.Tensor] = None, k_doc: Optional[torch.Tensor] = None,
                     want_dslope: bool = True, grads: Optional[Dict[str, torch.Tensor]] = None,
                     workspace: Optional[torch.Tensor] = None) -> Dict[str, torch.Tensor]:
-    """Gradients of affmae_attn_fwd, whose out and lse it takes -> dict(dq, dk, dv[, dslope [H] fp32: with slope])."""
+    """Gradients of affmae_attn_fwd, whose out and lse it takes -> dict(dq, dk, dv[, dslope [H] fp32: with slope
+    unless want_dslope is false]).  grads: buffers for any of these and nothing else."""
     lib = load_library()
     code = _dtype_code(q)
     dev = _current(q)
@@ -1047,7 +1057,8 @@ def affmae_attn_bwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torc
     B, Nq, _, H, _, _ = sizes
     at += [_on(dev, out, "out", q.dtype, q.shape), _on(dev, lse, "lse", torch.float32, (B, Nq, H)),
            _on(dev, dout, "dout", q.dtype, q.shape)]
-    g = dict(grads) if grads else {}
+    sloped = slope is not None and want_dslope
+    g = _given_grads(grads, "dq", "dk", "dv", *(("dslope",) if sloped else ()))
 
     def grad(name, like, type_):
         if name in g:
@@ -1056,7 +1067,6 @@ def affmae_attn_bwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torc
         return t.data_ptr()
 
     to = [grad("dq", q, q.dtype), grad("dk", k, q.dtype), grad("dv", v, q.dtype)]
-    sloped = slope is not None and want_dslope
     to.append(grad("dslope", slope, torch.float32) if sloped else None)
     need = lib.affmae_attn_bwd_workspace_bytes(*sizes, code, q_doc is not None, sloped)
     workspace, ws_at, size = _workspace_on(dev, workspace, need, q.device)
