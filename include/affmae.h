@@ -616,8 +616,9 @@ int affmae_rotary_bwd(const void* dq_out, const void* dk_out, const void* q_out,
  * B * Hk * ceil(Nq * H / Hk / 128) and B * Hk * ceil(Nk / 128) <= 2^24 - 8
  * (AFFMAE_ERR_UNSUPPORTED otherwise).
  * Errors: AFFMAE_ERR_NULL, AFFMAE_ERR_DTYPE, AFFMAE_ERR_SHAPE (sizes < 1, H % Hk, a scale
- * or cap that is not finite, cap < 0 or above 0 and so small that scale / cap is not
- * finite, misaligned tensors), AFFMAE_ERR_UNSUPPORTED, AFFMAE_ERR_WORKSPACE.
+ * or cap that is not finite, cap < 0, or above 0 and below 1e-30 or so small that scale /
+ * cap is not finite, cap above 1.17e38, without a cap |scale| above 2.35e38, misaligned
+ * tensors), AFFMAE_ERR_UNSUPPORTED, AFFMAE_ERR_WORKSPACE.
  */
 size_t affmae_attn_fwd_workspace_bytes(int B, int Nq, int Nk, int H, int Hk, int d, int dtype, int docs);
 int affmae_attn_fwd(const void* q, const void* k, const void* v, const float* q_xy, const float* k_xy, const float* slope,

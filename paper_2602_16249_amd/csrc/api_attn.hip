@@ -36,6 +36,8 @@ int check_attn(int B, int Nq, int Nk, int H, int Hk, int d, int dtype) {
 int check_terms(float scale, float cap, const float* q_xy, const float* k_xy, const float* slope, const int32_t* q_doc, const int32_t* k_doc) {
   if ((q_xy == nullptr) != (slope == nullptr) || (k_xy == nullptr) != (slope == nullptr) || (q_doc == nullptr) != (k_doc == nullptr)) return AFFMAE_ERR_NULL;
   if (!finite(scale) || !finite(cap) || cap < 0.f || (cap > 0.f && (cap < 1e-30f || !finite(scale / cap)))) return AFFMAE_ERR_SHAPE;
+  // (scores are in units of log 2: scale log2 e without a cap, and 2 cap log2 e, are numbers of the kernels)
+  if (cap > 0.f ? !finite(cap * 2.88539008f) : !finite(scale * 1.44269504f)) return AFFMAE_ERR_SHAPE;
   if (misaligned(q_xy, 8) || misaligned(k_xy, 8) || misaligned(slope, 4) || misaligned(q_doc, 4) || misaligned(k_doc, 4)) return AFFMAE_ERR_SHAPE;
   return AFFMAE_OK;
 }

@@ -149,3 +149,11 @@ def test_binding_refuses_gradients_that_a_call_does_not_write(no_library):
     for grads, more in ((dict(dcoords=xy), {}), (dict(dq=x, dk=x), {}), (dict(dcoords=xy), dict(dk_out=x)), (dict(dfreq=freq), dict(q_out=x, want_dcoords=True))):
         with pytest.raises(ValueError, match="not written"):
             aff.affmae_rotary_bwd(x, xy, freq, grads=grads, **more)
+
+
+@pytest.mark.parametrize("scale,cap", [(3e38, 0.0), (-2.5e38, 0.0), (3e38, 3e38), (1.0, 2.5e38), (1.0, 3.4e38), (1.0, 2e38)])
+def test_attention_refuses_scales_and_caps_beyond_its_own_numbers(scale, cap):
+    """scale log2 e and 2 cap log2 e have to be finite: the scores are in units of log 2."""
+    lib = aff.load_library()
+    assert lib.affmae_attn_fwd(P, P, P, None, None, None, None, None, 2, 100, 70, 4, 2, 32, scale, cap, 1, P, P, P, 1 << 30, None) == -2
+    assert lib.affmae_attn_bwd(P, P, P, None, None, None, None, None, P, P, P, 2, 100, 70, 4, 2, 32, scale, cap, 1, P, P, P, None, P, 1 << 30, None) == -2
