@@ -22,8 +22,6 @@
 namespace affmae {
 namespace {
 
-int width(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : 128; }
-
 template <typename T, int D, int TERMS, bool DOCS, bool ALONE>
 __global__ __launch_bounds__(kAttnThreads, (kAttnWaves<T, D>)) void attn_bwd_query_kernel(AttnParams p) {
   using R = TileRows<T, D, ALONE>;
@@ -42,9 +40,14 @@ __global__ __launch_bounds__(kAttnThreads, (kAttnWaves<T, D>)) void attn_bwd_que
   const bool busy = r0 < p.rows;
   Row own = own_row(p, b, hk, r0);
   const Source<T, D, true> keys(p, p.k, b, hk), values(p, p.v, b, hk);
-  Fixed<T, D> q[1], g[1];
-  q[0].load((const char*)p.q + own.at * p.d * R::E, half, p.d * R::E, own.there);
-  g[0].load((const char*)p.dout + own.at * p.d * R::E, half, p.d * R::E, own.there);
+  Fixed<T, D> q, g;
+  if (own.there) {
+    q.load((const char*)p.q + own.at * p.d * R::E, half, p.d * R::E);
+    g.load((const char*)p.dout + own.at * p.d * R::E, half, p.d * R::E);
+  } else {
+    q.zero();
+    g.zero();
+  }
   float sum = 0.f;  // D
 #pragma unroll
   for (int s = 0; s < R::kSteps; ++s) {
@@ -52,8 +55,8 @@ __global__ __launch_bounds__(kAttnThreads, (kAttnWaves<T, D>)) void attn_bwd_que
     Piece<T> o;
     o.zero();
     if (own.there && at < p.d * R::E) __builtin_memcpy(&o, (const char*)p.out + own.at * p.d * R::E + at, 16);
-    sum += Piece<T>::dot(g[0].x[s], o);
-    if (p.negate) q[0].x[s].negate();
+    sum += Piece<T>::dot(g.x[s], o);
+    if (p.negate) q.x[s].negate();
   }
   sum = other_half_sum(sum);
   const float seen = own.there ? p.lse[own.at] : 0.f;
@@ -82,11 +85,11 @@ __global__ __launch_bounds__(kAttnThreads, (kAttnWaves<T, D>)) void attn_bwd_que
     }
     keys.template load<ALONE>(dst, t * BN, pads);
     values.template load<ALONE>(dst + R::kBytes, t * BN, pads);
-    about.load<TERMS, DOCS, ALONE, BN>(notes[ALONE ? wave : buffer], t * BN, wave, lane);
+    about.load<TERMS, DOCS, ALONE>(notes[ALONE ? wave : buffer], t * BN, wave, lane);
   };
 
-  q[0].arrive();
-  g[0].arrive();
+  q.arrive();
+  g.arrive();
   arrive(own);
   arrive(lse);
   arrive(sum);
@@ -109,18 +112,18 @@ __global__ __launch_bounds__(kAttnThreads, (kAttnWaves<T, D>)) void attn_bwd_que
       const KeyNotes& n = notes[ALONE ? wave : buffer];
 #pragma unroll kTogether
       for (int kb = 0; kb < R::kBlocks; ++kb) {
-        f32x16 s[1], dp[1];
-        row_products<T, D, 1>(kt, kb, q, s, lane, p.d);
-        row_products<T, D, 1>(vt, kb, g, dp, lane, p.d);
+        f32x16 s, dp;
+        row_products<T, D>(kt, kb, q, s, lane, p.d);
+        row_products<T, D>(vt, kb, g, dp, lane, p.d);
         const auto slopes = [&](auto near, auto hides) __attribute__((always_inline)) {
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
             const int j = 32 * kb + 16 * (i >> 3) + 8 * half + (i & 7);
             float bend, distance, dx = 0.f, dy = 0.f;
             if constexpr (TERMS & kDistance) dx = own.x - n.x[j], dy = own.y - n.y[j];
-            const float z = score<T, TERMS, near>(s[0][i], p, dx, dy, own.slope, lse, bend, distance);
+            const float z = score<T, TERMS, near>(s[i], p, dx, dy, own.slope, lse, bend, distance);
             float pr = __builtin_amdgcn_exp2f(z);
-            float dz = pr * (dp[0][i] - sum);
+            float dz = pr * (dp[i] - sum);
             if constexpr (hides) {  // (keys behind the last one, too: their p, exp(0 - lse), may not fit 32 bits)
               const bool off = j - 8 * half >= left || (DOCS && n.doc[j] != own.doc);
               pr = off ? 0.f : pr;
@@ -137,14 +140,14 @@ __global__ __launch_bounds__(kAttnThreads, (kAttnWaves<T, D>)) void attn_bwd_que
               dz *= bends;
               if constexpr (REST) pr *= bends;
             }
-            s[0][i] = dz;
-            dp[0][i] = pr;
+            s[i] = dz;
+            dp[i] = pr;
           }
         };
         using yes = std::true_type;
         using no = std::false_type;
         bool near = false;
-        if constexpr ((TERMS & kCap) && D < 128) near = all_near(s[0], p.near);
+        if constexpr ((TERMS & kCap) && D < 128) near = all_near(s, p.near);
         if (masked || D == 128) {  // (one way through where two would not fit the registers)
           if (near) slopes(yes{}, yes{});
           else slopes(no{}, yes{});
@@ -152,9 +155,9 @@ __global__ __launch_bounds__(kAttnThreads, (kAttnWaves<T, D>)) void attn_bwd_que
           if (near) slopes(yes{}, no{});
           else slopes(no{}, no{});
         }
-        const Weights<T> w(s[0]);
+        const Weights<T> w(s);
         if constexpr (REST) {
-          const Weights<T> wp(dp[0]);
+          const Weights<T> wp(dp);
           column_products<D, 2>(kt, kb, {&w, &wp}, {dq, keys_seen}, lane, p.d);
         } else {
           column_products<D, 1>(kt, kb, {&w}, {dq}, lane, p.d);
@@ -255,7 +258,7 @@ hipError_t launch(const AttnParams& p, hipStream_t stream) {
 }
 template <typename T, int TERMS>
 hipError_t launch_width(const AttnParams& p, hipStream_t stream) {
-  switch (width(p.d)) {
+  switch (attn_width(p.d)) {
     case 32: return launch<T, 32, TERMS>(p, stream);
     case 64: return launch<T, 64, TERMS>(p, stream);
     default: return launch<T, 128, TERMS>(p, stream);
@@ -339,37 +342,17 @@ __global__ __launch_bounds__(1024) void attn_bwd_slope_kernel(const float* rows,
   }
 }
 
-// Blocks of 128 or of 32 rows (or keys) and splits of the other side, as in the forward.
-constexpr int kLeast = 256;
-struct Side {
-  bool alone;
-  int blocks, splits, split_tiles;
-};
-Side side(long long own, long long other, long long heads, int D, int el, bool docs) {
-  Side s;
-  s.alone = attn_alone((own + kAttnRows - 1) / kAttnRows * heads, docs);
-  const int BN = attn_tile_rows(D, el, s.alone);
-  const int per = s.alone ? 32 : kAttnRows;
-  s.blocks = (int)((own + per - 1) / per);
-  const int tiles = (int)((other + BN - 1) / BN);
-  const long long groups = heads * s.blocks;
-  const long long want = std::max(1ll, std::min(512 / groups, other / kLeast));
-  s.split_tiles = (int)((tiles + want - 1) / want);
-  s.splits = (tiles + s.split_tiles - 1) / s.split_tiles;
-  return s;
-}
-
 struct Layout {
-  Side query, key;
+  AttnSide query, key;
   size_t spans, rowsum, rowlse, rowrest, rowslope, part_q, seen_q, part_k, part_v, total;  // places in the workspace
   bool rest;  // D is put right
 };
 Layout layout(int B, int Nq, int Nk, int H, int Hk, int d, int dtype, bool docs, bool want_dslope) {
   Layout l;
-  const int D = width(d), el = dtype == 1 ? 2 : 4;
+  const int D = attn_width(d), el = dtype == 1 ? 2 : 4;
   const long long rows = (long long)Nq * (H / Hk);
-  l.query = side(rows, Nk, (long long)B * Hk, D, el, docs);
-  l.key = side(Nk, rows, (long long)B * Hk, D, el, docs);
+  l.query = attn_side(rows, Nk, (long long)B * Hk, D, el, docs);
+  l.key = attn_side(Nk, rows, (long long)B * Hk, D, el, docs);
   size_t off = 0;
   const auto take = [&](size_t bytes) {
     const size_t at = off;

@@ -28,26 +28,25 @@ struct RowSource {
     }
     if (images) doc = uniform(buffer_of((const char*)(p.q_doc + (size_t)b * p.Nq), 4ll * p.Nq));
   }
-  template <int TERMS, bool DOCS, bool ALONE, int BN>
+  // of 64 rows, whatever a tile has (KeySource::load)
+  template <int TERMS, bool DOCS, bool ALONE>
   __device__ __forceinline__ void load(RowNotes& n, int r0, int wave, int lane) const {
     const int r = r0 + lane;
-    if (lane < BN) {
-      const bool there = r < rows;
-      if (ALONE || wave == 0) lds_load<4>(lds_at(n.lse), lse, there ? (uint32_t)r * 4u : kNowhere);
-      if (ALONE || wave == 1) lds_load<4>(lds_at(n.sum), sum, there ? (uint32_t)r * 4u : kNowhere);
-      if constexpr (DOCS || (TERMS & kDistance)) {
-        const int i = exact_div(r, G, g_magic);
-        if constexpr (TERMS & kDistance) {
-          if (ALONE || wave == 2) {
-            const uint32_t at = there ? (uint32_t)i * 8u : kNowhere;
-            lds_load<4>(lds_at(n.x), xy, at);
-            lds_load<4>(lds_at(n.y), xy, at + 4);
-          }
-          if (ALONE || wave == 3) lds_load<4>(lds_at(n.slope), slope, there ? (uint32_t)(r - i * G) * 4u : kNowhere);
+    const bool there = r < rows;
+    if (ALONE || wave == 0) lds_load<4>(lds_at(n.lse), lse, there ? (uint32_t)r * 4u : kNowhere);
+    if (ALONE || wave == 1) lds_load<4>(lds_at(n.sum), sum, there ? (uint32_t)r * 4u : kNowhere);
+    if constexpr (DOCS || (TERMS & kDistance)) {
+      const int i = exact_div(r, G, g_magic);
+      if constexpr (TERMS & kDistance) {
+        if (ALONE || wave == 2) {
+          const uint32_t at = there ? (uint32_t)i * 8u : kNowhere;
+          lds_load<4>(lds_at(n.x), xy, at);
+          lds_load<4>(lds_at(n.y), xy, at + 4);
         }
-        if constexpr (DOCS)
-          if (ALONE || wave == 0) lds_load<4>(lds_at(n.doc), doc, there ? (uint32_t)i * 4u : kNowhere);
+        if (ALONE || wave == 3) lds_load<4>(lds_at(n.slope), slope, there ? (uint32_t)(r - i * G) * 4u : kNowhere);
       }
+      if constexpr (DOCS)
+        if (ALONE || wave == 0) lds_load<4>(lds_at(n.doc), doc, there ? (uint32_t)i * 4u : kNowhere);
     }
   }
 };
@@ -78,12 +77,13 @@ __global__ __launch_bounds__(kAttnThreads, (sizeof(T) == 4 && D > 32 ? 1 : 2)) v
   }
   int own_doc = DOCS ? max(p.k_doc[token], -1) : 0;
   const Source<T, D, false> queries(p, p.q, b, hk), douts(p, p.dout, b, hk);
-  Fixed<T, D> k[1], v[1];
-  k[0].load((const char*)p.k + own_at * p.d * R::E, half, p.d * R::E, there);
-  v[0].load((const char*)p.v + own_at * p.d * R::E, half, p.d * R::E, there);
+  Fixed<T, D> k, v;
+  const int own_bytes = there ? p.d * R::E : 0;  // (a branch around the loads: 92 us instead of 85 with 32 channels and distances)
+  k.load((const char*)p.k + own_at * p.d * R::E, half, own_bytes);
+  v.load((const char*)p.v + own_at * p.d * R::E, half, own_bytes);
   if (p.negate) {
 #pragma unroll
-    for (int s = 0; s < R::kSteps; ++s) k[0].x[s].negate();
+    for (int s = 0; s < R::kSteps; ++s) k.x[s].negate();
   }
 
   const int tiles = (p.rows + BN - 1) / BN;
@@ -109,11 +109,11 @@ __global__ __launch_bounds__(kAttnThreads, (sizeof(T) == 4 && D > 32 ? 1 : 2)) v
     }
     queries.template load<ALONE>(dst, t * BN, pads);
     douts.template load<ALONE>(dst + R::kBytes, t * BN, pads);
-    about.load<TERMS, DOCS, ALONE, BN>(notes[ALONE ? wave : buffer], t * BN, wave, lane);
+    about.load<TERMS, DOCS, ALONE>(notes[ALONE ? wave : buffer], t * BN, wave, lane);
   };
 
-  k[0].arrive();
-  v[0].arrive();
+  k.arrive();
+  v.arrive();
   arrive(own_x);
   arrive(own_y);
   arrive(own_doc);
@@ -134,31 +134,31 @@ __global__ __launch_bounds__(kAttnThreads, (sizeof(T) == 4 && D > 32 ? 1 : 2)) v
       const RowNotes& n = notes[ALONE ? wave : buffer];
 #pragma unroll kTogether
       for (int rb = 0; rb < R::kBlocks; ++rb) {
-        f32x16 s[1], dp[1];
-        row_products<T, D, 1>(qt, rb, k, s, lane, p.d);
-        row_products<T, D, 1>(gt, rb, v, dp, lane, p.d);
+        f32x16 s, dp;
+        row_products<T, D>(qt, rb, k, s, lane, p.d);
+        row_products<T, D>(gt, rb, v, dp, lane, p.d);
         const auto slopes = [&](auto near, auto hides) __attribute__((always_inline)) {
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
             const int r = 32 * rb + 16 * (i >> 3) + 8 * half + (i & 7);
             float bend, distance, dx = 0.f, dy = 0.f, slope = 0.f;
             if constexpr (TERMS & kDistance) dx = n.x[r] - own_x, dy = n.y[r] - own_y, slope = n.slope[r] * kLog2e;
-            const float z = score<T, TERMS, near>(s[0][i], p, dx, dy, slope, n.lse[r], bend, distance);
-            float pr = __builtin_amdgcn_exp2f(z), ds = pr * (dp[0][i] - n.sum[r]);
+            const float z = score<T, TERMS, near>(s[i], p, dx, dy, slope, n.lse[r], bend, distance);
+            float pr = __builtin_amdgcn_exp2f(z), ds = pr * (dp[i] - n.sum[r]);
             if constexpr (TERMS & kCap) ds *= bend_slope(bend, p);
             if constexpr (hides) {
               const bool off = n.doc[r] != own_doc;
               pr = off ? 0.f : pr;
               ds = off ? 0.f : ds;
             }
-            s[0][i] = pr;
-            dp[0][i] = ds;
+            s[i] = pr;
+            dp[i] = ds;
           }
         };
         using yes = std::true_type;
         using no = std::false_type;
         bool near = false;
-        if constexpr ((TERMS & kCap) && D < 128) near = all_near(s[0], p.near);
+        if constexpr ((TERMS & kCap) && D < 128) near = all_near(s, p.near);
         if (DOCS && (D == 128 || masked)) {  // (one way through where two would not fit the registers)
           if (near) slopes(yes{}, yes{});
           else slopes(no{}, yes{});
@@ -166,7 +166,7 @@ __global__ __launch_bounds__(kAttnThreads, (sizeof(T) == 4 && D > 32 ? 1 : 2)) v
           if (near) slopes(yes{}, no{});
           else slopes(no{}, no{});
         }
-        const Weights<T> wp(s[0]), ws(dp[0]);
+        const Weights<T> wp(s), ws(dp);
         column_products<D, 1>(gt, rb, {&wp}, {dv}, lane, p.d);
         column_products<D, 1>(qt, rb, {&ws}, {dk}, lane, p.d);
       }
@@ -228,9 +228,11 @@ hipError_t launch(const AttnParams& p, hipStream_t stream) {
 }
 template <typename T, int TERMS>
 hipError_t launch_width(const AttnParams& p, hipStream_t stream) {
-  if (p.d <= 32) return launch<T, 32, TERMS>(p, stream);
-  if (p.d <= 64) return launch<T, 64, TERMS>(p, stream);
-  return launch<T, 128, TERMS>(p, stream);
+  switch (attn_width(p.d)) {
+    case 32: return launch<T, 32, TERMS>(p, stream);
+    case 64: return launch<T, 64, TERMS>(p, stream);
+    default: return launch<T, 128, TERMS>(p, stream);
+  }
 }
 template <typename T>
 hipError_t launch_terms(const AttnParams& p, hipStream_t stream) {

@@ -18,6 +18,8 @@
 #include "dense_common.h"
 #include "direct_lds.h"
 
+#include <algorithm>
+
 namespace affmae {
 
 typedef __attribute__((ext_vector_type(16))) float f32x16;
@@ -90,6 +92,28 @@ constexpr int kAttnWaves = sizeof(T) == 4 && D == 128 ? 1 : 2;
 // of 11 images each, 4 heads of 32 (504) 80 / 53.
 inline bool attn_alone(long long blocks, bool docs) { return blocks < (docs ? 512 : 256); }
 inline int attn_tile_rows(int D, int el, bool alone) { return D * el > 256 || (alone && D * el > 128) ? 32 : 64; }
+inline int attn_width(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : 128; }  // channels that a kernel is built for
+
+// Blocks of `own` rows (or keys), of 128 or of 32 whose waves share the `other` side out; where these do not fill the chip's 256 CUs twice, the other
+// side is split over workgroups too, kAttnLeast of it each at least.
+constexpr int kAttnLeast = 256;
+struct AttnSide {
+  bool alone;
+  int blocks, splits, split_tiles;
+};
+inline AttnSide attn_side(long long own, long long other, long long heads, int D, int el, bool docs) {
+  AttnSide s;
+  s.alone = attn_alone((own + kAttnRows - 1) / kAttnRows * heads, docs);
+  const int BN = attn_tile_rows(D, el, s.alone);
+  const int per = s.alone ? 32 : kAttnRows;
+  s.blocks = (int)((own + per - 1) / per);
+  const int tiles = (int)((other + BN - 1) / BN);
+  const long long groups = heads * s.blocks;
+  const long long want = std::max(1ll, std::min(512 / groups, other / kAttnLeast));
+  s.split_tiles = (int)((tiles + want - 1) / want);
+  s.splits = (tiles + s.split_tiles - 1) / s.split_tiles;
+  return s;
+}
 
 __device__ __forceinline__ int swap23(int m) { return (m & ~12) | (m & 4) << 1 | (m & 8) >> 1; }
 
@@ -118,10 +142,6 @@ struct Source {
     doc = ids ? ids + (long long)b * N : nullptr;
   }
   __device__ __forceinline__ int token(int r) const { return KEYS ? r : exact_div(r, G, g_magic); }
-  __device__ __forceinline__ long long offset(int r) const {
-    const int i = token(r);
-    return (long long)i * stride + (KEYS ? 0 : (r - i * G) * row_bytes);
-  }
   // rows r0 .. r0 + BN - 1 into LDS at `dst`, by the workgroup or by a wave; what is not there, and with `pads` rows of padding, as
   // zeros
   template <bool ALONE>
@@ -195,12 +215,16 @@ template <typename T, int D>
 struct Fixed {
   using R = TileRows<T, D>;
   Piece<T> x[R::kSteps];
-  __device__ __forceinline__ void load(const char* row, int half, int row_bytes, bool there) {
+  __device__ __forceinline__ void zero() {
+#pragma unroll
+    for (int s = 0; s < R::kSteps; ++s) x[s].zero();
+  }
+  __device__ __forceinline__ void load(const char* row, int half, int row_bytes) {
 #pragma unroll
     for (int s = 0; s < R::kSteps; ++s) {
       x[s].zero();
       const int at = (2 * s + half) * 16;
-      if (there && at < row_bytes) __builtin_memcpy(&x[s], row + at, 16);
+      if (at < row_bytes) __builtin_memcpy(&x[s], row + at, 16);
     }
   }
   // Waits for them.  (The compiler would wait where they are first used, inside the loop, in every turn of it, and so for the next tile.)
@@ -210,22 +234,20 @@ struct Fixed {
   }
 };
 
-// s[n][m] = <row perm(m) of block `block` in LDS, the rows of column block n>
-template <typename T, int D, int NB>
-__device__ __forceinline__ void row_products(const char* tile, int block, const Fixed<T, D> (&fixed)[NB], f32x16 (&s)[NB], int lane, int d) {
+// s[m] = <row perm(m) of block `block` in LDS, the row of the lane's column>
+template <typename T, int D>
+__device__ __forceinline__ void row_products(const char* tile, int block, const Fixed<T, D>& fixed, f32x16& s, int lane, int d) {
   using R = TileRows<T, D>;
   const int row = swap23(lane & 31);
   const char* at = tile + block * 32 * R::RB + row * R::RB;
   const int m = (R::mix(row) ^ (lane >> 5)) << 4;
-#pragma unroll
-  for (int n = 0; n < NB; ++n) s[n] = f32x16{};
+  s = f32x16{};
 #pragma unroll
   for (int step = 0; step < R::kSteps; ++step) {
     if (sizeof(T) == 4 && step > 0 && step * 8 >= d) break;  // (256 cycles a step; of bf16 it is 32, less than a branch between the reads costs)
     Piece<T> a;
     __builtin_memcpy(&a, at + (m ^ (step << 5)), 16);
-#pragma unroll
-    for (int n = 0; n < NB; ++n) s[n] = multiply(a, fixed[n].x[step], s[n]);
+    s = multiply(a, fixed.x[step], s);
   }
 }
 
@@ -499,20 +521,19 @@ struct KeySource {
     if (places) xy = uniform(buffer_of((const char*)(p.k_xy + 2 * (size_t)b * p.Nk), 8ll * p.Nk));
     if (images) doc = uniform(buffer_of((const char*)(p.k_doc + (size_t)b * p.Nk), 4ll * p.Nk));
   }
-  // by one wave, or by waves 0 (places) and 1 (images) of a workgroup
-  template <int TERMS, bool DOCS, bool ALONE, int BN>
+  // of 64 tokens, whatever a tile has, by one wave, or by waves 0 (places) and 1 (images) of a workgroup.  (All lanes: at the end of a region for a
+  // tile's 32 the compiler has put copies of registers where the other lanes were still off, in a kernel that uses all its registers.)
+  template <int TERMS, bool DOCS, bool ALONE>
   __device__ __forceinline__ void load(KeyNotes& n, int k0, int wave, int lane) const {
     const int j = k0 + lane;
-    if (lane < BN) {
-      if constexpr (TERMS & kDistance)
-        if (ALONE || wave == 0) {
-          const uint32_t at = j < rows ? (uint32_t)j * 8u : kNowhere;
-          lds_load<4>(lds_at(n.x), xy, at);
-          lds_load<4>(lds_at(n.y), xy, at + 4);
-        }
-      if constexpr (DOCS)
-        if (ALONE || wave == 1) lds_load<4>(lds_at(n.doc), doc, j < rows ? (uint32_t)j * 4u : kNowhere);
-    }
+    if constexpr (TERMS & kDistance)
+      if (ALONE || wave == 0) {
+        const uint32_t at = j < rows ? (uint32_t)j * 8u : kNowhere;
+        lds_load<4>(lds_at(n.x), xy, at);
+        lds_load<4>(lds_at(n.y), xy, at + 4);
+      }
+    if constexpr (DOCS)
+      if (ALONE || wave == 1) lds_load<4>(lds_at(n.doc), doc, j < rows ? (uint32_t)j * 4u : kNowhere);
   }
 };
 

@@ -46,7 +46,7 @@ __device__ __forceinline__ void join_waves(char* lds, int wave, int lane, f32x16
 template <typename T, int D, int TERMS, bool DOCS, bool ALONE>
 __global__ __launch_bounds__(kAttnThreads, (sizeof(T) == 4 ? kAttnWaves<T, D> : D == 32 ? 4 : D == 64 && !ALONE ? 3 : 2)) void attn_fwd_kernel(AttnParams p) {
   using R = TileRows<T, D, ALONE>;
-  constexpr int BN = R::BN, NB = 1;
+  constexpr int BN = R::BN;
   extern __shared__ __align__(16) char lds[];
   __shared__ KeyNotes notes[ALONE ? 4 : 2];
   const int work = xcd_contiguous_block(blockIdx.x, gridDim.x);
@@ -55,20 +55,17 @@ __global__ __launch_bounds__(kAttnThreads, (sizeof(T) == 4 ? kAttnWaves<T, D> : 
   const int split = group / (p.B * p.Hk), bh = group - split * p.B * p.Hk, b = bh / p.Hk, hk = bh - b * p.Hk;
   const int lane = threadIdx.x & 63, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  constexpr int kRows = ALONE ? 32 : kAttnRows * NB;
-  const int block0 = block * kRows, r0 = ALONE ? block0 : block0 + wave * 32 * NB;
+  constexpr int kRows = ALONE ? 32 : kAttnRows;
+  const int block0 = block * kRows, r0 = ALONE ? block0 : block0 + wave * 32;
   const bool busy = r0 < p.rows;
   const Source<T, D, true> keys(p, p.k, b, hk), values(p, p.v, b, hk);
-  Row own[NB];
-  Fixed<T, D> q[NB];
+  Row own = own_row(p, b, hk, r0);
+  Fixed<T, D> q;
+  if (own.there) q.load((const char*)p.q + own.at * p.d * R::E, half, p.d * R::E);
+  else q.zero();
+  if (p.negate) {
 #pragma unroll
-  for (int n = 0; n < NB; ++n) {
-    own[n] = own_row(p, b, hk, r0 + 32 * n);
-    q[n].load((const char*)p.q + own[n].at * p.d * R::E, half, p.d * R::E, own[n].there);
-    if (p.negate) {
-#pragma unroll
-      for (int s = 0; s < R::kSteps; ++s) q[n].x[s].negate();
-    }
+    for (int s = 0; s < R::kSteps; ++s) q.x[s].negate();
   }
 
   const int tiles = (p.Nk + BN - 1) / BN;
@@ -94,20 +91,17 @@ __global__ __launch_bounds__(kAttnThreads, (sizeof(T) == 4 ? kAttnWaves<T, D> : 
     }
     keys.template load<ALONE>(dst, t * BN, pads);
     values.template load<ALONE>(dst + R::kBytes, t * BN, pads);
-    about.load<TERMS, DOCS, ALONE, BN>(notes[ALONE ? wave : buffer], t * BN, wave, lane);
+    about.load<TERMS, DOCS, ALONE>(notes[ALONE ? wave : buffer], t * BN, wave, lane);
   };
 
-#pragma unroll
-  for (int n = 0; n < NB; ++n) {
-    q[n].arrive();
-    arrive(own[n]);
-  }
-  f32x16 o[NB][D / 32] = {};
+  q.arrive();
+  arrive(own);
+  f32x16 o[D / 32] = {};
   // The exponentials are taken from a score of the row that lies within 2^12 of the largest one (in p) so far: m.  It is found in the row's
   // first tile, and again where the sum over a tile says that a score lies above it, which hardly ever happens: floating
   // values lose nothing by being larger than 1, and the maximum of every tile took a tenth of the vector instructions.
   float m = -__builtin_inff(), l = 0.f;
-  if (DOCS && own[0].doc < 0) m = 0.f;  // (padding: nothing to find)
+  if (DOCS && own.doc < 0) m = 0.f;  // (padding: nothing to find)
   bool masked = false;
   int t = walk.skip(p.Nk, ALONE ? wave : 0);
   if (t < walk.end) fetch(t, 0, masked);
@@ -121,9 +115,9 @@ __global__ __launch_bounds__(kAttnThreads, (sizeof(T) == 4 ? kAttnWaves<T, D> : 
     const char* kt = lds + (ALONE ? wave : buffer) * 2 * R::kBytes;
     const char* vt = kt + R::kBytes;
     if (busy) {
-      f32x16 s[R::kBlocks][1];
+      f32x16 s[R::kBlocks];
 #pragma unroll
-      for (int kb = 0; kb < R::kBlocks; ++kb) row_products<T, D, 1>(kt, kb, q, s[kb], lane, p.d);
+      for (int kb = 0; kb < R::kBlocks; ++kb) row_products<T, D>(kt, kb, q, s[kb], lane, p.d);
       const KeyNotes& about_key = notes[ALONE ? wave : buffer];
       const int left = p.Nk - t * BN - 8 * half;  // keys of the tile that are there, from the lane's first one on
       // s becomes score - from, hidden ones -infinity
@@ -134,10 +128,10 @@ __global__ __launch_bounds__(kAttnThreads, (sizeof(T) == 4 ? kAttnWaves<T, D> : 
           for (int i = 0; i < 16; ++i) {
             const int j = 32 * kb + 16 * (i >> 3) + 8 * half + (i & 7);
             float bend, distance, dx = 0.f, dy = 0.f;
-            if constexpr (TERMS & kDistance) dx = own[0].x - about_key.x[j], dy = own[0].y - about_key.y[j];
-            float z = score<T, TERMS, near>(s[kb][0][i], p, dx, dy, own[0].slope, from, bend, distance);
-            if constexpr (hides) z = j - 8 * half >= left || (DOCS && about_key.doc[j] != own[0].doc) ? -__builtin_inff() : z;
-            s[kb][0][i] = z;
+            if constexpr (TERMS & kDistance) dx = own.x - about_key.x[j], dy = own.y - about_key.y[j];
+            float z = score<T, TERMS, near>(s[kb][i], p, dx, dy, own.slope, from, bend, distance);
+            if constexpr (hides) z = j - 8 * half >= left || (DOCS && about_key.doc[j] != own.doc) ? -__builtin_inff() : z;
+            s[kb][i] = z;
           }
       };
       const auto exponentials = [&]() __attribute__((always_inline)) {
@@ -146,8 +140,8 @@ __global__ __launch_bounds__(kAttnThreads, (sizeof(T) == 4 ? kAttnWaves<T, D> : 
         for (int kb = 0; kb < R::kBlocks; ++kb)
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
-            s[kb][0][i] = __builtin_amdgcn_exp2f(s[kb][0][i]);
-            sum += s[kb][0][i];
+            s[kb][i] = __builtin_amdgcn_exp2f(s[kb][i]);
+            sum += s[kb][i];
           }
         return sum;
       };
@@ -156,7 +150,7 @@ __global__ __launch_bounds__(kAttnThreads, (sizeof(T) == 4 ? kAttnWaves<T, D> : 
       const auto is_near = [&]() __attribute__((always_inline)) {
         bool near = true;
 #pragma unroll
-        for (int kb = 0; kb < R::kBlocks; ++kb) near = near && all_near(s[kb][0], p.near);
+        for (int kb = 0; kb < R::kBlocks; ++kb) near = near && all_near(s[kb], p.near);
         return near;
       };
       bool search = masked || __any(m == -__builtin_inff()), near = false;
@@ -170,7 +164,7 @@ __global__ __launch_bounds__(kAttnThreads, (sizeof(T) == 4 ? kAttnWaves<T, D> : 
         search = __any(!(sum < 4096.f));
         if (search) {
 #pragma unroll
-          for (int kb = 0; kb < R::kBlocks; ++kb) row_products<T, D, 1>(kt, kb, q, s[kb], lane, p.d);
+          for (int kb = 0; kb < R::kBlocks; ++kb) row_products<T, D>(kt, kb, q, s[kb], lane, p.d);
         } else {
           l += sum;
         }
@@ -187,7 +181,7 @@ __global__ __launch_bounds__(kAttnThreads, (sizeof(T) == 4 ? kAttnWaves<T, D> : 
 #pragma unroll
         for (int kb = 0; kb < R::kBlocks; ++kb)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) top = fmaxf(top, s[kb][0][i]);
+          for (int i = 0; i < 16; ++i) top = fmaxf(top, s[kb][i]);
         top = other_half_max(top);
         if (__any(top > m)) {
           const float before = m;
@@ -195,19 +189,19 @@ __global__ __launch_bounds__(kAttnThreads, (sizeof(T) == 4 ? kAttnWaves<T, D> : 
           const float shrink = m == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f(before - m);
           l *= shrink;
 #pragma unroll
-          for (int db = 0; db < D / 32; ++db) o[0][db] *= shrink;
+          for (int db = 0; db < D / 32; ++db) o[db] *= shrink;
         }
         const float from = m == -__builtin_inff() ? 0.f : m;
 #pragma unroll
         for (int kb = 0; kb < R::kBlocks; ++kb)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) s[kb][0][i] -= from;
+          for (int i = 0; i < 16; ++i) s[kb][i] -= from;
         l += exponentials();
       }
 #pragma unroll
       for (int kb = 0; kb < R::kBlocks; ++kb) {
-        const Weights<T> w(s[kb][0]);
-        column_products<D, 1>(vt, kb, {&w}, {o[0]}, lane, p.d);
+        const Weights<T> w(s[kb]);
+        column_products<D, 1>(vt, kb, {&w}, {o}, lane, p.d);
       }
     }
     if (ALONE && following < walk.end) {
@@ -218,31 +212,28 @@ __global__ __launch_bounds__(kAttnThreads, (sizeof(T) == 4 ? kAttnWaves<T, D> : 
     masked = next_masked;
   }
 
-  if constexpr (ALONE) join_waves<D>(lds, wave, lane, o[0], m, l);
+  if constexpr (ALONE) join_waves<D>(lds, wave, lane, o, m, l);
   if (!busy) return;
+  const float seen = ALONE ? l : other_half_sum(l), sum = DOCS && own.doc < 0 ? 0.f : seen;
+  const bool none = sum == 0.f;  // (a NaN stays one)
+  const float part = 1.f / sum;
+  const float lse = none ? -__builtin_inff() : __builtin_fmaf(m, kLn2, __logf(sum));
+  if (!own.there) return;
+  const size_t all = (size_t)p.B * p.Nq * p.H;
 #pragma unroll
-  for (int n = 0; n < NB; ++n) {
-    const float seen = ALONE ? l : other_half_sum(l), sum = DOCS && own[n].doc < 0 ? 0.f : seen;
-    const bool none = sum == 0.f;  // (a NaN stays one)
-    const float part = 1.f / sum;
-    const float lse = none ? -__builtin_inff() : __builtin_fmaf(m, kLn2, __logf(sum));
-    if (!own[n].there) continue;
-    const size_t all = (size_t)p.B * p.Nq * p.H;
+  for (int db = 0; db < D / 32; ++db)
 #pragma unroll
-    for (int db = 0; db < D / 32; ++db)
+    for (int g = 0; g < 4; ++g) {
+      const int ch = 32 * db + 8 * g + 4 * half;
+      if (ch < p.d && (!ALONE || g == wave)) {
+        float v[4];
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const int ch = 32 * db + 8 * g + 4 * half;
-        if (ch < p.d && (!ALONE || g == wave)) {
-          float v[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) v[e] = none ? 0.f : o[n][db][4 * g + e] * part;
-          if (p.part) store_piece<4>(p.part + ((size_t)split * all + own[n].at) * p.d + ch, v);
-          else store_piece<4>((T*)p.o + own[n].at * p.d + ch, v);
-        }
+        for (int e = 0; e < 4; ++e) v[e] = none ? 0.f : o[db][4 * g + e] * part;
+        if (p.part) store_piece<4>(p.part + ((size_t)split * all + own.at) * p.d + ch, v);
+        else store_piece<4>((T*)p.o + own.at * p.d + ch, v);
       }
-    if (half == 0 && (!ALONE || wave == 0)) (p.part ? p.part + (size_t)p.splits * all * p.d + (size_t)split * all : p.lse_out)[own[n].at] = lse;
-  }
+    }
+  if (half == 0 && (!ALONE || wave == 0)) (p.part ? p.part + (size_t)p.splits * all * p.d + (size_t)split * all : p.lse_out)[own.at] = lse;
 }
 
 // out = sum over splits of exp(lse_s - lse) out_s, lse = log sum exp lse_s.  A thread takes four channels of a (query, head) for every `lanes`th
@@ -310,29 +301,6 @@ __global__ __launch_bounds__(256) void attn_spans_kernel(const int32_t* q_doc, c
   if (lane == 0) (q ? to_q : to_k)[n] = Span{lo, hi, pad, 0};
 }
 
-// Blocks of 128 rows, or of 32 whose waves share the keys out (attn_alone); where these do not fill the chip's 256 CUs twice, the keys are split over
-// workgroups too, kLeastKeys each at least.
-constexpr int kLeastKeys = 256;
-struct Plan {
-  bool alone;
-  int blocks, splits, split_tiles;
-};
-Plan plan(int B, int Nq, int Nk, int H, int Hk, int D, int el, bool docs) {
-  const long long rows = (long long)Nq * (H / Hk), heads = (long long)B * Hk;
-  Plan l;
-  l.alone = attn_alone((rows + kAttnRows - 1) / kAttnRows * heads, docs);
-  const int BN = attn_tile_rows(D, el, l.alone);
-  const int per = l.alone ? 32 : kAttnRows;
-  l.blocks = (int)((rows + per - 1) / per);
-  const int tiles = (Nk + BN - 1) / BN;
-  const long long groups = heads * l.blocks;
-  const long long want = std::max(1ll, std::min<long long>(512 / groups, Nk / kLeastKeys));
-  l.split_tiles = (int)((tiles + want - 1) / want);
-  l.splits = (tiles + l.split_tiles - 1) / l.split_tiles;
-  return l;
-}
-int width(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : 128; }
-
 template <typename T, int D, int TERMS, bool DOCS, bool ALONE>
 hipError_t launch_kernel(const AttnParams& p, hipStream_t stream) {
   const size_t lds = (ALONE ? 8 : 4) * TileRows<T, D, ALONE>::kBytes;
@@ -353,7 +321,7 @@ hipError_t launch(const AttnParams& p, hipStream_t stream) {
 }
 template <typename T, int TERMS>
 hipError_t launch_width(const AttnParams& p, hipStream_t stream) {
-  switch (width(p.d)) {
+  switch (attn_width(p.d)) {
     case 32: return launch<T, 32, TERMS>(p, stream);
     case 64: return launch<T, 64, TERMS>(p, stream);
     default: return launch<T, 128, TERMS>(p, stream);
@@ -363,6 +331,10 @@ template <typename T>
 hipError_t launch_terms(const AttnParams& p, hipStream_t stream) {
   if (p.cap > 0.f) return p.slope ? launch_width<T, kCap | kDistance>(p, stream) : launch_width<T, kCap>(p, stream);
   return p.slope ? launch_width<T, kDistance>(p, stream) : launch_width<T, 0>(p, stream);
+}
+
+AttnSide side(int B, int Nq, int Nk, int H, int Hk, int d, int dtype, bool docs) {
+  return attn_side((long long)Nq * (H / Hk), Nk, (long long)B * Hk, attn_width(d), dtype == 1 ? 2 : 4, docs);
 }
 
 }  // namespace
@@ -408,7 +380,7 @@ hipError_t launch_attn_spans(const AttnArgs& a, Span* q_span, Span* k_span, hipS
 }
 
 size_t attn_fwd_workspace_bytes(int B, int Nq, int Nk, int H, int Hk, int d, int dtype, bool docs) {
-  const Plan l = plan(B, Nq, Nk, H, Hk, width(d), dtype == 1 ? 2 : 4, docs);
+  const AttnSide l = side(B, Nq, Nk, H, Hk, d, dtype, docs);
   return (docs ? attn_span_bytes(B, Nq, Nk) : 0) + (l.splits > 1 ? (size_t)l.splits * B * Nq * H * (d + 1) * sizeof(float) : 0);
 }
 
@@ -416,7 +388,7 @@ hipError_t launch_attn_fwd(const AttnArgs& a, hipStream_t stream) {
   AttnParams p = attn_params(a, static_cast<Span*>(a.workspace));
   p.o = a.out;
   p.lse_out = a.lse;
-  const Plan l = plan(a.B, a.Nq, a.Nk, a.H, a.Hk, width(a.d), a.dtype == 1 ? 2 : 4, a.q_doc != nullptr);
+  const AttnSide l = side(a.B, a.Nq, a.Nk, a.H, a.Hk, a.d, a.dtype, a.q_doc != nullptr);
   p.alone = l.alone; p.blocks = l.blocks; p.splits = l.splits; p.split_tiles = l.split_tiles;
   if (p.splits > 1) p.part = reinterpret_cast<float*>(static_cast<char*>(a.workspace) + (a.q_doc ? attn_span_bytes(a.B, a.Nq, a.Nk) : 0));
   p.blocks_magic = div_magic(p.blocks);
