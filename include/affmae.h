@@ -551,8 +551,9 @@ int affmae_norm_bwd(const void* x, const void* gamma, const void* beta, const fl
  *     t = sum_a coords[b,n,a] freq[c,a]
  *     (x0, x1) -> (x0 cos t - x1 sin t, x0 sin t + x1 cos t)
  * so that freq says which axis, or which direction of several, a pair follows, and how
- * fast; a row of zeros leaves its pair as it is.  Angles are 64-bit up to the sine: an
- * angle t is off by at most |t| 2^-52, sine and cosine by 2^-22 besides, for |t| < 2^40.
+ * fast; a row of zeros leaves its pair as it is.  Angles are 64-bit up to the sine: t is off
+ * by at most 2^-51 times the sum of its terms' absolute values (which is more than |t|
+ * where terms cancel), sine and cosine by 2^-22 besides, for |t| < 2^40.
  *
  * affmae_rotary_fwd
  *   q, q_out  [B,N,H,d] dtype     k, k_out  [B,N,Hk,d] dtype, or both NULL with Hk = 0:
@@ -583,19 +584,25 @@ int affmae_rotary_bwd(const void* dq_out, const void* dk_out, const void* q_out,
                       float* dcoords, void* stream);
 
 /*
- * Attention between all tokens of an image: the point decoder's self- and cross-attention,
- * and encoder stages short enough for it (paper, Sec. "AFFMAE": the decoder's blocks).
+ * Attention between all tokens of an image: the self-attention of the point decoder's
+ * blocks (paper, Sec. "AFFMAE"; their cross-attention is another one, over the virtual
+ * sampled tokens), and encoder stages short enough for it; queries and keys may be
+ * different tokens.
  * For every image b, query i and head h, with key head hk = h / (H / Hk),
  *     z_j = scale <q[b,i,h,:], k[b,j,hk,:]>
  *     z_j = cap tanh(z_j / cap)                                if cap > 0
  *     z_j = z_j - slope[h] |q_xy[b,i] - k_xy[b,j]|             if slope is given
  *     j is hidden unless q_doc[b,i] == k_doc[b,j] >= 0         if q_doc is given
  *     out[b,i,h,:] = sum_j softmax(z)_j v[b,j,hk,:],   lse[b,i,h] = log(sum_j exp(z_j))
- * without storing the scores, with fp32 statistics and sums whatever the storage type.  A
- * query that sees no key gets out = 0 and lse = -infinity.
+ * without storing the scores, with fp32 statistics and sums whatever the storage type; for
+ * bf16 the softmax' values are rounded to bf16 as operands of the product with v (each by
+ * at most 2^-8 of it; lse is not touched by that).  A query that sees no key gets out = 0
+ * and lse = -infinity.
  *
  *   q            in  [B,Nq,H,d] dtype    k, v  in  [B,Nk,Hk,d] dtype, Hk a divisor of H
- *   q_xy, k_xy   in  [B,Nq,2], [B,Nk,2] fp32, finite, and slope in [H] fp32: all or none
+ *   q_xy, k_xy   in  [B,Nq,2], [B,Nk,2] fp32, finite, and slope in [H] fp32: all or none.
+ *                Distances are roots of fp32 sums of squares: two tokens' coordinates differ
+ *                by less than 1e18 (and what is below 1e-18 counts as 0).
  *   q_doc, k_doc in  [B,Nq], [B,Nk] int32 or both NULL: images that share a row (what masks
  *                leave of them has different lengths).  Any ids in any order; tokens of
  *                an image lying together are what lets whole tiles be skipped.  A negative
@@ -607,7 +614,8 @@ int affmae_rotary_bwd(const void* dq_out, const void* dk_out, const void* q_out,
  * affmae_attn_bwd   gradients of L = <dout, out>, from the forward call's out and lse:
  *   dq [B,Nq,H,d], dk, dv [B,Nk,Hk,d] out dtype (of padding: zeros), dslope out [H] fp32 or
  *   NULL.  fp32 sums in a fixed order.  For bf16 the operands p and dS of the products are
- *   rounded to bf16.
+ *   rounded to bf16; <dout, out> is put right for what the bf16 out was rounded by, in a
+ *   row of any length.  (q_xy and k_xy are taken as given: they have no gradient.)
  *   workspace    affmae_attn_bwd_workspace_bytes(...) bytes
  *
  * Outputs must not overlap inputs or each other.  q, k, v, out, dout and gradients are

@@ -256,7 +256,7 @@ __device__ __forceinline__ void row_products(const char* tile, int block, const 
 template <typename T>
 struct Weights;
 template <>
-struct Weights<bf16_t> {  // (off by at most 2^-8 of each; products of bf16 values are exact and sums 32-bit)
+struct Weights<bf16_t> {  // (off by at most 2^-8 of each, what the matrix instructions take; products of bf16 values are exact and sums 32-bit)
   Frag8 w[2];
   __device__ __forceinline__ Weights(const f32x16& x) {
 #pragma unroll
@@ -308,7 +308,7 @@ __device__ __forceinline__ void column_products(const char* tile, int block, con
 
 // Terms of the scores that a kernel is built for.
 enum { kCap = 1, kDistance = 2 };
-// tanh x up to |x| = kNear is x times a polynomial of x^2, fitted by least squares to a relative error of 5e-8 (2e-9 for fp32 tensors), beyond
+// tanh x up to |x| = kNear is x times a polynomial of x^2, fitted by least squares to a relative error of 5e-8 (4e-9 for fp32 tensors), beyond
 // it 1 - 2 / (exp(2 x) + 1), of which the 1 is most there (near 0 it would leave an error of 1e-7, times the cap).  Caps are many
 // times the usual score, so that as a rule no lane of a wave is beyond: then cap tanh(scale s / cap) log2 e is s q(s^2) with the constants
 // in q's coefficients, and the second form is not worked out.

@@ -32,7 +32,7 @@ struct RotaryParams {
 };
 
 // sin and cos of theta.  A far token's angle does not fit 32 bits (at 10^6 an fp32 angle is off by 0.06): the sum and its
-// remainder after quarter turns are 64-bit, pi / 2 in two parts, so that the error is theta 2^-53; the rest of at most pi / 4 goes
+// remainder after quarter turns are 64-bit, pi / 2 in two parts, so that the error of that is theta 2^-53; the rest of at most pi / 4 goes
 // through the Taylor series in 32 bits (the terms left out are below 2e-9 and 2.5e-9).
 __device__ __forceinline__ void sin_cos(double theta, float& s, float& c) {
   constexpr double kHalfPi = 1.5707963267948966, kRest = 6.123233995736766e-17;  // pi / 2 = 1.57079632679489661923132...
