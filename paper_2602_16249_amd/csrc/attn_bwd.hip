@@ -6,14 +6,17 @@
 // run, and grouped heads' gradients add up in registers.
 //
 // Bound by the vector ALU with 32 channels (16 x 1024 tokens, 8 heads, distances: 90 us, key kernel 85), by matrix instructions with 128 (8 x 4096, 6
-// heads: 769 us, 1073 TFLOP/s, near the rate of a large library product; key kernel 814 us, 1013).
+// heads: 756 to 776 us, 1063 to 1091 TFLOP/s, near the rate of a large library product; key kernel 808 to 838 us, 984 to 1020); 48 x 2048 tokens, 6
+// heads of 64: 638 us, key kernel 693.
 //
 // D from the bf16 out is off by what out was rounded by, which counts where few keys share a row's weight, in a row of any length (500
 // queries near the sum of two keys, of 2 of 64 channels or of 1024 of 128: dq off by 0.0049 and 0.0060 of its size, dk by 0.0029 and
 // 0.0055, rows with one key in front by all of their own).  The row's dZ sum to 0 if D is right, so their sum is what D lacks: the key kernel
 // gets it, and dq is put right at the end by as much of sum_j p_ij k_j, one more product (dq 0.0025, dk at most 0.0025).  How many keys
 // share a row's weight is not known beforehand, so every bf16 row has it.  With 128 channels that product is not hidden behind the
-// exponentials: 8 x 4096 tokens, 6 heads 769 us, 546 without it.
+// exponentials (8 x 4096 tokens, 6 heads: 546 us without it), and its sums take registers: the forms of 128 channels spill, 6 to 87 of them.  Room for
+// one wave a SIMD, where nothing spills, is worse all the same (885 us instead of 776 on the same day), but for images with distances
+// (96 x 1024 tokens of one head, both kernels: 322 us, 307 with one wave; capped 446, 364).
 #include "attn_common.h"
 #include "timing.h"
 

@@ -92,7 +92,7 @@ constexpr int kAttnWaves = sizeof(T) == 4 && D == 128 ? 1 : 2;
 // 56 / 55 with 384; 64 channels 32 / 25 and 75 / 68 with 248, 27 / 30 and 75 / 83 with 288; 128 channels 42 / 39 and 127 / 140 with 248, 39 / 51
 // and 139 / 182 with 288.  With images it depends on their lengths, which the host does not see; rows of 2048 tokens, 496 blocks: 3 images
 // 89 / 54 and 163 / 111 (32 channels), 8 images 44 / 34 and 82 / 67 (32) or 51 / 57 and 104 / 130 (64), 24 images 28 / 28 and 52 / 53 (32) or
-// 30 / 43 and 63 / 97 (64), from where on blocks of 128 win by 288 blocks; few long ones by no less than 640.
+// 30 / 43 and 63 / 97 (64).  Blocks of 128 win from 288 blocks on where images are many and short, from more than 640 where they are few.
 inline bool attn_alone(long long blocks, bool docs) { return blocks < (docs ? 512 : 256); }
 inline int attn_tile_rows(int D, int el, bool alone) { return D * el > 256 || (alone && D * el > 128) ? 32 : 64; }
 inline int attn_width(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : 128; }  // channels that a kernel is built for

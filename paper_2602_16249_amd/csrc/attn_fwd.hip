@@ -4,9 +4,9 @@
 // in one pass over the keys with a running reference and sum of every row (attn_common.h: the tiles and their layout).
 //
 // Bound by the vector ALU up to 64 channels (a product, an exponential that takes the time of two, a sum and half a conversion a
-// pair, beside 8 cycles of matrix instructions for 64 channels), by both with 128: 8 x 4096 tokens, 6 heads of 64 255 us (808 TFLOP/s; 306 while
-// a tile waited for the next one), of 128 409 us (1010); 16 x 1024, 8 heads of 32 with distances 68 us.  Two rows of 8001 tokens of 11 images
-// each, capped, 4 heads of 32: 50 us.  One query of 12 heads on 3, 4 x 16384 keys of 64: 14.5 us (3.5 TB/s) and 5.4 for the join.
+// pair, beside 8 cycles of matrix instructions for 64 channels), by both with 128: 8 x 4096 tokens, 6 heads of 64 a call of 240 us (859 TFLOP/s), of 128
+// 410 to 420 us (982 to 1005); 48 x 2048, 6 heads of 64 375 us; 16 x 1024, 8 heads of 32 with distances 66 to 68 us.  Two rows of 8001 tokens of 11
+// images each, capped, 4 heads of 32: 50 us.  One query of 12 heads on 3, 4 x 16384 keys of 64: 14.5 us (3.5 TB/s) and 5.6 for the join.
 #include "attn_common.h"
 #include "timing.h"
 
@@ -41,8 +41,10 @@ __device__ __forceinline__ void join_waves(char* lds, int wave, int lane, f32x16
   l = sum;
 }
 
-// Registers: bf16 heads of 32 channels leave room for four waves a SIMD (packed images 50 us and distances 68; three 56 and 70, five spill, 133 and
-// 215), of 64 for three (255 us; two 292, four spill, 1229), in blocks of 32 rows for two (one query 14.5 us; three spill, 16.3), as everything else.
+// Registers: bf16 heads of 32 channels leave room for four waves a SIMD (packed images 50 us and distances 66; three 55 and 69, five spill, 133 and
+// 215; a chip that is not full gains by three, as the forms of blocks of 32 rows with images spill up to 14 registers under four: 16 x 1024 tokens of one
+// head 19.2 us, 16.8 under three), of 64 for three (255 us; two 292, four spill, 1229), in blocks of 32 rows for two (one query 14.5 us; three
+// spill, 16.3), as everything else.
 template <typename T, int D, int TERMS, bool DOCS, bool ALONE>
 __global__ __launch_bounds__(kAttnThreads, (sizeof(T) == 4 ? kAttnWaves<T, D> : D == 32 ? 4 : D == 64 && !ALONE ? 3 : 2)) void attn_fwd_kernel(AttnParams p) {
   using R = TileRows<T, D, ALONE>;

@@ -22,14 +22,15 @@ WRITES = re.compile(r"v_(?!cmp|readlane|readfirstlane|writelane)|scratch_|ds_|gl
 
 
 def _missed(text):
-    """(kernel, instructions) that stand between the target of a branch around a region and the instruction that widens the mask there."""
+    """(kernel, instructions) that stand between the target of a branch around a region, or the end of a loop that lanes leave one by one, and the
+    instruction that widens the mask there."""
     found = []
     kernel, code, targets = "", [], set()
 
     def finish():
         for at in targets:
             block = []
-            for op in code[places[at]:places[at] + 64] if at in places else ():
+            for op in code[places[at]:places[at] + 500] if at in places else ():
                 if WIDENS.match(op):
                     if block:
                         found.append((kernel, block))
@@ -39,12 +40,12 @@ def _missed(text):
                 if WRITES.match(op):
                     block.append(op)
 
-    places, start = {}, 0
+    places, start, loop_ends = {}, 0, False
     for line in text.splitlines():
         head = re.match(r"^0*([0-9a-f]+) <(\S+)>:", line)
         if head:
             finish()
-            kernel, start, code, targets, places = head[2], int(head[1], 16), [], set(), {}
+            kernel, start, code, targets, places, loop_ends = head[2], int(head[1], 16), [], set(), {}, False
             continue
         m = LINE.match(line)
         if not m:
@@ -54,6 +55,9 @@ def _missed(text):
         code.append(op)
         if m[1] == "s_cbranch_execz" and m[4]:
             targets.add(start + int(m[5] or "0", 16))
+        if loop_ends:
+            targets.add(int(m[3], 16))
+        loop_ends = m[1] == "s_cbranch_execnz" and int(m[2]) >= 0x8000  # (backwards)
     finish()
     return found
 
