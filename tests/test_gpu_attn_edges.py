@@ -6,7 +6,7 @@ import torch
 
 import paper_2602_16249_amd as aff
 from oracle import attn as oa
-from test_gpu_attn import HALF, _check, _close, _stored
+from test_gpu_attn import HALF, _case, _check, _close, _stored
 
 pytestmark = pytest.mark.gpu
 
@@ -90,3 +90,32 @@ def test_gradients_of_keys_beyond_32_bits():
     assert float((others + 2 * least * D).abs().max()) <= 2 * least * D * (2 ** -7 + 0.002)
     del k, v, got, dk, others
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("shape", [(1, 1, 4097, 6, 2, 64), (2, 65, 129, 3, 3, 40), (1, 9, 2999, 4, 2, 128), (1, 2500, 40, 2, 2, 128), (66, 20, 150, 4, 4, 32)])
+@pytest.mark.parametrize("docs", [None, "any"])
+def test_workspaces_of_just_the_size_asked_for(dtype, shape, docs):
+    """Nothing behind the workspace is written, with the gradient of the slopes and without it, and the other gradients are the same."""
+    dev, _, terms, _ = _case(dtype, *shape, cap=6.0, distance=True, docs=docs, poison=False)
+    lib = aff.load_library()
+    code = {"f32": 0, "bf16": 1}[dtype]
+
+    def guarded(need):
+        buf = torch.full((need + 4096,), 171, dtype=torch.uint8, device="cuda")
+        return buf, buf[:need]
+
+    def whole(buf, need):
+        return bool((buf[need:] == 171).all())
+
+    need = lib.affmae_attn_fwd_workspace_bytes(*shape, code, docs is not None)
+    buf, ws = guarded(need)
+    out, lse = aff.affmae_attn_fwd(dev["q"], dev["k"], dev["v"], 0.2, 6.0, workspace=ws, **terms)
+    assert whole(buf, need)
+    results = []
+    for want in (True, False):
+        need = lib.affmae_attn_bwd_workspace_bytes(*shape, code, docs is not None, want)
+        buf, ws = guarded(need)
+        results.append(aff.affmae_attn_bwd(dev["q"], dev["k"], dev["v"], out, lse, dev["dout"], 0.2, 6.0, want_dslope=want, workspace=ws, **terms))
+        assert whole(buf, need)
+    assert sorted(results[1]) == ["dk", "dq", "dv"] and all(torch.equal(results[0][n], results[1][n]) for n in results[1])
